@@ -59,7 +59,8 @@ typedef enum sieve_status {
 
 typedef enum sieve_dtype {
   SIEVE_F32 = 0, /* IEEE binary32 storage, fp32 MFMA accumulate                 */
-  SIEVE_F16 = 1  /* IEEE binary16 storage, exact products, fp32 MFMA accumulate */
+  SIEVE_F16 = 1, /* IEEE binary16 storage, exact products, fp32 MFMA accumulate */
+  SIEVE_BF16 = 2 /* bfloat16 storage: the text-encoder operators only           */
 } sieve_dtype;
 
 /* Any W >= min(nprobe_max, nlist) disables early stopping; this value is the
@@ -316,6 +317,161 @@ typedef struct sieve_round {
 } sieve_round;
 SIEVE_API int sieve_round_log(const sieve_index* idx, sieve_round* out, int32_t max,
                               int32_t* n_rounds);
+
+/* ---- Text-encoder operators ------------------------------------------------
+ * The vectors of an index are rows that a text encoder wrote, and tau separates
+ * near duplicates only for an encoder trained to do so.  These are the encoder's
+ * own operators over a packed batch of documents, for embedding a corpus and for
+ * training: layer norm, and attention with a learned relative position bias, each
+ * with its backward pass.
+ *
+ * They follow the conventions above (argument checks before any HIP call, errors
+ * leave the outputs untouched, device pointers), with three differences:
+ *   - They are asynchronous: a call enqueues its kernels on the stream and returns
+ *     without waiting, allocates nothing and may be captured into a graph.
+ *   - dtype is SIEVE_F32, SIEVE_F16 or SIEVE_BF16; sums, softmax statistics and
+ *     gradients accumulate in fp32 whatever it is.
+ *   - Results do not depend on timing: no atomic's order enters a sum, so equal
+ *     calls give equal bits.
+ */
+
+/*
+ * sieve_norm_forward -- layer norm over rows of n values.
+ *   h = x (+ residual, the sum rounded to dtype), mean and variance (divided by n)
+ *   of a row of h, rstd = 1 / sqrt(variance + eps),
+ *   y = (h - mean) * rstd * weight (+ bias).
+ *   x            [rows, n] of dtype, rows x_stride values apart (>= n).
+ *   residual     NULL or [rows, n] of dtype, rows residual_stride values apart.
+ *   weight, bias [n] of wdtype, which is dtype or SIEVE_F32; bias may be NULL.
+ *   eps          >= 0.
+ *   y            [rows, n] of dtype, contiguous.
+ *   h            [rows, n] of dtype, contiguous: x + residual.  With a residual it is
+ *                required; without one it must be NULL (x is h).
+ *   mean, rstd   [rows] fp32, or both NULL where no backward pass follows.
+ * rows >= 0, 1 <= n <= 65536 (else SIEVE_EUNSUPPORTED).  y may be x or residual
+ * where these are contiguous and not needed after, and so may h; y and h differ.
+ */
+SIEVE_API int sieve_norm_forward(const void* x, int64_t x_stride, const void* residual,
+                                 int64_t residual_stride, const void* weight, const void* bias,
+                                 int32_t dtype, int32_t wdtype, int64_t rows, int32_t n, float eps,
+                                 void* y, void* h, float* mean, float* rstd, void* stream);
+
+/*
+ * sieve_norm_backward -- gradients of sieve_norm_forward.  With u = (h - mean) rstd
+ * and g = dy * weight:
+ *   dx = rstd (g - mean(g) - u mean(g u)) (+ dh), dweight = sum over rows of dy u,
+ *   dbias = sum over rows of dy.
+ * dx is the gradient of x and of residual alike.
+ *   dy           [rows, n] of dtype, rows dy_stride values apart.
+ *   h            [rows, n], rows h_stride values apart: the forward pass's h (x where it
+ *                had no residual), with its mean and rstd.
+ *   dh           NULL or [rows, n] of dtype, contiguous: the gradient that reaches h by
+ *                another way (the branch that skips the layer).
+ *   dx           [rows, n] of dtype, contiguous (may be dh, or a contiguous dy).
+ *   dweight, dbias  [n] of wdtype, each may be NULL.
+ *   workspace    device memory of sieve_norm_workspace(rows, n) bytes, 16-byte aligned
+ *                (only used in the call; may be NULL where that is 0).
+ * rows = 0 writes zeros to dweight and dbias.
+ */
+SIEVE_API int sieve_norm_backward(const void* dy, int64_t dy_stride, const void* h,
+                                  int64_t h_stride, const void* weight, const float* mean,
+                                  const float* rstd, const void* dh, int32_t dtype,
+                                  int32_t wdtype, int64_t rows, int32_t n, void* dx, void* dweight,
+                                  void* dbias, void* workspace, int64_t workspace_bytes,
+                                  void* stream);
+/* Bytes that sieve_norm_backward needs, or a negative sieve_status. */
+SIEVE_API int64_t sieve_norm_workspace(int64_t rows, int32_t n);
+
+/*
+ * Attention over a packed batch.  The tokens of all sequences lie one after another;
+ * sequence s has the queries q_offsets[s] .. q_offsets[s+1]-1 and the keys
+ * k_offsets[s] .. k_offsets[s+1]-1, and query i (0-based) of it stands at position
+ * i + (keys - queries), so that queries fewer than the keys are the sequence's last.
+ * A query head h reads key head h / (heads / kv_heads).
+ *   score = scale * <q_i, k_j> + bias[bucket(j - position of i)][h]
+ *   out_i = sum over the keys j that i sees of softmax(score)_j v_j
+ * A key is seen unless key_mask leaves it out or, with causal, it lies after the
+ * query's position.  A query that sees no key gets out = 0 and lse = -infinity, and
+ * gives no gradient.  What keys and values hold where key_mask leaves them out is not
+ * used, infinities and NaN included, and their gradients are 0.
+ *
+ * bucket(r) of a relative position r (sides = 2, or 1 with causal; side = num_buckets /
+ * sides buckets each; r > 0 is the second side, and with causal it never occurs): with
+ * m = |r| and e = side / 2, m itself below e, else
+ * e + floor((side - e) log(m / e) / log(max_distance / e)), at most side - 1.
+ */
+typedef struct sieve_attn_desc {
+  int32_t dtype;
+  int32_t heads, kv_heads;       /* kv_heads divides heads                             */
+  int32_t head_dim;              /* 1 .. SIEVE_ATTN_MAX_DIM                            */
+  int32_t causal;                /* 0 or 1                                             */
+  int32_t num_buckets;           /* 0 (no bias), or even, 4 .. 256                     */
+  int32_t max_distance;          /* with a bias: more than side / 2, and
+                                    (heads / kv_heads) * (2 max_distance + 129)
+                                    <= SIEVE_ATTN_BIAS_SPAN                            */
+  float scale;                   /* > 0 and finite                                     */
+  int64_t nseq;                  /* >= 0                                               */
+  const int64_t* q_offsets;      /* HOST [nseq + 1], non-decreasing from 0             */
+  const int64_t* k_offsets;      /* HOST [nseq + 1], or NULL: the same as q_offsets    */
+} sieve_attn_desc;
+#define SIEVE_ATTN_MAX_DIM 128
+#define SIEVE_ATTN_BIAS_SPAN 3080
+
+/* Rows of a packed tensor by token and head: value (t, h, c) is
+ * data[t * token_stride + h * head_stride + c] (strides in values, 1 between the values
+ * of a head).  16-byte loads are used where the data, both strides and head_dim are
+ * multiples of 16 bytes.  Gradients and outputs must not overlap their own rows. */
+typedef struct sieve_heads {
+  void* data;
+  int64_t token_stride, head_stride;
+} sieve_heads;
+
+typedef struct sieve_attn sieve_attn; /* opaque, owned by the library */
+
+/*
+ * sieve_attn_create -- plan the attention of one batch's lengths: checks the
+ * description, cuts the work into tiles and copies their list to the current device
+ * (synchronous).  Every layer and both passes over the batch share the plan; any number of
+ * calls on any streams may use it at once.  A sequence may have up to 2^31 - 2^16 rows
+ * (queries times heads / kv_heads) and keys (else SIEVE_EUNSUPPORTED).
+ * sieve_attn_free waits for the device's work (as hipFree does).
+ */
+SIEVE_API int sieve_attn_create(const sieve_attn_desc* desc, void* stream, sieve_attn** out);
+SIEVE_API void sieve_attn_free(sieve_attn* plan);
+
+/* Bytes of device workspace that the forward (backward = 0) or the backward pass
+ * (backward = 1) needs, or a negative sieve_status. */
+SIEVE_API int64_t sieve_attn_workspace(const sieve_attn* plan, int32_t backward);
+
+/*
+ * sieve_attn_forward
+ *   q, o         rows of the queries, heads each; k, v: rows of the keys, kv_heads each.
+ *   key_mask     NULL or [keys] bytes: 0 leaves the key out for every query.
+ *   bias         [num_buckets, heads] of dtype, or NULL where the plan has no buckets.
+ *   lse          NULL or [queries, heads] fp32: the logarithm of the sum of exp(score).
+ *   workspace    device memory of sieve_attn_workspace(plan, 0) bytes, 16-byte aligned.
+ */
+SIEVE_API int sieve_attn_forward(const sieve_attn* plan, const sieve_heads* q,
+                                 const sieve_heads* k, const sieve_heads* v,
+                                 const uint8_t* key_mask, const void* bias, const sieve_heads* o,
+                                 float* lse, void* workspace, int64_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * sieve_attn_backward -- the gradients, from the gradient of the output and the forward
+ * pass's inputs, output and lse; the probabilities are recomputed, not kept.
+ *   dout         the output's gradient; dq, dk, dv: the gradients written (dk and dv are
+ *                sums over the query heads that share a key head).
+ *   dbias        NULL or [num_buckets, heads] of dtype.
+ * Other arguments as for the forward pass (workspace: sieve_attn_workspace(plan, 1)).
+ */
+SIEVE_API int sieve_attn_backward(const sieve_attn* plan, const sieve_heads* dout,
+                                  const sieve_heads* q, const sieve_heads* k,
+                                  const sieve_heads* v, const sieve_heads* o, const float* lse,
+                                  const uint8_t* key_mask, const void* bias,
+                                  const sieve_heads* dq, const sieve_heads* dk,
+                                  const sieve_heads* dv, void* dbias, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
 
 /* Release an index and its cached workspace.  NULL is a no-op. */
 SIEVE_API void sieve_free_index(sieve_index* idx);

@@ -17,7 +17,8 @@ import torch
 
 __all__ = ["SieveError", "Index", "Stats", "Round", "load_library", "LIB_PATH", "W_INF",
            "K_MAX", "F32", "F16", "search_multi", "LOOKAHEAD_OFF", "LOOKAHEAD_COMMITTED",
-           "LOOKAHEAD_SERIAL", "LOOKAHEAD_SPECULATIVE"]
+           "LOOKAHEAD_SERIAL", "LOOKAHEAD_SPECULATIVE", "AttentionPlan", "BF16", "attention",
+           "layer_norm", "layer_norm_backward", "layer_norm_forward"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsieve.so")
 W_INF = 0x7FFFFFFF
@@ -344,3 +345,7 @@ def search_multi_calibrated(indexes, queries: torch.Tensor, exclude_ids: Optiona
             op.data_ptr(), ws, ctypes.byref(st) if st is not None else None, _stream(stream)))
     out = (oi, osc, op, [int(x) for x in ws])
     return out + (st,) if with_stats else out
+
+
+from .encoder import (AttentionPlan, BF16, attention, layer_norm, layer_norm_backward,  # noqa: E402
+                      layer_norm_forward)

@@ -26,16 +26,17 @@
 #include "host_limits.h"
 #include "sieve_internal.h"
 
-namespace sieve {
-}
-
 using namespace sieve;
 
 namespace {
 
 thread_local std::string g_err;
 
-int fail(int code, const char* fmt, ...) {
+}  // namespace
+
+namespace sieve {
+void clear_error() { g_err.clear(); }
+int set_error(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -44,6 +45,11 @@ int fail(int code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
+}  // namespace sieve
+
+namespace {
+
+constexpr auto& fail = set_error;
 
 #define HIP_TRY(expr)                                                                  \
   do {                                                                                 \

@@ -1,0 +1,70 @@
+// attn.h -- work items, arguments and launchers of the packed attention
+// (attn.hip: plan and C ABI; attn_kernels.h: the kernels, compiled once for each
+// type by attn_f32.hip, attn_f16.hip and attn_bf16.hip).
+#pragma once
+
+#include "enc_common.h"
+
+namespace sieve {
+
+// One work-group's share.  The rows of a sequence for one key head are its queries
+// times the G = heads / kv_heads query heads that read it: row r is query r / G,
+// head kvh * G + r % G, so that the heads of a group share every key they load.
+struct AttnItem {
+  int64_t q0, k0;   // first query and key token of the sequence in the packed batch
+  int32_t nq, nk;   // its queries and keys
+  int32_t kvh;
+  int32_t row;      // first row of the tile (forward, dq), or first key (dk and dv)
+  int32_t lo, hi;   // keys to go through (forward, dq), or rows (dk and dv)
+  int32_t part;     // forward: slot of a partial result, -1 where the item is a whole row
+                    // tile; dq: number of the row tile among all sequences
+  int32_t tile0, ntiles;  // dk and dv: the sequence's row tiles of the dq pass
+  int32_t pad;
+};
+
+// One row tile whose keys several items shared.
+struct AttnJoin {
+  int64_t q0;
+  int32_t nq, kvh, row, part0, parts, pad;
+};
+
+constexpr int kAttnThreads = 256;
+constexpr int kAttnPad = 64;      // relative positions past the distance in the bias table
+constexpr int kAttnRows = 128;    // rows of a tile: 4 waves of 32
+constexpr int kAttnFewRows = 32;  // rows of a tile whose 4 waves share the keys out
+constexpr int kAttnKeys = 128;    // keys of a dk and dv tile
+
+struct AttnArgs {
+  const AttnItem* items;
+  const AttnJoin* joins;
+  int32_t nitems, njoins;
+  sieve_heads q, k, v, o, dout, dq, dk, dv;
+  const uint8_t* key_mask;
+  const void* bias;
+  float* lse;        // written by the forward pass, read by the backward pass
+  int32_t G, heads, kv_heads, d, causal;
+  int32_t vec;       // every row may be moved in 16-byte pieces
+  float scale;
+  // bias: table entry i of a head is relative position i - distance - kAttnPad
+  int32_t nb, distance, span;
+  const int16_t* bucket_of;  // [span]
+  const int16_t* range;      // [nb][2]: first entry of a bucket and the one past its last
+  void* dbias;
+  // workspace
+  float* part_o;     // [parts][rows][DP] unnormalised sums, then [parts][rows][2]: max and sum
+  float* part_ml;
+  float* dsum;       // [queries][heads]: the rows' sums of dout * o
+  float* part_bias;  // [kv_heads][row tiles][G][nb]
+  float* part_max;   // [kv_heads][row tiles]: the largest |dS| (16-bit floats only)
+  int32_t row_tiles;
+};
+
+enum AttnKind { kAttnFwd, kAttnFwdFew, kAttnJoin, kAttnJoinFew, kAttnDq, kAttnDkv };
+
+// Launch one pass; dp is the padded head size (32, 64 or 128), grid the number of
+// work-groups.
+hipError_t attn_launch_f32(AttnKind kind, int dp, const AttnArgs& a, int grid, hipStream_t s);
+hipError_t attn_launch_f16(AttnKind kind, int dp, const AttnArgs& a, int grid, hipStream_t s);
+hipError_t attn_launch_bf16(AttnKind kind, int dp, const AttnArgs& a, int grid, hipStream_t s);
+
+}  // namespace sieve

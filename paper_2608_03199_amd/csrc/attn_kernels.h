@@ -1,0 +1,1089 @@
+// attn_kernels.h -- attention over packed sequences, forward and backward, on 32x32
+// MFMA tiles.
+//
+//   S = scale Q K^T + bias, P = softmax(S), O = P V
+//   D = rowsum(dO O), dP = dO V^T, dS = P (dP - D)
+//   dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO, dbias = sums of dS by bucket
+//
+// Every product is laid out so that one lane holds one row of queries (forward, dQ)
+// or one key (dK, dV) and its registers run along the axis that is summed next:
+//
+//   S^T = K Q^T puts query lane % 32 in a lane, and keys 8 g + 4 (lane / 32) + t in
+//   register 4 g + t.  The row's maximum and sum are then sums over registers and one
+//   exchange between the wave's halves, the rescale of O^T = V^T P^T is by a lane's own
+//   factor, and the registers 8 s .. 8 s + 7 already are the B operand of the next
+//   product's 16-key step s, with the keys in the order {16 s + 4 h + 0..3,
+//   16 s + 8 + 4 h + 0..3}.  The order of a sum's terms is free as long as both operands
+//   agree, so the A operand (V^T, K^T) is read from LDS in that order: two transposing
+//   8-byte reads for 16-bit values, eight 4-byte reads for 32-bit ones.  Probabilities
+//   never pass through LDS.
+//
+// The key and value tiles go through registers into LDS rows padded by 16 bytes, loaded
+// one tile ahead.  Rows that a mask leaves out, or past the sequence's end, are stored as
+// zeros: what they hold never meets a product.
+//
+// P and dS are rounded to the inputs' type for the second products, as those run on the
+// 16-bit matrix units; S, dP, the statistics and every accumulator are fp32.  bfloat16
+// keeps fp32's range.  binary16 does not, so there the values are scaled by powers of two
+// that the end takes out exactly: P by 2^6 below a running maximum that lags by at most
+// 2^8 (forward) or by 2^14 (backward, where P <= 1), and dS by what brings its largest
+// magnitude to 2^13 .. 2^14.
+#pragma once
+
+#include "attn.h"
+
+namespace sieve {
+namespace {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <typename T>
+struct Vec8 {
+  typedef T type __attribute__((ext_vector_type(8)));
+};
+template <typename T>
+using vec8 = typename Vec8<T>::type;
+
+__device__ __forceinline__ f32x16 mma(vec8<f16> a, vec8<f16> b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(vec8<bf16> a, vec8<bf16> b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// 16 terms in fp32: step j multiplies element j of both halves' operands
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+// Row stride of an LDS tile.
+template <typename T, int DP>
+constexpr int lds_row() {
+  return DP + 16 / (int)sizeof(T);
+}
+
+// Values 16 c + 8 h .. + 7 of a row: the operand whose summed axis is the head's.
+template <typename T, int DP>
+__device__ __forceinline__ vec8<T> frag_along(const T* s, int row, int c, int h) {
+  const EncVec<T, 8> q = enc_load<T, 8>(s + row * lds_row<T, DP>() + 16 * c + 8 * h);
+  return __builtin_bit_cast(vec8<T>, q);
+}
+
+// Value col + lane % 32 of the rows row + {4 h + 0..3, 8 + 4 h + 0..3}: the operand whose
+// summed axis is the tile's rows.  The transposing read gives lane i of each 16 the i-th
+// column of the 4 rows that the 16 lanes' addresses cover.
+template <typename T, int DP>
+__device__ __forceinline__ vec8<T> frag_across(const T* s, int row, int col, int lane) {
+  constexpr int kLd = lds_row<T, DP>();
+  const int h = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    const int i = lane & 15;
+    const T* p = s + (row + 4 * h + (i >> 2)) * kLd + col + (lane & 16) + (i & 3) * 4;
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    union {
+      s16x4 half[2];
+      vec8<T> all;
+    } u;
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kLd));
+    return u.all;
+  } else {
+    const T* p = s + (row + 4 * h) * kLd + col + (lane & 31);
+    vec8<T> r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      r[j] = p[j * kLd];
+      r[4 + j] = p[(8 + j) * kLd];
+    }
+    return r;
+  }
+}
+
+// Registers 8 s .. 8 s + 7 as an operand, rounded to nearest.
+template <typename T>
+__device__ __forceinline__ vec8<T> frag_of(const f32x16& x, int s) {
+  const f32x8 v = s == 0 ? __builtin_shufflevector(x, x, 0, 1, 2, 3, 4, 5, 6, 7)
+                         : __builtin_shufflevector(x, x, 8, 9, 10, 11, 12, 13, 14, 15);
+  return __builtin_convertvector(v, vec8<T>);
+}
+
+// Offset of packed row r (query r / G, head r % G of the group).
+__device__ __forceinline__ int64_t row_at(const sieve_heads& x, int64_t q0, int kvh, int G, int r) {
+  const int tok = G == 1 ? r : r / G;
+  return (q0 + tok) * x.token_stride + (int64_t)(kvh * G + (r - tok * G)) * x.head_stride;
+}
+
+// One row's values 16 c + 8 h .. + 7 for all c, from global memory; zeros past the head's
+// size, or all zeros where the row is not there.
+template <typename T, int DP>
+__device__ __forceinline__ void load_frags(const T* p, bool ok, int d, int vec, int h,
+                                           vec8<T> (&f)[DP / 16]) {
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) {
+    const int col = 16 * c + 8 * h;
+    EncVec<T, 8> q;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q.v[j] = (T)0.f;
+    if (ok && col < d) {
+      if (vec && (sizeof(T) == 2 || col + 8 <= d)) {
+        q = enc_load<T, 8>(p + col);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (col + j < d) q.v[j] = p[col + j];
+      }
+    }
+    f[c] = __builtin_bit_cast(vec8<T>, q);
+  }
+}
+
+// A tile of ROWS rows on its way from global memory through registers into LDS.
+template <typename T, int DP, int ROWS>
+struct Stage {
+  static constexpr int kE = 16 / sizeof(T);           // values of a 16-byte piece
+  static constexpr int kPieces = DP / kE;             // pieces of a row
+  static constexpr int kAll = ROWS * kPieces;
+  static constexpr int kN = (kAll + kAttnThreads - 1) / kAttnThreads;
+  enc_u32x4 r[kN];
+
+  // row_of(i): where row i of the tile lies, or null where it is to be zeros
+  template <typename F>
+  __device__ __forceinline__ void load(F row_of, int d, int vec) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int idx = threadIdx.x + i * kAttnThreads;
+      const int row = idx / kPieces, col = (idx % kPieces) * kE;
+      r[i] = enc_u32x4{0, 0, 0, 0};
+      if (kAll % kAttnThreads != 0 && idx >= kAll) continue;
+      if (col >= d) continue;
+      const T* p = row_of(row);
+      if (!p) continue;
+      if (vec) {
+        r[i] = *(const enc_u32x4*)(p + col);
+      } else {
+        EncVec<T, kE> q;
+#pragma unroll
+        for (int j = 0; j < kE; ++j) q.v[j] = col + j < d ? p[col + j] : (T)0.f;
+        r[i] = __builtin_bit_cast(enc_u32x4, q);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* s) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int idx = threadIdx.x + i * kAttnThreads;
+      if (kAll % kAttnThreads != 0 && idx >= kAll) continue;
+      const int row = idx / kPieces, col = (idx % kPieces) * kE;
+      *(enc_u32x4*)(s + row * lds_row<T, DP>() + col) = r[i];
+    }
+  }
+};
+
+// Accumulators X^T (rows: the head's values 32 b + 8 g + 4 h + t in register 4 g + t,
+// column: the lane's row) times f, to a row in global memory.
+template <typename T, int DP>
+__device__ __forceinline__ void store_row(T* p, const f32x16 (&x)[DP / 32], float f, int d,
+                                          int vec, int h) {
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = 32 * b + 8 * g + 4 * h;
+      typedef T vec4 __attribute__((ext_vector_type(4)));
+      const f32x4 v = {x[b][4 * g] * f, x[b][4 * g + 1] * f, x[b][4 * g + 2] * f,
+                       x[b][4 * g + 3] * f};
+      const vec4 q = __builtin_convertvector(v, vec4);
+      if (vec && col + 4 <= d) {
+        *(vec4*)(p + col) = q;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + j < d) p[col + j] = q[j];
+      }
+    }
+  }
+}
+
+// The group's bias tables into LDS, times log2(e): s[g * span + entry].
+template <typename T>
+__device__ __forceinline__ void load_bias(const AttnArgs& a, int kvh, float* s) {
+  for (int i = threadIdx.x; i < a.G * a.span; i += kAttnThreads) {
+    const int g = i / a.span;
+    const int bucket = a.bucket_of[i - g * a.span];
+    s[i] = (float)((const T*)a.bias)[(int64_t)bucket * a.heads + kvh * a.G + g] * kLog2e;
+  }
+}
+
+// Bits 0..31: key base + bit is in the item's range and not masked.  Loaded a tile ahead.
+__device__ __forceinline__ bool key_ok(const AttnArgs& a, const AttnItem& it, int key) {
+  if (key >= it.hi) return false;
+  return !a.key_mask || a.key_mask[it.k0 + key] != 0;
+}
+
+// Bits 0..31: key base + bit is not after position pos.
+__device__ __forceinline__ uint32_t upto(int pos, int base) {
+  const int lim = pos - base;
+  return lim >= 31 ? ~0u : lim < 0 ? 0u : (2u << lim) - 1;
+}
+
+// Scores of 32 keys (base ..) for the lane's row, in units of log2: scaled, biased, and
+// -infinity where bits (this half's view) has a 0.  lo, hi: bias past the distance.
+template <bool kBias>
+__device__ __forceinline__ void finish_scores(f32x16& s, float scale2, const float* table,
+                                              int distance, int pos, int pos_min, int pos_max,
+                                              float lo, float hi, int base, int h, uint32_t bits) {
+  if constexpr (kBias) {
+    if (base - pos_max >= distance || base + 31 - pos_min <= -distance) {
+      const float far = base > pos_min ? hi : lo;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = s[r] * scale2 + far;
+    } else {
+      const float* t = table + (base + 4 * h - pos + distance + kAttnPad);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = s[r] * scale2 + t[8 * (r >> 2) + (r & 3)];
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] *= scale2;
+  }
+  if (!__all(bits == ~0u)) {
+    const uint32_t mine = bits >> (4 * h);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      s[r] = mine >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : -INFINITY;
+  }
+}
+
+// What a lane knows about its row.
+struct LaneRow {
+  int r, tok, g, pos;  // row, query, head in the group, position
+  int pos_min, pos_max;  // over the wave's rows
+  bool live;
+};
+__device__ __forceinline__ LaneRow lane_row(const AttnItem& it, int G, int first, int lane) {
+  LaneRow x;
+  const int rows = it.nq * G;
+  x.r = first + (lane & 31);
+  x.live = x.r < rows;
+  const int r = x.live ? x.r : (rows > 0 ? rows - 1 : 0);
+  x.tok = G == 1 ? r : r / G;
+  x.g = r - x.tok * G;
+  const int shift = it.nk - it.nq;
+  x.pos = x.tok + shift;
+  const int last = first + 31 < rows ? first + 31 : rows - 1;
+  const int head = first < rows ? first : rows - 1;
+  x.pos_min = head / G + shift;
+  x.pos_max = last / G + shift;
+  return x;
+}
+
+template <typename T>
+constexpr float kShift = __is_same(T, f16) ? 6.f : 0.f;
+constexpr float kLag = 8.f;  // a running maximum is left to lag by this many powers of two
+
+// ---- forward ----------------------------------------------------------------------------
+// WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
+// each wave takes every fourth block of 32 keys, and LDS joins the four at the end: for
+// few rows, where the keys' and values' bytes bound the time.
+
+template <typename T, int DP, int WK>
+struct FwdShape {
+  static constexpr int kBlocks = WK == 1 && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave
+  static constexpr int kTile = 32 * kBlocks * WK;                    // keys of a tile
+  static constexpr int kBufs = WK == 1 ? 2 : 1;
+  static constexpr int kTileBytes = kTile * lds_row<T, DP>() * (int)sizeof(T);
+  static constexpr int kStageBytes = 2 * kBufs * kTileBytes;
+  static constexpr int kJoinBytes = WK == 1 ? 0 : (WK * 32 * (DP + 4) + 2 * WK * 32) * 4;
+  static constexpr int kBytes = kStageBytes > kJoinBytes ? kStageBytes : kJoinBytes;
+  static constexpr int kRows = WK == 1 ? kAttnRows : kAttnFewRows;
+};
+
+template <typename T, int DP, int WK, bool kBias>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_forward_kernel(AttnArgs a) {
+  using Shape = FwdShape<T, DP, WK>;
+  constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
+  constexpr int kTileN = kTile * lds_row<T, DP>();
+  extern __shared__ __align__(16) uint8_t smem[];
+  T* s_k = (T*)smem;
+  T* s_v = s_k + Shape::kBufs * kTileN;
+  float* s_bias = (float*)(smem + Shape::kBytes);
+  const AttnItem it = a.items[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int G = a.G, d = a.d, vec = a.vec;
+  const LaneRow me = lane_row(it, G, it.row + (WK == 1 ? wave * 32 : 0), lane);
+  const float scale2 = a.scale * kLog2e;
+  const bool wave_live = WK == 4 || it.row + wave * 32 < it.nq * G;
+
+  const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
+  const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
+  Stage<T, DP, kTile> st_k, st_v;
+  bool ok[kBlocks];
+  auto fetch = [&](int base) {
+    st_k.load([&](int i) { return key_ok(a, it, base + i)
+                                      ? k0 + (int64_t)(base + i) * a.k.token_stride : nullptr; },
+              d, vec);
+    st_v.load([&](int i) { return key_ok(a, it, base + i)
+                                      ? v0 + (int64_t)(base + i) * a.v.token_stride : nullptr; },
+              d, vec);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+      ok[b] = key_ok(a, it, base + 32 * ((WK == 1 ? 0 : wave) + b) + (lane & 31));
+  };
+  if (it.lo < it.hi) fetch(it.lo);
+
+  vec8<T> q[DP / 16];
+  {
+    const T* p = (const T*)a.q.data + (me.live ? row_at(a.q, it.q0, it.kvh, G, me.r) : 0);
+    load_frags<T, DP>(p, me.live, d, vec, h, q);
+  }
+  float lo = 0.f, hi = 0.f;
+  const float* table = nullptr;
+  if constexpr (kBias) {
+    load_bias<T>(a, it.kvh, s_bias);
+    __syncthreads();
+    table = s_bias + me.g * a.span;
+    lo = table[0];
+    hi = table[a.span - 1];
+  }
+  f32x16 o[DP / 32];
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
+  float m = -INFINITY, l = 0.f;
+
+  int buf = 0;
+  if (it.lo < it.hi) {
+    st_k.store(s_k);
+    st_v.store(s_v);
+    __syncthreads();
+  }
+  for (int base = it.lo; base < it.hi; base += kTile) {
+    const int first = base + (WK == 1 ? 0 : wave * 32);
+    uint32_t bits[kBlocks], any = 0;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      bits[b] = (uint32_t)__ballot(ok[b]);
+      if (a.causal) bits[b] &= upto(me.pos, first + 32 * b);
+      any |= bits[b];
+    }
+    const bool more = base + kTile < it.hi;
+    if (more) fetch(base + kTile);
+    if (wave_live && __any(any != 0)) {
+      const T* sk = s_k + buf * kTileN + (WK == 1 ? 0 : wave * 32) * lds_row<T, DP>();
+      const T* sv = s_v + buf * kTileN + (WK == 1 ? 0 : wave * 32) * lds_row<T, DP>();
+      f32x16 s[kBlocks];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        s[b] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c)
+          s[b] = mma(frag_along<T, DP>(sk, 32 * b + (lane & 31), c, h), q[c], s[b]);
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        finish_scores<kBias>(s[b], scale2, table, a.distance, me.pos, me.pos_min, me.pos_max, lo,
+                             hi, first + 32 * b, h, bits[b]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m + kLag)) {
+        const float next = fmaxf(m, top);
+        const float f = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.f : next));
+        m = next;
+        l *= f;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[b][r] *= f;
+      }
+      const float off = (m == -INFINITY ? 0.f : m) - kShift<T>;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - off);
+          l += s[b][r];
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const vec8<T> p = frag_of<T>(s[b], c);
+#pragma unroll
+          for (int e = 0; e < DP / 32; ++e)
+            o[e] = mma(frag_across<T, DP>(sv, 32 * b + 16 * c, 32 * e, lane), p, o[e]);
+        }
+      }
+    }
+    if (Shape::kBufs == 1) __syncthreads();
+    if (more) {
+      buf ^= Shape::kBufs - 1;
+      st_k.store(s_k + buf * kTileN);
+      st_v.store(s_v + buf * kTileN);
+      __syncthreads();
+    }
+  }
+  l += __shfl_xor(l, 32);
+  float at = (m == -INFINITY ? 0.f : m) - kShift<T>;  // the sums are relative to 2^at
+
+  if constexpr (WK == 4) {
+    // join the waves: sums relative to the largest maximum
+    float* s_o = (float*)smem;
+    float* s_ml = s_o + WK * 32 * (DP + 4);
+    __syncthreads();
+    if (h == 0) {
+      s_ml[(wave * 32 + lane) * 2] = l == 0.f ? -INFINITY : at;
+      s_ml[(wave * 32 + lane) * 2 + 1] = l;
+    }
+    __syncthreads();
+    float most = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) most = fmaxf(most, s_ml[(w * 32 + (lane & 31)) * 2]);
+    if (most == -INFINITY) most = 0.f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      const float* p = s_ml + (w * 32 + (lane & 31)) * 2;
+      sum += p[1] == 0.f ? 0.f : p[1] * __builtin_amdgcn_exp2f(p[0] - most);
+    }
+    const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(at - most);
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = {o[b][4 * g] * f, o[b][4 * g + 1] * f, o[b][4 * g + 2] * f,
+                         o[b][4 * g + 3] * f};
+        *(f32x4*)(s_o + (wave * 32 + (lane & 31)) * (DP + 4) + 32 * b + 8 * g + 4 * h) = v;
+      }
+    __syncthreads();
+    if (wave) return;
+    l = sum;
+    at = most;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 v = {};
+#pragma unroll
+        for (int w = 0; w < WK; ++w)
+          v += *(const f32x4*)(s_o + (w * 32 + (lane & 31)) * (DP + 4) + 32 * b + 8 * g + 4 * h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[b][4 * g + j] = v[j];
+      }
+  }
+  if (it.part >= 0) {
+    const int64_t slot = (int64_t)it.part * Shape::kRows + (WK == 1 ? wave * 32 : 0) + (lane & 31);
+    float* p = a.part_o + slot * DP;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(f32x4*)(p + 32 * b + 8 * g + 4 * h) =
+            f32x4{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
+    if (h == 0) {
+      a.part_ml[slot * 2] = l == 0.f ? -INFINITY : at;
+      a.part_ml[slot * 2 + 1] = l;
+    }
+    return;
+  }
+  if (!me.live) return;
+  store_row<T, DP>((T*)a.o.data + row_at(a.o, it.q0, it.kvh, G, me.r), o,
+                   l == 0.f ? 0.f : 1.f / l, d, vec, h);
+  if (a.lse && h == 0)
+    a.lse[(it.q0 + me.tok) * a.heads + it.kvh * G + me.g] =
+        l == 0.f ? -INFINITY : (at + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Partial rows of one tile to whole ones: 8 threads a row.
+template <typename T, int DP, int ROWS>
+__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
+  const AttnJoin j = a.joins[blockIdx.x];
+  const int rows = j.nq * a.G;
+  for (int i = threadIdx.x / 8; i < ROWS; i += kAttnThreads / 8) {
+    const int r = j.row + i;
+    if (r >= rows) break;
+    float most = -INFINITY;
+    for (int p = 0; p < j.parts; ++p)
+      most = fmaxf(most, a.part_ml[((int64_t)(j.part0 + p) * ROWS + i) * 2]);
+    if (most == -INFINITY) most = 0.f;
+    float l = 0.f;
+    constexpr int kN = DP / 8;
+    float v[kN];
+#pragma unroll
+    for (int e = 0; e < kN; ++e) v[e] = 0.f;
+    for (int p = 0; p < j.parts; ++p) {
+      const int64_t slot = (int64_t)(j.part0 + p) * ROWS + i;
+      const float lp = a.part_ml[slot * 2 + 1];
+      if (lp == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[slot * 2] - most);
+      l += lp * f;
+      const float* o = a.part_o + slot * DP + (threadIdx.x & 7) * 4;
+#pragma unroll
+      for (int e = 0; e < kN / 4; ++e) {
+        const f32x4 x = *(const f32x4*)(o + 32 * e);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[4 * e + t] += f * x[t];
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* to = (T*)a.o.data + row_at(a.o, j.q0, j.kvh, a.G, r);
+#pragma unroll
+    for (int e = 0; e < kN / 4; ++e)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int col = 32 * e + (threadIdx.x & 7) * 4 + t;
+        if (col < a.d) to[col] = (T)(v[4 * e + t] * inv);
+      }
+    if (a.lse && (threadIdx.x & 7) == 0) {
+      const int tok = r / a.G;
+      a.lse[(j.q0 + tok) * a.heads + j.kvh * a.G + (r - tok * a.G)] =
+          l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+  }
+}
+
+// ---- backward: dQ and the bias table's gradient ------------------------------------------
+// A wave takes 32 of the tile's 128 rows and goes through the keys as the forward pass does.
+// It writes D for the second kernel.
+//
+// The bias table's gradient is a sum along diagonals.  Where a block of keys is past the
+// distance it all falls into one bucket, and the lane adds it up in a register; nearer, each
+// value is added in LDS to the sum of its relative position.  One instruction's 32 lanes of a
+// half have 32 different (head, position) pairs, and every wave and half has sums of its own,
+// so no two additions ever meet and their order is the program's.
+
+template <typename T, int DP>
+struct DqShape {
+  static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 ? 2 : 1;
+  static constexpr int kTile = 32 * kBlocks;
+  static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kBytes = 2 * kBufs * kTile * lds_row<T, DP>() * (int)sizeof(T);
+};
+constexpr int kSums = 2 * kAttnThreads / 64;  // copies of the sums by position: wave and half
+
+template <typename T, int DP, bool kBias>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
+  using Shape = DqShape<T, DP>;
+  constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
+  constexpr int kTileN = kTile * lds_row<T, DP>();
+  constexpr bool kScaled = __is_same(T, f16);
+  extern __shared__ __align__(16) uint8_t smem[];
+  T* s_k = (T*)smem;
+  T* s_v = s_k + Shape::kBufs * kTileN;
+  float* s_bias = (float*)(smem + Shape::kBytes);
+  float* s_sum = s_bias + a.G * a.span;            // [wave][half][G][span]
+  float* s_far = s_sum + kSums * a.G * a.span;     // [wave][half][32][2]
+  __shared__ float s_max[kAttnThreads / 64];
+  const AttnItem it = a.items[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int G = a.G, d = a.d, vec = a.vec;
+  const LaneRow me = lane_row(it, G, it.row + wave * 32, lane);
+  const float scale2 = a.scale * kLog2e;
+  const bool wave_live = it.row + wave * 32 < it.nq * G;
+  const bool want_bias = kBias && a.dbias;
+
+  const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
+  const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
+  Stage<T, DP, kTile> st_k, st_v;
+  bool ok[kBlocks];
+  auto fetch = [&](int base) {
+    st_k.load([&](int i) { return key_ok(a, it, base + i)
+                                      ? k0 + (int64_t)(base + i) * a.k.token_stride : nullptr; },
+              d, vec);
+    st_v.load([&](int i) { return key_ok(a, it, base + i)
+                                      ? v0 + (int64_t)(base + i) * a.v.token_stride : nullptr; },
+              d, vec);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) ok[b] = key_ok(a, it, base + 32 * b + (lane & 31));
+  };
+  if (it.lo < it.hi) fetch(it.lo);
+
+  const int64_t at = (it.q0 + me.tok) * a.heads + it.kvh * G + me.g;
+  // a row that saw no key has lse = -infinity; as +infinity it makes every P 0
+  float lse2 = INFINITY, dsum = 0.f;
+  vec8<T> q[DP / 16], dout[DP / 16];
+  {
+    const float lse = me.live ? a.lse[at] : -INFINITY;
+    const bool some = lse != -INFINITY;
+    if (some) lse2 = lse * kLog2e;
+    const T* pq = (const T*)a.q.data + (me.live ? row_at(a.q, it.q0, it.kvh, G, me.r) : 0);
+    const T* pd = (const T*)a.dout.data + (me.live ? row_at(a.dout, it.q0, it.kvh, G, me.r) : 0);
+    const T* po = (const T*)a.o.data + (me.live ? row_at(a.o, it.q0, it.kvh, G, me.r) : 0);
+    vec8<T> out[DP / 16];
+    load_frags<T, DP>(pq, some, d, vec, h, q);
+    load_frags<T, DP>(pd, some, d, vec, h, dout);
+    load_frags<T, DP>(po, some, d, vec, h, out);
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dsum += (float)dout[c][j] * (float)out[c][j];
+    dsum += __shfl_xor(dsum, 32);
+    if (me.live && h == 0) a.dsum[at] = dsum;
+  }
+  float lo = 0.f, hi = 0.f, far_lo = 0.f, far_hi = 0.f;
+  const float* table = nullptr;
+  float* sums = nullptr;
+  if constexpr (kBias) {
+    load_bias<T>(a, it.kvh, s_bias);
+    if (want_bias)
+      for (int i = threadIdx.x; i < kSums * G * a.span; i += kAttnThreads) s_sum[i] = 0.f;
+    __syncthreads();
+    table = s_bias + me.g * a.span;
+    lo = table[0];
+    hi = table[a.span - 1];
+    sums = s_sum + ((wave * 2 + h) * G + me.g) * a.span;
+  }
+  f32x16 dq[DP / 32];
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
+  float most = 0.f;                  // largest |dS| of the row so far
+  float up = kScaled ? 0x1p40f : 1;  // dS is rounded times this
+
+  int buf = 0;
+  if (it.lo < it.hi) {
+    st_k.store(s_k);
+    st_v.store(s_v);
+    __syncthreads();
+  }
+  for (int base = it.lo; base < it.hi; base += kTile) {
+    uint32_t bits[kBlocks], any = 0;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      bits[b] = (uint32_t)__ballot(ok[b]);
+      if (a.causal) bits[b] &= upto(me.pos, base + 32 * b);
+      any |= bits[b];
+    }
+    const bool more = base + kTile < it.hi;
+    if (more) fetch(base + kTile);
+    if (wave_live && __any(any != 0)) {
+      const T* sk = s_k + buf * kTileN;
+      const T* sv = s_v + buf * kTileN;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) {
+          s = mma(frag_along<T, DP>(sk, 32 * b + (lane & 31), c, h), q[c], s);
+          dp = mma(frag_along<T, DP>(sv, 32 * b + (lane & 31), c, h), dout[c], dp);
+        }
+        const int first = base + 32 * b;
+        finish_scores<kBias>(s, scale2, table, a.distance, me.pos, me.pos_min, me.pos_max, lo, hi,
+                             first, h, bits[b]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[r] = __builtin_amdgcn_exp2f(s[r] - lse2) * (dp[r] - dsum);  // dS
+        if (!__all(bits[b] == ~0u)) {
+          // P = 0 there, but dP need not be a number
+          const uint32_t mine = bits[b] >> (4 * h);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[r] = mine >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : 0.f;
+        }
+        if constexpr (kBias) {
+          if (want_bias) {
+            if (first - me.pos_max >= a.distance || first + 31 - me.pos_min <= -a.distance) {
+              float t = 0.f;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) t += s[r];
+              if (first > me.pos_min) far_hi += t;
+              else far_lo += t;
+            } else if (me.live) {
+              float* t = sums + (first + 4 * h - me.pos + a.distance + kAttnPad);
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                __hip_atomic_fetch_add(t + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+          }
+        }
+        if constexpr (kScaled) {
+          float t = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) t = fmaxf(t, fabsf(s[r]));
+          t = fmaxf(t, __shfl_xor(t, 32));
+          most = fmaxf(most, t);
+          if (__any(most * up >= 0x1p15f)) {
+            // the largest so far to 2^13 .. 2^14
+            const float next =
+                most * up >= 0x1p15f
+                    ? __builtin_amdgcn_ldexpf(1.f, 14 - __builtin_amdgcn_frexp_expf(most))
+                    : up;
+            const float f = next / up;
+            up = next;
+#pragma unroll
+            for (int e = 0; e < DP / 32; ++e)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) dq[e][r] *= f;
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= up;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const vec8<T> p = frag_of<T>(s, c);
+#pragma unroll
+          for (int e = 0; e < DP / 32; ++e)
+            dq[e] = mma(frag_across<T, DP>(sk, 32 * b + 16 * c, 32 * e, lane), p, dq[e]);
+        }
+      }
+    }
+    if (Shape::kBufs == 1) __syncthreads();
+    if (more) {
+      buf ^= Shape::kBufs - 1;
+      st_k.store(s_k + buf * kTileN);
+      st_v.store(s_v + buf * kTileN);
+      __syncthreads();
+    }
+  }
+  if (me.live)
+    store_row<T, DP>((T*)a.dq.data + row_at(a.dq, it.q0, it.kvh, G, me.r), dq, a.scale / up, d,
+                     vec, h);
+  if constexpr (kScaled) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    if (lane == 0) s_max[wave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0)
+      a.part_max[(int64_t)it.kvh * a.row_tiles + it.part] =
+          fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  }
+  if constexpr (kBias) {
+    if (!want_bias) return;
+    s_far[(wave * 64 + h * 32 + (lane & 31)) * 2] = me.live ? far_lo : 0.f;
+    s_far[(wave * 64 + h * 32 + (lane & 31)) * 2 + 1] = me.live ? far_hi : 0.f;
+    __syncthreads();
+    const int all = G * a.span;
+    for (int i = threadIdx.x; i < all; i += kAttnThreads) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < kSums; ++w) t += s_sum[w * all + i];
+      s_sum[i] = t;  // entry i belongs to this thread alone
+    }
+    __syncthreads();
+    // 8 threads a bucket
+    float* to = a.part_bias + ((int64_t)it.kvh * a.row_tiles + it.part) * G * a.nb;
+    const int bucket_lo = a.bucket_of[0], bucket_hi = a.bucket_of[a.span - 1];
+    const int sub = threadIdx.x & 7;
+    for (int i = threadIdx.x >> 3; i < G * a.nb; i += kAttnThreads / 8) {
+      const int g = i / a.nb, b = i - g * a.nb;
+      float t = 0.f;
+      for (int e = a.range[2 * b] + sub; e < a.range[2 * b + 1]; e += 8)
+        t += s_sum[g * a.span + e];
+      if (b == bucket_lo || b == bucket_hi) {
+        // copy `sub` of the sums past the distance: the rows of this head
+        for (int row = 0; row < 32; ++row)
+          if ((it.row + (sub >> 1) * 32 + row) % G == g) {
+            if (b == bucket_lo) t += s_far[(sub * 32 + row) * 2];
+            if (b == bucket_hi) t += s_far[(sub * 32 + row) * 2 + 1];
+          }
+      }
+#pragma unroll
+      for (int o = 4; o; o >>= 1) t += __shfl_xor(t, o);
+      if (sub == 0) to[i] = t;
+    }
+  }
+}
+
+// ---- backward: dK and dV -------------------------------------------------------------------
+// A wave takes 32 of the tile's 128 keys, one a lane, and goes through the rows that see
+// them: all query heads of the group, so that the sum over a shared head is the accumulator's.
+// S = Q K^T puts rows 8 g + 4 h + t in registers 4 g + t.  The last `heads` work-groups of a
+// launch with a bias add up its gradient's partial sums instead.
+
+template <typename T, int DP>
+struct DkvShape {
+  static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 ? 2 : 1;  // 32-row blocks of a tile
+  static constexpr int kTile = 32 * kBlocks;
+  static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kTileBytes = kTile * lds_row<T, DP>() * (int)sizeof(T);
+  static constexpr int kBytes = kBufs * (2 * kTileBytes + 4 * kTile * 4);
+};
+
+template <typename T>
+__device__ __forceinline__ void reduce_bias(const AttnArgs& a, int head, float* s) {
+  // threads: nb (rounded up to a power of two) x groups of row tiles
+  int wide = 4;
+  while (wide < a.nb) wide *= 2;
+  const int groups = kAttnThreads / wide, b = threadIdx.x % wide, g = threadIdx.x / wide;
+  const int kvh = head / a.G;
+  const float* p = a.part_bias + ((int64_t)kvh * a.row_tiles * a.G + (head - kvh * a.G)) * a.nb;
+  float t = 0.f;
+  if (b < a.nb)
+    for (int i = g; i < a.row_tiles; i += groups) t += p[(int64_t)i * a.G * a.nb + b];
+  s[threadIdx.x] = t;
+  __syncthreads();
+  if (g == 0 && b < a.nb) {
+    t = 0.f;
+    for (int i = 0; i < groups; ++i) t += s[i * wide + b];
+    ((T*)a.dbias)[(int64_t)b * a.heads + head] = (T)t;
+  }
+}
+
+template <typename T, int DP, bool kBias>
+__global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
+  using Shape = DkvShape<T, DP>;
+  constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
+  constexpr int kTileN = kTile * lds_row<T, DP>();
+  constexpr bool kScaled = __is_same(T, f16);
+  extern __shared__ __align__(16) uint8_t smem[];
+  if (kBias && (int)blockIdx.x >= a.nitems) {
+    reduce_bias<T>(a, blockIdx.x - a.nitems, (float*)smem);
+    return;
+  }
+  T* s_q = (T*)smem;
+  T* s_do = s_q + Shape::kBufs * kTileN;
+  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][lse2, D, table offset, pos][row]
+  float* s_bias = (float*)(smem + Shape::kBytes);
+  const AttnItem it = a.items[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int G = a.G, d = a.d, vec = a.vec, shift = it.nk - it.nq;
+  const float scale2 = a.scale * kLog2e;
+  const int key0 = it.row + wave * 32, key = key0 + (lane & 31);
+  const bool wave_live = key0 < it.nk;
+  const bool there = key < it.nk;
+  const bool live = there && (!a.key_mask || a.key_mask[it.k0 + key] != 0);
+
+  Stage<T, DP, kTile> st_q, st_do;
+  float row_lse = 0.f, row_d = 0.f;
+  int row_off = 0, row_pos = 0;
+  auto fetch = [&](int base) {
+    // a row that saw no key is zeros whatever it holds
+    auto seen = [&](int r) {
+      if (r >= it.hi) return false;
+      const int tok = G == 1 ? r : r / G;
+      return a.lse[(it.q0 + tok) * a.heads + it.kvh * G + (r - tok * G)] != -INFINITY;
+    };
+    st_q.load([&](int i) { return seen(base + i)
+                                      ? (const T*)a.q.data + row_at(a.q, it.q0, it.kvh, G, base + i)
+                                      : nullptr; },
+              d, vec);
+    st_do.load([&](int i) { return seen(base + i) ? (const T*)a.dout.data +
+                                                        row_at(a.dout, it.q0, it.kvh, G, base + i)
+                                                  : nullptr; },
+               d, vec);
+    if (threadIdx.x < kTile) {
+      const int r = base + threadIdx.x;
+      row_lse = INFINITY;
+      row_d = 0.f;
+      row_off = row_pos = 0;
+      if (r < it.hi) {
+        const int tok = G == 1 ? r : r / G, g = r - tok * G;
+        const int64_t at = (it.q0 + tok) * a.heads + it.kvh * G + g;
+        const float lse = a.lse[at];
+        if (lse != -INFINITY) row_lse = lse * kLog2e;
+        row_d = a.dsum[at];
+        row_pos = tok + shift;
+        if (kBias) row_off = g * a.span;
+      }
+    }
+  };
+  auto put = [&](int b) {
+    st_q.store(s_q + b * kTileN);
+    st_do.store(s_do + b * kTileN);
+    if (threadIdx.x < kTile) {
+      float* p = s_row + b * 4 * kTile + threadIdx.x;
+      p[0] = row_lse;
+      p[kTile] = row_d;
+      ((int*)p)[2 * kTile] = row_off;
+      ((int*)p)[3 * kTile] = row_pos;
+    }
+  };
+  if (it.lo < it.hi) fetch(it.lo);
+
+  vec8<T> k[DP / 16], v[DP / 16];
+  {
+    const int64_t tok = it.k0 + (live ? key : 0);
+    load_frags<T, DP>((const T*)a.k.data + tok * a.k.token_stride + it.kvh * a.k.head_stride, live,
+                      d, vec, h, k);
+    load_frags<T, DP>((const T*)a.v.data + tok * a.v.token_stride + it.kvh * a.v.head_stride, live,
+                      d, vec, h, v);
+  }
+  if constexpr (kBias) load_bias<T>(a, it.kvh, s_bias);
+  float up = 1.f;  // dS is rounded times this, and P times 2^14 (f16 only)
+  if constexpr (kScaled) {
+    float most = 0.f;
+    const float* p = a.part_max + (int64_t)it.kvh * a.row_tiles + it.tile0;
+    for (int i = lane; i < it.ntiles; i += 64) most = fmaxf(most, p[i]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    const int e = most > 0.f && most < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
+    up = __builtin_amdgcn_ldexpf(1.f, e < 40 ? e : 40);
+  }
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = f32x16{};
+
+  int buf = 0;
+  if (it.lo < it.hi) put(0);
+  __syncthreads();
+  for (int base = it.lo; base < it.hi; base += kTile) {
+    const bool more = base + kTile < it.hi;
+    if (more) fetch(base + kTile);
+    if (wave_live) {
+      const T* sq = s_q + buf * kTileN;
+      const T* sd = s_do + buf * kTileN;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const int first = base + 32 * b;
+        const int last = (first + 31 < it.hi ? first + 31 : it.hi - 1);
+        if (first >= it.hi) continue;
+        const int pos_min = first / G + shift, pos_max = last / G + shift;
+        if (a.causal && pos_max < key0) continue;
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) {
+          s = mma(frag_along<T, DP>(sq, 32 * b + (lane & 31), c, h), k[c], s);
+          dp = mma(frag_along<T, DP>(sd, 32 * b + (lane & 31), c, h), v[c], dp);
+        }
+        const float* rows = s_row + buf * 4 * kTile + 32 * b + 4 * h;
+        f32x4 lse[4], dsum[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          lse[g] = *(const f32x4*)(rows + 8 * g);
+          dsum[g] = *(const f32x4*)(rows + kTile + 8 * g);
+        }
+        if constexpr (kBias) {
+          const int dist = a.distance;
+          if (G == 1 && (key0 - pos_max >= dist || key0 + 31 - pos_min <= -dist)) {
+            const float far = s_bias[key0 > pos_min ? a.span - 1 : 0];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = s[r] * scale2 + far;
+          } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const i32x4 off = *(const i32x4*)(rows + 2 * kTile + 8 * g);
+              const i32x4 pos = *(const i32x4*)(rows + 3 * kTile + 8 * g);
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                int rel = key - pos[t];
+                rel = rel < -dist ? -dist : rel > dist ? dist : rel;
+                s[4 * g + t] = s[4 * g + t] * scale2 + s_bias[off[t] + rel + dist + kAttnPad];
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= scale2;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(s[r] - lse[r >> 2][r & 3]);
+          dp[r] -= dsum[r >> 2][r & 3];
+        }
+        if (a.causal && pos_min < key0 + 31) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const i32x4 pos = *(const i32x4*)(rows + 3 * kTile + 8 * g);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (key > pos[t]) s[4 * g + t] = dp[4 * g + t] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dp[r] *= s[r];
+          if constexpr (kScaled) {
+            dp[r] *= up;
+            s[r] *= 0x1p14f;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const vec8<T> p = frag_of<T>(s, c), ds = frag_of<T>(dp, c);
+#pragma unroll
+          for (int e = 0; e < DP / 32; ++e) {
+            dv[e] = mma(frag_across<T, DP>(sd, 32 * b + 16 * c, 32 * e, lane), p, dv[e]);
+            dk[e] = mma(frag_across<T, DP>(sq, 32 * b + 16 * c, 32 * e, lane), ds, dk[e]);
+          }
+        }
+      }
+    }
+    if (Shape::kBufs == 1) __syncthreads();
+    if (more) {
+      buf ^= Shape::kBufs - 1;
+      put(buf);
+      __syncthreads();
+    }
+  }
+  if (!there) return;
+  if (!live) {
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = f32x16{};
+  }
+  const int64_t tok = it.k0 + key;
+  store_row<T, DP>((T*)a.dk.data + tok * a.dk.token_stride + it.kvh * a.dk.head_stride, dk,
+                   a.scale / up, d, vec, h);
+  store_row<T, DP>((T*)a.dv.data + tok * a.dv.token_stride + it.kvh * a.dv.head_stride, dv,
+                   kScaled ? 0x1p-14f : 1.f, d, vec, h);
+}
+
+// ---- launch ----------------------------------------------------------------------------------
+
+constexpr int kMaxLds = 160 * 1024;
+
+template <typename K>
+hipError_t launch(K kernel, const AttnArgs& a, int grid, size_t lds, hipStream_t s) {
+  if (lds > kMaxLds) return hipErrorInvalidValue;
+  if (lds > 64 * 1024) {  // more has to be asked for, once for each kernel
+    const hipError_t e = hipFuncSetAttribute(
+        (const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<grid, kAttnThreads, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t launch_dp(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
+  const size_t table = a.bias ? (size_t)a.G * a.span * sizeof(float) : 0;
+  switch (kind) {
+    case kAttnFwd: {
+      const size_t lds = FwdShape<T, DP, 1>::kBytes + table;
+      return a.bias ? launch(attn_forward_kernel<T, DP, 1, true>, a, grid, lds, s)
+                    : launch(attn_forward_kernel<T, DP, 1, false>, a, grid, lds, s);
+    }
+    case kAttnFwdFew: {
+      const size_t lds = FwdShape<T, DP, 4>::kBytes + table;
+      return a.bias ? launch(attn_forward_kernel<T, DP, 4, true>, a, grid, lds, s)
+                    : launch(attn_forward_kernel<T, DP, 4, false>, a, grid, lds, s);
+    }
+    case kAttnJoin:
+      return launch(attn_join_kernel<T, DP, kAttnRows>, a, grid, 0, s);
+    case kAttnJoinFew:
+      return launch(attn_join_kernel<T, DP, kAttnFewRows>, a, grid, 0, s);
+    case kAttnDq: {
+      const size_t sums =
+          a.dbias ? kSums * table + (kAttnThreads / 64) * 64 * 2 * sizeof(float) : 0;
+      const size_t lds = DqShape<T, DP>::kBytes + table + sums;
+      return a.bias ? launch(attn_dq_kernel<T, DP, true>, a, grid, lds, s)
+                    : launch(attn_dq_kernel<T, DP, false>, a, grid, lds, s);
+    }
+    case kAttnDkv: {
+      const size_t lds = DkvShape<T, DP>::kBytes + table;
+      return a.bias ? launch(attn_dkv_kernel<T, DP, true>, a, grid, lds, s)
+                    : launch(attn_dkv_kernel<T, DP, false>, a, grid, lds, s);
+    }
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t launch_type(AttnKind kind, int dp, const AttnArgs& a, int grid, hipStream_t s) {
+  if (grid <= 0) return hipSuccess;
+  switch (dp) {
+    case 32: return launch_dp<T, 32>(kind, a, grid, s);
+    case 64: return launch_dp<T, 64>(kind, a, grid, s);
+    case 128: return launch_dp<T, 128>(kind, a, grid, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+}  // namespace sieve

@@ -1,0 +1,511 @@
+// norm.hip -- layer norm over rows, forward and backward, with the residual sum
+// in front of it and the reduction of the weights' gradients.
+//
+//   h = x + residual, u = (h - mean) rstd, y = u w + b
+//   g = dy w, dx = rstd (g - mean(g) - u mean(g u)) + dh
+//   dw = sum_rows dy u, db = sum_rows dy
+//
+// Each value is read once and written once, so memory bounds every kernel here.
+// A row stays in the registers of one wave (up to 2,048 values) or one work-group
+// (up to 8,192): the mean is taken first and the variance from the differences, in
+// fp32 without the cancellation of a sum of squares.  Longer rows are read again,
+// from the L2, by the looping kernels.
+//
+// The weights' gradients: a thread owns the same columns of every row its wave
+// takes, so it sums them in registers; the work-group's waves add up through LDS,
+// each work-group writes one partial row, and a second kernel adds those in a fixed
+// order.  No atomics: equal calls give equal bits.
+#include "enc_common.h"
+
+using namespace sieve;
+
+namespace {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxN = 65536;
+constexpr int kBigThreads = 1024;
+constexpr int kMaxParts = 1024;  // work-groups of the backward pass: 4 a CU
+
+struct NormFwd {
+  const void *x, *residual, *w, *b;
+  int64_t x_stride, r_stride, rows;
+  int n;
+  float eps;
+  void *y, *h;
+  float *mean, *rstd;
+};
+
+struct NormBwd {
+  const void *dy, *h, *w, *dh;
+  const float *mean, *rstd;
+  int64_t dy_stride, h_stride, rows;
+  int n;
+  void *dx, *dw, *db;
+  float* part;  // [work-group][2][n]; null where there is one work-group
+};
+
+// Column of value e of a thread: 8 neighbours at a time (16-byte moves), or, where
+// the rows are not aligned, one neighbour a thread.
+template <int NT, bool kVec>
+__device__ __forceinline__ int column(int e, int t) {
+  return kVec ? ((e >> 3) * NT + t) * 8 + (e & 7) : e * NT + t;
+}
+
+// Values of a row; 0 past its end.
+template <typename T, int NE, int NT, bool kVec>
+__device__ __forceinline__ void load_row(const T* p, int n, int t, float (&v)[NE]) {
+  if constexpr (kVec) {
+#pragma unroll
+    for (int c = 0; c < NE / 8; ++c) {
+      const int col = (c * NT + t) * 8;
+      if (col < n) {
+        const EncVec<T, 8> q = enc_load<T, 8>(p + col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[c * 8 + j] = (float)q.v[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[c * 8 + j] = 0.f;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      const int col = e * NT + t;
+      v[e] = col < n ? (float)p[col] : 0.f;
+    }
+  }
+}
+
+template <typename T, int NE, int NT, bool kVec>
+__device__ __forceinline__ void store_row(T* p, int n, int t, const float (&v)[NE]) {
+  if constexpr (kVec) {
+#pragma unroll
+    for (int c = 0; c < NE / 8; ++c) {
+      const int col = (c * NT + t) * 8;
+      if (col < n) {
+        EncVec<T, 8> q;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q.v[j] = (T)v[c * 8 + j];
+        enc_store<T, 8>(p + col, q);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      const int col = e * NT + t;
+      if (col < n) p[col] = (T)v[e];
+    }
+  }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// Sums over the threads of a row: a wave's, or the work-group's through LDS.
+template <int NT>
+__device__ __forceinline__ float row_sum(float v, float* s) {
+  v = wave_sum(v);
+  if constexpr (NT > 64) {
+    __syncthreads();  // the previous sum has been read
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v += s[i];
+  }
+  return v;
+}
+
+template <int NT>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float* s) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+      s[(threadIdx.x >> 6) * 2] = a;
+      s[(threadIdx.x >> 6) * 2 + 1] = b;
+    }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) {
+      a += s[i * 2];
+      b += s[i * 2 + 1];
+    }
+  }
+}
+
+template <typename T, typename W, int NE, int NT, bool kVec>
+__global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormFwd a) {
+  __shared__ float s_sum[kWaves];
+  const int t = threadIdx.x % NT;
+  constexpr int kRows = kThreads / NT;  // rows of a work-group at a time
+  const int n = a.n;
+  const float inv = 1.f / (float)n;
+  float w[NE], b[NE];
+  load_row<W, NE, NT, kVec>((const W*)a.w, n, t, w);
+  if (a.b) {
+    load_row<W, NE, NT, kVec>((const W*)a.b, n, t, b);
+  } else {
+#pragma unroll
+    for (int e = 0; e < NE; ++e) b[e] = 0.f;
+  }
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT; row < a.rows;
+       row += (int64_t)gridDim.x * kRows) {
+    float v[NE];
+    load_row<T, NE, NT, kVec>((const T*)a.x + row * a.x_stride, n, t, v);
+    if (a.residual) {
+      float r[NE];
+      load_row<T, NE, NT, kVec>((const T*)a.residual + row * a.r_stride, n, t, r);
+      // the sum is rounded to the activations' type: the backward pass and the next
+      // layer read it in that type, and the norm is of what they read
+#pragma unroll
+      for (int e = 0; e < NE; ++e) v[e] = (float)(T)(v[e] + r[e]);
+      store_row<T, NE, NT, kVec>((T*)a.h + row * n, n, t, v);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) sum += v[e];
+    const float mean = row_sum<NT>(sum, s_sum) * inv;
+    float sq = 0.f;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      v[e] = column<NT, kVec>(e, t) < n ? v[e] - mean : 0.f;
+      sq += v[e] * v[e];
+    }
+    const float rstd = 1.f / sqrtf(row_sum<NT>(sq, s_sum) * inv + a.eps);
+#pragma unroll
+    for (int e = 0; e < NE; ++e) v[e] = v[e] * rstd * w[e] + b[e];
+    store_row<T, NE, NT, kVec>((T*)a.y + row * n, n, t, v);
+    if (t == 0 && a.mean) {
+      a.mean[row] = mean;
+      a.rstd[row] = rstd;
+    }
+  }
+}
+
+template <typename T, typename W, int NE, int NT, bool kVec>
+__global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
+  __shared__ float s_sum[2 * kWaves];
+  // one wave's columns at a time go through LDS to the work-group's sum
+  __shared__ float s_cols[NT == 64 ? kWaves * 64 * 8 : 1];
+  const int t = threadIdx.x % NT;
+  constexpr int kRows = kThreads / NT;
+  const int n = a.n;
+  const float inv = 1.f / (float)n;
+  float w[NE], dw[NE], db[NE];
+  load_row<W, NE, NT, kVec>((const W*)a.w, n, t, w);
+#pragma unroll
+  for (int e = 0; e < NE; ++e) dw[e] = db[e] = 0.f;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT; row < a.rows;
+       row += (int64_t)gridDim.x * kRows) {
+    float u[NE], g[NE];
+    load_row<T, NE, NT, kVec>((const T*)a.h + row * a.h_stride, n, t, u);
+    load_row<T, NE, NT, kVec>((const T*)a.dy + row * a.dy_stride, n, t, g);
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float sg = 0.f, sgu = 0.f;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      u[e] = column<NT, kVec>(e, t) < n ? (u[e] - mean) * rstd : 0.f;
+      dw[e] += g[e] * u[e];
+      db[e] += g[e];
+      g[e] *= w[e];
+      sg += g[e];
+      sgu += g[e] * u[e];
+    }
+    row_sum2<NT>(sg, sgu, s_sum);
+    sg *= inv;
+    sgu *= inv;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) g[e] = rstd * (g[e] - sg - u[e] * sgu);
+    if (a.dh) {
+      load_row<T, NE, NT, kVec>((const T*)a.dh + row * n, n, t, u);
+#pragma unroll
+      for (int e = 0; e < NE; ++e) g[e] += u[e];
+    }
+    store_row<T, NE, NT, kVec>((T*)a.dx + row * n, n, t, g);
+  }
+  if (!a.dw && !a.db) return;
+  if constexpr (NT == 64) {
+    // the waves of the work-group, 8 of a thread's columns at a time, in wave order
+    const int wave = threadIdx.x / 64;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+#pragma unroll
+      for (int c = 0; c < NE / 8; ++c) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          s_cols[(wave * 8 + j) * 64 + t] = part ? db[c * 8 + j] : dw[c * 8 + j];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float v = 0.f;
+#pragma unroll
+            for (int q = 0; q < kWaves; ++q) v += s_cols[(q * 8 + j) * 64 + t];
+            (part ? db : dw)[c * 8 + j] = v;
+          }
+        }
+      }
+    }
+    if (wave) return;
+  }
+  if (a.part) {
+    float* p = a.part + (int64_t)blockIdx.x * 2 * n;
+    store_row<float, NE, NT, kVec>(p, n, t, dw);
+    store_row<float, NE, NT, kVec>(p + n, n, t, db);
+  } else {
+    if (a.dw) store_row<W, NE, NT, kVec>((W*)a.dw, n, t, dw);
+    if (a.db) store_row<W, NE, NT, kVec>((W*)a.db, n, t, db);
+  }
+}
+
+// Rows too long for the registers: a work-group a row, the row read once a step.
+template <typename T, typename W>
+__global__ __launch_bounds__(kBigThreads) void norm_forward_big_kernel(NormFwd a) {
+  __shared__ float s_sum[kBigThreads / 64];
+  const int t = threadIdx.x, n = a.n;
+  const float inv = 1.f / (float)n;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* h = (const T*)a.x + row * a.x_stride;
+    float sum = 0.f;
+    if (a.residual) {
+      const T* x = h;
+      const T* r = (const T*)a.residual + row * a.r_stride;
+      T* to = (T*)a.h + row * n;
+      for (int c = t; c < n; c += kBigThreads) {
+        const T v = (T)((float)x[c] + (float)r[c]);
+        to[c] = v;  // read again below by this thread alone
+        sum += (float)v;
+      }
+      h = to;
+    } else {
+      for (int c = t; c < n; c += kBigThreads) sum += (float)h[c];
+    }
+    const float mean = row_sum<kBigThreads>(sum, s_sum) * inv;
+    float sq = 0.f;
+    for (int c = t; c < n; c += kBigThreads) {
+      const float d = (float)h[c] - mean;
+      sq += d * d;
+    }
+    const float rstd = 1.f / sqrtf(row_sum<kBigThreads>(sq, s_sum) * inv + a.eps);
+    T* y = (T*)a.y + row * n;
+    for (int c = t; c < n; c += kBigThreads)
+      y[c] = (T)(((float)h[c] - mean) * rstd * (float)((const W*)a.w)[c] +
+                 (a.b ? (float)((const W*)a.b)[c] : 0.f));
+    if (t == 0 && a.mean) {
+      a.mean[row] = mean;
+      a.rstd[row] = rstd;
+    }
+  }
+}
+
+// As above; the columns' sums stay in the work-group's partial row, which a thread
+// reads and writes at its own columns only.
+template <typename T, typename W>
+__global__ __launch_bounds__(kBigThreads) void norm_backward_big_kernel(NormBwd a) {
+  __shared__ float s_sum[2 * kBigThreads / 64];
+  const int t = threadIdx.x, n = a.n;
+  const float inv = 1.f / (float)n;
+  float* part = a.part + (int64_t)blockIdx.x * 2 * n;
+  for (int c = t; c < 2 * n; c += kBigThreads) part[c] = 0.f;
+  __syncthreads();
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* h = (const T*)a.h + row * a.h_stride;
+    const T* dy = (const T*)a.dy + row * a.dy_stride;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float sg = 0.f, sgu = 0.f;
+    for (int c = t; c < n; c += kBigThreads) {
+      const float u = ((float)h[c] - mean) * rstd, d = (float)dy[c];
+      const float g = d * (float)((const W*)a.w)[c];
+      part[c] += d * u;
+      part[n + c] += d;
+      sg += g;
+      sgu += g * u;
+    }
+    row_sum2<kBigThreads>(sg, sgu, s_sum);
+    sg *= inv;
+    sgu *= inv;
+    T* dx = (T*)a.dx + row * n;
+    const T* dh = a.dh ? (const T*)a.dh + row * n : nullptr;
+    for (int c = t; c < n; c += kBigThreads) {
+      const float u = ((float)h[c] - mean) * rstd;
+      const float g = (float)dy[c] * (float)((const W*)a.w)[c];
+      dx[c] = (T)(rstd * (g - sg - u * sgu) + (dh ? (float)dh[c] : 0.f));
+    }
+  }
+}
+
+// Adds the partial rows: a work-group takes 32 of the 2 n columns, its 32 groups of 32
+// threads every 32nd row each, and LDS adds the groups in order.
+template <typename W>
+__global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restrict__ part,
+                                                           int parts, int n, W* dw, W* db) {
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int64_t col = (int64_t)blockIdx.x * 32 + c;
+  float v = 0.f;
+  if (col < 2 * n)
+    for (int p = g; p < parts; p += 32) v += part[(int64_t)p * 2 * n + col];
+  s[g][c] = v;
+  __syncthreads();
+  if (g == 0 && col < 2 * n) {
+    v = 0.f;
+    for (int i = 0; i < 32; ++i) v += s[i][c];
+    if (col < n) {
+      if (dw) dw[col] = (W)v;
+    } else if (db) {
+      db[col - n] = (W)v;
+    }
+  }
+}
+
+// Work-groups of the backward pass: 4 rows a work-group at a time where a wave holds a
+// row.  A multiple of that many rows each evens the waves' loads.
+int backward_groups(int64_t rows, int n) {
+  const int at_a_time = n <= 2048 ? kWaves : 1;
+  const int64_t steps = (rows + at_a_time - 1) / at_a_time;
+  return (int)(steps < kMaxParts ? (steps > 0 ? steps : 1) : kMaxParts);
+}
+
+template <typename T, typename W, int NE, int NT, bool kVec>
+void forward_on(const NormFwd& a, hipStream_t s) {
+  constexpr int kRows = kThreads / NT;
+  const int64_t want = (a.rows + kRows - 1) / kRows;
+  const int grid = (int)(want < 8192 ? want : 8192);
+  norm_forward_kernel<T, W, NE, NT, kVec><<<grid, kThreads, 0, s>>>(a);
+}
+
+template <typename T, typename W>
+void forward_typed(const NormFwd& a, bool vec, hipStream_t s) {
+  const int n = a.n;
+#define GO(NE, NT)                                                 \
+  return vec ? forward_on<T, W, NE, NT, true>(a, s) : forward_on<T, W, NE, NT, false>(a, s)
+  if (n <= 512) GO(8, 64);
+  if (n <= 1024) GO(16, 64);
+  if (n <= 2048) GO(32, 64);
+  if (n <= 4096) GO(16, 256);
+  if (n <= 8192) GO(32, 256);
+#undef GO
+  const int grid = (int)(a.rows < 4096 ? a.rows : 4096);
+  norm_forward_big_kernel<T, W><<<grid, kBigThreads, 0, s>>>(a);
+}
+
+template <typename T, typename W>
+void backward_typed(const NormBwd& a, bool vec, int groups, hipStream_t s) {
+  const int n = a.n;
+#define GO(NE, NT)                                                                     \
+  vec ? norm_backward_kernel<T, W, NE, NT, true><<<groups, kThreads, 0, s>>>(a)        \
+      : norm_backward_kernel<T, W, NE, NT, false><<<groups, kThreads, 0, s>>>(a)
+  if (n <= 512) GO(8, 64);
+  else if (n <= 1024) GO(16, 64);
+  else if (n <= 2048) GO(32, 64);
+  else if (n <= 4096) GO(16, 256);
+  else if (n <= 8192) GO(32, 256);
+  else norm_backward_big_kernel<T, W><<<groups, kBigThreads, 0, s>>>(a);
+#undef GO
+  if (a.part && (a.dw || a.db))
+    norm_reduce_kernel<W><<<(2 * n + 31) / 32, 1024, 0, s>>>(a.part, groups, n, (W*)a.dw,
+                                                             (W*)a.db);
+}
+
+int check_norm(int32_t dtype, int32_t wdtype, int64_t rows, int32_t n) {
+  if (!enc_dtype_ok(dtype)) return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16", dtype);
+  if (wdtype != dtype && wdtype != SIEVE_F32)
+    return set_error(SIEVE_EINVAL, "wdtype = %d must be dtype or SIEVE_F32", wdtype);
+  if (rows < 0) return set_error(SIEVE_EINVAL, "rows is negative");
+  if (n < 1) return set_error(SIEVE_EINVAL, "n = %d must be >= 1", n);
+  if (n > kMaxN) return set_error(SIEVE_EUNSUPPORTED, "n = %d is above %d", n, kMaxN);
+  return SIEVE_OK;
+}
+
+bool vec_ok(const void* p, int64_t stride, int size) {
+  return ((uintptr_t)p & 15) == 0 && (stride * size & 15) == 0;
+}
+
+template <typename F>
+void by_type(int32_t dtype, int32_t wdtype, F f) {
+  if (dtype == SIEVE_F32) f(float{}, float{});
+  else if (dtype == SIEVE_F16 && wdtype == SIEVE_F16) f(f16{}, f16{});
+  else if (dtype == SIEVE_F16) f(f16{}, float{});
+  else if (wdtype == SIEVE_BF16) f(bf16{}, bf16{});
+  else f(bf16{}, float{});
+}
+
+}  // namespace
+
+SIEVE_API int sieve_norm_forward(const void* x, int64_t x_stride, const void* residual,
+                                 int64_t residual_stride, const void* weight, const void* bias,
+                                 int32_t dtype, int32_t wdtype, int64_t rows, int32_t n, float eps,
+                                 void* y, void* h, float* mean, float* rstd, void* stream) {
+  clear_error();
+  if (int st = check_norm(dtype, wdtype, rows, n)) return st;
+  if (!(eps >= 0.f)) return set_error(SIEVE_EINVAL, "eps must be >= 0");
+  if (rows == 0) return SIEVE_OK;
+  if (!x || !weight || !y) return set_error(SIEVE_EINVAL, "x, weight and y must be non-NULL");
+  if ((residual != nullptr) != (h != nullptr))
+    return set_error(SIEVE_EINVAL, "h is given with a residual, and only then");
+  if ((mean != nullptr) != (rstd != nullptr))
+    return set_error(SIEVE_EINVAL, "mean and rstd are given together");
+  if (x_stride < n || (residual && residual_stride < n))
+    return set_error(SIEVE_EINVAL, "a row stride is below n = %d", n);
+  if (h && h == y) return set_error(SIEVE_EINVAL, "y and h are the same buffer");
+  const int sz = enc_size(dtype), wsz = enc_size(wdtype);
+  const bool vec = n % 8 == 0 && vec_ok(x, x_stride, sz) && vec_ok(y, n, sz) &&
+                   vec_ok(weight, n, wsz) && (!bias || vec_ok(bias, n, wsz)) &&
+                   (!residual || (vec_ok(residual, residual_stride, sz) && vec_ok(h, n, sz)));
+  const NormFwd a{x, residual, weight, bias, x_stride, residual_stride, rows, n, eps,
+                  y, h, mean, rstd};
+  by_type(dtype, wdtype, [&](auto t, auto w) {
+    forward_typed<decltype(t), decltype(w)>(a, vec, (hipStream_t)stream);
+  });
+  ENC_HIP_TRY(hipGetLastError());
+  return SIEVE_OK;
+}
+
+SIEVE_API int64_t sieve_norm_workspace(int64_t rows, int32_t n) {
+  clear_error();
+  if (int st = check_norm(SIEVE_F32, SIEVE_F32, rows, n)) return st;
+  const int groups = backward_groups(rows, n);
+  return groups == 1 && n <= 8192 ? 0 : (int64_t)groups * 2 * n * (int64_t)sizeof(float);
+}
+
+SIEVE_API int sieve_norm_backward(const void* dy, int64_t dy_stride, const void* h,
+                                  int64_t h_stride, const void* weight, const float* mean,
+                                  const float* rstd, const void* dh, int32_t dtype,
+                                  int32_t wdtype, int64_t rows, int32_t n, void* dx, void* dweight,
+                                  void* dbias, void* workspace, int64_t workspace_bytes,
+                                  void* stream) {
+  clear_error();
+  if (int st = check_norm(dtype, wdtype, rows, n)) return st;
+  if (!weight) return set_error(SIEVE_EINVAL, "weight must be non-NULL");
+  if (rows > 0 && (!dy || !h || !mean || !rstd || !dx))
+    return set_error(SIEVE_EINVAL, "dy, h, mean, rstd and dx must be non-NULL when rows > 0");
+  if (rows > 0 && (dy_stride < n || h_stride < n))
+    return set_error(SIEVE_EINVAL, "a row stride is below n = %d", n);
+  const int64_t need = sieve_norm_workspace(rows, n);
+  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
+    return set_error(SIEVE_EINVAL, "workspace must be 16-byte aligned and hold %lld bytes",
+                     (long long)need);
+  const int sz = enc_size(dtype), wsz = enc_size(wdtype);
+  const bool vec = n % 8 == 0 && vec_ok(dy, dy_stride, sz) && vec_ok(h, h_stride, sz) &&
+                   vec_ok(weight, n, wsz) && vec_ok(dx, n, sz) && vec_ok(dweight, n, wsz) &&
+                   vec_ok(dbias, n, wsz) && (!dh || vec_ok(dh, n, sz));
+  const NormBwd a{dy, h, weight, dh, mean, rstd, dy_stride, h_stride, rows, n, dx, dweight, dbias,
+                  need > 0 ? (float*)workspace : nullptr};
+  const int groups = backward_groups(rows, n);
+  by_type(dtype, wdtype, [&](auto t, auto w) {
+    backward_typed<decltype(t), decltype(w)>(a, vec, groups, (hipStream_t)stream);
+  });
+  ENC_HIP_TRY(hipGetLastError());
+  return SIEVE_OK;
+}

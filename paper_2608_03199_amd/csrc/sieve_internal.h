@@ -9,6 +9,11 @@
 
 namespace sieve {
 
+// The calling thread's error message (sieve_last_error): set_error formats it
+// and returns code.
+void clear_error();
+int set_error(int code, const char* fmt, ...);
+
 // One ready item (q_i, j) of Sec. 4.2: query index and 0-based probe rank.
 struct Item {
   int32_t q;

@@ -1,0 +1,408 @@
+"""Text-encoder operators of libsieve: layer norm and packed attention with a learned
+relative position bias, forward and backward (``include/sieve.h``).
+
+The ``*_forward`` / ``*_backward`` functions and ``AttentionPlan``'s methods marshal arguments
+of single kernels' calls; ``layer_norm`` and ``attention`` join them for torch's autograd.  All
+calls are asynchronous on the given or current stream.  Outputs and workspace come from torch's
+allocator on that stream; there is no CPU fallback.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+import math
+from typing import Optional, Tuple
+
+import torch
+
+from . import F16, F32, SieveError, _check, load_library
+
+__all__ = ["AttentionPlan", "BF16", "attention", "layer_norm", "layer_norm_backward",
+           "layer_norm_forward"]
+
+BF16 = 2
+_CODES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
+class _Desc(ctypes.Structure):
+    """Mirror of ``sieve_attn_desc``."""
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("num_buckets", ctypes.c_int32),
+                ("max_distance", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("nseq", ctypes.c_int64), ("q_offsets", ctypes.c_void_p),
+                ("k_offsets", ctypes.c_void_p)]
+
+
+class _Heads(ctypes.Structure):
+    """Mirror of ``sieve_heads``."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+_ready = None
+
+
+def _library():
+    global _ready
+    if _ready is not None:
+        return _ready
+    lib = load_library()
+    P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    H = ctypes.POINTER(_Heads)
+    lib.sieve_norm_forward.restype = ctypes.c_int
+    lib.sieve_norm_forward.argtypes = [P, i64, P, i64, P, P, i32, i32, i64, i32, f32, P, P, P, P, P]
+    lib.sieve_norm_backward.restype = ctypes.c_int
+    lib.sieve_norm_backward.argtypes = [P, i64, P, i64, P, P, P, P, i32, i32, i64, i32, P, P, P, P,
+                                        i64, P]
+    lib.sieve_norm_workspace.restype = i64
+    lib.sieve_norm_workspace.argtypes = [i64, i32]
+    lib.sieve_attn_create.restype = ctypes.c_int
+    lib.sieve_attn_create.argtypes = [ctypes.POINTER(_Desc), P, ctypes.POINTER(P)]
+    lib.sieve_attn_free.restype = None
+    lib.sieve_attn_free.argtypes = [P]
+    lib.sieve_attn_workspace.restype = i64
+    lib.sieve_attn_workspace.argtypes = [P, i32]
+    lib.sieve_attn_forward.restype = ctypes.c_int
+    lib.sieve_attn_forward.argtypes = [P, H, H, H, P, P, H, P, P, i64, P]
+    lib.sieve_attn_backward.restype = ctypes.c_int
+    lib.sieve_attn_backward.argtypes = [P, H, H, H, H, H, P, P, P, H, H, H, P, P, i64, P]
+    _ready = lib
+    return lib
+
+
+def _on(device: torch.device, stream):
+    """The device and the stream that the call's allocations and kernels belong to."""
+    stack = contextlib.ExitStack()
+    stack.enter_context(torch.cuda.device(device))
+    if stream is not None:
+        stack.enter_context(torch.cuda.stream(stream))
+    return stack
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
+def _workspace(lib, size: int, device):
+    if size < 0:
+        _check(lib, int(size))
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _code(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {t.dtype} of {name} (float32, float16 or bfloat16)")
+    return _CODES[t.dtype]
+
+
+def _rows(t: torch.Tensor, n: int) -> torch.Tensor:
+    """[rows, n] with neighbouring values side by side; copied only where that is not a view."""
+    t = t.reshape(-1, n)
+    return t if t.stride(1) == 1 or n == 1 else t.contiguous()
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+# ---- layer norm ---------------------------------------------------------------------------
+
+
+def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                       eps: float = 1e-5, residual: Optional[torch.Tensor] = None, stream=None):
+    """Layer norm over the last axis of ``x`` (+ ``residual``).  Returns ``(y, h, mean, rstd)``:
+    ``h`` is the sum that was normed (``x`` itself without a residual), ``mean`` and ``rstd`` are
+    fp32, one a row.  ``weight`` and ``bias`` are of x's dtype or float32."""
+    _need(x.is_cuda, "x must be a GPU tensor")
+    _need(x.dim() >= 1 and x.shape[-1] >= 1, "x must have a last axis of at least one value")
+    n = int(x.shape[-1])
+    code = _code(x, "x")
+    _check_affine(x, weight, bias, n)
+    if residual is not None:
+        _need(residual.shape == x.shape and residual.dtype == x.dtype and
+              residual.device == x.device, "residual must match x")
+    lib = _library()
+    with _on(x.device, stream):
+        s = torch.cuda.current_stream().cuda_stream
+        xr = _rows(x, n)
+        rr = _rows(residual, n) if residual is not None else None
+        w, b = weight.contiguous(), None if bias is None else bias.contiguous()
+        rows = xr.shape[0]
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        h = torch.empty_like(y) if rr is not None else None
+        stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+        mean, rstd = stats[0], stats[1]
+        if rows:
+            if _row_overlap(xr):
+                xr = xr.contiguous()
+            if rr is not None and _row_overlap(rr):
+                rr = rr.contiguous()
+            _check(lib, lib.sieve_norm_forward(
+                xr.data_ptr(), _row_stride(xr), _ptr(rr), 0 if rr is None else _row_stride(rr),
+                w.data_ptr(), _ptr(b), code, _CODES[w.dtype], rows, n, float(eps), y.data_ptr(),
+                _ptr(h), mean.data_ptr(), rstd.data_ptr(), s))
+    return y, x if h is None else h, mean, rstd
+
+
+def _row_overlap(t: torch.Tensor) -> bool:
+    """Rows closer than their length (an expanded tensor): the kernels take none such."""
+    return t.shape[0] > 1 and t.stride(0) < t.shape[1]
+
+
+def _check_affine(x, weight, bias, n):
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is None:
+            continue
+        _need(t.shape == (n,) and t.device == x.device, f"{name} must be [{n}] on x's device")
+        if t.dtype not in (x.dtype, torch.float32):
+            raise TypeError(f"{name} must be of x's dtype or float32")
+    if bias is not None and bias.dtype != weight.dtype:
+        raise TypeError("weight and bias must share a dtype")
+
+
+def layer_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor,
+                        mean: torch.Tensor, rstd: torch.Tensor,
+                        dh: Optional[torch.Tensor] = None, weight_grad: bool = True,
+                        bias_grad: bool = True, stream=None):
+    """Gradients of ``layer_norm_forward`` from its ``h``, ``mean`` and ``rstd``.  ``dh`` is the
+    gradient that reaches ``h`` by another way.  Returns ``(dx, dweight, dbias)``; ``dx`` is the
+    gradient of x and of the residual alike, the other two are None where not asked for."""
+    _need(h.is_cuda, "h must be a GPU tensor")
+    n = int(h.shape[-1]) if h.dim() else 0
+    _need(n >= 1, "h must have a last axis of at least one value")
+    code = _code(h, "h")
+    _check_affine(h, weight, None, n)
+    rows = h.numel() // n
+    for name, t in (("dy", dy), ("dh", dh)):
+        if t is not None:
+            _need(t.shape == h.shape and t.dtype == h.dtype and t.device == h.device,
+                  f"{name} must match h")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _need(t.numel() == rows and t.dtype == torch.float32 and t.device == h.device and
+              t.is_contiguous(), f"{name} must be the forward pass's, one float32 a row")
+    lib = _library()
+    with _on(h.device, stream):
+        s = torch.cuda.current_stream().cuda_stream
+        hr, dr = _rows(h, n), _rows(dy, n)
+        if _row_overlap(hr):
+            hr = hr.contiguous()
+        if _row_overlap(dr):
+            dr = dr.contiguous()
+        er = None if dh is None else dh.contiguous()
+        w = weight.contiguous()
+        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        dw = torch.empty_like(w) if weight_grad else None
+        db = torch.empty_like(w) if bias_grad else None
+        size = lib.sieve_norm_workspace(rows, n)
+        space = _workspace(lib, size, h.device)
+        _check(lib, lib.sieve_norm_backward(
+            _ptr(dr), _row_stride(dr), _ptr(hr), _row_stride(hr), w.data_ptr(), _ptr(mean),
+            _ptr(rstd), _ptr(er), code, _CODES[w.dtype], rows, n, _ptr(dx), _ptr(dw), _ptr(db),
+            _ptr(space), int(size), s))
+    return dx, dw, db
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, residual):
+        y, h, mean, rstd = layer_norm_forward(x, weight, bias, eps, residual)
+        ctx.save_for_backward(h, weight, mean, rstd)
+        ctx.has_bias, ctx.has_residual = bias is not None, residual is not None
+        if ctx.has_residual:
+            return y, h
+        return y
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        h, weight, mean, rstd = ctx.saved_tensors
+        if dy is None:
+            dy = torch.zeros_like(h)
+        dx, dw, db = layer_norm_backward(dy, h, weight, mean, rstd, dh, ctx.needs_input_grad[1],
+                                         ctx.has_bias and ctx.needs_input_grad[2])
+        return dx, dw, db, None, dx if ctx.has_residual else None
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, residual: Optional[torch.Tensor] = None):
+    """Differentiable layer norm.  Returns ``y``, or ``(y, x + residual)`` with a residual."""
+    return _LayerNorm.apply(x, weight, bias, eps, residual)
+
+
+# ---- attention ----------------------------------------------------------------------------
+
+
+def _offsets(t, name: str) -> torch.Tensor:
+    t = torch.as_tensor(t)
+    _need(t.dim() == 1 and t.numel() >= 1 and not t.is_floating_point(),
+          f"{name} must be whole numbers, one more than the sequences")
+    return t.to(device="cpu", dtype=torch.int64).contiguous()
+
+
+class AttentionPlan:
+    """The attention of one packed batch (``sieve_attn_create``): sequence ``s`` has the queries
+    ``q_offsets[s] .. q_offsets[s+1]-1`` and the keys ``k_offsets[s] .. k_offsets[s+1]-1``
+    (``q_offsets`` where that is not given).  Queries fewer than the keys are the sequence's last.
+    Every layer and both passes over the batch share the plan.  ``num_buckets`` > 0 adds a
+    learned bias ``[num_buckets, heads]`` by buckets of the relative position."""
+
+    def __init__(self, q_offsets, k_offsets=None, *, heads: int, kv_heads: Optional[int] = None,
+                 head_dim: int, dtype: torch.dtype, causal: bool = False,
+                 scale: Optional[float] = None, num_buckets: int = 0, max_distance: int = 0,
+                 device=None):
+        self._h = None
+        lib = _library()
+        if dtype not in _CODES:
+            raise TypeError(f"unsupported dtype {dtype} (float32, float16 or bfloat16)")
+        qo = _offsets(q_offsets, "q_offsets")
+        ko = qo if k_offsets is None else _offsets(k_offsets, "k_offsets")
+        _need(qo.numel() == ko.numel(), "q_offsets and k_offsets must have as many sequences")
+        self.heads, self.kv_heads = int(heads), int(heads if kv_heads is None else kv_heads)
+        self.head_dim, self.dtype, self.causal = int(head_dim), dtype, bool(causal)
+        self.num_buckets, self.max_distance = int(num_buckets), int(max_distance)
+        self.queries, self.keys = int(qo[-1]), int(ko[-1])
+        _need(self.head_dim >= 1, "head_dim must be at least 1")
+        self.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None \
+            else torch.device(device)
+        desc = _Desc(_CODES[dtype], self.heads, self.kv_heads, self.head_dim, int(self.causal),
+                     self.num_buckets, self.max_distance, self.scale, qo.numel() - 1,
+                     qo.data_ptr(), ko.data_ptr())
+        handle = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(lib, lib.sieve_attn_create(ctypes.byref(desc),
+                                              torch.cuda.current_stream().cuda_stream,
+                                              ctypes.byref(handle)))
+        self._h, self._lib = handle, lib
+        self._space = [int(lib.sieve_attn_workspace(handle, b)) for b in (0, 1)]
+
+    def close(self):
+        if self._h is not None and self._h.value:
+            self._lib.sieve_attn_free(self._h)
+        self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _tensor(self, t: torch.Tensor, name: str, tokens: int, heads: int) -> torch.Tensor:
+        if t.dtype != self.dtype:
+            raise TypeError(f"{name} must be {self.dtype}, not {t.dtype}")
+        _need(t.is_cuda and t.device == self._device(), f"{name} must be on the plan's device")
+        _need(tuple(t.shape) == (tokens, heads, self.head_dim),
+              f"{name} must be [{tokens}, {heads}, {self.head_dim}], not {list(t.shape)}")
+        return t
+
+    def _device(self):
+        d = self.device
+        return d if d.index is not None else torch.device("cuda", 0)
+
+    def _inputs(self, q, k, v, key_mask, bias):
+        if self._h is None:
+            raise SieveError(-1, "the plan is closed")
+        q = self._tensor(q, "q", self.queries, self.heads)
+        k = self._tensor(k, "k", self.keys, self.kv_heads)
+        v = self._tensor(v, "v", self.keys, self.kv_heads)
+        if key_mask is not None:
+            _need(key_mask.dtype in (torch.bool, torch.uint8) and
+                  tuple(key_mask.shape) == (self.keys,) and key_mask.device == q.device,
+                  f"key_mask must be [{self.keys}] bool on the plan's device")
+            key_mask = key_mask.contiguous()
+        _need((bias is not None) == (self.num_buckets > 0),
+              "bias is given with a plan that has buckets, and only then")
+        if bias is not None:
+            if bias.dtype != self.dtype:
+                raise TypeError(f"bias must be {self.dtype}, not {bias.dtype}")
+            _need(tuple(bias.shape) == (self.num_buckets, self.heads) and
+                  bias.device == q.device, f"bias must be [{self.num_buckets}, {self.heads}]")
+            bias = bias.contiguous()
+        return q, k, v, key_mask, bias
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                key_mask: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """``q`` [queries, heads, head_dim], ``k`` and ``v`` [keys, kv_heads, head_dim], any
+        strides with neighbouring values side by side; ``key_mask`` [keys], False: not seen.
+        Returns ``(out, lse)``: the output and the fp32 logarithm of each row's sum."""
+        with _on(self._device(), stream):
+            s = torch.cuda.current_stream().cuda_stream
+            q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
+            out = torch.empty((self.queries, self.heads, self.head_dim), dtype=self.dtype,
+                              device=q.device)
+            lse = torch.empty((self.queries, self.heads), dtype=torch.float32, device=q.device)
+            space = _workspace(self._lib, self._space[0], q.device)
+            q, k, v = (_heads(t) for t in (q, k, v))
+            _check(self._lib, self._lib.sieve_attn_forward(
+                self._h, q, k, v, _ptr(key_mask), _ptr(bias), _heads(out), _ptr(lse), _ptr(space),
+                self._space[0], s))
+        return out, lse
+
+    def backward(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 out: torch.Tensor, lse: torch.Tensor, key_mask: Optional[torch.Tensor] = None,
+                 bias: Optional[torch.Tensor] = None, bias_grad: Optional[bool] = None,
+                 stream=None):
+        """Gradients from the output's, and the forward pass's inputs and results.  Returns
+        ``(dq, dk, dv, dbias)``; ``dbias`` is None without a bias (or with ``bias_grad=False``)."""
+        with _on(self._device(), stream):
+            s = torch.cuda.current_stream().cuda_stream
+            q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
+            dout = self._tensor(dout, "dout", self.queries, self.heads)
+            out = self._tensor(out, "out", self.queries, self.heads)
+            _need(tuple(lse.shape) == (self.queries, self.heads) and lse.is_contiguous() and
+                  lse.dtype == torch.float32 and lse.device == q.device,
+                  "lse must be the forward pass's")
+            dq = torch.empty((self.queries, self.heads, self.head_dim), dtype=self.dtype,
+                             device=q.device)
+            dk = torch.empty((self.keys, self.kv_heads, self.head_dim), dtype=self.dtype,
+                             device=q.device)
+            dv = torch.empty_like(dk)
+            want = bias is not None and bias_grad is not False
+            dbias = torch.empty_like(bias) if want else None
+            space = _workspace(self._lib, self._space[1], q.device)
+            dout, q, k, v, out = (_heads(t) for t in (dout, q, k, v, out))
+            _check(self._lib, self._lib.sieve_attn_backward(
+                self._h, dout, q, k, v, out, _ptr(lse), _ptr(key_mask), _ptr(bias), _heads(dq),
+                _heads(dk), _heads(dv), _ptr(dbias), _ptr(space), self._space[1], s))
+        return dq, dk, dv, dbias
+
+
+class _View(_Heads):
+    """A ``sieve_heads`` that keeps the tensor it points into."""
+    keep = None
+
+
+def _heads(t: torch.Tensor) -> _View:
+    if t.numel() and ((t.shape[2] > 1 and t.stride(2) != 1) or min(t.stride()) < 0):
+        t = t.contiguous()
+    h = _View(_ptr(t), t.stride(0), t.stride(1))
+    h.keep = t
+    return h
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, plan, key_mask, bias):
+        out, lse = plan.forward(q, k, v, key_mask, bias)
+        ctx.save_for_backward(q, k, v, out, lse, key_mask, bias)
+        ctx.plan = plan
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, lse, key_mask, bias = ctx.saved_tensors
+        dq, dk, dv, dbias = ctx.plan.backward(dout, q, k, v, out, lse, key_mask, bias,
+                                              bias_grad=ctx.needs_input_grad[5])
+        return dq, dk, dv, None, None, dbias
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: AttentionPlan,
+              key_mask: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None):
+    """Differentiable attention over ``plan``'s packed batch (see ``AttentionPlan.forward``)."""
+    return _Attention.apply(q, k, v, plan, key_mask, bias)
