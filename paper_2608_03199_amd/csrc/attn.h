@@ -43,7 +43,9 @@ struct AttnArgs {
   const void* bias;
   float* lse;        // written by the forward pass, read by the backward pass
   int32_t G, heads, kv_heads, d, causal;
-  int32_t vec;       // every row may be moved in 16-byte pieces
+  int32_t g_shift;   // log2(G), or -1 where G is no power of two
+  int32_t vec;       // every row may be moved in 16-byte pieces, at offsets of 32 bits from
+                     // its tile's first
   float scale;
   // bias: table entry i of a head is relative position i - distance - kAttnPad
   int32_t nb, distance, span;

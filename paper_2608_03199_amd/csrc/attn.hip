@@ -299,9 +299,15 @@ int check_heads(const sieve_heads* x, const char* name) {
     return set_error(SIEVE_EINVAL, "%s has a negative stride", name);
   return SIEVE_OK;
 }
-bool heads_vec(const sieve_heads& x, int size) {
-  return (((uintptr_t)x.data | (uint64_t)(x.token_stride * size) |
-           (uint64_t)(x.head_stride * size)) & 15) == 0;
+// Whether rows may be moved in 16-byte pieces at 32-bit offsets from a tile's first row.
+bool heads_vec(const sieve_heads& x, int size, int G) {
+  if ((((uintptr_t)x.data | (uint64_t)(x.token_stride * size) |
+        (uint64_t)(x.head_stride * size)) & 15) != 0)
+    return false;
+  constexpr int64_t kMost = int64_t(1) << 40;  // far past 2^31: keeps the products small
+  return std::min(x.token_stride, kMost) * kAttnRows * size +
+             std::min(x.head_stride, kMost) * G * size <
+         (int64_t(1) << 31);
 }
 
 int check_plan(const sieve_attn* p) {
@@ -323,6 +329,7 @@ AttnArgs common_args(const sieve_attn* p, const uint8_t* key_mask, const void* b
   a.key_mask = key_mask;
   a.bias = p->nb ? bias : nullptr;
   a.G = p->heads / p->kv_heads;
+  a.g_shift = (a.G & (a.G - 1)) == 0 ? __builtin_ctz(a.G) : -1;
   a.heads = p->heads;
   a.kv_heads = p->kv_heads;
   a.d = p->d;
@@ -407,8 +414,8 @@ SIEVE_API int sieve_attn_forward(const sieve_attn* plan, const sieve_heads* q,
   }
   a.lse = lse;
   const int size = enc_size(p->dtype);
-  a.vec = p->d * size % 16 == 0 && heads_vec(a.q, size) && heads_vec(a.o, size) &&
-          heads_vec(a.k, size) && heads_vec(a.v, size);
+  a.vec = p->d * size % 16 == 0 && heads_vec(a.q, size, a.G) && heads_vec(a.o, size, a.G) &&
+          heads_vec(a.k, size, 1) && heads_vec(a.v, size, 1);
   a.part_o = (float*)workspace;
   a.part_ml = (float*)((uint8_t*)workspace + sp.ml);
   a.items = p->fwd;
@@ -464,8 +471,10 @@ SIEVE_API int sieve_attn_backward(const sieve_attn* plan, const sieve_heads* dou
   a.dbias = dbias;
   const int size = enc_size(p->dtype);
   a.vec = p->d * size % 16 == 0;
-  for (const sieve_heads* x : {&a.q, &a.k, &a.v, &a.o, &a.dout, &a.dq, &a.dk, &a.dv})
-    a.vec = a.vec && heads_vec(*x, size);
+  for (const sieve_heads* x : {&a.q, &a.o, &a.dout, &a.dq})
+    a.vec = a.vec && heads_vec(*x, size, a.G);
+  for (const sieve_heads* x : {&a.k, &a.v, &a.dk, &a.dv})
+    a.vec = a.vec && heads_vec(*x, size, 1);
   uint8_t* w = (uint8_t*)workspace;
   a.dsum = (float*)w;
   a.part_bias = (float*)(w + sp.bias);

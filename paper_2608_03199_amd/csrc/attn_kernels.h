@@ -108,6 +108,11 @@ __device__ __forceinline__ vec8<T> frag_across(const T* s, int row, int col, int
   }
 }
 
+template <typename T>
+__device__ __forceinline__ EncVec<T, 8> as_vec(vec8<T> v) {
+  return __builtin_bit_cast(EncVec<T, 8>, v);
+}
+
 // Registers 8 s .. 8 s + 7 as an operand, rounded to nearest.
 template <typename T>
 __device__ __forceinline__ vec8<T> frag_of(const f32x16& x, int s) {
@@ -116,16 +121,24 @@ __device__ __forceinline__ vec8<T> frag_of(const f32x16& x, int s) {
   return __builtin_convertvector(v, vec8<T>);
 }
 
+// Query of packed row r: a shift where the group's size is a power of two, as it nearly
+// always is (a division by a variable is some 30 instructions).
+__device__ __forceinline__ int query_of(const AttnArgs& a, int r) {
+  return a.g_shift >= 0 ? r >> a.g_shift : r / a.G;
+}
+
 // Offset of packed row r (query r / G, head r % G of the group).
-__device__ __forceinline__ int64_t row_at(const sieve_heads& x, int64_t q0, int kvh, int G, int r) {
-  const int tok = G == 1 ? r : r / G;
-  return (q0 + tok) * x.token_stride + (int64_t)(kvh * G + (r - tok * G)) * x.head_stride;
+__device__ __forceinline__ int64_t row_at(const AttnArgs& a, const sieve_heads& x,
+                                          const AttnItem& it, int r) {
+  const int tok = query_of(a, r);
+  return (it.q0 + tok) * x.token_stride +
+         (int64_t)(it.kvh * a.G + (r - tok * a.G)) * x.head_stride;
 }
 
 // One row's values 16 c + 8 h .. + 7 for all c, from global memory; zeros past the head's
 // size, or all zeros where the row is not there.
-template <typename T, int DP>
-__device__ __forceinline__ void load_frags(const T* p, bool ok, int d, int vec, int h,
+template <typename T, int DP, bool kVec>
+__device__ __forceinline__ void load_frags(const T* p, bool ok, int d, int h,
                                            vec8<T> (&f)[DP / 16]) {
 #pragma unroll
   for (int c = 0; c < DP / 16; ++c) {
@@ -134,7 +147,7 @@ __device__ __forceinline__ void load_frags(const T* p, bool ok, int d, int vec, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) q.v[j] = (T)0.f;
     if (ok && col < d) {
-      if (vec && (sizeof(T) == 2 || col + 8 <= d)) {
+      if (kVec && (sizeof(T) == 2 || col + 8 <= d)) {
         q = enc_load<T, 8>(p + col);
       } else {
 #pragma unroll
@@ -146,8 +159,25 @@ __device__ __forceinline__ void load_frags(const T* p, bool ok, int d, int vec, 
   }
 }
 
-// A tile of ROWS rows on its way from global memory through registers into LDS.
-template <typename T, int DP, int ROWS>
+// Loads of 16 bytes at a 32-bit offset from a base that the whole wave shares; kNowhere loads
+// zeros.  A row that is not there costs a select instead of a branch.
+constexpr uint32_t kNowhere = 0x80000000u;
+struct Buffer {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ explicit Buffer(const void* base)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)kNowhere,
+                                               0x00027000)) {}
+  __device__ __forceinline__ enc_u32x4 load(uint32_t offset) const {
+    return __builtin_bit_cast(enc_u32x4,
+                              __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)offset, 0, 0));
+  }
+};
+
+// A tile of ROWS rows on its way from global memory through registers into LDS.  Whether a
+// row counts (a mask, a row without keys) is itself loaded: the rows are loaded without
+// waiting for it, and dropped on their way into LDS.
+// kVec: the rows may be moved in 16-byte pieces and a tile spans less than 2^31 bytes.
+template <typename T, int DP, int ROWS, bool kVec>
 struct Stage {
   static constexpr int kE = 16 / sizeof(T);           // values of a 16-byte piece
   static constexpr int kPieces = DP / kE;             // pieces of a row
@@ -155,44 +185,90 @@ struct Stage {
   static constexpr int kN = (kAll + kAttnThreads - 1) / kAttnThreads;
   enc_u32x4 r[kN];
 
-  // row_of(i): where row i of the tile lies, or null where it is to be zeros
+  // row and first value of this thread's piece i
+  static __device__ __forceinline__ int row(int i) {
+    return (threadIdx.x + i * kAttnThreads) / kPieces;
+  }
+  static __device__ __forceinline__ int col(int i) {
+    return ((threadIdx.x + i * kAttnThreads) % kPieces) * kE;
+  }
+  static __device__ __forceinline__ bool mine(int i) {
+    return kAll % kAttnThreads == 0 || threadIdx.x + i * kAttnThreads < kAll;
+  }
+  // at(i): piece i's offset in values from base; rows: how many of the tile's there are
   template <typename F>
-  __device__ __forceinline__ void load(F row_of, int d, int vec) {
+  __device__ __forceinline__ void load(const T* base, F at, int rows, int d) {
+    const Buffer from(base);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int idx = threadIdx.x + i * kAttnThreads;
-      const int row = idx / kPieces, col = (idx % kPieces) * kE;
-      r[i] = enc_u32x4{0, 0, 0, 0};
-      if (kAll % kAttnThreads != 0 && idx >= kAll) continue;
-      if (col >= d) continue;
-      const T* p = row_of(row);
-      if (!p) continue;
-      if (vec) {
-        r[i] = *(const enc_u32x4*)(p + col);
+      const bool there = mine(i) && row(i) < rows && col(i) < d;
+      if constexpr (kVec) {
+        r[i] = from.load(there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere);
       } else {
         EncVec<T, kE> q;
 #pragma unroll
-        for (int j = 0; j < kE; ++j) q.v[j] = col + j < d ? p[col + j] : (T)0.f;
+        for (int j = 0; j < kE; ++j) q.v[j] = there && col(i) + j < d ? base[at(i) + j] : (T)0.f;
         r[i] = __builtin_bit_cast(enc_u32x4, q);
       }
     }
   }
+  __device__ __forceinline__ void drop(int i) { r[i] = enc_u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void store(T* s) const {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int idx = threadIdx.x + i * kAttnThreads;
-      if (kAll % kAttnThreads != 0 && idx >= kAll) continue;
-      const int row = idx / kPieces, col = (idx % kPieces) * kE;
-      *(enc_u32x4*)(s + row * lds_row<T, DP>() + col) = r[i];
+    for (int i = 0; i < kN; ++i)
+      if (mine(i)) *(enc_u32x4*)(s + row(i) * lds_row<T, DP>() + col(i)) = r[i];
+  }
+};
+
+// The keys and values of a tile, and what the mask says of their rows.
+template <typename T, int DP, int KEYS, bool kVec>
+struct KeyStage {
+  using Tile = Stage<T, DP, KEYS, kVec>;
+  Tile k, v;
+  uint8_t keep[Tile::kN];
+
+  // k0, v0: the sequence's first row; keys base .. hi - 1 at most
+  __device__ __forceinline__ void load(const AttnArgs& a, const uint8_t* mask, const T* k0,
+                                       const T* v0, int base, int hi) {
+    const int64_t ks = a.k.token_stride, vs = a.v.token_stride;
+    if constexpr (kVec) {
+      k.load(k0 + base * ks, [&](int i) { return Tile::row(i) * (int)ks + Tile::col(i); },
+             hi - base, a.d);
+      v.load(v0 + base * vs, [&](int i) { return Tile::row(i) * (int)vs + Tile::col(i); },
+             hi - base, a.d);
+    } else {
+      k.load(k0 + base * ks, [&](int i) { return Tile::row(i) * ks + Tile::col(i); }, hi - base,
+             a.d);
+      v.load(v0 + base * vs, [&](int i) { return Tile::row(i) * vs + Tile::col(i); }, hi - base,
+             a.d);
     }
+    if (mask) {
+#pragma unroll
+      for (int i = 0; i < Tile::kN; ++i) {
+        const int key = base + Tile::row(i);
+        keep[i] = key < hi ? mask[key] : 0;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(const uint8_t* mask, T* s_k, T* s_v) {
+    if (mask) {
+#pragma unroll
+      for (int i = 0; i < Tile::kN; ++i)
+        if (!keep[i]) {
+          k.drop(i);
+          v.drop(i);
+        }
+    }
+    k.store(s_k);
+    v.store(s_v);
   }
 };
 
 // Accumulators X^T (rows: the head's values 32 b + 8 g + 4 h + t in register 4 g + t,
 // column: the lane's row) times f, to a row in global memory.
-template <typename T, int DP>
+template <typename T, int DP, bool kVec>
 __device__ __forceinline__ void store_row(T* p, const f32x16 (&x)[DP / 32], float f, int d,
-                                          int vec, int h) {
+                                          int h) {
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b) {
 #pragma unroll
@@ -202,7 +278,7 @@ __device__ __forceinline__ void store_row(T* p, const f32x16 (&x)[DP / 32], floa
       const f32x4 v = {x[b][4 * g] * f, x[b][4 * g + 1] * f, x[b][4 * g + 2] * f,
                        x[b][4 * g + 3] * f};
       const vec4 q = __builtin_convertvector(v, vec4);
-      if (vec && col + 4 <= d) {
+      if (kVec && col + 4 <= d) {
         *(vec4*)(p + col) = q;
       } else {
 #pragma unroll
@@ -223,10 +299,10 @@ __device__ __forceinline__ void load_bias(const AttnArgs& a, int kvh, float* s) 
   }
 }
 
-// Bits 0..31: key base + bit is in the item's range and not masked.  Loaded a tile ahead.
-__device__ __forceinline__ bool key_ok(const AttnArgs& a, const AttnItem& it, int key) {
-  if (key >= it.hi) return false;
-  return !a.key_mask || a.key_mask[it.k0 + key] != 0;
+// Not 0: the key is in the item's range and not masked.  Loaded a tile ahead.
+__device__ __forceinline__ uint8_t key_ok(const uint8_t* mask, int key, int hi) {
+  if (key >= hi) return 0;
+  return mask ? mask[key] : 1;
 }
 
 // Bits 0..31: key base + bit is not after position pos.
@@ -269,20 +345,22 @@ struct LaneRow {
   int pos_min, pos_max;  // over the wave's rows
   bool live;
 };
-__device__ __forceinline__ LaneRow lane_row(const AttnItem& it, int G, int first, int lane) {
+__device__ __forceinline__ LaneRow lane_row(const AttnArgs& a, const AttnItem& it, int first,
+                                            int lane) {
   LaneRow x;
+  const int G = a.G;
   const int rows = it.nq * G;
   x.r = first + (lane & 31);
   x.live = x.r < rows;
   const int r = x.live ? x.r : (rows > 0 ? rows - 1 : 0);
-  x.tok = G == 1 ? r : r / G;
+  x.tok = query_of(a, r);
   x.g = r - x.tok * G;
   const int shift = it.nk - it.nq;
   x.pos = x.tok + shift;
   const int last = first + 31 < rows ? first + 31 : rows - 1;
   const int head = first < rows ? first : rows - 1;
-  x.pos_min = head / G + shift;
-  x.pos_max = last / G + shift;
+  x.pos_min = query_of(a, head) + shift;
+  x.pos_max = query_of(a, last) + shift;
   return x;
 }
 
@@ -307,7 +385,7 @@ struct FwdShape {
   static constexpr int kRows = WK == 1 ? kAttnRows : kAttnFewRows;
 };
 
-template <typename T, int DP, int WK, bool kBias>
+template <typename T, int DP, int WK, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_forward_kernel(AttnArgs a) {
   using Shape = FwdShape<T, DP, WK>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
@@ -318,32 +396,27 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int G = a.G, d = a.d, vec = a.vec;
-  const LaneRow me = lane_row(it, G, it.row + (WK == 1 ? wave * 32 : 0), lane);
+  const int G = a.G, d = a.d;
+  const LaneRow me = lane_row(a, it, it.row + (WK == 1 ? wave * 32 : 0), lane);
   const float scale2 = a.scale * kLog2e;
   const bool wave_live = WK == 4 || it.row + wave * 32 < it.nq * G;
 
   const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
-  Stage<T, DP, kTile> st_k, st_v;
-  bool ok[kBlocks];
+  const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
+  KeyStage<T, DP, kTile, kVec> stage;
+  uint8_t ok[kBlocks];
   auto fetch = [&](int base) {
-    st_k.load([&](int i) { return key_ok(a, it, base + i)
-                                      ? k0 + (int64_t)(base + i) * a.k.token_stride : nullptr; },
-              d, vec);
-    st_v.load([&](int i) { return key_ok(a, it, base + i)
-                                      ? v0 + (int64_t)(base + i) * a.v.token_stride : nullptr; },
-              d, vec);
+    stage.load(a, mask, k0, v0, base, it.hi);
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-      ok[b] = key_ok(a, it, base + 32 * ((WK == 1 ? 0 : wave) + b) + (lane & 31));
+    for (int b = 0; b < kBlocks; ++b) ok[b] = key_ok(mask, base + 32 * ((WK == 1 ? 0 : wave) + b) + (lane & 31), it.hi);
   };
   if (it.lo < it.hi) fetch(it.lo);
 
   vec8<T> q[DP / 16];
   {
-    const T* p = (const T*)a.q.data + (me.live ? row_at(a.q, it.q0, it.kvh, G, me.r) : 0);
-    load_frags<T, DP>(p, me.live, d, vec, h, q);
+    const T* p = (const T*)a.q.data + (me.live ? row_at(a, a.q, it, me.r) : 0);
+    load_frags<T, DP, kVec>(p, me.live, d, h, q);
   }
   float lo = 0.f, hi = 0.f;
   const float* table = nullptr;
@@ -361,8 +434,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 
   int buf = 0;
   if (it.lo < it.hi) {
-    st_k.store(s_k);
-    st_v.store(s_v);
+    stage.store(mask, s_k, s_v);
     __syncthreads();
   }
   for (int base = it.lo; base < it.hi; base += kTile) {
@@ -370,7 +442,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     uint32_t bits[kBlocks], any = 0;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      bits[b] = (uint32_t)__ballot(ok[b]);
+      bits[b] = (uint32_t)__ballot(ok[b] != 0);
       if (a.causal) bits[b] &= upto(me.pos, first + 32 * b);
       any |= bits[b];
     }
@@ -426,8 +498,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     if (Shape::kBufs == 1) __syncthreads();
     if (more) {
       buf ^= Shape::kBufs - 1;
-      st_k.store(s_k + buf * kTileN);
-      st_v.store(s_v + buf * kTileN);
+      stage.store(mask, s_k + buf * kTileN, s_v + buf * kTileN);
       __syncthreads();
     }
   }
@@ -494,8 +565,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     return;
   }
   if (!me.live) return;
-  store_row<T, DP>((T*)a.o.data + row_at(a.o, it.q0, it.kvh, G, me.r), o,
-                   l == 0.f ? 0.f : 1.f / l, d, vec, h);
+  store_row<T, DP, kVec>((T*)a.o.data + row_at(a, a.o, it, me.r), o,
+                   l == 0.f ? 0.f : 1.f / l, d, h);
   if (a.lse && h == 0)
     a.lse[(it.q0 + me.tok) * a.heads + it.kvh * G + me.g] =
         l == 0.f ? -INFINITY : (at + __builtin_amdgcn_logf(l)) * kLn2;
@@ -533,7 +604,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
       }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* to = (T*)a.o.data + row_at(a.o, j.q0, j.kvh, a.G, r);
+    const int tok = query_of(a, r);
+    const int head = j.kvh * a.G + (r - tok * a.G);
+    T* to = (T*)a.o.data + (j.q0 + tok) * a.o.token_stride + head * a.o.head_stride;
 #pragma unroll
     for (int e = 0; e < kN / 4; ++e)
 #pragma unroll
@@ -541,11 +614,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
         const int col = 32 * e + (threadIdx.x & 7) * 4 + t;
         if (col < a.d) to[col] = (T)(v[4 * e + t] * inv);
       }
-    if (a.lse && (threadIdx.x & 7) == 0) {
-      const int tok = r / a.G;
-      a.lse[(j.q0 + tok) * a.heads + j.kvh * a.G + (r - tok * a.G)] =
+    if (a.lse && (threadIdx.x & 7) == 0)
+      a.lse[(j.q0 + tok) * a.heads + head] =
           l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
-    }
   }
 }
 
@@ -554,10 +625,11 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
 // It writes D for the second kernel.
 //
 // The bias table's gradient is a sum along diagonals.  Where a block of keys is past the
-// distance it all falls into one bucket, and the lane adds it up in a register; nearer, each
-// value is added in LDS to the sum of its relative position.  One instruction's 32 lanes of a
-// half have 32 different (head, position) pairs, and every wave and half has sums of its own,
-// so no two additions ever meet and their order is the program's.
+// distance it all falls into one bucket, and the lane adds it up in a register.  Nearer, the
+// wave writes its 32x32 block of dS to LDS with zeros beside every row, so that a lane can
+// read down a whole diagonal without a test (row i's value at relative position p + i lies at
+// a constant step from row i - 1's), and adds the result to its own sums by position.  No
+// atomics: the order of additions is the program's.
 
 template <typename T, int DP>
 struct DqShape {
@@ -566,9 +638,49 @@ struct DqShape {
   static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
   static constexpr int kBytes = 2 * kBufs * kTile * lds_row<T, DP>() * (int)sizeof(T);
 };
-constexpr int kSums = 2 * kAttnThreads / 64;  // copies of the sums by position: wave and half
+constexpr int kAttnWaves = kAttnThreads / 64;
+// A row of the dS block: 32 values, then at least 31 zeros, and 4 words that spread the
+// rows' 16-byte stores over the banks; 32 zeros stand before the first row.
+constexpr int kDiagRow = 68;
+constexpr int kDiagWords = 32 * kDiagRow + 32;
 
-template <typename T, int DP, bool kBias>
+// Adds the diagonals of the wave's block (rows: packed rows from `first_row`, columns: keys
+// from `base`) to the wave's sums by relative position.
+__device__ __forceinline__ void add_diagonals(const AttnArgs& a, const AttnItem& it,
+                                              const float* block, float* sums, int first_row,
+                                              int base, int pos0, int lane) {
+  const int G = a.G;
+  // relative position of (row 0, key 0) as an entry of the sums
+  const int entry = base - pos0 + a.distance + kAttnPad;
+  if (G == 1) {
+    // lane: diagonal key - row = lane - 31
+    const float* p = block + lane - 31;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t += p[i * (kDiagRow + 1)];
+    if (lane < 63) sums[entry + lane - 31] += t;
+    return;
+  }
+  // rows of head g: every G-th, their queries one apart
+  const int rows = (30 + G) / G + 1;  // at most, counted from row 0's query
+  const int wide = 31 + rows;         // diagonals of a head
+  const int tok0 = query_of(a, first_row);
+  for (int x = lane; x < G * wide; x += 64) {
+    const int g = x / wide, diag = x - g * wide - (rows - 1);
+    float t = 0.f;
+    // first row of head g at or after first_row
+    int r = g - (first_row - tok0 * G);
+    if (r < 0) r += G;
+    const int tok = query_of(a, first_row + r) - tok0;
+    for (int i = tok; r < 32; r += G, ++i) {
+      const int key = diag + i;
+      if (key >= 0 && key < 32) t += block[r * kDiagRow + key];
+    }
+    sums[g * a.span + entry + diag] += t;
+  }
+}
+
+template <typename T, int DP, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
   using Shape = DqShape<T, DP>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
@@ -578,30 +690,27 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_k = (T*)smem;
   T* s_v = s_k + Shape::kBufs * kTileN;
   float* s_bias = (float*)(smem + Shape::kBytes);
-  float* s_sum = s_bias + a.G * a.span;            // [wave][half][G][span]
-  float* s_far = s_sum + kSums * a.G * a.span;     // [wave][half][32][2]
-  __shared__ float s_max[kAttnThreads / 64];
+  float* s_sum = s_bias + a.G * a.span;             // [wave][G][span]
+  float* s_far = s_sum + kAttnWaves * a.G * a.span;  // [wave][half][32][2]
+  float* s_diag = s_far + kAttnWaves * 128;          // [wave][kDiagWords]
+  __shared__ float s_max[kAttnWaves];
   const AttnItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int G = a.G, d = a.d, vec = a.vec;
-  const LaneRow me = lane_row(it, G, it.row + wave * 32, lane);
+  const int G = a.G, d = a.d;
+  const LaneRow me = lane_row(a, it, it.row + wave * 32, lane);
   const float scale2 = a.scale * kLog2e;
   const bool wave_live = it.row + wave * 32 < it.nq * G;
   const bool want_bias = kBias && a.dbias;
 
   const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
-  Stage<T, DP, kTile> st_k, st_v;
-  bool ok[kBlocks];
+  const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
+  KeyStage<T, DP, kTile, kVec> stage;
+  uint8_t ok[kBlocks];
   auto fetch = [&](int base) {
-    st_k.load([&](int i) { return key_ok(a, it, base + i)
-                                      ? k0 + (int64_t)(base + i) * a.k.token_stride : nullptr; },
-              d, vec);
-    st_v.load([&](int i) { return key_ok(a, it, base + i)
-                                      ? v0 + (int64_t)(base + i) * a.v.token_stride : nullptr; },
-              d, vec);
+    stage.load(a, mask, k0, v0, base, it.hi);
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) ok[b] = key_ok(a, it, base + 32 * b + (lane & 31));
+    for (int b = 0; b < kBlocks; ++b) ok[b] = key_ok(mask, base + 32 * b + (lane & 31), it.hi);
   };
   if (it.lo < it.hi) fetch(it.lo);
 
@@ -613,13 +722,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     const float lse = me.live ? a.lse[at] : -INFINITY;
     const bool some = lse != -INFINITY;
     if (some) lse2 = lse * kLog2e;
-    const T* pq = (const T*)a.q.data + (me.live ? row_at(a.q, it.q0, it.kvh, G, me.r) : 0);
-    const T* pd = (const T*)a.dout.data + (me.live ? row_at(a.dout, it.q0, it.kvh, G, me.r) : 0);
-    const T* po = (const T*)a.o.data + (me.live ? row_at(a.o, it.q0, it.kvh, G, me.r) : 0);
+    const T* pq = (const T*)a.q.data + (me.live ? row_at(a, a.q, it, me.r) : 0);
+    const T* pd = (const T*)a.dout.data + (me.live ? row_at(a, a.dout, it, me.r) : 0);
+    const T* po = (const T*)a.o.data + (me.live ? row_at(a, a.o, it, me.r) : 0);
     vec8<T> out[DP / 16];
-    load_frags<T, DP>(pq, some, d, vec, h, q);
-    load_frags<T, DP>(pd, some, d, vec, h, dout);
-    load_frags<T, DP>(po, some, d, vec, h, out);
+    load_frags<T, DP, kVec>(pq, some, d, h, q);
+    load_frags<T, DP, kVec>(pd, some, d, h, dout);
+    load_frags<T, DP, kVec>(po, some, d, h, out);
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
@@ -629,16 +738,19 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   }
   float lo = 0.f, hi = 0.f, far_lo = 0.f, far_hi = 0.f;
   const float* table = nullptr;
-  float* sums = nullptr;
+  float *sums = nullptr, *block = nullptr;
   if constexpr (kBias) {
     load_bias<T>(a, it.kvh, s_bias);
-    if (want_bias)
-      for (int i = threadIdx.x; i < kSums * G * a.span; i += kAttnThreads) s_sum[i] = 0.f;
+    if (want_bias) {
+      for (int i = threadIdx.x; i < kAttnWaves * G * a.span; i += kAttnThreads) s_sum[i] = 0.f;
+      for (int i = threadIdx.x; i < kAttnWaves * kDiagWords; i += kAttnThreads) s_diag[i] = 0.f;
+    }
     __syncthreads();
     table = s_bias + me.g * a.span;
     lo = table[0];
     hi = table[a.span - 1];
-    sums = s_sum + ((wave * 2 + h) * G + me.g) * a.span;
+    sums = s_sum + wave * G * a.span;
+    block = s_diag + wave * kDiagWords + 32;
   }
   f32x16 dq[DP / 32];
 #pragma unroll
@@ -648,15 +760,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 
   int buf = 0;
   if (it.lo < it.hi) {
-    st_k.store(s_k);
-    st_v.store(s_v);
+    stage.store(mask, s_k, s_v);
     __syncthreads();
   }
   for (int base = it.lo; base < it.hi; base += kTile) {
     uint32_t bits[kBlocks], any = 0;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      bits[b] = (uint32_t)__ballot(ok[b]);
+      bits[b] = (uint32_t)__ballot(ok[b] != 0);
       if (a.causal) bits[b] &= upto(me.pos, base + 32 * b);
       any |= bits[b];
     }
@@ -694,12 +805,19 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
               for (int r = 0; r < 16; ++r) t += s[r];
               if (first > me.pos_min) far_hi += t;
               else far_lo += t;
-            } else if (me.live) {
-              float* t = sums + (first + 4 * h - me.pos + a.distance + kAttnPad);
+            } else {
+              // rows past the sequence's end have dS = 0
 #pragma unroll
-              for (int r = 0; r < 16; ++r)
-                __hip_atomic_fetch_add(t + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_WORKGROUP);
+              for (int g = 0; g < 4; ++g)
+                *(f32x4*)(block + (lane & 31) * kDiagRow + 8 * g + 4 * h) =
+                    f32x4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
+              __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+              __builtin_amdgcn_wave_barrier();
+              __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+              add_diagonals(a, it, block, sums, it.row + wave * 32, first, me.pos_min, lane);
+              __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+              __builtin_amdgcn_wave_barrier();
+              __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             }
           }
         }
@@ -737,14 +855,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     if (Shape::kBufs == 1) __syncthreads();
     if (more) {
       buf ^= Shape::kBufs - 1;
-      st_k.store(s_k + buf * kTileN);
-      st_v.store(s_v + buf * kTileN);
+      stage.store(mask, s_k + buf * kTileN, s_v + buf * kTileN);
       __syncthreads();
     }
   }
   if (me.live)
-    store_row<T, DP>((T*)a.dq.data + row_at(a.dq, it.q0, it.kvh, G, me.r), dq, a.scale / up, d,
-                     vec, h);
+    store_row<T, DP, kVec>((T*)a.dq.data + row_at(a, a.dq, it, me.r), dq, a.scale / up, d,
+                     h);
   if constexpr (kScaled) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
@@ -763,7 +880,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     for (int i = threadIdx.x; i < all; i += kAttnThreads) {
       float t = 0.f;
 #pragma unroll
-      for (int w = 0; w < kSums; ++w) t += s_sum[w * all + i];
+      for (int w = 0; w < kAttnWaves; ++w) t += s_sum[w * all + i];
       s_sum[i] = t;  // entry i belongs to this thread alone
     }
     __syncthreads();
@@ -803,7 +920,12 @@ struct DkvShape {
   static constexpr int kTile = 32 * kBlocks;
   static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
   static constexpr int kTileBytes = kTile * lds_row<T, DP>() * (int)sizeof(T);
-  static constexpr int kBytes = kBufs * (2 * kTileBytes + 4 * kTile * 4);
+  // The tile's values as operands in registers, or, where the accumulators leave no room
+  // for them at two waves a SIMD, in LDS.
+  static constexpr bool kValuesInLds = DP * sizeof(T) >= 256;
+  static constexpr int kValueBytes =
+      kValuesInLds ? kAttnKeys * lds_row<T, DP>() * (int)sizeof(T) : 0;
+  static constexpr int kBytes = kValueBytes + kBufs * (2 * kTileBytes + 4 * kTile * 4);
 };
 
 template <typename T>
@@ -826,8 +948,8 @@ __device__ __forceinline__ void reduce_bias(const AttnArgs& a, int head, float* 
   }
 }
 
-template <typename T, int DP, bool kBias>
-__global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
+template <typename T, int DP, bool kBias, bool kVec>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
   using Shape = DkvShape<T, DP>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
   constexpr int kTileN = kTile * lds_row<T, DP>();
@@ -837,60 +959,81 @@ __global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kern
     reduce_bias<T>(a, blockIdx.x - a.nitems, (float*)smem);
     return;
   }
-  T* s_q = (T*)smem;
+  T* s_val = (T*)smem;
+  T* s_q = (T*)(smem + Shape::kValueBytes);
   T* s_do = s_q + Shape::kBufs * kTileN;
-  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][lse2, D, table offset, pos][row]
+  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][lse2, -D, table offset, pos][row]
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int G = a.G, d = a.d, vec = a.vec, shift = it.nk - it.nq;
+  const int G = a.G, d = a.d, shift = it.nk - it.nq;
   const float scale2 = a.scale * kLog2e;
   const int key0 = it.row + wave * 32, key = key0 + (lane & 31);
   const bool wave_live = key0 < it.nk;
   const bool there = key < it.nk;
   const bool live = there && (!a.key_mask || a.key_mask[it.k0 + key] != 0);
 
-  Stage<T, DP, kTile> st_q, st_do;
-  float row_lse = 0.f, row_d = 0.f;
+  // Rows that saw no key are zeros whatever they hold: their lse tells, loaded with them.
+  using Tile = Stage<T, DP, kTile, kVec>;
+  Tile st_q, st_do;
+  constexpr int kN = Tile::kN;
+  float piece_lse[kN], row_lse = 0.f, row_d = 0.f;
   int row_off = 0, row_pos = 0;
+  const float* lse0 = a.lse + it.q0 * a.heads + it.kvh * G;  // the sequence's first row
+  const float* dsum0 = a.dsum + it.q0 * a.heads + it.kvh * G;
+  const T* q0 = (const T*)a.q.data + it.q0 * a.q.token_stride + it.kvh * G * a.q.head_stride;
+  const T* do0 =
+      (const T*)a.dout.data + it.q0 * a.dout.token_stride + it.kvh * G * a.dout.head_stride;
   auto fetch = [&](int base) {
-    // a row that saw no key is zeros whatever it holds
-    auto seen = [&](int r) {
-      if (r >= it.hi) return false;
-      const int tok = G == 1 ? r : r / G;
-      return a.lse[(it.q0 + tok) * a.heads + it.kvh * G + (r - tok * G)] != -INFINITY;
+    const int tok0 = query_of(a, base);
+    auto at = [&](const sieve_heads& x, int i) {
+      const int r = base + Tile::row(i), tok = query_of(a, r);
+      if constexpr (kVec)
+        return (tok - tok0) * (int)x.token_stride + (r - tok * G) * (int)x.head_stride +
+               Tile::col(i);
+      else
+        return (tok - tok0) * x.token_stride + (r - tok * G) * x.head_stride + Tile::col(i);
     };
-    st_q.load([&](int i) { return seen(base + i)
-                                      ? (const T*)a.q.data + row_at(a.q, it.q0, it.kvh, G, base + i)
-                                      : nullptr; },
-              d, vec);
-    st_do.load([&](int i) { return seen(base + i) ? (const T*)a.dout.data +
-                                                        row_at(a.dout, it.q0, it.kvh, G, base + i)
-                                                  : nullptr; },
-               d, vec);
+    st_q.load(q0 + tok0 * a.q.token_stride, [&](int i) { return at(a.q, i); }, it.hi - base, d);
+    st_do.load(do0 + tok0 * a.dout.token_stride, [&](int i) { return at(a.dout, i); },
+               it.hi - base, d);
+    auto stat = [&](int r) {
+      const int tok = query_of(a, r);
+      return (int64_t)tok * a.heads + (r - tok * G);
+    };
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int r = base + Tile::row(i);
+      piece_lse[i] = r < it.hi ? lse0[stat(r)] : -INFINITY;
+    }
     if (threadIdx.x < kTile) {
       const int r = base + threadIdx.x;
-      row_lse = INFINITY;
+      row_lse = -INFINITY;
       row_d = 0.f;
       row_off = row_pos = 0;
       if (r < it.hi) {
-        const int tok = G == 1 ? r : r / G, g = r - tok * G;
-        const int64_t at = (it.q0 + tok) * a.heads + it.kvh * G + g;
-        const float lse = a.lse[at];
-        if (lse != -INFINITY) row_lse = lse * kLog2e;
-        row_d = a.dsum[at];
+        const int64_t j = stat(r);
+        row_lse = lse0[j];
+        row_d = dsum0[j];
+        const int tok = query_of(a, r);
         row_pos = tok + shift;
-        if (kBias) row_off = g * a.span;
+        if (kBias) row_off = (r - tok * G) * a.span;
       }
     }
   };
   auto put = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (piece_lse[i] == -INFINITY) {
+        st_q.drop(i);
+        st_do.drop(i);
+      }
     st_q.store(s_q + b * kTileN);
     st_do.store(s_do + b * kTileN);
     if (threadIdx.x < kTile) {
       float* p = s_row + b * 4 * kTile + threadIdx.x;
-      p[0] = row_lse;
-      p[kTile] = row_d;
+      p[0] = row_lse == -INFINITY ? INFINITY : row_lse * kLog2e;
+      p[kTile] = -row_d;
       ((int*)p)[2 * kTile] = row_off;
       ((int*)p)[3 * kTile] = row_pos;
     }
@@ -900,10 +1043,16 @@ __global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kern
   vec8<T> k[DP / 16], v[DP / 16];
   {
     const int64_t tok = it.k0 + (live ? key : 0);
-    load_frags<T, DP>((const T*)a.k.data + tok * a.k.token_stride + it.kvh * a.k.head_stride, live,
-                      d, vec, h, k);
-    load_frags<T, DP>((const T*)a.v.data + tok * a.v.token_stride + it.kvh * a.v.head_stride, live,
-                      d, vec, h, v);
+    load_frags<T, DP, kVec>((const T*)a.k.data + tok * a.k.token_stride + it.kvh * a.k.head_stride, live,
+                      d, h, k);
+    load_frags<T, DP, kVec>((const T*)a.v.data + tok * a.v.token_stride + it.kvh * a.v.head_stride, live,
+                      d, h, v);
+    if constexpr (Shape::kValuesInLds) {  // a wave reads its own 32 rows only
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c)
+        enc_store<T, 8>(s_val + (wave * 32 + (lane & 31)) * lds_row<T, DP>() + 16 * c + 8 * h,
+                        as_vec<T>(v[c]));
+    }
   }
   if constexpr (kBias) load_bias<T>(a, it.kvh, s_bias);
   float up = 1.f;  // dS is rounded times this, and P times 2^14 (f16 only)
@@ -934,20 +1083,26 @@ __global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kern
         const int first = base + 32 * b;
         const int last = (first + 31 < it.hi ? first + 31 : it.hi - 1);
         if (first >= it.hi) continue;
-        const int pos_min = first / G + shift, pos_max = last / G + shift;
+        const int pos_min = query_of(a, first) + shift, pos_max = query_of(a, last) + shift;
         if (a.causal && pos_max < key0) continue;
-        f32x16 s = {}, dp = {};
+        const float* rows = s_row + buf * 4 * kTile + 32 * b + 4 * h;
+        // dP - D: the products are added to -D
+        f32x16 s = {}, dp;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 x = *(const f32x4*)(rows + kTile + 8 * g);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) dp[4 * g + t] = x[t];
+        }
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
           s = mma(frag_along<T, DP>(sq, 32 * b + (lane & 31), c, h), k[c], s);
-          dp = mma(frag_along<T, DP>(sd, 32 * b + (lane & 31), c, h), v[c], dp);
-        }
-        const float* rows = s_row + buf * 4 * kTile + 32 * b + 4 * h;
-        f32x4 lse[4], dsum[4];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          lse[g] = *(const f32x4*)(rows + 8 * g);
-          dsum[g] = *(const f32x4*)(rows + kTile + 8 * g);
+          vec8<T> val;
+          if constexpr (Shape::kValuesInLds)
+            val = frag_along<T, DP>(s_val, wave * 32 + (lane & 31), c, h);
+          else
+            val = v[c];
+          dp = mma(frag_along<T, DP>(sd, 32 * b + (lane & 31), c, h), val, dp);
         }
         if constexpr (kBias) {
           const int dist = a.distance;
@@ -973,9 +1128,11 @@ __global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kern
           for (int r = 0; r < 16; ++r) s[r] *= scale2;
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[r] = __builtin_amdgcn_exp2f(s[r] - lse[r >> 2][r & 3]);
-          dp[r] -= dsum[r >> 2][r & 3];
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 lse = *(const f32x4*)(rows + 8 * g);
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            s[4 * g + t] = __builtin_amdgcn_exp2f(s[4 * g + t] - lse[t]);
         }
         if (a.causal && pos_min < key0 + 31) {
 #pragma unroll
@@ -1018,10 +1175,10 @@ __global__ __launch_bounds__(kAttnThreads, DP == 128 ? 1 : 2) void attn_dkv_kern
     for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = f32x16{};
   }
   const int64_t tok = it.k0 + key;
-  store_row<T, DP>((T*)a.dk.data + tok * a.dk.token_stride + it.kvh * a.dk.head_stride, dk,
-                   a.scale / up, d, vec, h);
-  store_row<T, DP>((T*)a.dv.data + tok * a.dv.token_stride + it.kvh * a.dv.head_stride, dv,
-                   kScaled ? 0x1p-14f : 1.f, d, vec, h);
+  store_row<T, DP, kVec>((T*)a.dk.data + tok * a.dk.token_stride + it.kvh * a.dk.head_stride, dk,
+                   a.scale / up, d, h);
+  store_row<T, DP, kVec>((T*)a.dv.data + tok * a.dv.token_stride + it.kvh * a.dv.head_stride, dv,
+                   kScaled ? 0x1p-14f : 1.f, d, h);
 }
 
 // ---- launch ----------------------------------------------------------------------------------
@@ -1040,38 +1197,39 @@ hipError_t launch(K kernel, const AttnArgs& a, int grid, size_t lds, hipStream_t
   return hipGetLastError();
 }
 
-template <typename T, int DP>
-hipError_t launch_dp(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
-  const size_t table = a.bias ? (size_t)a.G * a.span * sizeof(float) : 0;
+template <typename T, int DP, bool kBias, bool kVec>
+hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
+  const size_t table = kBias ? (size_t)a.G * a.span * sizeof(float) : 0;
   switch (kind) {
-    case kAttnFwd: {
-      const size_t lds = FwdShape<T, DP, 1>::kBytes + table;
-      return a.bias ? launch(attn_forward_kernel<T, DP, 1, true>, a, grid, lds, s)
-                    : launch(attn_forward_kernel<T, DP, 1, false>, a, grid, lds, s);
-    }
-    case kAttnFwdFew: {
-      const size_t lds = FwdShape<T, DP, 4>::kBytes + table;
-      return a.bias ? launch(attn_forward_kernel<T, DP, 4, true>, a, grid, lds, s)
-                    : launch(attn_forward_kernel<T, DP, 4, false>, a, grid, lds, s);
-    }
-    case kAttnJoin:
-      return launch(attn_join_kernel<T, DP, kAttnRows>, a, grid, 0, s);
-    case kAttnJoinFew:
-      return launch(attn_join_kernel<T, DP, kAttnFewRows>, a, grid, 0, s);
+    case kAttnFwd:
+      return launch(attn_forward_kernel<T, DP, 1, kBias, kVec>, a, grid,
+                    FwdShape<T, DP, 1>::kBytes + table, s);
+    case kAttnFwdFew:
+      return launch(attn_forward_kernel<T, DP, 4, kBias, kVec>, a, grid,
+                    FwdShape<T, DP, 4>::kBytes + table, s);
     case kAttnDq: {
       const size_t sums =
-          a.dbias ? kSums * table + (kAttnThreads / 64) * 64 * 2 * sizeof(float) : 0;
-      const size_t lds = DqShape<T, DP>::kBytes + table + sums;
-      return a.bias ? launch(attn_dq_kernel<T, DP, true>, a, grid, lds, s)
-                    : launch(attn_dq_kernel<T, DP, false>, a, grid, lds, s);
+          a.dbias ? kAttnWaves * (table + (128 + kDiagWords) * sizeof(float)) : 0;
+      return launch(attn_dq_kernel<T, DP, kBias, kVec>, a, grid,
+                    DqShape<T, DP>::kBytes + table + sums, s);
     }
-    case kAttnDkv: {
-      const size_t lds = DkvShape<T, DP>::kBytes + table;
-      return a.bias ? launch(attn_dkv_kernel<T, DP, true>, a, grid, lds, s)
-                    : launch(attn_dkv_kernel<T, DP, false>, a, grid, lds, s);
-    }
+    case kAttnDkv:
+      return launch(attn_dkv_kernel<T, DP, kBias, kVec>, a, grid,
+                    DkvShape<T, DP>::kBytes + table, s);
+    default:
+      return hipErrorInvalidValue;
   }
-  return hipErrorInvalidValue;
+}
+
+template <typename T, int DP>
+hipError_t launch_dp(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
+  if (kind == kAttnJoin) return launch(attn_join_kernel<T, DP, kAttnRows>, a, grid, 0, s);
+  if (kind == kAttnJoinFew) return launch(attn_join_kernel<T, DP, kAttnFewRows>, a, grid, 0, s);
+  if (a.bias)
+    return a.vec ? launch_as<T, DP, true, true>(kind, a, grid, s)
+                 : launch_as<T, DP, true, false>(kind, a, grid, s);
+  return a.vec ? launch_as<T, DP, false, true>(kind, a, grid, s)
+               : launch_as<T, DP, false, false>(kind, a, grid, s);
 }
 
 template <typename T>
