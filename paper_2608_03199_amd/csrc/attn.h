@@ -16,16 +16,17 @@ struct AttnItem {
   int32_t kvh;
   int32_t row;      // first row of the tile (forward, dq), or first key (dk and dv)
   int32_t lo, hi;   // keys to go through (forward, dq), or rows (dk and dv)
-  int32_t part;     // forward: slot of a partial result, -1 where the item is a whole row
-                    // tile; dq: number of the row tile among all sequences
+  int32_t part;     // forward, dk and dv: slot of a partial result, -1 where the item is its
+                    // whole tile; dq: number of the row tile among all sequences
   int32_t tile0, ntiles;  // dk and dv: the sequence's row tiles of the dq pass
   int32_t pad;
 };
 
-// One row tile whose keys several items shared.
+// One row tile whose keys, or key tile whose rows, several items shared.
 struct AttnJoin {
-  int64_t q0;
-  int32_t nq, kvh, row, part0, parts, pad;
+  int64_t t0;                // first query (key) token of the sequence
+  int32_t n, kvh, row;       // its queries (keys), the head, the tile's first row (key)
+  int32_t part0, parts, pad;
 };
 
 constexpr int kAttnThreads = 256;
@@ -55,13 +56,16 @@ struct AttnArgs {
   // workspace
   float* part_o;     // [parts][rows][DP] unnormalised sums, then [parts][rows][2]: max and sum
   float* part_ml;
+  float* part_kv;    // [parts][dk, dv][kAttnKeys][DP]
   float* dsum;       // [queries][heads]: the rows' sums of dout * o
   float* part_bias;  // [kv_heads][row tiles][G][nb]
   float* part_max;   // [kv_heads][row tiles]: the largest |dS| (16-bit floats only)
   int32_t row_tiles;
 };
 
-enum AttnKind { kAttnFwd, kAttnFwdFew, kAttnJoin, kAttnJoinFew, kAttnDq, kAttnDkv };
+enum AttnKind {
+  kAttnFwd, kAttnFwdFew, kAttnJoin, kAttnJoinFew, kAttnDq, kAttnDkv, kAttnDkvJoin
+};
 
 // Launch one pass; dp is the padded head size (32, 64 or 128), grid the number of
 // work-groups.

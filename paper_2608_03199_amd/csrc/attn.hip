@@ -27,10 +27,11 @@ struct sieve_attn {
   bool few = false;          // every tile of rows has at most kAttnFewRows
   int32_t row_tiles = 0;     // dq tiles of one key head
   int32_t parts = 0;         // partial results of the forward pass
-  int32_t nfwd = 0, ndq = 0, ndkv = 0, njoins = 0;
+  int32_t kv_parts = 0;      // partial results of dk and dv
+  int32_t nfwd = 0, ndq = 0, ndkv = 0, njoins = 0, nkv_joins = 0;
   void* mem = nullptr;       // everything below
   const AttnItem *fwd = nullptr, *dq = nullptr, *dkv = nullptr;
-  const AttnJoin* joins = nullptr;
+  const AttnJoin *joins = nullptr, *kv_joins = nullptr;
   const int16_t *bucket_of = nullptr, *range = nullptr;
 };
 
@@ -42,6 +43,11 @@ constexpr int64_t kMaxRows = (int64_t(1) << 31) - (int64_t(1) << 16);
 // kMinKeys to an item (below that the joining costs more than the reading).
 constexpr int kWantItems = 1024;
 constexpr int kMinKeys = 512;
+// The same for dK and dV, whose items are tiles of keys and share out their rows.  More items
+// than the GPU holds at once (two to each of 256 CUs) also even out the causal tiles, the
+// first of which are seen by every row and the last by few.
+constexpr int kWantKvItems = 1024;
+constexpr int kMinRows = 1024;
 
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 
@@ -81,6 +87,39 @@ void order_items(std::vector<AttnItem>& items) {
   for (size_t i = 0; at < (size_t)n; ++i)
     for (int x = 0; x < kXcds; ++x)
       if (i < runs[x].size()) items[at++] = runs[x][i];
+}
+
+// Cuts the ranges of a list that is too short for the GPU into shares of about the same
+// length, a multiple of 128 and at least `least`; join_of(item) starts the record that brings
+// an item's shares together.
+template <typename F>
+void share_out(std::vector<AttnItem>& items, std::vector<AttnJoin>& joins, int want, int least,
+               int32_t& parts, F join_of) {
+  if (items.empty() || (int64_t)items.size() >= 2 * (int64_t)want) return;
+  int64_t total = 0;
+  for (const auto& x : items) total += x.hi - x.lo;
+  const int64_t share = std::max<int64_t>(least, (total / want + 127) / 128 * 128);
+  std::vector<AttnItem> cut;
+  for (const auto& x : items) {
+    const int64_t length = (int64_t)x.hi - x.lo, n = (length + share / 2) / share;
+    if (n < 2) {
+      cut.push_back(x);
+      continue;
+    }
+    const int64_t each = ((length + n - 1) / n + 127) / 128 * 128;
+    AttnJoin j = join_of(x);
+    j.part0 = parts;
+    for (int64_t at = x.lo; at < x.hi; at += each) {
+      AttnItem y = x;
+      y.lo = (int32_t)at;
+      y.hi = (int32_t)std::min<int64_t>(at + each, x.hi);
+      y.part = parts++;
+      ++j.parts;
+      cut.push_back(y);
+    }
+    joins.push_back(j);
+  }
+  items.swap(cut);
 }
 
 int check_desc(const sieve_attn_desc& c) {
@@ -154,7 +193,7 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
   p->row_tiles = (int32_t)row_tiles;
 
   std::vector<AttnItem> fwd, dq, dkv;
-  std::vector<AttnJoin> joins;
+  std::vector<AttnJoin> joins, kv_joins;
   const int tile = p->few ? kAttnFewRows : kAttnRows;
   int32_t tile0 = 0;
   for (int64_t s = 0; s < c.nseq; ++s) {
@@ -186,6 +225,7 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
         dq.push_back(x);
       }
       x.hi = (int32_t)rows;
+      x.part = -1;
       for (int64_t k = 0; k < x.nk; k += kAttnKeys) {
         x.row = (int32_t)k;
         x.lo = c.causal ? (int32_t)std::clamp<int64_t>((k - shift) * G, 0, rows) : 0;
@@ -193,32 +233,11 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
       }
     }
   }
-  // too few items to fill the GPU: share the keys of the long ones out
-  if (!fwd.empty() && fwd.size() < kWantItems) {
-    int64_t total = 0;
-    for (const auto& x : fwd) total += x.hi;
-    const int64_t share =
-        std::max<int64_t>(kMinKeys, ((total / kWantItems + 127) / 128) * 128);
-    std::vector<AttnItem> cut;
-    for (const auto& x : fwd) {
-      const int n = (int)((x.hi + share / 2) / share);
-      if (n < 2) {
-        cut.push_back(x);
-        continue;
-      }
-      const int each = ((x.hi + n - 1) / n + 127) / 128 * 128;
-      AttnJoin j{x.q0, x.nq, x.kvh, x.row, p->parts, 0, 0};
-      AttnItem y = x;
-      for (y.lo = 0; y.lo < x.hi; y.lo += each) {
-        y.hi = std::min(y.lo + each, x.hi);
-        y.part = p->parts++;
-        ++j.parts;
-        cut.push_back(y);
-      }
-      joins.push_back(j);
-    }
-    fwd.swap(cut);
-  }
+  // too few items to fill the GPU: share the keys (the rows) of the long ones out
+  share_out(fwd, joins, kWantItems, kMinKeys, p->parts,
+            [](const AttnItem& x) { return AttnJoin{x.q0, x.nq, x.kvh, x.row, 0, 0, 0}; });
+  share_out(dkv, kv_joins, kWantKvItems, kMinRows, p->kv_parts,
+            [](const AttnItem& x) { return AttnJoin{x.k0, x.nk, x.kvh, x.row, 0, 0, 0}; });
   order_items(fwd);
   order_items(dq);
   order_items(dkv);
@@ -240,10 +259,11 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
   p->ndq = (int32_t)dq.size();
   p->ndkv = (int32_t)dkv.size();
   p->njoins = (int32_t)joins.size();
+  p->nkv_joins = (int32_t)kv_joins.size();
 
   // one allocation, one copy
   std::vector<uint8_t> host;
-  size_t at[6];
+  size_t at[7];
   auto add = [&](int i, const void* v, size_t bytes) {
     at[i] = host.size();
     host.resize(round256(host.size() + bytes));
@@ -255,6 +275,7 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
   add(3, joins.data(), joins.size() * sizeof(AttnJoin));
   add(4, buckets.data(), buckets.size() * sizeof(int16_t));
   add(5, range.data(), range.size() * sizeof(int16_t));
+  add(6, kv_joins.data(), kv_joins.size() * sizeof(AttnJoin));
   ENC_HIP_TRY(hipGetDevice(&p->device));
   if (host.empty()) return SIEVE_OK;
   ENC_HIP_TRY(hipMalloc(&p->mem, host.size()));
@@ -267,6 +288,7 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
   p->joins = (const AttnJoin*)(m + at[3]);
   p->bucket_of = (const int16_t*)(m + at[4]);
   p->range = (const int16_t*)(m + at[5]);
+  p->kv_joins = (const AttnJoin*)(m + at[6]);
   return SIEVE_OK;
 }
 
@@ -282,14 +304,15 @@ FwdSpace fwd_space(const sieve_attn* p) {
   return s;
 }
 struct BwdSpace {
-  int64_t bias, most, bytes;
+  int64_t bias, most, kv, bytes;
 };
 BwdSpace bwd_space(const sieve_attn* p) {
   BwdSpace s;
   const int64_t tiles = (int64_t)p->row_tiles * p->kv_heads;
   s.bias = round256(p->queries * p->heads * (int64_t)sizeof(float));
   s.most = s.bias + round256(tiles * (p->heads / p->kv_heads) * p->nb * (int64_t)sizeof(float));
-  s.bytes = s.most + (p->dtype == SIEVE_F16 ? tiles * (int64_t)sizeof(float) : 0);
+  s.kv = s.most + round256(p->dtype == SIEVE_F16 ? tiles * (int64_t)sizeof(float) : 0);
+  s.bytes = s.kv + (int64_t)p->kv_parts * 2 * kAttnKeys * p->dp * (int64_t)sizeof(float);
   return s;
 }
 
@@ -479,6 +502,7 @@ SIEVE_API int sieve_attn_backward(const sieve_attn* plan, const sieve_heads* dou
   a.dsum = (float*)w;
   a.part_bias = (float*)(w + sp.bias);
   a.part_max = (float*)(w + sp.most);
+  a.part_kv = (float*)(w + sp.kv);
   hipStream_t s = (hipStream_t)stream;
   a.items = p->dq;
   a.nitems = p->ndq;
@@ -486,5 +510,8 @@ SIEVE_API int sieve_attn_backward(const sieve_attn* plan, const sieve_heads* dou
   a.items = p->dkv;
   a.nitems = p->ndkv;
   ENC_HIP_TRY(launch(p, kAttnDkv, a, p->ndkv + (dbias ? p->heads : 0), s));
+  a.joins = p->kv_joins;
+  a.njoins = p->nkv_joins;
+  ENC_HIP_TRY(launch(p, kAttnDkvJoin, a, p->nkv_joins, s));
   return SIEVE_OK;
 }

@@ -192,6 +192,11 @@ struct Stage {
   static __device__ __forceinline__ int col(int i) {
     return ((threadIdx.x + i * kAttnThreads) % kPieces) * kE;
   }
+  // the type of an offset within a tile
+  static __device__ __forceinline__ auto off_zero() {
+    if constexpr (kVec) return 0;
+    else return (int64_t)0;
+  }
   static __device__ __forceinline__ bool mine(int i) {
     return kAll % kAttnThreads == 0 || threadIdx.x + i * kAttnThreads < kAll;
   }
@@ -576,7 +581,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 template <typename T, int DP, int ROWS>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
   const AttnJoin j = a.joins[blockIdx.x];
-  const int rows = j.nq * a.G;
+  const int rows = j.n * a.G;
   for (int i = threadIdx.x / 8; i < ROWS; i += kAttnThreads / 8) {
     const int r = j.row + i;
     if (r >= rows) break;
@@ -606,7 +611,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int tok = query_of(a, r);
     const int head = j.kvh * a.G + (r - tok * a.G);
-    T* to = (T*)a.o.data + (j.q0 + tok) * a.o.token_stride + head * a.o.head_stride;
+    T* to = (T*)a.o.data + (j.t0 + tok) * a.o.token_stride + head * a.o.head_stride;
 #pragma unroll
     for (int e = 0; e < kN / 4; ++e)
 #pragma unroll
@@ -615,7 +620,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
         if (col < a.d) to[col] = (T)(v[4 * e + t] * inv);
       }
     if (a.lse && (threadIdx.x & 7) == 0)
-      a.lse[(j.q0 + tok) * a.heads + head] =
+      a.lse[(j.t0 + tok) * a.heads + head] =
           l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
   }
 }
@@ -631,9 +636,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
 // a constant step from row i - 1's), and adds the result to its own sums by position.  No
 // atomics: the order of additions is the program's.
 
-template <typename T, int DP>
+// With a bias the tile is 32 keys, so that two work-groups' LDS fits a CU beside the sums.
+template <typename T, int DP, bool kBias>
 struct DqShape {
-  static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 ? 2 : 1;
+  static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 && !kBias ? 2 : 1;
   static constexpr int kTile = 32 * kBlocks;
   static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
   static constexpr int kBytes = 2 * kBufs * kTile * lds_row<T, DP>() * (int)sizeof(T);
@@ -682,7 +688,7 @@ __device__ __forceinline__ void add_diagonals(const AttnArgs& a, const AttnItem&
 
 template <typename T, int DP, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
-  using Shape = DqShape<T, DP>;
+  using Shape = DqShape<T, DP, kBias>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
   constexpr int kTileN = kTile * lds_row<T, DP>();
   constexpr bool kScaled = __is_same(T, f16);
@@ -690,9 +696,10 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_k = (T*)smem;
   T* s_v = s_k + Shape::kBufs * kTileN;
   float* s_bias = (float*)(smem + Shape::kBytes);
-  float* s_sum = s_bias + a.G * a.span;             // [wave][G][span]
-  float* s_far = s_sum + kAttnWaves * a.G * a.span;  // [wave][half][32][2]
-  float* s_diag = s_far + kAttnWaves * 128;          // [wave][kDiagWords]
+  float* s_diag = s_bias;                            // [wave][kDiagWords]
+  float* s_far = s_diag + kAttnWaves * kDiagWords;   // [wave][half][32][2]
+  if (kBias && a.dbias) s_bias = s_far + kAttnWaves * 128;
+  float* s_sum = s_bias + a.G * a.span;              // [wave][G][span]
   __shared__ float s_max[kAttnWaves];
   const AttnItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
@@ -743,7 +750,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     load_bias<T>(a, it.kvh, s_bias);
     if (want_bias) {
       for (int i = threadIdx.x; i < kAttnWaves * G * a.span; i += kAttnThreads) s_sum[i] = 0.f;
-      for (int i = threadIdx.x; i < kAttnWaves * kDiagWords; i += kAttnThreads) s_diag[i] = 0.f;
+      for (int i = threadIdx.x; i < kAttnWaves * kDiagWords / 4; i += kAttnThreads)
+        ((f32x4*)s_diag)[i] = f32x4{};
     }
     __syncthreads();
     table = s_bias + me.g * a.span;
@@ -984,53 +992,64 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const T* q0 = (const T*)a.q.data + it.q0 * a.q.token_stride + it.kvh * G * a.q.head_stride;
   const T* do0 =
       (const T*)a.dout.data + it.q0 * a.dout.token_stride + it.kvh * G * a.dout.head_stride;
-  auto fetch = [&](int base) {
+  // Offsets of a tile's pieces and rows from its first query.  Where G divides the tile they
+  // are the same for every tile.
+  const bool fixed = a.g_shift >= 0 && G <= 32;
+  const bool row_mine = threadIdx.x < kTile;
+  // a row without keys is only possible with a mask or a table that holds -infinity
+  const bool some_empty = a.key_mask || kBias;
+  typedef decltype(Tile::off_zero()) Off;
+  Off off_q[kN], off_do[kN];
+  int off_lse[kN], off_row = 0, tok_row = 0;
+  auto offsets = [&](int base) {
     const int tok0 = query_of(a, base);
-    auto at = [&](const sieve_heads& x, int i) {
-      const int r = base + Tile::row(i), tok = query_of(a, r);
-      if constexpr (kVec)
-        return (tok - tok0) * (int)x.token_stride + (r - tok * G) * (int)x.head_stride +
-               Tile::col(i);
-      else
-        return (tok - tok0) * x.token_stride + (r - tok * G) * x.head_stride + Tile::col(i);
-    };
-    st_q.load(q0 + tok0 * a.q.token_stride, [&](int i) { return at(a.q, i); }, it.hi - base, d);
-    st_do.load(do0 + tok0 * a.dout.token_stride, [&](int i) { return at(a.dout, i); },
-               it.hi - base, d);
-    auto stat = [&](int r) {
-      const int tok = query_of(a, r);
-      return (int64_t)tok * a.heads + (r - tok * G);
-    };
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int r = base + Tile::row(i);
-      piece_lse[i] = r < it.hi ? lse0[stat(r)] : -INFINITY;
+      const int r = base + Tile::row(i), tok = query_of(a, r);
+      const Off t = tok - tok0, g = r - tok * G;
+      off_q[i] = t * (Off)a.q.token_stride + g * (Off)a.q.head_stride + Tile::col(i);
+      off_do[i] = t * (Off)a.dout.token_stride + g * (Off)a.dout.head_stride + Tile::col(i);
+      off_lse[i] = (int)t * a.heads + (int)g;
     }
-    if (threadIdx.x < kTile) {
-      const int r = base + threadIdx.x;
+    const int r = base + (int)threadIdx.x, tok = query_of(a, r);
+    tok_row = tok - tok0;
+    off_row = tok_row * a.heads + (r - tok * G);
+    if (kBias) row_off = (r - tok * G) * a.span;
+  };
+  auto fetch = [&](int base) {
+    if (!fixed) offsets(base);
+    const int tok0 = query_of(a, base);
+    st_q.load(q0 + tok0 * a.q.token_stride, [&](int i) { return off_q[i]; }, it.hi - base, d);
+    st_do.load(do0 + tok0 * a.dout.token_stride, [&](int i) { return off_do[i]; }, it.hi - base, d);
+    const float* lse = lse0 + (int64_t)tok0 * a.heads;
+    if (some_empty) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+        piece_lse[i] = base + Tile::row(i) < it.hi ? lse[off_lse[i]] : -INFINITY;
+    }
+    if (row_mine) {
       row_lse = -INFINITY;
       row_d = 0.f;
-      row_off = row_pos = 0;
-      if (r < it.hi) {
-        const int64_t j = stat(r);
-        row_lse = lse0[j];
-        row_d = dsum0[j];
-        const int tok = query_of(a, r);
-        row_pos = tok + shift;
-        if (kBias) row_off = (r - tok * G) * a.span;
+      row_pos = tok0 + tok_row + shift;
+      if (base + (int)threadIdx.x < it.hi) {
+        row_lse = lse[off_row];
+        row_d = (dsum0 + (int64_t)tok0 * a.heads)[off_row];
       }
     }
   };
+  offsets(it.lo);
   auto put = [&](int b) {
+    if (some_empty) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i)
-      if (piece_lse[i] == -INFINITY) {
-        st_q.drop(i);
-        st_do.drop(i);
-      }
+      for (int i = 0; i < kN; ++i)
+        if (piece_lse[i] == -INFINITY) {
+          st_q.drop(i);
+          st_do.drop(i);
+        }
+    }
     st_q.store(s_q + b * kTileN);
     st_do.store(s_do + b * kTileN);
-    if (threadIdx.x < kTile) {
+    if (row_mine) {
       float* p = s_row + b * 4 * kTile + threadIdx.x;
       p[0] = row_lse == -INFINITY ? INFINITY : row_lse * kLog2e;
       p[kTile] = -row_d;
@@ -1174,11 +1193,46 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = f32x16{};
   }
+  if (it.part >= 0) {
+    float* p = a.part_kv + ((int64_t)it.part * 2 * kAttnKeys + wave * 32 + (lane & 31)) * DP;
+    const float fk = a.scale / up, fv = kScaled ? 0x1p-14f : 1.f;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int col = 32 * b + 8 * g + 4 * h;
+        *(f32x4*)(p + col) = f32x4{dk[b][4 * g] * fk, dk[b][4 * g + 1] * fk,
+                                   dk[b][4 * g + 2] * fk, dk[b][4 * g + 3] * fk};
+        *(f32x4*)(p + kAttnKeys * DP + col) =
+            f32x4{dv[b][4 * g] * fv, dv[b][4 * g + 1] * fv, dv[b][4 * g + 2] * fv,
+                  dv[b][4 * g + 3] * fv};
+      }
+    return;
+  }
   const int64_t tok = it.k0 + key;
   store_row<T, DP, kVec>((T*)a.dk.data + tok * a.dk.token_stride + it.kvh * a.dk.head_stride, dk,
                    a.scale / up, d, h);
   store_row<T, DP, kVec>((T*)a.dv.data + tok * a.dv.token_stride + it.kvh * a.dv.head_stride, dv,
                    kScaled ? 0x1p-14f : 1.f, d, h);
+}
+
+// Partial sums of one key tile to its gradients.
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads) void attn_dkv_join_kernel(AttnArgs a) {
+  const AttnJoin j = a.joins[blockIdx.x];
+  constexpr int kAll = 2 * kAttnKeys * DP / 4;  // values, four a thread
+  for (int i = threadIdx.x; i < kAll; i += kAttnThreads) {
+    const int col = i % (DP / 4) * 4, key = j.row + i / (DP / 4) % kAttnKeys;
+    if (key >= j.n || col >= a.d) continue;
+    f32x4 v = {};
+    const f32x4* p = (const f32x4*)a.part_kv + (int64_t)j.part0 * kAll + i;
+    for (int n = 0; n < j.parts; ++n) v += p[(int64_t)n * kAll];
+    const sieve_heads& to = i < kAll / 2 ? a.dk : a.dv;
+    T* t = (T*)to.data + (j.t0 + key) * to.token_stride + j.kvh * to.head_stride + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.d) t[e] = (T)v[e];
+  }
 }
 
 // ---- launch ----------------------------------------------------------------------------------
@@ -1211,7 +1265,7 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
       const size_t sums =
           a.dbias ? kAttnWaves * (table + (128 + kDiagWords) * sizeof(float)) : 0;
       return launch(attn_dq_kernel<T, DP, kBias, kVec>, a, grid,
-                    DqShape<T, DP>::kBytes + table + sums, s);
+                    DqShape<T, DP, kBias>::kBytes + table + sums, s);
     }
     case kAttnDkv:
       return launch(attn_dkv_kernel<T, DP, kBias, kVec>, a, grid,
@@ -1223,6 +1277,7 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
 
 template <typename T, int DP>
 hipError_t launch_dp(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
+  if (kind == kAttnDkvJoin) return launch(attn_dkv_join_kernel<T, DP>, a, grid, 0, s);
   if (kind == kAttnJoin) return launch(attn_join_kernel<T, DP, kAttnRows>, a, grid, 0, s);
   if (kind == kAttnJoinFew) return launch(attn_join_kernel<T, DP, kAttnFewRows>, a, grid, 0, s);
   if (a.bias)
