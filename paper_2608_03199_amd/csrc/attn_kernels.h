@@ -18,9 +18,10 @@
 //   8-byte reads for 16-bit values, eight 4-byte reads for 32-bit ones.  Probabilities
 //   never pass through LDS.
 //
-// The key and value tiles go through registers into LDS rows padded by 16 bytes, loaded
-// one tile ahead.  Rows that a mask leaves out, or past the sequence's end, are stored as
-// zeros: what they hold never meets a product.
+// The tiles are loaded one ahead, straight into LDS where the rows may be moved in 16-byte
+// pieces.  An LDS row's pieces are permuted by its number (piece_of) so that both ways to
+// read a tile touch every bank equally.  Rows that a mask leaves out, or past the sequence's
+// end, are zeros there: what they hold never meets a product.
 //
 // P and dS are rounded to the inputs' type for the second products, as those run on the
 // 16-bit matrix units; S, dP, the statistics and every accumulator are fp32.  bfloat16
@@ -65,52 +66,84 @@ __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
   return c;
 }
 
-// Row stride of an LDS tile.
+// An LDS tile has rows of DP values.  Piece c (16 bytes) of row r lies at piece
+// c ^ piece_of(r) of the row.  64 banks of 4 bytes hold 16 pieces: a row (or two, or four of
+// the shorter ones).  Along the head (32 rows, one piece of each) and across the rows (4 rows
+// by 2 or 4 neighbouring pieces, twice) every 16 pieces then fall on 16 different places.
 template <typename T, int DP>
-constexpr int lds_row() {
-  return DP + 16 / (int)sizeof(T);
+__device__ __forceinline__ int piece_of(int row) {
+  constexpr int kPieces = DP * (int)sizeof(T) / 16;
+  if constexpr (kPieces >= 16) return (row & 3) << 2 | (row >> 2 & 3);
+  else if constexpr (kPieces == 8) return (row & 2) << 1 | (row >> 2 & 3);
+  else return row >> 2 & 3;
 }
 
-// Values 16 c + 8 h .. + 7 of a row: the operand whose summed axis is the head's.
+// Values 16 c + 8 h .. + 7 of the rows row0 + lane % 32 (row0 a multiple of 32): the operand
+// whose summed axis is the head's.
 template <typename T, int DP>
-__device__ __forceinline__ vec8<T> frag_along(const T* s, int row, int c, int h) {
-  const EncVec<T, 8> q = enc_load<T, 8>(s + row * lds_row<T, DP>() + 16 * c + 8 * h);
-  return __builtin_bit_cast(vec8<T>, q);
-}
-
-// Value col + lane % 32 of the rows row + {4 h + 0..3, 8 + 4 h + 0..3}: the operand whose
-// summed axis is the tile's rows.  The transposing read gives lane i of each 16 the i-th
-// column of the 4 rows that the 16 lanes' addresses cover.
-template <typename T, int DP>
-__device__ __forceinline__ vec8<T> frag_across(const T* s, int row, int col, int lane) {
-  constexpr int kLd = lds_row<T, DP>();
-  const int h = lane >> 5;
+__device__ __forceinline__ vec8<T> frag_along(const T* s, int row0, int c, int lane) {
+  constexpr int kE = 16 / (int)sizeof(T);
+  const int row = lane & 31, h = lane >> 5;
+  // the first piece's place; the others differ in the bits that c sets
+  const int at = row * DP + (((8 / kE) * h) ^ piece_of<T, DP>(row)) * kE;
+  const T* p = s + row0 * DP;
   if constexpr (sizeof(T) == 2) {
-    const int i = lane & 15;
-    const T* p = s + (row + 4 * h + (i >> 2)) * kLd + col + (lane & 16) + (i & 3) * 4;
+    return __builtin_bit_cast(vec8<T>, enc_load<T, 8>(p + (at ^ (16 * c))));
+  } else {
+    EncVec<T, 4> q[2] = {enc_load<T, 4>(p + (at ^ (16 * c))),
+                         enc_load<T, 4>(p + (at ^ (16 * c) ^ 4))};
+    return __builtin_bit_cast(vec8<T>, q);
+  }
+}
+
+// The same place, written.
+template <typename T, int DP>
+__device__ __forceinline__ void put_along(T* s, int row0, int c, int lane, vec8<T> v) {
+  constexpr int kE = 16 / (int)sizeof(T);
+  const int row = lane & 31, h = lane >> 5;
+  const int at = row * DP + (((8 / kE) * h) ^ piece_of<T, DP>(row)) * kE;
+  T* p = s + row0 * DP;
+  const EncVec<T, 8> q = __builtin_bit_cast(EncVec<T, 8>, v);
+  if constexpr (sizeof(T) == 2) {
+    enc_store<T, 8>(p + (at ^ (16 * c)), q);
+  } else {
+    enc_store<T, 4>(p + (at ^ (16 * c)), EncVec<T, 4>{q.v[0], q.v[1], q.v[2], q.v[3]});
+    enc_store<T, 4>(p + (at ^ (16 * c) ^ 4), EncVec<T, 4>{q.v[4], q.v[5], q.v[6], q.v[7]});
+  }
+}
+
+// Value col + lane % 32 of the rows row0 + {4 h + 0..3, 8 + 4 h + 0..3} (row0 a multiple of
+// 16, col of 32): the operand whose summed axis is the tile's rows.  The transposing read
+// gives lane i of each 16 the i-th column of the 4 rows that the 16 lanes' addresses cover.
+template <typename T, int DP>
+__device__ __forceinline__ vec8<T> frag_across(const T* s, int row0, int col, int lane) {
+  constexpr int kE = 16 / (int)sizeof(T);
+  const int h = lane >> 5;
+  const T* p = s + row0 * DP;
+  if constexpr (sizeof(T) == 2) {
+    const int i = lane & 15, row = 4 * h + (i >> 2);
+    const int piece = (lane >> 3 & 2) + (i >> 1 & 1);
+    const int at = row * DP + (piece ^ piece_of<T, DP>(row)) * kE + (i & 1) * 4;
+    // 8 rows on, piece_of differs in bit 1
+    const int next = (at ^ (2 * kE)) + 8 * DP;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     union {
       s16x4 half[2];
       vec8<T> all;
     } u;
-    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kLd));
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (at ^ col)));
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (next ^ col)));
     return u.all;
   } else {
-    const T* p = s + (row + 4 * h) * kLd + col + (lane & 31);
     vec8<T> r;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      r[j] = p[j * kLd];
-      r[4 + j] = p[(8 + j) * kLd];
+    for (int j = 0; j < 8; ++j) {
+      const int row = 4 * h + (j & 3) + (j & 4) * 2;
+      const int at = ((lane & 31) / kE ^ piece_of<T, DP>(row)) * kE + lane % kE;
+      r[j] = p[row * DP + (at ^ col)];
     }
     return r;
   }
-}
-
-template <typename T>
-__device__ __forceinline__ EncVec<T, 8> as_vec(vec8<T> v) {
-  return __builtin_bit_cast(EncVec<T, 8>, v);
 }
 
 // Registers 8 s .. 8 s + 7 as an operand, rounded to nearest.
@@ -171,26 +204,42 @@ struct Buffer {
     return __builtin_bit_cast(enc_u32x4,
                               __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)offset, 0, 0));
   }
+  // into LDS, 16 bytes a lane from `to`, which the wave shares
+  __device__ __forceinline__ void load_lds(uint32_t offset, void* to) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void*)to, 16, (int)offset, 0, 0, 0);
+  }
 };
 
-// A tile of ROWS rows on its way from global memory through registers into LDS.  Whether a
-// row counts (a mask, a row without keys) is itself loaded: the rows are loaded without
-// waiting for it, and dropped on their way into LDS.
+// Waits for the wave's own loads (gfx9 encoding: vmcnt 0, the other counts not waited for).
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+  asm volatile("" ::: "memory");
+}
+
+// A tile of ROWS rows on its way from global memory into LDS, a 16-byte piece a thread at a
+// time in the order of their places.  Whether a row counts (a mask, a row without keys) is
+// itself loaded: the rows are loaded without waiting for it, and cleared when both are there.
 // kVec: the rows may be moved in 16-byte pieces and a tile spans less than 2^31 bytes.
-template <typename T, int DP, int ROWS, bool kVec>
+// kDirect: the loads write LDS themselves (the buffer they go to is not being read).
+template <typename T, int DP, int ROWS, bool kVec, bool kDirect>
 struct Stage {
+  static_assert(kVec || !kDirect);
   static constexpr int kE = 16 / sizeof(T);           // values of a 16-byte piece
   static constexpr int kPieces = DP / kE;             // pieces of a row
   static constexpr int kAll = ROWS * kPieces;
   static constexpr int kN = (kAll + kAttnThreads - 1) / kAttnThreads;
-  enc_u32x4 r[kN];
+  static_assert(kAll % 64 == 0);
+  static constexpr bool kDirectLoads = kDirect;
+  enc_u32x4 r[kDirect ? 1 : kN];
 
   // row and first value of this thread's piece i
   static __device__ __forceinline__ int row(int i) {
     return (threadIdx.x + i * kAttnThreads) / kPieces;
   }
   static __device__ __forceinline__ int col(int i) {
-    return ((threadIdx.x + i * kAttnThreads) % kPieces) * kE;
+    return ((threadIdx.x + i * kAttnThreads) % kPieces ^ piece_of<T, DP>(row(i))) * kE;
   }
   // the type of an offset within a tile
   static __device__ __forceinline__ auto off_zero() {
@@ -200,53 +249,65 @@ struct Stage {
   static __device__ __forceinline__ bool mine(int i) {
     return kAll % kAttnThreads == 0 || threadIdx.x + i * kAttnThreads < kAll;
   }
-  // at(i): piece i's offset in values from base; rows: how many of the tile's there are
+  // at(i): piece i's offset in values from base; rows: how many of the tile's there are;
+  // s: the tile's place in LDS
   template <typename F>
-  __device__ __forceinline__ void load(const T* base, F at, int rows, int d) {
+  __device__ __forceinline__ void load(const T* base, F at, int rows, int d, T* s) {
     const Buffer from(base);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const bool there = mine(i) && row(i) < rows && col(i) < d;
-      if constexpr (kVec) {
-        r[i] = from.load(there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere);
+      const bool there = row(i) < rows && col(i) < d;
+      if constexpr (kDirect) {
+        if (mine(i))
+          from.load_lds(there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere,
+                        s + (i * kAttnThreads + (threadIdx.x & ~63)) * kE);
+      } else if constexpr (kVec) {
+        r[i] = from.load(mine(i) && there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere);
       } else {
         EncVec<T, kE> q;
 #pragma unroll
-        for (int j = 0; j < kE; ++j) q.v[j] = there && col(i) + j < d ? base[at(i) + j] : (T)0.f;
+        for (int j = 0; j < kE; ++j)
+          q.v[j] = mine(i) && there && col(i) + j < d ? base[at(i) + j] : (T)0.f;
         r[i] = __builtin_bit_cast(enc_u32x4, q);
       }
     }
   }
-  __device__ __forceinline__ void drop(int i) { r[i] = enc_u32x4{0, 0, 0, 0}; }
-  __device__ __forceinline__ void store(T* s) const {
+  // the pieces are in LDS after this and the next barrier; keep(i): whether piece i counts
+  template <typename F>
+  __device__ __forceinline__ void store(T* s, bool check, F keep) {
+    if constexpr (kDirect) {
+      if (check) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i)
-      if (mine(i)) *(enc_u32x4*)(s + row(i) * lds_row<T, DP>() + col(i)) = r[i];
+        for (int i = 0; i < kN; ++i)
+          if (mine(i) && !keep(i))
+            *(enc_u32x4*)(s + (threadIdx.x + i * kAttnThreads) * kE) = enc_u32x4{0, 0, 0, 0};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+        if (mine(i))
+          *(enc_u32x4*)(s + (threadIdx.x + i * kAttnThreads) * kE) =
+              check && !keep(i) ? enc_u32x4{0, 0, 0, 0} : r[i];
+    }
   }
 };
 
 // The keys and values of a tile, and what the mask says of their rows.
-template <typename T, int DP, int KEYS, bool kVec>
+template <typename T, int DP, int KEYS, bool kVec, bool kDirect>
 struct KeyStage {
-  using Tile = Stage<T, DP, KEYS, kVec>;
+  using Tile = Stage<T, DP, KEYS, kVec, kDirect>;
   Tile k, v;
   uint8_t keep[Tile::kN];
 
   // k0, v0: the sequence's first row; keys base .. hi - 1 at most
   __device__ __forceinline__ void load(const AttnArgs& a, const uint8_t* mask, const T* k0,
-                                       const T* v0, int base, int hi) {
-    const int64_t ks = a.k.token_stride, vs = a.v.token_stride;
-    if constexpr (kVec) {
-      k.load(k0 + base * ks, [&](int i) { return Tile::row(i) * (int)ks + Tile::col(i); },
-             hi - base, a.d);
-      v.load(v0 + base * vs, [&](int i) { return Tile::row(i) * (int)vs + Tile::col(i); },
-             hi - base, a.d);
-    } else {
-      k.load(k0 + base * ks, [&](int i) { return Tile::row(i) * ks + Tile::col(i); }, hi - base,
-             a.d);
-      v.load(v0 + base * vs, [&](int i) { return Tile::row(i) * vs + Tile::col(i); }, hi - base,
-             a.d);
-    }
+                                       const T* v0, int base, int hi, T* s_k, T* s_v) {
+    typedef decltype(Tile::off_zero()) Off;
+    const Off ks = (Off)a.k.token_stride, vs = (Off)a.v.token_stride;
+    k.load(k0 + base * a.k.token_stride, [&](int i) { return Tile::row(i) * ks + Tile::col(i); },
+           hi - base, a.d, s_k);
+    v.load(v0 + base * a.v.token_stride, [&](int i) { return Tile::row(i) * vs + Tile::col(i); },
+           hi - base, a.d, s_v);
     if (mask) {
 #pragma unroll
       for (int i = 0; i < Tile::kN; ++i) {
@@ -256,16 +317,9 @@ struct KeyStage {
     }
   }
   __device__ __forceinline__ void store(const uint8_t* mask, T* s_k, T* s_v) {
-    if (mask) {
-#pragma unroll
-      for (int i = 0; i < Tile::kN; ++i)
-        if (!keep[i]) {
-          k.drop(i);
-          v.drop(i);
-        }
-    }
-    k.store(s_k);
-    v.store(s_v);
+    if (kDirect) wait_loads();
+    k.store(s_k, mask != nullptr, [&](int i) { return keep[i] != 0; });
+    v.store(s_v, mask != nullptr, [&](int i) { return keep[i] != 0; });
   }
 };
 
@@ -382,8 +436,8 @@ template <typename T, int DP, int WK>
 struct FwdShape {
   static constexpr int kBlocks = WK == 1 && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave
   static constexpr int kTile = 32 * kBlocks * WK;                    // keys of a tile
-  static constexpr int kBufs = WK == 1 ? 2 : 1;
-  static constexpr int kTileBytes = kTile * lds_row<T, DP>() * (int)sizeof(T);
+  static constexpr int kTileBytes = kTile * DP * (int)sizeof(T);
+  static constexpr int kBufs = 4 * kTileBytes <= 128 * 1024 ? 2 : 1;
   static constexpr int kStageBytes = 2 * kBufs * kTileBytes;
   static constexpr int kJoinBytes = WK == 1 ? 0 : (WK * 32 * (DP + 4) + 2 * WK * 32) * 4;
   static constexpr int kBytes = kStageBytes > kJoinBytes ? kStageBytes : kJoinBytes;
@@ -394,7 +448,7 @@ template <typename T, int DP, int WK, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_forward_kernel(AttnArgs a) {
   using Shape = FwdShape<T, DP, WK>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
-  constexpr int kTileN = kTile * lds_row<T, DP>();
+  constexpr int kTileN = kTile * DP;
   extern __shared__ __align__(16) uint8_t smem[];
   T* s_k = (T*)smem;
   T* s_v = s_k + Shape::kBufs * kTileN;
@@ -409,14 +463,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
   const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
-  KeyStage<T, DP, kTile, kVec> stage;
+  KeyStage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2> stage;
   uint8_t ok[kBlocks];
-  auto fetch = [&](int base) {
-    stage.load(a, mask, k0, v0, base, it.hi);
+  auto fetch = [&](int base, int b) {
+    stage.load(a, mask, k0, v0, base, it.hi, s_k + b * kTileN, s_v + b * kTileN);
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) ok[b] = key_ok(mask, base + 32 * ((WK == 1 ? 0 : wave) + b) + (lane & 31), it.hi);
+    for (int i = 0; i < kBlocks; ++i) ok[i] = key_ok(mask, base + 32 * ((WK == 1 ? 0 : wave) + i) + (lane & 31), it.hi);
   };
-  if (it.lo < it.hi) fetch(it.lo);
+  if (it.lo < it.hi) fetch(it.lo, 0);
 
   vec8<T> q[DP / 16];
   {
@@ -452,17 +506,17 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       any |= bits[b];
     }
     const bool more = base + kTile < it.hi;
-    if (more) fetch(base + kTile);
+    if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
     if (wave_live && __any(any != 0)) {
-      const T* sk = s_k + buf * kTileN + (WK == 1 ? 0 : wave * 32) * lds_row<T, DP>();
-      const T* sv = s_v + buf * kTileN + (WK == 1 ? 0 : wave * 32) * lds_row<T, DP>();
+      const T* sk = s_k + buf * kTileN + (WK == 1 ? 0 : wave * 32) * DP;
+      const T* sv = s_v + buf * kTileN + (WK == 1 ? 0 : wave * 32) * DP;
       f32x16 s[kBlocks];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         s[b] = f32x16{};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c)
-          s[b] = mma(frag_along<T, DP>(sk, 32 * b + (lane & 31), c, h), q[c], s[b]);
+          s[b] = mma(frag_along<T, DP>(sk, 32 * b, c, lane), q[c], s[b]);
       }
       float top = -INFINITY;
 #pragma unroll
@@ -641,8 +695,8 @@ template <typename T, int DP, bool kBias>
 struct DqShape {
   static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 && !kBias ? 2 : 1;
   static constexpr int kTile = 32 * kBlocks;
-  static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int kBytes = 2 * kBufs * kTile * lds_row<T, DP>() * (int)sizeof(T);
+  static constexpr int kBufs = 2;
+  static constexpr int kBytes = 2 * kBufs * kTile * DP * (int)sizeof(T);
 };
 constexpr int kAttnWaves = kAttnThreads / 64;
 // A row of the dS block: 32 values, then at least 31 zeros, and 4 words that spread the
@@ -690,15 +744,15 @@ template <typename T, int DP, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
   using Shape = DqShape<T, DP, kBias>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
-  constexpr int kTileN = kTile * lds_row<T, DP>();
+  constexpr int kTileN = kTile * DP;
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
   T* s_k = (T*)smem;
   T* s_v = s_k + Shape::kBufs * kTileN;
   float* s_bias = (float*)(smem + Shape::kBytes);
   float* s_diag = s_bias;                            // [wave][kDiagWords]
-  float* s_far = s_diag + kAttnWaves * kDiagWords;   // [wave][half][32][2]
-  if (kBias && a.dbias) s_bias = s_far + kAttnWaves * 128;
+  float* s_far = s_diag;                             // [wave][half][32][2], after the keys
+  if (kBias && a.dbias) s_bias = s_diag + kAttnWaves * kDiagWords;
   float* s_sum = s_bias + a.G * a.span;              // [wave][G][span]
   __shared__ float s_max[kAttnWaves];
   const AttnItem it = a.items[blockIdx.x];
@@ -712,14 +766,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
   const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
-  KeyStage<T, DP, kTile, kVec> stage;
+  KeyStage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2> stage;
   uint8_t ok[kBlocks];
-  auto fetch = [&](int base) {
-    stage.load(a, mask, k0, v0, base, it.hi);
+  auto fetch = [&](int base, int b) {
+    stage.load(a, mask, k0, v0, base, it.hi, s_k + b * kTileN, s_v + b * kTileN);
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) ok[b] = key_ok(mask, base + 32 * b + (lane & 31), it.hi);
+    for (int i = 0; i < kBlocks; ++i) ok[i] = key_ok(mask, base + 32 * i + (lane & 31), it.hi);
   };
-  if (it.lo < it.hi) fetch(it.lo);
+  if (it.lo < it.hi) fetch(it.lo, 0);
 
   const int64_t at = (it.q0 + me.tok) * a.heads + it.kvh * G + me.g;
   // a row that saw no key has lse = -infinity; as +infinity it makes every P 0
@@ -780,7 +834,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       any |= bits[b];
     }
     const bool more = base + kTile < it.hi;
-    if (more) fetch(base + kTile);
+    if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
     if (wave_live && __any(any != 0)) {
       const T* sk = s_k + buf * kTileN;
       const T* sv = s_v + buf * kTileN;
@@ -789,8 +843,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
-          s = mma(frag_along<T, DP>(sk, 32 * b + (lane & 31), c, h), q[c], s);
-          dp = mma(frag_along<T, DP>(sv, 32 * b + (lane & 31), c, h), dout[c], dp);
+          s = mma(frag_along<T, DP>(sk, 32 * b, c, lane), q[c], s);
+          dp = mma(frag_along<T, DP>(sv, 32 * b, c, lane), dout[c], dp);
         }
         const int first = base + 32 * b;
         finish_scores<kBias>(s, scale2, table, a.distance, me.pos, me.pos_min, me.pos_max, lo, hi,
@@ -881,6 +935,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   }
   if constexpr (kBias) {
     if (!want_bias) return;
+    __syncthreads();
     s_far[(wave * 64 + h * 32 + (lane & 31)) * 2] = me.live ? far_lo : 0.f;
     s_far[(wave * 64 + h * 32 + (lane & 31)) * 2 + 1] = me.live ? far_hi : 0.f;
     __syncthreads();
@@ -926,13 +981,13 @@ template <typename T, int DP>
 struct DkvShape {
   static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 ? 2 : 1;  // 32-row blocks of a tile
   static constexpr int kTile = 32 * kBlocks;
-  static constexpr int kBufs = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int kTileBytes = kTile * lds_row<T, DP>() * (int)sizeof(T);
+  static constexpr int kBufs = 2;
+  static constexpr int kTileBytes = kTile * DP * (int)sizeof(T);
   // The tile's values as operands in registers, or, where the accumulators leave no room
   // for them at two waves a SIMD, in LDS.
   static constexpr bool kValuesInLds = DP * sizeof(T) >= 256;
   static constexpr int kValueBytes =
-      kValuesInLds ? kAttnKeys * lds_row<T, DP>() * (int)sizeof(T) : 0;
+      kValuesInLds ? kAttnKeys * DP * (int)sizeof(T) : 0;
   static constexpr int kBytes = kValueBytes + kBufs * (2 * kTileBytes + 4 * kTile * 4);
 };
 
@@ -960,7 +1015,7 @@ template <typename T, int DP, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
   using Shape = DkvShape<T, DP>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
-  constexpr int kTileN = kTile * lds_row<T, DP>();
+  constexpr int kTileN = kTile * DP;
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
   if (kBias && (int)blockIdx.x >= a.nitems) {
@@ -982,7 +1037,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const bool live = there && (!a.key_mask || a.key_mask[it.k0 + key] != 0);
 
   // Rows that saw no key are zeros whatever they hold: their lse tells, loaded with them.
-  using Tile = Stage<T, DP, kTile, kVec>;
+  using Tile = Stage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2>;
   Tile st_q, st_do;
   constexpr int kN = Tile::kN;
   float piece_lse[kN], row_lse = 0.f, row_d = 0.f;
@@ -1016,11 +1071,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     off_row = tok_row * a.heads + (r - tok * G);
     if (kBias) row_off = (r - tok * G) * a.span;
   };
-  auto fetch = [&](int base) {
+  auto fetch = [&](int base, int b) {
     if (!fixed) offsets(base);
     const int tok0 = query_of(a, base);
-    st_q.load(q0 + tok0 * a.q.token_stride, [&](int i) { return off_q[i]; }, it.hi - base, d);
-    st_do.load(do0 + tok0 * a.dout.token_stride, [&](int i) { return off_do[i]; }, it.hi - base, d);
+    st_q.load(q0 + tok0 * a.q.token_stride, [&](int i) { return off_q[i]; }, it.hi - base, d,
+              s_q + b * kTileN);
+    st_do.load(do0 + tok0 * a.dout.token_stride, [&](int i) { return off_do[i]; }, it.hi - base, d,
+               s_do + b * kTileN);
     const float* lse = lse0 + (int64_t)tok0 * a.heads;
     if (some_empty) {
 #pragma unroll
@@ -1039,16 +1096,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   };
   offsets(it.lo);
   auto put = [&](int b) {
-    if (some_empty) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i)
-        if (piece_lse[i] == -INFINITY) {
-          st_q.drop(i);
-          st_do.drop(i);
-        }
-    }
-    st_q.store(s_q + b * kTileN);
-    st_do.store(s_do + b * kTileN);
+    if (Tile::kDirectLoads) wait_loads();
+    st_q.store(s_q + b * kTileN, some_empty, [&](int i) { return piece_lse[i] != -INFINITY; });
+    st_do.store(s_do + b * kTileN, some_empty, [&](int i) { return piece_lse[i] != -INFINITY; });
     if (row_mine) {
       float* p = s_row + b * 4 * kTile + threadIdx.x;
       p[0] = row_lse == -INFINITY ? INFINITY : row_lse * kLog2e;
@@ -1057,7 +1107,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       ((int*)p)[3 * kTile] = row_pos;
     }
   };
-  if (it.lo < it.hi) fetch(it.lo);
+  if (it.lo < it.hi) fetch(it.lo, 0);
 
   vec8<T> k[DP / 16], v[DP / 16];
   {
@@ -1069,8 +1119,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     if constexpr (Shape::kValuesInLds) {  // a wave reads its own 32 rows only
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c)
-        enc_store<T, 8>(s_val + (wave * 32 + (lane & 31)) * lds_row<T, DP>() + 16 * c + 8 * h,
-                        as_vec<T>(v[c]));
+        put_along<T, DP>(s_val, wave * 32, c, lane, v[c]);
     }
   }
   if constexpr (kBias) load_bias<T>(a, it.kvh, s_bias);
@@ -1093,7 +1142,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   __syncthreads();
   for (int base = it.lo; base < it.hi; base += kTile) {
     const bool more = base + kTile < it.hi;
-    if (more) fetch(base + kTile);
+    if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
     if (wave_live) {
       const T* sq = s_q + buf * kTileN;
       const T* sd = s_do + buf * kTileN;
@@ -1115,13 +1164,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         }
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
-          s = mma(frag_along<T, DP>(sq, 32 * b + (lane & 31), c, h), k[c], s);
+          s = mma(frag_along<T, DP>(sq, 32 * b, c, lane), k[c], s);
           vec8<T> val;
           if constexpr (Shape::kValuesInLds)
-            val = frag_along<T, DP>(s_val, wave * 32 + (lane & 31), c, h);
+            val = frag_along<T, DP>(s_val, wave * 32, c, lane);
           else
             val = v[c];
-          dp = mma(frag_along<T, DP>(sd, 32 * b + (lane & 31), c, h), val, dp);
+          dp = mma(frag_along<T, DP>(sd, 32 * b, c, lane), val, dp);
         }
         if constexpr (kBias) {
           const int dist = a.distance;
@@ -1263,7 +1312,7 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
                     FwdShape<T, DP, 4>::kBytes + table, s);
     case kAttnDq: {
       const size_t sums =
-          a.dbias ? kAttnWaves * (table + (128 + kDiagWords) * sizeof(float)) : 0;
+          a.dbias ? kAttnWaves * (table + kDiagWords * sizeof(float)) : 0;
       return launch(attn_dq_kernel<T, DP, kBias, kVec>, a, grid,
                     DqShape<T, DP, kBias>::kBytes + table + sums, s);
     }
