@@ -44,7 +44,8 @@ struct AttnArgs {
   const void* bias;
   float* lse;        // written by the forward pass, read by the backward pass
   int32_t G, heads, kv_heads, d, causal;
-  int32_t g_shift;   // log2(G), or -1 where G is no power of two
+  uint32_t g_mul;    // division by G (query_of in attn_kernels.h)
+  int32_t g_shift;
   int32_t vec;       // every row may be moved in 16-byte pieces, at offsets of 32 bits from
                      // its tile's first
   float scale;

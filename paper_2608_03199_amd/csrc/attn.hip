@@ -352,7 +352,8 @@ AttnArgs common_args(const sieve_attn* p, const uint8_t* key_mask, const void* b
   a.key_mask = key_mask;
   a.bias = p->nb ? bias : nullptr;
   a.G = p->heads / p->kv_heads;
-  a.g_shift = (a.G & (a.G - 1)) == 0 ? __builtin_ctz(a.G) : -1;
+  while ((int64_t(1) << a.g_shift) < a.G) ++a.g_shift;
+  a.g_mul = (uint32_t)(((uint64_t(1) << (31 + a.g_shift)) + a.G - 1) / a.G);
   a.heads = p->heads;
   a.kv_heads = p->kv_heads;
   a.d = p->d;

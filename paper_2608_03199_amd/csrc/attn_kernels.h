@@ -78,69 +78,94 @@ __device__ __forceinline__ int piece_of(int row) {
   else return row >> 2 & 3;
 }
 
-// Values 16 c + 8 h .. + 7 of the rows row0 + lane % 32 (row0 a multiple of 32): the operand
-// whose summed axis is the head's.
+// LDS is addressed by its own 32-bit byte addresses: a lane's place in a tile is worked out
+// once, and what a read adds to it is an exclusive or with a constant and a constant offset
+// (tiles start at multiples of their rows' bytes: the kernels have no LDS but the dynamic
+// part, which starts at 0).
+typedef uint32_t lds_addr;
+template <typename V>
+__device__ __forceinline__ V lds_read(lds_addr at) {
+  return *(const __attribute__((address_space(3))) V*)(uintptr_t)at;
+}
+template <typename V>
+__device__ __forceinline__ void lds_write(lds_addr at, V v) {
+  *(__attribute__((address_space(3))) V*)(uintptr_t)at = v;
+}
+__device__ __forceinline__ lds_addr lds_of(const void* p) {
+  return (lds_addr)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// A lane's place for frag_along and frag_across, from the start of a tile.
 template <typename T, int DP>
-__device__ __forceinline__ vec8<T> frag_along(const T* s, int row0, int c, int lane) {
-  constexpr int kE = 16 / (int)sizeof(T);
+__device__ __forceinline__ lds_addr lane_along(int lane) {
   const int row = lane & 31, h = lane >> 5;
-  // the first piece's place; the others differ in the bits that c sets
-  const int at = row * DP + (((8 / kE) * h) ^ piece_of<T, DP>(row)) * kE;
-  const T* p = s + row0 * DP;
+  return row * DP * (int)sizeof(T) +
+         ((sizeof(T) == 2 ? h : 2 * h) ^ piece_of<T, DP>(row)) * 16;
+}
+template <typename T, int DP>
+__device__ __forceinline__ lds_addr lane_across(int lane) {
+  const int h = lane >> 5;
   if constexpr (sizeof(T) == 2) {
-    return __builtin_bit_cast(vec8<T>, enc_load<T, 8>(p + (at ^ (16 * c))));
+    const int i = lane & 15, row = 4 * h + (i >> 2);
+    const int piece = (lane >> 3 & 2) + (i >> 1 & 1);
+    return row * DP * 2 + (piece ^ piece_of<T, DP>(row)) * 16 + (i & 1) * 8;
   } else {
-    EncVec<T, 4> q[2] = {enc_load<T, 4>(p + (at ^ (16 * c))),
-                         enc_load<T, 4>(p + (at ^ (16 * c) ^ 4))};
-    return __builtin_bit_cast(vec8<T>, q);
+    // rows 4 h + 0..3: the row's number within 4 changes piece_of by a constant
+    return 4 * h * DP * 4 + ((lane & 31) / 4 ^ piece_of<T, DP>(4 * h)) * 16 + (lane & 3) * 4;
+  }
+}
+
+// Values 16 c + 8 h .. + 7 of the rows row0 + lane % 32 (row0 a multiple of 32): the operand
+// whose summed axis is the head's.  at: the tile's start plus lane_along.
+template <typename T, int DP>
+__device__ __forceinline__ vec8<T> frag_along(lds_addr at, int row0, int c) {
+  const int add = row0 * DP * (int)sizeof(T);
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_bit_cast(vec8<T>, lds_read<enc_u32x4>((at ^ (32 * c)) + add));
+  } else {
+    const f32x4 p = lds_read<f32x4>((at ^ (64 * c)) + add);
+    const f32x4 q = lds_read<f32x4>((at ^ (64 * c) ^ 16) + add);
+    return __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 }
 
 // The same place, written.
 template <typename T, int DP>
-__device__ __forceinline__ void put_along(T* s, int row0, int c, int lane, vec8<T> v) {
-  constexpr int kE = 16 / (int)sizeof(T);
-  const int row = lane & 31, h = lane >> 5;
-  const int at = row * DP + (((8 / kE) * h) ^ piece_of<T, DP>(row)) * kE;
-  T* p = s + row0 * DP;
-  const EncVec<T, 8> q = __builtin_bit_cast(EncVec<T, 8>, v);
+__device__ __forceinline__ void put_along(lds_addr at, int row0, int c, vec8<T> v) {
+  const int add = row0 * DP * (int)sizeof(T);
   if constexpr (sizeof(T) == 2) {
-    enc_store<T, 8>(p + (at ^ (16 * c)), q);
+    lds_write((at ^ (32 * c)) + add, __builtin_bit_cast(enc_u32x4, v));
   } else {
-    enc_store<T, 4>(p + (at ^ (16 * c)), EncVec<T, 4>{q.v[0], q.v[1], q.v[2], q.v[3]});
-    enc_store<T, 4>(p + (at ^ (16 * c) ^ 4), EncVec<T, 4>{q.v[4], q.v[5], q.v[6], q.v[7]});
+    lds_write((at ^ (64 * c)) + add, __builtin_shufflevector(v, v, 0, 1, 2, 3));
+    lds_write((at ^ (64 * c) ^ 16) + add, __builtin_shufflevector(v, v, 4, 5, 6, 7));
   }
 }
 
 // Value col + lane % 32 of the rows row0 + {4 h + 0..3, 8 + 4 h + 0..3} (row0 a multiple of
 // 16, col of 32): the operand whose summed axis is the tile's rows.  The transposing read
 // gives lane i of each 16 the i-th column of the 4 rows that the 16 lanes' addresses cover.
+// at: the tile's start plus lane_across.
 template <typename T, int DP>
-__device__ __forceinline__ vec8<T> frag_across(const T* s, int row0, int col, int lane) {
-  constexpr int kE = 16 / (int)sizeof(T);
-  const int h = lane >> 5;
-  const T* p = s + row0 * DP;
+__device__ __forceinline__ vec8<T> frag_across(lds_addr at, int row0, int col) {
+  constexpr int kRow = DP * (int)sizeof(T);
+  const int x = col * (int)sizeof(T), add = row0 * kRow;
   if constexpr (sizeof(T) == 2) {
-    const int i = lane & 15, row = 4 * h + (i >> 2);
-    const int piece = (lane >> 3 & 2) + (i >> 1 & 1);
-    const int at = row * DP + (piece ^ piece_of<T, DP>(row)) * kE + (i & 1) * 4;
-    // 8 rows on, piece_of differs in bit 1
-    const int next = (at ^ (2 * kE)) + 8 * DP;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     union {
       s16x4 half[2];
       vec8<T> all;
     } u;
-    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (at ^ col)));
-    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (next ^ col)));
+    // 8 rows on, piece_of differs in bit 1
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ x) + add));
+    u.half[1] =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ x ^ 32) + add + 8 * kRow));
     return u.all;
   } else {
     vec8<T> r;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int row = 4 * h + (j & 3) + (j & 4) * 2;
-      const int at = ((lane & 31) / kE ^ piece_of<T, DP>(row)) * kE + lane % kE;
-      r[j] = p[row * DP + (at ^ col)];
+      const int row = (j & 3) + (j & 4) * 2;
+      r[j] = lds_read<float>((at ^ x ^ (piece_of<T, DP>(row) * 16)) + add + row * kRow);
     }
     return r;
   }
@@ -154,10 +179,10 @@ __device__ __forceinline__ vec8<T> frag_of(const f32x16& x, int s) {
   return __builtin_convertvector(v, vec8<T>);
 }
 
-// Query of packed row r: a shift where the group's size is a power of two, as it nearly
-// always is (a division by a variable is some 30 instructions).
+// Query of packed row r: r / G for r < 2^31, by the multiplier ceil(2^(31 + s) / G) with
+// 2^(s-1) < G <= 2^s (its excess over the quotient is below 2^s, so the error stays below 1/G).
 __device__ __forceinline__ int query_of(const AttnArgs& a, int r) {
-  return a.g_shift >= 0 ? r >> a.g_shift : r / a.G;
+  return (int)(__umulhi((uint32_t)r << 1, a.g_mul) >> a.g_shift);
 }
 
 // Offset of packed row r (query r / G, head r % G of the group).
@@ -490,6 +515,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
   float m = -INFINITY, l = 0.f;
+  const int skip = WK == 1 ? 0 : wave * 32 * DP;  // the wave's keys in a tile
+  const lds_addr k_al = lds_of(s_k + skip) + lane_along<T, DP>(lane);
+  const lds_addr v_ac = lds_of(s_v + skip) + lane_across<T, DP>(lane);
 
   int buf = 0;
   if (it.lo < it.hi) {
@@ -508,15 +536,15 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     const bool more = base + kTile < it.hi;
     if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
     if (wave_live && __any(any != 0)) {
-      const T* sk = s_k + buf * kTileN + (WK == 1 ? 0 : wave * 32) * DP;
-      const T* sv = s_v + buf * kTileN + (WK == 1 ? 0 : wave * 32) * DP;
+      const lds_addr sk = k_al + buf * kTileN * (int)sizeof(T);
+      const lds_addr sv = v_ac + buf * kTileN * (int)sizeof(T);
       f32x16 s[kBlocks];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         s[b] = f32x16{};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c)
-          s[b] = mma(frag_along<T, DP>(sk, 32 * b, c, lane), q[c], s[b]);
+          s[b] = mma(frag_along<T, DP>(sk, 32 * b, c), q[c], s[b]);
       }
       float top = -INFINITY;
 #pragma unroll
@@ -550,7 +578,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           const vec8<T> p = frag_of<T>(s[b], c);
 #pragma unroll
           for (int e = 0; e < DP / 32; ++e)
-            o[e] = mma(frag_across<T, DP>(sv, 32 * b + 16 * c, 32 * e, lane), p, o[e]);
+            o[e] = mma(frag_across<T, DP>(sv, 32 * b + 16 * c, 32 * e), p, o[e]);
         }
       }
     }
@@ -754,7 +782,6 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   float* s_far = s_diag;                             // [wave][half][32][2], after the keys
   if (kBias && a.dbias) s_bias = s_diag + kAttnWaves * kDiagWords;
   float* s_sum = s_bias + a.G * a.span;              // [wave][G][span]
-  __shared__ float s_max[kAttnWaves];
   const AttnItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
   const int G = a.G, d = a.d;
@@ -817,6 +844,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
+  const lds_addr k_al = lds_of(s_k) + lane_along<T, DP>(lane);
+  const lds_addr k_ac = lds_of(s_k) + lane_across<T, DP>(lane);
   float most = 0.f;                  // largest |dS| of the row so far
   float up = kScaled ? 0x1p40f : 1;  // dS is rounded times this
 
@@ -836,15 +865,16 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     const bool more = base + kTile < it.hi;
     if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
     if (wave_live && __any(any != 0)) {
-      const T* sk = s_k + buf * kTileN;
-      const T* sv = s_v + buf * kTileN;
+      const lds_addr sk = k_al + buf * kTileN * (int)sizeof(T);
+      const lds_addr sv = sk + (lds_addr)((s_v - s_k) * sizeof(T));
+      const lds_addr sk_ac = k_ac + buf * kTileN * (int)sizeof(T);
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
-          s = mma(frag_along<T, DP>(sk, 32 * b, c, lane), q[c], s);
-          dp = mma(frag_along<T, DP>(sv, 32 * b, c, lane), dout[c], dp);
+          s = mma(frag_along<T, DP>(sk, 32 * b, c), q[c], s);
+          dp = mma(frag_along<T, DP>(sv, 32 * b, c), dout[c], dp);
         }
         const int first = base + 32 * b;
         finish_scores<kBias>(s, scale2, table, a.distance, me.pos, me.pos_min, me.pos_max, lo, hi,
@@ -910,7 +940,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           const vec8<T> p = frag_of<T>(s, c);
 #pragma unroll
           for (int e = 0; e < DP / 32; ++e)
-            dq[e] = mma(frag_across<T, DP>(sk, 32 * b + 16 * c, 32 * e, lane), p, dq[e]);
+            dq[e] = mma(frag_across<T, DP>(sk_ac, 32 * b + 16 * c, 32 * e), p, dq[e]);
         }
       }
     }
@@ -927,6 +957,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   if constexpr (kScaled) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    float* s_max = (float*)smem;
+    __syncthreads();  // the last tile has been read
     if (lane == 0) s_max[wave] = most;
     __syncthreads();
     if (threadIdx.x == 0)
@@ -1049,7 +1081,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       (const T*)a.dout.data + it.q0 * a.dout.token_stride + it.kvh * G * a.dout.head_stride;
   // Offsets of a tile's pieces and rows from its first query.  Where G divides the tile they
   // are the same for every tile.
-  const bool fixed = a.g_shift >= 0 && G <= 32;
+  const bool fixed = (G & (G - 1)) == 0 && G <= 32;
   const bool row_mine = threadIdx.x < kTile;
   // a row without keys is only possible with a mask or a table that holds -infinity
   const bool some_empty = a.key_mask || kBias;
@@ -1109,6 +1141,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   };
   if (it.lo < it.hi) fetch(it.lo, 0);
 
+  const lds_addr q_al = lds_of(s_q) + lane_along<T, DP>(lane);
+  const lds_addr q_ac = lds_of(s_q) + lane_across<T, DP>(lane);
+  const lds_addr val_al = lds_of(s_val + wave * 32 * DP) + lane_along<T, DP>(lane);
   vec8<T> k[DP / 16], v[DP / 16];
   {
     const int64_t tok = it.k0 + (live ? key : 0);
@@ -1119,7 +1154,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     if constexpr (Shape::kValuesInLds) {  // a wave reads its own 32 rows only
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c)
-        put_along<T, DP>(s_val, wave * 32, c, lane, v[c]);
+        put_along<T, DP>(val_al, 0, c, v[c]);
     }
   }
   if constexpr (kBias) load_bias<T>(a, it.kvh, s_bias);
@@ -1144,8 +1179,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     const bool more = base + kTile < it.hi;
     if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
     if (wave_live) {
-      const T* sq = s_q + buf * kTileN;
-      const T* sd = s_do + buf * kTileN;
+      constexpr int kApart = Shape::kBufs * kTileN * (int)sizeof(T);  // s_do - s_q
+      lds_addr sq = q_al + buf * kTileN * (int)sizeof(T);
+      lds_addr sq_ac = q_ac + buf * kTileN * (int)sizeof(T);
+      lds_addr val_at = val_al;
+      // Work the reads' addresses out at each tile: kept over the loop they would fill the
+      // registers that the accumulators leave.
+      if constexpr (Shape::kValuesInLds) asm volatile("" : "+v"(sq), "+v"(sq_ac), "+v"(val_at));
+      const lds_addr sd = sq + kApart, sd_ac = sq_ac + kApart;
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         const int first = base + 32 * b;
@@ -1164,13 +1205,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         }
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
-          s = mma(frag_along<T, DP>(sq, 32 * b, c, lane), k[c], s);
+          s = mma(frag_along<T, DP>(sq, 32 * b, c), k[c], s);
           vec8<T> val;
           if constexpr (Shape::kValuesInLds)
-            val = frag_along<T, DP>(s_val, wave * 32, c, lane);
+            val = frag_along<T, DP>(val_at, 0, c);
           else
             val = v[c];
-          dp = mma(frag_along<T, DP>(sd, 32 * b, c, lane), val, dp);
+          dp = mma(frag_along<T, DP>(sd, 32 * b, c), val, dp);
         }
         if constexpr (kBias) {
           const int dist = a.distance;
@@ -1224,8 +1265,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           const vec8<T> p = frag_of<T>(s, c), ds = frag_of<T>(dp, c);
 #pragma unroll
           for (int e = 0; e < DP / 32; ++e) {
-            dv[e] = mma(frag_across<T, DP>(sd, 32 * b + 16 * c, 32 * e, lane), p, dv[e]);
-            dk[e] = mma(frag_across<T, DP>(sq, 32 * b + 16 * c, 32 * e, lane), ds, dk[e]);
+            dv[e] = mma(frag_across<T, DP>(sd_ac, 32 * b + 16 * c, 32 * e), p, dv[e]);
+            dk[e] = mma(frag_across<T, DP>(sq_ac, 32 * b + 16 * c, 32 * e), ds, dk[e]);
           }
         }
       }
