@@ -185,6 +185,11 @@ __device__ __forceinline__ int query_of(const AttnArgs& a, int r) {
   return (int)(__umulhi((uint32_t)r << 1, a.g_mul) >> a.g_shift);
 }
 
+// The wave's number, known to be the same in all lanes.
+__device__ __forceinline__ int wave_id() {
+  return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+}
+
 // Offset of packed row r (query r / G, head r % G of the group).
 __device__ __forceinline__ int64_t row_at(const AttnArgs& a, const sieve_heads& x,
                                           const AttnItem& it, int r) {
@@ -285,7 +290,7 @@ struct Stage {
       if constexpr (kDirect) {
         if (mine(i))
           from.load_lds(there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere,
-                        s + (i * kAttnThreads + (threadIdx.x & ~63)) * kE);
+                        s + (i * kAttnThreads + wave_id() * 64) * kE);
       } else if constexpr (kVec) {
         r[i] = from.load(mine(i) && there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere);
       } else {
@@ -395,8 +400,9 @@ __device__ __forceinline__ uint32_t upto(int pos, int base) {
   return lim >= 31 ? ~0u : lim < 0 ? 0u : (2u << lim) - 1;
 }
 
-// Scores of 32 keys (base ..) for the lane's row, in units of log2: scaled, biased, and
-// -infinity where bits (this half's view) has a 0.  lo, hi: bias past the distance.
+// Products of 32 keys (base ..) with the lane's row to scores: s * scale2 + bias, in units of
+// log2, and -infinity where bits (of the keys) has a 0.  Without a bias the products stay as
+// they are.  lo, hi: bias past the distance.
 template <bool kBias>
 __device__ __forceinline__ void finish_scores(f32x16& s, float scale2, const float* table,
                                               int distance, int pos, int pos_min, int pos_max,
@@ -411,9 +417,6 @@ __device__ __forceinline__ void finish_scores(f32x16& s, float scale2, const flo
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = s[r] * scale2 + t[8 * (r >> 2) + (r & 3)];
     }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] *= scale2;
   }
   if (!__all(bits == ~0u)) {
     const uint32_t mine = bits >> (4 * h);
@@ -479,7 +482,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_v = s_k + Shape::kBufs * kTileN;
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
   const int G = a.G, d = a.d;
   const LaneRow me = lane_row(a, it, it.row + (WK == 1 ? wave * 32 : 0), lane);
   const float scale2 = a.scale * kLog2e;
@@ -555,6 +558,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
       }
       top = fmaxf(top, __shfl_xor(top, 32));
+      if constexpr (!kBias) top *= scale2;
       if (__any(top > m + kLag)) {
         const float next = fmaxf(m, top);
         const float f = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.f : next));
@@ -570,7 +574,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - off);
+          s[b][r] = __builtin_amdgcn_exp2f(kBias ? s[b][r] - off : s[b][r] * scale2 - off);
           l += s[b][r];
         }
 #pragma unroll
@@ -783,7 +787,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   if (kBias && a.dbias) s_bias = s_diag + kAttnWaves * kDiagWords;
   float* s_sum = s_bias + a.G * a.span;              // [wave][G][span]
   const AttnItem it = a.items[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
   const int G = a.G, d = a.d;
   const LaneRow me = lane_row(a, it, it.row + wave * 32, lane);
   const float scale2 = a.scale * kLog2e;
@@ -881,7 +885,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
                              first, h, bits[b]);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          s[r] = __builtin_amdgcn_exp2f(s[r] - lse2) * (dp[r] - dsum);  // dS
+          s[r] = __builtin_amdgcn_exp2f(kBias ? s[r] - lse2 : s[r] * scale2 - lse2) *
+                 (dp[r] - dsum);  // dS
         if (!__all(bits[b] == ~0u)) {
           // P = 0 there, but dP need not be a number
           const uint32_t mine = bits[b] >> (4 * h);
@@ -1060,7 +1065,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][lse2, -D, table offset, pos][row]
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
   const int G = a.G, d = a.d, shift = it.nk - it.nq;
   const float scale2 = a.scale * kLog2e;
   const int key0 = it.row + wave * 32, key = key0 + (lane & 31);
@@ -1219,6 +1224,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
             const float far = s_bias[key0 > pos_min ? a.span - 1 : 0];
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = s[r] * scale2 + far;
+          } else if (G == 1) {
+            // row 8 g + 4 h + t of the block stands at first + shift + that
+            const float* table =
+                s_bias + (key - (first + shift) - 4 * h + dist + kAttnPad) - 27;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              s[r] = s[r] * scale2 + table[27 - 8 * (r >> 2) - (r & 3)];
           } else {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
