@@ -26,9 +26,8 @@
 // P and dS are rounded to the inputs' type for the second products, as those run on the
 // 16-bit matrix units; S, dP, the statistics and every accumulator are fp32.  bfloat16
 // keeps fp32's range.  binary16 does not, so there the values are scaled by powers of two
-// that the end takes out exactly: P by 2^6 below a running maximum that lags by at most
-// 2^8 (forward) or by 2^14 (backward, where P <= 1), and dS by what brings its largest
-// magnitude to 2^13 .. 2^14.
+// that the end takes out exactly: P by 2^11 at the running maximum (forward) or by 2^14
+// (backward, where P <= 1), and dS by what brings its largest magnitude to 2^13 .. 2^14.
 #pragma once
 
 #include "attn.h"
@@ -378,14 +377,27 @@ __device__ __forceinline__ void store_row(T* p, const f32x16 (&x)[DP / 32], floa
   }
 }
 
-// The group's bias tables into LDS, times log2(e): s[g * span + entry].
+// The group's bias tables into LDS, times log2(e): s[g * span + entry].  The first entries'
+// buckets and values are loaded side by side; the values change places within the wave where
+// there are at most 64 of them.
 template <typename T>
 __device__ __forceinline__ void load_bias(const AttnArgs& a, int kvh, float* s) {
-  for (int i = threadIdx.x; i < a.G * a.span; i += kAttnThreads) {
-    const int g = i / a.span;
-    const int bucket = a.bucket_of[i - g * a.span];
-    s[i] = (float)((const T*)a.bias)[(int64_t)bucket * a.heads + kvh * a.G + g] * kLog2e;
+  const T* bias = (const T*)a.bias + kvh * a.G;
+  if (a.nb <= 64) {
+    const int lane = threadIdx.x & 63;
+    for (int g = 0; g < a.G; ++g) {
+      const float mine = lane < a.nb ? (float)bias[(int64_t)lane * a.heads + g] * kLog2e : 0.f;
+      for (int i = threadIdx.x; i - lane < a.span; i += kAttnThreads) {
+        const int bucket = i < a.span ? a.bucket_of[i] : 0;
+        const float v = __shfl(mine, bucket);
+        if (i < a.span) s[g * a.span + i] = v;
+      }
+    }
+    return;
   }
+  for (int g = 0; g < a.G; ++g)
+    for (int i = threadIdx.x; i < a.span; i += kAttnThreads)
+      s[g * a.span + i] = (float)bias[(int64_t)a.bucket_of[i] * a.heads + g] * kLog2e;
 }
 
 // Not 0: the key is in the item's range and not masked.  Loaded a tile ahead.
@@ -451,9 +463,38 @@ __device__ __forceinline__ LaneRow lane_row(const AttnArgs& a, const AttnItem& i
   return x;
 }
 
+
+// The running maximum may lag by kLag powers of two before the sums are brought to a new one,
+// and P is 2^kShift at it.  For binary16, 2^(kLag + kShift) has to stay below 65504 and what
+// 2^kShift pushes below 2^-14 loses bits.
 template <typename T>
-constexpr float kShift = __is_same(T, f16) ? 6.f : 0.f;
-constexpr float kLag = 8.f;  // a running maximum is left to lag by this many powers of two
+constexpr float kLag = __is_same(T, f16) ? 4.f : 8.f;
+template <typename T>
+constexpr float kShift = __is_same(T, f16) ? 11.f : 0.f;
+
+// x plus the sum of an operand's eight values: of the rounded probabilities, which are what
+// the second product adds up, two to an instruction.
+__device__ __forceinline__ float add_up(vec8<f16> p, float x) {
+  typedef f16 pair __attribute__((ext_vector_type(2)));
+  const pair one = {(f16)1.f, (f16)1.f};
+  x = __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 0, 1), one, x, false);
+  x = __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 2, 3), one, x, false);
+  x = __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 4, 5), one, x, false);
+  return __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 6, 7), one, x, false);
+}
+__device__ __forceinline__ float add_up(vec8<bf16> p, float x) {
+  typedef bf16 pair __attribute__((ext_vector_type(2)));
+  const pair one = {(bf16)1.f, (bf16)1.f};
+  x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 0, 1), one, x, false);
+  x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 2, 3), one, x, false);
+  x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 4, 5), one, x, false);
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 6, 7), one, x, false);
+}
+__device__ __forceinline__ float add_up(f32x8 p, float x) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x += p[j];
+  return x;
+}
 
 // ---- forward ----------------------------------------------------------------------------
 // WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
@@ -559,7 +600,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       }
       top = fmaxf(top, __shfl_xor(top, 32));
       if constexpr (!kBias) top *= scale2;
-      if (__any(top > m + kLag)) {
+      if (__any(top > m + kLag<T>)) {
         const float next = fmaxf(m, top);
         const float f = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.f : next));
         m = next;
@@ -573,13 +614,12 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 16; ++r)
           s[b][r] = __builtin_amdgcn_exp2f(kBias ? s[b][r] - off : s[b][r] * scale2 - off);
-          l += s[b][r];
-        }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const vec8<T> p = frag_of<T>(s[b], c);
+          l = add_up(p, l);
 #pragma unroll
           for (int e = 0; e < DP / 32; ++e)
             o[e] = mma(frag_across<T, DP>(sv, 32 * b + 16 * c, 32 * e), p, o[e]);
@@ -1062,7 +1102,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_val = (T*)smem;
   T* s_q = (T*)(smem + Shape::kValueBytes);
   T* s_do = s_q + Shape::kBufs * kTileN;
-  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][lse2, -D, table offset, pos][row]
+  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][-lse / scale, -D, table offset, pos][row]
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
@@ -1138,7 +1178,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     st_do.store(s_do + b * kTileN, some_empty, [&](int i) { return piece_lse[i] != -INFINITY; });
     if (row_mine) {
       float* p = s_row + b * 4 * kTile + threadIdx.x;
-      p[0] = row_lse == -INFINITY ? INFINITY : row_lse * kLog2e;
+      p[0] = row_lse == -INFINITY ? -INFINITY : -row_lse / a.scale;
       p[kTile] = -row_d;
       ((int*)p)[2 * kTile] = row_off;
       ((int*)p)[3 * kTile] = row_pos;
@@ -1200,13 +1240,18 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         const int pos_min = query_of(a, first) + shift, pos_max = query_of(a, last) + shift;
         if (a.causal && pos_max < key0) continue;
         const float* rows = s_row + buf * 4 * kTile + 32 * b + 4 * h;
-        // dP - D: the products are added to -D
-        f32x16 s = {}, dp;
+        // S - lse and dP - D: the products are added to what is subtracted.  A row without
+        // keys has -infinity there, and P = 0.
+        f32x16 s, dp;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const f32x4 x = *(const f32x4*)(rows + kTile + 8 * g);
+          const f32x4 x = *(const f32x4*)(rows + 8 * g);
+          const f32x4 y = *(const f32x4*)(rows + kTile + 8 * g);
 #pragma unroll
-          for (int t = 0; t < 4; ++t) dp[4 * g + t] = x[t];
+          for (int t = 0; t < 4; ++t) {
+            s[4 * g + t] = x[t];
+            dp[4 * g + t] = y[t];
+          }
         }
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
@@ -1249,12 +1294,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           for (int r = 0; r < 16; ++r) s[r] *= scale2;
         }
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 lse = *(const f32x4*)(rows + 8 * g);
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-            s[4 * g + t] = __builtin_amdgcn_exp2f(s[4 * g + t] - lse[t]);
-        }
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
         if (a.causal && pos_min < key0 + 31) {
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
