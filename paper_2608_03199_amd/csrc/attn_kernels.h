@@ -757,10 +757,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
 //
 // The bias table's gradient is a sum along diagonals.  Where a block of keys is past the
 // distance it all falls into one bucket, and the lane adds it up in a register.  Nearer, the
-// wave writes its 32x32 block of dS to LDS with zeros beside every row, so that a lane can
-// read down a whole diagonal without a test (row i's value at relative position p + i lies at
-// a constant step from row i - 1's), and adds the result to its own sums by position.  No
-// atomics: the order of additions is the program's.
+// wave writes its 32x32 block of dS to LDS, 16 rows at a time, with zeros beside every row, so
+// that a lane can read down a whole diagonal without a test (row i's value at relative
+// position p + i lies at a constant step from row i - 1's), and adds the result to its own
+// sums by position.  No atomics: the order of additions is the program's.
 
 // With a bias the tile is 32 keys, so that two work-groups' LDS fits a CU beside the sums.
 template <typename T, int DP, bool kBias>
@@ -773,24 +773,24 @@ struct DqShape {
 constexpr int kAttnWaves = kAttnThreads / 64;
 // A row of the dS block: 32 values, then at least 31 zeros, and 4 words that spread the
 // rows' 16-byte stores over the banks; 32 zeros stand before the first row.
-constexpr int kDiagRow = 68;
-constexpr int kDiagWords = 32 * kDiagRow + 32;
+constexpr int kDiagRow = 68, kDiagRows = 16;
+constexpr int kDiagWords = kDiagRows * kDiagRow + 32;
 
-// Adds the diagonals of the wave's block (rows: packed rows from `first_row`, columns: keys
-// from `base`) to the wave's sums by relative position.
-__device__ __forceinline__ void add_diagonals(const AttnArgs& a, const AttnItem& it,
-                                              const float* block, float* sums, int first_row,
-                                              int base, int pos0, int lane) {
+// Adds the diagonals of half of the wave's block (rows: packed rows from `first_row`, the half
+// starting at row `from`; columns: keys from `base`) to the wave's sums by relative position.
+__device__ __forceinline__ void add_diagonals(const AttnArgs& a, const float* block, float* sums,
+                                              int first_row, int from, int base, int pos0,
+                                              int lane) {
   const int G = a.G;
   // relative position of (row 0, key 0) as an entry of the sums
   const int entry = base - pos0 + a.distance + kAttnPad;
   if (G == 1) {
-    // lane: diagonal key - row = lane - 31
-    const float* p = block + lane - 31;
+    // diagonals key - (row - from) = -15 .. 31
+    const float* p = block + lane - (kDiagRows - 1);
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) t += p[i * (kDiagRow + 1)];
-    if (lane < 63) sums[entry + lane - 31] += t;
+    for (int i = 0; i < kDiagRows; ++i) t += p[i * (kDiagRow + 1)];
+    if (lane < 31 + kDiagRows) sums[entry - from + lane - (kDiagRows - 1)] += t;
     return;
   }
   // rows of head g: every G-th, their queries one apart
@@ -800,16 +800,23 @@ __device__ __forceinline__ void add_diagonals(const AttnArgs& a, const AttnItem&
   for (int x = lane; x < G * wide; x += 64) {
     const int g = x / wide, diag = x - g * wide - (rows - 1);
     float t = 0.f;
-    // first row of head g at or after first_row
-    int r = g - (first_row - tok0 * G);
+    // first row of head g at or after the half's first
+    const int start = first_row + from, tok = query_of(a, start);
+    int r = g - (start - tok * G);
     if (r < 0) r += G;
-    const int tok = query_of(a, first_row + r) - tok0;
-    for (int i = tok; r < 32; r += G, ++i) {
+    for (int i = query_of(a, start + r) - tok0; r < kDiagRows; r += G, ++i) {
       const int key = diag + i;
       if (key >= 0 && key < 32) t += block[r * kDiagRow + key];
     }
     sums[g * a.span + entry + diag] += t;
   }
+}
+
+// Order of a wave's own LDS writes and reads.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 template <typename T, int DP, bool kBias, bool kVec>
@@ -871,6 +878,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   float lo = 0.f, hi = 0.f, far_lo = 0.f, far_hi = 0.f;
   const float* table = nullptr;
   float *sums = nullptr, *block = nullptr;
+  int range0 = 0, range1 = 0;
   if constexpr (kBias) {
     load_bias<T>(a, it.kvh, s_bias);
     if (want_bias) {
@@ -884,6 +892,11 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     hi = table[a.span - 1];
     sums = s_sum + wave * G * a.span;
     block = s_diag + wave * kDiagWords + 32;
+    if (want_bias && (int)threadIdx.x >> 3 < G * a.nb) {
+      const int b = ((int)threadIdx.x >> 3) % a.nb;
+      range0 = a.range[2 * b];
+      range1 = a.range[2 * b + 1];
+    }
   }
   f32x16 dq[DP / 32];
 #pragma unroll
@@ -945,16 +958,18 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
             } else {
               // rows past the sequence's end have dS = 0
 #pragma unroll
-              for (int g = 0; g < 4; ++g)
-                *(f32x4*)(block + (lane & 31) * kDiagRow + 8 * g + 4 * h) =
-                    f32x4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
-              __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-              __builtin_amdgcn_wave_barrier();
-              __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-              add_diagonals(a, it, block, sums, it.row + wave * 32, first, me.pos_min, lane);
-              __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-              __builtin_amdgcn_wave_barrier();
-              __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+              for (int half = 0; half < 2; ++half) {
+                if ((lane >> 4 & 1) == half) {
+#pragma unroll
+                  for (int g = 0; g < 4; ++g)
+                    *(f32x4*)(block + (lane & 15) * kDiagRow + 8 * g + 4 * h) =
+                        f32x4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
+                }
+                wave_sync();
+                add_diagonals(a, block, sums, it.row + wave * 32, half * 16, first, me.pos_min,
+                              lane);
+                wave_sync();
+              }
             }
           }
         }
@@ -1012,9 +1027,17 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   }
   if constexpr (kBias) {
     if (!want_bias) return;
+    if (!me.live) far_lo = far_hi = 0.f;
+    if (G == 1) {  // the wave's rows are one head's: lane 0 takes the sum
+#pragma unroll
+      for (int o = 32; o; o >>= 1) {
+        far_lo += __shfl_xor(far_lo, o);
+        far_hi += __shfl_xor(far_hi, o);
+      }
+    }
     __syncthreads();
-    s_far[(wave * 64 + h * 32 + (lane & 31)) * 2] = me.live ? far_lo : 0.f;
-    s_far[(wave * 64 + h * 32 + (lane & 31)) * 2 + 1] = me.live ? far_hi : 0.f;
+    s_far[(wave * 64 + h * 32 + (lane & 31)) * 2] = far_lo;
+    s_far[(wave * 64 + h * 32 + (lane & 31)) * 2 + 1] = far_hi;
     __syncthreads();
     const int all = G * a.span;
     for (int i = threadIdx.x; i < all; i += kAttnThreads) {
@@ -1026,20 +1049,32 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     __syncthreads();
     // 8 threads a bucket
     float* to = a.part_bias + ((int64_t)it.kvh * a.row_tiles + it.part) * G * a.nb;
-    const int bucket_lo = a.bucket_of[0], bucket_hi = a.bucket_of[a.span - 1];
     const int sub = threadIdx.x & 7;
     for (int i = threadIdx.x >> 3; i < G * a.nb; i += kAttnThreads / 8) {
       const int g = i / a.nb, b = i - g * a.nb;
+      int from = range0, to_entry = range1;  // of the first bucket, loaded at the start
+      if (i >= kAttnThreads / 8) {
+        from = a.range[2 * b];
+        to_entry = a.range[2 * b + 1];
+      }
+      // the first and the last entry stand for what lies past the distance
+      const bool has_lo = from == 0 && to_entry > 0, has_hi = to_entry == a.span;
       float t = 0.f;
-      for (int e = a.range[2 * b] + sub; e < a.range[2 * b + 1]; e += 8)
-        t += s_sum[g * a.span + e];
-      if (b == bucket_lo || b == bucket_hi) {
-        // copy `sub` of the sums past the distance: the rows of this head
-        for (int row = 0; row < 32; ++row)
-          if ((it.row + (sub >> 1) * 32 + row) % G == g) {
-            if (b == bucket_lo) t += s_far[(sub * 32 + row) * 2];
-            if (b == bucket_hi) t += s_far[(sub * 32 + row) * 2 + 1];
+      for (int e = from + sub; e < to_entry; e += 8) t += s_sum[g * a.span + e];
+      if (has_lo || has_hi) {
+        if (G == 1) {
+          if (sub < kAttnWaves)
+            t += (has_lo ? s_far[sub * 128] : 0.f) + (has_hi ? s_far[sub * 128 + 1] : 0.f);
+        } else {
+          // copy `sub` of the sums past the distance: the rows of this head
+          const int row0 = it.row + (sub >> 1) * 32;
+          int row = g - (row0 - query_of(a, row0) * G);
+          if (row < 0) row += G;
+          for (; row < 32; row += G) {
+            if (has_lo) t += s_far[(sub * 32 + row) * 2];
+            if (has_hi) t += s_far[(sub * 32 + row) * 2 + 1];
           }
+        }
       }
 #pragma unroll
       for (int o = 4; o; o >>= 1) t += __shfl_xor(t, o);
@@ -1051,8 +1086,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 // ---- backward: dK and dV -------------------------------------------------------------------
 // A wave takes 32 of the tile's 128 keys, one a lane, and goes through the rows that see
 // them: all query heads of the group, so that the sum over a shared head is the accumulator's.
-// S = Q K^T puts rows 8 g + 4 h + t in registers 4 g + t.  The last `heads` work-groups of a
-// launch with a bias add up its gradient's partial sums instead.
+// S = Q K^T puts rows 8 g + 4 h + t in registers 4 g + t.  The first `heads` work-groups of a
+// launch with a bias's gradient add up its partial sums instead.
 
 template <typename T, int DP>
 struct DkvShape {
@@ -1070,21 +1105,27 @@ struct DkvShape {
 
 template <typename T>
 __device__ __forceinline__ void reduce_bias(const AttnArgs& a, int head, float* s) {
-  // threads: nb (rounded up to a power of two) x groups of row tiles
-  int wide = 4;
-  while (wide < a.nb) wide *= 2;
+  // threads: nb / 2 pairs of buckets (rounded up to a power of two) x groups of row tiles
+  int wide = 2;
+  while (wide < a.nb / 2) wide *= 2;
   const int groups = kAttnThreads / wide, b = threadIdx.x % wide, g = threadIdx.x / wide;
   const int kvh = head / a.G;
-  const float* p = a.part_bias + ((int64_t)kvh * a.row_tiles * a.G + (head - kvh * a.G)) * a.nb;
-  float t = 0.f;
-  if (b < a.nb)
-    for (int i = g; i < a.row_tiles; i += groups) t += p[(int64_t)i * a.G * a.nb + b];
-  s[threadIdx.x] = t;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2* p = (const f32x2*)(a.part_bias +
+                                  ((int64_t)kvh * a.row_tiles * a.G + (head - kvh * a.G)) * a.nb) + b;
+  const int64_t step = (int64_t)a.G * a.nb / 2;
+  f32x2 t = {};
+  if (2 * b < a.nb) {
+#pragma unroll 8
+    for (int i = g; i < a.row_tiles; i += groups) t += p[i * step];
+  }
+  ((f32x2*)s)[threadIdx.x] = t;
   __syncthreads();
-  if (g == 0 && b < a.nb) {
-    t = 0.f;
-    for (int i = 0; i < groups; ++i) t += s[i * wide + b];
-    ((T*)a.dbias)[(int64_t)b * a.heads + head] = (T)t;
+  if (g == 0 && 2 * b < a.nb) {
+    t = f32x2{};
+    for (int i = 0; i < groups; ++i) t += ((f32x2*)s)[i * wide + b];
+    ((T*)a.dbias)[(int64_t)(2 * b) * a.heads + head] = (T)t[0];
+    ((T*)a.dbias)[(int64_t)(2 * b + 1) * a.heads + head] = (T)t[1];
   }
 }
 
@@ -1095,8 +1136,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   constexpr int kTileN = kTile * DP;
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
-  if (kBias && (int)blockIdx.x >= a.nitems) {
-    reduce_bias<T>(a, blockIdx.x - a.nitems, (float*)smem);
+  const int reducers = (int)gridDim.x - a.nitems;
+  if (kBias && (int)blockIdx.x < reducers) {
+    reduce_bias<T>(a, blockIdx.x, (float*)smem);
     return;
   }
   T* s_val = (T*)smem;
@@ -1104,7 +1146,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_do = s_q + Shape::kBufs * kTileN;
   float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][-lse / scale, -D, table offset, pos][row]
   float* s_bias = (float*)(smem + Shape::kBytes);
-  const AttnItem it = a.items[blockIdx.x];
+  const AttnItem it = a.items[blockIdx.x - reducers];
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
   const int G = a.G, d = a.d, shift = it.nk - it.nq;
   const float scale2 = a.scale * kLog2e;
