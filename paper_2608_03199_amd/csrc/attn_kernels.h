@@ -703,52 +703,42 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         l == 0.f ? -INFINITY : (at + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Partial rows of one tile to whole ones: 8 threads a row.
+// Partial rows of one tile to whole ones: DP / 4 threads a row, kJoinRows rows a work-group.
+template <int DP>
+constexpr int kJoinRows = kAttnThreads / (DP / 4);
+
 template <typename T, int DP, int ROWS>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
-  const AttnJoin j = a.joins[blockIdx.x];
-  const int rows = j.n * a.G;
-  for (int i = threadIdx.x / 8; i < ROWS; i += kAttnThreads / 8) {
-    const int r = j.row + i;
-    if (r >= rows) break;
-    float most = -INFINITY;
-    for (int p = 0; p < j.parts; ++p)
-      most = fmaxf(most, a.part_ml[((int64_t)(j.part0 + p) * ROWS + i) * 2]);
-    if (most == -INFINITY) most = 0.f;
-    float l = 0.f;
-    constexpr int kN = DP / 8;
-    float v[kN];
-#pragma unroll
-    for (int e = 0; e < kN; ++e) v[e] = 0.f;
-    for (int p = 0; p < j.parts; ++p) {
-      const int64_t slot = (int64_t)(j.part0 + p) * ROWS + i;
-      const float lp = a.part_ml[slot * 2 + 1];
-      if (lp == 0.f) continue;
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[slot * 2] - most);
-      l += lp * f;
-      const float* o = a.part_o + slot * DP + (threadIdx.x & 7) * 4;
-#pragma unroll
-      for (int e = 0; e < kN / 4; ++e) {
-        const f32x4 x = *(const f32x4*)(o + 32 * e);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) v[4 * e + t] += f * x[t];
-      }
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int tok = query_of(a, r);
-    const int head = j.kvh * a.G + (r - tok * a.G);
-    T* to = (T*)a.o.data + (j.t0 + tok) * a.o.token_stride + head * a.o.head_stride;
-#pragma unroll
-    for (int e = 0; e < kN / 4; ++e)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int col = 32 * e + (threadIdx.x & 7) * 4 + t;
-        if (col < a.d) to[col] = (T)(v[4 * e + t] * inv);
-      }
-    if (a.lse && (threadIdx.x & 7) == 0)
-      a.lse[(j.t0 + tok) * a.heads + head] =
-          l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
+  constexpr int kGroups = (ROWS + kJoinRows<DP> - 1) / kJoinRows<DP>;
+  const AttnJoin j = a.joins[blockIdx.x / kGroups];
+  const int i = blockIdx.x % kGroups * kJoinRows<DP> + threadIdx.x / (DP / 4);
+  const int r = j.row + i, c = threadIdx.x % (DP / 4) * 4;
+  if (i >= ROWS || r >= j.n * a.G) return;
+  const float* ml = a.part_ml + ((int64_t)j.part0 * ROWS + i) * 2;
+  float most = -INFINITY;
+#pragma unroll 4
+  for (int p = 0; p < j.parts; ++p) most = fmaxf(most, ml[(int64_t)p * ROWS * 2]);
+  if (most == -INFINITY) most = 0.f;
+  const float* o = a.part_o + ((int64_t)j.part0 * ROWS + i) * DP + c;
+  float l = 0.f;
+  f32x4 v = {};
+#pragma unroll 4
+  for (int p = 0; p < j.parts; ++p) {
+    const float lp = ml[(int64_t)p * ROWS * 2 + 1];
+    // a part without keys has l = 0 and o = 0
+    const float f = lp == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[(int64_t)p * ROWS * 2] - most);
+    l += lp * f;
+    v += *(const f32x4*)(o + (int64_t)p * ROWS * DP) * f;
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int tok = query_of(a, r), head = j.kvh * a.G + (r - tok * a.G);
+  T* to = (T*)a.o.data + (j.t0 + tok) * a.o.token_stride + head * a.o.head_stride + c;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    if (c + t < a.d) to[t] = (T)(v[t] * inv);
+  if (a.lse && c == 0)
+    a.lse[(j.t0 + tok) * a.heads + head] =
+        l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ---- backward: dQ and the bias table's gradient ------------------------------------------
@@ -1400,16 +1390,21 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
                    kScaled ? 0x1p-14f : 1.f, d, h);
 }
 
-// Partial sums of one key tile to its gradients.
+// Partial sums of one key tile to its gradients, kDkvJoinGroups work-groups a tile.
+constexpr int kDkvJoinGroups = 8;
+
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads) void attn_dkv_join_kernel(AttnArgs a) {
-  const AttnJoin j = a.joins[blockIdx.x];
+  const AttnJoin j = a.joins[blockIdx.x / kDkvJoinGroups];
   constexpr int kAll = 2 * kAttnKeys * DP / 4;  // values, four a thread
-  for (int i = threadIdx.x; i < kAll; i += kAttnThreads) {
+  constexpr int kEach = kAll / kDkvJoinGroups;
+  const int first = blockIdx.x % kDkvJoinGroups * kEach;
+  for (int i = first + threadIdx.x; i < first + kEach; i += kAttnThreads) {
     const int col = i % (DP / 4) * 4, key = j.row + i / (DP / 4) % kAttnKeys;
     if (key >= j.n || col >= a.d) continue;
     f32x4 v = {};
     const f32x4* p = (const f32x4*)a.part_kv + (int64_t)j.part0 * kAll + i;
+#pragma unroll 4
     for (int n = 0; n < j.parts; ++n) v += p[(int64_t)n * kAll];
     const sieve_heads& to = i < kAll / 2 ? a.dk : a.dv;
     T* t = (T*)to.data + (j.t0 + key) * to.token_stride + j.kvh * to.head_stride + col;
@@ -1423,15 +1418,15 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_join_kernel(AttnArgs a)
 
 constexpr int kMaxLds = 160 * 1024;
 
-template <typename K>
-hipError_t launch(K kernel, const AttnArgs& a, int grid, size_t lds, hipStream_t s) {
+template <void (*kKernel)(AttnArgs)>
+hipError_t launch(const AttnArgs& a, int grid, size_t lds, hipStream_t s) {
   if (lds > kMaxLds) return hipErrorInvalidValue;
   if (lds > 64 * 1024) {  // more has to be asked for, once for each kernel
-    const hipError_t e = hipFuncSetAttribute(
-        (const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
+    static const hipError_t asked = hipFuncSetAttribute(
+        (const void*)kKernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+    if (asked != hipSuccess) return asked;
   }
-  kernel<<<grid, kAttnThreads, lds, s>>>(a);
+  kKernel<<<grid, kAttnThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -1440,20 +1435,16 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
   const size_t table = kBias ? (size_t)a.G * a.span * sizeof(float) : 0;
   switch (kind) {
     case kAttnFwd:
-      return launch(attn_forward_kernel<T, DP, 1, kBias, kVec>, a, grid,
-                    FwdShape<T, DP, 1>::kBytes + table, s);
+      return launch<attn_forward_kernel<T, DP, 1, kBias, kVec>>(a, grid, FwdShape<T, DP, 1>::kBytes + table, s);
     case kAttnFwdFew:
-      return launch(attn_forward_kernel<T, DP, 4, kBias, kVec>, a, grid,
-                    FwdShape<T, DP, 4>::kBytes + table, s);
+      return launch<attn_forward_kernel<T, DP, 4, kBias, kVec>>(a, grid, FwdShape<T, DP, 4>::kBytes + table, s);
     case kAttnDq: {
       const size_t sums =
           a.dbias ? kAttnWaves * (table + kDiagWords * sizeof(float)) : 0;
-      return launch(attn_dq_kernel<T, DP, kBias, kVec>, a, grid,
-                    DqShape<T, DP, kBias>::kBytes + table + sums, s);
+      return launch<attn_dq_kernel<T, DP, kBias, kVec>>(a, grid, DqShape<T, DP, kBias>::kBytes + table + sums, s);
     }
     case kAttnDkv:
-      return launch(attn_dkv_kernel<T, DP, kBias, kVec>, a, grid,
-                    DkvShape<T, DP>::kBytes + table, s);
+      return launch<attn_dkv_kernel<T, DP, kBias, kVec>>(a, grid, DkvShape<T, DP>::kBytes + table, s);
     default:
       return hipErrorInvalidValue;
   }
@@ -1461,9 +1452,11 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
 
 template <typename T, int DP>
 hipError_t launch_dp(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
-  if (kind == kAttnDkvJoin) return launch(attn_dkv_join_kernel<T, DP>, a, grid, 0, s);
-  if (kind == kAttnJoin) return launch(attn_join_kernel<T, DP, kAttnRows>, a, grid, 0, s);
-  if (kind == kAttnJoinFew) return launch(attn_join_kernel<T, DP, kAttnFewRows>, a, grid, 0, s);
+  if (kind == kAttnDkvJoin) return launch<attn_dkv_join_kernel<T, DP>>(a, grid * kDkvJoinGroups, 0, s);
+  if (kind == kAttnJoin) return launch<attn_join_kernel<T, DP, kAttnRows>>(
+        a, grid * ((kAttnRows + kJoinRows<DP> - 1) / kJoinRows<DP>), 0, s);
+  if (kind == kAttnJoinFew) return launch<attn_join_kernel<T, DP, kAttnFewRows>>(
+        a, grid * ((kAttnFewRows + kJoinRows<DP> - 1) / kJoinRows<DP>), 0, s);
   if (a.bias)
     return a.vec ? launch_as<T, DP, true, true>(kind, a, grid, s)
                  : launch_as<T, DP, true, false>(kind, a, grid, s);

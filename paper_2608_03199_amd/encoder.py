@@ -71,13 +71,22 @@ def _library():
     return lib
 
 
+_nothing = contextlib.nullcontext()
+
+
 def _on(device: torch.device, stream):
     """The device and the stream that the call's allocations and kernels belong to."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return _nothing
     stack = contextlib.ExitStack()
     stack.enter_context(torch.cuda.device(device))
     if stream is not None:
         stack.enter_context(torch.cuda.stream(stream))
     return stack
+
+
+def _raw_stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -101,14 +110,15 @@ def _code(t: torch.Tensor, name: str) -> int:
     return _CODES[t.dtype]
 
 
-def _rows(t: torch.Tensor, n: int) -> torch.Tensor:
-    """[rows, n] with neighbouring values side by side; copied only where that is not a view."""
+def _rows(t: torch.Tensor, n: int):
+    """``t`` as rows of n values side by side, at least n apart, and how far apart; copied only
+    where that is not a view."""
+    if t.is_contiguous():
+        return t, n
     t = t.reshape(-1, n)
-    return t if t.stride(1) == 1 or n == 1 else t.contiguous()
-
-
-def _row_stride(t: torch.Tensor) -> int:
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    if t.shape[0] > 1 and t.stride(0) >= n and (n == 1 or t.stride(1) == 1):
+        return t, t.stride(0)
+    return t.contiguous(), n
 
 
 # ---- layer norm ---------------------------------------------------------------------------
@@ -129,30 +139,22 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[tor
               residual.device == x.device, "residual must match x")
     lib = _library()
     with _on(x.device, stream):
-        s = torch.cuda.current_stream().cuda_stream
-        xr = _rows(x, n)
-        rr = _rows(residual, n) if residual is not None else None
+        s = _raw_stream()
+        xr, x_stride = _rows(x, n)
+        rr, r_stride = (None, 0) if residual is None else _rows(residual, n)
         w, b = weight.contiguous(), None if bias is None else bias.contiguous()
-        rows = xr.shape[0]
+        rows = x.numel() // n
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        h = torch.empty_like(y) if rr is not None else None
-        stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
+        h = None if rr is None else torch.empty_like(y)
+        mean, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32,
+                                 device=x.device).unbind(0)
         if rows:
-            if _row_overlap(xr):
-                xr = xr.contiguous()
-            if rr is not None and _row_overlap(rr):
-                rr = rr.contiguous()
             _check(lib, lib.sieve_norm_forward(
-                xr.data_ptr(), _row_stride(xr), _ptr(rr), 0 if rr is None else _row_stride(rr),
-                w.data_ptr(), _ptr(b), code, _CODES[w.dtype], rows, n, float(eps), y.data_ptr(),
-                _ptr(h), mean.data_ptr(), rstd.data_ptr(), s))
+                xr.data_ptr(), x_stride, None if rr is None else rr.data_ptr(), r_stride,
+                w.data_ptr(), None if b is None else b.data_ptr(), code, _CODES[w.dtype], rows, n,
+                eps, y.data_ptr(), None if h is None else h.data_ptr(), mean.data_ptr(),
+                rstd.data_ptr(), s))
     return y, x if h is None else h, mean, rstd
-
-
-def _row_overlap(t: torch.Tensor) -> bool:
-    """Rows closer than their length (an expanded tensor): the kernels take none such."""
-    return t.shape[0] > 1 and t.stride(0) < t.shape[1]
 
 
 def _check_affine(x, weight, bias, n):
@@ -188,12 +190,9 @@ def layer_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor,
               t.is_contiguous(), f"{name} must be the forward pass's, one float32 a row")
     lib = _library()
     with _on(h.device, stream):
-        s = torch.cuda.current_stream().cuda_stream
-        hr, dr = _rows(h, n), _rows(dy, n)
-        if _row_overlap(hr):
-            hr = hr.contiguous()
-        if _row_overlap(dr):
-            dr = dr.contiguous()
+        s = _raw_stream()
+        hr, h_stride = _rows(h, n)
+        dr, dy_stride = _rows(dy, n)
         er = None if dh is None else dh.contiguous()
         w = weight.contiguous()
         dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
@@ -202,7 +201,7 @@ def layer_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor,
         size = lib.sieve_norm_workspace(rows, n)
         space = _workspace(lib, size, h.device)
         _check(lib, lib.sieve_norm_backward(
-            _ptr(dr), _row_stride(dr), _ptr(hr), _row_stride(hr), w.data_ptr(), _ptr(mean),
+            _ptr(dr), dy_stride, _ptr(hr), h_stride, w.data_ptr(), _ptr(mean),
             _ptr(rstd), _ptr(er), code, _CODES[w.dtype], rows, n, _ptr(dx), _ptr(dw), _ptr(db),
             _ptr(space), int(size), s))
     return dx, dw, db
@@ -268,8 +267,12 @@ class AttentionPlan:
         self.queries, self.keys = int(qo[-1]), int(ko[-1])
         _need(self.head_dim >= 1, "head_dim must be at least 1")
         self.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
-        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None \
-            else torch.device(device)
+        device = torch.device("cuda" if device is None else device)
+        _need(device.type == "cuda", "a plan needs a GPU")
+        self.device = device if device.index is not None else \
+            torch.device("cuda", torch.cuda.current_device())
+        self._q_shape = torch.Size((self.queries, self.heads, self.head_dim))
+        self._k_shape = torch.Size((self.keys, self.kv_heads, self.head_dim))
         desc = _Desc(_CODES[dtype], self.heads, self.kv_heads, self.head_dim, int(self.causal),
                      self.num_buckets, self.max_distance, self.scale, qo.numel() - 1,
                      qo.data_ptr(), ko.data_ptr())
@@ -292,27 +295,23 @@ class AttentionPlan:
         except Exception:
             pass
 
-    def _tensor(self, t: torch.Tensor, name: str, tokens: int, heads: int) -> torch.Tensor:
+    def _tensor(self, t: torch.Tensor, name: str, shape) -> torch.Tensor:
         if t.dtype != self.dtype:
             raise TypeError(f"{name} must be {self.dtype}, not {t.dtype}")
-        _need(t.is_cuda and t.device == self._device(), f"{name} must be on the plan's device")
-        _need(tuple(t.shape) == (tokens, heads, self.head_dim),
-              f"{name} must be [{tokens}, {heads}, {self.head_dim}], not {list(t.shape)}")
-        return t
-
-    def _device(self):
-        d = self.device
-        return d if d.index is not None else torch.device("cuda", 0)
+        if t.shape != shape or t.device != self.device:
+            raise ValueError(f"{name} must be {list(shape)} on {self.device}, "
+                             f"not {list(t.shape)} on {t.device}")
+        return _side_by_side(t)
 
     def _inputs(self, q, k, v, key_mask, bias):
         if self._h is None:
             raise SieveError(-1, "the plan is closed")
-        q = self._tensor(q, "q", self.queries, self.heads)
-        k = self._tensor(k, "k", self.keys, self.kv_heads)
-        v = self._tensor(v, "v", self.keys, self.kv_heads)
+        q = self._tensor(q, "q", self._q_shape)
+        k = self._tensor(k, "k", self._k_shape)
+        v = self._tensor(v, "v", self._k_shape)
         if key_mask is not None:
             _need(key_mask.dtype in (torch.bool, torch.uint8) and
-                  tuple(key_mask.shape) == (self.keys,) and key_mask.device == q.device,
+                  key_mask.shape == (self.keys,) and key_mask.device == self.device,
                   f"key_mask must be [{self.keys}] bool on the plan's device")
             key_mask = key_mask.contiguous()
         _need((bias is not None) == (self.num_buckets > 0),
@@ -320,8 +319,8 @@ class AttentionPlan:
         if bias is not None:
             if bias.dtype != self.dtype:
                 raise TypeError(f"bias must be {self.dtype}, not {bias.dtype}")
-            _need(tuple(bias.shape) == (self.num_buckets, self.heads) and
-                  bias.device == q.device, f"bias must be [{self.num_buckets}, {self.heads}]")
+            _need(bias.shape == (self.num_buckets, self.heads) and bias.device == self.device,
+                  f"bias must be [{self.num_buckets}, {self.heads}] on the plan's device")
             bias = bias.contiguous()
         return q, k, v, key_mask, bias
 
@@ -331,17 +330,15 @@ class AttentionPlan:
         """``q`` [queries, heads, head_dim], ``k`` and ``v`` [keys, kv_heads, head_dim], any
         strides with neighbouring values side by side; ``key_mask`` [keys], False: not seen.
         Returns ``(out, lse)``: the output and the fp32 logarithm of each row's sum."""
-        with _on(self._device(), stream):
-            s = torch.cuda.current_stream().cuda_stream
+        with _on(self.device, stream):
+            s = _raw_stream()
             q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
-            out = torch.empty((self.queries, self.heads, self.head_dim), dtype=self.dtype,
-                              device=q.device)
-            lse = torch.empty((self.queries, self.heads), dtype=torch.float32, device=q.device)
-            space = _workspace(self._lib, self._space[0], q.device)
-            q, k, v = (_heads(t) for t in (q, k, v))
+            out = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
+            lse = torch.empty((self.queries, self.heads), dtype=torch.float32, device=self.device)
+            space = _workspace(self._lib, self._space[0], self.device)
             _check(self._lib, self._lib.sieve_attn_forward(
-                self._h, q, k, v, _ptr(key_mask), _ptr(bias), _heads(out), _ptr(lse), _ptr(space),
-                self._space[0], s))
+                self._h, _heads(q), _heads(k), _heads(v), _ptr(key_mask), _ptr(bias), _heads(out),
+                lse.data_ptr(), _ptr(space), self._space[0], s))
         return out, lse
 
     def backward(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -350,40 +347,35 @@ class AttentionPlan:
                  stream=None):
         """Gradients from the output's, and the forward pass's inputs and results.  Returns
         ``(dq, dk, dv, dbias)``; ``dbias`` is None without a bias (or with ``bias_grad=False``)."""
-        with _on(self._device(), stream):
-            s = torch.cuda.current_stream().cuda_stream
+        with _on(self.device, stream):
+            s = _raw_stream()
             q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
-            dout = self._tensor(dout, "dout", self.queries, self.heads)
-            out = self._tensor(out, "out", self.queries, self.heads)
-            _need(tuple(lse.shape) == (self.queries, self.heads) and lse.is_contiguous() and
-                  lse.dtype == torch.float32 and lse.device == q.device,
+            dout = self._tensor(dout, "dout", self._q_shape)
+            out = self._tensor(out, "out", self._q_shape)
+            _need(lse.shape == self._q_shape[:2] and lse.is_contiguous() and
+                  lse.dtype == torch.float32 and lse.device == self.device,
                   "lse must be the forward pass's")
-            dq = torch.empty((self.queries, self.heads, self.head_dim), dtype=self.dtype,
-                             device=q.device)
-            dk = torch.empty((self.keys, self.kv_heads, self.head_dim), dtype=self.dtype,
-                             device=q.device)
+            dq = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
+            dk = torch.empty(self._k_shape, dtype=self.dtype, device=self.device)
             dv = torch.empty_like(dk)
             want = bias is not None and bias_grad is not False
             dbias = torch.empty_like(bias) if want else None
-            space = _workspace(self._lib, self._space[1], q.device)
-            dout, q, k, v, out = (_heads(t) for t in (dout, q, k, v, out))
+            space = _workspace(self._lib, self._space[1], self.device)
             _check(self._lib, self._lib.sieve_attn_backward(
-                self._h, dout, q, k, v, out, _ptr(lse), _ptr(key_mask), _ptr(bias), _heads(dq),
-                _heads(dk), _heads(dv), _ptr(dbias), _ptr(space), self._space[1], s))
+                self._h, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), _ptr(lse),
+                _ptr(key_mask), _ptr(bias), _heads(dq), _heads(dk), _heads(dv), _ptr(dbias),
+                _ptr(space), self._space[1], s))
         return dq, dk, dv, dbias
 
 
-class _View(_Heads):
-    """A ``sieve_heads`` that keeps the tensor it points into."""
-    keep = None
+def _side_by_side(t: torch.Tensor) -> torch.Tensor:
+    """A view that the kernels take (a head's values side by side), else a copy."""
+    return t if t.stride(2) == 1 or t.shape[2] == 1 or t.numel() == 0 else t.contiguous()
 
 
-def _heads(t: torch.Tensor) -> _View:
-    if t.numel() and ((t.shape[2] > 1 and t.stride(2) != 1) or min(t.stride()) < 0):
-        t = t.contiguous()
-    h = _View(_ptr(t), t.stride(0), t.stride(1))
-    h.keep = t
-    return h
+def _heads(t: torch.Tensor) -> _Heads:
+    token, head, _ = t.stride()
+    return _Heads(t.data_ptr(), token, head)
 
 
 class _Attention(torch.autograd.Function):
