@@ -393,7 +393,8 @@ SIEVE_API int64_t sieve_norm_workspace(int64_t rows, int32_t n);
  * A key is seen unless key_mask leaves it out or, with causal, it lies after the
  * query's position.  A query that sees no key gets out = 0 and lse = -infinity, and
  * gives no gradient.  What keys and values hold where key_mask leaves them out is not
- * used, infinities and NaN included, and their gradients are 0.
+ * used, infinities and NaN included, and their gradients are 0.  With causal, what they
+ * hold after a query's position does not reach that query's output or gradient.
  *
  * bucket(r) of a relative position r (sides = 2, or 1 with causal; side = num_buckets /
  * sides buckets each; r > 0 is the second side, and with causal it never occurs): with
@@ -433,7 +434,8 @@ typedef struct sieve_attn sieve_attn; /* opaque, owned by the library */
  * description, cuts the work into tiles and copies their list to the current device
  * (synchronous).  Every layer and both passes over the batch share the plan; any number of
  * calls on any streams may use it at once.  A sequence may have up to 2^31 - 2^16 rows
- * (queries times heads / kv_heads) and keys (else SIEVE_EUNSUPPORTED).
+ * (queries times heads / kv_heads) and keys, a batch 2^40 tokens and about 2^25 tiles of 128
+ * rows or keys by key head (else SIEVE_EUNSUPPORTED).
  * sieve_attn_free waits for the device's work (as hipFree does).
  */
 SIEVE_API int sieve_attn_create(const sieve_attn_desc* desc, void* stream, sieve_attn** out);

@@ -3,37 +3,12 @@
 // type by attn_f32.hip, attn_f16.hip and attn_bf16.hip).
 #pragma once
 
+#include "attn_plan.h"
 #include "enc_common.h"
 
 namespace sieve {
 
-// One work-group's share.  The rows of a sequence for one key head are its queries
-// times the G = heads / kv_heads query heads that read it: row r is query r / G,
-// head kvh * G + r % G, so that the heads of a group share every key they load.
-struct AttnItem {
-  int64_t q0, k0;   // first query and key token of the sequence in the packed batch
-  int32_t nq, nk;   // its queries and keys
-  int32_t kvh;
-  int32_t row;      // first row of the tile (forward, dq), or first key (dk and dv)
-  int32_t lo, hi;   // keys to go through (forward, dq), or rows (dk and dv)
-  int32_t part;     // forward, dk and dv: slot of a partial result, -1 where the item is its
-                    // whole tile; dq: number of the row tile among all sequences
-  int32_t tile0, ntiles;  // dk and dv: the sequence's row tiles of the dq pass
-  int32_t pad;
-};
-
-// One row tile whose keys, or key tile whose rows, several items shared.
-struct AttnJoin {
-  int64_t t0;                // first query (key) token of the sequence
-  int32_t n, kvh, row;       // its queries (keys), the head, the tile's first row (key)
-  int32_t part0, parts, pad;
-};
-
 constexpr int kAttnThreads = 256;
-constexpr int kAttnPad = 64;      // relative positions past the distance in the bias table
-constexpr int kAttnRows = 128;    // rows of a tile: 4 waves of 32
-constexpr int kAttnFewRows = 32;  // rows of a tile whose 4 waves share the keys out
-constexpr int kAttnKeys = 128;    // keys of a dk and dv tile
 
 struct AttnArgs {
   const AttnItem* items;

@@ -1,11 +1,7 @@
 // attn.hip -- the packed attention's plan (work items for a batch's lengths) and C ABI.
 //
-// A plan cuts every sequence into row tiles (forward, dQ) and key tiles (dK, dV) for each
-// key head and writes the list once; a work-group of a launch takes one item of it, so
-// ragged batches launch no empty work-groups.  The items of a sequence and key head follow
-// one another, the list is cut into eight runs of equal cost, one for each XCD (consecutive
-// work-groups go to consecutive XCDs), so that an L2 reads a sequence's keys once, and in a
-// run the longest items come first, so that no long one is left at the end.
+// A plan cuts a batch's work into items (attn_plan.h), copies their lists to the device
+// once, and serves every layer and both passes over the batch.
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -37,90 +33,7 @@ struct sieve_attn {
 
 namespace {
 
-constexpr int kXcds = 8;
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - (int64_t(1) << 16);
-// A forward pass with fewer items than this shares the keys of its row tiles out, at least
-// kMinKeys to an item (below that the joining costs more than the reading).
-constexpr int kWantItems = 1024;
-constexpr int kMinKeys = 512;
-// The same for dK and dV, whose items are tiles of keys and share out their rows.  More items
-// than the GPU holds at once (two to each of 256 CUs) also even out the causal tiles, the
-// first of which are seen by every row and the last by few.
-constexpr int kWantKvItems = 1024;
-constexpr int kMinRows = 1024;
-
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
-
-// Bucket of a relative position (key minus query).  The logarithm's edges are decided in
-// 80-bit arithmetic with room for its rounding: where the exact value is a whole number the
-// result is that number.
-int bucket_of(int rel, int buckets, int distance, bool causal) {
-  const int side = causal ? buckets : buckets / 2;
-  const int base = rel > 0 && !causal ? side : 0;
-  const int m = causal ? std::max(-rel, 0) : std::abs(rel);
-  const int exact = side / 2;
-  if (m < exact) return base + m;
-  if (m >= distance) return base + side - 1;
-  const long double x = (side - exact) * (logl((long double)m / exact) /
-                                          logl((long double)distance / exact));
-  return base + std::min(exact + (int)floorl(x + 1e-12L), side - 1);
-}
-
-// The order of a list of items (see the top of the file).
-void order_items(std::vector<AttnItem>& items) {
-  const int64_t n = (int64_t)items.size();
-  if (n < 2) return;
-  // an item's cost: its rows or keys to go through, and a fixed part for its start and end
-  auto cost = [](const AttnItem& x) { return (int64_t)(x.hi - x.lo) + 256; };
-  int64_t total = 0;
-  for (const auto& x : items) total += cost(x);
-  std::vector<AttnItem> runs[kXcds];
-  int64_t sum = 0;
-  for (const auto& x : items) {
-    runs[std::min<int64_t>(sum * kXcds / total, kXcds - 1)].push_back(x);
-    sum += cost(x);
-  }
-  for (auto& r : runs)
-    std::stable_sort(r.begin(), r.end(),
-                     [&](const AttnItem& p, const AttnItem& q) { return cost(p) > cost(q); });
-  size_t at = 0;
-  for (size_t i = 0; at < (size_t)n; ++i)
-    for (int x = 0; x < kXcds; ++x)
-      if (i < runs[x].size()) items[at++] = runs[x][i];
-}
-
-// Cuts the ranges of a list that is too short for the GPU into shares of about the same
-// length, a multiple of 128 and at least `least`; join_of(item) starts the record that brings
-// an item's shares together.
-template <typename F>
-void share_out(std::vector<AttnItem>& items, std::vector<AttnJoin>& joins, int want, int least,
-               int32_t& parts, F join_of) {
-  if (items.empty() || (int64_t)items.size() >= 2 * (int64_t)want) return;
-  int64_t total = 0;
-  for (const auto& x : items) total += x.hi - x.lo;
-  const int64_t share = std::max<int64_t>(least, (total / want + 127) / 128 * 128);
-  std::vector<AttnItem> cut;
-  for (const auto& x : items) {
-    const int64_t length = (int64_t)x.hi - x.lo, n = (length + share / 2) / share;
-    if (n < 2) {
-      cut.push_back(x);
-      continue;
-    }
-    const int64_t each = ((length + n - 1) / n + 127) / 128 * 128;
-    AttnJoin j = join_of(x);
-    j.part0 = parts;
-    for (int64_t at = x.lo; at < x.hi; at += each) {
-      AttnItem y = x;
-      y.lo = (int32_t)at;
-      y.hi = (int32_t)std::min<int64_t>(at + each, x.hi);
-      y.part = parts++;
-      ++j.parts;
-      cut.push_back(y);
-    }
-    joins.push_back(j);
-  }
-  items.swap(cut);
-}
 
 int check_desc(const sieve_attn_desc& c) {
   if (!enc_dtype_ok(c.dtype)) return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16", c.dtype);
@@ -160,10 +73,12 @@ int check_desc(const sieve_attn_desc& c) {
     for (int64_t s = 0; s < c.nseq; ++s) {
       if (o[s + 1] < o[s])
         return set_error(SIEVE_EINVAL, "%s decreases at %lld", name, (long long)s);
-      if ((o[s + 1] - o[s]) * (which ? 1 : G) > kMaxRows)
+      if (o[s + 1] - o[s] > kMaxRows / (which ? 1 : G))
         return set_error(SIEVE_EUNSUPPORTED, "sequence %lld of %s is too long", (long long)s,
                          name);
     }
+    if (o[c.nseq] > kMaxTokens)
+      return set_error(SIEVE_EUNSUPPORTED, "%s ends above %lld", name, (long long)kMaxTokens);
   }
   return SIEVE_OK;
 }
@@ -180,67 +95,13 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
   p->scale = c.scale;
   p->queries = c.nseq ? qo[c.nseq] : 0;
   p->keys = c.nseq ? ko[c.nseq] : 0;
-  int64_t most_rows = 0, row_tiles = 0;
-  for (int64_t s = 0; s < c.nseq; ++s) {
-    const int64_t rows = (qo[s + 1] - qo[s]) * G;
-    most_rows = std::max(most_rows, rows);
-    row_tiles += (rows + kAttnRows - 1) / kAttnRows;
-  }
-  p->few = most_rows <= kAttnFewRows;
-  if (row_tiles * c.kv_heads > INT32_MAX / 2 ||
-      (p->keys / kAttnKeys + c.nseq) * c.kv_heads > INT32_MAX / 2)
+  AttnLists lists;
+  if (!make_lists(qo, ko, c.nseq, c.kv_heads, G, c.causal != 0, &lists))
     return set_error(SIEVE_EUNSUPPORTED, "the batch has too many tiles");
-  p->row_tiles = (int32_t)row_tiles;
-
-  std::vector<AttnItem> fwd, dq, dkv;
-  std::vector<AttnJoin> joins, kv_joins;
-  const int tile = p->few ? kAttnFewRows : kAttnRows;
-  int32_t tile0 = 0;
-  for (int64_t s = 0; s < c.nseq; ++s) {
-    AttnItem x{};
-    x.q0 = qo[s];
-    x.k0 = ko[s];
-    x.nq = (int32_t)(qo[s + 1] - qo[s]);
-    x.nk = (int32_t)(ko[s + 1] - ko[s]);
-    const int64_t rows = (int64_t)x.nq * G, shift = (int64_t)x.nk - x.nq;
-    x.tile0 = tile0;
-    x.ntiles = (int32_t)((rows + kAttnRows - 1) / kAttnRows);
-    tile0 += x.ntiles;
-    // keys that rows up to `last` see
-    auto keys_of = [&](int64_t last) {
-      return c.causal ? (int32_t)std::clamp<int64_t>(last / G + shift + 1, 0, x.nk) : x.nk;
-    };
-    for (x.kvh = 0; x.kvh < c.kv_heads; ++x.kvh) {
-      x.lo = 0;
-      x.part = -1;
-      for (int64_t r = 0; r < rows; r += tile) {
-        x.row = (int32_t)r;
-        x.hi = keys_of(std::min<int64_t>(r + tile, rows) - 1);
-        fwd.push_back(x);
-      }
-      for (int64_t r = 0; r < rows; r += kAttnRows) {
-        x.row = (int32_t)r;
-        x.hi = keys_of(std::min<int64_t>(r + kAttnRows, rows) - 1);
-        x.part = x.tile0 + (int32_t)(r / kAttnRows);
-        dq.push_back(x);
-      }
-      x.hi = (int32_t)rows;
-      x.part = -1;
-      for (int64_t k = 0; k < x.nk; k += kAttnKeys) {
-        x.row = (int32_t)k;
-        x.lo = c.causal ? (int32_t)std::clamp<int64_t>((k - shift) * G, 0, rows) : 0;
-        dkv.push_back(x);
-      }
-    }
-  }
-  // too few items to fill the GPU: share the keys (the rows) of the long ones out
-  share_out(fwd, joins, kWantItems, kMinKeys, p->parts,
-            [](const AttnItem& x) { return AttnJoin{x.q0, x.nq, x.kvh, x.row, 0, 0, 0}; });
-  share_out(dkv, kv_joins, kWantKvItems, kMinRows, p->kv_parts,
-            [](const AttnItem& x) { return AttnJoin{x.k0, x.nk, x.kvh, x.row, 0, 0, 0}; });
-  order_items(fwd);
-  order_items(dq);
-  order_items(dkv);
+  p->few = lists.few;
+  p->row_tiles = lists.row_tiles;
+  p->parts = lists.parts;
+  p->kv_parts = lists.kv_parts;
   std::vector<int16_t> buckets, range;
   if (c.num_buckets) {
     p->nb = c.num_buckets;
@@ -255,11 +116,11 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
       range[2 * b + 1] = (int16_t)(i + 1);
     }
   }
-  p->nfwd = (int32_t)fwd.size();
-  p->ndq = (int32_t)dq.size();
-  p->ndkv = (int32_t)dkv.size();
-  p->njoins = (int32_t)joins.size();
-  p->nkv_joins = (int32_t)kv_joins.size();
+  p->nfwd = (int32_t)lists.fwd.size();
+  p->ndq = (int32_t)lists.dq.size();
+  p->ndkv = (int32_t)lists.dkv.size();
+  p->njoins = (int32_t)lists.joins.size();
+  p->nkv_joins = (int32_t)lists.kv_joins.size();
 
   // one allocation, one copy
   std::vector<uint8_t> host;
@@ -269,13 +130,13 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
     host.resize(round256(host.size() + bytes));
     if (bytes) memcpy(host.data() + at[i], v, bytes);
   };
-  add(0, fwd.data(), fwd.size() * sizeof(AttnItem));
-  add(1, dq.data(), dq.size() * sizeof(AttnItem));
-  add(2, dkv.data(), dkv.size() * sizeof(AttnItem));
-  add(3, joins.data(), joins.size() * sizeof(AttnJoin));
+  add(0, lists.fwd.data(), lists.fwd.size() * sizeof(AttnItem));
+  add(1, lists.dq.data(), lists.dq.size() * sizeof(AttnItem));
+  add(2, lists.dkv.data(), lists.dkv.size() * sizeof(AttnItem));
+  add(3, lists.joins.data(), lists.joins.size() * sizeof(AttnJoin));
   add(4, buckets.data(), buckets.size() * sizeof(int16_t));
   add(5, range.data(), range.size() * sizeof(int16_t));
-  add(6, kv_joins.data(), kv_joins.size() * sizeof(AttnJoin));
+  add(6, lists.kv_joins.data(), lists.kv_joins.size() * sizeof(AttnJoin));
   ENC_HIP_TRY(hipGetDevice(&p->device));
   if (host.empty()) return SIEVE_OK;
   ENC_HIP_TRY(hipMalloc(&p->mem, host.size()));
@@ -329,7 +190,7 @@ bool heads_vec(const sieve_heads& x, int size, int G) {
     return false;
   constexpr int64_t kMost = int64_t(1) << 40;  // far past 2^31: keeps the products small
   return std::min(x.token_stride, kMost) * kAttnRows * size +
-             std::min(x.head_stride, kMost) * G * size <
+             std::min(x.head_stride, kMost) * G * size + SIEVE_ATTN_MAX_DIM * size <
          (int64_t(1) << 31);
 }
 

@@ -27,7 +27,7 @@
 // 16-bit matrix units; S, dP, the statistics and every accumulator are fp32.  bfloat16
 // keeps fp32's range.  binary16 does not, so there the values are scaled by powers of two
 // that the end takes out exactly: P by 2^11 at the running maximum (forward) or by 2^14
-// (backward, where P <= 1), and dS by what brings its largest magnitude to 2^13 .. 2^14.
+// (dV, where P <= 1), and dS by what brings its largest magnitude to 2^13 .. 2^14.
 #pragma once
 
 #include "attn.h"
@@ -496,6 +496,95 @@ __device__ __forceinline__ float add_up(f32x8 p, float x) {
   return x;
 }
 
+// Whether the 32 rows from row0 of a tile hold an infinity or NaN in the wave's columns.
+// (A bfloat16 sum may also overflow: the answer is then the careful path, which is right too.)
+template <typename T, int DP>
+__device__ __forceinline__ bool odd_values(lds_addr at, int row0) {
+  float x = 0.f;
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int e = 0; e < DP / 32; ++e)
+      x = add_up(frag_across<T, DP>(at, row0 + 16 * c, 32 * e), x);
+  return __any(!(fabsf(x) < INFINITY));
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ float wave_add(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// One row again, without products of keys that it does not see: where a block that causal
+// rows see in part holds infinities or NaN, 0 times such a value would reach the rows before
+// it.  A wave a row, 64 keys at a time, a key a lane for the scores and two values a lane for
+// the sums.  Rare, and slow next to the products it replaces.
+//   kGrad = false: acc += P v relative to 2^m, with the sum l; true: acc += dS k, with m the
+//   row's lse in units of log2 and l its D.
+template <typename T, bool kBias, bool kGrad>
+__device__ void careful_row(const AttnArgs& a, const AttnItem& it, const float* bias, int r,
+                            int lane, float (&acc)[2], float& m, float& l) {
+  const int tok = query_of(a, r), pos = tok + it.nk - it.nq, d = a.d;
+  const float* table = kBias ? bias + (r - tok * a.G) * a.span : nullptr;
+  const T* q = (const T*)a.q.data + row_at(a, a.q, it, r);
+  const T* dout = kGrad ? (const T*)a.dout.data + row_at(a, a.dout, it, r) : nullptr;
+  const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
+  const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
+  const float scale2 = a.scale * kLog2e;
+  acc[0] = acc[1] = 0.f;
+  if (!kGrad) {
+    m = -INFINITY;
+    l = 0.f;
+  }
+  const int end = a.causal && pos + 1 < it.hi ? pos + 1 : it.hi;
+  for (int base = it.lo; base < end; base += 64) {
+    const int key = base + lane;
+    const bool seen = key < end && (!a.key_mask || a.key_mask[it.k0 + key] != 0);
+    float s = -INFINITY, dp = 0.f;
+    if (seen) {
+      const T* k = k0 + key * a.k.token_stride;
+      s = 0.f;
+      for (int c = 0; c < d; ++c) s += (float)q[c] * (float)k[c];
+      s *= scale2;
+      if (kBias) {
+        int rel = key - pos;
+        rel = rel < -a.distance ? -a.distance : rel > a.distance ? a.distance : rel;
+        s += table[rel + a.distance + kAttnPad];
+      }
+      if (kGrad) {
+        const T* v = v0 + key * a.v.token_stride;
+        for (int c = 0; c < d; ++c) dp += (float)dout[c] * (float)v[c];
+      }
+    }
+    float x;  // what the key's row is multiplied with
+    if (kGrad) {
+      x = seen ? __builtin_amdgcn_exp2f(s - m) * (dp - l) : 0.f;
+    } else {
+      const float next = fmaxf(m, wave_max(s)), at = next == -INFINITY ? 0.f : next;
+      const float f = __builtin_amdgcn_exp2f(m - at);
+      x = seen ? __builtin_amdgcn_exp2f(s - at) : 0.f;
+      l = l * f + wave_add(x);
+      acc[0] *= f;
+      acc[1] *= f;
+      m = next;
+    }
+    const uint64_t these = __ballot(seen);
+    for (int j = 0; j < 64; ++j) {
+      if (!(these >> j & 1)) continue;
+      const float xj = __shfl(x, j);
+      const T* row = kGrad ? k0 + (int64_t)(base + j) * a.k.token_stride
+                           : v0 + (int64_t)(base + j) * a.v.token_stride;
+      if (lane < d) acc[0] += xj * (float)row[lane];
+      if (lane + 64 < d) acc[1] += xj * (float)row[lane + 64];
+    }
+  }
+}
+
 // ---- forward ----------------------------------------------------------------------------
 // WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
 // each wave takes every fourth block of 32 keys, and LDS joins the four at the end: for
@@ -508,7 +597,7 @@ struct FwdShape {
   static constexpr int kTileBytes = kTile * DP * (int)sizeof(T);
   static constexpr int kBufs = 4 * kTileBytes <= 128 * 1024 ? 2 : 1;
   static constexpr int kStageBytes = 2 * kBufs * kTileBytes;
-  static constexpr int kJoinBytes = WK == 1 ? 0 : (WK * 32 * (DP + 4) + 2 * WK * 32) * 4;
+  static constexpr int kJoinBytes = WK == 1 ? 0 : (WK * 32 * (DP + 4) + 2 * WK * 32 + WK) * 4;
   static constexpr int kBytes = kStageBytes > kJoinBytes ? kStageBytes : kJoinBytes;
   static constexpr int kRows = WK == 1 ? kAttnRows : kAttnFewRows;
 };
@@ -559,6 +648,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
   float m = -INFINITY, l = 0.f;
+  bool odd = false;  // the wave's rows have to be done again (careful_row)
   const int skip = WK == 1 ? 0 : wave * 32 * DP;  // the wave's keys in a tile
   const lds_addr k_al = lds_of(s_k + skip) + lane_along<T, DP>(lane);
   const lds_addr v_ac = lds_of(s_v + skip) + lane_across<T, DP>(lane);
@@ -611,6 +701,11 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           for (int r = 0; r < 16; ++r) o[b][r] *= f;
       }
       const float off = (m == -INFINITY ? 0.f : m) - kShift<T>;
+      if (a.causal) {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+          if (!__all(bits[b] == ~0u)) odd |= odd_values<T, DP>(sv, 32 * b);
+      }
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
@@ -640,12 +735,15 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     // join the waves: sums relative to the largest maximum
     float* s_o = (float*)smem;
     float* s_ml = s_o + WK * 32 * (DP + 4);
+    int* s_odd = (int*)(s_ml + 2 * WK * 32);
     __syncthreads();
+    if (lane == 0) s_odd[wave] = odd;
     if (h == 0) {
       s_ml[(wave * 32 + lane) * 2] = l == 0.f ? -INFINITY : at;
       s_ml[(wave * 32 + lane) * 2 + 1] = l;
     }
     __syncthreads();
+    odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
     float most = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < WK; ++w) most = fmaxf(most, s_ml[(w * 32 + (lane & 31)) * 2]);
@@ -665,7 +763,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         *(f32x4*)(s_o + (wave * 32 + (lane & 31)) * (DP + 4) + 32 * b + 8 * g + 4 * h) = v;
       }
     __syncthreads();
-    if (wave) return;
+    if (wave && !odd) return;
     l = sum;
     at = most;
 #pragma unroll
@@ -679,6 +777,35 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[b][4 * g + j] = v[j];
       }
+  }
+  if (__builtin_expect(odd, 0)) {
+    const int each = 32 / WK, first = WK == 1 ? wave * 32 : wave * each;
+    for (int i = first; i < first + each && it.row + i < it.nq * G; ++i) {
+      float acc[2], max_, sum_;
+      careful_row<T, kBias, false>(a, it, s_bias, it.row + i, lane, acc, max_, sum_);
+      const int64_t slot = (int64_t)it.part * Shape::kRows + i;
+      const int r = it.row + i, tok = query_of(a, r);
+      const float inv = sum_ == 0.f ? 0.f : 1.f / sum_;
+#pragma unroll
+      for (int e = 0; e < (DP + 63) / 64; ++e) {
+        const int col = lane + 64 * e;
+        if (it.part >= 0) {
+          if (col < DP) a.part_o[slot * DP + col] = acc[e];
+        } else if (col < d) {
+          ((T*)a.o.data + row_at(a, a.o, it, r))[col] = (T)(acc[e] * inv);
+        }
+      }
+      if (lane == 0) {
+        if (it.part >= 0) {
+          a.part_ml[slot * 2] = max_;
+          a.part_ml[slot * 2 + 1] = sum_;
+        } else if (a.lse) {
+          a.lse[(it.q0 + tok) * a.heads + it.kvh * G + (r - tok * G)] =
+              sum_ == 0.f ? -INFINITY : (max_ + __builtin_amdgcn_logf(sum_)) * kLn2;
+        }
+      }
+    }
+    return;
   }
   if (it.part >= 0) {
     const int64_t slot = (int64_t)it.part * Shape::kRows + (WK == 1 ? wave * 32 : 0) + (lane & 31);
@@ -740,6 +867,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
     a.lse[(j.t0 + tok) * a.heads + head] =
         l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
 }
+
+// The backward pass's probabilities are at most 1 and are computed times 2^kUp: the exponential
+// unit returns 0 for results below the normal range, which this leaves room for.
+constexpr float kUp = 24.f, kUpOut = 0x1p-24f;
 
 // ---- backward: dQ and the bias table's gradient ------------------------------------------
 // A wave takes 32 of the tile's 128 rows and goes through the keys as the forward pass does.
@@ -850,7 +981,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   {
     const float lse = me.live ? a.lse[at] : -INFINITY;
     const bool some = lse != -INFINITY;
-    if (some) lse2 = lse * kLog2e;
+    if (some) lse2 = lse * kLog2e - kUp;
     const T* pq = (const T*)a.q.data + (me.live ? row_at(a, a.q, it, me.r) : 0);
     const T* pd = (const T*)a.dout.data + (me.live ? row_at(a, a.dout, it, me.r) : 0);
     const T* po = (const T*)a.o.data + (me.live ? row_at(a, a.o, it, me.r) : 0);
@@ -893,8 +1024,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
   const lds_addr k_al = lds_of(s_k) + lane_along<T, DP>(lane);
   const lds_addr k_ac = lds_of(s_k) + lane_across<T, DP>(lane);
-  float most = 0.f;                  // largest |dS| of the row so far
-  float up = kScaled ? 0x1p40f : 1;  // dS is rounded times this
+  bool odd = false;                  // the wave's dQ has to be done again (careful_row)
+  float most = 0.f;                  // largest |dS| of the row so far, times 2^kUp
+  float up = kScaled ? 0x1p16f : 1;  // and is rounded times this
 
   int buf = 0;
   if (it.lo < it.hi) {
@@ -985,6 +1117,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] *= up;
         }
+        if (a.causal && !__all(bits[b] == ~0u)) odd |= odd_values<T, DP>(sk_ac, 32 * b);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const vec8<T> p = frag_of<T>(s, c);
@@ -1001,8 +1134,21 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       __syncthreads();
     }
   }
-  if (me.live)
-    store_row<T, DP, kVec>((T*)a.dq.data + row_at(a, a.dq, it, me.r), dq, a.scale / up, d,
+  if (__builtin_expect(odd, 0)) {
+    const int first = it.row + wave * 32;
+    for (int i = 0; i < 32 && first + i < it.nq * G; ++i) {
+      float acc[2];
+      float m_ = __shfl(lse2, i) + kUp, l_ = __shfl(dsum, i);
+      careful_row<T, kBias, true>(a, it, s_bias, first + i, lane, acc, m_, l_);
+#pragma unroll
+      for (int e = 0; e < (DP + 63) / 64; ++e)
+        if (lane + 64 * e < d)
+          ((T*)a.dq.data + row_at(a, a.dq, it, first + i))[lane + 64 * e] =
+              (T)(acc[e] * a.scale);
+    }
+  } else if (me.live)
+    store_row<T, DP, kVec>((T*)a.dq.data + row_at(a, a.dq, it, me.r), dq,
+                           a.scale / up * kUpOut, d,
                      h);
   if constexpr (kScaled) {
 #pragma unroll
@@ -1013,7 +1159,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     __syncthreads();
     if (threadIdx.x == 0)
       a.part_max[(int64_t)it.kvh * a.row_tiles + it.part] =
-          fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+          fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])) * kUpOut;
   }
   if constexpr (kBias) {
     if (!want_bias) return;
@@ -1068,7 +1214,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       }
 #pragma unroll
       for (int o = 4; o; o >>= 1) t += __shfl_xor(t, o);
-      if (sub == 0) to[i] = t;
+      if (sub == 0) to[i] = t * kUpOut;
     }
   }
 }
@@ -1126,6 +1272,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   constexpr int kTileN = kTile * DP;
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
+  // P is computed, and rounded, times 2^kUpP
+  constexpr float kUpP = kScaled ? 14.f : kUp, kUpPOut = kScaled ? 0x1p-14f : kUpOut;
   const int reducers = (int)gridDim.x - a.nitems;
   if (kBias && (int)blockIdx.x < reducers) {
     reduce_bias<T>(a, blockIdx.x, (float*)smem);
@@ -1134,7 +1282,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_val = (T*)smem;
   T* s_q = (T*)(smem + Shape::kValueBytes);
   T* s_do = s_q + Shape::kBufs * kTileN;
-  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][-lse / scale, -D, table offset, pos][row]
+  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][the row's exponent, -D, table offset, pos][row]
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x - reducers];
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
@@ -1210,7 +1358,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     st_do.store(s_do + b * kTileN, some_empty, [&](int i) { return piece_lse[i] != -INFINITY; });
     if (row_mine) {
       float* p = s_row + b * 4 * kTile + threadIdx.x;
-      p[0] = row_lse == -INFINITY ? -INFINITY : -row_lse / a.scale;
+      p[0] = row_lse == -INFINITY ? -INFINITY : (kUpP - row_lse * kLog2e) / scale2;
       p[kTile] = -row_d;
       ((int*)p)[2 * kTile] = row_off;
       ((int*)p)[3 * kTile] = row_pos;
@@ -1235,7 +1383,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     }
   }
   if constexpr (kBias) load_bias<T>(a, it.kvh, s_bias);
-  float up = 1.f;  // dS is rounded times this, and P times 2^14 (f16 only)
+  float up = 1.f;  // what brings dS times 2^kUpP to where it is rounded
   if constexpr (kScaled) {
     float most = 0.f;
     const float* p = a.part_max + (int64_t)it.kvh * a.row_tiles + it.tile0;
@@ -1243,7 +1391,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
     for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     const int e = most > 0.f && most < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
-    up = __builtin_amdgcn_ldexpf(1.f, e < 40 ? e : 40);
+    up = __builtin_amdgcn_ldexpf(kUpPOut, e < 40 ? e : 40);
   }
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -1339,10 +1487,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           dp[r] *= s[r];
-          if constexpr (kScaled) {
-            dp[r] *= up;
-            s[r] *= 0x1p14f;
-          }
+          if constexpr (kScaled) dp[r] *= up;
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -1369,7 +1514,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   }
   if (it.part >= 0) {
     float* p = a.part_kv + ((int64_t)it.part * 2 * kAttnKeys + wave * 32 + (lane & 31)) * DP;
-    const float fk = a.scale / up, fv = kScaled ? 0x1p-14f : 1.f;
+    const float fk = a.scale / up * kUpPOut, fv = kUpPOut;
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
@@ -1385,9 +1530,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   }
   const int64_t tok = it.k0 + key;
   store_row<T, DP, kVec>((T*)a.dk.data + tok * a.dk.token_stride + it.kvh * a.dk.head_stride, dk,
-                   a.scale / up, d, h);
+                   a.scale / up * kUpPOut, d, h);
   store_row<T, DP, kVec>((T*)a.dv.data + tok * a.dv.token_stride + it.kvh * a.dv.head_stride, dv,
-                   kScaled ? 0x1p-14f : 1.f, d, h);
+                   kUpPOut, d, h);
 }
 
 // Partial sums of one key tile to its gradients, kDkvJoinGroups work-groups a tile.
