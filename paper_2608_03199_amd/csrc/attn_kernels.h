@@ -975,6 +975,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   if (it.lo < it.hi) fetch(it.lo, 0);
 
   const int64_t at = (it.q0 + me.tok) * a.heads + it.kvh * G + me.g;
+  // Where a row's keys fit one block, D is summed from P dP there: the output is rounded, which
+  // costs short rows more than the rounding of dS.
+  const bool one_block = it.hi <= 32 && it.hi > 0;
   // a row that saw no key has lse = -infinity; as +infinity it makes every P 0
   float lse2 = INFINITY, dsum = 0.f;
   vec8<T> q[DP / 16], dout[DP / 16];
@@ -1060,15 +1063,23 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
                              first, h, bits[b]);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          s[r] = __builtin_amdgcn_exp2f(kBias ? s[r] - lse2 : s[r] * scale2 - lse2) *
-                 (dp[r] - dsum);  // dS
+          s[r] = __builtin_amdgcn_exp2f(kBias ? s[r] - lse2 : s[r] * scale2 - lse2);
         if (!__all(bits[b] == ~0u)) {
           // P = 0 there, but dP need not be a number
           const uint32_t mine = bits[b] >> (4 * h);
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            s[r] = mine >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : 0.f;
+            dp[r] = mine >> (8 * (r >> 2) + (r & 3)) & 1 ? dp[r] : 0.f;
         }
+        if (b == 0 && one_block) {
+          float t = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) t += s[r] == 0.f ? 0.f : s[r] * dp[r];
+          dsum = (t + __shfl_xor(t, 32)) * kUpOut;
+          if (me.live && h == 0) a.dsum[at] = dsum;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= dp[r] - dsum;  // dS
         if constexpr (kBias) {
           if (want_bias) {
             if (first - me.pos_max >= a.distance || first + 31 - me.pos_min <= -a.distance) {
@@ -1273,6 +1284,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
   // P is computed, and rounded, times 2^kUpP
+  constexpr bool kStartAtRow = sizeof(T) == 2;
   constexpr float kUpP = kScaled ? 14.f : kUp, kUpPOut = kScaled ? 0x1p-14f : kUpOut;
   const int reducers = (int)gridDim.x - a.nitems;
   if (kBias && (int)blockIdx.x < reducers) {
@@ -1358,7 +1370,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     st_do.store(s_do + b * kTileN, some_empty, [&](int i) { return piece_lse[i] != -INFINITY; });
     if (row_mine) {
       float* p = s_row + b * 4 * kTile + threadIdx.x;
-      p[0] = row_lse == -INFINITY ? -INFINITY : (kUpP - row_lse * kLog2e) / scale2;
+      p[0] = row_lse == -INFINITY ? -INFINITY
+                                  : (kUpP - row_lse * kLog2e) / (kStartAtRow ? scale2 : 1.f);
       p[kTile] = -row_d;
       ((int*)p)[2 * kTile] = row_off;
       ((int*)p)[3 * kTile] = row_pos;
@@ -1420,8 +1433,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         const int pos_min = query_of(a, first) + shift, pos_max = query_of(a, last) + shift;
         if (a.causal && pos_max < key0) continue;
         const float* rows = s_row + buf * 4 * kTile + 32 * b + 4 * h;
-        // S - lse and dP - D: the products are added to what is subtracted.  A row without
-        // keys has -infinity there, and P = 0.
+        // S - lse and dP - D: the products are added to what is subtracted (but for S in fp32,
+        // where adding its products to a larger number would cost bits).  A row without keys
+        // has -infinity there, and P = 0.
         f32x16 s, dp;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -1429,7 +1443,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           const f32x4 y = *(const f32x4*)(rows + kTile + 8 * g);
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            s[4 * g + t] = x[t];
+            s[4 * g + t] = kStartAtRow ? x[t] : 0.f;
             dp[4 * g + t] = y[t];
           }
         }
@@ -1472,6 +1486,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         } else {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] *= scale2;
+        }
+        if constexpr (!kStartAtRow) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const f32x4 x = *(const f32x4*)(rows + 8 * g);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[4 * g + t] += x[t];
+          }
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
