@@ -43,7 +43,7 @@ enum AttnKind {
   kAttnFwd, kAttnFwdFew, kAttnJoin, kAttnJoinFew, kAttnDq, kAttnDkv, kAttnDkvJoin
 };
 
-// Launch one pass; dp is the padded head size (32, 64 or 128), grid the number of
+// Launch one pass; dp is the padded head size (32, 64, 96 or 128), grid the number of
 // work-groups.
 hipError_t attn_launch_f32(AttnKind kind, int dp, const AttnArgs& a, int grid, hipStream_t s);
 hipError_t attn_launch_f16(AttnKind kind, int dp, const AttnArgs& a, int grid, hipStream_t s);

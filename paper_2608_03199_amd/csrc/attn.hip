@@ -90,7 +90,7 @@ int create(const sieve_attn_desc& c, hipStream_t stream, sieve_attn* p) {
   p->heads = c.heads;
   p->kv_heads = c.kv_heads;
   p->d = c.head_dim;
-  p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
+  p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : c.head_dim <= 96 ? 96 : 128;
   p->causal = c.causal;
   p->scale = c.scale;
   p->queries = c.nseq ? qo[c.nseq] : 0;

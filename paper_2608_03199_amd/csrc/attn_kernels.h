@@ -65,13 +65,16 @@ __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
   return c;
 }
 
-// An LDS tile has rows of DP values.  Piece c (16 bytes) of row r lies at piece
+// An LDS tile has rows of kPitch values: DP, or the next power of two.  Piece c (16 bytes) of row r lies at piece
 // c ^ piece_of(r) of the row.  64 banks of 4 bytes hold 16 pieces: a row (or two, or four of
 // the shorter ones).  Along the head (32 rows, one piece of each) and across the rows (4 rows
 // by 2 or 4 neighbouring pieces, twice) every 16 pieces then fall on 16 different places.
+template <int DP>
+constexpr int kPitch = DP == 96 ? 128 : DP;
+
 template <typename T, int DP>
 __device__ __forceinline__ int piece_of(int row) {
-  constexpr int kPieces = DP * (int)sizeof(T) / 16;
+  constexpr int kPieces = kPitch<DP> * (int)sizeof(T) / 16;
   if constexpr (kPieces >= 16) return (row & 3) << 2 | (row >> 2 & 3);
   else if constexpr (kPieces == 8) return (row & 2) << 1 | (row >> 2 & 3);
   else return row >> 2 & 3;
@@ -98,7 +101,7 @@ __device__ __forceinline__ lds_addr lds_of(const void* p) {
 template <typename T, int DP>
 __device__ __forceinline__ lds_addr lane_along(int lane) {
   const int row = lane & 31, h = lane >> 5;
-  return row * DP * (int)sizeof(T) +
+  return row * kPitch<DP> * (int)sizeof(T) +
          ((sizeof(T) == 2 ? h : 2 * h) ^ piece_of<T, DP>(row)) * 16;
 }
 template <typename T, int DP>
@@ -107,10 +110,10 @@ __device__ __forceinline__ lds_addr lane_across(int lane) {
   if constexpr (sizeof(T) == 2) {
     const int i = lane & 15, row = 4 * h + (i >> 2);
     const int piece = (lane >> 3 & 2) + (i >> 1 & 1);
-    return row * DP * 2 + (piece ^ piece_of<T, DP>(row)) * 16 + (i & 1) * 8;
+    return row * kPitch<DP> * 2 + (piece ^ piece_of<T, DP>(row)) * 16 + (i & 1) * 8;
   } else {
     // rows 4 h + 0..3: the row's number within 4 changes piece_of by a constant
-    return 4 * h * DP * 4 + ((lane & 31) / 4 ^ piece_of<T, DP>(4 * h)) * 16 + (lane & 3) * 4;
+    return 4 * h * kPitch<DP> * 4 + ((lane & 31) / 4 ^ piece_of<T, DP>(4 * h)) * 16 + (lane & 3) * 4;
   }
 }
 
@@ -118,7 +121,7 @@ __device__ __forceinline__ lds_addr lane_across(int lane) {
 // whose summed axis is the head's.  at: the tile's start plus lane_along.
 template <typename T, int DP>
 __device__ __forceinline__ vec8<T> frag_along(lds_addr at, int row0, int c) {
-  const int add = row0 * DP * (int)sizeof(T);
+  const int add = row0 * kPitch<DP> * (int)sizeof(T);
   if constexpr (sizeof(T) == 2) {
     return __builtin_bit_cast(vec8<T>, lds_read<enc_u32x4>((at ^ (32 * c)) + add));
   } else {
@@ -131,7 +134,7 @@ __device__ __forceinline__ vec8<T> frag_along(lds_addr at, int row0, int c) {
 // The same place, written.
 template <typename T, int DP>
 __device__ __forceinline__ void put_along(lds_addr at, int row0, int c, vec8<T> v) {
-  const int add = row0 * DP * (int)sizeof(T);
+  const int add = row0 * kPitch<DP> * (int)sizeof(T);
   if constexpr (sizeof(T) == 2) {
     lds_write((at ^ (32 * c)) + add, __builtin_bit_cast(enc_u32x4, v));
   } else {
@@ -146,7 +149,7 @@ __device__ __forceinline__ void put_along(lds_addr at, int row0, int c, vec8<T> 
 // at: the tile's start plus lane_across.
 template <typename T, int DP>
 __device__ __forceinline__ vec8<T> frag_across(lds_addr at, int row0, int col) {
-  constexpr int kRow = DP * (int)sizeof(T);
+  constexpr int kRow = kPitch<DP> * (int)sizeof(T);
   const int x = col * (int)sizeof(T), add = row0 * kRow;
   if constexpr (sizeof(T) == 2) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -256,7 +259,7 @@ template <typename T, int DP, int ROWS, bool kVec, bool kDirect>
 struct Stage {
   static_assert(kVec || !kDirect);
   static constexpr int kE = 16 / sizeof(T);           // values of a 16-byte piece
-  static constexpr int kPieces = DP / kE;             // pieces of a row
+  static constexpr int kPieces = kPitch<DP> / kE;     // pieces of a row
   static constexpr int kAll = ROWS * kPieces;
   static constexpr int kN = (kAll + kAttnThreads - 1) / kAttnThreads;
   static_assert(kAll % 64 == 0);
@@ -594,7 +597,7 @@ template <typename T, int DP, int WK>
 struct FwdShape {
   static constexpr int kBlocks = WK == 1 && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave
   static constexpr int kTile = 32 * kBlocks * WK;                    // keys of a tile
-  static constexpr int kTileBytes = kTile * DP * (int)sizeof(T);
+  static constexpr int kTileBytes = kTile * kPitch<DP> * (int)sizeof(T);
   static constexpr int kBufs = 4 * kTileBytes <= 128 * 1024 ? 2 : 1;
   static constexpr int kStageBytes = 2 * kBufs * kTileBytes;
   static constexpr int kJoinBytes = WK == 1 ? 0 : (WK * 32 * (DP + 4) + 2 * WK * 32 + WK) * 4;
@@ -606,7 +609,7 @@ template <typename T, int DP, int WK, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_forward_kernel(AttnArgs a) {
   using Shape = FwdShape<T, DP, WK>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
-  constexpr int kTileN = kTile * DP;
+  constexpr int kTileN = kTile * kPitch<DP>;
   extern __shared__ __align__(16) uint8_t smem[];
   T* s_k = (T*)smem;
   T* s_v = s_k + Shape::kBufs * kTileN;
@@ -649,7 +652,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
   float m = -INFINITY, l = 0.f;
   bool odd = false;  // the wave's rows have to be done again (careful_row)
-  const int skip = WK == 1 ? 0 : wave * 32 * DP;  // the wave's keys in a tile
+  const int skip = WK == 1 ? 0 : wave * 32 * kPitch<DP>;  // the wave's keys in a tile
   const lds_addr k_al = lds_of(s_k + skip) + lane_along<T, DP>(lane);
   const lds_addr v_ac = lds_of(s_v + skip) + lane_across<T, DP>(lane);
 
@@ -677,8 +680,10 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       for (int b = 0; b < kBlocks; ++b) {
         s[b] = f32x16{};
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c)
+        for (int c = 0; c < DP / 16; ++c) {
+          if (sizeof(T) == 4 && 16 * c >= d) break;  // zeros; 8 slow products each
           s[b] = mma(frag_along<T, DP>(sk, 32 * b, c), q[c], s[b]);
+        }
       }
       float top = -INFINITY;
 #pragma unroll
@@ -840,7 +845,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
   const AttnJoin j = a.joins[blockIdx.x / kGroups];
   const int i = blockIdx.x % kGroups * kJoinRows<DP> + threadIdx.x / (DP / 4);
   const int r = j.row + i, c = threadIdx.x % (DP / 4) * 4;
-  if (i >= ROWS || r >= j.n * a.G) return;
+  if (threadIdx.x >= kJoinRows<DP> * (DP / 4) || i >= ROWS || r >= j.n * a.G) return;
   const float* ml = a.part_ml + ((int64_t)j.part0 * ROWS + i) * 2;
   float most = -INFINITY;
 #pragma unroll 4
@@ -889,7 +894,7 @@ struct DqShape {
   static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 && !kBias ? 2 : 1;
   static constexpr int kTile = 32 * kBlocks;
   static constexpr int kBufs = 2;
-  static constexpr int kBytes = 2 * kBufs * kTile * DP * (int)sizeof(T);
+  static constexpr int kBytes = 2 * kBufs * kTile * kPitch<DP> * (int)sizeof(T);
 };
 constexpr int kAttnWaves = kAttnThreads / 64;
 // A row of the dS block: 32 values, then at least 31 zeros, and 4 words that spread the
@@ -944,7 +949,7 @@ template <typename T, int DP, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
   using Shape = DqShape<T, DP, kBias>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
-  constexpr int kTileN = kTile * DP;
+  constexpr int kTileN = kTile * kPitch<DP>;
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
   T* s_k = (T*)smem;
@@ -1055,6 +1060,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
+          if (sizeof(T) == 4 && 16 * c >= d) break;
           s = mma(frag_along<T, DP>(sk, 32 * b, c), q[c], s);
           dp = mma(frag_along<T, DP>(sv, 32 * b, c), dout[c], dp);
         }
@@ -1241,12 +1247,12 @@ struct DkvShape {
   static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 ? 2 : 1;  // 32-row blocks of a tile
   static constexpr int kTile = 32 * kBlocks;
   static constexpr int kBufs = 2;
-  static constexpr int kTileBytes = kTile * DP * (int)sizeof(T);
+  static constexpr int kTileBytes = kTile * kPitch<DP> * (int)sizeof(T);
   // The tile's values as operands in registers, or, where the accumulators leave no room
   // for them at two waves a SIMD, in LDS.
   static constexpr bool kValuesInLds = DP * sizeof(T) >= 256;
   static constexpr int kValueBytes =
-      kValuesInLds ? kAttnKeys * DP * (int)sizeof(T) : 0;
+      kValuesInLds ? kAttnKeys * kPitch<DP> * (int)sizeof(T) : 0;
   static constexpr int kBytes = kValueBytes + kBufs * (2 * kTileBytes + 4 * kTile * 4);
 };
 
@@ -1280,7 +1286,7 @@ template <typename T, int DP, bool kBias, bool kVec>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
   using Shape = DkvShape<T, DP>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
-  constexpr int kTileN = kTile * DP;
+  constexpr int kTileN = kTile * kPitch<DP>;
   constexpr bool kScaled = __is_same(T, f16);
   extern __shared__ __align__(16) uint8_t smem[];
   // P is computed, and rounded, times 2^kUpP
@@ -1381,7 +1387,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 
   const lds_addr q_al = lds_of(s_q) + lane_along<T, DP>(lane);
   const lds_addr q_ac = lds_of(s_q) + lane_across<T, DP>(lane);
-  const lds_addr val_al = lds_of(s_val + wave * 32 * DP) + lane_along<T, DP>(lane);
+  const lds_addr val_al = lds_of(s_val + wave * 32 * kPitch<DP>) + lane_along<T, DP>(lane);
   vec8<T> k[DP / 16], v[DP / 16];
   {
     const int64_t tok = it.k0 + (live ? key : 0);
@@ -1449,6 +1455,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         }
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
+          if (sizeof(T) == 4 && 16 * c >= d) break;
           s = mma(frag_along<T, DP>(sq, 32 * b, c), k[c], s);
           vec8<T> val;
           if constexpr (Shape::kValuesInLds)
@@ -1637,6 +1644,7 @@ hipError_t launch_type(AttnKind kind, int dp, const AttnArgs& a, int grid, hipSt
   switch (dp) {
     case 32: return launch_dp<T, 32>(kind, a, grid, s);
     case 64: return launch_dp<T, 64>(kind, a, grid, s);
+    case 96: return launch_dp<T, 96>(kind, a, grid, s);
     case 128: return launch_dp<T, 128>(kind, a, grid, s);
   }
   return hipErrorInvalidValue;

@@ -28,7 +28,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxN = 65536;
 constexpr int kBigThreads = 1024;
-constexpr int kMaxParts = 1024;  // work-groups of the backward pass: 4 a CU
+constexpr int kMaxParts = 512;  // work-groups of the backward pass: 2 a CU
 
 struct NormFwd {
   const void *x, *residual, *w, *b;
@@ -79,6 +79,34 @@ __device__ __forceinline__ void load_row(const T* p, int n, int t, float (&v)[NE
     }
   }
 }
+
+// A row's values as they lie in memory, so that the next row can be on its way while one is
+// worked on at half of the registers (or all, in 32 bits).
+template <typename T, int NE, int NT, bool kVec>
+struct RawRow {
+  EncVec<T, 8> v[NE / 8];
+
+  __device__ __forceinline__ void load(const T* p, int n, int t) {
+#pragma unroll
+    for (int c = 0; c < NE / 8; ++c) {
+      if constexpr (kVec) {
+        const int col = (c * NT + t) * 8;
+        if (col < n) v[c] = enc_load<T, 8>(p + col);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int col = (c * 8 + j) * NT + t;
+          if (col < n) v[c].v[j] = p[col];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int n, int t, float (&f)[NE]) const {
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+      f[e] = column<NT, kVec>(e, t) < n ? (float)v[e / 8].v[e % 8] : 0.f;
+  }
+};
 
 template <typename T, int NE, int NT, bool kVec>
 __device__ __forceinline__ void store_row(T* p, int n, int t, const float (&v)[NE]) {
@@ -205,12 +233,23 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
   load_row<W, NE, NT, kVec>((const W*)a.w, n, t, w);
 #pragma unroll
   for (int e = 0; e < NE; ++e) dw[e] = db[e] = 0.f;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT; row < a.rows;
-       row += (int64_t)gridDim.x * kRows) {
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT;
+  RawRow<T, NE, NT, kVec> next_h, next_dy;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto fetch = [&](int64_t r) {
+    next_h.load((const T*)a.h + r * a.h_stride, n, t);
+    next_dy.load((const T*)a.dy + r * a.dy_stride, n, t);
+    next_mean = a.mean[r];
+    next_rstd = a.rstd[r];
+  };
+  if (row < a.rows) fetch(row);
+  for (; row < a.rows; row += step) {
     float u[NE], g[NE];
-    load_row<T, NE, NT, kVec>((const T*)a.h + row * a.h_stride, n, t, u);
-    load_row<T, NE, NT, kVec>((const T*)a.dy + row * a.dy_stride, n, t, g);
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    next_h.get(n, t, u);
+    next_dy.get(n, t, g);
+    const float mean = next_mean, rstd = next_rstd;
+    if (row + step < a.rows) fetch(row + step);
     float sg = 0.f, sgu = 0.f;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
@@ -354,8 +393,10 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
   const int64_t col = (int64_t)blockIdx.x * 32 + c;
   float v = 0.f;
-  if (col < 2 * n)
+  if (col < 2 * n) {
+#pragma unroll 8
     for (int p = g; p < parts; p += 32) v += part[(int64_t)p * 2 * n + col];
+  }
   s[g][c] = v;
   __syncthreads();
   if (g == 0 && col < 2 * n) {
