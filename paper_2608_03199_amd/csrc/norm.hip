@@ -6,15 +6,17 @@
 //   dw = sum_rows dy u, db = sum_rows dy
 //
 // Each value is read once and written once, so memory bounds every kernel here.
-// A row stays in the registers of one wave (up to 2,048 values) or one work-group
-// (up to 8,192): the mean is taken first and the variance from the differences, in
+// A row stays in the registers of a quarter of a wave (up to 128 values), a wave (up to
+// 2,048) or a work-group (up to 8,192): the mean is taken first and the variance from the differences, in
 // fp32 without the cancellation of a sum of squares.  Longer rows are read again,
 // from the L2, by the looping kernels.
 //
-// The weights' gradients: a thread owns the same columns of every row its wave
-// takes, so it sums them in registers; the work-group's waves add up through LDS,
+// The weights' gradients: a thread owns the same columns of every row it takes, so it
+// sums them in registers; the work-group's rows add up through LDS,
 // each work-group writes one partial row, and a second kernel adds those in a fixed
 // order.  No atomics: equal calls give equal bits.
+#include <type_traits>
+
 #include "enc_common.h"
 
 using namespace sieve;
@@ -27,6 +29,7 @@ typedef _Float16 f16;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxN = 65536;
+constexpr int kMaxHeld = 8192;  // longest row that stays in registers
 constexpr int kBigThreads = 1024;
 constexpr int kMaxParts = 512;  // work-groups of the backward pass: 2 a CU
 
@@ -48,33 +51,50 @@ struct NormBwd {
   float* part;  // [work-group][2][n]; null where there is one work-group
 };
 
-// Column of value e of a thread: 8 neighbours at a time (16-byte moves), or, where
-// the rows are not aligned, one neighbour a thread.
-template <int NT, bool kVec>
+// Column of value e of a thread: E neighbours at a time (one move), or, where the rows are
+// not aligned (E = 0), one neighbour a thread.
+template <int NT, int E>
 __device__ __forceinline__ int column(int e, int t) {
-  return kVec ? ((e >> 3) * NT + t) * 8 + (e & 7) : e * NT + t;
+  return E ? ((e / (E ? E : 1)) * NT + t) * E + e % (E ? E : 1) : e * NT + t;
+}
+
+// E neighbours in moves of at most 16 bytes.
+template <typename T, int E>
+__device__ __forceinline__ EncVec<T, E> load_some(const T* p) {
+  if constexpr (E * sizeof(T) >= 16) {
+    return enc_load<T, E>(p);
+  } else {
+    return __builtin_bit_cast(EncVec<T, E>, *(const uint2*)p);
+  }
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_some(T* p, const EncVec<T, E>& v) {
+  if constexpr (E * sizeof(T) >= 16)
+    enc_store<T, E>(p, v);
+  else
+    *(uint2*)p = __builtin_bit_cast(uint2, v);
 }
 
 // Values of a row; 0 past its end.
-template <typename T, int NE, int NT, bool kVec>
+template <typename T, int NE, int NT, int E>
 __device__ __forceinline__ void load_row(const T* p, int n, int t, float (&v)[NE]) {
-  if constexpr (kVec) {
+  if constexpr (E != 0) {
 #pragma unroll
-    for (int c = 0; c < NE / 8; ++c) {
-      const int col = (c * NT + t) * 8;
+    for (int e = 0; e < NE; e += E) {
+      const int col = column<NT, E>(e, t);
       if (col < n) {
-        const EncVec<T, 8> q = enc_load<T, 8>(p + col);
+        const EncVec<T, E> q = load_some<T, E>(p + col);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[c * 8 + j] = (float)q.v[j];
+        for (int j = 0; j < E; ++j) v[e + j] = (float)q.v[j];
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[c * 8 + j] = 0.f;
+        for (int j = 0; j < E; ++j) v[e + j] = 0.f;
       }
     }
   } else {
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
-      const int col = e * NT + t;
+      const int col = column<NT, E>(e, t);
       v[e] = col < n ? (float)p[col] : 0.f;
     }
   }
@@ -82,64 +102,69 @@ __device__ __forceinline__ void load_row(const T* p, int n, int t, float (&v)[NE
 
 // A row's values as they lie in memory, so that the next row can be on its way while one is
 // worked on at half of the registers (or all, in 32 bits).
-template <typename T, int NE, int NT, bool kVec>
+template <typename T, int NE, int NT, int E>
 struct RawRow {
-  EncVec<T, 8> v[NE / 8];
+  T v[NE];
 
   __device__ __forceinline__ void load(const T* p, int n, int t) {
+    if constexpr (E != 0) {
 #pragma unroll
-    for (int c = 0; c < NE / 8; ++c) {
-      if constexpr (kVec) {
-        const int col = (c * NT + t) * 8;
-        if (col < n) v[c] = enc_load<T, 8>(p + col);
-      } else {
+      for (int e = 0; e < NE; e += E) {
+        const int col = column<NT, E>(e, t);
+        if (col < n) {
+          const EncVec<T, E> q = load_some<T, E>(p + col);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int col = (c * 8 + j) * NT + t;
-          if (col < n) v[c].v[j] = p[col];
+          for (int j = 0; j < E; ++j) v[e + j] = q.v[j];
         }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const int col = column<NT, E>(e, t);
+        if (col < n) v[e] = p[col];
       }
     }
   }
   __device__ __forceinline__ void get(int n, int t, float (&f)[NE]) const {
 #pragma unroll
-    for (int e = 0; e < NE; ++e)
-      f[e] = column<NT, kVec>(e, t) < n ? (float)v[e / 8].v[e % 8] : 0.f;
+    for (int e = 0; e < NE; ++e) f[e] = column<NT, E>(e, t) < n ? (float)v[e] : 0.f;
   }
 };
 
-template <typename T, int NE, int NT, bool kVec>
+template <typename T, int NE, int NT, int E>
 __device__ __forceinline__ void store_row(T* p, int n, int t, const float (&v)[NE]) {
-  if constexpr (kVec) {
+  if constexpr (E != 0) {
 #pragma unroll
-    for (int c = 0; c < NE / 8; ++c) {
-      const int col = (c * NT + t) * 8;
+    for (int e = 0; e < NE; e += E) {
+      const int col = column<NT, E>(e, t);
       if (col < n) {
-        EncVec<T, 8> q;
+        EncVec<T, E> q;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q.v[j] = (T)v[c * 8 + j];
-        enc_store<T, 8>(p + col, q);
+        for (int j = 0; j < E; ++j) q.v[j] = (T)v[e + j];
+        store_some<T, E>(p + col, q);
       }
     }
   } else {
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
-      const int col = e * NT + t;
+      const int col = column<NT, E>(e, t);
       if (col < n) p[col] = (T)v[e];
     }
   }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
+// The sum over a row's threads within the wave.
+template <int NT>
+__device__ __forceinline__ float lane_sum(float v) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  for (int o = (NT < 64 ? NT : 64) / 2; o; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
 
-// Sums over the threads of a row: a wave's, or the work-group's through LDS.
+// Sums over the threads of a row: part of a wave, a wave, or the work-group through LDS.
 template <int NT>
 __device__ __forceinline__ float row_sum(float v, float* s) {
-  v = wave_sum(v);
+  v = lane_sum<NT>(v);
   if constexpr (NT > 64) {
     __syncthreads();  // the previous sum has been read
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
@@ -153,8 +178,8 @@ __device__ __forceinline__ float row_sum(float v, float* s) {
 
 template <int NT>
 __device__ __forceinline__ void row_sum2(float& a, float& b, float* s) {
-  a = wave_sum(a);
-  b = wave_sum(b);
+  a = lane_sum<NT>(a);
+  b = lane_sum<NT>(b);
   if constexpr (NT > 64) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
@@ -171,7 +196,7 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float* s) {
   }
 }
 
-template <typename T, typename W, int NE, int NT, bool kVec>
+template <typename T, typename W, int NE, int NT, int E>
 __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormFwd a) {
   __shared__ float s_sum[kWaves];
   const int t = threadIdx.x % NT;
@@ -179,9 +204,9 @@ __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormFwd a) {
   const int n = a.n;
   const float inv = 1.f / (float)n;
   float w[NE], b[NE];
-  load_row<W, NE, NT, kVec>((const W*)a.w, n, t, w);
+  load_row<W, NE, NT, E>((const W*)a.w, n, t, w);
   if (a.b) {
-    load_row<W, NE, NT, kVec>((const W*)a.b, n, t, b);
+    load_row<W, NE, NT, E>((const W*)a.b, n, t, b);
   } else {
 #pragma unroll
     for (int e = 0; e < NE; ++e) b[e] = 0.f;
@@ -189,15 +214,15 @@ __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormFwd a) {
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT; row < a.rows;
        row += (int64_t)gridDim.x * kRows) {
     float v[NE];
-    load_row<T, NE, NT, kVec>((const T*)a.x + row * a.x_stride, n, t, v);
+    load_row<T, NE, NT, E>((const T*)a.x + row * a.x_stride, n, t, v);
     if (a.residual) {
       float r[NE];
-      load_row<T, NE, NT, kVec>((const T*)a.residual + row * a.r_stride, n, t, r);
+      load_row<T, NE, NT, E>((const T*)a.residual + row * a.r_stride, n, t, r);
       // the sum is rounded to the activations' type: the backward pass and the next
       // layer read it in that type, and the norm is of what they read
 #pragma unroll
       for (int e = 0; e < NE; ++e) v[e] = (float)(T)(v[e] + r[e]);
-      store_row<T, NE, NT, kVec>((T*)a.h + row * n, n, t, v);
+      store_row<T, NE, NT, E>((T*)a.h + row * n, n, t, v);
     }
     float sum = 0.f;
 #pragma unroll
@@ -206,13 +231,13 @@ __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormFwd a) {
     float sq = 0.f;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
-      v[e] = column<NT, kVec>(e, t) < n ? v[e] - mean : 0.f;
+      v[e] = column<NT, E>(e, t) < n ? v[e] - mean : 0.f;
       sq += v[e] * v[e];
     }
     const float rstd = 1.f / sqrtf(row_sum<NT>(sq, s_sum) * inv + a.eps);
 #pragma unroll
     for (int e = 0; e < NE; ++e) v[e] = v[e] * rstd * w[e] + b[e];
-    store_row<T, NE, NT, kVec>((T*)a.y + row * n, n, t, v);
+    store_row<T, NE, NT, E>((T*)a.y + row * n, n, t, v);
     if (t == 0 && a.mean) {
       a.mean[row] = mean;
       a.rstd[row] = rstd;
@@ -220,22 +245,22 @@ __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormFwd a) {
   }
 }
 
-template <typename T, typename W, int NE, int NT, bool kVec>
+template <typename T, typename W, int NE, int NT, int E>
 __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
   __shared__ float s_sum[2 * kWaves];
   // one wave's columns at a time go through LDS to the work-group's sum
-  __shared__ float s_cols[NT == 64 ? kWaves * 64 * 8 : 1];
+  __shared__ float s_cols[NT <= 64 ? kWaves * 64 * 4 : 1];
   const int t = threadIdx.x % NT;
   constexpr int kRows = kThreads / NT;
   const int n = a.n;
   const float inv = 1.f / (float)n;
   float w[NE], dw[NE], db[NE];
-  load_row<W, NE, NT, kVec>((const W*)a.w, n, t, w);
+  load_row<W, NE, NT, E>((const W*)a.w, n, t, w);
 #pragma unroll
   for (int e = 0; e < NE; ++e) dw[e] = db[e] = 0.f;
   const int64_t step = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT;
-  RawRow<T, NE, NT, kVec> next_h, next_dy;
+  RawRow<T, NE, NT, E> next_h, next_dy;
   float next_mean = 0.f, next_rstd = 0.f;
   auto fetch = [&](int64_t r) {
     next_h.load((const T*)a.h + r * a.h_stride, n, t);
@@ -253,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
     float sg = 0.f, sgu = 0.f;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
-      u[e] = column<NT, kVec>(e, t) < n ? (u[e] - mean) * rstd : 0.f;
+      u[e] = column<NT, E>(e, t) < n ? (u[e] - mean) * rstd : 0.f;
       dw[e] += g[e] * u[e];
       db[e] += g[e];
       g[e] *= w[e];
@@ -266,45 +291,49 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
 #pragma unroll
     for (int e = 0; e < NE; ++e) g[e] = rstd * (g[e] - sg - u[e] * sgu);
     if (a.dh) {
-      load_row<T, NE, NT, kVec>((const T*)a.dh + row * n, n, t, u);
+      load_row<T, NE, NT, E>((const T*)a.dh + row * n, n, t, u);
 #pragma unroll
       for (int e = 0; e < NE; ++e) g[e] += u[e];
     }
-    store_row<T, NE, NT, kVec>((T*)a.dx + row * n, n, t, g);
+    store_row<T, NE, NT, E>((T*)a.dx + row * n, n, t, g);
   }
   if (!a.dw && !a.db) return;
-  if constexpr (NT == 64) {
-    // the waves of the work-group, 8 of a thread's columns at a time, in wave order
-    const int wave = threadIdx.x / 64;
+  if constexpr (NT <= 64) {
+    // the rows that share a wave, then the waves in order, 4 of a thread's columns at a time
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
+      float(&x)[NE] = part ? db : dw;
 #pragma unroll
-      for (int c = 0; c < NE / 8; ++c) {
+      for (int e = 0; e < NE; ++e)
+#pragma unroll
+        for (int o = 32; o >= NT; o >>= 1) x[e] += __shfl_xor(x[e], o);
+#pragma unroll
+      for (int c = 0; c < NE; c += 4) {
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          s_cols[(wave * 8 + j) * 64 + t] = part ? db[c * 8 + j] : dw[c * 8 + j];
+        for (int j = 0; j < 4; ++j) s_cols[(wave * 4 + j) * 64 + lane] = x[c + j];
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < 4; ++j) {
             float v = 0.f;
 #pragma unroll
-            for (int q = 0; q < kWaves; ++q) v += s_cols[(q * 8 + j) * 64 + t];
-            (part ? db : dw)[c * 8 + j] = v;
+            for (int q = 0; q < kWaves; ++q) v += s_cols[(q * 4 + j) * 64 + lane];
+            x[c + j] = v;
           }
         }
       }
     }
-    if (wave) return;
+    if (threadIdx.x >= NT) return;
   }
   if (a.part) {
     float* p = a.part + (int64_t)blockIdx.x * 2 * n;
-    store_row<float, NE, NT, kVec>(p, n, t, dw);
-    store_row<float, NE, NT, kVec>(p + n, n, t, db);
+    store_row<float, NE, NT, E>(p, n, t, dw);
+    store_row<float, NE, NT, E>(p + n, n, t, db);
   } else {
-    if (a.dw) store_row<W, NE, NT, kVec>((W*)a.dw, n, t, dw);
-    if (a.db) store_row<W, NE, NT, kVec>((W*)a.db, n, t, db);
+    if (a.dw) store_row<W, NE, NT, E>((W*)a.dw, n, t, dw);
+    if (a.db) store_row<W, NE, NT, E>((W*)a.db, n, t, db);
   }
 }
 
@@ -410,50 +439,58 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
   }
 }
 
-// Work-groups of the backward pass: 4 rows a work-group at a time where a wave holds a
-// row.  A multiple of that many rows each evens the waves' loads.
+// How a row is spread: NE values a thread (in moves of E, or 0), NT threads.  The smallest
+// that holds it; 768 values, which moves of 8 would fill to three quarters, in moves of 4.
+// f(NE, NT, E of an aligned row) as constants; false for rows that are too long.
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <typename F>
+bool by_length(int n, F f) {
+  if (n <= 128) f(Int<8>{}, Int<16>{}, Int<8>{});
+  else if (n <= 512) f(Int<8>{}, Int<64>{}, Int<8>{});
+  else if (n <= 768) f(Int<12>{}, Int<64>{}, Int<4>{});
+  else if (n <= 1024) f(Int<16>{}, Int<64>{}, Int<8>{});
+  else if (n <= 1536) f(Int<24>{}, Int<64>{}, Int<8>{});
+  else if (n <= 2048) f(Int<32>{}, Int<64>{}, Int<8>{});
+  else if (n <= 4096) f(Int<16>{}, Int<256>{}, Int<8>{});
+  else if (n <= kMaxHeld) f(Int<32>{}, Int<256>{}, Int<8>{});
+  else return false;
+  return true;
+}
+
+// Work-groups of the backward pass.
 int backward_groups(int64_t rows, int n) {
-  const int at_a_time = n <= 2048 ? kWaves : 1;
+  int at_a_time = 1;  // rows of a work-group
+  by_length(n, [&](auto, auto nt, auto) { at_a_time = kThreads / nt; });
   const int64_t steps = (rows + at_a_time - 1) / at_a_time;
   return (int)(steps < kMaxParts ? (steps > 0 ? steps : 1) : kMaxParts);
 }
 
-template <typename T, typename W, int NE, int NT, bool kVec>
-void forward_on(const NormFwd& a, hipStream_t s) {
-  constexpr int kRows = kThreads / NT;
-  const int64_t want = (a.rows + kRows - 1) / kRows;
-  const int grid = (int)(want < 8192 ? want : 8192);
-  norm_forward_kernel<T, W, NE, NT, kVec><<<grid, kThreads, 0, s>>>(a);
-}
-
 template <typename T, typename W>
 void forward_typed(const NormFwd& a, bool vec, hipStream_t s) {
-  const int n = a.n;
-#define GO(NE, NT)                                                 \
-  return vec ? forward_on<T, W, NE, NT, true>(a, s) : forward_on<T, W, NE, NT, false>(a, s)
-  if (n <= 512) GO(8, 64);
-  if (n <= 1024) GO(16, 64);
-  if (n <= 2048) GO(32, 64);
-  if (n <= 4096) GO(16, 256);
-  if (n <= 8192) GO(32, 256);
-#undef GO
-  const int grid = (int)(a.rows < 4096 ? a.rows : 4096);
-  norm_forward_big_kernel<T, W><<<grid, kBigThreads, 0, s>>>(a);
+  const bool held = by_length(a.n, [&](auto ne, auto nt, auto e) {
+    constexpr int kNE = decltype(ne)::value, kNT = decltype(nt)::value, kE = decltype(e)::value;
+    constexpr int kRows = kThreads / kNT;
+    const int64_t want = (a.rows + kRows - 1) / kRows;
+    const int grid = (int)(want < 8192 ? want : 8192);
+    if (vec) norm_forward_kernel<T, W, kNE, kNT, kE><<<grid, kThreads, 0, s>>>(a);
+    else norm_forward_kernel<T, W, kNE, kNT, 0><<<grid, kThreads, 0, s>>>(a);
+  });
+  if (!held) {
+    const int grid = (int)(a.rows < 4096 ? a.rows : 4096);
+    norm_forward_big_kernel<T, W><<<grid, kBigThreads, 0, s>>>(a);
+  }
 }
 
 template <typename T, typename W>
 void backward_typed(const NormBwd& a, bool vec, int groups, hipStream_t s) {
   const int n = a.n;
-#define GO(NE, NT)                                                                     \
-  vec ? norm_backward_kernel<T, W, NE, NT, true><<<groups, kThreads, 0, s>>>(a)        \
-      : norm_backward_kernel<T, W, NE, NT, false><<<groups, kThreads, 0, s>>>(a)
-  if (n <= 512) GO(8, 64);
-  else if (n <= 1024) GO(16, 64);
-  else if (n <= 2048) GO(32, 64);
-  else if (n <= 4096) GO(16, 256);
-  else if (n <= 8192) GO(32, 256);
-  else norm_backward_big_kernel<T, W><<<groups, kBigThreads, 0, s>>>(a);
-#undef GO
+  const bool held = by_length(n, [&](auto ne, auto nt, auto e) {
+    constexpr int kNE = decltype(ne)::value, kNT = decltype(nt)::value, kE = decltype(e)::value;
+    if (vec) norm_backward_kernel<T, W, kNE, kNT, kE><<<groups, kThreads, 0, s>>>(a);
+    else norm_backward_kernel<T, W, kNE, kNT, 0><<<groups, kThreads, 0, s>>>(a);
+  });
+  if (!held) norm_backward_big_kernel<T, W><<<groups, kBigThreads, 0, s>>>(a);
   if (a.part && (a.dw || a.db))
     norm_reduce_kernel<W><<<(2 * n + 31) / 32, 1024, 0, s>>>(a.part, groups, n, (W*)a.dw,
                                                              (W*)a.db);
@@ -517,7 +554,7 @@ SIEVE_API int64_t sieve_norm_workspace(int64_t rows, int32_t n) {
   clear_error();
   if (int st = check_norm(SIEVE_F32, SIEVE_F32, rows, n)) return st;
   const int groups = backward_groups(rows, n);
-  return groups == 1 && n <= 8192 ? 0 : (int64_t)groups * 2 * n * (int64_t)sizeof(float);
+  return groups == 1 && n <= kMaxHeld ? 0 : (int64_t)groups * 2 * n * (int64_t)sizeof(float);
 }
 
 SIEVE_API int sieve_norm_backward(const void* dy, int64_t dy_stride, const void* h,
