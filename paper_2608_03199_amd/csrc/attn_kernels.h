@@ -30,6 +30,8 @@
 // (dV, where P <= 1), and dS by what brings its largest magnitude to 2^13 .. 2^14.
 #pragma once
 
+#include <type_traits>
+
 #include "attn.h"
 
 namespace sieve {
@@ -131,15 +133,27 @@ __device__ __forceinline__ vec8<T> frag_along(lds_addr at, int row0, int c) {
   }
 }
 
-// The same place, written.
-template <typename T, int DP>
-__device__ __forceinline__ void put_along(lds_addr at, int row0, int c, vec8<T> v) {
-  const int add = row0 * kPitch<DP> * (int)sizeof(T);
+// Operands that a wave keeps in LDS for itself, in the lanes' order: chunk c at
+// at + c * kFragBytes, at being the wave's place plus 16 bytes a lane.
+template <typename T>
+constexpr int kFragBytes = 64 * 8 * (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ vec8<T> frag_kept(lds_addr at, int c) {
   if constexpr (sizeof(T) == 2) {
-    lds_write((at ^ (32 * c)) + add, __builtin_bit_cast(enc_u32x4, v));
+    return __builtin_bit_cast(vec8<T>, lds_read<enc_u32x4>(at + c * kFragBytes<T>));
   } else {
-    lds_write((at ^ (64 * c)) + add, __builtin_shufflevector(v, v, 0, 1, 2, 3));
-    lds_write((at ^ (64 * c) ^ 16) + add, __builtin_shufflevector(v, v, 4, 5, 6, 7));
+    const f32x4 p = lds_read<f32x4>(at + c * kFragBytes<T>);
+    const f32x4 q = lds_read<f32x4>(at + c * kFragBytes<T> + 1024);
+    return __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void keep_frag(lds_addr at, int c, vec8<T> v) {
+  if constexpr (sizeof(T) == 2) {
+    lds_write(at + c * kFragBytes<T>, __builtin_bit_cast(enc_u32x4, v));
+  } else {
+    lds_write(at + c * kFragBytes<T>, __builtin_shufflevector(v, v, 0, 1, 2, 3));
+    lds_write(at + c * kFragBytes<T> + 1024, __builtin_shufflevector(v, v, 4, 5, 6, 7));
   }
 }
 
@@ -187,6 +201,15 @@ __device__ __forceinline__ int query_of(const AttnArgs& a, int r) {
   return (int)(__umulhi((uint32_t)r << 1, a.g_mul) >> a.g_shift);
 }
 
+// The value of the lane 32 away.
+__device__ __forceinline__ float other_half(float v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  // lanes 32..63 of the first and 0..31 of the second change places
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
 // The wave's number, known to be the same in all lanes.
 __device__ __forceinline__ int wave_id() {
   return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -212,8 +235,17 @@ __device__ __forceinline__ void load_frags(const T* p, bool ok, int d, int h,
 #pragma unroll
     for (int j = 0; j < 8; ++j) q.v[j] = (T)0.f;
     if (ok && col < d) {
-      if (kVec && (sizeof(T) == 2 || col + 8 <= d)) {
+      if constexpr (kVec && sizeof(T) == 2) {
         q = enc_load<T, 8>(p + col);
+      } else if constexpr (kVec) {  // d is a multiple of 4
+        const EncVec<T, 4> a = enc_load<T, 4>(p + col);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q.v[j] = a.v[j];
+        if (col + 4 < d) {
+          const EncVec<T, 4> b = enc_load<T, 4>(p + col + 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) q.v[4 + j] = b.v[j];
+        }
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -273,35 +305,51 @@ struct Stage {
   static __device__ __forceinline__ int col(int i) {
     return ((threadIdx.x + i * kAttnThreads) % kPieces ^ piece_of<T, DP>(row(i))) * kE;
   }
-  // the type of an offset within a tile
-  static __device__ __forceinline__ auto off_zero() {
-    if constexpr (kVec) return 0;
-    else return (int64_t)0;
-  }
   static __device__ __forceinline__ bool mine(int i) {
     return kAll % kAttnThreads == 0 || threadIdx.x + i * kAttnThreads < kAll;
   }
-  // at(i): piece i's offset in values from base; rows: how many of the tile's there are;
-  // s: the tile's place in LDS
+  // Offsets of the pieces from a tile's first row, worked out once: at(row, col) in values,
+  // kNowhere past the head's size.
+  typedef std::conditional_t<kVec, uint32_t, int64_t> Off;
+  Off off[kN];
   template <typename F>
-  __device__ __forceinline__ void load(const T* base, F at, int rows, int d, T* s) {
-    const Buffer from(base);
+  __device__ __forceinline__ void place(F at, int d) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const bool there = row(i) < rows && col(i) < d;
-      if constexpr (kDirect) {
-        if (mine(i))
-          from.load_lds(there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere,
-                        s + (i * kAttnThreads + wave_id() * 64) * kE);
-      } else if constexpr (kVec) {
-        r[i] = from.load(mine(i) && there ? (uint32_t)at(i) * (uint32_t)sizeof(T) : kNowhere);
+      if constexpr (kVec)
+        off[i] = col(i) < d && mine(i) ? (uint32_t)at(row(i), col(i)) * (uint32_t)sizeof(T)
+                                       : kNowhere;
+      else
+        off[i] = at(row(i), col(i));
+    }
+  }
+  // rows: how many of the tile's there are; s: the tile's place in LDS
+  __device__ __forceinline__ void load(const T* base, int rows, int d, T* s) {
+    const Buffer from(base);
+    if constexpr (kVec) {
+      if (rows >= ROWS) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) move(from, off[i], i, s);
       } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) move(from, row(i) < rows ? off[i] : kNowhere, i, s);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
         EncVec<T, kE> q;
 #pragma unroll
         for (int j = 0; j < kE; ++j)
-          q.v[j] = mine(i) && there && col(i) + j < d ? base[at(i) + j] : (T)0.f;
+          q.v[j] = mine(i) && row(i) < rows && col(i) + j < d ? base[off[i] + j] : (T)0.f;
         r[i] = __builtin_bit_cast(enc_u32x4, q);
       }
+    }
+  }
+  __device__ __forceinline__ void move(const Buffer& from, uint32_t offset, int i, T* s) {
+    if constexpr (kDirect) {
+      if (mine(i)) from.load_lds(offset, s + (i * kAttnThreads + wave_id() * 64) * kE);
+    } else {
+      r[i] = from.load(offset);
     }
   }
   // the pieces are in LDS after this and the next barrier; keep(i): whether piece i counts
@@ -331,15 +379,16 @@ struct KeyStage {
   Tile k, v;
   uint8_t keep[Tile::kN];
 
+  __device__ __forceinline__ void place(const AttnArgs& a) {
+    const int64_t ks = a.k.token_stride, vs = a.v.token_stride;
+    k.place([&](int row, int col) { return row * ks + col; }, a.d);
+    v.place([&](int row, int col) { return row * vs + col; }, a.d);
+  }
   // k0, v0: the sequence's first row; keys base .. hi - 1 at most
   __device__ __forceinline__ void load(const AttnArgs& a, const uint8_t* mask, const T* k0,
                                        const T* v0, int base, int hi, T* s_k, T* s_v) {
-    typedef decltype(Tile::off_zero()) Off;
-    const Off ks = (Off)a.k.token_stride, vs = (Off)a.v.token_stride;
-    k.load(k0 + base * a.k.token_stride, [&](int i) { return Tile::row(i) * ks + Tile::col(i); },
-           hi - base, a.d, s_k);
-    v.load(v0 + base * a.v.token_stride, [&](int i) { return Tile::row(i) * vs + Tile::col(i); },
-           hi - base, a.d, s_v);
+    k.load(k0 + base * a.k.token_stride, hi - base, a.d, s_k);
+    v.load(v0 + base * a.v.token_stride, hi - base, a.d, s_v);
     if (mask) {
 #pragma unroll
       for (int i = 0; i < Tile::kN; ++i) {
@@ -369,8 +418,8 @@ __device__ __forceinline__ void store_row(T* p, const f32x16 (&x)[DP / 32], floa
       const f32x4 v = {x[b][4 * g] * f, x[b][4 * g + 1] * f, x[b][4 * g + 2] * f,
                        x[b][4 * g + 3] * f};
       const vec4 q = __builtin_convertvector(v, vec4);
-      if (kVec && col + 4 <= d) {
-        *(vec4*)(p + col) = q;
+      if constexpr (kVec) {  // d is a multiple of 4
+        if (col < d) *(vec4*)(p + col) = q;
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -417,11 +466,12 @@ __device__ __forceinline__ uint32_t upto(int pos, int base) {
 
 // Products of 32 keys (base ..) with the lane's row to scores: s * scale2 + bias, in units of
 // log2, and -infinity where bits (of the keys) has a 0.  Without a bias the products stay as
-// they are.  lo, hi: bias past the distance.
+// they are.  lo, hi: bias past the distance; dp: set to 0 in the same places.
 template <bool kBias>
 __device__ __forceinline__ void finish_scores(f32x16& s, float scale2, const float* table,
                                               int distance, int pos, int pos_min, int pos_max,
-                                              float lo, float hi, int base, int h, uint32_t bits) {
+                                              float lo, float hi, int base, int h, uint32_t bits,
+                                              f32x16* dp = nullptr) {
   if constexpr (kBias) {
     if (base - pos_max >= distance || base + 31 - pos_min <= -distance) {
       const float far = base > pos_min ? hi : lo;
@@ -436,8 +486,11 @@ __device__ __forceinline__ void finish_scores(f32x16& s, float scale2, const flo
   if (!__all(bits == ~0u)) {
     const uint32_t mine = bits >> (4 * h);
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      s[r] = mine >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : -INFINITY;
+    for (int r = 0; r < 16; ++r) {
+      const bool seen = mine >> (8 * (r >> 2) + (r & 3)) & 1;
+      s[r] = seen ? s[r] : -INFINITY;
+      if (dp) (*dp)[r] = seen ? (*dp)[r] : 0.f;  // P = 0 there, but dP need not be a number
+    }
   }
 }
 
@@ -625,11 +678,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
   const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
   KeyStage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2> stage;
+  stage.place(a);
   uint8_t ok[kBlocks];
   auto fetch = [&](int base, int b) {
     stage.load(a, mask, k0, v0, base, it.hi, s_k + b * kTileN, s_v + b * kTileN);
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i) ok[i] = key_ok(mask, base + 32 * ((WK == 1 ? 0 : wave) + i) + (lane & 31), it.hi);
+    for (int i = 0; i < kBlocks; ++i)
+      if (mask || base + kTile > it.hi)
+        ok[i] = key_ok(mask, base + 32 * ((WK == 1 ? 0 : wave) + i) + (lane & 31), it.hi);
   };
   if (it.lo < it.hi) fetch(it.lo, 0);
 
@@ -666,7 +722,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     uint32_t bits[kBlocks], any = 0;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      bits[b] = (uint32_t)__ballot(ok[b] != 0);
+      bits[b] = mask || base + kTile > it.hi ? (uint32_t)__ballot(ok[b] != 0) : ~0u;
       if (a.causal) bits[b] &= upto(me.pos, first + 32 * b);
       any |= bits[b];
     }
@@ -696,7 +752,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
       }
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = fmaxf(top, other_half(top));
       if constexpr (!kBias) top *= scale2;
       if (__any(top > m + kLag<T>)) {
         const float next = fmaxf(m, top);
@@ -736,7 +792,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       __syncthreads();
     }
   }
-  l += __shfl_xor(l, 32);
+  l += other_half(l);
   float at = (m == -INFINITY ? 0.f : m) - kShift<T>;  // the sums are relative to 2^at
 
   if constexpr (WK == 4) {
@@ -974,11 +1030,13 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
   const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
   KeyStage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2> stage;
+  stage.place(a);
   uint8_t ok[kBlocks];
   auto fetch = [&](int base, int b) {
     stage.load(a, mask, k0, v0, base, it.hi, s_k + b * kTileN, s_v + b * kTileN);
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i) ok[i] = key_ok(mask, base + 32 * i + (lane & 31), it.hi);
+    for (int i = 0; i < kBlocks; ++i)
+      if (mask || base + kTile > it.hi) ok[i] = key_ok(mask, base + 32 * i + (lane & 31), it.hi);
   };
   if (it.lo < it.hi) fetch(it.lo, 0);
 
@@ -1004,7 +1062,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
       for (int j = 0; j < 8; ++j) dsum += (float)dout[c][j] * (float)out[c][j];
-    dsum += __shfl_xor(dsum, 32);
+    dsum += other_half(dsum);
     if (me.live && h == 0) a.dsum[at] = dsum;
   }
   float lo = 0.f, hi = 0.f, far_lo = 0.f, far_hi = 0.f;
@@ -1048,7 +1106,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     uint32_t bits[kBlocks], any = 0;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      bits[b] = (uint32_t)__ballot(ok[b] != 0);
+      bits[b] = mask || base + kTile > it.hi ? (uint32_t)__ballot(ok[b] != 0) : ~0u;
       if (a.causal) bits[b] &= upto(me.pos, base + 32 * b);
       any |= bits[b];
     }
@@ -1069,22 +1127,15 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         }
         const int first = base + 32 * b;
         finish_scores<kBias>(s, scale2, table, a.distance, me.pos, me.pos_min, me.pos_max, lo, hi,
-                             first, h, bits[b]);
+                             first, h, bits[b], &dp);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           s[r] = __builtin_amdgcn_exp2f(kBias ? s[r] - lse2 : s[r] * scale2 - lse2);
-        if (!__all(bits[b] == ~0u)) {
-          // P = 0 there, but dP need not be a number
-          const uint32_t mine = bits[b] >> (4 * h);
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            dp[r] = mine >> (8 * (r >> 2) + (r & 3)) & 1 ? dp[r] : 0.f;
-        }
         if (b == 0 && one_block) {
           float t = 0.f;
 #pragma unroll
           for (int r = 0; r < 16; ++r) t += s[r] == 0.f ? 0.f : s[r] * dp[r];
-          dsum = (t + __shfl_xor(t, 32)) * kUpOut;
+          dsum = (t + other_half(t)) * kUpOut;
           if (me.live && h == 0) a.dsum[at] = dsum;
         }
 #pragma unroll
@@ -1119,7 +1170,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
           float t = 0.f;
 #pragma unroll
           for (int r = 0; r < 16; ++r) t = fmaxf(t, fabsf(s[r]));
-          t = fmaxf(t, __shfl_xor(t, 32));
+          t = fmaxf(t, other_half(t));
           most = fmaxf(most, t);
           if (__any(most * up >= 0x1p15f)) {
             // the largest so far to 2^13 .. 2^14
@@ -1251,11 +1302,15 @@ struct DkvShape {
   static constexpr int kTile = 32 * kBlocks;
   static constexpr int kBufs = 2;
   static constexpr int kTileBytes = kTile * kPitch<DP> * (int)sizeof(T);
-  // The tile's values as operands in registers, or, where the accumulators leave no room
-  // for them at two waves a SIMD, in LDS.
-  static constexpr bool kValuesInLds = DP * sizeof(T) >= 256;
-  static constexpr int kValueBytes =
-      kValuesInLds ? kAttnKeys * kPitch<DP> * (int)sizeof(T) : 0;
+  // Chunks of 16 of the keys' and the values' operands that stay in registers.  The others are
+  // in LDS: with them the accumulators would not fit two waves a SIMD (where the loop ran with
+  // five chunks spilled to memory, each of which waited for the next tile's loads, 2 x 8,192
+  // tokens of 16 heads took 4.7 ms against 4.1).
+  static constexpr int kChunks = DP / 16;
+  static constexpr int kKeptV = DP * sizeof(T) >= 256 ? 0 : kChunks;
+  static constexpr int kKeptK = DP == 128 && sizeof(T) == 2 ? 5 : kChunks;
+  static constexpr int kWaveBytes = (2 * kChunks - kKeptK - kKeptV) * kFragBytes<T>;
+  static constexpr int kValueBytes = kAttnThreads / 64 * kWaveBytes;
   static constexpr int kBytes = kValueBytes + kBufs * (2 * kTileBytes + 4 * kTile * 4);
 };
 
@@ -1300,7 +1355,6 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     reduce_bias<T>(a, blockIdx.x, (float*)smem);
     return;
   }
-  T* s_val = (T*)smem;
   T* s_q = (T*)(smem + Shape::kValueBytes);
   T* s_do = s_q + Shape::kBufs * kTileN;
   float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][the row's exponent, -D, table offset, pos][row]
@@ -1331,18 +1385,19 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const bool row_mine = threadIdx.x < kTile;
   // a row without keys is only possible with a mask or a table that holds -infinity
   const bool some_empty = a.key_mask || kBias;
-  typedef decltype(Tile::off_zero()) Off;
-  Off off_q[kN], off_do[kN];
   int off_lse[kN], off_row = 0, tok_row = 0;
   auto offsets = [&](int base) {
     const int tok0 = query_of(a, base);
+    auto in = [&](const sieve_heads& x, int row, int col) {
+      const int r = base + row, tok = query_of(a, r);
+      return (tok - tok0) * x.token_stride + (r - tok * G) * x.head_stride + col;
+    };
+    st_q.place([&](int row, int col) { return in(a.q, row, col); }, d);
+    st_do.place([&](int row, int col) { return in(a.dout, row, col); }, d);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int r = base + Tile::row(i), tok = query_of(a, r);
-      const Off t = tok - tok0, g = r - tok * G;
-      off_q[i] = t * (Off)a.q.token_stride + g * (Off)a.q.head_stride + Tile::col(i);
-      off_do[i] = t * (Off)a.dout.token_stride + g * (Off)a.dout.head_stride + Tile::col(i);
-      off_lse[i] = (int)t * a.heads + (int)g;
+      off_lse[i] = (tok - tok0) * a.heads + (r - tok * G);
     }
     const int r = base + (int)threadIdx.x, tok = query_of(a, r);
     tok_row = tok - tok0;
@@ -1352,10 +1407,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   auto fetch = [&](int base, int b) {
     if (!fixed) offsets(base);
     const int tok0 = query_of(a, base);
-    st_q.load(q0 + tok0 * a.q.token_stride, [&](int i) { return off_q[i]; }, it.hi - base, d,
-              s_q + b * kTileN);
-    st_do.load(do0 + tok0 * a.dout.token_stride, [&](int i) { return off_do[i]; }, it.hi - base, d,
-               s_do + b * kTileN);
+    st_q.load(q0 + tok0 * a.q.token_stride, it.hi - base, d, s_q + b * kTileN);
+    st_do.load(do0 + tok0 * a.dout.token_stride, it.hi - base, d, s_do + b * kTileN);
     const float* lse = lse0 + (int64_t)tok0 * a.heads;
     if (some_empty) {
 #pragma unroll
@@ -1390,7 +1443,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 
   const lds_addr q_al = lds_of(s_q) + lane_along<T, DP>(lane);
   const lds_addr q_ac = lds_of(s_q) + lane_across<T, DP>(lane);
-  const lds_addr val_al = lds_of(s_val + wave * 32 * kPitch<DP>) + lane_along<T, DP>(lane);
+  // chunks of the values, then of the keys
+  const lds_addr kept = lds_of(smem) + wave * Shape::kWaveBytes + lane * 16;
+  constexpr int kKeptK = Shape::kKeptK, kKeptV = Shape::kKeptV, kMoreV = Shape::kChunks - kKeptV;
   vec8<T> k[DP / 16], v[DP / 16];
   {
     const int64_t tok = it.k0 + (live ? key : 0);
@@ -1398,11 +1453,10 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
                       d, h, k);
     load_frags<T, DP, kVec>((const T*)a.v.data + tok * a.v.token_stride + it.kvh * a.v.head_stride, live,
                       d, h, v);
-    if constexpr (Shape::kValuesInLds) {  // a wave reads its own 32 rows only
 #pragma unroll
-      for (int c = 0; c < DP / 16; ++c)
-        put_along<T, DP>(val_al, 0, c, v[c]);
-    }
+    for (int c = kKeptV; c < DP / 16; ++c) keep_frag<T>(kept, c - kKeptV, v[c]);
+#pragma unroll
+    for (int c = kKeptK; c < DP / 16; ++c) keep_frag<T>(kept, kMoreV + c - kKeptK, k[c]);
   }
   if constexpr (kBias) load_bias<T>(a, it.kvh, s_bias);
   float up = 1.f;  // what brings dS times 2^kUpP to where it is rounded
@@ -1429,10 +1483,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       constexpr int kApart = Shape::kBufs * kTileN * (int)sizeof(T);  // s_do - s_q
       lds_addr sq = q_al + buf * kTileN * (int)sizeof(T);
       lds_addr sq_ac = q_ac + buf * kTileN * (int)sizeof(T);
-      lds_addr val_at = val_al;
       // Work the reads' addresses out at each tile: kept over the loop they would fill the
       // registers that the accumulators leave.
-      if constexpr (Shape::kValuesInLds) asm volatile("" : "+v"(sq), "+v"(sq_ac), "+v"(val_at));
+      if constexpr (kMoreV > 0) asm volatile("" : "+v"(sq), "+v"(sq_ac));
       const lds_addr sd = sq + kApart, sd_ac = sq_ac + kApart;
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
@@ -1459,13 +1512,11 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
           if (sizeof(T) == 4 && 16 * c >= d) break;
-          s = mma(frag_along<T, DP>(sq, 32 * b, c), k[c], s);
-          vec8<T> val;
-          if constexpr (Shape::kValuesInLds)
-            val = frag_along<T, DP>(val_at, 0, c);
-          else
-            val = v[c];
-          dp = mma(frag_along<T, DP>(sd, 32 * b, c), val, dp);
+          const vec8<T> key_c =
+              c < kKeptK ? k[c] : frag_kept<T>(kept, kMoreV + c - kKeptK);
+          const vec8<T> val_c = c < kKeptV ? v[c] : frag_kept<T>(kept, c - kKeptV);
+          s = mma(frag_along<T, DP>(sq, 32 * b, c), key_c, s);
+          dp = mma(frag_along<T, DP>(sd, 32 * b, c), val_c, dp);
         }
         if constexpr (kBias) {
           const int dist = a.distance;
