@@ -14,6 +14,7 @@ import math
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import F16, F32, SieveError, _check, load_library
 
@@ -71,22 +72,30 @@ def _library():
     return lib
 
 
-_nothing = contextlib.nullcontext()
-
-
+@contextlib.contextmanager
 def _on(device: torch.device, stream):
     """The device and the stream that the call's allocations and kernels belong to."""
-    if stream is None and device.index == torch.cuda.current_device():
-        return _nothing
-    stack = contextlib.ExitStack()
-    stack.enter_context(torch.cuda.device(device))
-    if stream is not None:
-        stack.enter_context(torch.cuda.stream(stream))
-    return stack
+    with torch.cuda.device(device):
+        if stream is None:
+            yield
+        else:
+            with torch.cuda.stream(stream):
+                yield
 
 
-def _raw_stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _here(device: torch.device, stream) -> bool:
+    """Whether a call is to run on the current device and stream: the short way."""
+    return stream is None and device.index == torch.cuda.current_device()
+
+
+# the current stream's handle without a Stream object around it, where torch has that
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _raw_stream(device: torch.device) -> int:
+    if _current_handle is not None:
+        return _current_handle(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -130,31 +139,39 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[tor
     ``h`` is the sum that was normed (``x`` itself without a residual), ``mean`` and ``rstd`` are
     fp32, one a row.  ``weight`` and ``bias`` are of x's dtype or float32."""
     _need(x.is_cuda, "x must be a GPU tensor")
-    _need(x.dim() >= 1 and x.shape[-1] >= 1, "x must have a last axis of at least one value")
-    n = int(x.shape[-1])
+    if _here(x.device, stream):
+        return _norm_forward(x, weight, bias, eps, residual)
+    with _on(x.device, stream):
+        return _norm_forward(x, weight, bias, eps, residual)
+
+
+def _norm_forward(x, weight, bias, eps, residual):
+    shape = x.shape
+    _need(len(shape) >= 1 and shape[-1] >= 1, "x must have a last axis of at least one value")
+    n = shape[-1]
     code = _code(x, "x")
     _check_affine(x, weight, bias, n)
-    if residual is not None:
-        _need(residual.shape == x.shape and residual.dtype == x.dtype and
-              residual.device == x.device, "residual must match x")
     lib = _library()
-    with _on(x.device, stream):
-        s = _raw_stream()
-        xr, x_stride = _rows(x, n)
-        rr, r_stride = (None, 0) if residual is None else _rows(residual, n)
-        w, b = weight.contiguous(), None if bias is None else bias.contiguous()
-        rows = x.numel() // n
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        h = None if rr is None else torch.empty_like(y)
-        mean, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32,
-                                 device=x.device).unbind(0)
-        if rows:
-            _check(lib, lib.sieve_norm_forward(
-                xr.data_ptr(), x_stride, None if rr is None else rr.data_ptr(), r_stride,
-                w.data_ptr(), None if b is None else b.data_ptr(), code, _CODES[w.dtype], rows, n,
-                eps, y.data_ptr(), None if h is None else h.data_ptr(), mean.data_ptr(),
-                rstd.data_ptr(), s))
-    return y, x if h is None else h, mean, rstd
+    xr, x_stride = _rows(x, n)
+    rr, r_stride, h = None, 0, None
+    y = x.new_empty(shape)
+    if residual is not None:
+        _need(residual.shape == shape and residual.dtype is x.dtype and
+              residual.device == x.device, "residual must match x")
+        rr, r_stride = _rows(residual, n)
+        h = x.new_empty(shape)
+    w = weight.contiguous()
+    b = None if bias is None else bias.contiguous()
+    rows = x.numel() // n
+    stats = x.new_empty((2,) + shape[:-1], dtype=torch.float32)
+    if rows:
+        at = stats.data_ptr()
+        _check(lib, lib.sieve_norm_forward(
+            xr.data_ptr(), x_stride, None if rr is None else rr.data_ptr(), r_stride,
+            w.data_ptr(), None if b is None else b.data_ptr(), code, _CODES[w.dtype], rows, n, eps,
+            y.data_ptr(), None if h is None else h.data_ptr(), at, at + 4 * rows,
+            _raw_stream(x.device)))
+    return y, x if h is None else h, stats[0], stats[1]
 
 
 def _check_affine(x, weight, bias, n):
@@ -176,34 +193,41 @@ def layer_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor,
     gradient that reaches ``h`` by another way.  Returns ``(dx, dweight, dbias)``; ``dx`` is the
     gradient of x and of the residual alike, the other two are None where not asked for."""
     _need(h.is_cuda, "h must be a GPU tensor")
-    n = int(h.shape[-1]) if h.dim() else 0
-    _need(n >= 1, "h must have a last axis of at least one value")
+    args = (dy, h, weight, mean, rstd, dh, weight_grad, bias_grad)
+    if _here(h.device, stream):
+        return _norm_backward(*args)
+    with _on(h.device, stream):
+        return _norm_backward(*args)
+
+
+def _norm_backward(dy, h, weight, mean, rstd, dh, weight_grad, bias_grad):
+    shape = h.shape
+    _need(len(shape) >= 1 and shape[-1] >= 1, "h must have a last axis of at least one value")
+    n = shape[-1]
     code = _code(h, "h")
     _check_affine(h, weight, None, n)
     rows = h.numel() // n
     for name, t in (("dy", dy), ("dh", dh)):
         if t is not None:
-            _need(t.shape == h.shape and t.dtype == h.dtype and t.device == h.device,
+            _need(t.shape == shape and t.dtype is h.dtype and t.device == h.device,
                   f"{name} must match h")
     for name, t in (("mean", mean), ("rstd", rstd)):
-        _need(t.numel() == rows and t.dtype == torch.float32 and t.device == h.device and
+        _need(t.numel() == rows and t.dtype is torch.float32 and t.device == h.device and
               t.is_contiguous(), f"{name} must be the forward pass's, one float32 a row")
     lib = _library()
-    with _on(h.device, stream):
-        s = _raw_stream()
-        hr, h_stride = _rows(h, n)
-        dr, dy_stride = _rows(dy, n)
-        er = None if dh is None else dh.contiguous()
-        w = weight.contiguous()
-        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        dw = torch.empty_like(w) if weight_grad else None
-        db = torch.empty_like(w) if bias_grad else None
-        size = lib.sieve_norm_workspace(rows, n)
-        space = _workspace(lib, size, h.device)
-        _check(lib, lib.sieve_norm_backward(
-            _ptr(dr), dy_stride, _ptr(hr), h_stride, w.data_ptr(), _ptr(mean),
-            _ptr(rstd), _ptr(er), code, _CODES[w.dtype], rows, n, _ptr(dx), _ptr(dw), _ptr(db),
-            _ptr(space), int(size), s))
+    hr, h_stride = _rows(h, n)
+    dr, dy_stride = _rows(dy, n)
+    er = None if dh is None else dh.contiguous()
+    w = weight.contiguous()
+    dx = h.new_empty(shape)
+    dw = w.new_empty(n) if weight_grad else None
+    db = w.new_empty(n) if bias_grad else None
+    size = lib.sieve_norm_workspace(rows, n)
+    space = _workspace(lib, size, h.device)
+    _check(lib, lib.sieve_norm_backward(
+        _ptr(dr), dy_stride, _ptr(hr), h_stride, w.data_ptr(), _ptr(mean), _ptr(rstd), _ptr(er),
+        code, _CODES[w.dtype], rows, n, _ptr(dx), _ptr(dw), _ptr(db), _ptr(space), size,
+        _raw_stream(h.device)))
     return dx, dw, db
 
 
@@ -218,6 +242,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh=None):
         h, weight, mean, rstd = ctx.saved_tensors
         if dy is None:
@@ -273,13 +298,14 @@ class AttentionPlan:
             torch.device("cuda", torch.cuda.current_device())
         self._q_shape = torch.Size((self.queries, self.heads, self.head_dim))
         self._k_shape = torch.Size((self.keys, self.kv_heads, self.head_dim))
+        self._lse_shape = self._q_shape[:2]
         desc = _Desc(_CODES[dtype], self.heads, self.kv_heads, self.head_dim, int(self.causal),
                      self.num_buckets, self.max_distance, self.scale, qo.numel() - 1,
                      qo.data_ptr(), ko.data_ptr())
         handle = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(lib, lib.sieve_attn_create(ctypes.byref(desc),
-                                              torch.cuda.current_stream().cuda_stream,
+                                              _raw_stream(self.device),
                                               ctypes.byref(handle)))
         self._h, self._lib = handle, lib
         self._space = [int(lib.sieve_attn_workspace(handle, b)) for b in (0, 1)]
@@ -296,6 +322,9 @@ class AttentionPlan:
             pass
 
     def _tensor(self, t: torch.Tensor, name: str, shape) -> torch.Tensor:
+        if t.dtype is self.dtype and t.shape == shape and t.device == self.device and \
+                t.stride(2) == 1:
+            return t
         if t.dtype != self.dtype:
             raise TypeError(f"{name} must be {self.dtype}, not {t.dtype}")
         if t.shape != shape or t.device != self.device:
@@ -330,15 +359,20 @@ class AttentionPlan:
         """``q`` [queries, heads, head_dim], ``k`` and ``v`` [keys, kv_heads, head_dim], any
         strides with neighbouring values side by side; ``key_mask`` [keys], False: not seen.
         Returns ``(out, lse)``: the output and the fp32 logarithm of each row's sum."""
+        if _here(self.device, stream):
+            return self._forward(q, k, v, key_mask, bias)
         with _on(self.device, stream):
-            s = _raw_stream()
-            q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
-            out = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
-            lse = torch.empty((self.queries, self.heads), dtype=torch.float32, device=self.device)
-            space = _workspace(self._lib, self._space[0], self.device)
-            _check(self._lib, self._lib.sieve_attn_forward(
-                self._h, _heads(q), _heads(k), _heads(v), _ptr(key_mask), _ptr(bias), _heads(out),
-                lse.data_ptr(), _ptr(space), self._space[0], s))
+            return self._forward(q, k, v, key_mask, bias)
+
+    def _forward(self, q, k, v, key_mask, bias):
+        q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
+        out = q.new_empty(self._q_shape)
+        lse = q.new_empty(self._lse_shape, dtype=torch.float32)
+        size = self._space[0]
+        space = _workspace(self._lib, size, self.device) if size else None
+        _check(self._lib, self._lib.sieve_attn_forward(
+            self._h, _heads(q), _heads(k), _heads(v), _ptr(key_mask), _ptr(bias), _heads(out),
+            lse.data_ptr(), _ptr(space), size, _raw_stream(self.device)))
         return out, lse
 
     def backward(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -347,24 +381,27 @@ class AttentionPlan:
                  stream=None):
         """Gradients from the output's, and the forward pass's inputs and results.  Returns
         ``(dq, dk, dv, dbias)``; ``dbias`` is None without a bias (or with ``bias_grad=False``)."""
+        args = (dout, q, k, v, out, lse, key_mask, bias, bias_grad)
+        if _here(self.device, stream):
+            return self._backward(*args)
         with _on(self.device, stream):
-            s = _raw_stream()
-            q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
-            dout = self._tensor(dout, "dout", self._q_shape)
-            out = self._tensor(out, "out", self._q_shape)
-            _need(lse.shape == self._q_shape[:2] and lse.is_contiguous() and
-                  lse.dtype == torch.float32 and lse.device == self.device,
-                  "lse must be the forward pass's")
-            dq = torch.empty(self._q_shape, dtype=self.dtype, device=self.device)
-            dk = torch.empty(self._k_shape, dtype=self.dtype, device=self.device)
-            dv = torch.empty_like(dk)
-            want = bias is not None and bias_grad is not False
-            dbias = torch.empty_like(bias) if want else None
-            space = _workspace(self._lib, self._space[1], self.device)
-            _check(self._lib, self._lib.sieve_attn_backward(
-                self._h, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), _ptr(lse),
-                _ptr(key_mask), _ptr(bias), _heads(dq), _heads(dk), _heads(dv), _ptr(dbias),
-                _ptr(space), self._space[1], s))
+            return self._backward(*args)
+
+    def _backward(self, dout, q, k, v, out, lse, key_mask, bias, bias_grad):
+        q, k, v, key_mask, bias = self._inputs(q, k, v, key_mask, bias)
+        dout = self._tensor(dout, "dout", self._q_shape)
+        out = self._tensor(out, "out", self._q_shape)
+        _need(lse.shape == self._lse_shape and lse.dtype is torch.float32 and
+              lse.is_contiguous() and lse.device == self.device, "lse must be the forward pass's")
+        dq = q.new_empty(self._q_shape)
+        dk, dv = k.new_empty(self._k_shape), v.new_empty(self._k_shape)
+        dbias = bias.new_empty(bias.shape) if bias is not None and bias_grad is not False else None
+        size = self._space[1]
+        space = _workspace(self._lib, size, self.device) if size else None
+        _check(self._lib, self._lib.sieve_attn_backward(
+            self._h, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), _ptr(lse),
+            _ptr(key_mask), _ptr(bias), _heads(dq), _heads(dk), _heads(dv), _ptr(dbias),
+            _ptr(space), size, _raw_stream(self.device)))
         return dq, dk, dv, dbias
 
 
@@ -387,6 +424,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, key_mask, bias = ctx.saved_tensors
         dq, dk, dv, dbias = ctx.plan.backward(dout, q, k, v, out, lse, key_mask, bias,
