@@ -1049,19 +1049,29 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   vec8<T> q[DP / 16], dout[DP / 16];
   {
     const float lse = me.live ? a.lse[at] : -INFINITY;
-    const bool some = lse != -INFINITY;
-    if (some) lse2 = lse * kLog2e - kUp;
     const T* pq = (const T*)a.q.data + (me.live ? row_at(a, a.q, it, me.r) : 0);
     const T* pd = (const T*)a.dout.data + (me.live ? row_at(a, a.dout, it, me.r) : 0);
     const T* po = (const T*)a.o.data + (me.live ? row_at(a, a.o, it, me.r) : 0);
     vec8<T> out[DP / 16];
-    load_frags<T, DP, kVec>(pq, some, d, h, q);
-    load_frags<T, DP, kVec>(pd, some, d, h, dout);
-    load_frags<T, DP, kVec>(po, some, d, h, out);
+    load_frags<T, DP, kVec>(pq, me.live, d, h, q);
+    load_frags<T, DP, kVec>(pd, me.live, d, h, dout);
+    load_frags<T, DP, kVec>(po, me.live, d, h, out);
+    const bool some = lse != -INFINITY;
+    if (some) lse2 = lse * kLog2e - kUp;
+    if (!__all(some)) {  // rows without keys, whatever they hold
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          q[c][j] = some ? q[c][j] : (T)0.f;
+          dout[c][j] = some ? dout[c][j] : (T)0.f;
+        }
+    }
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
       for (int j = 0; j < 8; ++j) dsum += (float)dout[c][j] * (float)out[c][j];
+    if (!some) dsum = 0.f;
     dsum += other_half(dsum);
     if (me.live && h == 0) a.dsum[at] = dsum;
   }

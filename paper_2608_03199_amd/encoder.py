@@ -8,6 +8,7 @@ allocator on that stream; there is no CPU fallback.
 """
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes
 import math
@@ -50,7 +51,6 @@ def _library():
         return _ready
     lib = load_library()
     P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-    H = ctypes.POINTER(_Heads)
     lib.sieve_norm_forward.restype = ctypes.c_int
     lib.sieve_norm_forward.argtypes = [P, i64, P, i64, P, P, i32, i32, i64, i32, f32, P, P, P, P, P]
     lib.sieve_norm_backward.restype = ctypes.c_int
@@ -65,9 +65,9 @@ def _library():
     lib.sieve_attn_workspace.restype = i64
     lib.sieve_attn_workspace.argtypes = [P, i32]
     lib.sieve_attn_forward.restype = ctypes.c_int
-    lib.sieve_attn_forward.argtypes = [P, H, H, H, P, P, H, P, P, i64, P]
+    lib.sieve_attn_forward.argtypes = [P, P, P, P, P, P, P, P, P, i64, P]
     lib.sieve_attn_backward.restype = ctypes.c_int
-    lib.sieve_attn_backward.argtypes = [P, H, H, H, H, H, P, P, P, H, H, H, P, P, i64, P]
+    lib.sieve_attn_backward.argtypes = [P] * 14 + [i64, P]
     _ready = lib
     return lib
 
@@ -370,9 +370,10 @@ class AttentionPlan:
         lse = q.new_empty(self._lse_shape, dtype=torch.float32)
         size = self._space[0]
         space = _workspace(self._lib, size, self.device) if size else None
+        held, (hq, hk, hv, ho) = _heads(q, k, v, out)
         _check(self._lib, self._lib.sieve_attn_forward(
-            self._h, _heads(q), _heads(k), _heads(v), _ptr(key_mask), _ptr(bias), _heads(out),
-            lse.data_ptr(), _ptr(space), size, _raw_stream(self.device)))
+            self._h, hq, hk, hv, _ptr(key_mask), _ptr(bias), ho, lse.data_ptr(), _ptr(space),
+            size, _raw_stream(self.device)))
         return out, lse
 
     def backward(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -398,10 +399,10 @@ class AttentionPlan:
         dbias = bias.new_empty(bias.shape) if bias is not None and bias_grad is not False else None
         size = self._space[1]
         space = _workspace(self._lib, size, self.device) if size else None
+        held, (hdo, hq, hk, hv, ho, hdq, hdk, hdv) = _heads(dout, q, k, v, out, dq, dk, dv)
         _check(self._lib, self._lib.sieve_attn_backward(
-            self._h, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), _ptr(lse),
-            _ptr(key_mask), _ptr(bias), _heads(dq), _heads(dk), _heads(dv), _ptr(dbias),
-            _ptr(space), size, _raw_stream(self.device)))
+            self._h, hdo, hq, hk, hv, ho, _ptr(lse), _ptr(key_mask), _ptr(bias), hdq, hdk, hdv,
+            _ptr(dbias), _ptr(space), size, _raw_stream(self.device)))
         return dq, dk, dv, dbias
 
 
@@ -410,9 +411,19 @@ def _side_by_side(t: torch.Tensor) -> torch.Tensor:
     return t if t.stride(2) == 1 or t.shape[2] == 1 or t.numel() == 0 else t.contiguous()
 
 
-def _heads(t: torch.Tensor) -> _Heads:
-    token, head, _ = t.stride()
-    return _Heads(t.data_ptr(), token, head)
+_HEADS_SIZE = ctypes.sizeof(_Heads)
+
+
+def _heads(*tensors: torch.Tensor):
+    """The tensors' ``sieve_heads`` one after another: what holds them, and their addresses.
+    (One array of whole numbers: a ctypes structure each costs a microsecond each.)"""
+    fields = []
+    for t in tensors:
+        token, head, _ = t.stride()
+        fields += (t.data_ptr(), token, head)
+    held = array.array("q", fields)
+    first = held.buffer_info()[0]
+    return held, range(first, first + len(tensors) * _HEADS_SIZE, _HEADS_SIZE)
 
 
 class _Attention(torch.autograd.Function):
