@@ -522,7 +522,8 @@ __device__ __forceinline__ LaneRow lane_row(const AttnArgs& a, const AttnItem& i
 
 // The running maximum may lag by kLag powers of two before the sums are brought to a new one,
 // and P is 2^kShift at it.  For binary16, 2^(kLag + kShift) has to stay below 65504 and what
-// 2^kShift pushes below 2^-14 loses bits.
+// 2^kShift pushes below 2^-14 loses bits.  2 x 8,192 tokens of 16 heads of 128, bf16: 1,054 us,
+// without a lag 1,100; 4 x 8,192 of 12 heads of 64: 926, 962.
 template <typename T>
 constexpr float kLag = __is_same(T, f16) ? 4.f : 8.f;
 template <typename T>
@@ -644,7 +645,11 @@ __device__ void careful_row(const AttnArgs& a, const AttnItem& it, const float* 
 // ---- forward ----------------------------------------------------------------------------
 // WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
 // each wave takes every fourth block of 32 keys, and LDS joins the four at the end: for
-// few rows, where the keys' and values' bytes bound the time.
+// few rows, where the keys' and values' bytes bound the time.  Long sequences: matrix and
+// vector issue (matrix units 37-40% busy); 12,007 causal tokens, 16 heads over 4 of 128, bf16,
+// 690 us, 857 TFLOP/s.  Few rows: memory; one query over 32 documents of 1,000..30,000 222 us
+// with the join, 5.0 TB/s.  Tiles of 64 keys: with 32 the 12,007 tokens took 755 us against 670,
+// 4 x 8,192 of 12 heads of 64 977 against 926.
 
 template <typename T, int DP, int WK>
 struct FwdShape {
@@ -895,6 +900,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 }
 
 // Partial rows of one tile to whole ones: DP / 4 threads a row, kJoinRows rows a work-group.
+// Latency: 12 us after the pooled queries above.
 template <int DP>
 constexpr int kJoinRows = kAttnThreads / (DP / 4);
 
@@ -946,8 +952,17 @@ constexpr float kUp = 24.f, kUpOut = 0x1p-24f;
 // that a lane can read down a whole diagonal without a test (row i's value at relative
 // position p + i lies at a constant step from row i - 1's), and adds the result to its own
 // sums by position.  No atomics: the order of additions is the program's.
+//
+// Issue bounds it.  Two causal documents of 5,000..6,100 (16 heads over 4 of 128, bf16) 452 us;
+// 256 documents of 16..512 (12 heads of 64, f16) with a bias's gradient 365.  That gradient adds
+// 70 to 110 us to a backward pass of 552 to 560.
+//
+// dS is rounded to the inputs' type for the product and D comes from the rounded output: dQ and
+// dK in 16 bits are up to 1.8 times as far from exact as one rounding of the result.
 
-// With a bias the tile is 32 keys, so that two work-groups' LDS fits a CU beside the sums.
+// With a bias the tile is 32 keys, so that two work-groups' LDS fits a CU beside the sums: the
+// 256 documents' backward pass takes 630 us, with 64 keys 749.  Without one 64 keys are faster
+// (4 x 8,192 of 12 heads of 64: 2,850 against 2,960).
 template <typename T, int DP, bool kBias>
 struct DqShape {
   static constexpr int kBlocks = sizeof(T) == 2 && DP <= 64 && !kBias ? 2 : 1;
@@ -1304,7 +1319,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 // A wave takes 32 of the tile's 128 keys, one a lane, and goes through the rows that see
 // them: all query heads of the group, so that the sum over a shared head is the accumulator's.
 // S = Q K^T puts rows 8 g + 4 h + t in registers 4 g + t.  The first `heads` work-groups of a
-// launch with a bias's gradient add up its partial sums instead.
+// launch with a bias's gradient add up its partial sums instead.  Issue bounds it: the two
+// causal documents above 597 us (and 25 to join), the 256 documents 358.
 
 template <typename T, int DP>
 struct DkvShape {
@@ -1314,8 +1330,8 @@ struct DkvShape {
   static constexpr int kTileBytes = kTile * kPitch<DP> * (int)sizeof(T);
   // Chunks of 16 of the keys' and the values' operands that stay in registers.  The others are
   // in LDS: with them the accumulators would not fit two waves a SIMD (where the loop ran with
-  // five chunks spilled to memory, each of which waited for the next tile's loads, 2 x 8,192
-  // tokens of 16 heads took 4.7 ms against 4.1).
+  // registers spilled to memory, each read of which waits for the next tile's loads: 2 x 8,192
+  // tokens of 16 heads, backward, 4.5 ms with all chunks of K in registers, 3.7 with five).
   static constexpr int kChunks = DP / 16;
   static constexpr int kKeptV = DP * sizeof(T) >= 256 ? 0 : kChunks;
   static constexpr int kKeptK = DP == 128 && sizeof(T) == 2 ? 5 : kChunks;

@@ -5,7 +5,8 @@
 //   g = dy w, dx = rstd (g - mean(g) - u mean(g u)) + dh
 //   dw = sum_rows dy u, db = sum_rows dy
 //
-// Each value is read once and written once, so memory bounds every kernel here.
+// Each value is read once and written once, so memory bounds every kernel here but the looping
+// ones.  65,536 x 1,024 bf16: forward 47 us, 5.7 TB/s; backward with its reduction 80 us, 5.0 TB/s.
 // A row stays in the registers of a quarter of a wave (up to 128 values), a wave (up to
 // 2,048) or a work-group (up to 8,192): the mean is taken first and the variance from the differences, in
 // fp32 without the cancellation of a sum of squares.  Longer rows are read again,
@@ -31,7 +32,9 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kMaxN = 65536;
 constexpr int kMaxHeld = 8192;  // longest row that stays in registers
 constexpr int kBigThreads = 1024;
-constexpr int kMaxParts = 512;  // work-groups of the backward pass: 2 a CU
+// Work-groups of the backward pass: 2 a CU.  65,536 x 1,024 bf16 81 us, with 256 93, with 1,024
+// 90; 65,536 x 768 f16 61, 78 and 59.
+constexpr int kMaxParts = 512;
 
 struct NormFwd {
   const void *x, *residual, *w, *b;
@@ -337,7 +340,8 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
   }
 }
 
-// Rows too long for the registers: a work-group a row, the row read once a step.
+// Rows too long for the registers: a work-group a row, the row read once a step.  The steps'
+// latency bounds it: 4,096 x 16,384 bf16 119 us, 2.3 TB/s counting each value once.
 template <typename T, typename W>
 __global__ __launch_bounds__(kBigThreads) void norm_forward_big_kernel(NormFwd a) {
   __shared__ float s_sum[kBigThreads / 64];
@@ -378,7 +382,8 @@ __global__ __launch_bounds__(kBigThreads) void norm_forward_big_kernel(NormFwd a
 }
 
 // As above; the columns' sums stay in the work-group's partial row, which a thread
-// reads and writes at its own columns only.
+// reads and writes at its own columns only.  4,096 x 16,384 bf16: 359 us, 1.1 TB/s counting each
+// value once.
 template <typename T, typename W>
 __global__ __launch_bounds__(kBigThreads) void norm_backward_big_kernel(NormBwd a) {
   __shared__ float s_sum[2 * kBigThreads / 64];
@@ -414,7 +419,8 @@ __global__ __launch_bounds__(kBigThreads) void norm_backward_big_kernel(NormBwd 
 }
 
 // Adds the partial rows: a work-group takes 32 of the 2 n columns, its 32 groups of 32
-// threads every 32nd row each, and LDS adds the groups in order.
+// threads every 32nd row each, and LDS adds the groups in order.  Latency: 512 rows of 1,024
+// columns 5 us.
 template <typename W>
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restrict__ part,
                                                            int parts, int n, W* dw, W* db) {
@@ -441,6 +447,8 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
 
 // How a row is spread: NE values a thread (in moves of E, or 0), NT threads.  The smallest
 // that holds it; 768 values, which moves of 8 would fill to three quarters, in moves of 4.
+// 65,536 x 768 f16, forward and backward: 44 and 61 us, as a row of 1,024 47 and 79.
+// 262,144 x 128 f16: 26 and 39 us, with 64 threads a row 64 and 145.
 // f(NE, NT, E of an aligned row) as constants; false for rows that are too long.
 template <int N>
 using Int = std::integral_constant<int, N>;
