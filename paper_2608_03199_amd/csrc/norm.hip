@@ -340,8 +340,9 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBwd a) {
   }
 }
 
-// Rows too long for the registers: a work-group a row, the row read once a step.  The steps'
-// latency bounds it: 4,096 x 16,384 bf16 119 us, 2.3 TB/s counting each value once.
+// Rows too long for the registers: a work-group a row, the row read once a step.  4,096 x
+// 16,384 bf16 119 us, 2.3 TB/s counting each value once; what bounds it was not looked into, its
+// moves are of one value.
 template <typename T, typename W>
 __global__ __launch_bounds__(kBigThreads) void norm_forward_big_kernel(NormFwd a) {
   __shared__ float s_sum[kBigThreads / 64];
