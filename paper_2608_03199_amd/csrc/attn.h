@@ -9,6 +9,8 @@
 namespace sieve {
 
 constexpr int kAttnThreads = 256;
+constexpr int kAttnStats = 3;  // of a partial row: maximum, sum of the probabilities as the
+                               // second product takes them, and as they were before rounding
 
 struct AttnArgs {
   const AttnItem* items;
@@ -30,7 +32,7 @@ struct AttnArgs {
   const int16_t* range;      // [nb][2]: first entry of a bucket and the one past its last
   void* dbias;
   // workspace
-  float* part_o;     // [parts][rows][DP] unnormalised sums, then [parts][rows][2]: max and sum
+  float* part_o;     // [parts][rows][DP] unnormalised sums, then [parts][rows][kAttnStats]
   float* part_ml;
   float* part_kv;    // [parts][dk, dv][kAttnKeys][DP]
   float* dsum;       // [queries][heads]: the rows' sums of dout * o

@@ -161,7 +161,7 @@ FwdSpace fwd_space(const sieve_attn* p) {
   const int64_t rows = (int64_t)p->parts * (p->few ? kAttnFewRows : kAttnRows);
   FwdSpace s;
   s.ml = round256(rows * p->dp * (int64_t)sizeof(float));
-  s.bytes = p->parts ? s.ml + rows * 2 * (int64_t)sizeof(float) : 0;
+  s.bytes = p->parts ? s.ml + rows * kAttnStats * (int64_t)sizeof(float) : 0;
   return s;
 }
 struct BwdSpace {

@@ -530,7 +530,8 @@ template <typename T>
 constexpr float kShift = __is_same(T, f16) ? 11.f : 0.f;
 
 // x plus the sum of an operand's eight values: of the rounded probabilities, which are what
-// the second product adds up, two to an instruction.
+// the second product adds up and so what its result is divided by, two to an instruction.
+// lse is of the probabilities before they are rounded, summed in fp32 beside them.
 __device__ __forceinline__ float add_up(vec8<f16> p, float x) {
   typedef f16 pair __attribute__((ext_vector_type(2)));
   const pair one = {(f16)1.f, (f16)1.f};
@@ -658,7 +659,8 @@ struct FwdShape {
   static constexpr int kTileBytes = kTile * kPitch<DP> * (int)sizeof(T);
   static constexpr int kBufs = 4 * kTileBytes <= 128 * 1024 ? 2 : 1;
   static constexpr int kStageBytes = 2 * kBufs * kTileBytes;
-  static constexpr int kJoinBytes = WK == 1 ? 0 : (WK * 32 * (DP + 4) + 2 * WK * 32 + WK) * 4;
+  static constexpr int kJoinBytes =
+      WK == 1 ? 0 : (WK * 32 * (DP + 4) + kAttnStats * WK * 32 + WK) * 4;
   static constexpr int kBytes = kStageBytes > kJoinBytes ? kStageBytes : kJoinBytes;
   static constexpr int kRows = WK == 1 ? kAttnRows : kAttnFewRows;
 };
@@ -668,6 +670,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   using Shape = FwdShape<T, DP, WK>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
   constexpr int kTileN = kTile * kPitch<DP>;
+  constexpr bool kTwoSums = sizeof(T) == 2;
   extern __shared__ __align__(16) uint8_t smem[];
   T* s_k = (T*)smem;
   T* s_v = s_k + Shape::kBufs * kTileN;
@@ -711,7 +714,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   f32x16 o[DP / 32];
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, full = 0.f;  // full: l of the probabilities as they were
   bool odd = false;  // the wave's rows have to be done again (careful_row)
   const int skip = WK == 1 ? 0 : wave * 32 * kPitch<DP>;  // the wave's keys in a tile
   const lds_addr k_al = lds_of(s_k + skip) + lane_along<T, DP>(lane);
@@ -764,6 +767,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         const float f = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.f : next));
         m = next;
         l *= f;
+        full *= f;
 #pragma unroll
         for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
@@ -780,6 +784,10 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           s[b][r] = __builtin_amdgcn_exp2f(kBias ? s[b][r] - off : s[b][r] * scale2 - off);
+        if constexpr (kTwoSums) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) full += s[b][r];
+        }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const vec8<T> p = frag_of<T>(s[b], c);
@@ -798,29 +806,34 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     }
   }
   l += other_half(l);
+  full = kTwoSums ? full + other_half(full) : l;
   float at = (m == -INFINITY ? 0.f : m) - kShift<T>;  // the sums are relative to 2^at
 
   if constexpr (WK == 4) {
     // join the waves: sums relative to the largest maximum
     float* s_o = (float*)smem;
     float* s_ml = s_o + WK * 32 * (DP + 4);
-    int* s_odd = (int*)(s_ml + 2 * WK * 32);
+    int* s_odd = (int*)(s_ml + kAttnStats * WK * 32);
     __syncthreads();
     if (lane == 0) s_odd[wave] = odd;
     if (h == 0) {
-      s_ml[(wave * 32 + lane) * 2] = l == 0.f ? -INFINITY : at;
-      s_ml[(wave * 32 + lane) * 2 + 1] = l;
+      float* p = s_ml + (wave * 32 + lane) * kAttnStats;
+      p[0] = l == 0.f ? -INFINITY : at;
+      p[1] = l;
+      p[2] = full;
     }
     __syncthreads();
     odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
-    float most = -INFINITY, sum = 0.f;
+    float most = -INFINITY, sum = 0.f, full_sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WK; ++w) most = fmaxf(most, s_ml[(w * 32 + (lane & 31)) * 2]);
+    for (int w = 0; w < WK; ++w) most = fmaxf(most, s_ml[(w * 32 + (lane & 31)) * kAttnStats]);
     if (most == -INFINITY) most = 0.f;
 #pragma unroll
     for (int w = 0; w < WK; ++w) {
-      const float* p = s_ml + (w * 32 + (lane & 31)) * 2;
-      sum += p[1] == 0.f ? 0.f : p[1] * __builtin_amdgcn_exp2f(p[0] - most);
+      const float* p = s_ml + (w * 32 + (lane & 31)) * kAttnStats;
+      const float f = p[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(p[0] - most);
+      sum += p[1] * f;
+      full_sum += p[2] * f;
     }
     const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(at - most);
 #pragma unroll
@@ -834,6 +847,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     __syncthreads();
     if (wave && !odd) return;
     l = sum;
+    full = full_sum;
     at = most;
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
@@ -866,8 +880,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       }
       if (lane == 0) {
         if (it.part >= 0) {
-          a.part_ml[slot * 2] = max_;
-          a.part_ml[slot * 2 + 1] = sum_;
+          a.part_ml[slot * kAttnStats] = max_;
+          a.part_ml[slot * kAttnStats + 1] = a.part_ml[slot * kAttnStats + 2] = sum_;
         } else if (a.lse) {
           a.lse[(it.q0 + tok) * a.heads + it.kvh * G + (r - tok * G)] =
               sum_ == 0.f ? -INFINITY : (max_ + __builtin_amdgcn_logf(sum_)) * kLn2;
@@ -886,8 +900,9 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         *(f32x4*)(p + 32 * b + 8 * g + 4 * h) =
             f32x4{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
     if (h == 0) {
-      a.part_ml[slot * 2] = l == 0.f ? -INFINITY : at;
-      a.part_ml[slot * 2 + 1] = l;
+      a.part_ml[slot * kAttnStats] = l == 0.f ? -INFINITY : at;
+      a.part_ml[slot * kAttnStats + 1] = l;
+      a.part_ml[slot * kAttnStats + 2] = full;
     }
     return;
   }
@@ -896,7 +911,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
                    l == 0.f ? 0.f : 1.f / l, d, h);
   if (a.lse && h == 0)
     a.lse[(it.q0 + me.tok) * a.heads + it.kvh * G + me.g] =
-        l == 0.f ? -INFINITY : (at + __builtin_amdgcn_logf(l)) * kLn2;
+        l == 0.f ? -INFINITY : (at + __builtin_amdgcn_logf(full)) * kLn2;
 }
 
 // Partial rows of one tile to whole ones: DP / 4 threads a row, kJoinRows rows a work-group.
@@ -911,20 +926,21 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
   const int i = blockIdx.x % kGroups * kJoinRows<DP> + threadIdx.x / (DP / 4);
   const int r = j.row + i, c = threadIdx.x % (DP / 4) * 4;
   if (threadIdx.x >= kJoinRows<DP> * (DP / 4) || i >= ROWS || r >= j.n * a.G) return;
-  const float* ml = a.part_ml + ((int64_t)j.part0 * ROWS + i) * 2;
+  const float* ml = a.part_ml + ((int64_t)j.part0 * ROWS + i) * kAttnStats;
   float most = -INFINITY;
 #pragma unroll 4
-  for (int p = 0; p < j.parts; ++p) most = fmaxf(most, ml[(int64_t)p * ROWS * 2]);
+  for (int p = 0; p < j.parts; ++p) most = fmaxf(most, ml[(int64_t)p * ROWS * kAttnStats]);
   if (most == -INFINITY) most = 0.f;
   const float* o = a.part_o + ((int64_t)j.part0 * ROWS + i) * DP + c;
-  float l = 0.f;
+  float l = 0.f, full = 0.f;
   f32x4 v = {};
 #pragma unroll 4
   for (int p = 0; p < j.parts; ++p) {
-    const float lp = ml[(int64_t)p * ROWS * 2 + 1];
+    const float* at = ml + (int64_t)p * ROWS * kAttnStats;
     // a part without keys has l = 0 and o = 0
-    const float f = lp == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[(int64_t)p * ROWS * 2] - most);
-    l += lp * f;
+    const float f = at[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(at[0] - most);
+    l += at[1] * f;
+    full += at[2] * f;
     v += *(const f32x4*)(o + (int64_t)p * ROWS * DP) * f;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -935,7 +951,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
     if (c + t < a.d) to[t] = (T)(v[t] * inv);
   if (a.lse && c == 0)
     a.lse[(j.t0 + tok) * a.heads + head] =
-        l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * kLn2;
+        l == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(full)) * kLn2;
 }
 
 // The backward pass's probabilities are at most 1 and are computed times 2^kUp: the exponential
