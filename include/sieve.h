@@ -394,7 +394,8 @@ SIEVE_API int64_t sieve_norm_workspace(int64_t rows, int32_t n);
  * query's position.  A query that sees no key gets out = 0 and lse = -infinity, and
  * gives no gradient.  What keys and values hold where key_mask leaves them out is not
  * used, infinities and NaN included, and their gradients are 0.  With causal, what they
- * hold after a query's position does not reach that query's output or gradient.
+ * hold after a query's position does not reach that query's output or gradient, and what
+ * q and dout hold for a query does not reach the gradients of the keys after its position.
  *
  * bucket(r) of a relative position r (sides = 2, or 1 with causal; side = num_buckets /
  * sides buckets each; r > 0 is the second side, and with causal it never occurs): with

@@ -643,6 +643,77 @@ __device__ void careful_row(const AttnArgs& a, const AttnItem& it, const float* 
   }
 }
 
+// The kernel's arguments, read again from where the launch put them (its one parameter is the
+// first thing there).  A rare path that takes them from here does not keep the ones that only it
+// needs in scalar registers over the loop before it.
+__device__ __forceinline__ AttnArgs args_again() {
+  typedef const __attribute__((address_space(4))) uint64_t* Words;
+  static_assert(sizeof(AttnArgs) % 8 == 0 && std::is_trivially_copyable<AttnArgs>::value);
+  Words from = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(from));
+  uint64_t words[sizeof(AttnArgs) / 8];
+#pragma unroll
+  for (size_t i = 0; i < sizeof(AttnArgs) / 8; ++i) words[i] = from[i];
+  AttnArgs a;
+  __builtin_memcpy(&a, words, sizeof(a));
+  return a;
+}
+
+// One key's gradients again, without products of rows that do not see it: the mirror image of
+// the above for dK and dV, where a block that is causal in part holds infinities or NaN in q or
+// dout.  A wave a key, 64 rows at a time, a row a lane for P and dS and two values a lane for
+// the sums: dk += dS q, dv += P dout.
+template <typename T, bool kBias>
+__device__ void careful_key(const AttnArgs& a, const AttnItem& it, const float* bias, int key,
+                            int lane, float (&dk)[2], float (&dv)[2]) {
+  const int d = a.d, shift = it.nk - it.nq;
+  const T* k = (const T*)a.k.data + (it.k0 + key) * a.k.token_stride + it.kvh * a.k.head_stride;
+  const T* v = (const T*)a.v.data + (it.k0 + key) * a.v.token_stride + it.kvh * a.v.head_stride;
+  const float scale2 = a.scale * kLog2e;
+  dk[0] = dk[1] = dv[0] = dv[1] = 0.f;
+  for (int base = it.lo; base < it.hi; base += 64) {
+    const int r = base + lane;
+    float p = 0.f, ds = 0.f;
+    bool sees = false;
+    if (r < it.hi) {
+      const int tok = query_of(a, r), pos = tok + shift, g = r - tok * a.G;
+      const int64_t at = (it.q0 + tok) * a.heads + it.kvh * a.G + g;
+      const float lse = a.lse[at];
+      sees = key <= pos && lse != -INFINITY;
+      if (sees) {
+        const T* q = (const T*)a.q.data + row_at(a, a.q, it, r);
+        const T* dout = (const T*)a.dout.data + row_at(a, a.dout, it, r);
+        float s = 0.f, dp = 0.f;
+        for (int c = 0; c < d; ++c) {
+          s += (float)q[c] * (float)k[c];
+          dp += (float)dout[c] * (float)v[c];
+        }
+        s *= scale2;
+        if (kBias) {
+          int rel = key - pos;
+          rel = rel < -a.distance ? -a.distance : rel > a.distance ? a.distance : rel;
+          s += bias[g * a.span + rel + a.distance + kAttnPad];
+        }
+        p = __builtin_amdgcn_exp2f(s - lse * kLog2e);
+        ds = p * (dp - a.dsum[at]);
+      }
+    }
+    const uint64_t these = __ballot(sees);
+    for (int j = 0; j < 64; ++j) {
+      if (!(these >> j & 1)) continue;
+      const float pj = __shfl(p, j), dsj = __shfl(ds, j);
+      const T* q = (const T*)a.q.data + row_at(a, a.q, it, base + j);
+      const T* dout = (const T*)a.dout.data + row_at(a, a.dout, it, base + j);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (lane + 64 * e < d) {
+          dk[e] += dsj * (float)q[lane + 64 * e];
+          dv[e] += pj * (float)dout[lane + 64 * e];
+        }
+    }
+  }
+}
+
 // ---- forward ----------------------------------------------------------------------------
 // WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
 // each wave takes every fourth block of 32 keys, and LDS joins the four at the end: for
@@ -1353,7 +1424,9 @@ struct DkvShape {
   static constexpr int kKeptK = DP == 128 && sizeof(T) == 2 ? 5 : kChunks;
   static constexpr int kWaveBytes = (2 * kChunks - kKeptK - kKeptV) * kFragBytes<T>;
   static constexpr int kValueBytes = kAttnThreads / 64 * kWaveBytes;
-  static constexpr int kBytes = kValueBytes + kBufs * (2 * kTileBytes + 4 * kTile * 4);
+  static constexpr int kOddBytes = 16;  // of each buffer: whether its rows hold odd values
+  static constexpr int kBytes =
+      kValueBytes + kBufs * (2 * kTileBytes + 4 * kTile * 4) + kOddBytes;
 };
 
 template <typename T>
@@ -1400,6 +1473,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   T* s_q = (T*)(smem + Shape::kValueBytes);
   T* s_do = s_q + Shape::kBufs * kTileN;
   float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][the row's exponent, -D, table offset, pos][row]
+  int* s_odd = (int*)(smem + Shape::kBytes - Shape::kOddBytes);  // [buf]
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x - reducers];
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
@@ -1416,6 +1490,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   constexpr int kN = Tile::kN;
   float piece_lse[kN], row_lse = 0.f, row_d = 0.f;
   int row_off = 0, row_pos = 0;
+  bool row_there = false;
   const float* lse0 = a.lse + it.q0 * a.heads + it.kvh * G;  // the sequence's first row
   const float* dsum0 = a.dsum + it.q0 * a.heads + it.kvh * G;
   const T* q0 = (const T*)a.q.data + it.q0 * a.q.token_stride + it.kvh * G * a.q.head_stride;
@@ -1461,7 +1536,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       row_lse = -INFINITY;
       row_d = 0.f;
       row_pos = tok0 + tok_row + shift;
-      if (base + (int)threadIdx.x < it.hi) {
+      row_there = base + (int)threadIdx.x < it.hi;
+      if (row_there) {
         row_lse = lse[off_row];
         row_d = (dsum0 + (int64_t)tok0 * a.heads)[off_row];
       }
@@ -1479,6 +1555,14 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       p[kTile] = -row_d;
       ((int*)p)[2 * kTile] = row_off;
       ((int*)p)[3 * kTile] = row_pos;
+    }
+    // Infinities and NaN in a row's q or dout reach its lse or D.  A row of scores of -infinity
+    // alone is cleared above where that may come of a mask or the bias.
+    if (a.causal && wave == 0) {
+      const bool bad = !(row_lse < INFINITY) || !(fabsf(row_d) < INFINITY) ||
+                       (row_lse == -INFINITY && row_there && !some_empty);
+      const bool any = __any(bad);
+      if (lane == 0) s_odd[b] = any;
     }
   };
   if (it.lo < it.hi) fetch(it.lo, 0);
@@ -1514,6 +1598,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = f32x16{};
+  bool odd = false;  // the wave's keys have to be done again (careful_key)
 
   int buf = 0;
   if (it.lo < it.hi) put(0);
@@ -1601,6 +1686,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
         if (a.causal && pos_min < key0 + 31) {
+          odd |= __builtin_amdgcn_readfirstlane(s_odd[buf]) != 0;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const i32x4 pos = *(const i32x4*)(rows + 3 * kTile + 8 * g);
@@ -1631,6 +1717,33 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       put(buf);
       __syncthreads();
     }
+  }
+  if (__builtin_expect(odd, 0)) {
+    const AttnArgs c = args_again();
+    const AttnItem item = c.items[blockIdx.x - ((int)gridDim.x - c.nitems)];
+    for (int i = 0; i < 32 && key0 + i < item.nk; ++i) {
+      float ck[2] = {}, cv[2] = {};
+      const int64_t tok = item.k0 + key0 + i;
+      if (!c.key_mask || c.key_mask[tok] != 0)
+        careful_key<T, kBias>(c, item, s_bias, key0 + i, lane, ck, cv);
+      T* to_k = (T*)c.dk.data + tok * c.dk.token_stride + item.kvh * c.dk.head_stride;
+      T* to_v = (T*)c.dv.data + tok * c.dv.token_stride + item.kvh * c.dv.head_stride;
+      const int64_t slot = (int64_t)item.part * 2 * kAttnKeys + wave * 32 + i;
+#pragma unroll
+      for (int e = 0; e < (DP + 63) / 64; ++e) {
+        const int col = lane + 64 * e;
+        if (item.part >= 0) {
+          if (col < DP) {
+            c.part_kv[slot * DP + col] = ck[e] * c.scale;
+            c.part_kv[(slot + kAttnKeys) * DP + col] = cv[e];
+          }
+        } else if (col < c.d) {
+          to_k[col] = (T)(ck[e] * c.scale);
+          to_v[col] = (T)cv[e];
+        }
+      }
+    }
+    return;
   }
   if (!there) return;
   if (!live) {

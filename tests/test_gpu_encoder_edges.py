@@ -1,5 +1,7 @@
 """The text-encoder operators where their arithmetic is easiest to get wrong: statistics of 16-bit
 rows, values that are not numbers, and biases far below the scores."""
+import math
+
 import pytest
 import torch
 
@@ -48,3 +50,38 @@ def test_attention_lse_in_16_bits_is_of_unrounded_probabilities(ps, dtype, qlens
     _, lse = plan.forward(q.cuda(), k.cuda(), v.cuda(), bias=None if bias is None else bias.cuda())
     val, tol = attention(q, k, v, qo, ko, causal, None, None, bias, 40)
     check("lse", lse, val["lse"], tol["lse"] - (tol["lse"] > 0) * UNIT[dt])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("lens, heads, kv_heads, d", [
+    ([150, 20, 400], 2, 2, 64), ([150, 20, 400], 4, 1, 128), ([150, 20, 400], 3, 1, 20),
+    ([2300], 2, 1, 96)])
+@pytest.mark.parametrize("buckets", [0, 8])
+def test_attention_causal_earlier_rows_do_not_reach_later_keys(ps, dtype, lens, heads, kv_heads, d,
+                                                               buckets):
+    """A row whose q and dout are not numbers gives nothing to the keys after its position: their
+    gradients are as without it."""
+    dt, rnd = DTYPES[dtype], _rnd(32)
+    o = _offsets(lens)
+    n = int(o[-1])
+    q, k, v = rnd(n, heads, d).to(dt), rnd(n, kv_heads, d).to(dt), rnd(n, kv_heads, d).to(dt)
+    dout = rnd(n, heads, d).to(dt)
+    bias = rnd(buckets, heads).to(dt) if buckets else None
+    odd_q, odd_dout = q.clone(), dout.clone()
+    later = torch.zeros(n, dtype=torch.bool)
+    for s, length in enumerate(lens):
+        row = int(o[s]) + length // 4 + 2
+        odd_q[row, 0], odd_dout[row, 0] = math.nan, math.inf
+        q[row, 0], dout[row, 0] = 0, 0  # what the oracle has there does not matter after it
+        later[row + 1:int(o[s + 1])] = True
+    plan = ps.AttentionPlan(o, heads=heads, kv_heads=kv_heads, head_dim=d, dtype=dt, causal=True,
+                            num_buckets=buckets, max_distance=30 if buckets else 0)
+    b = None if bias is None else bias.cuda()
+    out, lse = plan.forward(odd_q.cuda(), k.cuda(), v.cuda(), bias=b)
+    _, dk, dv, _ = plan.backward(odd_dout.cuda(), odd_q.cuda(), k.cuda(), v.cuda(), out, lse, bias=b)
+    val, tol = attention(q, k, v, o, o, True, bias=bias, distance=30, dout=dout)
+    check("dk", dk.cpu()[later], val["dk"][later], tol["dk"][later])
+    check("dv", dv.cpu()[later], val["dv"][later], tol["dv"][later])
+    # and what sees it shows it
+    assert not torch.isfinite(dk.cpu()[int(o[0]) + lens[0] // 4 + 2, 0]).all()
+    assert not torch.isfinite(dv.cpu()[int(o[0]) + lens[0] // 4 + 2, 0]).any()
