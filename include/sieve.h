@@ -390,7 +390,9 @@ SIEVE_API int64_t sieve_norm_workspace(int64_t rows, int32_t n);
  * A query head h reads key head h / (heads / kv_heads).
  *   score = scale * <q_i, k_j> + bias[bucket(j - position of i)][h]
  *   out_i = sum over the keys j that i sees of softmax(score)_j v_j
- * A key is seen unless key_mask leaves it out or, with causal, it lies after the
+ * A bias counts within +-2^20 (fp32 keeps nothing of a score that is added to more), and one
+ * of -infinity forbids its bucket.
+ * A key is seen unless key_mask or the bias leaves it out or, with causal, it lies after the
  * query's position.  A query that sees no key gets out = 0 and lse = -infinity, and
  * gives no gradient.  What keys and values hold where key_mask leaves them out is not
  * used, infinities and NaN included, and their gradients are 0.  With causal, what they

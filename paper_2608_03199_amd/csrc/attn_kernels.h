@@ -429,6 +429,16 @@ __device__ __forceinline__ void store_row(T* p, const f32x16 (&x)[DP / 32], floa
   }
 }
 
+// A bias in units of log2, held to +-2^20: past that fp32 keeps nothing of the score it is added
+// to, the backward pass could not tell a row's probabilities from its lse, and the lowest values
+// of fp32 and bfloat16 would become -infinity.  -infinity itself forbids; NaN stays.
+__device__ __forceinline__ float held_bias(float b) {
+  constexpr float kMost = 0x1p20f;
+  if (b < -kMost && b > -INFINITY) b = -kMost;
+  if (b > kMost && b < INFINITY) b = kMost;
+  return b * kLog2e;
+}
+
 // The group's bias tables into LDS, times log2(e): s[g * span + entry].  The first entries'
 // buckets and values are loaded side by side; the values change places within the wave where
 // there are at most 64 of them.
@@ -438,7 +448,7 @@ __device__ __forceinline__ void load_bias(const AttnArgs& a, int kvh, float* s) 
   if (a.nb <= 64) {
     const int lane = threadIdx.x & 63;
     for (int g = 0; g < a.G; ++g) {
-      const float mine = lane < a.nb ? (float)bias[(int64_t)lane * a.heads + g] * kLog2e : 0.f;
+      const float mine = lane < a.nb ? held_bias((float)bias[(int64_t)lane * a.heads + g]) : 0.f;
       for (int i = threadIdx.x; i - lane < a.span; i += kAttnThreads) {
         const int bucket = i < a.span ? a.bucket_of[i] : 0;
         const float v = __shfl(mine, bucket);
@@ -449,7 +459,7 @@ __device__ __forceinline__ void load_bias(const AttnArgs& a, int kvh, float* s) 
   }
   for (int g = 0; g < a.G; ++g)
     for (int i = threadIdx.x; i < a.span; i += kAttnThreads)
-      s[g * a.span + i] = (float)bias[(int64_t)a.bucket_of[i] * a.heads + g] * kLog2e;
+      s[g * a.span + i] = held_bias((float)bias[(int64_t)a.bucket_of[i] * a.heads + g]);
 }
 
 // Not 0: the key is in the item's range and not masked.  Loaded a tile ahead.

@@ -85,3 +85,50 @@ def test_attention_causal_earlier_rows_do_not_reach_later_keys(ps, dtype, lens, 
     # and what sees it shows it
     assert not torch.isfinite(dk.cpu()[int(o[0]) + lens[0] // 4 + 2, 0]).all()
     assert not torch.isfinite(dv.cpu()[int(o[0]) + lens[0] // 4 + 2, 0]).any()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("value", ["lowest", -1e30, -1e9, -3e6, 1e9, "largest"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_bias_far_from_the_scores(ps, dtype, value, causal):
+    """A row all of whose keys have a bias of the type's lowest value, or one that fp32 cannot add
+    scores to: as with the limit that the bias is held to, in both passes."""
+    dt, rnd = DTYPES[dtype], _rnd(33)
+    info = torch.finfo(dt)
+    value = info.min if value == "lowest" else info.max if value == "largest" else value
+    value = max(info.min, min(info.max, value))
+    o = _offsets([60, 200])
+    q, k, v = rnd(260, 2, 32).to(dt), rnd(260, 2, 32).to(dt), rnd(260, 2, 32).to(dt)
+    dout = rnd(260, 2, 32).to(dt)
+    bias = rnd(8, 2).to(dt)
+    bias[:, 1] = value  # every key of head 1
+    held = bias.double().clamp(-2.0 ** 20, 2.0 ** 20)
+    plan = ps.AttentionPlan(o, heads=2, head_dim=32, dtype=dt, causal=causal, num_buckets=8,
+                            max_distance=30)
+    out, lse = plan.forward(q.cuda(), k.cuda(), v.cuda(), bias=bias.cuda())
+    grads = plan.backward(dout.cuda(), q.cuda(), k.cuda(), v.cuda(), out, lse, bias=bias.cuda())
+    val, tol = attention(q, k, v, o, o, causal, bias=held, distance=30, dout=dout)
+    for name, got in zip(("out", "dq", "dk", "dv", "dbias", "lse"), (out, *grads, lse)):
+        check(name, got, val[name], tol[name])
+    # head 0 is none of it
+    val, tol = attention(q[:, :1], k[:, :1], v[:, :1], o, o, causal, bias=bias[:, :1], distance=30,
+                         dout=dout[:, :1])
+    for name, got in zip(("out", "dq", "dk", "dv"), (out,) + tuple(grads[:3])):
+        check(name, got[:, :1], val[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("buckets, distance", [(8, 30), (128, 40)])
+def test_attention_bias_that_is_not_a_number(ps, dtype, buckets, distance):
+    """The limit of a bias leaves NaN, and -infinity forbids as before; the lowest value does not."""
+    dt, rnd = DTYPES[dtype], _rnd(34)
+    q = rnd(50, 4, 32).to(dt).cuda()
+    bias = rnd(buckets, 4).to(dt)
+    bias[:, 1], bias[:, 2], bias[:, 3] = math.nan, -math.inf, torch.finfo(dt).min
+    plan = ps.AttentionPlan([0, 50], heads=4, head_dim=32, dtype=dt, num_buckets=buckets,
+                            max_distance=distance)
+    out, lse = plan.forward(q, q, q, bias=bias.cuda())
+    assert torch.isfinite(out[:, 0]).all() and torch.isnan(out[:, 1]).all()
+    assert not out[:, 2].any() and torch.isneginf(lse[:, 2]).all()
+    assert torch.isfinite(out[:, 3]).all() and out[:, 3].any(1).all()
+    assert (lse[:, 3] + 2.0 ** 20).abs().max() < 64
