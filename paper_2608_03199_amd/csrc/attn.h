@@ -8,7 +8,6 @@
 
 namespace sieve {
 
-constexpr int kAttnThreads = 256;
 constexpr int kAttnStats = 3;  // of a partial row: maximum, sum of the probabilities as the
                                // second product takes them, and as they were before rounding
 

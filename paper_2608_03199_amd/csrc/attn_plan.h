@@ -47,7 +47,9 @@ constexpr int kAttnKeys = 128;    // keys of a dk and dv tile
 constexpr int kXcds = 8;
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - (int64_t(1) << 16);  // of a sequence
 constexpr int64_t kMaxTokens = int64_t(1) << 40;                       // of a batch
-constexpr int64_t kMaxItems = int64_t(1) << 25;                        // of a list, uncut
+// Items of a list: work-groups of a launch, which may have fewer than 2^32 threads.
+constexpr int kAttnThreads = 256;
+constexpr int64_t kMaxItems = ((int64_t(1) << 32) - 1) / kAttnThreads;
 // A forward pass with fewer items than this shares the keys of its row tiles out, at least
 // kMinKeys to an item (below that the joining costs more than the reading).  bf16, 16 heads
 // over 4 of 128: one query over 20,000 keys 31 us, not shared out 207; one query over 32
@@ -147,20 +149,39 @@ struct AttnLists {
   std::vector<AttnJoin> joins, kv_joins;
 };
 
+// Sizes of a batch's lists before they are shared out (which only adds to short ones).
+struct AttnCounts {
+  bool few;               // AttnLists::few
+  int64_t fwd, dq, dkv;   // items
+};
+inline AttnCounts count_items(const int64_t* qo, const int64_t* ko, int64_t nseq, int kv_heads,
+                              int G) {
+  int64_t most_rows = 0, rows128 = 0, rows32 = 0, keys = 0;
+  for (int64_t s = 0; s < nseq; ++s) {
+    const int64_t rows = (qo[s + 1] - qo[s]) * G;
+    most_rows = std::max(most_rows, rows);
+    rows128 += (rows + kAttnRows - 1) / kAttnRows;
+    rows32 += (rows + kAttnFewRows - 1) / kAttnFewRows;
+    keys += (ko[s + 1] - ko[s] + kAttnKeys - 1) / kAttnKeys;
+  }
+  const bool few = most_rows <= kAttnFewRows;
+  return {few, (few ? rows32 : rows128) * kv_heads, rows128 * kv_heads, keys * kv_heads};
+}
+
+// Whether each list fits a launch; that of dK and dV has a work-group more for each head, for
+// the bias's gradient.
+inline bool lists_fit(const AttnCounts& n, int64_t heads) {
+  return n.fwd <= kMaxItems && n.dq <= kMaxItems && n.dkv + heads <= kMaxItems;
+}
+
 // The items of a batch: qo and ko are nseq + 1 offsets each, G query heads to a key head.
 // False where there are too many.
 inline bool make_lists(const int64_t* qo, const int64_t* ko, int64_t nseq, int kv_heads, int G,
                        bool causal, AttnLists* out) {
   AttnLists& p = *out;
-  int64_t most_rows = 0, row_tiles = 0;
-  for (int64_t s = 0; s < nseq; ++s) {
-    const int64_t rows = (qo[s + 1] - qo[s]) * G;
-    most_rows = std::max(most_rows, rows);
-    row_tiles += (rows + kAttnFewRows - 1) / kAttnFewRows;  // at most
-  }
-  p.few = most_rows <= kAttnFewRows;
-  const int64_t key_tiles = (nseq ? ko[nseq] : 0) / kAttnKeys + nseq;
-  if (row_tiles > kMaxItems / kv_heads || key_tiles > kMaxItems / kv_heads) return false;
+  const AttnCounts counts = count_items(qo, ko, nseq, kv_heads, G);
+  if (!lists_fit(counts, (int64_t)kv_heads * G)) return false;
+  p.few = counts.few;
   const int tile = p.few ? kAttnFewRows : kAttnRows;
   int32_t tile0 = 0;
   for (int64_t s = 0; s < nseq; ++s) {
