@@ -235,6 +235,7 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps, residual):
         y, h, mean, rstd = layer_norm_forward(x, weight, bias, eps, residual)
+        ctx.set_materialize_grads(False)  # an output that nothing uses has no gradient
         ctx.save_for_backward(h, weight, mean, rstd)
         ctx.has_bias, ctx.has_residual = bias is not None, residual is not None
         if ctx.has_residual:
@@ -245,10 +246,13 @@ class _LayerNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy, dh=None):
         h, weight, mean, rstd = ctx.saved_tensors
-        if dy is None:
-            dy = torch.zeros_like(h)
-        dx, dw, db = layer_norm_backward(dy, h, weight, mean, rstd, dh, ctx.needs_input_grad[1],
-                                         ctx.has_bias and ctx.needs_input_grad[2])
+        want_w, want_b = ctx.needs_input_grad[1], ctx.has_bias and ctx.needs_input_grad[2]
+        if dy is None:  # only the sum was used
+            dx = dh
+            dw = torch.zeros_like(weight) if want_w else None
+            db = torch.zeros_like(weight) if want_b else None
+        else:
+            dx, dw, db = layer_norm_backward(dy, h, weight, mean, rstd, dh, want_w, want_b)
         return dx, dw, db, None, dx if ctx.has_residual else None
 
 
