@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "attn.h"
+#include "once_per_device.h"
 
 namespace sieve {
 namespace {
@@ -1814,10 +1815,16 @@ constexpr int kMaxLds = 160 * 1024;
 template <void (*kKernel)(AttnArgs)>
 hipError_t launch(const AttnArgs& a, int grid, size_t lds, hipStream_t s) {
   if (lds > kMaxLds) return hipErrorInvalidValue;
-  if (lds > 64 * 1024) {  // more has to be asked for, once for each kernel
-    static const hipError_t asked = hipFuncSetAttribute(
-        (const void*)kKernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
-    if (asked != hipSuccess) return asked;
+  if (lds > 64 * 1024) {  // more has to be asked for, once for each kernel and device
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    e = once_per_device(done, device, [] {
+      return hipFuncSetAttribute((const void*)kKernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                 kMaxLds);
+    });
+    if (e != hipSuccess) return e;
   }
   kKernel<<<grid, kAttnThreads, lds, s>>>(a);
   return hipGetLastError();

@@ -66,3 +66,33 @@ int main() {
 def test_lists_that_no_launch_takes_are_refused(tmp_path):
     """Before any part of them runs: a plan's lists are launched one work-group an item."""
     _run(tmp_path, "fit", FIT)
+
+
+DEVICES = r'''
+#include <stdio.h>
+#include "once_per_device.h"
+using namespace sieve;
+#define NEED(x) do { if (!(x)) { printf("failed: %s (line %d)\n", #x, __LINE__); return 1; } } while (0)
+int main() {
+  std::atomic<uint64_t> done{0};
+  int calls = 0, answer = 0;
+  auto ask = [&] { ++calls; return answer; };
+  NEED(once_per_device(done, 0, ask) == 0 && calls == 1);
+  NEED(once_per_device(done, 0, ask) == 0 && calls == 1);  // known
+  NEED(once_per_device(done, 1, ask) == 0 && calls == 2);  // another device
+  NEED(once_per_device(done, 63, ask) == 0 && calls == 3);
+  answer = 5;
+  NEED(once_per_device(done, 2, ask) == 5 && calls == 4);  // a failure is not remembered
+  answer = 0;
+  NEED(once_per_device(done, 2, ask) == 0 && calls == 5);
+  NEED(once_per_device(done, 2, ask) == 0 && calls == 5);
+  NEED(once_per_device(done, 64, ask) == 0 && once_per_device(done, 64, ask) == 0 && calls == 7);
+  printf("ok\n");
+}
+'''
+
+
+def test_large_lds_is_asked_for_on_every_device(tmp_path):
+    """A process may have plans on several devices; what one was asked for does not hold for
+    another."""
+    _run(tmp_path, "devices", DEVICES)
