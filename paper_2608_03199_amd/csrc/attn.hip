@@ -20,7 +20,7 @@ struct sieve_attn {
   int32_t nb = 0, distance = 0, span = 0;
   float scale = 0.f;
   int64_t queries = 0, keys = 0;
-  bool few = false;          // every tile of rows has at most kAttnFewRows
+  bool few = false;          // forward tiles are of kAttnFewRows rows
   int32_t row_tiles = 0;     // dq tiles of one key head
   int32_t parts = 0;         // partial results of the forward pass
   int32_t kv_parts = 0;      // partial results of dk and dv

@@ -39,9 +39,17 @@ struct AttnJoin {
 
 constexpr int kAttnPad = 64;      // relative positions past the distance in the bias table
 constexpr int kAttnRows = 128;    // rows of a tile: 4 waves of 32
-// Rows of a tile whose 4 waves share the keys out, where no sequence has more.  One query over 32
-// documents of 1,000..30,000 (16 heads over 4 of 128, bf16): 227 us, with tiles of 128 rows 247.
+// Rows of a tile whose 4 waves share the keys out, where no sequence has more and one has more
+// than kAttnFewKeys keys.  One query over 32 documents of 1,000..30,000 (16 heads over 4 of 128,
+// bf16): 227 us, with tiles of 128 rows 247; over 8 documents of 512 10.1, not 14.8; over 512 of
+// 2,048 (8 heads over 2 of 128, f32) 532, not 1,176.  Up to 64 keys the waves have nothing to
+// share: 512 documents of 4..32 tokens (12 heads of 64, f16) 27 us with tiles of 128 rows, with
+// these 55; 512 queries over 64 keys each 10.1 and 18.9 (16 over 4 of 64, f16), 72 and 152 (12 of
+// 64, f32), and in no case measured slower by more than 3%.  Between, it depends on the type and
+// how many there are: 512 queries over 512 keys each 108 and 137 (16 over 4 of 128, bf16), 309
+// and 169 (8 over 2 of 128, f32).
 constexpr int kAttnFewRows = 32;
+constexpr int kAttnFewKeys = 64;
 constexpr int kAttnKeys = 128;    // keys of a dk and dv tile
 
 constexpr int kXcds = 8;
@@ -142,7 +150,7 @@ void share_out(std::vector<AttnItem>& items, std::vector<AttnJoin>& joins, int w
 }
 
 struct AttnLists {
-  bool few = false;       // every sequence has at most kAttnFewRows rows for a key head
+  bool few = false;       // forward tiles are of kAttnFewRows rows (its comment)
   int32_t row_tiles = 0;  // dq tiles of one key head
   int32_t parts = 0, kv_parts = 0;  // partial results of the forward pass, and of dk and dv
   std::vector<AttnItem> fwd, dq, dkv;
@@ -156,15 +164,16 @@ struct AttnCounts {
 };
 inline AttnCounts count_items(const int64_t* qo, const int64_t* ko, int64_t nseq, int kv_heads,
                               int G) {
-  int64_t most_rows = 0, rows128 = 0, rows32 = 0, keys = 0;
+  int64_t most_rows = 0, most_keys = 0, rows128 = 0, rows32 = 0, keys = 0;
   for (int64_t s = 0; s < nseq; ++s) {
     const int64_t rows = (qo[s + 1] - qo[s]) * G;
     most_rows = std::max(most_rows, rows);
+    most_keys = std::max(most_keys, ko[s + 1] - ko[s]);
     rows128 += (rows + kAttnRows - 1) / kAttnRows;
     rows32 += (rows + kAttnFewRows - 1) / kAttnFewRows;
     keys += (ko[s + 1] - ko[s] + kAttnKeys - 1) / kAttnKeys;
   }
-  const bool few = most_rows <= kAttnFewRows;
+  const bool few = most_rows <= kAttnFewRows && most_keys > kAttnFewKeys;
   return {few, (few ? rows32 : rows128) * kv_heads, rows128 * kv_heads, keys * kv_heads};
 }
 

@@ -96,3 +96,29 @@ def test_large_lds_is_asked_for_on_every_device(tmp_path):
     """A process may have plans on several devices; what one was asked for does not hold for
     another."""
     _run(tmp_path, "devices", DEVICES)
+
+
+FEW = r'''
+#include <stdio.h>
+#include "attn_plan.h"
+using namespace sieve;
+#define NEED(x) do { if (!(x)) { printf("failed: %s (line %d)\n", #x, __LINE__); return 1; } } while (0)
+static bool few(int64_t rows, int64_t keys, int G) {
+  const std::vector<int64_t> qo{0, rows, 2 * rows}, ko{0, 1, 1 + keys};
+  AttnLists p;
+  if (!make_lists(qo.data(), ko.data(), 2, 2, G, false, &p)) return false;
+  return p.few;
+}
+int main() {
+  NEED(!few(32, 32, 1) && !few(1, 64, 1) && !few(1, 64, 8));  // short texts, short contexts
+  NEED(few(1, 65, 1) && few(32, 65, 1) && few(4, 20000, 8));
+  NEED(!few(33, 20000, 1) && !few(5, 20000, 8));              // rows: queries times their group
+  printf("ok\n");
+}
+'''
+
+
+def test_waves_share_keys_only_where_there_are_some(tmp_path):
+    """Tiles of few rows share the keys among four waves: a batch of short texts has none to
+    share, whatever its rows."""
+    _run(tmp_path, "few", FEW)
