@@ -14,12 +14,12 @@ constexpr int kAttnStats = 3;  // of a partial row: maximum, sum of the probabil
 struct AttnArgs {
   const AttnItem* items;
   const AttnJoin* joins;
-  int32_t nitems, njoins;
+  int32_t nitems;
   sieve_heads q, k, v, o, dout, dq, dk, dv;
   const uint8_t* key_mask;
   const void* bias;
   float* lse;        // written by the forward pass, read by the backward pass
-  int32_t G, heads, kv_heads, d, causal;
+  int32_t G, heads, d, causal;
   uint32_t g_mul;    // division by G (query_of in attn_kernels.h)
   int32_t g_shift;
   int32_t vec;       // every row may be moved in 16-byte pieces, at offsets of 32 bits from

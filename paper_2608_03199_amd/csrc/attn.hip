@@ -36,7 +36,9 @@ namespace {
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 
 int check_desc(const sieve_attn_desc& c) {
-  if (!enc_dtype_ok(c.dtype)) return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16", c.dtype);
+  if (!enc_dtype_ok(c.dtype))
+    return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16",
+                     c.dtype);
   if (c.heads < 1 || c.kv_heads < 1 || c.heads % c.kv_heads)
     return set_error(SIEVE_EINVAL, "heads = %d must be a multiple of kv_heads = %d", c.heads,
                      c.kv_heads);
@@ -216,7 +218,6 @@ AttnArgs common_args(const sieve_attn* p, const uint8_t* key_mask, const void* b
   while ((int64_t(1) << a.g_shift) < a.G) ++a.g_shift;
   a.g_mul = (uint32_t)(((uint64_t(1) << (31 + a.g_shift)) + a.G - 1) / a.G);
   a.heads = p->heads;
-  a.kv_heads = p->kv_heads;
   a.d = p->d;
   a.causal = p->causal;
   a.scale = p->scale;
@@ -306,7 +307,6 @@ SIEVE_API int sieve_attn_forward(const sieve_attn* plan, const sieve_heads* q,
   a.items = p->fwd;
   a.joins = p->joins;
   a.nitems = p->nfwd;
-  a.njoins = p->njoins;
   hipStream_t s = (hipStream_t)stream;
   ENC_HIP_TRY(launch(p, p->few ? kAttnFwdFew : kAttnFwd, a, p->nfwd, s));
   ENC_HIP_TRY(launch(p, p->few ? kAttnJoinFew : kAttnJoin, a, p->njoins, s));
@@ -373,7 +373,6 @@ SIEVE_API int sieve_attn_backward(const sieve_attn* plan, const sieve_heads* dou
   a.nitems = p->ndkv;
   ENC_HIP_TRY(launch(p, kAttnDkv, a, p->ndkv + (dbias ? p->heads : 0), s));
   a.joins = p->kv_joins;
-  a.njoins = p->nkv_joins;
   ENC_HIP_TRY(launch(p, kAttnDkvJoin, a, p->nkv_joins, s));
   return SIEVE_OK;
 }

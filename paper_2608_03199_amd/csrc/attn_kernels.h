@@ -68,10 +68,11 @@ __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
   return c;
 }
 
-// An LDS tile has rows of kPitch values: DP, or the next power of two.  Piece c (16 bytes) of row r lies at piece
-// c ^ piece_of(r) of the row.  64 banks of 4 bytes hold 16 pieces: a row (or two, or four of
-// the shorter ones).  Along the head (32 rows, one piece of each) and across the rows (4 rows
-// by 2 or 4 neighbouring pieces, twice) every 16 pieces then fall on 16 different places.
+// An LDS tile has rows of kPitch values: DP, or the next power of two.  Piece c (16 bytes) of
+// row r lies at piece c ^ piece_of(r) of the row.  64 banks of 4 bytes hold 16 pieces: a row (or
+// two, or four of the shorter ones).  Along the head (32 rows, one piece of each) and across the
+// rows (4 rows by 2 or 4 neighbouring pieces, twice) every 16 pieces then fall on 16 different
+// places.
 template <int DP>
 constexpr int kPitch = DP == 96 ? 128 : DP;
 
@@ -116,7 +117,8 @@ __device__ __forceinline__ lds_addr lane_across(int lane) {
     return row * kPitch<DP> * 2 + (piece ^ piece_of<T, DP>(row)) * 16 + (i & 1) * 8;
   } else {
     // rows 4 h + 0..3: the row's number within 4 changes piece_of by a constant
-    return 4 * h * kPitch<DP> * 4 + ((lane & 31) / 4 ^ piece_of<T, DP>(4 * h)) * 16 + (lane & 3) * 4;
+    return 4 * h * kPitch<DP> * 4 + ((lane & 31) / 4 ^ piece_of<T, DP>(4 * h)) * 16 +
+           (lane & 3) * 4;
   }
 }
 
@@ -174,8 +176,8 @@ __device__ __forceinline__ vec8<T> frag_across(lds_addr at, int row0, int col) {
     } u;
     // 8 rows on, piece_of differs in bit 1
     u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ x) + add));
-    u.half[1] =
-        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ x ^ 32) + add + 8 * kRow));
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4*)(uintptr_t)((at ^ x ^ 32) + add + 8 * kRow));
     return u.all;
   } else {
     vec8<T> r;
@@ -530,7 +532,6 @@ __device__ __forceinline__ LaneRow lane_row(const AttnArgs& a, const AttnItem& i
   return x;
 }
 
-
 // The running maximum may lag by kLag powers of two before the sums are brought to a new one,
 // and P is 2^kShift at it.  For binary16, 2^(kLag + kShift) has to stay below 65504 and what
 // 2^kShift pushes below 2^-14 loses bits.  2 x 8,192 tokens of 16 heads of 128, bf16: 1,054 us,
@@ -725,6 +726,10 @@ __device__ void careful_key(const AttnArgs& a, const AttnItem& it, const float* 
   }
 }
 
+// Work-groups a CU that a kernel's registers are to leave room for.
+template <typename T, int DP>
+constexpr int kGroupsPerCu = sizeof(T) * DP > 256 ? 1 : 2;
+
 // ---- forward ----------------------------------------------------------------------------
 // WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
 // each wave takes every fourth block of 32 keys, and LDS joins the four at the end: for
@@ -748,7 +753,8 @@ struct FwdShape {
 };
 
 template <typename T, int DP, int WK, bool kBias, bool kVec>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_forward_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (kGroupsPerCu<T, DP>)) void attn_forward_kernel(
+    AttnArgs a) {
   using Shape = FwdShape<T, DP, WK>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
   constexpr int kTileN = kTile * kPitch<DP>;
@@ -1118,7 +1124,8 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 template <typename T, int DP, bool kBias, bool kVec>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dq_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (kGroupsPerCu<T, DP>)) void attn_dq_kernel(
+    AttnArgs a) {
   using Shape = DqShape<T, DP, kBias>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
   constexpr int kTileN = kTile * kPitch<DP>;
@@ -1142,7 +1149,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const T* k0 = (const T*)a.k.data + it.k0 * a.k.token_stride + it.kvh * a.k.head_stride;
   const T* v0 = (const T*)a.v.data + it.k0 * a.v.token_stride + it.kvh * a.v.head_stride;
   const uint8_t* mask = a.key_mask ? a.key_mask + it.k0 : nullptr;
-  KeyStage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2> stage;
+  KeyStage<T, DP, kTile, kVec, kVec> stage;
   stage.place(a);
   uint8_t ok[kBlocks];
   auto fetch = [&](int base, int b) {
@@ -1234,7 +1241,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
       any |= bits[b];
     }
     const bool more = base + kTile < it.hi;
-    if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
+    if (more) fetch(base + kTile, buf ^ 1);
     if (wave_live && __any(any != 0)) {
       const lds_addr sk = k_al + buf * kTileN * (int)sizeof(T);
       const lds_addr sv = sk + (lds_addr)((s_v - s_k) * sizeof(T));
@@ -1321,9 +1328,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         }
       }
     }
-    if (Shape::kBufs == 1) __syncthreads();
     if (more) {
-      buf ^= Shape::kBufs - 1;
+      buf ^= 1;
       stage.store(mask, s_k + buf * kTileN, s_v + buf * kTileN);
       __syncthreads();
     }
@@ -1342,8 +1348,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
     }
   } else if (me.live)
     store_row<T, DP, kVec>((T*)a.dq.data + row_at(a, a.dq, it, me.r), dq,
-                           a.scale / up * kUpOut, d,
-                     h);
+                           a.scale / up * kUpOut, d, h);
   if constexpr (kScaled) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
@@ -1448,8 +1453,8 @@ __device__ __forceinline__ void reduce_bias(const AttnArgs& a, int head, float* 
   const int groups = kAttnThreads / wide, b = threadIdx.x % wide, g = threadIdx.x / wide;
   const int kvh = head / a.G;
   typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const f32x2* p = (const f32x2*)(a.part_bias +
-                                  ((int64_t)kvh * a.row_tiles * a.G + (head - kvh * a.G)) * a.nb) + b;
+  const int64_t first = (int64_t)kvh * a.row_tiles * a.G + (head - kvh * a.G);
+  const f32x2* p = (const f32x2*)(a.part_bias + first * a.nb) + b;
   const int64_t step = (int64_t)a.G * a.nb / 2;
   f32x2 t = {};
   if (2 * b < a.nb) {
@@ -1467,7 +1472,8 @@ __device__ __forceinline__ void reduce_bias(const AttnArgs& a, int head, float* 
 }
 
 template <typename T, int DP, bool kBias, bool kVec>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (kGroupsPerCu<T, DP>)) void attn_dkv_kernel(
+    AttnArgs a) {
   using Shape = DkvShape<T, DP>;
   constexpr int kBlocks = Shape::kBlocks, kTile = Shape::kTile;
   constexpr int kTileN = kTile * kPitch<DP>;
@@ -1483,7 +1489,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   }
   T* s_q = (T*)(smem + Shape::kValueBytes);
   T* s_do = s_q + Shape::kBufs * kTileN;
-  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);  // [buf][the row's exponent, -D, table offset, pos][row]
+  // [buf][the row's exponent, -D, table offset, pos][row]
+  float* s_row = (float*)(s_do + Shape::kBufs * kTileN);
   int* s_odd = (int*)(smem + Shape::kBytes - Shape::kOddBytes);  // [buf]
   float* s_bias = (float*)(smem + Shape::kBytes);
   const AttnItem it = a.items[blockIdx.x - reducers];
@@ -1496,7 +1503,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   const bool live = there && (!a.key_mask || a.key_mask[it.k0 + key] != 0);
 
   // Rows that saw no key are zeros whatever they hold: their lse tells, loaded with them.
-  using Tile = Stage<T, DP, kTile, kVec, kVec && Shape::kBufs == 2>;
+  using Tile = Stage<T, DP, kTile, kVec, kVec>;
   Tile st_q, st_do;
   constexpr int kN = Tile::kN;
   float piece_lse[kN], row_lse = 0.f, row_d = 0.f;
@@ -1586,10 +1593,10 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   vec8<T> k[DP / 16], v[DP / 16];
   {
     const int64_t tok = it.k0 + (live ? key : 0);
-    load_frags<T, DP, kVec>((const T*)a.k.data + tok * a.k.token_stride + it.kvh * a.k.head_stride, live,
-                      d, h, k);
-    load_frags<T, DP, kVec>((const T*)a.v.data + tok * a.v.token_stride + it.kvh * a.v.head_stride, live,
-                      d, h, v);
+    const T* pk = (const T*)a.k.data + tok * a.k.token_stride + it.kvh * a.k.head_stride;
+    const T* pv = (const T*)a.v.data + tok * a.v.token_stride + it.kvh * a.v.head_stride;
+    load_frags<T, DP, kVec>(pk, live, d, h, k);
+    load_frags<T, DP, kVec>(pv, live, d, h, v);
 #pragma unroll
     for (int c = kKeptV; c < DP / 16; ++c) keep_frag<T>(kept, c - kKeptV, v[c]);
 #pragma unroll
@@ -1616,7 +1623,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
   __syncthreads();
   for (int base = it.lo; base < it.hi; base += kTile) {
     const bool more = base + kTile < it.hi;
-    if (more) fetch(base + kTile, buf ^ (Shape::kBufs - 1));
+    if (more) fetch(base + kTile, buf ^ 1);
     if (wave_live) {
       constexpr int kApart = Shape::kBufs * kTileN * (int)sizeof(T);  // s_do - s_q
       lds_addr sq = q_al + buf * kTileN * (int)sizeof(T);
@@ -1722,9 +1729,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) * DP > 256 ? 1 : 2) void at
         }
       }
     }
-    if (Shape::kBufs == 1) __syncthreads();
     if (more) {
-      buf ^= Shape::kBufs - 1;
+      buf ^= 1;
       put(buf);
       __syncthreads();
     }
@@ -1835,16 +1841,19 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
   const size_t table = kBias ? (size_t)a.G * a.span * sizeof(float) : 0;
   switch (kind) {
     case kAttnFwd:
-      return launch<attn_forward_kernel<T, DP, 1, kBias, kVec>>(a, grid, FwdShape<T, DP, 1>::kBytes + table, s);
+      return launch<attn_forward_kernel<T, DP, 1, kBias, kVec>>(
+          a, grid, FwdShape<T, DP, 1>::kBytes + table, s);
     case kAttnFwdFew:
-      return launch<attn_forward_kernel<T, DP, 4, kBias, kVec>>(a, grid, FwdShape<T, DP, 4>::kBytes + table, s);
+      return launch<attn_forward_kernel<T, DP, 4, kBias, kVec>>(
+          a, grid, FwdShape<T, DP, 4>::kBytes + table, s);
     case kAttnDq: {
-      const size_t sums =
-          a.dbias ? kAttnWaves * (table + kDiagWords * sizeof(float)) : 0;
-      return launch<attn_dq_kernel<T, DP, kBias, kVec>>(a, grid, DqShape<T, DP, kBias>::kBytes + table + sums, s);
+      const size_t sums = a.dbias ? kAttnWaves * (table + kDiagWords * sizeof(float)) : 0;
+      return launch<attn_dq_kernel<T, DP, kBias, kVec>>(
+          a, grid, DqShape<T, DP, kBias>::kBytes + table + sums, s);
     }
     case kAttnDkv:
-      return launch<attn_dkv_kernel<T, DP, kBias, kVec>>(a, grid, DkvShape<T, DP>::kBytes + table, s);
+      return launch<attn_dkv_kernel<T, DP, kBias, kVec>>(
+          a, grid, DkvShape<T, DP>::kBytes + table, s);
     default:
       return hipErrorInvalidValue;
   }
@@ -1852,11 +1861,14 @@ hipError_t launch_as(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) 
 
 template <typename T, int DP>
 hipError_t launch_dp(AttnKind kind, const AttnArgs& a, int grid, hipStream_t s) {
-  if (kind == kAttnDkvJoin) return launch<attn_dkv_join_kernel<T, DP>>(a, grid * kDkvJoinGroups, 0, s);
-  if (kind == kAttnJoin) return launch<attn_join_kernel<T, DP, kAttnRows>>(
-        a, grid * ((kAttnRows + kJoinRows<DP> - 1) / kJoinRows<DP>), 0, s);
-  if (kind == kAttnJoinFew) return launch<attn_join_kernel<T, DP, kAttnFewRows>>(
-        a, grid * ((kAttnFewRows + kJoinRows<DP> - 1) / kJoinRows<DP>), 0, s);
+  constexpr int kJoin = (kAttnRows + kJoinRows<DP> - 1) / kJoinRows<DP>;
+  constexpr int kJoinFew = (kAttnFewRows + kJoinRows<DP> - 1) / kJoinRows<DP>;
+  if (kind == kAttnDkvJoin)
+    return launch<attn_dkv_join_kernel<T, DP>>(a, grid * kDkvJoinGroups, 0, s);
+  if (kind == kAttnJoin)
+    return launch<attn_join_kernel<T, DP, kAttnRows>>(a, grid * kJoin, 0, s);
+  if (kind == kAttnJoinFew)
+    return launch<attn_join_kernel<T, DP, kAttnFewRows>>(a, grid * kJoinFew, 0, s);
   if (a.bias)
     return a.vec ? launch_as<T, DP, true, true>(kind, a, grid, s)
                  : launch_as<T, DP, true, false>(kind, a, grid, s);

@@ -8,9 +8,9 @@
 // Each value is read once and written once, so memory bounds every kernel here but the looping
 // ones.  65,536 x 1,024 bf16: forward 47 us, 5.7 TB/s; backward with its reduction 80 us, 5.0 TB/s.
 // A row stays in the registers of a quarter of a wave (up to 128 values), a wave (up to
-// 2,048) or a work-group (up to 8,192): the mean is taken first and the variance from the differences, in
-// fp32 without the cancellation of a sum of squares.  Longer rows are read again,
-// from the L2, by the looping kernels.
+// 2,048) or a work-group (up to 8,192): the mean is taken first and the variance from the
+// differences, in fp32 without the cancellation of a sum of squares.  Longer rows are read
+// again, from the L2, by the looping kernels.
 //
 // The weights' gradients: a thread owns the same columns of every row it takes, so it
 // sums them in registers; the work-group's rows add up through LDS,
@@ -506,7 +506,9 @@ void backward_typed(const NormBwd& a, bool vec, int groups, hipStream_t s) {
 }
 
 int check_norm(int32_t dtype, int32_t wdtype, int64_t rows, int32_t n) {
-  if (!enc_dtype_ok(dtype)) return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16", dtype);
+  if (!enc_dtype_ok(dtype))
+    return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16",
+                     dtype);
   if (wdtype != dtype && wdtype != SIEVE_F32)
     return set_error(SIEVE_EINVAL, "wdtype = %d must be dtype or SIEVE_F32", wdtype);
   if (rows < 0) return set_error(SIEVE_EINVAL, "rows is negative");
