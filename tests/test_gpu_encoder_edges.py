@@ -78,7 +78,8 @@ def test_attention_causal_earlier_rows_do_not_reach_later_keys(ps, dtype, lens, 
                             num_buckets=buckets, max_distance=30 if buckets else 0)
     b = None if bias is None else bias.cuda()
     out, lse = plan.forward(odd_q.cuda(), k.cuda(), v.cuda(), bias=b)
-    _, dk, dv, _ = plan.backward(odd_dout.cuda(), odd_q.cuda(), k.cuda(), v.cuda(), out, lse, bias=b)
+    _, dk, dv, _ = plan.backward(odd_dout.cuda(), odd_q.cuda(), k.cuda(), v.cuda(), out, lse,
+                                 bias=b)
     val, tol = attention(q, k, v, o, o, True, bias=bias, distance=30, dout=dout)
     check("dk", dk.cpu()[later], val["dk"][later], tol["dk"][later])
     check("dv", dv.cpu()[later], val["dv"][later], tol["dv"][later])
@@ -120,7 +121,8 @@ def test_attention_bias_far_from_the_scores(ps, dtype, value, causal):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("buckets, distance", [(8, 30), (128, 40)])
 def test_attention_bias_that_is_not_a_number(ps, dtype, buckets, distance):
-    """The limit of a bias leaves NaN, and -infinity forbids as before; the lowest value does not."""
+    """The limit of a bias leaves NaN, and -infinity forbids as before; the lowest value does
+    not."""
     dt, rnd = DTYPES[dtype], _rnd(34)
     q = rnd(50, 4, 32).to(dt).cuda()
     bias = rnd(buckets, 4).to(dt)
@@ -132,3 +134,26 @@ def test_attention_bias_that_is_not_a_number(ps, dtype, buckets, distance):
     assert not out[:, 2].any() and torch.isneginf(lse[:, 2]).all()
     assert torch.isfinite(out[:, 3]).all() and out[:, 3].any(1).all()
     assert (lse[:, 3] + 2.0 ** 20).abs().max() < 64
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("d", [64, 128, 40])
+def test_attention_few_causal_rows_before_odd_values(ps, dtype, d):
+    """The last queries of documents whose last key is not a number: those before it are as
+    without it, where waves share the keys of a tile and where work-groups do."""
+    dt, rnd = DTYPES[dtype], _rnd(35)
+    qo, ko = _offsets([3, 2, 5]), _offsets([300, 5000, 66])
+    q, dout = rnd(10, 4, d).to(dt), rnd(10, 4, d).to(dt)
+    k, v = rnd(5366, 2, d).to(dt), rnd(5366, 2, d).to(dt)
+    val, tol = attention(q, k, v, qo, ko, True, dout=dout)
+    odd_k, odd_v = k.clone(), v.clone()
+    last = ko[1:] - 1
+    odd_k[last], odd_v[last] = math.nan, math.inf
+    plan = ps.AttentionPlan(qo, ko, heads=4, kv_heads=2, head_dim=d, dtype=dt, causal=True)
+    out, lse = plan.forward(q.cuda(), odd_k.cuda(), odd_v.cuda())
+    dq = plan.backward(dout.cuda(), q.cuda(), odd_k.cuda(), odd_v.cuda(), out, lse)[0]
+    before = torch.ones(10, dtype=torch.bool)
+    before[qo[1:] - 1] = False
+    for name, got in (("out", out), ("lse", lse), ("dq", dq)):
+        check(name, got.cpu()[before], val[name][before], tol[name][before])
+    assert not torch.isfinite(out.cpu()[~before]).any()
