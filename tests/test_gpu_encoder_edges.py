@@ -157,3 +157,24 @@ def test_attention_few_causal_rows_before_odd_values(ps, dtype, d):
     for name, got in (("out", out), ("lse", lse), ("dq", dq)):
         check(name, got.cpu()[before], val[name][before], tol[name][before])
     assert not torch.isfinite(out.cpu()[~before]).any()
+
+
+def test_attention_gradient_probabilities_keep_32_bits(ps):
+    """The backward pass's probabilities in fp32, seen through dv: scores of 0 over n keys, an
+    output's gradient of 1, so that dv is the probability 1 / n.
+
+    What they are made of: lse in units of log2 (below 4), its product with ln 2 and back, each
+    rounded to nearest, half a unit of which is at most 2 E (E = 2^-24), a quarter on average, the
+    exponential and the result.  On average that is at most 3 E ln 2 + E, below 3.1 E.  A
+    statistic moved by a constant that makes it larger (by 24: 16 E, 5.5 E on average) is not."""
+    lens = [n for n in range(3, 16) if n & (n - 1)]
+    plan = ps.AttentionPlan(torch.arange(len(lens) + 1), _offsets(lens), heads=1, head_dim=4,
+                            dtype=torch.float32)
+    q, k = torch.zeros(len(lens), 1, 4).cuda(), torch.zeros(sum(lens), 1, 4).cuda()
+    v = torch.randn(sum(lens), 1, 4, generator=torch.Generator().manual_seed(36)).cuda()
+    out, lse = plan.forward(q, k, v)
+    dv = plan.backward(torch.ones_like(q), q, k, v, out, lse)[2]
+    n = torch.tensor([float(n) for n in lens for _ in range(n)], dtype=torch.float64)
+    off = (dv.double().cpu()[:, 0] * n[:, None] - 1).abs().amax(1)
+    per = torch.stack([x.max() for x in off.split(lens)])
+    assert float(per.mean()) < 3.1 * 2.0 ** -24
