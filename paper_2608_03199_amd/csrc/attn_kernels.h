@@ -1368,6 +1368,7 @@ __global__ __launch_bounds__(kAttnThreads, (kGroupsPerCu<T, DP>)) void attn_dq_k
     store_row<T, DP, kVec>((T*)a.dq.data + row_at(a, a.dq, it, me.r), dq,
                            a.scale / up * kUpOut, d, h);
   if constexpr (kScaled) {
+    if (!(most < INFINITY)) most = 0.f;  // such a row has no say in how the others are scaled
 #pragma unroll
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     float* s_max = (float*)smem;
@@ -1628,7 +1629,7 @@ __global__ __launch_bounds__(kAttnThreads, (kGroupsPerCu<T, DP>)) void attn_dkv_
     for (int i = lane; i < it.ntiles; i += 64) most = fmaxf(most, p[i]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    const int e = most > 0.f && most < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
+    const int e = most > 0.f ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
     up = __builtin_amdgcn_ldexpf(kUpPOut, e < 40 ? e : 40);
   }
   f32x16 dk[DP / 32], dv[DP / 32];

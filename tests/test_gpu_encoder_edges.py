@@ -178,3 +178,29 @@ def test_attention_gradient_probabilities_keep_32_bits(ps):
     off = (dv.double().cpu()[:, 0] * n[:, None] - 1).abs().amax(1)
     per = torch.stack([x.max() for x in off.split(lens)])
     assert float(per.mean()) < 3.1 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_small_half_precision_gradients_beside_an_infinite_one(ps, causal):
+    """binary16 scales dS by the largest of a sequence: a row whose dS is infinite is not it, so
+    that gradients of 1e-6 keep their relative precision where that row does not reach."""
+    rnd = _rnd(37)
+    o = _offsets([300, 40])
+    q, k, v = rnd(340, 2, 64).half(), rnd(340, 2, 64).half(), rnd(340, 2, 64).half()
+    dout = (rnd(340, 2, 64) * 1e-6).half()
+    dout[10, 0] = 0  # what the oracle has there does not matter past its reach
+    odd = dout.clone()
+    odd[10, 0, 0] = math.inf  # dP of that row is infinite of both signs, dS infinite or NaN
+    val, tol = attention(q, k, v, o, o, causal, dout=dout)
+    plan = ps.AttentionPlan(o, heads=2, head_dim=64, dtype=torch.float16, causal=causal)
+    out, lse = plan.forward(q.cuda(), k.cuda(), v.cuda())
+    dq, dk, dv, _ = plan.backward(odd.cuda(), q.cuda(), k.cuda(), v.cuda(), out, lse)
+    rows = torch.ones(340, dtype=torch.bool)
+    rows[10] = False
+    check("dq", dq.cpu()[rows], val["dq"][rows], tol["dq"][rows])
+    check("dq", dq.cpu()[:, 1], val["dq"][:, 1], tol["dq"][:, 1])
+    keys = torch.ones(340, dtype=torch.bool)
+    keys[:300 if not causal else 11] = False
+    for name, got in (("dk", dk), ("dv", dv)):
+        check(name, got.cpu()[keys], val[name][keys], tol[name][keys])
+        check(name, got.cpu()[:, 1], val[name][:, 1], tol[name][:, 1])
