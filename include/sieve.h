@@ -439,7 +439,8 @@ typedef struct sieve_attn sieve_attn; /* opaque, owned by the library */
  * calls on any streams may use it at once.  A sequence may have up to 2^31 - 2^16 rows
  * (queries times heads / kv_heads) and keys, a batch 2^40 tokens and by key head about 2^24
  * tiles of 128 rows (32 where no sequence has more) or keys (else SIEVE_EUNSUPPORTED).
- * sieve_attn_free waits for the device's work (as hipFree does).
+ * sieve_attn_free waits for the device's work (as hipFree does).  Neither may be called while
+ * a stream is being captured.
  */
 SIEVE_API int sieve_attn_create(const sieve_attn_desc* desc, void* stream, sieve_attn** out);
 SIEVE_API void sieve_attn_free(sieve_attn* plan);

@@ -24,7 +24,8 @@
 // end, are zeros there: what they hold never meets a product.
 //
 // P and dS are rounded to the inputs' type for the second products, as those run on the
-// 16-bit matrix units; S, dP, the statistics and every accumulator are fp32.  bfloat16
+// 16-bit matrix units; S, dP, the statistics (of P before it is rounded; only the output's
+// divisor is of P as the product takes it) and every accumulator are fp32.  bfloat16
 // keeps fp32's range.  binary16 does not, so there the values are scaled by powers of two
 // that the end takes out exactly: P by 2^11 at the running maximum (forward) or by 2^14
 // (dV, where P <= 1), and dS by what brings its largest magnitude to 2^13 .. 2^14.
@@ -734,10 +735,11 @@ constexpr int kGroupsPerCu = sizeof(T) * DP > 256 ? 1 : 2;
 // WK = 1: a wave takes 32 of the tile's 128 rows and all keys.  WK = 4: the tile is 32 rows,
 // each wave takes every fourth block of 32 keys, and LDS joins the four at the end: for
 // few rows, where the keys' and values' bytes bound the time.  Long sequences: matrix and
-// vector issue (matrix units 37-40% busy); 12,007 causal tokens, 16 heads over 4 of 128, bf16,
-// 690 us, 857 TFLOP/s.  Few rows: memory; one query over 32 documents of 1,000..30,000 222 us
-// with the join, 5.0 TB/s.  Tiles of 64 keys: with 32 the 12,007 tokens took 755 us against 670,
-// 4 x 8,192 of 12 heads of 64 977 against 926.
+// vector issue (matrix units 36-38% busy); 12,007 causal tokens, 16 heads over 4 of 128, bf16,
+// 718 us, 823 TFLOP/s (of it 28 us for the sum that lse is made from).  Few rows: memory; one
+// query over 32 documents of 1,000..30,000 224 us with the join, 4.9 TB/s.  Tiles of 64 keys:
+// with 32 the 12,007 tokens took 755 us against 670, 4 x 8,192 of 12 heads of 64 977 against 926
+// (before that sum).
 
 template <typename T, int DP, int WK>
 struct FwdShape {
@@ -1075,8 +1077,8 @@ __device__ __forceinline__ float exp2_up(float v) {
 // position p + i lies at a constant step from row i - 1's), and adds the result to its own
 // sums by position.  No atomics: the order of additions is the program's.
 //
-// Issue bounds it.  Two causal documents of 5,000..6,100 (16 heads over 4 of 128, bf16) 452 us;
-// 256 documents of 16..512 (12 heads of 64, f16) with a bias's gradient 365.  That gradient adds
+// Issue bounds it.  Two causal documents of 5,000..6,100 (16 heads over 4 of 128, bf16) 459 us;
+// 256 documents of 16..512 (12 heads of 64, f16) with a bias's gradient 371.  That gradient adds
 // 70 to 110 us to a backward pass of 552 to 560.
 //
 // dS is rounded to the inputs' type for the product and D comes from the rounded output: dQ and
@@ -1442,7 +1444,7 @@ __global__ __launch_bounds__(kAttnThreads, (kGroupsPerCu<T, DP>)) void attn_dq_k
 // them: all query heads of the group, so that the sum over a shared head is the accumulator's.
 // S = Q K^T puts rows 8 g + 4 h + t in registers 4 g + t.  The first `heads` work-groups of a
 // launch with a bias's gradient add up its partial sums instead.  Issue bounds it: the two
-// causal documents above 597 us (and 25 to join), the 256 documents 358.
+// causal documents above 647 us (and 25 to join), the 256 documents 368.
 
 template <typename T, int DP>
 struct DkvShape {
