@@ -479,6 +479,43 @@ SIEVE_API int sieve_attn_backward(const sieve_attn* plan, const sieve_heads* dou
                                   const sieve_heads* dv, void* dbias, void* workspace,
                                   int64_t workspace_bytes, void* stream);
 
+/*
+ * sieve_embed_forward -- rows of a table by token number, the encoder's input.
+ *   out[t] = scale * table[ids[t]], rounded to dtype once.
+ *   ids          [count] int32 or int64 (id_bytes 4 or 8).  A number that is not in
+ *                0 .. vocab-1 (padding, say -1) reads nothing: its row is zeros.
+ *   table        [vocab, n] of tdtype, which is dtype or SIEVE_F32, rows table_stride
+ *                values apart (>= n).
+ *   out          [count, n] of dtype, contiguous.
+ * 0 <= count <= 2^31-1, 1 <= vocab <= 2^31-2, 1 <= n <= 65536 (above these
+ * SIEVE_EUNSUPPORTED).
+ */
+SIEVE_API int sieve_embed_forward(const void* ids, int32_t id_bytes, int64_t count,
+                                  const void* table, int64_t table_stride, int32_t tdtype,
+                                  int64_t vocab, int32_t n, float scale, void* out, int32_t dtype,
+                                  void* stream);
+
+/*
+ * sieve_embed_backward -- the gradient of the table of sieve_embed_forward.
+ *   dtable[v] = scale * sum over the t with ids[t] = v of dy[t]
+ *   dy           [count, n] of dtype, rows dy_stride values apart (>= n).  Rows whose
+ *                number is not in the table are not used, whatever they hold.
+ *   accumulate   0: dtable is written whole, zeros in rows that no number names.
+ *                1: the sums are added to what dtable holds (a table that is also the
+ *                loss's), other rows are left as they are.
+ *   dtable       [vocab, n] of tdtype, which is dtype or SIEVE_F32, contiguous.
+ *   workspace    device memory of sieve_embed_workspace(count, vocab, n) bytes, 16-byte
+ *                aligned (only used in the call; may be NULL where count is 0).
+ * Sums are fp32 in an order that depends on the numbers alone.  Limits as above.
+ */
+SIEVE_API int sieve_embed_backward(const void* dy, int64_t dy_stride, int32_t dtype,
+                                   const void* ids, int32_t id_bytes, int64_t count, int64_t vocab,
+                                   int32_t n, float scale, int32_t accumulate, void* dtable,
+                                   int32_t tdtype, void* workspace, int64_t workspace_bytes,
+                                   void* stream);
+/* Bytes that sieve_embed_backward needs, or a negative sieve_status. */
+SIEVE_API int64_t sieve_embed_workspace(int64_t count, int64_t vocab, int32_t n);
+
 /* Release an index and its cached workspace.  NULL is a no-op. */
 SIEVE_API void sieve_free_index(sieve_index* idx);
 

@@ -1,0 +1,148 @@
+"""Operators of libsieve around a text encoder's blocks: the table's lookup with its gradient
+(``include/sieve.h``).
+
+As in ``encoder.py``, the ``*_forward`` / ``*_backward`` functions marshal the arguments of the
+library's calls, ``embed`` joins them for torch's autograd, all calls are asynchronous on the
+given or current stream, and there is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import _check
+from .encoder import _CODES, _code, _here, _need, _on, _ptr, _raw_stream, _rows, _workspace
+from .encoder import _library as _encoder_library
+
+__all__ = ["embed", "embed_backward", "embed_forward"]
+
+_ready = None
+
+
+def _library():
+    global _ready
+    if _ready is not None:
+        return _ready
+    lib = _encoder_library()
+    P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    lib.sieve_embed_forward.restype = ctypes.c_int
+    lib.sieve_embed_forward.argtypes = [P, i32, i64, P, i64, i32, i64, i32, f32, P, i32, P]
+    lib.sieve_embed_workspace.restype = i64
+    lib.sieve_embed_workspace.argtypes = [i64, i64, i32]
+    lib.sieve_embed_backward.restype = ctypes.c_int
+    lib.sieve_embed_backward.argtypes = [P, i64, i32, P, i32, i64, i64, i32, f32, i32, P, i32, P,
+                                         i64, P]
+    _ready = lib
+    return lib
+
+
+# ---- embedding ----------------------------------------------------------------------------
+
+_WHOLE = {torch.int32: 4, torch.int64: 8}
+
+
+def _numbers(t: torch.Tensor, name: str, device):
+    """Whole numbers of 4 or 8 bytes on the device, one after another, and their size."""
+    if t.dtype not in _WHOLE:
+        raise TypeError(f"{name} must be int32 or int64, not {t.dtype}")
+    _need(t.device == device, f"{name} must be on {device}")
+    return t.contiguous(), _WHOLE[t.dtype]
+
+
+def embed_forward(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
+                  dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """``scale * table[ids]`` as ``dtype`` (the table's, unless it is float32 and another is
+    asked for): [*ids.shape, n].  A number that is not in the table gives a row of zeros."""
+    _need(table.is_cuda, "table must be a GPU tensor")
+    if _here(table.device, stream):
+        return _embed_forward(ids, table, scale, dtype)
+    with _on(table.device, stream):
+        return _embed_forward(ids, table, scale, dtype)
+
+
+def _embed_forward(ids, table, scale, dtype):
+    _need(table.dim() == 2 and table.shape[0] >= 1 and table.shape[1] >= 1,
+          "table must be [vocab, n]")
+    dtype = table.dtype if dtype is None else dtype
+    tcode = _code(table, "table")
+    _check_pair(dtype, table.dtype)
+    lib = _library()
+    ids, size = _numbers(ids, "ids", table.device)
+    vocab, n = table.shape
+    tr, stride = _rows(table, n)
+    out = table.new_empty(ids.shape + (n,), dtype=dtype)
+    if ids.numel():
+        _check(lib, lib.sieve_embed_forward(ids.data_ptr(), size, ids.numel(), tr.data_ptr(),
+                                            stride, tcode, vocab, n, scale, out.data_ptr(),
+                                            _CODES[dtype], _raw_stream(table.device)))
+    return out
+
+
+def _check_pair(dtype, tdtype):
+    if dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {dtype} (float32, float16 or bfloat16)")
+    if tdtype not in (dtype, torch.float32):
+        raise TypeError("the table must be of the rows' dtype or float32")
+
+
+def embed_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0,
+                   dtype: Optional[torch.dtype] = None, into: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """The gradient [vocab, n] of ``embed_forward``'s table, of ``dtype`` (dy's, or float32).
+    ``into``: a gradient of the table that this one is added to, and returned (of a tied output
+    layer, say); rows that no number names are then left as they are."""
+    _need(dy.is_cuda, "dy must be a GPU tensor")
+    if _here(dy.device, stream):
+        return _embed_backward(dy, ids, vocab, scale, dtype, into)
+    with _on(dy.device, stream):
+        return _embed_backward(dy, ids, vocab, scale, dtype, into)
+
+
+def _embed_backward(dy, ids, vocab, scale, dtype, into):
+    shape = dy.shape
+    _need(len(shape) >= 1 and shape[-1] >= 1, "dy must have a last axis of at least one value")
+    n, vocab = shape[-1], int(vocab)
+    _need(ids.shape == shape[:-1], f"ids must be {list(shape[:-1])}")
+    _need(vocab >= 1, "vocab must be at least 1")
+    dtype = (dy.dtype if into is None else into.dtype) if dtype is None else dtype
+    code = _code(dy, "dy")
+    _check_pair(dy.dtype, dtype)
+    if into is not None:
+        _need(into.shape == (vocab, n) and into.dtype is dtype and into.device == dy.device and
+              into.is_contiguous(), f"into must be a contiguous [{vocab}, {n}] of {dtype} on "
+                                    f"dy's device")
+    lib = _library()
+    ids, size = _numbers(ids, "ids", dy.device)
+    dr, stride = _rows(dy, n)
+    count = ids.numel()
+    need = lib.sieve_embed_workspace(count, vocab, n)
+    space = _workspace(lib, need, dy.device)
+    out = dy.new_empty((vocab, n), dtype=dtype) if into is None else into
+    _check(lib, lib.sieve_embed_backward(_ptr(dr), stride, code, _ptr(ids), size, count, vocab, n,
+                                         scale, int(into is not None), out.data_ptr(),
+                                         _CODES[dtype], _ptr(space), need,
+                                         _raw_stream(dy.device)))
+    return out
+
+
+class _Embed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, table, scale, dtype):
+        ctx.save_for_backward(ids)
+        ctx.vocab, ctx.scale, ctx.dtype = table.shape[0], scale, table.dtype
+        return embed_forward(ids, table, scale, dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        return None, embed_backward(dy, ids, ctx.vocab, ctx.scale, ctx.dtype), None, None
+
+
+def embed(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
+          dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """Differentiable ``embed_forward``."""
+    return _Embed.apply(ids, table, scale, dtype)

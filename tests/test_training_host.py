@@ -1,0 +1,54 @@
+"""CPU-side checks of the operators around the encoder's blocks: argument errors before any HIP
+call, limits, workspaces."""
+import ctypes
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2608_03199_amd as ps
+    if not os.path.exists(ps.LIB_PATH):
+        from paper_2608_03199_amd import build
+        build.build()
+    from paper_2608_03199_amd import training
+    return training._library()
+
+
+P, NONE = ctypes.c_void_p(0x1000), None
+
+
+def test_embed_argument_errors_without_a_gpu(lib):
+    def forward(ids=P, size=8, count=4, table=P, stride=8, tdt=0, vocab=5, n=8, out=P, dt=0):
+        return lib.sieve_embed_forward(ids, size, count, table, stride, tdt, vocab, n, 1.0, out,
+                                       dt, NONE)
+
+    assert forward(dt=3) == -1 and b"dtype" in lib.sieve_last_error()
+    assert forward(tdt=1, dt=2) == -1 and b"tdtype" in lib.sieve_last_error()
+    assert forward(tdt=1, dt=0) == -1
+    assert forward(size=2) == -1 and b"id_bytes" in lib.sieve_last_error()
+    assert forward(count=-1) == -1 and forward(vocab=0) == -1 and forward(n=0) == -1
+    assert forward(n=65537, stride=65537) == -4
+    assert forward(count=1 << 31) == -4 and forward(vocab=(1 << 31) - 1) == -4
+    assert forward(ids=NONE) == -1 and forward(table=NONE) == -1 and forward(out=NONE) == -1
+    assert forward(stride=7) == -1 and b"stride" in lib.sieve_last_error()
+    assert forward(count=0, ids=NONE, out=NONE) == 0
+
+    def backward(dy=P, stride=8, dt=0, ids=P, size=8, count=4, vocab=5, n=8, acc=0, out=P, tdt=0,
+                 ws=P, bytes=1 << 30):
+        return lib.sieve_embed_backward(dy, stride, dt, ids, size, count, vocab, n, 1.0, acc, out,
+                                        tdt, ws, bytes, NONE)
+
+    assert backward(acc=2) == -1 and b"accumulate" in lib.sieve_last_error()
+    assert backward(out=NONE) == -1 and backward(dy=NONE) == -1 and backward(ids=NONE) == -1
+    assert backward(stride=7) == -1
+    assert backward(ws=NONE) == -1 and b"workspace" in lib.sieve_last_error()
+    assert backward(ws=ctypes.c_void_p(0x1008)) == -1 and backward(bytes=100) == -1
+    assert backward(count=0, acc=1, dy=NONE, ids=NONE, ws=NONE, bytes=0) == 0
+    assert lib.sieve_embed_workspace(0, 5, 8) == 0
+    assert lib.sieve_embed_workspace(4, 0, 8) == -1 and lib.sieve_embed_workspace(4, 5, 0) == -1
+    # two pairs of whole numbers a token, and a 1/31 of the batch's rows in fp32
+    assert 16 * 65536 < lib.sieve_embed_workspace(65536, 50000, 1024) < \
+        16 * 65536 + 65536 * 1024 * 4 // 31 + (1 << 20)
+    assert lib.sieve_embed_workspace((1 << 31) - 1, (1 << 31) - 2, 65536) > 0
