@@ -516,6 +516,54 @@ SIEVE_API int sieve_embed_backward(const void* dy, int64_t dy_stride, int32_t dt
 /* Bytes that sieve_embed_backward needs, or a negative sieve_status. */
 SIEVE_API int64_t sieve_embed_workspace(int64_t count, int64_t vocab, int32_t n);
 
+/*
+ * sieve_loss_forward -- softmax cross entropy of rows against a table of vectors, without
+ * keeping the logits: an encoder's output layer against its table, or, with scale = 1 /
+ * temperature, one half of a batch of pairs against the other.
+ *   s_tv = scale * h_t . table_v,  lse_t = log sum_v exp s_tv,  loss_t = lse_t - s_t,target
+ *   h            [rows, n] of dtype, rows h_stride values apart (>= n).
+ *   table        [vocab, n] of dtype, rows table_stride values apart (>= n).
+ *   targets      [rows] int32 or int64 (target_bytes 4 or 8).  A row whose target is not in
+ *                0 .. vocab-1 (say -100) is left out: its loss is 0, and it gives no gradient,
+ *                whatever it holds.
+ *   scale        > 0 and finite.
+ *   loss         [rows] fp32, or NULL; lse: [rows] fp32 (of every row).
+ *   workspace    device memory of sieve_loss_workspace(rows, vocab, n, dtype, 0) bytes,
+ *                16-byte aligned (only used in the call).
+ * Products are summed in fp32.  0 <= rows <= 2^24, 1 <= vocab <= 2^24, 1 <= n <= 65536 (above
+ * these SIEVE_EUNSUPPORTED).
+ */
+SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* table,
+                                 int64_t table_stride, int32_t dtype, int64_t rows, int64_t vocab,
+                                 int32_t n, const void* targets, int32_t target_bytes, float scale,
+                                 float* loss, float* lse, void* workspace, int64_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * sieve_loss_backward -- gradients of sieve_loss_forward.  With p_tv = exp(s_tv - lse_t) and
+ * g_tv = (p_tv - [v = target_t]) * dloss_t (rounded to dtype for the products),
+ *   dh_t = scale * sum_v g_tv table_v,  dtable_v = scale * sum_t g_tv h_t
+ *   dloss        [rows] fp32: the gradient of each row's loss.  A row with dloss = 0 is left
+ *                out, as one without a target is.
+ *   lse          [rows]: the forward pass's.
+ *   dh           NULL or [rows, n] of dtype, contiguous; zeros in rows that are left out.
+ *   dtable       NULL or [vocab, n] of dtype, contiguous.
+ *   workspace    device memory of sieve_loss_workspace(rows, vocab, n, dtype, 1) bytes,
+ *                16-byte aligned (only used in the call).
+ * rows = 0 writes zeros to dtable (no workspace is needed).  The gradient of scale is
+ * sum(dh * h) / scale.
+ */
+SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_stride,
+                                  const void* table, int64_t table_stride, int32_t dtype,
+                                  int64_t rows, int64_t vocab, int32_t n, const void* targets,
+                                  int32_t target_bytes, const float* lse, float scale, void* dh,
+                                  void* dtable, void* workspace, int64_t workspace_bytes,
+                                  void* stream);
+/* Bytes that the forward (backward = 0) or the backward pass (1) needs, or a negative
+ * sieve_status. */
+SIEVE_API int64_t sieve_loss_workspace(int64_t rows, int64_t vocab, int32_t n, int32_t dtype,
+                                       int32_t backward);
+
 /* Release an index and its cached workspace.  NULL is a no-op. */
 SIEVE_API void sieve_free_index(sieve_index* idx);
 

@@ -19,7 +19,8 @@ __all__ = ["SieveError", "Index", "Stats", "Round", "load_library", "LIB_PATH", 
            "K_MAX", "F32", "F16", "search_multi", "LOOKAHEAD_OFF", "LOOKAHEAD_COMMITTED",
            "LOOKAHEAD_SERIAL", "LOOKAHEAD_SPECULATIVE", "AttentionPlan", "BF16", "attention",
            "layer_norm", "layer_norm_backward", "layer_norm_forward", "embed", "embed_backward",
-           "embed_forward"]
+           "embed_forward", "linear_cross_entropy", "linear_cross_entropy_backward",
+           "linear_cross_entropy_forward"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsieve.so")
 W_INF = 0x7FFFFFFF
@@ -350,4 +351,5 @@ def search_multi_calibrated(indexes, queries: torch.Tensor, exclude_ids: Optiona
 
 from .encoder import (AttentionPlan, BF16, attention, layer_norm, layer_norm_backward,  # noqa: E402
                       layer_norm_forward)
-from .training import embed, embed_backward, embed_forward  # noqa: E402
+from .training import (embed, embed_backward, embed_forward, linear_cross_entropy,  # noqa: E402
+                       linear_cross_entropy_backward, linear_cross_entropy_forward)

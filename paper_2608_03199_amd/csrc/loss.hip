@@ -1,0 +1,744 @@
+// loss.hip -- softmax cross entropy of hidden states against a table of vectors, without
+// keeping the logits, and its gradients.
+//
+//   s_tv = scale h_t . w_v,  lse_t = log sum_v exp s_tv,  loss_t = lse_t - s_t,target
+//   g_tv = (exp(s_tv - lse_t) - [v = target_t]) dloss_t
+//   dh_t = scale sum_v g_tv w_v,  dw_v = scale sum_t g_tv h_t
+//
+// Forward: tiles of logits stay in accumulators, and what leaves a tile is each row's maximum
+// and sum of exponentials over its 256 vectors; a second kernel joins them.
+//
+// Backward: the logits are computed again, a piece of the vocabulary at a time; the piece's g is
+// rounded to 16 bits and kept until both gradients' products have read it (a workspace of at most
+// 2^27 values, which the last-level cache holds for the most part).  dw of the piece is then
+// complete; dh is summed in fp32 over the pieces.
+//
+// The matrix units bound all of it: 2 rows vocab n operations for the loss, 6 for the gradients.
+//
+// 16-bit inputs are multiplied as they are.  32-bit ones come as three bf16 planes whose sum is
+// the value (8 bits each), six products of planes: what is left out is below fp32's last bit.
+//
+// g is rounded once, to the inputs' type; binary16 does not have fp32's range, so there it is
+// scaled by 2^14.  dloss enters g by its mantissa only: its power of two goes, exactly, into a
+// row's factor of dh and into the copy of h that dw's product reads.
+#include <math.h>
+
+#include <algorithm>
+
+#include "mm_tile.h"
+#include "once_per_device.h"
+
+using namespace sieve;
+
+namespace {
+
+typedef mm_bf16 bf16;
+typedef mm_f16 f16;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kBM = 256, kBN = 128;       // a tile's vectors and rows (or rows and columns)
+constexpr int kHigh = 8;                  // tiles of m before the next of n, see mm_tile_of
+constexpr int64_t kMaxRows = 1 << 24;     // of h, and of the table
+constexpr int kMaxN = 65536;
+constexpr int64_t kPieceValues = 1 << 27;  // of g
+constexpr int64_t kMaxPiece = 65536;       // vectors
+constexpr int64_t kRowChunk = 65536;       // rows of h in one launch of the forward pass
+constexpr float kHalfScale = 16384.f;      // what g in binary16 is scaled by
+
+struct Targets {
+  const void* p;
+  int bytes;
+  int64_t vocab;
+  // the row's vector, or -1
+  __device__ __forceinline__ int64_t at(int64_t row) const {
+    const int64_t t = bytes == 8 ? ((const int64_t*)p)[row] : (int64_t)((const int32_t*)p)[row];
+    return t >= 0 && t < vocab ? t : -1;
+  }
+};
+
+__device__ __forceinline__ float other_half(float v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// The LDS address of what a kernel holds there.
+__device__ __forceinline__ uint32_t lds_of(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// Two rows' parts of a sum of exponentials: (maximum, sum), in base 2.
+struct Part {
+  float top, sum;
+};
+__device__ __forceinline__ Part join(Part a, Part b) {
+  const float top = fmaxf(a.top, b.top);
+  const float at = top == -INFINITY ? 0.f : top;
+  return {top, a.sum * exp2_of(a.top - at) + b.sum * exp2_of(b.top - at)};
+}
+
+struct Logits {
+  MmOperand w, h;        // a piece of the table; the rows
+  int64_t v_first;       // the piece's first vector
+  int64_t t_first;       // the rows' first
+  int64_t k;             // n, up to the next multiple of 8
+  int pairs;
+  uint32_t tiles_m, tiles_n;
+  float c2;              // scale log2(e)
+  Targets targets;
+  // forward
+  Part* part;            // [tile of 256 vectors][rows]
+  float* target_logit;   // [rows], in base 2
+  // backward
+  const float *lse, *dloss;
+  void* g;               // [planes][rows][g_stride]
+  int64_t g_stride, g_plane;
+};
+
+typedef mm_f32x16 f32x16;
+
+// The value of a row's target vector, where this lane holds it: rel is its place among the
+// wave's rows of the tile.
+template <int kI>
+__device__ __forceinline__ bool find_value(const f32x16 (&acc)[kI], int64_t rel, float& x) {
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < kI; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (rel == i * 32 + (r >> 2) * 8 + (int)(threadIdx.x >> 5 & 1) * 4 + (r & 3)) {
+        x = acc[i][r];
+        found = true;
+      }
+  return found;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kMmThreads, 2) void loss_forward_kernel(Logits a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+  uint32_t tm, tn;
+  mm_tile_of(blockIdx.x, a.tiles_m, a.tiles_n, kHigh, tm, tn);
+  const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
+  typedef MmTile<T, kBM, kBN, false, false> Tile;
+  Tile t;
+  t.run(a.w, m0, a.h, n0, 0, a.k, a.pairs, lds_of(lds_memory));
+  Part* s_part = (Part*)lds_memory;
+  const int wave_m = (int)threadIdx.x >> 7;
+  const int64_t left = a.w.rows - m0 - wave_m * (kBM / 2);  // vectors from the wave's first
+#pragma unroll
+  for (int j = 0; j < Tile::kJ; ++j) {
+    f32x16 acc[Tile::kI];
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < Tile::kI; ++i) {
+      acc[i] = t.acc[i][j];
+      if (left < kBM / 2) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (mm_row<kBM>(i, r) - wave_m * (kBM / 2) >= left) acc[i][r] = -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][r]);
+    }
+    top = fmaxf(top, other_half(top));
+    const float top2 = top * a.c2, at = top == -INFINITY ? 0.f : top2;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < Tile::kI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum += exp2_of(fmaf(acc[i][r], a.c2, -at));
+    sum += other_half(sum);
+    const int col = mm_col<kBN>(j);
+    const int64_t row = n0 + col;
+    int64_t rel = -1;
+    if (row < a.h.rows) {
+      const int64_t v = a.targets.at(a.t_first + row);
+      if (v >= 0) rel = v - a.v_first - m0 - wave_m * (kBM / 2);
+    }
+    if (__any(rel >= 0 && rel < kBM / 2)) {
+      float x;
+      if (find_value(acc, rel, x)) a.target_logit[row] = x * a.c2;
+    }
+    if ((threadIdx.x & 32) == 0) s_part[wave_m * kBN + col] = Part{top2, sum};
+  }
+  __syncthreads();
+  if (threadIdx.x < kBN && n0 + threadIdx.x < a.h.rows)
+    a.part[(int64_t)tm * a.h.rows + n0 + threadIdx.x] =
+        join(s_part[threadIdx.x], s_part[kBN + threadIdx.x]);
+}
+
+// Joins the tiles' parts: a work-group takes 32 rows, its 8 groups of 32 threads every 8th tile.
+__global__ __launch_bounds__(256) void loss_join_kernel(const Part* part, const float* target_logit,
+                                                        Targets targets, int64_t t_first,
+                                                        int64_t rows, int64_t tiles, float* loss,
+                                                        float* lse) {
+  __shared__ Part s[8][32];
+  const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * 32 + c;
+  Part p{-INFINITY, 0.f};
+  if (row < rows) {
+#pragma unroll 4
+    for (int64_t i = g; i < tiles; i += 8) p = join(p, part[i * rows + row]);
+  }
+  s[g][c] = p;
+  __syncthreads();
+  if (g != 0 || row >= rows) return;
+  for (int i = 1; i < 8; ++i) p = join(p, s[i][c]);
+  const float more = log2f(p.sum);
+  lse[t_first + row] = (p.top + more) * kLn2;
+  if (loss)
+    loss[t_first + row] =
+        targets.at(t_first + row) < 0 ? 0.f : (more + (p.top - target_logit[row])) * kLn2;
+}
+
+// A row's dloss as mantissa and power of two; (0, 0) where the row gives no gradient.
+struct Weight {
+  float mantissa;
+  int power;
+};
+__device__ __forceinline__ Weight weight_of(const Targets& targets, const float* dloss,
+                                            int64_t row) {
+  const float d = dloss[row];
+  if (targets.at(row) < 0 || d == 0.f) return {0.f, 0};
+  if (!isfinite(d)) return {d, 0};
+  int e;
+  const float m = frexpf(d, &e);
+  return {2.f * m, e - 1};
+}
+
+// The largest power of two among the rows' weights, and so at most 2^power times as much weighs
+// each of them.
+__global__ __launch_bounds__(1024) void loss_power_kernel(Targets targets, const float* dloss,
+                                                          int64_t rows, int* power) {
+  __shared__ int s[16];
+  int top = -1000;
+  for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+    const Weight w = weight_of(targets, dloss, r);
+    if (w.mantissa != 0.f) top = max(top, w.power);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = max(top, __shfl_xor(top, o));
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) top = max(top, s[i]);
+    *power = top == -1000 ? 0 : top;
+  }
+}
+
+// v as 8-bit parts, largest first; what is not finite is the first part's alone.
+__device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
+  auto cut = [](float x) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+  };
+  const float a = isfinite(v) ? cut(v) : v;
+  const float b = isfinite(v) ? cut(v - a) : 0.f;
+  p[0] = (bf16)a;
+  p[1] = (bf16)b;
+  p[2] = (bf16)(isfinite(v) ? v - a - b : 0.f);
+}
+
+// Rows of n values as the products take them: zeros up to the next multiple of 8, 32-bit values
+// as planes; with dloss each row times its weight's power of two, or zeros where it has none.
+struct Pack {
+  const void* x;
+  int64_t stride, rows;
+  int n, k;
+  void* to;
+  int64_t plane;
+  const float* dloss;
+  Targets targets;
+  const int* power;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
+  typedef std::conditional_t<std::is_same_v<T, float>, bf16, T> U;
+  const int per = a.k / 8;
+  const int64_t all = a.rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+       i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int col = (int)(i % per) * 8;
+    float factor = 1.f;
+    if (a.dloss) {
+      const Weight w = weight_of(a.targets, a.dloss, row);
+      factor = w.mantissa == 0.f ? 0.f : ldexpf(1.f, w.power - *a.power);
+    }
+    const T* x = (const T*)a.x + row * a.stride + col;
+    EncVec<U, 8> out[3];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // the factor is a power of two: nothing is rounded but what leaves binary16's range
+      const float v = col + j < a.n && factor != 0.f ? (float)x[j] * factor : 0.f;
+      if constexpr (std::is_same_v<T, float>) {
+        bf16 p[3];
+        split3(v, p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) out[q].v[j] = p[q];
+      } else {
+        out[0].v[j] = (U)v;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < (std::is_same_v<T, float> ? 3 : 1); ++q)
+      enc_store<U, 8>((U*)a.to + q * a.plane + row * a.k + col, out[q]);
+  }
+}
+
+// g of a piece: the logits' tiles again, each value turned into its gradient.  F: the inputs'
+// type; T: the planes'.
+template <typename F, typename T>
+__global__ __launch_bounds__(kMmThreads, 2) void loss_gradient_kernel(Logits a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+  uint32_t tm, tn;
+  mm_tile_of(blockIdx.x, a.tiles_m, a.tiles_n, kHigh, tm, tn);
+  const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
+  typedef MmTile<T, kBM, kBN, false, false> Tile;
+  Tile t;
+  t.run(a.w, m0, a.h, n0, 0, a.k, a.pairs, lds_of(lds_memory));
+  const int wave_m = (int)threadIdx.x >> 7, half = (int)threadIdx.x >> 5 & 1;
+  const int64_t first = m0 + wave_m * (kBM / 2), left = a.w.rows - first;
+#pragma unroll
+  for (int j = 0; j < Tile::kJ; ++j) {
+    const int64_t row = n0 + mm_col<kBN>(j);
+    const bool there = row < a.h.rows;
+    int64_t rel = -1;
+    float weight = 0.f, lse2 = 0.f;
+    if (there) {
+      const int64_t v = a.targets.at(row);
+      if (v >= 0) rel = v - a.v_first - first;
+      weight = weight_of(a.targets, a.dloss, row).mantissa;
+      if constexpr (std::is_same_v<F, f16>) weight *= kHalfScale;
+      lse2 = a.lse[row] * kLog2e;
+    }
+    const bool here = __any(rel >= 0 && rel < kBM / 2);
+    T* g = (T*)a.g + row * a.g_stride + first + 8 * half;
+#pragma unroll
+    for (int i = 0; i < Tile::kI; ++i) {
+      f32x16 x = t.acc[i][j];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int v = i * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+        float p = exp2_of(fmaf(x[r], a.c2, -lse2));
+        if (here && rel == v) p -= 1.f;
+        // a row without weight gives nothing, whatever it holds; nor does what lies past the
+        // last vector
+        x[r] = weight == 0.f || v >= left ? 0.f : p * weight;
+      }
+      // pairs of 16-bit values; halves of a wave change places so that each lane has 8
+      // neighbours
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        constexpr int kPlanes = std::is_same_v<F, float> ? 3 : 1;
+        T part[kPlanes][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (kPlanes == 3) {
+            T p[3];
+            split3(x[8 * q + e], p);
+#pragma unroll
+            for (int z = 0; z < 3; ++z) part[z][e] = p[z];
+          } else {
+            part[0][e] = (T)x[8 * q + e];
+          }
+        }
+#pragma unroll
+        for (int z = 0; z < kPlanes; ++z) {
+          uint32_t d[4];
+          __builtin_memcpy(d, part[z], 16);
+          const u32x2 lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
+          const u32x2 hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
+          const enc_u32x4 out = {lo[0], hi[0], lo[1], hi[1]};
+          if (there) *(enc_u32x4*)(g + z * a.g_plane + i * 32 + 16 * q) = out;
+        }
+      }
+    }
+  }
+}
+
+// A gradient's product: out (m, n) in fp32, [split][rows of m][pitch], or added to what is there.
+struct Product {
+  MmOperand a, b;
+  int64_t k, per;        // values of k, and of a split
+  int pairs;
+  uint32_t tiles_m, tiles_n;
+  float* out;
+  int64_t pitch, split;  // values between rows, and between splits
+  int add;
+};
+
+template <typename T, bool kAcrossA>
+__global__ __launch_bounds__(kMmThreads, 2) void loss_product_kernel(Product a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+  const uint32_t tiles = a.tiles_m * a.tiles_n;
+  uint32_t tm, tn;
+  mm_tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n, kHigh, tm, tn);
+  const int64_t split = blockIdx.x / tiles;
+  const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
+  const int64_t k0 = split * a.per, k1 = k0 + a.per < a.k ? k0 + a.per : a.k;
+  typedef MmTile<T, kBM, kBN, kAcrossA, true> Tile;
+  Tile t;
+  t.run(a.a, m0, a.b, n0, k0, k1, a.pairs, lds_of(lds_memory));
+  float* out = a.out + split * a.split;
+#pragma unroll
+  for (int j = 0; j < Tile::kJ; ++j) {
+    const int64_t n = n0 + mm_col<kBN>(j);
+#pragma unroll
+    for (int i = 0; i < Tile::kI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int64_t m = m0 + mm_row<kBM>(i, r);
+        if (m < a.a.rows && n < a.b.rows) {
+          float* p = out + m * a.pitch + n;
+          *p = a.add ? *p + t.acc[i][j][r] : t.acc[i][j][r];
+        }
+      }
+  }
+}
+
+// The splits' sum, times the row's factor, rounded.
+struct Finish {
+  const float* x;
+  int64_t rows, pitch, split;
+  int splits, n;
+  float factor;            // scale, over what g was scaled by
+  void* out;
+  // dh: the row's own power of two, zeros where it has no weight; dw: the largest
+  const float* dloss;
+  Targets targets;
+  const int* power;
+};
+
+template <typename F>
+__global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
+  const int64_t all = a.rows * a.n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+       i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / a.n;
+    const int col = (int)(i % a.n);
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v += a.x[s * a.split + row * a.pitch + col];
+    if (a.dloss) {
+      const Weight w = weight_of(a.targets, a.dloss, row);
+      v = w.mantissa == 0.f ? 0.f : ldexpf(v * a.factor, w.power);
+    } else if (a.power) {  // none without rows: zeros
+      v = ldexpf(v * a.factor, *a.power);
+    }
+    ((F*)a.out)[i] = (F)v;
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
+
+struct Layout {
+  int64_t piece;                 // vectors of a piece, a multiple of 256
+  int64_t k;                     // n, up to the next multiple of 8
+  int planes, pairs;
+  int splits_h, splits_w;
+  int64_t h, w, part, target, g, weighed, dh, dw, power, bytes;
+};
+
+// How often a product of `tiles` tiles over k is split so that the chip's 512 places are taken.
+int splits_of(int64_t tiles, int64_t k) {
+  int64_t s = 512 / std::max<int64_t>(tiles, 1);
+  s = std::min(s, k / 1024);
+  return (int)std::max<int64_t>(s, 1);
+}
+
+Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool backward) {
+  Layout l{};
+  l.planes = dtype == SIEVE_F32 ? 3 : 1;
+  l.pairs = dtype == SIEVE_F32 ? 6 : 1;
+  l.k = (n + 7) & ~7;
+  int64_t piece = std::min(kPieceValues / (l.planes * std::max<int64_t>(rows, 1)), kMaxPiece);
+  piece = std::max<int64_t>(piece & ~int64_t(255), 256);
+  l.piece = std::min(piece, round256(vocab));
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t was = at;
+    at += round256(bytes);
+    return was;
+  };
+  l.h = take(rows * l.k * 2 * l.planes);
+  l.w = take(l.piece * l.k * 2 * l.planes);
+  if (!backward) {
+    const int64_t chunk = std::min(rows, kRowChunk);
+    l.part = take((vocab + kBM - 1) / kBM * chunk * (int64_t)sizeof(Part));
+    l.target = take(chunk * 4);
+  } else {
+    const int64_t tiles_n = (n + kBN - 1) / kBN;
+    l.splits_h = splits_of((rows + kBM - 1) / kBM * tiles_n, l.piece);
+    l.splits_w = splits_of((l.piece + kBM - 1) / kBM * tiles_n, rows);
+    l.g = take(rows * l.piece * 2 * l.planes);
+    l.weighed = take(rows * l.k * 2 * l.planes);
+    l.dh = take(l.splits_h * rows * l.k * 4);
+    l.dw = take(l.splits_w * l.piece * l.k * 4);
+    l.power = take(4);
+  }
+  l.bytes = at;
+  return l;
+}
+
+int check_loss(int64_t rows, int64_t vocab, int32_t n, int32_t dtype) {
+  if (!enc_dtype_ok(dtype))
+    return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16",
+                     dtype);
+  if (rows < 0) return set_error(SIEVE_EINVAL, "rows is negative");
+  if (vocab < 1) return set_error(SIEVE_EINVAL, "vocab must be >= 1");
+  if (n < 1) return set_error(SIEVE_EINVAL, "n = %d must be >= 1", n);
+  if (n > kMaxN) return set_error(SIEVE_EUNSUPPORTED, "n = %d is above %d", n, kMaxN);
+  if (rows > kMaxRows || vocab > kMaxRows)
+    return set_error(SIEVE_EUNSUPPORTED, "rows or vocab is above %lld", (long long)kMaxRows);
+  return SIEVE_OK;
+}
+
+int check_call(const void* h, int64_t h_stride, const void* table, int64_t table_stride, int32_t n,
+               const void* targets, int32_t target_bytes, float scale, const void* workspace,
+               int64_t bytes, int64_t need) {
+  if (!h || !table || !targets)
+    return set_error(SIEVE_EINVAL, "h, table and targets must be non-NULL");
+  if (target_bytes != 4 && target_bytes != 8)
+    return set_error(SIEVE_EINVAL, "target_bytes = %d must be 4 or 8", target_bytes);
+  if (h_stride < n || table_stride < n)
+    return set_error(SIEVE_EINVAL, "a row stride is below n = %d", n);
+  if (!(scale > 0.f) || scale == INFINITY)
+    return set_error(SIEVE_EINVAL, "scale must be > 0 and finite");
+  if (!workspace || bytes < need || ((uintptr_t)workspace & 15))
+    return set_error(SIEVE_EINVAL, "workspace must be 16-byte aligned and hold %lld bytes",
+                     (long long)need);
+  return SIEVE_OK;
+}
+
+int blocks_of(int64_t work) { return (int)std::min<int64_t>((work + 255) / 256, 8192); }
+
+template <typename T>
+void pack(const void* x, int64_t stride, int64_t rows, int32_t n, int64_t k, void* to,
+          int64_t plane, hipStream_t s, const float* dloss = nullptr, Targets targets = {},
+          const int* power = nullptr) {
+  const Pack a{x, stride, rows, n, (int)k, to, plane, dloss, targets, power};
+  loss_pack_kernel<T><<<blocks_of(rows * (k / 8)), 256, 0, s>>>(a);
+}
+
+// Whether rows may be multiplied where they lie.
+bool direct(const void* p, int64_t stride, int32_t n, int32_t dtype) {
+  return dtype != SIEVE_F32 && n % 8 == 0 && stride % 8 == 0 && stride <= kMmMaxStride &&
+         ((uintptr_t)p & 15) == 0;
+}
+
+// The operand of rows [0, rows) of x, packed into `to` where that is needed.
+template <typename T>
+MmOperand operand(const void* x, int64_t stride, int64_t rows, int32_t n, int32_t dtype, int64_t k,
+                  void* to, hipStream_t s) {
+  if (direct(x, stride, n, dtype)) return {x, stride, rows, 0};
+  pack<T>(x, stride, rows, n, k, to, rows * k, s);
+  return {to, k, rows, rows * k};
+}
+
+std::atomic<uint64_t> g_large_lds{0};
+
+template <typename K>
+hipError_t allow(K* kernel, int bytes) {
+  return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                             bytes);
+}
+
+constexpr int kLds = MmTile<bf16, kBM, kBN, false, false>::kLds;
+
+int allow_lds() {
+  int device = 0;
+  ENC_HIP_TRY(hipGetDevice(&device));
+  const hipError_t e = once_per_device(g_large_lds, device, [] {
+    hipError_t r = hipSuccess;
+    auto add = [&](hipError_t x) { r = r == hipSuccess ? x : r; };
+    add(allow(loss_forward_kernel<f16>, kLds));
+    add(allow(loss_forward_kernel<bf16>, kLds));
+    add(allow(loss_gradient_kernel<f16, f16>, kLds));
+    add(allow(loss_gradient_kernel<bf16, bf16>, kLds));
+    add(allow(loss_gradient_kernel<float, bf16>, kLds));
+    add(allow(loss_product_kernel<f16, false>, kLds));
+    add(allow(loss_product_kernel<f16, true>, kLds));
+    add(allow(loss_product_kernel<bf16, false>, kLds));
+    add(allow(loss_product_kernel<bf16, true>, kLds));
+    return r;
+  });
+  ENC_HIP_TRY(e);
+  return SIEVE_OK;
+}
+
+// f(inputs' type, planes' type)
+template <typename F>
+void by_type(int32_t dtype, F f) {
+  if (dtype == SIEVE_F32) f(float{}, bf16{});
+  else if (dtype == SIEVE_F16) f(f16{}, f16{});
+  else f(bf16{}, bf16{});
+}
+
+uint32_t tiles_of(int64_t n, int size) { return (uint32_t)((n + size - 1) / size); }
+
+}  // namespace
+
+SIEVE_API int64_t sieve_loss_workspace(int64_t rows, int64_t vocab, int32_t n, int32_t dtype,
+                                       int32_t backward) {
+  clear_error();
+  if (int st = check_loss(rows, vocab, n, dtype)) return st;
+  if (backward != 0 && backward != 1) return set_error(SIEVE_EINVAL, "backward must be 0 or 1");
+  return rows ? layout_of(rows, vocab, n, dtype, backward != 0).bytes : 0;
+}
+
+SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* table,
+                                 int64_t table_stride, int32_t dtype, int64_t rows, int64_t vocab,
+                                 int32_t n, const void* targets, int32_t target_bytes, float scale,
+                                 float* loss, float* lse, void* workspace, int64_t workspace_bytes,
+                                 void* stream) {
+  clear_error();
+  if (int st = check_loss(rows, vocab, n, dtype)) return st;
+  if (rows == 0) return SIEVE_OK;
+  const Layout l = layout_of(rows, vocab, n, dtype, false);
+  if (int st = check_call(h, h_stride, table, table_stride, n, targets, target_bytes, scale,
+                          workspace, workspace_bytes, l.bytes))
+    return st;
+  if (!lse) return set_error(SIEVE_EINVAL, "lse must be non-NULL");
+  if (int st = allow_lds()) return st;
+  char* w = (char*)workspace;
+  hipStream_t s = (hipStream_t)stream;
+  by_type(dtype, [&](auto f, auto t) {
+    typedef decltype(f) F;
+    typedef decltype(t) T;
+    Logits a{};
+    a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
+    a.k = l.k;
+    a.pairs = l.pairs;
+    a.c2 = scale * kLog2e;
+    a.targets = {targets, target_bytes, vocab};
+    a.target_logit = (float*)(w + l.target);
+    const MmOperand all_h = a.h;
+    // a table that has to be packed is taken in pieces; any is, where a launch would be too large
+    const bool as_is = direct(table, table_stride, n, dtype);
+    const int64_t piece = as_is ? int64_t(1) << 20 : l.piece;
+    for (int64_t t0 = 0; t0 < rows; t0 += kRowChunk) {
+      a.h = all_h;
+      a.h.p = (const char*)all_h.p + t0 * all_h.stride * 2;
+      a.h.rows = std::min(rows - t0, kRowChunk);
+      a.t_first = t0;
+      a.tiles_n = tiles_of(a.h.rows, kBN);
+      for (int64_t v0 = 0; v0 < vocab; v0 += piece) {
+        const int64_t vs = std::min(piece, vocab - v0);
+        a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
+                         w + l.w, s);
+        a.v_first = v0;
+        a.tiles_m = tiles_of(vs, kBM);
+        a.part = (Part*)(w + l.part) + v0 / kBM * a.h.rows;
+        loss_forward_kernel<T><<<a.tiles_m * a.tiles_n, kMmThreads, kLds, s>>>(a);
+      }
+      loss_join_kernel<<<tiles_of(a.h.rows, 32), 256, 0, s>>>(
+          (const Part*)(w + l.part), a.target_logit, a.targets, t0, a.h.rows,
+          tiles_of(vocab, kBM), loss, lse);
+    }
+  });
+  ENC_HIP_TRY(hipGetLastError());
+  return SIEVE_OK;
+}
+
+SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_stride,
+                                  const void* table, int64_t table_stride, int32_t dtype,
+                                  int64_t rows, int64_t vocab, int32_t n, const void* targets,
+                                  int32_t target_bytes, const float* lse, float scale, void* dh,
+                                  void* dtable, void* workspace, int64_t workspace_bytes,
+                                  void* stream) {
+  clear_error();
+  if (int st = check_loss(rows, vocab, n, dtype)) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const Layout l = layout_of(rows, vocab, n, dtype, true);
+  if (rows > 0) {
+    if (int st = check_call(h, h_stride, table, table_stride, n, targets, target_bytes, scale,
+                            workspace, workspace_bytes, l.bytes))
+      return st;
+    if (!dloss || !lse) return set_error(SIEVE_EINVAL, "dloss and lse must be non-NULL");
+  }
+  if (!dh && !dtable) return SIEVE_OK;
+  if (rows == 0 && !dtable) return SIEVE_OK;
+  if (rows > 0)
+    if (int st = allow_lds()) return st;
+  char* w = (char*)workspace;
+  by_type(dtype, [&](auto f, auto t) {
+    typedef decltype(f) F;
+    typedef decltype(t) T;
+    const Targets tg{targets, target_bytes, vocab};
+    const float factor = std::is_same_v<F, f16> ? scale / kHalfScale : scale;
+    if (rows == 0) {
+      const Finish fin{nullptr, vocab, 0, 0, 0, n, 0.f, dtable, nullptr, tg, nullptr};
+      loss_finish_kernel<F><<<blocks_of(vocab * n), 256, 0, s>>>(fin);
+      return;
+    }
+    int* power = (int*)(w + l.power);
+    loss_power_kernel<<<1, 1024, 0, s>>>(tg, dloss, rows, power);
+    Logits a{};
+    a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
+    if (dtable)
+      pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, s, dloss, tg, power);
+    a.k = l.k;
+    a.pairs = l.pairs;
+    a.c2 = scale * kLog2e;
+    a.targets = tg;
+    a.lse = lse;
+    a.dloss = dloss;
+    a.g = w + l.g;
+    a.g_stride = l.piece;
+    a.g_plane = rows * l.piece;
+    a.tiles_n = tiles_of(rows, kBN);
+    for (int64_t v0 = 0; v0 < vocab; v0 += l.piece) {
+      const int64_t vs = std::min(l.piece, vocab - v0);
+      a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
+                       w + l.w, s);
+      a.v_first = v0;
+      a.tiles_m = tiles_of(vs, kBM);
+      loss_gradient_kernel<F, T><<<a.tiles_m * a.tiles_n, kMmThreads, kLds, s>>>(a);
+      Product p{};
+      p.pairs = l.pairs;
+      p.pitch = l.k;
+      p.tiles_n = tiles_of(n, kBN);
+      if (dh) {
+        p.a = {a.g, l.piece, rows, a.g_plane};
+        p.b = a.w;
+        p.b.rows = n;
+        p.k = vs;
+        p.per = ((vs + l.splits_h - 1) / l.splits_h + kMmStep - 1) / kMmStep * kMmStep;
+        p.tiles_m = tiles_of(rows, kBM);
+        p.out = (float*)(w + l.dh);
+        p.split = rows * l.k;
+        p.add = v0 > 0;
+        loss_product_kernel<T, false>
+            <<<p.tiles_m * p.tiles_n * l.splits_h, kMmThreads, kLds, s>>>(p);
+      }
+      if (dtable) {
+        p.a = {a.g, l.piece, l.piece, a.g_plane};
+        p.b = {w + l.weighed, l.k, n, rows * l.k};
+        p.k = rows;
+        p.per = ((rows + l.splits_w - 1) / l.splits_w + kMmStep - 1) / kMmStep * kMmStep;
+        p.tiles_m = tiles_of(vs, kBM);
+        p.out = (float*)(w + l.dw);
+        p.split = l.piece * l.k;
+        p.add = 0;
+        loss_product_kernel<T, true>
+            <<<p.tiles_m * p.tiles_n * l.splits_w, kMmThreads, kLds, s>>>(p);
+        const Finish fin{(const float*)(w + l.dw), vs, l.k, l.piece * l.k, l.splits_w, n, factor,
+                         (F*)dtable + v0 * n, nullptr, tg, power};
+        loss_finish_kernel<F><<<blocks_of(vs * n), 256, 0, s>>>(fin);
+      }
+    }
+    if (dh) {
+      const Finish fin{(const float*)(w + l.dh), rows, l.k, rows * l.k, l.splits_h, n, factor, dh,
+                       dloss, tg, power};
+      loss_finish_kernel<F><<<blocks_of(rows * n), 256, 0, s>>>(fin);
+    }
+  });
+  ENC_HIP_TRY(hipGetLastError());
+  return SIEVE_OK;
+}

@@ -1,8 +1,8 @@
-"""Operators of libsieve around a text encoder's blocks: the table's lookup with its gradient
-(``include/sieve.h``).
+"""Operators of libsieve around a text encoder's blocks: the table's lookup, and the cross entropy of
+hidden states against a table, each with its gradient (``include/sieve.h``).
 
 As in ``encoder.py``, the ``*_forward`` / ``*_backward`` functions marshal the arguments of the
-library's calls, ``embed`` joins them for torch's autograd, all calls are asynchronous on the
+library's calls, the others join them for torch's autograd, all calls are asynchronous on the
 given or current stream, and there is no CPU fallback.
 """
 from __future__ import annotations
@@ -17,7 +17,8 @@ from . import _check
 from .encoder import _CODES, _code, _here, _need, _on, _ptr, _raw_stream, _rows, _workspace
 from .encoder import _library as _encoder_library
 
-__all__ = ["embed", "embed_backward", "embed_forward"]
+__all__ = ["embed", "embed_backward", "embed_forward", "linear_cross_entropy",
+           "linear_cross_entropy_backward", "linear_cross_entropy_forward"]
 
 _ready = None
 
@@ -35,6 +36,14 @@ def _library():
     lib.sieve_embed_backward.restype = ctypes.c_int
     lib.sieve_embed_backward.argtypes = [P, i64, i32, P, i32, i64, i64, i32, f32, i32, P, i32, P,
                                          i64, P]
+    lib.sieve_loss_workspace.restype = i64
+    lib.sieve_loss_workspace.argtypes = [i64, i64, i32, i32, i32]
+    lib.sieve_loss_forward.restype = ctypes.c_int
+    lib.sieve_loss_forward.argtypes = [P, i64, P, i64, i32, i64, i64, i32, P, i32, f32, P, P, P,
+                                       i64, P]
+    lib.sieve_loss_backward.restype = ctypes.c_int
+    lib.sieve_loss_backward.argtypes = [P, P, i64, P, i64, i32, i64, i64, i32, P, i32, P, f32, P,
+                                        P, P, i64, P]
     _ready = lib
     return lib
 
@@ -146,3 +155,105 @@ def embed(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
           dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """Differentiable ``embed_forward``."""
     return _Embed.apply(ids, table, scale, dtype)
+
+
+# ---- cross entropy ------------------------------------------------------------------------
+
+
+def linear_cross_entropy_forward(h: torch.Tensor, table: torch.Tensor, targets: torch.Tensor,
+                                 scale: float = 1.0, stream=None):
+    """Softmax cross entropy of the logits ``scale * h @ table.T`` without keeping them: ``h``
+    [..., n] and ``table`` [vocab, n] of one dtype, ``targets`` [...] whole numbers.  Returns
+    ``(loss, lse)``, fp32 of targets' shape: each row's loss, and the logarithm of its sum.  A row
+    whose target is not in the table (-100, say) is left out: its loss is 0."""
+    _need(h.is_cuda, "h must be a GPU tensor")
+    if _here(h.device, stream):
+        return _loss_forward(h, table, targets, scale)
+    with _on(h.device, stream):
+        return _loss_forward(h, table, targets, scale)
+
+
+def _loss_inputs(h, table, targets):
+    shape = h.shape
+    _need(len(shape) >= 1 and shape[-1] >= 1, "h must have a last axis of at least one value")
+    n = shape[-1]
+    code = _code(h, "h")
+    if table.dtype != h.dtype:
+        raise TypeError(f"table must be {h.dtype}, not {table.dtype}")
+    _need(table.dim() == 2 and table.shape[0] >= 1 and table.shape[1] == n and
+          table.device == h.device, f"table must be [vocab, {n}] on h's device")
+    _need(targets.shape == shape[:-1], f"targets must be {list(shape[:-1])}")
+    targets, size = _numbers(targets, "targets", h.device)
+    hr, h_stride = _rows(h, n)
+    tr, t_stride = _rows(table, n)
+    return (hr, h_stride, tr, t_stride, code, targets.numel(), table.shape[0], n, targets, size)
+
+
+def _loss_forward(h, table, targets, scale):
+    lib = _library()
+    hr, h_stride, tr, t_stride, code, rows, vocab, n, tg, size = _loss_inputs(h, table, targets)
+    out = h.new_empty((2,) + targets.shape, dtype=torch.float32)
+    need = lib.sieve_loss_workspace(rows, vocab, n, code, 0)
+    space = _workspace(lib, need, h.device)
+    if rows:
+        at = out.data_ptr()
+        _check(lib, lib.sieve_loss_forward(hr.data_ptr(), h_stride, tr.data_ptr(), t_stride, code,
+                                           rows, vocab, n, tg.data_ptr(), size, scale, at,
+                                           at + 4 * rows, _ptr(space), need,
+                                           _raw_stream(h.device)))
+    return out[0], out[1]
+
+
+def linear_cross_entropy_backward(dloss: torch.Tensor, h: torch.Tensor, table: torch.Tensor,
+                                  targets: torch.Tensor, lse: torch.Tensor, scale: float = 1.0,
+                                  h_grad: bool = True, table_grad: bool = True, stream=None):
+    """Gradients of ``linear_cross_entropy_forward`` from the gradient of each row's loss (fp32),
+    the forward pass's inputs and its ``lse``; the logits are computed again.  Returns ``(dh,
+    dtable)``, None where not asked for."""
+    _need(h.is_cuda, "h must be a GPU tensor")
+    args = (dloss, h, table, targets, lse, scale, h_grad, table_grad)
+    if _here(h.device, stream):
+        return _loss_backward(*args)
+    with _on(h.device, stream):
+        return _loss_backward(*args)
+
+
+def _loss_backward(dloss, h, table, targets, lse, scale, h_grad, table_grad):
+    lib = _library()
+    hr, h_stride, tr, t_stride, code, rows, vocab, n, tg, size = _loss_inputs(h, table, targets)
+    for name, t in (("dloss", dloss), ("lse", lse)):
+        _need(t.shape == targets.shape and t.dtype is torch.float32 and t.device == h.device,
+              f"{name} must be {list(targets.shape)} float32 on h's device")
+    dloss, lse = dloss.contiguous(), lse.contiguous()
+    dh = h.new_empty(h.shape) if h_grad else None
+    dtable = h.new_empty((vocab, n)) if table_grad else None
+    need = lib.sieve_loss_workspace(rows, vocab, n, code, 1)
+    space = _workspace(lib, need, h.device)
+    _check(lib, lib.sieve_loss_backward(
+        _ptr(dloss), _ptr(hr), h_stride, tr.data_ptr(), t_stride, code, rows, vocab, n, _ptr(tg),
+        size, _ptr(lse), scale, _ptr(dh), _ptr(dtable), _ptr(space), need, _raw_stream(h.device)))
+    return dh, dtable
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, table, targets, scale):
+        loss, lse = linear_cross_entropy_forward(h, table, targets, scale)
+        ctx.save_for_backward(h, table, targets, lse)
+        ctx.scale = scale
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        h, table, targets, lse = ctx.saved_tensors
+        dh, dtable = linear_cross_entropy_backward(
+            dloss, h, table, targets, lse, ctx.scale, ctx.needs_input_grad[0],
+            ctx.needs_input_grad[1])
+        return dh, dtable, None, None
+
+
+def linear_cross_entropy(h: torch.Tensor, table: torch.Tensor, targets: torch.Tensor,
+                         scale: float = 1.0) -> torch.Tensor:
+    """Differentiable ``linear_cross_entropy_forward``: each row's loss."""
+    return _LinearCrossEntropy.apply(h, table, targets, scale)

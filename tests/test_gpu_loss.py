@@ -1,0 +1,338 @@
+"""Cross entropy without logits, and its gradients, on the GPU against the 64-bit oracle, value by
+value within the bounds that training_reference.py derives."""
+import math
+
+import pytest
+import torch
+
+from encoder_reference import check
+from training_reference import cross_entropy, near
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+#: a rounding's rms share of a value is about u / sqrt(3) at the most; g and the gradient are
+#: rounded (sqrt 2), and the sums add as much again as fp32 leaves of them
+RMS = {"f32": 4e-6, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def ps():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    import paper_2608_03199_amd as ps
+    ps.load_library()
+    return ps
+
+
+def _rnd(seed):
+    g = torch.Generator().manual_seed(seed)
+    return g, lambda *s: torch.randn(*s, generator=g)
+
+
+def _inputs(rows, vocab, n, dt, seed, left_out=0.1, ragged=True):
+    g, rnd = _rnd(seed)
+    table = rnd(vocab, n) * n ** -0.5 * 1.5
+    targets = torch.randint(vocab, (rows,), generator=g)
+    h = rnd(rows, n) + 3 * torch.rand(rows, 1, generator=g) * table[targets]
+    u = torch.rand(rows, generator=g)
+    targets = torch.where(u < left_out, -100, torch.where(u < 1.3 * left_out, vocab, targets))
+    dloss = (0.1 + torch.rand(rows, generator=g)) / rows if ragged else \
+        torch.full((rows,), 1.0 / rows)
+    return h.to(dt), table.to(dt), targets, dloss
+
+
+def _run(ps, h, table, targets, dloss, scale=1.0, **more):
+    c = [t.cuda() for t in (h, table, targets, dloss)]
+    loss, lse = ps.linear_cross_entropy_forward(*c[:3], scale)
+    dh, dtable = ps.linear_cross_entropy_backward(c[3], *c[:3], lse, scale, **more)
+    return {"loss": loss, "lse": lse, "dh": dh, "dtable": dtable}
+
+
+SIZES = [(1, 1, 1), (1, 1000, 64), (2, 3, 5), (5, 256, 8), (16, 257, 32), (17, 255, 40),
+         (31, 2000, 77), (33, 4097, 128), (64, 512, 96), (100, 300, 515), (127, 129, 257),
+         (128, 256, 256), (129, 513, 264), (260, 1000, 768), (300, 5000, 200), (700, 2500, 1000),
+         (1500, 700, 72), (40, 33000, 64), (3, 70, 2056)]
+
+
+@pytest.mark.parametrize("rows, vocab, n", SIZES)
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_loss(ps, rows, vocab, n, dtype):
+    x = _inputs(rows, vocab, n, DTYPES[dtype], rows + 3 * n)
+    val, tol = cross_entropy(*x[:3], 1.0, x[3])
+    got = _run(ps, *x)
+    for name in val:
+        check(name, got[name], val[name], tol[name])
+    if rows > 16:
+        for name in ("dh", "dtable"):
+            near(name, got[name], val[name], RMS[dtype])
+    again = _run(ps, *x)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("scale", [0.05, 50.0])
+def test_loss_of_pairs(ps, dtype, scale):
+    """Unit vectors against unit vectors at a temperature."""
+    g, rnd = _rnd(3)
+    table = torch.nn.functional.normalize(rnd(600, 192), dim=1)
+    near_ = torch.rand(300, 1, generator=g)
+    h = torch.nn.functional.normalize(near_ * table[:300] + (1 - near_) * 0.07 * rnd(300, 192), dim=1)
+    h, table = h.to(DTYPES[dtype]), table.to(DTYPES[dtype])
+    dloss = torch.full((300,), 1 / 300)
+    val, tol = cross_entropy(h, table, torch.arange(300), scale, dloss)
+    got = _run(ps, h, table, torch.arange(300), dloss, scale)
+    for name in val:
+        check(name, got[name], val[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_loss_pieces_of_the_vocabulary(ps, dtype):
+    """More gradients than a piece holds: rows times vocabulary of several pieces."""
+    dt = DTYPES[dtype]
+    h, table, targets, dloss = _inputs(4200, 70001, 16, dt, 9, ragged=False)
+    got = _run(ps, h, table, targets, dloss)
+    # the 64-bit values on the GPU, in chunks of rows; float32 torch products would be too far off
+    x, w = h.double().cuda(), table.double().cuda()
+    dh, dw = torch.zeros_like(x), torch.zeros_like(w)
+    lse = torch.zeros(4200, dtype=torch.float64).cuda()
+    for at in torch.arange(4200).cuda().split(600):
+        s = x[at] @ w.T
+        lse[at] = torch.logsumexp(s, 1)
+        p = torch.softmax(s, 1)
+        t = targets.cuda()[at]
+        live = (t >= 0) & (t < 70001)
+        p[torch.arange(len(at)).cuda()[live], t[live]] -= 1
+        p *= (live * dloss.cuda()[at].double())[:, None]
+        dh[at] = p @ w
+        dw += p.T @ x[at]
+    near("lse", got["lse"], lse.cpu(), 2e-6)
+    near("dh", got["dh"], dh.cpu(), RMS[dtype])
+    near("dtable", got["dtable"], dw.cpu(), RMS[dtype])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_loss_left_out_rows_are_not_used(ps, dtype):
+    """Rows without a target or a weight: whatever they hold, they give no gradient, and nothing
+    of them reaches the others'."""
+    h, table, targets, dloss = _inputs(70, 300, 40, DTYPES[dtype], 5, left_out=0.0)
+    out = torch.zeros(70, dtype=torch.bool)
+    out[[0, 7, 31, 32, 69]] = True
+    targets[[0, 7, 31]] = -1
+    targets[32] = 300
+    dloss[69] = 0.0
+    val, tol = cross_entropy(h, table, targets, 1.0, dloss)
+    h[0], h[7], h[31], h[69] = math.nan, math.inf, -math.inf, math.nan
+    dloss[7], dloss[32] = math.nan, math.inf
+    got = _run(ps, h, table, targets, dloss)
+    for name in ("dh", "dtable"):
+        check(name, got[name], val[name], tol[name])
+    assert not got["dh"][out.cuda()].any() and not got["loss"][[0, 7, 31, 32]].any()
+    keep = ~out
+    for name in ("loss", "lse"):
+        check(name, got[name][keep.cuda()], val[name][keep], tol[name][keep])
+    # none is left
+    got = _run(ps, h, table, torch.full((70,), -100), dloss)
+    assert not got["dh"].any() and not got["dtable"].any() and not got["loss"].any()
+
+
+def test_loss_of_rows_that_are_not_numbers(ps):
+    """They stay in their rows, and reach the table's gradient, which is a sum over them."""
+    h, table, targets, dloss = _inputs(70, 300, 40, torch.bfloat16, 5, left_out=0.0)
+    h[3] = math.nan
+    got = _run(ps, h, table, targets, dloss)
+    rest = torch.arange(70) != 3
+    for name in ("loss", "lse"):
+        assert got[name][3].isnan() and got[name][rest.cuda()].isfinite().all()
+    assert got["dh"][3].isnan().all() and got["dh"][rest.cuda()].isfinite().all()
+    assert got["dtable"].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_loss_weights_of_any_size(ps, dtype):
+    """dloss far from 1, and rows whose weights differ by many powers of two."""
+    h, table, targets, _ = _inputs(90, 400, 64, DTYPES[dtype], 6)
+    g, rnd = _rnd(7)
+    for size in (2.0 ** -60 if dtype != "f16" else 2.0 ** -9, 1.0, 2.0 ** 9):
+        for spread in (0, 10):
+            dloss = size * rnd(90) * torch.exp2(-spread * torch.rand(90, generator=g))
+            val, tol = cross_entropy(h, table, targets, 1.0, dloss)
+            got = _run(ps, h, table, targets, dloss)
+            for name in val:
+                check(name, got[name], val[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_loss_peaked(ps, dtype):
+    """Targets that hold nearly all of their row's sum, and logits in the hundreds."""
+    h, table, targets, dloss = _inputs(60, 500, 64, DTYPES[dtype], 8, left_out=0.0)
+    h = (table[targets].float() * 40).to(h.dtype)
+    val, tol = cross_entropy(h, table, targets, 4.0, dloss)
+    got = _run(ps, h, table, targets, dloss, 4.0)
+    assert float(val["lse"].max()) > 200
+    for name in val:
+        check(name, got[name], val[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_loss_strides_and_shapes(ps, dtype):
+    dt = DTYPES[dtype]
+    g, rnd = _rnd(4)
+    wide_h, wide_t = rnd(4, 5, 3, 200).to(dt), (rnd(90, 200) * 0.2).to(dt)
+    targets = torch.randint(-1, 90, (4, 5, 3), generator=g)
+    dloss = torch.rand(4, 5, 3, generator=g)
+    for lo, hi in ((0, 64), (8, 72), (3, 67), (1, 200), (5, 6)):
+        n = hi - lo
+        val, tol = cross_entropy(wide_h[..., lo:hi].reshape(-1, n), wide_t[:, lo:hi],
+                                 targets.reshape(-1), 1.0, dloss.reshape(-1))
+        for it in (torch.int64, torch.int32):
+            c = (wide_h.cuda()[..., lo:hi], wide_t.cuda()[:, lo:hi], targets.to(it).cuda())
+            loss, lse = ps.linear_cross_entropy_forward(*c)
+            assert loss.shape == lse.shape == targets.shape
+            dh, dtable = ps.linear_cross_entropy_backward(dloss.cuda(), *c, lse)
+            assert dh.shape == (4, 5, 3, n) and dtable.shape == (90, n)
+            for name, x in (("loss", loss), ("lse", lse), ("dh", dh), ("dtable", dtable)):
+                check(name, x.reshape(val[name].shape), val[name], tol[name])
+    # transposed tables, expanded weights
+    c = (wide_h[..., :90].cuda(), wide_t.cuda()[:, :90].t(), targets.cuda())
+    val, tol = cross_entropy(wide_h[..., :90].reshape(-1, 90), wide_t[:, :90].t(),
+                             targets.reshape(-1), 1.0, torch.ones(60))
+    _, lse = ps.linear_cross_entropy_forward(*c)
+    one = torch.ones((), device="cuda").expand(4, 5, 3)
+    dh, dtable = ps.linear_cross_entropy_backward(one, *c, lse)
+    check("dh", dh.reshape(60, 90), val["dh"], tol["dh"])
+    check("dtable", dtable, val["dtable"], tol["dtable"])
+
+
+def test_loss_one_gradient_and_nothing(ps):
+    x = _inputs(50, 70, 24, torch.float16, 2)
+    both = _run(ps, *x)
+    for want in ((True, False), (False, True), (False, False)):
+        got = _run(ps, *x, h_grad=want[0], table_grad=want[1])
+        for name, w in zip(("dh", "dtable"), want):
+            assert (got[name] is not None) == w
+            assert not w or torch.equal(got[name], both[name])
+    got = _run(ps, x[0][:0], x[1], x[2][:0], x[3][:0])
+    assert got["loss"].shape == (0,) and got["dh"].shape == (0, 24)
+    assert got["dtable"].shape == (70, 24) and not got["dtable"].any()
+    loss, lse = ps.linear_cross_entropy_forward(x[0][0].cuda(), x[1].cuda(), x[2][0].cuda())
+    assert loss.shape == () and torch.equal(lse, both["lse"][0])
+
+
+def test_loss_autograd_streams_and_graph(ps):
+    h, table, targets, dloss = _inputs(200, 900, 96, torch.bfloat16, 11)
+    val, tol = cross_entropy(h, table, targets, 0.5, dloss)
+    a, b = h.cuda().requires_grad_(), table.cuda().requires_grad_()
+    loss = ps.linear_cross_entropy(a, b, targets.cuda(), 0.5)
+    (loss * dloss.cuda()).sum().backward()
+    check("loss", loss, val["loss"], tol["loss"])
+    check("dh", a.grad, val["dh"], tol["dh"])
+    check("dtable", b.grad, val["dtable"], tol["dtable"])
+    s = torch.cuda.Stream()
+    c = [t.cuda() for t in (h, table, targets, dloss)]
+    s.wait_stream(torch.cuda.current_stream())
+    loss, lse = ps.linear_cross_entropy_forward(*c[:3], 0.5, stream=s)
+    dh, dtable = ps.linear_cross_entropy_backward(c[3], *c[:3], lse, 0.5, stream=s)
+    s.synchronize()
+    check("dh", dh, val["dh"], tol["dh"])
+
+    def step():
+        loss, lse = ps.linear_cross_entropy_forward(*c[:3], 0.5)
+        return (loss, lse) + ps.linear_cross_entropy_backward(c[3], *c[:3], lse, 0.5)
+
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for k in range(4):
+        for t, new in zip(c, _inputs(200, 900, 96, torch.bfloat16, 20 + k)):
+            t.copy_(new)
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(held, want)), k
+
+
+def test_loss_against_differences(ps):
+    """The summed loss's change along a direction against the gradients.  The step's truncation
+    error is the oracle's at the same step; a loss is off by at most its bound."""
+    h, table, targets, dloss = _inputs(40, 60, 24, torch.float32, 13)
+    g, rnd = _rnd(14)
+    got = _run(ps, h, table, targets, dloss)
+    val, tol = cross_entropy(h, table, targets, 1.0, dloss)
+    step = 2.0 ** -5
+    live = dloss.double() * ((targets >= 0) & (targets < 60))
+    for name, way in (("dh", rnd(40, 24)), ("dtable", rnd(60, 24))):
+        def at(s):
+            return (h + s * way if name == "dh" else h), (table + s * way if name != "dh" else table)
+
+        def gpu(s):
+            a, b = at(s)
+            loss, _ = ps.linear_cross_entropy_forward(a.cuda(), b.cuda(), targets.cuda())
+            return float((loss.double().cpu() * live).sum())
+
+        def oracle(s):
+            v, t = cross_entropy(*at(s), targets, 1.0)
+            return float((v["loss"] * live).sum()), float((t["loss"] * live).sum())
+
+        (hi, hi_tol), (lo, lo_tol) = oracle(step), oracle(-step)
+        truncation = abs((hi - lo) / (2 * step) - float((val[name] * way.double()).sum()))
+        slope = float((got[name].double().cpu() * way.double()).sum())
+        bound = truncation + (hi_tol + lo_tol) / (2 * step) + \
+            float((tol[name] * way.double().abs()).sum())
+        assert abs((gpu(step) - gpu(-step)) / (2 * step) - slope) <= bound
+
+
+def test_loss_with_the_input_table(ps):
+    """A table at both ends: the lookup's gradient is added to the loss's."""
+    g, rnd = _rnd(15)
+    table = (rnd(80, 32) * 0.3).half()
+    ids, targets = torch.randint(80, (50,), generator=g), torch.randint(-1, 80, (50,), generator=g)
+    w = [t.cuda().requires_grad_() for t in (table, table)]
+    for tied in (False, True):
+        first, last = (w[0], w[0]) if tied else w
+        for t in w:
+            t.grad = None
+        hidden = ps.embed(ids.cuda(), first, 4.0)
+        ps.linear_cross_entropy(hidden, last, targets.cuda()).sum().backward()
+        if not tied:
+            separate = [t.grad.clone() for t in w]
+    # torch rounds the sum of the two once more
+    both = separate[0].double() + separate[1].double()
+    assert float((w[0].grad.double() - both).abs().max()) <= 2.0 ** -11 * float(both.abs().max())
+    with torch.no_grad():
+        hidden = ps.embed_forward(ids.cuda(), w[0], 4.0)
+        _, lse = ps.linear_cross_entropy_forward(hidden, w[0], targets.cuda())
+        dh, dtable = ps.linear_cross_entropy_backward(torch.ones(50).cuda(), hidden, w[0],
+                                                      targets.cuda(), lse)
+        ps.embed_backward(dh, ids.cuda(), 80, 4.0, into=dtable)
+    assert float((dtable.double() - both).abs().max()) <= 2.0 ** -10 * float(both.abs().max())
+
+
+def test_loss_refusals(ps):
+    h, table, targets = torch.zeros(3, 8).cuda(), torch.zeros(5, 8).cuda(), torch.zeros(3).long().cuda()
+    f = ps.linear_cross_entropy_forward
+    for bad in ((h, table.half(), targets), (h.double(), table.double(), targets),
+                (h, table, targets.float())):
+        with pytest.raises(TypeError):
+            f(*bad)
+    for bad in ((h.cpu(), table, targets), (h, table.cpu(), targets), (h, table, targets.cpu()),
+                (h, table[:, :7], targets), (h, table[0], targets), (h, table[:0], targets),
+                (h, table, targets[:2])):
+        with pytest.raises(ValueError):
+            f(*bad)
+    for scale in (0.0, -1.0, math.inf, math.nan):
+        with pytest.raises(ps.SieveError):
+            f(h, table, targets, scale)
+    with pytest.raises(ps.SieveError):
+        f(torch.zeros(1, 65537).cuda(), torch.zeros(2, 65537).cuda(), targets[:1])
+    lse = torch.zeros(3).cuda()
+    b = ps.linear_cross_entropy_backward
+    for bad in ((lse[:2], h, table, targets, lse), (lse, h, table, targets, lse.half()),
+                (lse.cpu(), h, table, targets, lse), (lse.half(), h, table, targets, lse)):
+        with pytest.raises(ValueError):
+            b(*bad)
+    with pytest.raises(ps.SieveError):
+        b(lse, h, table, targets, lse, 0.0)

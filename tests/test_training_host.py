@@ -52,3 +52,41 @@ def test_embed_argument_errors_without_a_gpu(lib):
     assert 16 * 65536 < lib.sieve_embed_workspace(65536, 50000, 1024) < \
         16 * 65536 + 65536 * 1024 * 4 // 31 + (1 << 20)
     assert lib.sieve_embed_workspace((1 << 31) - 1, (1 << 31) - 2, 65536) > 0
+
+
+def test_loss_argument_errors_without_a_gpu(lib):
+    def forward(h=P, hs=8, table=P, ts=8, dt=0, rows=4, vocab=5, n=8, targets=P, size=8, scale=1.0,
+                lse=P, ws=P, bytes=1 << 40):
+        return lib.sieve_loss_forward(h, hs, table, ts, dt, rows, vocab, n, targets, size, scale, P,
+                                      lse, ws, bytes, NONE)
+
+    assert forward(dt=3) == -1 and b"dtype" in lib.sieve_last_error()
+    assert forward(rows=-1) == -1 and forward(vocab=0) == -1 and forward(n=0) == -1
+    assert forward(n=65537, hs=65537, ts=65537) == -4
+    assert forward(rows=(1 << 24) + 1) == -4 and forward(vocab=(1 << 24) + 1) == -4
+    assert forward(h=NONE) == -1 and forward(table=NONE) == -1 and forward(targets=NONE) == -1
+    assert forward(lse=NONE) == -1
+    assert forward(size=2) == -1 and b"target_bytes" in lib.sieve_last_error()
+    assert forward(hs=7) == -1 and forward(ts=7) == -1
+    for scale in (0.0, -1.0, float("inf"), float("nan")):
+        assert forward(scale=scale) == -1 and b"scale" in lib.sieve_last_error()
+    assert forward(ws=NONE) == -1 and forward(ws=ctypes.c_void_p(0x1008)) == -1
+    assert forward(bytes=16) == -1 and b"workspace" in lib.sieve_last_error()
+    assert forward(rows=0, h=NONE, targets=NONE, ws=NONE) == 0
+
+    def backward(dloss=P, h=P, table=P, rows=4, lse=P, scale=1.0, dh=P, dtable=P, ws=P,
+                 bytes=1 << 40, dt=0, vocab=5):
+        return lib.sieve_loss_backward(dloss, h, 8, table, 8, dt, rows, vocab, 8, P, 8, lse, scale,
+                                       dh, dtable, ws, bytes, NONE)
+
+    assert backward(dt=-1) == -1 and backward(vocab=0) == -1
+    assert backward(dloss=NONE) == -1 and backward(lse=NONE) == -1 and backward(h=NONE) == -1
+    assert backward(scale=0.0) == -1 and backward(ws=NONE) == -1 and backward(bytes=16) == -1
+    assert backward(dh=NONE, dtable=NONE) == 0
+    assert backward(rows=0, dtable=NONE, ws=NONE) == 0
+    assert lib.sieve_loss_workspace(4, 5, 8, 0, 2) == -1
+    assert lib.sieve_loss_workspace(4, 5, 8, 7, 0) == -1
+    assert lib.sieve_loss_workspace(0, 5, 8, 0, 1) == 0
+    # no logits: a large vocabulary takes no more than some pieces of its gradients
+    assert lib.sieve_loss_workspace(8192, 1 << 20, 768, 2, 0) < 8192 * (1 << 20) * 2 // 16
+    assert lib.sieve_loss_workspace(8192, 1 << 20, 768, 2, 1) < 8192 * (1 << 20) * 2 // 16

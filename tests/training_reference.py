@@ -36,3 +36,62 @@ def embed(ids, table, scale, dtype, dy=None, into=None):
     val["dtable"] = total
     tol["dtable"] = UNIT[out] * total.abs() + (1 + UNIT[out]) * steps * E * size + TINY[out]
     return val, tol
+
+
+def cross_entropy(h, table, targets, scale, dloss=None):
+    """({name: value}, {name: bound}) of loss and lse, and of dh and dtable with dloss."""
+    dt, n, vocab = h.dtype, h.shape[1], table.shape[0]
+    u, c = UNIT[dt], float(torch.tensor(scale, dtype=torch.float32))
+    x, w = h.double(), table.double()
+    live = (targets >= 0) & (targets < vocab)
+    at = targets.long().clamp(0, vocab - 1)
+    s = c * (x @ w.T)
+    # a logit: n products of 16-bit values, exact, or 6 n of 32-bit values' parts, added in fp32
+    # (2 E each: the matrix units need not round to nearest); the parts left out are below 8 E
+    terms = (6 * n + 16) * 2 * E if dt is torch.float32 else (n + 16) * 2 * E
+    ds = c * (x.abs() @ w.abs().T) * (terms + 8 * E) + 4 * E * s.abs()
+    lse = torch.logsumexp(s, 1)
+    # exponentials and the logarithm to 2^-21, sums of up to vocab of them
+    many = (min(vocab, 300) + vocab / 256 + 16) * E
+    d_lse = ds.max(1).values + 2.0 ** -20 + many + 4 * E * (lse.abs() + s.abs().max(1).values)
+    own = s.gather(1, at[:, None])[:, 0]
+    loss = torch.where(live, lse - own, 0.0)
+    val = {"lse": lse, "loss": loss}
+    tol = {"lse": d_lse, "loss": (d_lse + ds.gather(1, at[:, None])[:, 0] + 4 * E * own.abs()) * live}
+    if dloss is None:
+        return val, tol
+    weight = torch.where(live, dloss.double(), 0.0)
+    p = torch.exp(s - lse[:, None])
+    one = torch.zeros_like(p)
+    one[torch.arange(len(at)), at] = 1.0
+    g = (p - one) * weight[:, None]
+    d_p = p * (ds + d_lse[:, None] + 2.0 ** -20 + 4 * E * (s.abs() + lse.abs()[:, None]))
+    # rounded to the inputs' type; binary16 times 2^14 and the mantissa of dloss
+    d_g = (1 + u) * d_p * weight.abs()[:, None] + (u + 4 * E) * g.abs()
+    # an exponential below fp32's normal range (2^-126) may be zero, and so may g, or a part of it
+    # that a matrix unit reads, below that of its type
+    d_g = d_g + 2.0 ** -126 * (weight.abs()[:, None] + 3)
+    if dt is torch.float16:
+        d_g = d_g + 2.0 ** -39 * weight.abs()[:, None]
+
+    def product(a, d_a, b, k):
+        total = a @ b
+        size, far = a.abs() @ b.abs(), d_a @ b.abs()
+        parts = 6 * k if dt is torch.float32 else k
+        e = c * (far + ((parts + 16) * 2 + 16) * E * (size + far))
+        return c * total, e + u * (c * total.abs() + e) + TINY[dt]
+
+    val["dh"], tol["dh"] = product(g, d_g, w, vocab)
+    held = torch.where(weight[:, None] != 0, x, 0.0)
+    val["dtable"], tol["dtable"] = product(g.T, d_g.T, held, len(at))
+    if dt is torch.float16:
+        # rows of far smaller weight may fall below the type's normal range
+        top = weight.abs().max() if len(at) else 0.0
+        tol["dtable"] = tol["dtable"] + c * top * 2.0 ** -23 * (g != 0).sum(0)[:, None]
+    return val, tol
+
+
+def near(name, got, want, bound):
+    """Whether the error's norm is at most ``bound`` times the value's."""
+    d = float((got.detach().double().cpu() - want).norm())
+    assert d <= bound * float(want.norm()), f"{name}: off by {d / float(want.norm()):.3g}"
