@@ -564,6 +564,33 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
 SIEVE_API int64_t sieve_loss_workspace(int64_t rows, int64_t vocab, int32_t n, int32_t dtype,
                                        int32_t backward);
 
+/*
+ * sieve_orthogonalize -- each of a stack of matrices made nearly orthogonal, as an optimizer
+ * does with the momentum of a layer's weights.
+ *   x = g / (|g| + eps) with |g| the root of the sum of the matrix's squares, then `steps`
+ *   times x = a x + b (x x^T) x + c (x x^T)^2 x, which maps each singular value s in [0, 1] to
+ *   a s + b s^3 + c s^5 and leaves the singular vectors; rounded to dtype once.
+ *   g            [batch, m, n] of dtype, matrices batch_stride and rows row_stride (>= n)
+ *                values apart.
+ *   steps        0 .. 1000.
+ *   coefficients HOST [3]: a, b, c, with which singular values that start in [0, 1] stay below
+ *                3.9, and p(s) / s below 15.9 (else SIEVE_EUNSUPPORTED): 3.4445, -4.775, 2.0315
+ *                for a few steps, or 1.875, -1.25, 0.375, which converge.
+ *   eps          >= 0 and finite.
+ *   x            [batch, m, n] of dtype, contiguous (may be a contiguous g).
+ *   workspace    device memory of sieve_orthogonalize_workspace(batch, m, n) bytes, 16-byte
+ *                aligned (only used in the call).
+ * Between the steps matrices are kept to 24 bits and products summed in fp32 whatever dtype is;
+ * the sum of squares is in 64 bits.  batch >= 0, 1 <= m, n <= 65536 (above these
+ * SIEVE_EUNSUPPORTED).
+ */
+SIEVE_API int sieve_orthogonalize(const void* g, int64_t batch_stride, int64_t row_stride,
+                                  int32_t dtype, int64_t batch, int64_t m, int64_t n,
+                                  int32_t steps, const float* coefficients, float eps, void* x,
+                                  void* workspace, int64_t workspace_bytes, void* stream);
+/* Bytes that sieve_orthogonalize needs, or a negative sieve_status. */
+SIEVE_API int64_t sieve_orthogonalize_workspace(int64_t batch, int64_t m, int64_t n);
+
 /* Release an index and its cached workspace.  NULL is a no-op. */
 SIEVE_API void sieve_free_index(sieve_index* idx);
 

@@ -20,7 +20,7 @@ __all__ = ["SieveError", "Index", "Stats", "Round", "load_library", "LIB_PATH", 
            "LOOKAHEAD_SERIAL", "LOOKAHEAD_SPECULATIVE", "AttentionPlan", "BF16", "attention",
            "layer_norm", "layer_norm_backward", "layer_norm_forward", "embed", "embed_backward",
            "embed_forward", "linear_cross_entropy", "linear_cross_entropy_backward",
-           "linear_cross_entropy_forward"]
+           "linear_cross_entropy_forward", "orthogonalize"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsieve.so")
 W_INF = 0x7FFFFFFF
@@ -352,4 +352,5 @@ def search_multi_calibrated(indexes, queries: torch.Tensor, exclude_ids: Optiona
 from .encoder import (AttentionPlan, BF16, attention, layer_norm, layer_norm_backward,  # noqa: E402
                       layer_norm_forward)
 from .training import (embed, embed_backward, embed_forward, linear_cross_entropy,  # noqa: E402
-                       linear_cross_entropy_backward, linear_cross_entropy_forward)
+                       linear_cross_entropy_backward, linear_cross_entropy_forward,
+                       orthogonalize)

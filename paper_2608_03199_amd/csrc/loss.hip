@@ -37,7 +37,7 @@ typedef mm_f16 f16;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kBM = 256, kBN = 128;       // a tile's vectors and rows (or rows and columns)
-constexpr int kHigh = 8;                  // tiles of m before the next of n, see mm_tile_of
+constexpr int kHigh = 8;                  // tiles of m before the next of n, see mm_tile_at
 constexpr int64_t kMaxRows = 1 << 24;     // of h, and of the table
 constexpr int kMaxN = 65536;
 constexpr int64_t kPieceValues = 1 << 27;  // of g
@@ -120,7 +120,7 @@ template <typename T>
 __global__ __launch_bounds__(kMmThreads, 2) void loss_forward_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   uint32_t tm, tn;
-  mm_tile_of(blockIdx.x, a.tiles_m, a.tiles_n, kHigh, tm, tn);
+  mm_tile_at(mm_place_of(blockIdx.x, gridDim.x), a.tiles_m, a.tiles_n, kHigh, tm, tn);
   const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
   typedef MmTile<T, kBM, kBN, false, false> Tile;
   Tile t;
@@ -295,7 +295,7 @@ template <typename F, typename T>
 __global__ __launch_bounds__(kMmThreads, 2) void loss_gradient_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   uint32_t tm, tn;
-  mm_tile_of(blockIdx.x, a.tiles_m, a.tiles_n, kHigh, tm, tn);
+  mm_tile_at(mm_place_of(blockIdx.x, gridDim.x), a.tiles_m, a.tiles_n, kHigh, tm, tn);
   const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
   typedef MmTile<T, kBM, kBN, false, false> Tile;
   Tile t;
@@ -377,8 +377,9 @@ __global__ __launch_bounds__(kMmThreads, 2) void loss_product_kernel(Product a) 
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   const uint32_t tiles = a.tiles_m * a.tiles_n;
   uint32_t tm, tn;
-  mm_tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n, kHigh, tm, tn);
-  const int64_t split = blockIdx.x / tiles;
+  const uint32_t place = mm_place_of(blockIdx.x, gridDim.x);
+  mm_tile_at(place % tiles, a.tiles_m, a.tiles_n, kHigh, tm, tn);
+  const int64_t split = place / tiles;
   const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
   const int64_t k0 = split * a.per, k1 = k0 + a.per < a.k ? k0 + a.per : a.k;
   typedef MmTile<T, kBM, kBN, kAcrossA, true> Tile;

@@ -249,16 +249,18 @@ struct MmTile {
   }
 };
 
-// The tile of a work-group: consecutive work-groups go to the chip's eight dies in turn, each
-// with an L2 of its own, so a die takes a run of tiles, and runs go through `high` tiles of m
-// before the next of n.
-__device__ __forceinline__ void mm_tile_of(uint32_t index, uint32_t tiles_m, uint32_t tiles_n,
+// The place of a work-group among `all`: consecutive work-groups go to the chip's eight dies in
+// turn, each with an L2 of its own, so a die takes a run of places.
+__device__ __forceinline__ uint32_t mm_place_of(uint32_t index, uint32_t all) {
+  const uint32_t each = all / 8, more = all % 8, die = index % 8;
+  return die * each + (die < more ? die : more) + index / 8;
+}
+
+// The tile at a place: runs go through `high` tiles of m before the next of n.
+__device__ __forceinline__ void mm_tile_at(uint32_t place, uint32_t tiles_m, uint32_t tiles_n,
                                            uint32_t high, uint32_t& tm, uint32_t& tn) {
-  const uint32_t all = tiles_m * tiles_n, each = all / 8, more = all % 8;
-  const uint32_t die = index % 8, place = index / 8;
-  const uint32_t i = die * each + (die < more ? die : more) + place;
   const uint32_t strip = high * tiles_n;
-  const uint32_t s = i / strip, in = i % strip;
+  const uint32_t s = place / strip, in = place % strip;
   const uint32_t rows = tiles_m - s * high < high ? tiles_m - s * high : high;
   tm = s * high + in % rows;
   tn = in / rows;

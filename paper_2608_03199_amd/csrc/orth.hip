@@ -1,0 +1,381 @@
+// orth.hip -- a stack of matrices made nearly orthogonal by a polynomial iteration, as an
+// optimizer does with the momentum of a layer's weights.
+//
+//   X = G / (|G| + eps),  then `steps` times  X <- B X,  B = a I + b A + c A A,  A = X X^T
+//
+// (with |G| the root of the sum of squares; matrices taller than wide: A = X^T X, X <- X B).  Each
+// step maps every singular value s of X to a s + b s^3 + c s^5 and leaves the singular vectors.
+//
+// A step is three products and nothing else: A and A A are symmetric, so only the tiles on and
+// below the diagonal are computed and written to both sides; B is made in the epilogue of A A,
+// with a on its diagonal, so that the third product's accumulators are the next X.
+//
+// What is weak in G is multiplied by up to a^steps (484 for the usual five), and rounding errors
+// with it, so 16-bit values are not enough between the products, whatever G's type is.  Every
+// matrix is kept as two binary16 parts, hi = round(v), lo = round(v - hi): 24 bits together, and
+// a product is hi hi + hi lo + lo hi, summed in fp32.  That is fp32's precision at a third of
+// the 16-bit rate, 5 times the fp32 matrix rate.  All values are bounded by singular values, so
+// fixed powers of two keep them in binary16's range (kScale): |X| below 4, |A| and |B| below 16,
+// which the host checks for the coefficients that it is given.
+//
+// The matrix units bound it from some 256 x 256 on, launches below.
+#include <math.h>
+
+#include <algorithm>
+
+#include "mm_tile.h"
+#include "once_per_device.h"
+
+using namespace sieve;
+
+namespace {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+constexpr int kTileSize = 128;
+constexpr float kScaleX = 16384.f, kScaleA = 4096.f;  // of X; of A and B
+constexpr double kMaxX = 3.9, kMaxA = 15.9;           // below 65504 times these
+constexpr int kMaxSide = 65536;
+constexpr int kMaxSteps = 1000;
+constexpr int kSums = 64;                             // parts of a matrix's sum of squares
+constexpr int64_t kMostBytes = int64_t(1) << 31;      // of the workspace, for one matrix or more
+
+struct Source {
+  const void* g;
+  int64_t batch_stride, row_stride;
+  int64_t m, n, pitch;
+  float eps;
+  double* sums;          // [matrix][kSums]
+  f16* x;                // [plane][matrix][m][pitch]
+  int64_t plane;
+  void* out;             // without steps: the result
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void orth_norm_kernel(Source a) {
+  __shared__ double s[4];
+  const T* g = (const T*)a.g + blockIdx.y * a.batch_stride;
+  double sum = 0.0;
+  for (int64_t row = blockIdx.x; row < a.m; row += kSums)
+    for (int64_t col = threadIdx.x; col < a.n; col += 256) {
+      const double v = (double)(float)g[row * a.row_stride + col];
+      sum += v * v;
+    }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) a.sums[blockIdx.y * kSums + blockIdx.x] = s[0] + s[1] + s[2] + s[3];
+}
+
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
+  hi = (f16)v;
+  lo = (f16)(v - (float)hi);
+}
+
+// X of the matrix, zeros up to the pitch.
+template <typename T, bool kOut>
+__global__ __launch_bounds__(256) void orth_scale_kernel(Source a) {
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) sum += a.sums[blockIdx.y * kSums + i];
+  const double inv = 1.0 / (sqrt(sum) + (double)a.eps);
+  const T* g = (const T*)a.g + blockIdx.y * a.batch_stride;
+  const int64_t width = kOut ? a.n : a.pitch;
+  for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
+    const int64_t at = (blockIdx.y * a.m + row) * width;
+    for (int64_t col = threadIdx.x; col < width; col += 256) {
+      const float v =
+          col < a.n ? (float)((double)(float)g[row * a.row_stride + col] * inv) : 0.f;
+      if constexpr (kOut) ((T*)a.out)[at + col] = (T)v;
+      else split(v * kScaleX, a.x[at + col], a.x[a.plane + at + col]);
+    }
+  }
+}
+
+// One product of a step, for every matrix.
+struct Product {
+  MmOperand a, b;        // of the first matrix
+  int64_t a_next, b_next;
+  int64_t k;
+  int64_t rows, cols;    // that are written: zeros past the matrix's, up to the pitch
+  int64_t side;
+  uint32_t tiles, tiles_m, tiles_n;  // tiles of a matrix
+  float fa, fb, fc;      // B's coefficients
+  const f16* gram;       // A, for B
+  void* out;             // planes or the result
+  int64_t pitch, next, plane;
+};
+
+enum { kGram, kPolynomial, kUpdate, kLast };
+
+template <typename T, int kKind, bool kAcrossA, bool kAcrossB>
+__global__ __launch_bounds__(kMmThreads, 3) void orth_product_kernel(Product a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+  const uint32_t place = mm_place_of(blockIdx.x, gridDim.x);
+  const int64_t matrix = place / a.tiles;
+  const uint32_t in = place % a.tiles;
+  uint32_t tm, tn;
+  if constexpr (kKind == kGram || kKind == kPolynomial) {
+    // tiles on and below the diagonal, row by row
+    tm = (uint32_t)((sqrtf(8.f * in + 1.f) - 1.f) * 0.5f);
+    while (tm * (tm + 1) / 2 > in) --tm;
+    while ((tm + 1) * (tm + 2) / 2 <= in) ++tm;
+    tn = in - tm * (tm + 1) / 2;
+  } else {
+    mm_tile_at(in, a.tiles_m, a.tiles_n, 8, tm, tn);
+  }
+  const int64_t m0 = (int64_t)tm * kTileSize, n0 = (int64_t)tn * kTileSize;
+  MmOperand x = a.a, y = a.b;
+  x.p = (const f16*)x.p + matrix * a.a_next;
+  y.p = (const f16*)y.p + matrix * a.b_next;
+  typedef MmTile<f16, kTileSize, kTileSize, kAcrossA, kAcrossB> Tile;
+  Tile t;
+  t.run(x, m0, y, n0, 0, a.k, 3,
+        (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_memory);
+  const int64_t first = matrix * a.next;
+#pragma unroll
+  for (int j = 0; j < Tile::kJ; ++j) {
+    const int64_t n = n0 + mm_col<kTileSize>(j);
+#pragma unroll
+    for (int i = 0; i < Tile::kI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int64_t m = m0 + mm_row<kTileSize>(i, r);
+        if (m >= a.rows || n >= a.cols) continue;
+        float v = t.acc[i][j][r];
+        if constexpr (kKind == kLast) {
+          ((T*)a.out)[first + m * a.pitch + n] = (T)(v * (1.f / (kScaleA * kScaleX)));
+        } else if constexpr (kKind == kUpdate) {
+          f16* p = (f16*)a.out + first + m * a.pitch + n;
+          split(v * (1.f / kScaleA), p[0], p[a.plane]);
+        } else {
+          // one value for both sides: the lower one's
+          if (m < n) continue;
+          f16* p = (f16*)a.out + first;
+          const int64_t at = m * a.pitch + n, mirror = n * a.pitch + m;
+          if constexpr (kKind == kGram) {
+            v *= kScaleA / (kScaleX * kScaleX);
+          } else {
+            const f16* g = a.gram + first + at;
+            v = a.fc * (v * (1.f / kScaleA)) + a.fb * ((float)g[0] + (float)g[a.plane]);
+            if (m == n && m < a.side) v += a.fa * kScaleA;
+          }
+          f16 hi, lo;
+          split(v, hi, lo);
+          p[at] = p[mirror] = hi;
+          p[a.plane + at] = p[a.plane + mirror] = lo;
+        }
+      }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
+
+struct Layout {
+  int64_t side, pitch, side_pitch;  // of A and B; of X's rows; of A's and B's rows
+  int64_t batch;                    // matrices at a time
+  int64_t sums, x[2], gram, poly, bytes;
+};
+
+Layout layout_of(int64_t batch, int64_t m, int64_t n) {
+  Layout l{};
+  l.side = std::min(m, n);
+  l.pitch = (n + 7) & ~int64_t(7);
+  l.side_pitch = (l.side + 7) & ~int64_t(7);
+  const int64_t one = 2 * 2 * 2 * (m * l.pitch + l.side_pitch * l.side_pitch);
+  // a launch's work-groups have fewer than 2^32 threads
+  const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128);
+  l.batch = std::max<int64_t>(1, std::min({batch, kMostBytes / one, (int64_t(1) << 23) / tiles,
+                                           int64_t(65535)}));
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t was = at;
+    at += round256(bytes);
+    return was;
+  };
+  l.sums = take(l.batch * kSums * 8);
+  for (int i = 0; i < 2; ++i) l.x[i] = take(l.batch * m * l.pitch * 4);
+  l.gram = take(l.batch * l.side_pitch * l.side_pitch * 4);
+  l.poly = take(l.batch * l.side_pitch * l.side_pitch * 4);
+  l.bytes = at;
+  return l;
+}
+
+// Whether all values stay in range: singular values start in [0, 1], and a step maps
+// [0, s] into [0, max |p|] with p(x) = a x + b x^3 + c x^5; B's are p(x) / x.
+bool in_range(double a, double b, double c, int steps) {
+  double s = 1.0;
+  for (int i = 0; i < steps; ++i) {
+    auto p = [&](double x) { return fabs(x * (a + x * x * (b + x * x * c))); };
+    auto q = [&](double x2) { return fabs(a + x2 * (b + x2 * c)); };
+    double top = p(s), most = std::max(q(0.0), q(s * s));
+    if (c != 0.0) {
+      const double at = -b / (2.0 * c);
+      if (at > 0.0 && at < s * s) most = std::max(most, q(at));
+    }
+    // p' = a + 3 b x^2 + 5 c x^4
+    double roots[2] = {-1.0, -1.0};
+    if (c != 0.0) {
+      const double d = 9.0 * b * b - 20.0 * a * c;
+      if (d >= 0.0) {
+        roots[0] = (-3.0 * b + sqrt(d)) / (10.0 * c);
+        roots[1] = (-3.0 * b - sqrt(d)) / (10.0 * c);
+      }
+    } else if (b != 0.0) {
+      roots[0] = -a / (3.0 * b);
+    }
+    for (double r : roots)
+      if (r > 0.0 && r < s * s) top = std::max(top, p(sqrt(r)));
+    if (!(s * s <= kMaxA && most <= kMaxA && top <= kMaxX)) return false;
+    s = top;
+  }
+  return true;
+}
+
+int check_orth(int64_t batch, int64_t m, int64_t n) {
+  if (batch < 0) return set_error(SIEVE_EINVAL, "batch is negative");
+  if (m < 1 || n < 1) return set_error(SIEVE_EINVAL, "m and n must be >= 1");
+  if (m > kMaxSide || n > kMaxSide)
+    return set_error(SIEVE_EUNSUPPORTED, "m or n is above %d", kMaxSide);
+  return SIEVE_OK;
+}
+
+constexpr int kLds = MmTile<f16, kTileSize, kTileSize, false, false>::kLds;
+static_assert(kLds <= 65536, "no larger LDS has to be asked for");
+
+template <typename T>
+void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t m,
+         int64_t n, int steps, const float* coefficients, float eps, void* out, char* w,
+         const Layout& l, hipStream_t s) {
+  const bool tall = m > n;
+  Source src{g, batch_stride, row_stride, m, n, l.pitch, eps, (double*)(w + l.sums),
+             (f16*)(w + l.x[0]), batch * m * l.pitch, out};
+  orth_norm_kernel<T><<<dim3(kSums, (uint32_t)batch), 256, 0, s>>>(src);
+  const dim3 rows((uint32_t)std::min<int64_t>(m, 1024), (uint32_t)batch);
+  if (steps == 0) {
+    orth_scale_kernel<T, true><<<rows, 256, 0, s>>>(src);
+    return;
+  }
+  orth_scale_kernel<T, false><<<rows, 256, 0, s>>>(src);
+  const int64_t side = l.side, sp = l.side_pitch;
+  const int64_t square = sp * sp;
+  const uint32_t ts = (uint32_t)((side + kTileSize - 1) / kTileSize);
+  f16 *gram = (f16*)(w + l.gram), *poly = (f16*)(w + l.poly);
+  const MmOperand of_a{gram, sp, side, batch * square}, of_b{poly, sp, side, batch * square};
+  for (int i = 0; i < steps; ++i) {
+    const f16* x = (const f16*)(w + l.x[i & 1]);
+    f16* to = (f16*)(w + l.x[(i + 1) & 1]);
+    const bool last = i == steps - 1;
+    const uint32_t half = ts * (ts + 1) / 2;
+    // A: over the longer side
+    Product p{};
+    p.a = p.b = {x, l.pitch, side, src.plane};
+    p.a_next = p.b_next = m * l.pitch;
+    p.k = tall ? m : n;
+    p.rows = p.cols = sp;
+    p.side = side;
+    p.tiles = half;
+    p.out = gram;
+    p.pitch = sp;
+    p.next = square;
+    p.plane = batch * square;
+    if (tall)
+      orth_product_kernel<T, kGram, true, true>
+          <<<half * (uint32_t)batch, kMmThreads, kLds, s>>>(p);
+    else
+      orth_product_kernel<T, kGram, false, false>
+          <<<half * (uint32_t)batch, kMmThreads, kLds, s>>>(p);
+    // B
+    p.a = p.b = of_a;
+    p.a_next = p.b_next = square;
+    p.k = side;
+    p.fa = coefficients[0];
+    p.fb = coefficients[1];
+    p.fc = coefficients[2];
+    p.gram = gram;
+    p.out = poly;
+    orth_product_kernel<T, kPolynomial, false, false>
+        <<<half * (uint32_t)batch, kMmThreads, kLds, s>>>(p);
+    // the next X, or the result
+    p.a = tall ? MmOperand{x, l.pitch, m, src.plane} : of_b;
+    p.b = tall ? of_b : MmOperand{x, l.pitch, n, src.plane};
+    p.a_next = tall ? m * l.pitch : square;
+    p.b_next = tall ? square : m * l.pitch;
+    p.rows = m;
+    p.cols = last ? n : l.pitch;
+    p.tiles_m = (uint32_t)((m + kTileSize - 1) / kTileSize);
+    p.tiles_n = (uint32_t)((n + kTileSize - 1) / kTileSize);
+    p.tiles = p.tiles_m * p.tiles_n;
+    p.out = last ? out : (void*)to;
+    p.pitch = last ? n : l.pitch;
+    p.next = m * p.pitch;
+    p.plane = src.plane;
+    const uint32_t grid = p.tiles * (uint32_t)batch;
+    if (tall && last)
+      orth_product_kernel<T, kLast, false, false><<<grid, kMmThreads, kLds, s>>>(p);
+    else if (tall)
+      orth_product_kernel<T, kUpdate, false, false><<<grid, kMmThreads, kLds, s>>>(p);
+    else if (last)
+      orth_product_kernel<T, kLast, false, true><<<grid, kMmThreads, kLds, s>>>(p);
+    else
+      orth_product_kernel<T, kUpdate, false, true><<<grid, kMmThreads, kLds, s>>>(p);
+  }
+}
+
+}  // namespace
+
+SIEVE_API int64_t sieve_orthogonalize_workspace(int64_t batch, int64_t m, int64_t n) {
+  clear_error();
+  if (int st = check_orth(batch, m, n)) return st;
+  return batch ? layout_of(batch, m, n).bytes : 0;
+}
+
+SIEVE_API int sieve_orthogonalize(const void* g, int64_t batch_stride, int64_t row_stride,
+                                  int32_t dtype, int64_t batch, int64_t m, int64_t n,
+                                  int32_t steps, const float* coefficients, float eps, void* x,
+                                  void* workspace, int64_t workspace_bytes, void* stream) {
+  clear_error();
+  if (!enc_dtype_ok(dtype))
+    return set_error(SIEVE_EINVAL, "dtype = %d is not one of SIEVE_F32, SIEVE_F16, SIEVE_BF16",
+                     dtype);
+  if (int st = check_orth(batch, m, n)) return st;
+  if (steps < 0) return set_error(SIEVE_EINVAL, "steps is negative");
+  if (steps > kMaxSteps)
+    return set_error(SIEVE_EUNSUPPORTED, "steps = %d is above %d", steps, kMaxSteps);
+  if (!(eps >= 0.f) || eps == INFINITY)
+    return set_error(SIEVE_EINVAL, "eps must be >= 0 and finite");
+  if (!coefficients) return set_error(SIEVE_EINVAL, "coefficients must be non-NULL");
+  for (int i = 0; i < 3; ++i)
+    if (!isfinite(coefficients[i]))
+      return set_error(SIEVE_EINVAL, "coefficients must be finite");
+  if (!in_range(coefficients[0], coefficients[1], coefficients[2], steps))
+    return set_error(SIEVE_EUNSUPPORTED,
+                     "with these coefficients singular values in [0, 1] may grow past %g", kMaxX);
+  if (batch == 0) return SIEVE_OK;
+  if (!g || !x) return set_error(SIEVE_EINVAL, "g and x must be non-NULL");
+  if (row_stride < n || batch_stride < 0)
+    return set_error(SIEVE_EINVAL, "row_stride is below n, or batch_stride negative");
+  const Layout l = layout_of(batch, m, n);
+  if (!workspace || workspace_bytes < l.bytes || ((uintptr_t)workspace & 15))
+    return set_error(SIEVE_EINVAL, "workspace must be 16-byte aligned and hold %lld bytes",
+                     (long long)l.bytes);
+  const int size = enc_size(dtype);
+  for (int64_t z = 0; z < batch; z += l.batch) {
+    const int64_t some = std::min(l.batch, batch - z);
+    const char* from = (const char*)g + z * batch_stride * size;
+    char* to = (char*)x + z * m * n * size;
+    auto go = [&](auto t) {
+      run<decltype(t)>(from, batch_stride, row_stride, some, m, n, steps, coefficients, eps, to,
+                       (char*)workspace, l, (hipStream_t)stream);
+    };
+    if (dtype == SIEVE_F32) go(float{});
+    else if (dtype == SIEVE_F16) go(f16{});
+    else go(bf16{});
+  }
+  ENC_HIP_TRY(hipGetLastError());
+  return SIEVE_OK;
+}

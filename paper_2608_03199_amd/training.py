@@ -1,5 +1,6 @@
 """Operators of libsieve around a text encoder's blocks: the table's lookup, and the cross entropy of
-hidden states against a table, each with its gradient (``include/sieve.h``).
+hidden states against a table, each with its gradient; and the orthogonalised update of the
+matrices between them (``include/sieve.h``).
 
 As in ``encoder.py``, the ``*_forward`` / ``*_backward`` functions marshal the arguments of the
 library's calls, the others join them for torch's autograd, all calls are asynchronous on the
@@ -8,7 +9,7 @@ given or current stream, and there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -18,7 +19,7 @@ from .encoder import _CODES, _code, _here, _need, _on, _ptr, _raw_stream, _rows,
 from .encoder import _library as _encoder_library
 
 __all__ = ["embed", "embed_backward", "embed_forward", "linear_cross_entropy",
-           "linear_cross_entropy_backward", "linear_cross_entropy_forward"]
+           "linear_cross_entropy_backward", "linear_cross_entropy_forward", "orthogonalize"]
 
 _ready = None
 
@@ -44,6 +45,10 @@ def _library():
     lib.sieve_loss_backward.restype = ctypes.c_int
     lib.sieve_loss_backward.argtypes = [P, P, i64, P, i64, i32, i64, i64, i32, P, i32, P, f32, P,
                                         P, P, i64, P]
+    lib.sieve_orthogonalize_workspace.restype = i64
+    lib.sieve_orthogonalize_workspace.argtypes = [i64, i64, i64]
+    lib.sieve_orthogonalize.restype = ctypes.c_int
+    lib.sieve_orthogonalize.argtypes = [P, i64, i64, i32, i64, i64, i64, i32, P, f32, P, P, i64, P]
     _ready = lib
     return lib
 
@@ -257,3 +262,41 @@ def linear_cross_entropy(h: torch.Tensor, table: torch.Tensor, targets: torch.Te
                          scale: float = 1.0) -> torch.Tensor:
     """Differentiable ``linear_cross_entropy_forward``: each row's loss."""
     return _LinearCrossEntropy.apply(h, table, targets, scale)
+
+
+# ---- orthogonalised updates ---------------------------------------------------------------
+
+
+def orthogonalize(g: torch.Tensor, steps: int = 5,
+                  coefficients: Sequence[float] = (3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                  stream=None) -> torch.Tensor:
+    """Each matrix of ``g`` [..., m, n], divided by its norm (+ ``eps``), after ``steps`` times
+    ``x = a x + b (x x^T) x + c (x x^T)^2 x``: its singular vectors with singular values near 1.
+    Of g's shape and dtype; not differentiable."""
+    _need(g.is_cuda, "g must be a GPU tensor")
+    if _here(g.device, stream):
+        return _orthogonalize(g, steps, coefficients, eps)
+    with _on(g.device, stream):
+        return _orthogonalize(g, steps, coefficients, eps)
+
+
+def _orthogonalize(g, steps, coefficients, eps):
+    shape = g.shape
+    _need(len(shape) >= 2 and shape[-1] >= 1 and shape[-2] >= 1,
+          "g must have two last axes of at least one value")
+    code = _code(g, "g")
+    _need(len(coefficients) == 3, "coefficients must be three numbers")
+    lib = _library()
+    m, n = shape[-2:]
+    x = g.detach().reshape(-1, m, n)
+    batch = x.shape[0]
+    if not ((x.stride(2) == 1 or n == 1) and (x.stride(1) >= n or m == 1) and x.stride(0) >= 0):
+        x = x.contiguous()
+    out = g.new_empty(shape, requires_grad=False)
+    need = lib.sieve_orthogonalize_workspace(batch, m, n)
+    space = _workspace(lib, need, g.device)
+    _check(lib, lib.sieve_orthogonalize(
+        _ptr(x), x.stride(0), max(x.stride(1), n), code, batch, m, n, int(steps),
+        (ctypes.c_float * 3)(*coefficients), eps, _ptr(out), _ptr(space), need,
+        _raw_stream(g.device)))
+    return out

@@ -90,3 +90,33 @@ def test_loss_argument_errors_without_a_gpu(lib):
     # no logits: a large vocabulary takes no more than some pieces of its gradients
     assert lib.sieve_loss_workspace(8192, 1 << 20, 768, 2, 0) < 8192 * (1 << 20) * 2 // 16
     assert lib.sieve_loss_workspace(8192, 1 << 20, 768, 2, 1) < 8192 * (1 << 20) * 2 // 16
+
+
+def test_orthogonalize_argument_errors_without_a_gpu(lib):
+    def call(g=P, bs=64, rs=8, dt=0, batch=1, m=8, n=8, steps=5, c=(3.4445, -4.775, 2.0315),
+             eps=1e-7, x=P, ws=P, bytes=1 << 40):
+        three = None if c is None else (ctypes.c_float * 3)(*c)
+        return lib.sieve_orthogonalize(g, bs, rs, dt, batch, m, n, steps, three, eps, x, ws, bytes,
+                                       NONE)
+
+    inf, nan = float("inf"), float("nan")
+    assert call(dt=3) == -1 and call(batch=-1) == -1 and call(m=0) == -1 and call(n=0) == -1
+    assert call(m=65537) == -4 and call(n=65537, rs=65537) == -4
+    assert call(steps=-1) == -1 and call(steps=1001) == -4
+    assert call(eps=-1.0) == -1 and call(eps=nan) == -1 and call(eps=inf) == -1
+    assert call(c=None) == -1 and call(c=(nan, 0, 0)) == -1 and call(c=(1, inf, 0)) == -1
+    assert call(g=NONE) == -1 and call(x=NONE) == -1 and call(rs=7) == -1 and call(bs=-1) == -1
+    assert call(ws=NONE) == -1 and call(ws=ctypes.c_void_p(0x1008)) == -1 and call(bytes=8) == -1
+    assert call(batch=0, g=NONE, x=NONE, ws=NONE) == 0
+    # coefficients with which singular values leave the range: checked for the steps asked for
+    assert call(batch=0, steps=7, c=(1.2, 0, 0)) == 0 and call(batch=0, steps=8, c=(1.2, 0, 0)) == -4
+    assert call(batch=0, c=(16, -30, 14.5)) == -4 and b"singular" in lib.sieve_last_error()
+    assert call(batch=0, steps=1, c=(3.8, 0, 0)) == 0 and call(batch=0, steps=1, c=(4, 0, 0)) == -4
+    assert call(batch=0, steps=1000, c=(1.875, -1.25, 0.375)) == 0
+    assert call(batch=0, steps=1000, c=(3.4445, -4.775, 2.0315)) == 0
+    # a maximum inside [0, 1]: 8 x - 8 x^3 reaches 3.08 at 0.577 and is 0 at both ends
+    assert call(batch=0, steps=1, c=(8, -8, 0)) == 0 and call(batch=0, steps=1, c=(11, -11, 0)) == -4
+    assert lib.sieve_orthogonalize_workspace(0, 8, 8) == 0
+    assert lib.sieve_orthogonalize_workspace(1, 0, 8) == -1
+    # X twice, A and B, each in two parts of 2 bytes
+    assert lib.sieve_orthogonalize_workspace(2, 64, 128) == 2 * 8 * (64 * 128 + 64 * 64) + 1024

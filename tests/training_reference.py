@@ -95,3 +95,26 @@ def near(name, got, want, bound):
     """Whether the error's norm is at most ``bound`` times the value's."""
     d = float((got.detach().double().cpu() - want).norm())
     assert d <= bound * float(want.norm()), f"{name}: off by {d / float(want.norm()):.3g}"
+
+
+def orthogonalize(g, steps, coefficients, eps, dtype=torch.float64):
+    """The iteration in ``dtype``, on matrices as they lie."""
+    a, b, c = coefficients
+    x = g.to(dtype)
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + eps)
+    for _ in range(steps):
+        gram = x @ x.mT if x.shape[-2] <= x.shape[-1] else x.mT @ x
+        poly = b * gram + c * gram @ gram
+        x = a * x + (poly @ x if x.shape[-2] <= x.shape[-1] else x @ poly)
+    return x
+
+
+def orthogonalize_bound(g, steps, coefficients, eps):
+    """(value, bound of the error's norm over the value's).  Rounding errors grow with what is
+    weak in g, and nothing simpler than the iteration itself says by how much: the bound is four
+    times what fp32 arithmetic gets (values of 24 bits in two parts, three of their four products,
+    sums in fp32), and a rounding of the result."""
+    val = orthogonalize(g, steps, coefficients, eps)
+    single = orthogonalize(g, steps, coefficients, eps, torch.float32).double()
+    off = float((single - val).norm() / val.norm())
+    return val, 4 * off + 8 * E + (UNIT[g.dtype] if g.dtype is not torch.float32 else 0.0)
