@@ -6,7 +6,7 @@
 //   dh_t = scale sum_v g_tv w_v,  dw_v = scale sum_t g_tv h_t
 //
 // Forward: tiles of logits stay in accumulators, and what leaves a tile is each row's maximum
-// and sum of exponentials over its 256 vectors; a second kernel joins them.
+// and sum of exponentials over its vectors; a second kernel joins them.
 //
 // Backward: the logits are computed again, a piece of the vocabulary at a time; the piece's g is
 // rounded to 16 bits and kept until both gradients' products have read it (a workspace of at most
@@ -36,7 +36,7 @@ typedef mm_bf16 bf16;
 typedef mm_f16 f16;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kBM = 256, kBN = 128;       // a tile's vectors and rows (or rows and columns)
+constexpr int kStep = 64;                 // values of k a step
 constexpr int kHigh = 8;                  // tiles of m before the next of n, see mm_tile_at
 constexpr int64_t kMaxRows = 1 << 24;     // of h, and of the table
 constexpr int kMaxN = 65536;
@@ -44,6 +44,18 @@ constexpr int64_t kPieceValues = 1 << 27;  // of g
 constexpr int64_t kMaxPiece = 65536;       // vectors
 constexpr int64_t kRowChunk = 65536;       // rows of h in one launch of the forward pass
 constexpr float kHalfScale = 16384.f;      // what g in binary16 is scaled by
+
+// A work-group's tile: one large one has a CU to itself, small ones share it.
+template <int BM_, int BN_, int WM_, int WN_>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM_ * WN_;
+  template <typename T, bool kAcrossA, bool kAcrossB>
+  using Tile = MmTile<T, BM, BN, kAcrossA, kAcrossB, WM, WN, kStep, 2>;
+  static constexpr int kLds = Tile<mm_bf16, false, false>::kLds;
+};
+typedef Shape<256, 256, 2, 4> Large;
+typedef Shape<128, 128, 2, 2> Small;
+constexpr int kSmallest = 128;            // the lesser of the shapes' BM
 
 struct Targets {
   const void* p;
@@ -80,6 +92,13 @@ __device__ __forceinline__ Part join(Part a, Part b) {
   return {top, a.sum * exp2_of(a.top - at) + b.sum * exp2_of(b.top - at)};
 }
 
+// A row's dloss: the mantissa, with its sign, and the power of two; (0, 0) where the row gives
+// no gradient.
+struct Row {
+  float mantissa;
+  int power;
+};
+
 struct Logits {
   MmOperand w, h;        // a piece of the table; the rows
   int64_t v_first;       // the piece's first vector
@@ -90,10 +109,12 @@ struct Logits {
   float c2;              // scale log2(e)
   Targets targets;
   // forward
-  Part* part;            // [tile of 256 vectors][rows]
+  Part* part;            // [tile of vectors][rows]
   float* target_logit;   // [rows], in base 2
   // backward
-  const float *lse, *dloss;
+  const float* lse;
+  const Row* row;        // [rows]
+  float* rest;           // [rows]: what rounding took from the target's g
   void* g;               // [planes][rows][g_stride]
   int64_t g_stride, g_plane;
 };
@@ -116,18 +137,19 @@ __device__ __forceinline__ bool find_value(const f32x16 (&acc)[kI], int64_t rel,
   return found;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kMmThreads, 2) void loss_forward_kernel(Logits a) {
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads, 2) void loss_forward_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   uint32_t tm, tn;
   mm_tile_at(mm_place_of(blockIdx.x, gridDim.x), a.tiles_m, a.tiles_n, kHigh, tm, tn);
-  const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
-  typedef MmTile<T, kBM, kBN, false, false> Tile;
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  typedef typename S::template Tile<T, false, false> Tile;
   Tile t;
   t.run(a.w, m0, a.h, n0, 0, a.k, a.pairs, lds_of(lds_memory));
-  Part* s_part = (Part*)lds_memory;
-  const int wave_m = (int)threadIdx.x >> 7;
-  const int64_t left = a.w.rows - m0 - wave_m * (kBM / 2);  // vectors from the wave's first
+  Part* s_part = (Part*)lds_memory;      // [wave along the vectors][row]
+  constexpr int kWave = S::BM / S::WM;   // vectors of a wave
+  const int wave_m = (int)(threadIdx.x >> 6) / S::WN;
+  const int64_t first = m0 + wave_m * kWave, left = a.w.rows - first;
 #pragma unroll
   for (int j = 0; j < Tile::kJ; ++j) {
     f32x16 acc[Tile::kI];
@@ -135,10 +157,10 @@ __global__ __launch_bounds__(kMmThreads, 2) void loss_forward_kernel(Logits a) {
 #pragma unroll
     for (int i = 0; i < Tile::kI; ++i) {
       acc[i] = t.acc[i][j];
-      if (left < kBM / 2) {
+      if (left < kWave) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (mm_row<kBM>(i, r) - wave_m * (kBM / 2) >= left) acc[i][r] = -INFINITY;
+          if (Tile::row(i, r) - wave_m * kWave >= left) acc[i][r] = -INFINITY;
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][r]);
@@ -151,23 +173,26 @@ __global__ __launch_bounds__(kMmThreads, 2) void loss_forward_kernel(Logits a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum += exp2_of(fmaf(acc[i][r], a.c2, -at));
     sum += other_half(sum);
-    const int col = mm_col<kBN>(j);
+    const int col = Tile::col(j);
     const int64_t row = n0 + col;
     int64_t rel = -1;
     if (row < a.h.rows) {
       const int64_t v = a.targets.at(a.t_first + row);
-      if (v >= 0) rel = v - a.v_first - m0 - wave_m * (kBM / 2);
+      if (v >= 0) rel = v - a.v_first - first;
     }
-    if (__any(rel >= 0 && rel < kBM / 2)) {
+    if (__any(rel >= 0 && rel < kWave)) {
       float x;
       if (find_value(acc, rel, x)) a.target_logit[row] = x * a.c2;
     }
-    if ((threadIdx.x & 32) == 0) s_part[wave_m * kBN + col] = Part{top2, sum};
+    if ((threadIdx.x & 32) == 0) s_part[wave_m * S::BN + col] = Part{top2, sum};
   }
   __syncthreads();
-  if (threadIdx.x < kBN && n0 + threadIdx.x < a.h.rows)
-    a.part[(int64_t)tm * a.h.rows + n0 + threadIdx.x] =
-        join(s_part[threadIdx.x], s_part[kBN + threadIdx.x]);
+  if (threadIdx.x < S::BN && n0 + threadIdx.x < a.h.rows) {
+    Part p = s_part[threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < S::WM; ++i) p = join(p, s_part[i * S::BN + threadIdx.x]);
+    a.part[(int64_t)tm * a.h.rows + n0 + threadIdx.x] = p;
+  }
 }
 
 // Joins the tiles' parts: a work-group takes 32 rows, its 8 groups of 32 threads every 8th tile.
@@ -194,13 +219,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const Part* part, const 
         targets.at(t_first + row) < 0 ? 0.f : (more + (p.top - target_logit[row])) * kLn2;
 }
 
-// A row's dloss as mantissa and power of two; (0, 0) where the row gives no gradient.
-struct Weight {
-  float mantissa;
-  int power;
-};
-__device__ __forceinline__ Weight weight_of(const Targets& targets, const float* dloss,
-                                            int64_t row) {
+__device__ __forceinline__ Row row_of(const Targets& targets, const float* dloss, int64_t row) {
   const float d = dloss[row];
   if (targets.at(row) < 0 || d == 0.f) return {0.f, 0};
   if (!isfinite(d)) return {d, 0};
@@ -209,14 +228,14 @@ __device__ __forceinline__ Weight weight_of(const Targets& targets, const float*
   return {2.f * m, e - 1};
 }
 
-// The largest power of two among the rows' weights, and so at most 2^power times as much weighs
-// each of them.
-__global__ __launch_bounds__(1024) void loss_power_kernel(Targets targets, const float* dloss,
-                                                          int64_t rows, int* power) {
+// The rows' weights, and the largest of their powers of two.
+__global__ __launch_bounds__(1024) void loss_rows_kernel(Targets targets, const float* dloss,
+                                                         int64_t rows, Row* to, int* power) {
   __shared__ int s[16];
   int top = -1000;
   for (int64_t r = threadIdx.x; r < rows; r += 1024) {
-    const Weight w = weight_of(targets, dloss, r);
+    const Row w = row_of(targets, dloss, r);
+    to[r] = w;
     if (w.mantissa != 0.f) top = max(top, w.power);
   }
 #pragma unroll
@@ -242,15 +261,15 @@ __device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
 }
 
 // Rows of n values as the products take them: zeros up to the next multiple of 8, 32-bit values
-// as planes; with dloss each row times its weight's power of two, or zeros where it has none.
+// as planes; with `row` each row times its weight's power of two over the largest, or zeros where
+// it has none.
 struct Pack {
   const void* x;
   int64_t stride, rows;
   int n, k;
   void* to;
   int64_t plane;
-  const float* dloss;
-  Targets targets;
+  const Row* row;
   const int* power;
 };
 
@@ -264,8 +283,8 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
     const int64_t row = i / per;
     const int col = (int)(i % per) * 8;
     float factor = 1.f;
-    if (a.dloss) {
-      const Weight w = weight_of(a.targets, a.dloss, row);
+    if (a.row) {
+      const Row w = a.row[row];
       factor = w.mantissa == 0.f ? 0.f : ldexpf(1.f, w.power - *a.power);
     }
     const T* x = (const T*)a.x + row * a.stride + col;
@@ -291,43 +310,53 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
 
 // g of a piece: the logits' tiles again, each value turned into its gradient.  F: the inputs'
 // type; T: the planes'.
-template <typename F, typename T>
-__global__ __launch_bounds__(kMmThreads, 2) void loss_gradient_kernel(Logits a) {
+template <typename F, typename T, typename S>
+__global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   uint32_t tm, tn;
   mm_tile_at(mm_place_of(blockIdx.x, gridDim.x), a.tiles_m, a.tiles_n, kHigh, tm, tn);
-  const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
-  typedef MmTile<T, kBM, kBN, false, false> Tile;
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  typedef typename S::template Tile<T, false, false> Tile;
   Tile t;
   t.run(a.w, m0, a.h, n0, 0, a.k, a.pairs, lds_of(lds_memory));
-  const int wave_m = (int)threadIdx.x >> 7, half = (int)threadIdx.x >> 5 & 1;
-  const int64_t first = m0 + wave_m * (kBM / 2), left = a.w.rows - first;
+  constexpr int kWave = S::BM / S::WM;
+  const int wave_m = (int)(threadIdx.x >> 6) / S::WN, half = (int)threadIdx.x >> 5 & 1;
+  const int64_t first = m0 + wave_m * kWave;
+  const int left = (int)(a.w.rows - first < kWave ? a.w.rows - first : kWave);
 #pragma unroll
   for (int j = 0; j < Tile::kJ; ++j) {
-    const int64_t row = n0 + mm_col<kBN>(j);
+    const int64_t row = n0 + Tile::col(j);
     const bool there = row < a.h.rows;
-    int64_t rel = -1;
+    int rel = -1;
     float weight = 0.f, lse2 = 0.f;
     if (there) {
-      const int64_t v = a.targets.at(row);
-      if (v >= 0) rel = v - a.v_first - first;
-      weight = weight_of(a.targets, a.dloss, row).mantissa;
+      const int64_t v = a.targets.at(row), at = v - a.v_first - first;
+      if (v >= 0 && at >= 0 && at < kWave) rel = (int)at;
+      weight = a.row[row].mantissa;
       if constexpr (std::is_same_v<F, f16>) weight *= kHalfScale;
       lse2 = a.lse[row] * kLog2e;
     }
-    const bool here = __any(rel >= 0 && rel < kBM / 2);
+    const bool here = __any(rel >= 0);
     T* g = (T*)a.g + row * a.g_stride + first + 8 * half;
 #pragma unroll
     for (int i = 0; i < Tile::kI; ++i) {
       f32x16 x = t.acc[i][j];
+      float own = 0.f;  // the target's g, in its lane
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int v = i * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
         float p = exp2_of(fmaf(x[r], a.c2, -lse2));
-        if (here && rel == v) p -= 1.f;
+        if (here && rel == v) {
+          p -= 1.f;
+          own = p * weight;
+        }
         // a row without weight gives nothing, whatever it holds; nor does what lies past the
         // last vector
         x[r] = weight == 0.f || v >= left ? 0.f : p * weight;
+      }
+      if constexpr (!std::is_same_v<F, float>) {
+        if (here && rel >= i * 32 && rel < i * 32 + 32 && (rel >> 2 & 1) == half)
+          a.rest[row] = own - (float)(T)own;
       }
       // pairs of 16-bit values; halves of a wave change places so that each lane has 8
       // neighbours
@@ -361,40 +390,72 @@ __global__ __launch_bounds__(kMmThreads, 2) void loss_gradient_kernel(Logits a) 
   }
 }
 
-// A gradient's product: out (m, n) in fp32, [split][rows of m][pitch], or added to what is there.
+// What turns a sum of products into a gradient.
+struct Final {
+  void* out;               // [rows][n]
+  int n;
+  float factor;            // scale, over what g was scaled by
+  const int* power;        // dtable: the largest of the rows'
+  const Row* row;          // dh: the row's own; zeros where it has no weight
+  // dh of 16-bit inputs: what rounding took from the target's g, times the target's vector
+  const float* rest;
+  Targets targets;
+  const void* table;
+  int64_t t_stride;
+};
+
+// A gradient's value from its sum.
+template <typename F>
+__device__ __forceinline__ float final_of(const Final& a, int64_t row, int64_t col, float sum) {
+  if (!a.row) return a.power ? ldexpf(sum * a.factor, *a.power) : 0.f;
+  const Row w = a.row[row];
+  if (w.mantissa == 0.f) return 0.f;
+  if (a.rest)
+    sum += a.rest[row] * (float)((const F*)a.table)[a.targets.at(row) * a.t_stride + col];
+  return ldexpf(sum * a.factor, w.power);
+}
+
+// A gradient's product: sums in fp32, [split][rows of m][pitch], or added to what is there; or
+// the gradient itself.
 struct Product {
   MmOperand a, b;
   int64_t k, per;        // values of k, and of a split
   int pairs;
   uint32_t tiles_m, tiles_n;
+  int64_t rows;          // of m, that are written
   float* out;
   int64_t pitch, split;  // values between rows, and between splits
   int add;
+  Final final;
 };
 
-template <typename T, bool kAcrossA>
-__global__ __launch_bounds__(kMmThreads, 2) void loss_product_kernel(Product a) {
+template <typename F, typename T, typename S, bool kAcrossA, bool kFinal>
+__global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   const uint32_t tiles = a.tiles_m * a.tiles_n;
   uint32_t tm, tn;
   const uint32_t place = mm_place_of(blockIdx.x, gridDim.x);
   mm_tile_at(place % tiles, a.tiles_m, a.tiles_n, kHigh, tm, tn);
   const int64_t split = place / tiles;
-  const int64_t m0 = (int64_t)tm * kBM, n0 = (int64_t)tn * kBN;
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
   const int64_t k0 = split * a.per, k1 = k0 + a.per < a.k ? k0 + a.per : a.k;
-  typedef MmTile<T, kBM, kBN, kAcrossA, true> Tile;
+  typedef typename S::template Tile<T, kAcrossA, true> Tile;
   Tile t;
   t.run(a.a, m0, a.b, n0, k0, k1, a.pairs, lds_of(lds_memory));
   float* out = a.out + split * a.split;
 #pragma unroll
   for (int j = 0; j < Tile::kJ; ++j) {
-    const int64_t n = n0 + mm_col<kBN>(j);
+    const int64_t n = n0 + Tile::col(j);
+    if (n >= a.b.rows) continue;
 #pragma unroll
     for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + mm_row<kBM>(i, r);
-        if (m < a.a.rows && n < a.b.rows) {
+        const int64_t m = m0 + Tile::row(i, r);
+        if (m >= a.rows) continue;
+        if constexpr (kFinal) {
+          ((F*)a.final.out)[m * a.final.n + n] = (F)final_of<F>(a.final, m, n, t.acc[i][j][r]);
+        } else {
           float* p = out + m * a.pitch + n;
           *p = a.add ? *p + t.acc[i][j][r] : t.acc[i][j][r];
         }
@@ -402,35 +463,27 @@ __global__ __launch_bounds__(kMmThreads, 2) void loss_product_kernel(Product a) 
   }
 }
 
-// The splits' sum, times the row's factor, rounded.
+// The splits' sum as a gradient: a wave a row.
 struct Finish {
   const float* x;
   int64_t rows, pitch, split;
-  int splits, n;
-  float factor;            // scale, over what g was scaled by
-  void* out;
-  // dh: the row's own power of two, zeros where it has no weight; dw: the largest
-  const float* dloss;
-  Targets targets;
-  const int* power;
+  int splits;
+  Final final;
 };
 
 template <typename F>
 __global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
-  const int64_t all = a.rows * a.n;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
-       i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / a.n;
-    const int col = (int)(i % a.n);
-    float v = 0.f;
-    for (int s = 0; s < a.splits; ++s) v += a.x[s * a.split + row * a.pitch + col];
-    if (a.dloss) {
-      const Weight w = weight_of(a.targets, a.dloss, row);
-      v = w.mantissa == 0.f ? 0.f : ldexpf(v * a.factor, w.power);
-    } else if (a.power) {  // none without rows: zeros
-      v = ldexpf(v * a.factor, *a.power);
+  const int lane = threadIdx.x & 63;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows;
+       row += (int64_t)gridDim.x * 4) {
+    F* out = (F*)a.final.out + row * a.final.n;
+    const float* x = a.x + row * a.pitch;
+#pragma unroll 4
+    for (int col = lane; col < a.final.n; col += 64) {
+      float v = 0.f;
+      for (int s = 0; s < a.splits; ++s) v += x[s * a.split + col];
+      out[col] = (F)final_of<F>(a.final, row, col, v);
     }
-    ((F*)a.out)[i] = (F)v;
   }
 }
 
@@ -438,20 +491,41 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
 
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 
+// How a product is spread over the chip: the shape of its tiles, and into how many splits of k.
+struct Spread {
+  bool large;
+  int splits;
+};
+
+// The cheapest by what was measured: a large tile takes 29 ns a value of k at one work-group a
+// CU, a small one 16 ns at two, and 4 us each around it; splits are written, read and added at
+// 4 TB/s.
+Spread spread_of(int64_t m, int64_t n, int64_t k, int most) {
+  Spread best{false, 1};
+  double least = INFINITY;
+  for (int large = 0; large < 2; ++large) {
+    const int64_t side = large ? 256 : 128;
+    const int64_t tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
+    for (int s = 1; s <= most && (s == 1 || k / s >= 256); ++s) {
+      const double rounds = (double)((tiles * s + (large ? 255 : 511)) / (large ? 256 : 512));
+      double us = rounds * ((large ? 0.029 : 0.016) * (double)k / s + 4.0);
+      if (s > 1) us += 4.0 + (double)m * n * 8e-6 * s / 4.0;
+      if (us < least) {
+        least = us;
+        best = {large != 0, s};
+      }
+    }
+  }
+  return best;
+}
+
 struct Layout {
   int64_t piece;                 // vectors of a piece, a multiple of 256
   int64_t k;                     // n, up to the next multiple of 8
   int planes, pairs;
-  int splits_h, splits_w;
-  int64_t h, w, part, target, g, weighed, dh, dw, power, bytes;
+  Spread h_spread, w_spread;
+  int64_t h, w, part, target, g, weighed, row, rest, dh, dw, power, bytes;
 };
-
-// How often a product of `tiles` tiles over k is split so that the chip's 512 places are taken.
-int splits_of(int64_t tiles, int64_t k) {
-  int64_t s = 512 / std::max<int64_t>(tiles, 1);
-  s = std::min(s, k / 1024);
-  return (int)std::max<int64_t>(s, 1);
-}
 
 Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool backward) {
   Layout l{};
@@ -471,16 +545,18 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
   l.w = take(l.piece * l.k * 2 * l.planes);
   if (!backward) {
     const int64_t chunk = std::min(rows, kRowChunk);
-    l.part = take((vocab + kBM - 1) / kBM * chunk * (int64_t)sizeof(Part));
+    l.part = take((vocab + kSmallest - 1) / kSmallest * chunk * (int64_t)sizeof(Part));
     l.target = take(chunk * 4);
   } else {
-    const int64_t tiles_n = (n + kBN - 1) / kBN;
-    l.splits_h = splits_of((rows + kBM - 1) / kBM * tiles_n, l.piece);
-    l.splits_w = splits_of((l.piece + kBM - 1) / kBM * tiles_n, rows);
+    const int64_t vs = std::min(l.piece, vocab);
+    l.h_spread = spread_of(rows, n, vs * l.pairs, 16);
+    l.w_spread = spread_of(vs, n, rows * l.pairs, 16);
     l.g = take(rows * l.piece * 2 * l.planes);
     l.weighed = take(rows * l.k * 2 * l.planes);
-    l.dh = take(l.splits_h * rows * l.k * 4);
-    l.dw = take(l.splits_w * l.piece * l.k * 4);
+    l.row = take(rows * (int64_t)sizeof(Row));
+    l.rest = take(rows * 4);
+    l.dh = take(l.h_spread.splits * rows * l.k * 4);
+    l.dw = take(l.w_spread.splits * l.piece * l.k * 4);
     l.power = take(4);
   }
   l.bytes = at;
@@ -521,9 +597,9 @@ int blocks_of(int64_t work) { return (int)std::min<int64_t>((work + 255) / 256, 
 
 template <typename T>
 void pack(const void* x, int64_t stride, int64_t rows, int32_t n, int64_t k, void* to,
-          int64_t plane, hipStream_t s, const float* dloss = nullptr, Targets targets = {},
+          int64_t plane, hipStream_t s, const Row* row = nullptr,
           const int* power = nullptr) {
-  const Pack a{x, stride, rows, n, (int)k, to, plane, dloss, targets, power};
+  const Pack a{x, stride, rows, n, (int)k, to, plane, row, power};
   loss_pack_kernel<T><<<blocks_of(rows * (k / 8)), 256, 0, s>>>(a);
 }
 
@@ -550,24 +626,37 @@ hipError_t allow(K* kernel, int bytes) {
                              bytes);
 }
 
-constexpr int kLds = MmTile<bf16, kBM, kBN, false, false>::kLds;
+template <typename S>
+hipError_t allow_shape() {
+  hipError_t r = hipSuccess;
+  auto add = [&](auto* kernel) {
+    if (r == hipSuccess) r = allow(kernel, S::kLds);
+  };
+  add(loss_forward_kernel<f16, S>);
+  add(loss_forward_kernel<bf16, S>);
+  add(loss_gradient_kernel<f16, f16, S>);
+  add(loss_gradient_kernel<bf16, bf16, S>);
+  add(loss_gradient_kernel<float, bf16, S>);
+  auto products = [&](auto f, auto t) {
+    typedef decltype(f) F;
+    typedef decltype(t) T;
+    add(loss_product_kernel<F, T, S, false, false>);
+    add(loss_product_kernel<F, T, S, false, true>);
+    add(loss_product_kernel<F, T, S, true, false>);
+    add(loss_product_kernel<F, T, S, true, true>);
+  };
+  products(float{}, bf16{});
+  products(f16{}, f16{});
+  products(bf16{}, bf16{});
+  return r;
+}
 
 int allow_lds() {
   int device = 0;
   ENC_HIP_TRY(hipGetDevice(&device));
   const hipError_t e = once_per_device(g_large_lds, device, [] {
-    hipError_t r = hipSuccess;
-    auto add = [&](hipError_t x) { r = r == hipSuccess ? x : r; };
-    add(allow(loss_forward_kernel<f16>, kLds));
-    add(allow(loss_forward_kernel<bf16>, kLds));
-    add(allow(loss_gradient_kernel<f16, f16>, kLds));
-    add(allow(loss_gradient_kernel<bf16, bf16>, kLds));
-    add(allow(loss_gradient_kernel<float, bf16>, kLds));
-    add(allow(loss_product_kernel<f16, false>, kLds));
-    add(allow(loss_product_kernel<f16, true>, kLds));
-    add(allow(loss_product_kernel<bf16, false>, kLds));
-    add(allow(loss_product_kernel<bf16, true>, kLds));
-    return r;
+    const hipError_t r = allow_shape<Large>();
+    return r == hipSuccess ? allow_shape<Small>() : r;
   });
   ENC_HIP_TRY(e);
   return SIEVE_OK;
@@ -582,6 +671,39 @@ void by_type(int32_t dtype, F f) {
 }
 
 uint32_t tiles_of(int64_t n, int size) { return (uint32_t)((n + size - 1) / size); }
+
+// f(the shape)
+template <typename F>
+void by_shape(bool large, F f) {
+  if (large) f(Large{});
+  else f(Small{});
+}
+
+// Whether the logits' tiles are large.
+bool large_logits(int64_t vectors, int64_t rows, int64_t k) {
+  return spread_of(vectors, rows, k, 1).large;
+}
+
+// The product, and what turns its sums into the gradient where no later one adds to them.
+template <typename F, typename T, bool kAcrossA>
+void product(Product& p, const Spread& spread, bool last, hipStream_t s) {
+  by_shape(spread.large, [&](auto shape) {
+    typedef decltype(shape) S;
+    const int64_t each = (p.k + spread.splits - 1) / spread.splits;
+    p.per = (each + kStep - 1) / kStep * kStep;
+    p.tiles_m = tiles_of(p.rows, S::BM);
+    p.tiles_n = tiles_of(p.final.n, S::BN);
+    const uint32_t grid = p.tiles_m * p.tiles_n * spread.splits;
+    if (last && !p.add && spread.splits == 1)
+      loss_product_kernel<F, T, S, kAcrossA, true><<<grid, S::kThreads, S::kLds, s>>>(p);
+    else
+      loss_product_kernel<F, T, S, kAcrossA, false><<<grid, S::kThreads, S::kLds, s>>>(p);
+  });
+  if (last && (p.add || spread.splits > 1)) {
+    const Finish fin{p.out, p.rows, p.pitch, p.split, spread.splits, p.final};
+    loss_finish_kernel<F><<<(int)std::min<int64_t>((p.rows + 3) / 4, 8192), 256, 0, s>>>(fin);
+  }
+}
 
 }  // namespace
 
@@ -628,19 +750,24 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
       a.h.p = (const char*)all_h.p + t0 * all_h.stride * 2;
       a.h.rows = std::min(rows - t0, kRowChunk);
       a.t_first = t0;
-      a.tiles_n = tiles_of(a.h.rows, kBN);
+      const bool large = large_logits(std::min(piece, vocab), a.h.rows, l.k * l.pairs);
+      const int side = large ? Large::BM : Small::BM;
+      a.tiles_n = tiles_of(a.h.rows, side);
       for (int64_t v0 = 0; v0 < vocab; v0 += piece) {
         const int64_t vs = std::min(piece, vocab - v0);
         a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
                          w + l.w, s);
         a.v_first = v0;
-        a.tiles_m = tiles_of(vs, kBM);
-        a.part = (Part*)(w + l.part) + v0 / kBM * a.h.rows;
-        loss_forward_kernel<T><<<a.tiles_m * a.tiles_n, kMmThreads, kLds, s>>>(a);
+        a.tiles_m = tiles_of(vs, side);
+        a.part = (Part*)(w + l.part) + v0 / side * a.h.rows;
+        by_shape(large, [&](auto shape) {
+          typedef decltype(shape) S;
+          loss_forward_kernel<T, S><<<a.tiles_m * a.tiles_n, S::kThreads, S::kLds, s>>>(a);
+        });
       }
       loss_join_kernel<<<tiles_of(a.h.rows, 32), 256, 0, s>>>(
           (const Part*)(w + l.part), a.target_logit, a.targets, t0, a.h.rows,
-          tiles_of(vocab, kBM), loss, lse);
+          tiles_of(vocab, side), loss, lse);
     }
   });
   ENC_HIP_TRY(hipGetLastError());
@@ -674,70 +801,67 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     const Targets tg{targets, target_bytes, vocab};
     const float factor = std::is_same_v<F, f16> ? scale / kHalfScale : scale;
     if (rows == 0) {
-      const Finish fin{nullptr, vocab, 0, 0, 0, n, 0.f, dtable, nullptr, tg, nullptr};
-      loss_finish_kernel<F><<<blocks_of(vocab * n), 256, 0, s>>>(fin);
+      const Finish fin{nullptr, vocab, 0, 0, 0, {dtable, n, 0.f, nullptr, nullptr, nullptr, tg,
+                                                 nullptr, 0}};
+      loss_finish_kernel<F><<<(int)std::min<int64_t>((vocab + 3) / 4, 8192), 256, 0, s>>>(fin);
       return;
     }
     int* power = (int*)(w + l.power);
-    loss_power_kernel<<<1, 1024, 0, s>>>(tg, dloss, rows, power);
+    Row* row = (Row*)(w + l.row);
+    loss_rows_kernel<<<1, 1024, 0, s>>>(tg, dloss, rows, row, power);
     Logits a{};
     a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
-    if (dtable)
-      pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, s, dloss, tg, power);
+    if (dtable) pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, s, row, power);
     a.k = l.k;
     a.pairs = l.pairs;
     a.c2 = scale * kLog2e;
     a.targets = tg;
     a.lse = lse;
-    a.dloss = dloss;
+    a.row = row;
+    a.rest = (float*)(w + l.rest);
     a.g = w + l.g;
     a.g_stride = l.piece;
     a.g_plane = rows * l.piece;
-    a.tiles_n = tiles_of(rows, kBN);
+    const bool large = large_logits(std::min(l.piece, vocab), rows, l.k * l.pairs);
     for (int64_t v0 = 0; v0 < vocab; v0 += l.piece) {
       const int64_t vs = std::min(l.piece, vocab - v0);
+      const bool last = v0 + vs == vocab;
       a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
                        w + l.w, s);
       a.v_first = v0;
-      a.tiles_m = tiles_of(vs, kBM);
-      loss_gradient_kernel<F, T><<<a.tiles_m * a.tiles_n, kMmThreads, kLds, s>>>(a);
+      by_shape(large, [&](auto shape) {
+        typedef decltype(shape) S;
+        a.tiles_m = tiles_of(vs, S::BM);
+        a.tiles_n = tiles_of(rows, S::BN);
+        loss_gradient_kernel<F, T, S><<<a.tiles_m * a.tiles_n, S::kThreads, S::kLds, s>>>(a);
+      });
       Product p{};
       p.pairs = l.pairs;
       p.pitch = l.k;
-      p.tiles_n = tiles_of(n, kBN);
       if (dh) {
         p.a = {a.g, l.piece, rows, a.g_plane};
         p.b = a.w;
         p.b.rows = n;
         p.k = vs;
-        p.per = ((vs + l.splits_h - 1) / l.splits_h + kMmStep - 1) / kMmStep * kMmStep;
-        p.tiles_m = tiles_of(rows, kBM);
+        p.rows = rows;
         p.out = (float*)(w + l.dh);
         p.split = rows * l.k;
         p.add = v0 > 0;
-        loss_product_kernel<T, false>
-            <<<p.tiles_m * p.tiles_n * l.splits_h, kMmThreads, kLds, s>>>(p);
+        p.final = {dh, n, factor, nullptr, row, dtype == SIEVE_F32 ? nullptr : a.rest, tg, table,
+                   table_stride};
+        product<F, T, false>(p, l.h_spread, last, s);
       }
       if (dtable) {
         p.a = {a.g, l.piece, l.piece, a.g_plane};
         p.b = {w + l.weighed, l.k, n, rows * l.k};
         p.k = rows;
-        p.per = ((rows + l.splits_w - 1) / l.splits_w + kMmStep - 1) / kMmStep * kMmStep;
-        p.tiles_m = tiles_of(vs, kBM);
+        p.rows = vs;
         p.out = (float*)(w + l.dw);
         p.split = l.piece * l.k;
         p.add = 0;
-        loss_product_kernel<T, true>
-            <<<p.tiles_m * p.tiles_n * l.splits_w, kMmThreads, kLds, s>>>(p);
-        const Finish fin{(const float*)(w + l.dw), vs, l.k, l.piece * l.k, l.splits_w, n, factor,
-                         (F*)dtable + v0 * n, nullptr, tg, power};
-        loss_finish_kernel<F><<<blocks_of(vs * n), 256, 0, s>>>(fin);
+        p.final = {(F*)dtable + v0 * n, n, factor, power, nullptr, nullptr, tg, nullptr, 0};
+        product<F, T, true>(p, l.w_spread, true, s);
       }
-    }
-    if (dh) {
-      const Finish fin{(const float*)(w + l.dh), rows, l.k, rows * l.k, l.splits_h, n, factor, dh,
-                       dloss, tg, power};
-      loss_finish_kernel<F><<<blocks_of(rows * n), 256, 0, s>>>(fin);
     }
   });
   ENC_HIP_TRY(hipGetLastError());

@@ -30,9 +30,6 @@ typedef float mm_f32x16 __attribute__((ext_vector_type(16)));
 typedef short mm_s16x4 __attribute__((ext_vector_type(4)));
 typedef int mm_i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kMmThreads = 256;
-constexpr int kMmStep = 32;     // values of k a step
-constexpr int kMmStages = 3;
 constexpr int64_t kMmMaxStride = 1 << 20;  // values: offsets within a tile stay below 2^31 bytes
 constexpr uint32_t kMmNowhere = 0x80000000u;
 
@@ -76,37 +73,35 @@ __device__ __forceinline__ void mm_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// One operand's way into LDS, R rows of m or n.
-template <int R, bool kAcross>
+// One operand's way into LDS, R rows of m or n, kStep values of k at a time.
+template <int R, bool kAcross, int kStep, int kThreads>
 struct MmStage {
-  static constexpr int kBytes = R * kMmStep * 2;
-  static constexpr int kLoads = kBytes / 16 / kMmThreads;  // of a thread
-  static_assert(kBytes % (16 * kMmThreads) == 0);
-  static constexpr int kPieces = R / 8;                    // of a row, across k
+  static constexpr int kBytes = R * kStep * 2;
+  static constexpr int kLoads = kBytes / 16 / kThreads;  // of a thread
+  static_assert(kBytes % (16 * kThreads) == 0 && (kStep == 32 || kStep == 64));
+  static constexpr int kPitch = kAcross ? R * 2 : kStep * 2;  // bytes of a row
+  static constexpr int kPieces = kPitch / 16;
 
   uint32_t off[kLoads];
   int k_first;  // of this thread's first piece; the others lie kKStep on
-  static constexpr int kKStep = kAcross ? kMmThreads / kPieces : 0;
+  static constexpr int kKStep = kAcross ? kThreads / kPieces : 0;
 
   // Which piece of row `row` lies at place c is c ^ turn(row).
   static __device__ __forceinline__ int turn(int row) {
-    return kAcross ? (row & 3) << 2 | (row >> 2 & 3) : row >> 2 & 3;
+    if constexpr (!kAcross) return kStep == 32 ? row >> 2 & 3 : row >> 1 & 7;
+    else if constexpr (kPieces >= 16) return (row & 3) << 2 | (row >> 2 & 3);
+    else return (row & 2) << 1 | (row >> 2 & 3);
   }
 
   __device__ __forceinline__ void place(const MmOperand& x, int64_t row0) {
     const int64_t left = x.rows - row0;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = i * kMmThreads + (int)threadIdx.x;
-      if constexpr (kAcross) {
-        const int k = at / kPieces, piece = at % kPieces ^ turn(k);
-        off[i] = piece * 8 < left ? (uint32_t)(k * (uint32_t)x.stride + piece * 8) * 2 : kMmNowhere;
-        if (i == 0) k_first = k;
-      } else {
-        const int row = at / 4, piece = at % 4 ^ turn(row);
-        off[i] = row < left ? (uint32_t)(row * (uint32_t)x.stride + piece * 8) * 2 : kMmNowhere;
-        if (i == 0) k_first = piece * 8;
-      }
+      const int at = i * kThreads + (int)threadIdx.x;
+      const int row = at / kPieces, piece = at % kPieces ^ turn(row);
+      const uint32_t o = (uint32_t)(row * (uint32_t)x.stride + piece * 8) * 2;
+      off[i] = (kAcross ? piece * 8 : row) < left ? o : kMmNowhere;
+      if (i == 0) k_first = kAcross ? row : piece * 8;
     }
   }
 
@@ -124,7 +119,7 @@ struct MmStage {
       // no register is written: what arrives is waited for by count, before the barrier in
       // front of the step that reads it
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(wave_to + i * kMmThreads * 16), "v"(o), "s"(rsrc)
+                   ::"s"(wave_to + i * kThreads * 16), "v"(o), "s"(rsrc)
                    : "memory");
     }
   }
@@ -136,10 +131,10 @@ struct MmStage {
       // rows (k) 8 half + (i / 4), columns 16 (q & 1) + 4 (i & 3) of quarter q's lane i
       const int i = lane & 15, k = 8 * half + (i >> 2);
       const int piece = row0 / 8 + (lane >> 3 & 2) + (i >> 1 & 1);
-      return k * (R * 2) + ((piece ^ turn(k)) * 16) + (i & 1) * 8;
+      return k * kPitch + ((piece ^ turn(k)) * 16) + (i & 1) * 8;
     } else {
       const int row = row0 + (lane & 31);
-      return row * 64 + ((half ^ turn(row)) * 16);
+      return row * kPitch + ((half ^ turn(row)) * 16);
     }
   }
   // Values k = 16 s + 8 (lane / 32) .. + 7 of row 32 j + lane % 32 from the wave's first.
@@ -151,40 +146,41 @@ struct MmStage {
         mm_s16x4 half[2];
         enc_u32x4 all;
       } u;
-      const uint32_t x = (at ^ (j * 64)) + s * 16 * (R * 2);
+      const uint32_t x = (at ^ (j * 64)) + s * 16 * kPitch;
       u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)x);
       // 4 rows on, turn differs in bit 0
       u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_s16x4*)(uintptr_t)((x ^ 16) + 4 * (R * 2)));
+          (lds_s16x4*)(uintptr_t)((x ^ 16) + 4 * kPitch));
       return u.all;
     } else {
       return *(const __attribute__((address_space(3))) enc_u32x4*)(uintptr_t)((at ^ (s * 32)) +
-                                                                              j * 32 * 64);
+                                                                              j * 32 * kPitch);
     }
   }
 };
 
-// Register 4 g + t of tile (i, j) of a wave holds row mm_row(i, 4 g + t) and column
-// mm_col(j) of the work-group's values.
-template <int BM>
-__device__ __forceinline__ int mm_row(int i, int r) {
-  return (int)(threadIdx.x >> 7) * (BM / 2) + i * 32 + (r >> 2) * 8 +
-         (int)(threadIdx.x >> 5 & 1) * 4 + (r & 3);
-}
-template <int BN>
-__device__ __forceinline__ int mm_col(int j) {
-  return (int)(threadIdx.x >> 6 & 1) * (BN / 2) + j * 32 + (int)(threadIdx.x & 31);
-}
-
-template <typename T, int BM, int BN, bool kAcrossA, bool kAcrossB>
+// WM x WN waves own BM x BN values.
+template <typename T, int BM, int BN, bool kAcrossA, bool kAcrossB, int WM = 2, int WN = 2,
+          int kStep = 32, int kStages = 3>
 struct MmTile {
-  typedef MmStage<BM, kAcrossA> A;
-  typedef MmStage<BN, kAcrossB> B;
-  static constexpr int kI = BM / 64, kJ = BN / 64;
+  static constexpr int kThreads = 64 * WM * WN;
+  typedef MmStage<BM, kAcrossA, kStep, kThreads> A;
+  typedef MmStage<BN, kAcrossB, kStep, kThreads> B;
+  static constexpr int kI = BM / WM / 32, kJ = BN / WN / 32;
   static constexpr int kStage = A::kBytes + B::kBytes;
-  static constexpr int kLds = kMmStages * kStage;
+  static constexpr int kLds = kStages * kStage;
   static constexpr int kLoads = A::kLoads + B::kLoads;
   mm_f32x16 acc[kI][kJ];
+
+  // Register r of tile (i, j) of a wave holds row row(i, r) and column col(j) of the
+  // work-group's values.
+  static __device__ __forceinline__ int row(int i, int r) {
+    return (int)(threadIdx.x >> 6) / WN * (BM / WM) + i * 32 + (r >> 2) * 8 +
+           (int)(threadIdx.x >> 5 & 1) * 4 + (r & 3);
+  }
+  static __device__ __forceinline__ int col(int j) {
+    return (int)(threadIdx.x >> 6) % WN * (BN / WN) + j * 32 + (int)(threadIdx.x & 31);
+  }
 
   // lds: the address of kLds bytes, a multiple of 1024; free again on return.
   __device__ __forceinline__ void run(const MmOperand& a, int64_t m0, const MmOperand& b,
@@ -195,43 +191,44 @@ struct MmTile {
     sa.place(a, m0);
     sb.place(b, n0);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const uint32_t a_at = lds + A::lane_at((wave >> 1) * (BM / 2));
-    const uint32_t b_at = lds + A::kBytes + B::lane_at((wave & 1) * (BN / 2));
+    const uint32_t a_at = lds + A::lane_at(wave / WN * (BM / WM));
+    const uint32_t b_at = lds + A::kBytes + B::lane_at(wave % WN * (BN / WN));
 #pragma unroll
     for (int i = 0; i < kI; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    const int steps_k = (int)((k1 - k0 + kMmStep - 1) / kMmStep);
-    const int steps = steps_k * pairs;
+    const int steps = (int)((k1 - k0 + kStep - 1) / kStep) * pairs;
     if (steps <= 0) return;
     int64_t k = k0;
     int pair = 6 - pairs;
     // past the last step nothing is there: the loads are counted all the same
     auto load = [&](int buffer) {
-      const int left = pair < 6 ? (int)(k1 - k < kMmStep ? k1 - k : kMmStep) : 0;
+      const int left = pair < 6 ? (int)(k1 - k < kStep ? k1 - k : kStep) : 0;
       const int p = pair < 6 ? pair : 5;
-      const int64_t at_a = mm_plane_a(p) * a.plane + (kAcrossA ? k * a.stride + m0 : m0 * a.stride + k);
-      const int64_t at_b = mm_plane_b(p) * b.plane + (kAcrossB ? k * b.stride + n0 : n0 * b.stride + k);
+      const int64_t at_a =
+          mm_plane_a(p) * a.plane + (kAcrossA ? k * a.stride + m0 : m0 * a.stride + k);
+      const int64_t at_b =
+          mm_plane_b(p) * b.plane + (kAcrossB ? k * b.stride + n0 : n0 * b.stride + k);
       sa.load((const char*)a.p + at_a * 2, left, lds + buffer * kStage);
       sb.load((const char*)b.p + at_b * 2, left, lds + buffer * kStage + A::kBytes);
-      k += kMmStep;
+      k += kStep;
       if (k >= k1) {
         k = k0;
         ++pair;
       }
     };
-    load(0);
-    load(1);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) load(i);
     int buffer = 0;
     for (int step = 0; step < steps; ++step) {
-      mm_wait_loads<kLoads>();  // this step's; the next one's stay in flight
+      mm_wait_loads<(kStages - 2) * kLoads>();  // this step's; the next ones' stay in flight
       mm_barrier();
-      load(buffer == 0 ? 2 : buffer - 1);
+      load(buffer == 0 ? kStages - 1 : buffer - 1);
       const uint32_t at = buffer * kStage;
 #pragma unroll
-      for (int s = 0; s < kMmStep / 16; ++s) {
+      for (int s = 0; s < kStep / 16; ++s) {
         enc_u32x4 fa[kI], fb[kJ];
 #pragma unroll
         for (int j = 0; j < kJ; ++j) fb[j] = B::frag(b_at + at, j, s);
@@ -242,7 +239,7 @@ struct MmTile {
 #pragma unroll
           for (int j = 0; j < kJ; ++j) acc[i][j] = mm_mfma<T>(fa[i], fb[j], acc[i][j]);
       }
-      buffer = buffer == 2 ? 0 : buffer + 1;
+      buffer = buffer == kStages - 1 ? 0 : buffer + 1;
     }
     mm_wait_loads<0>();
     mm_barrier();

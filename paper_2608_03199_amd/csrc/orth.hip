@@ -33,6 +33,7 @@ namespace {
 typedef __bf16 bf16;
 typedef _Float16 f16;
 
+constexpr int kThreads = 256;
 constexpr int kTileSize = 128;
 constexpr float kScaleX = 16384.f, kScaleA = 4096.f;  // of X; of A and B
 constexpr double kMaxX = 3.9, kMaxA = 15.9;           // below 65504 times these
@@ -111,7 +112,7 @@ struct Product {
 enum { kGram, kPolynomial, kUpdate, kLast };
 
 template <typename T, int kKind, bool kAcrossA, bool kAcrossB>
-__global__ __launch_bounds__(kMmThreads, 3) void orth_product_kernel(Product a) {
+__global__ __launch_bounds__(kThreads, 3) void orth_product_kernel(Product a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
   const uint32_t place = mm_place_of(blockIdx.x, gridDim.x);
   const int64_t matrix = place / a.tiles;
@@ -137,12 +138,12 @@ __global__ __launch_bounds__(kMmThreads, 3) void orth_product_kernel(Product a) 
   const int64_t first = matrix * a.next;
 #pragma unroll
   for (int j = 0; j < Tile::kJ; ++j) {
-    const int64_t n = n0 + mm_col<kTileSize>(j);
+    const int64_t n = n0 + Tile::col(j);
 #pragma unroll
     for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + mm_row<kTileSize>(i, r);
+        const int64_t m = m0 + Tile::row(i, r);
         if (m >= a.rows || n >= a.cols) continue;
         float v = t.acc[i][j][r];
         if constexpr (kKind == kLast) {
@@ -285,10 +286,10 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     p.plane = batch * square;
     if (tall)
       orth_product_kernel<T, kGram, true, true>
-          <<<half * (uint32_t)batch, kMmThreads, kLds, s>>>(p);
+          <<<half * (uint32_t)batch, kThreads, kLds, s>>>(p);
     else
       orth_product_kernel<T, kGram, false, false>
-          <<<half * (uint32_t)batch, kMmThreads, kLds, s>>>(p);
+          <<<half * (uint32_t)batch, kThreads, kLds, s>>>(p);
     // B
     p.a = p.b = of_a;
     p.a_next = p.b_next = square;
@@ -299,7 +300,7 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     p.gram = gram;
     p.out = poly;
     orth_product_kernel<T, kPolynomial, false, false>
-        <<<half * (uint32_t)batch, kMmThreads, kLds, s>>>(p);
+        <<<half * (uint32_t)batch, kThreads, kLds, s>>>(p);
     // the next X, or the result
     p.a = tall ? MmOperand{x, l.pitch, m, src.plane} : of_b;
     p.b = tall ? of_b : MmOperand{x, l.pitch, n, src.plane};
@@ -316,13 +317,13 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     p.plane = src.plane;
     const uint32_t grid = p.tiles * (uint32_t)batch;
     if (tall && last)
-      orth_product_kernel<T, kLast, false, false><<<grid, kMmThreads, kLds, s>>>(p);
+      orth_product_kernel<T, kLast, false, false><<<grid, kThreads, kLds, s>>>(p);
     else if (tall)
-      orth_product_kernel<T, kUpdate, false, false><<<grid, kMmThreads, kLds, s>>>(p);
+      orth_product_kernel<T, kUpdate, false, false><<<grid, kThreads, kLds, s>>>(p);
     else if (last)
-      orth_product_kernel<T, kLast, false, true><<<grid, kMmThreads, kLds, s>>>(p);
+      orth_product_kernel<T, kLast, false, true><<<grid, kThreads, kLds, s>>>(p);
     else
-      orth_product_kernel<T, kUpdate, false, true><<<grid, kMmThreads, kLds, s>>>(p);
+      orth_product_kernel<T, kUpdate, false, true><<<grid, kThreads, kLds, s>>>(p);
   }
 }
 
