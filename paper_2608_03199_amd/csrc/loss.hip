@@ -51,7 +51,9 @@ struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM_ * WN_;
   template <typename T, bool kAcrossA, bool kAcrossB>
   using Tile = MmTile<T, BM, BN, kAcrossA, kAcrossB, WM, WN, kStep, 2>;
-  static constexpr int kLds = Tile<mm_bf16, false, false>::kLds;
+  static constexpr int kTileLds = Tile<mm_bf16, false, false>::kLds;
+  static constexpr int kLds = kTileLds + WM * BN * 8;  // and the forward pass's parts
+  static constexpr uint32_t kMost = BM == 256 ? 256 : 512;  // work-groups on the chip
 };
 typedef Shape<256, 256, 2, 4> Large;
 typedef Shape<128, 128, 2, 2> Small;
@@ -121,78 +123,112 @@ struct Logits {
 
 typedef mm_f32x16 f32x16;
 
-// The value of a row's target vector, where this lane holds it: rel is its place among the
-// wave's rows of the tile.
-template <int kI>
-__device__ __forceinline__ bool find_value(const f32x16 (&acc)[kI], int64_t rel, float& x) {
-  bool found = false;
+// x = f(x) for the value x of each of the wave's rows' targets that lie among its vectors: `rel`
+// from the wave's first, or -1.  There are few: one row at a time, its register found by a number
+// that the whole wave knows.
+template <int kI, typename F>
+__device__ __forceinline__ void each_target(f32x16 (&acc)[kI], int rel, F f) {
+  const int half = (int)threadIdx.x >> 5 & 1;
+  uint64_t some = __ballot(rel >= 0 && (rel >> 2 & 1) == half);
+  while (some) {
+    const int lane = __ffsll((unsigned long long)some) - 1;
+    some &= some - 1;
+    const int v = __builtin_amdgcn_readlane(rel, lane);
+    const int r = (v >> 3 & 3) * 4 + (v & 3);
+    const bool own = (int)(threadIdx.x & 63) == lane;
 #pragma unroll
-  for (int i = 0; i < kI; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (rel == i * 32 + (r >> 2) * 8 + (int)(threadIdx.x >> 5 & 1) * 4 + (r & 3)) {
-        x = acc[i][r];
-        found = true;
-      }
-  return found;
+    for (int i = 0; i < kI; ++i)
+      if (v >> 5 == i) acc[i][r] = own ? f(acc[i][r]) : acc[i][r];
+  }
 }
+
+// The tiles of a launch without splits, in order.
+template <typename S>
+struct Tiles {
+  MmPlaces at;
+  uint32_t tiles_m, tiles_n;
+  int64_t k;
+  __device__ __forceinline__ Tiles(uint32_t tm, uint32_t tn, int64_t k_)
+      : at(tm * tn), tiles_m(tm), tiles_n(tn), k(k_) {}
+  __device__ __forceinline__ void get(MmWork& w, uint32_t& tm) const {
+    uint32_t tn;
+    mm_tile_at(at.place, tiles_m, tiles_n, kHigh, tm, tn);
+    w = {(int64_t)tm * S::BM, (int64_t)tn * S::BN, 0, k};
+  }
+  __device__ __forceinline__ bool operator()(MmWork& w) {
+    if (!at.there()) return false;
+    uint32_t tm;
+    get(w, tm);
+    at.next();
+    return true;
+  }
+};
 
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, 2) void loss_forward_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
-  uint32_t tm, tn;
-  mm_tile_at(mm_place_of(blockIdx.x, gridDim.x), a.tiles_m, a.tiles_n, kHigh, tm, tn);
-  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  Part* s_part = (Part*)(lds_memory + S::kTileLds);  // [wave along the vectors][row]
   typedef typename S::template Tile<T, false, false> Tile;
-  Tile t;
-  t.run(a.w, m0, a.h, n0, 0, a.k, a.pairs, lds_of(lds_memory));
-  Part* s_part = (Part*)lds_memory;      // [wave along the vectors][row]
+  Tiles<S> ahead(a.tiles_m, a.tiles_n, a.k), tiles = ahead;
+  if (!tiles.at.there()) return;
+  Tile t(a.w, a.h, a.pairs, lds_of(lds_memory));
+  t.start(ahead);
   constexpr int kWave = S::BM / S::WM;   // vectors of a wave
-  const int wave_m = (int)(threadIdx.x >> 6) / S::WN;
-  const int64_t first = m0 + wave_m * kWave, left = a.w.rows - first;
+  const int wave_m = Tile::wave() / S::WN, half = (int)threadIdx.x >> 5 & 1;
+  for (; tiles.at.there(); tiles.at.next()) {
+    MmWork w;
+    uint32_t tm;
+    tiles.get(w, tm);
+    const int64_t first = w.m0 + wave_m * kWave;
+    const int left = (int)(a.w.rows - first < kWave ? a.w.rows - first : kWave);
+    int rel[Tile::kJ];  // where a row's target lies among the wave's vectors, or -1
 #pragma unroll
-  for (int j = 0; j < Tile::kJ; ++j) {
-    f32x16 acc[Tile::kI];
-    float top = -INFINITY;
+    for (int j = 0; j < Tile::kJ; ++j) {
+      const int64_t row = w.n0 + t.col0 + 32 * j;
+      const int64_t v = row < a.h.rows ? a.targets.at(a.t_first + row) : -1;
+      const int64_t at = v - a.v_first - first;
+      rel[j] = v >= 0 && at >= 0 && at < kWave ? (int)at : -1;
+    }
+    t.sum(t.steps_of(w), ahead);
 #pragma unroll
-    for (int i = 0; i < Tile::kI; ++i) {
-      acc[i] = t.acc[i][j];
-      if (left < kWave) {
+    for (int j = 0; j < Tile::kJ; ++j) {
+      f32x16 acc[Tile::kI];
+      float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (Tile::row(i, r) - wave_m * kWave >= left) acc[i][r] = -INFINITY;
+      for (int i = 0; i < Tile::kI; ++i) {
+        acc[i] = t.acc[i][j];
+        if (left < kWave) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (Tile::down(i, r) >= left - 4 * half) acc[i][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][r]);
       }
+      top = fmaxf(top, other_half(top));
+      const float top2 = top * a.c2, at = top == -INFINITY ? 0.f : top2;
+      float sum = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][r]);
-    }
-    top = fmaxf(top, other_half(top));
-    const float top2 = top * a.c2, at = top == -INFINITY ? 0.f : top2;
-    float sum = 0.f;
+      for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
-    for (int i = 0; i < Tile::kI; ++i)
+        for (int r = 0; r < 16; ++r) sum += exp2_of(fmaf(acc[i][r], a.c2, -at));
+      sum += other_half(sum);
+      each_target(acc, rel[j], [&](float x) {
+        a.target_logit[w.n0 + t.col0 + 32 * j] = x * a.c2;
+        return x;
+      });
+      if ((threadIdx.x & 32) == 0) s_part[wave_m * S::BN + t.col0 + 32 * j] = Part{top2, sum};
+    }
+    mm_barrier();
+    if (threadIdx.x < S::BN && w.n0 + threadIdx.x < a.h.rows) {
+      Part p = s_part[threadIdx.x];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum += exp2_of(fmaf(acc[i][r], a.c2, -at));
-    sum += other_half(sum);
-    const int col = Tile::col(j);
-    const int64_t row = n0 + col;
-    int64_t rel = -1;
-    if (row < a.h.rows) {
-      const int64_t v = a.targets.at(a.t_first + row);
-      if (v >= 0) rel = v - a.v_first - first;
+      for (int i = 1; i < S::WM; ++i) p = join(p, s_part[i * S::BN + threadIdx.x]);
+      a.part[(int64_t)tm * a.h.rows + w.n0 + threadIdx.x] = p;
     }
-    if (__any(rel >= 0 && rel < kWave)) {
-      float x;
-      if (find_value(acc, rel, x)) a.target_logit[row] = x * a.c2;
-    }
-    if ((threadIdx.x & 32) == 0) s_part[wave_m * S::BN + col] = Part{top2, sum};
+    // the next tile's first step has a barrier between these reads and the next parts
   }
-  __syncthreads();
-  if (threadIdx.x < S::BN && n0 + threadIdx.x < a.h.rows) {
-    Part p = s_part[threadIdx.x];
-#pragma unroll
-    for (int i = 1; i < S::WM; ++i) p = join(p, s_part[i * S::BN + threadIdx.x]);
-    a.part[(int64_t)tm * a.h.rows + n0 + threadIdx.x] = p;
-  }
+  t.stop();
 }
 
 // Joins the tiles' parts: a work-group takes 32 rows, its 8 groups of 32 threads every 8th tile.
@@ -313,81 +349,96 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
 template <typename F, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
-  uint32_t tm, tn;
-  mm_tile_at(mm_place_of(blockIdx.x, gridDim.x), a.tiles_m, a.tiles_n, kHigh, tm, tn);
-  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
   typedef typename S::template Tile<T, false, false> Tile;
-  Tile t;
-  t.run(a.w, m0, a.h, n0, 0, a.k, a.pairs, lds_of(lds_memory));
+  Tiles<S> ahead(a.tiles_m, a.tiles_n, a.k), tiles = ahead;
+  if (!tiles.at.there()) return;
+  Tile t(a.w, a.h, a.pairs, lds_of(lds_memory));
+  t.start(ahead);
   constexpr int kWave = S::BM / S::WM;
-  const int wave_m = (int)(threadIdx.x >> 6) / S::WN, half = (int)threadIdx.x >> 5 & 1;
-  const int64_t first = m0 + wave_m * kWave;
-  const int left = (int)(a.w.rows - first < kWave ? a.w.rows - first : kWave);
+  const int wave_m = Tile::wave() / S::WN, half = (int)threadIdx.x >> 5 & 1;
+  for (; tiles.at.there(); tiles.at.next()) {
+    MmWork w;
+    uint32_t tm;
+    tiles.get(w, tm);
+    const int64_t first = w.m0 + wave_m * kWave;
+    const int left = (int)(a.w.rows - first < kWave ? a.w.rows - first : kWave);
+    int rel[Tile::kJ];
+    float weight[Tile::kJ], lse2[Tile::kJ];
 #pragma unroll
-  for (int j = 0; j < Tile::kJ; ++j) {
-    const int64_t row = n0 + Tile::col(j);
-    const bool there = row < a.h.rows;
-    int rel = -1;
-    float weight = 0.f, lse2 = 0.f;
-    if (there) {
-      const int64_t v = a.targets.at(row), at = v - a.v_first - first;
-      if (v >= 0 && at >= 0 && at < kWave) rel = (int)at;
-      weight = a.row[row].mantissa;
-      if constexpr (std::is_same_v<F, f16>) weight *= kHalfScale;
-      lse2 = a.lse[row] * kLog2e;
+    for (int j = 0; j < Tile::kJ; ++j) {
+      const int64_t row = w.n0 + t.col0 + 32 * j;
+      rel[j] = -1;
+      weight[j] = lse2[j] = 0.f;
+      if (row < a.h.rows) {
+        const int64_t v = a.targets.at(row), at = v - a.v_first - first;
+        if (v >= 0 && at >= 0 && at < kWave) rel[j] = (int)at;
+        weight[j] = a.row[row].mantissa;
+        if constexpr (std::is_same_v<F, f16>) weight[j] *= kHalfScale;
+        lse2[j] = a.lse[row] * kLog2e;
+      }
     }
-    const bool here = __any(rel >= 0);
-    T* g = (T*)a.g + row * a.g_stride + first + 8 * half;
+    t.sum(t.steps_of(w), ahead);
 #pragma unroll
-    for (int i = 0; i < Tile::kI; ++i) {
-      f32x16 x = t.acc[i][j];
-      float own = 0.f;  // the target's g, in its lane
+    for (int j = 0; j < Tile::kJ; ++j) {
+      const int64_t row = w.n0 + t.col0 + 32 * j;
+      const bool there = row < a.h.rows;
+      T* g = (T*)a.g + row * a.g_stride + first + 8 * half;
+      f32x16 p[Tile::kI];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int v = i * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-        float p = exp2_of(fmaf(x[r], a.c2, -lse2));
-        if (here && rel == v) {
-          p -= 1.f;
-          own = p * weight;
-        }
-        // a row without weight gives nothing, whatever it holds; nor does what lies past the
-        // last vector
-        x[r] = weight == 0.f || v >= left ? 0.f : p * weight;
-      }
-      if constexpr (!std::is_same_v<F, float>) {
-        if (here && rel >= i * 32 && rel < i * 32 + 32 && (rel >> 2 & 1) == half)
+      for (int i = 0; i < Tile::kI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[i][r] = exp2_of(fmaf(t.acc[i][j][r], a.c2, -lse2[j]));
+      each_target(p, rel[j], [&](float x) {
+        x -= 1.f;
+        if constexpr (!std::is_same_v<F, float>) {
+          const float own = x * weight[j];
           a.rest[row] = own - (float)(T)own;
-      }
-      // pairs of 16-bit values; halves of a wave change places so that each lane has 8
-      // neighbours
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        constexpr int kPlanes = std::is_same_v<F, float> ? 3 : 1;
-        T part[kPlanes][8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if constexpr (kPlanes == 3) {
-            T p[3];
-            split3(x[8 * q + e], p);
-#pragma unroll
-            for (int z = 0; z < 3; ++z) part[z][e] = p[z];
-          } else {
-            part[0][e] = (T)x[8 * q + e];
-          }
         }
+        return x;
+      });
 #pragma unroll
-        for (int z = 0; z < kPlanes; ++z) {
-          uint32_t d[4];
-          __builtin_memcpy(d, part[z], 16);
-          const u32x2 lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
-          const u32x2 hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
-          const enc_u32x4 out = {lo[0], hi[0], lo[1], hi[1]};
-          if (there) *(enc_u32x4*)(g + z * a.g_plane + i * 32 + 16 * q) = out;
+      for (int i = 0; i < Tile::kI; ++i) {
+        f32x16 x = p[i];
+        if (left < kWave) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (Tile::down(i, r) >= left - 4 * half) x[r] = 0.f;
+        }
+        // a row without weight gives nothing, whatever it holds
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = weight[j] == 0.f ? 0.f : x[r] * weight[j];
+        // pairs of 16-bit values; halves of a wave change places so that each lane has 8
+        // neighbours
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          constexpr int kPlanes = std::is_same_v<F, float> ? 3 : 1;
+          T part[kPlanes][8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if constexpr (kPlanes == 3) {
+              T p[3];
+              split3(x[8 * q + e], p);
+#pragma unroll
+              for (int z = 0; z < 3; ++z) part[z][e] = p[z];
+            } else {
+              part[0][e] = (T)x[8 * q + e];
+            }
+          }
+#pragma unroll
+          for (int z = 0; z < kPlanes; ++z) {
+            uint32_t d[4];
+            __builtin_memcpy(d, part[z], 16);
+            const u32x2 lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
+            const u32x2 hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
+            const enc_u32x4 out = {lo[0], hi[0], lo[1], hi[1]};
+            if (there) *(enc_u32x4*)(g + z * a.g_plane + i * 32 + 16 * q) = out;
+          }
         }
       }
     }
   }
+  t.stop();
 }
 
 // What turns a sum of products into a gradient.
@@ -404,16 +455,28 @@ struct Final {
   int64_t t_stride;
 };
 
-// A gradient's value from its sum.
+// A row's values from their sums.
 template <typename F>
-__device__ __forceinline__ float final_of(const Final& a, int64_t row, int64_t col, float sum) {
-  if (!a.row) return a.power ? ldexpf(sum * a.factor, *a.power) : 0.f;
-  const Row w = a.row[row];
-  if (w.mantissa == 0.f) return 0.f;
-  if (a.rest)
-    sum += a.rest[row] * (float)((const F*)a.table)[a.targets.at(row) * a.t_stride + col];
-  return ldexpf(sum * a.factor, w.power);
-}
+struct Gradient {
+  float factor, rest = 0.f;
+  const F* target = nullptr;
+  __device__ __forceinline__ Gradient(const Final& a, int64_t row) {
+    if (!a.row) {
+      factor = a.power ? ldexpf(a.factor, *a.power) : 0.f;
+      return;
+    }
+    const Row w = a.row[row];
+    factor = w.mantissa == 0.f ? 0.f : ldexpf(a.factor, w.power);
+    if (a.rest && factor != 0.f) {
+      rest = a.rest[row];
+      target = (const F*)a.table + a.targets.at(row) * a.t_stride;
+    }
+  }
+  __device__ __forceinline__ float operator()(float sum, int64_t col) const {
+    if (target) sum += rest * (float)target[col];
+    return factor == 0.f ? 0.f : sum * factor;
+  }
+};
 
 // A gradient's product: sums in fp32, [split][rows of m][pitch], or added to what is there; or
 // the gradient itself.
@@ -421,7 +484,7 @@ struct Product {
   MmOperand a, b;
   int64_t k, per;        // values of k, and of a split
   int pairs;
-  uint32_t tiles_m, tiles_n;
+  uint32_t tiles_m, tiles_n, splits;
   int64_t rows;          // of m, that are written
   float* out;
   int64_t pitch, split;  // values between rows, and between splits
@@ -429,60 +492,120 @@ struct Product {
   Final final;
 };
 
+// The tiles of a product, split after split.
+template <typename S>
+struct Splits {
+  MmPlaces at;
+  uint32_t tiles_m, tiles_n;
+  int64_t k, per;
+  __device__ __forceinline__ explicit Splits(const Product& a)
+      : at(a.tiles_m * a.tiles_n * a.splits), tiles_m(a.tiles_m), tiles_n(a.tiles_n), k(a.k),
+        per(a.per) {}
+  __device__ __forceinline__ void get(MmWork& w, uint32_t& split) const {
+    const uint32_t tiles = tiles_m * tiles_n;
+    uint32_t tm, tn;
+    split = at.place / tiles;
+    mm_tile_at(at.place % tiles, tiles_m, tiles_n, kHigh, tm, tn);
+    const int64_t k0 = split * per;
+    w = {(int64_t)tm * S::BM, (int64_t)tn * S::BN, k0, k0 + per < k ? k0 + per : k};
+  }
+  __device__ __forceinline__ bool operator()(MmWork& w) {
+    if (!at.there()) return false;
+    uint32_t split;
+    get(w, split);
+    at.next();
+    return true;
+  }
+};
+
 template <typename F, typename T, typename S, bool kAcrossA, bool kFinal>
 __global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product a) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
-  const uint32_t tiles = a.tiles_m * a.tiles_n;
-  uint32_t tm, tn;
-  const uint32_t place = mm_place_of(blockIdx.x, gridDim.x);
-  mm_tile_at(place % tiles, a.tiles_m, a.tiles_n, kHigh, tm, tn);
-  const int64_t split = place / tiles;
-  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
-  const int64_t k0 = split * a.per, k1 = k0 + a.per < a.k ? k0 + a.per : a.k;
   typedef typename S::template Tile<T, kAcrossA, true> Tile;
-  Tile t;
-  t.run(a.a, m0, a.b, n0, k0, k1, a.pairs, lds_of(lds_memory));
-  float* out = a.out + split * a.split;
+  Splits<S> ahead(a), tiles = ahead;
+  if (!tiles.at.there()) return;
+  Tile t(a.a, a.b, a.pairs, lds_of(lds_memory));
+  t.start(ahead);
+  for (; tiles.at.there(); tiles.at.next()) {
+    MmWork w;
+    uint32_t split;
+    tiles.get(w, split);
+    t.sum(t.steps_of(w), ahead);
+    if constexpr (kFinal) {
+      const MmPatch<F> to((F*)a.final.out + w.m0 * a.final.n + w.n0, a.final.n, a.rows - w.m0,
+                          a.b.rows - w.n0);
+      typename MmPatch<F>::Lane lane[Tile::kJ];
 #pragma unroll
-  for (int j = 0; j < Tile::kJ; ++j) {
-    const int64_t n = n0 + Tile::col(j);
-    if (n >= a.b.rows) continue;
+      for (int j = 0; j < Tile::kJ; ++j) lane[j] = to.lane(t.row0, t.col0 + 32 * j);
 #pragma unroll
-    for (int i = 0; i < Tile::kI; ++i)
+      for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + Tile::row(i, r);
-        if (m >= a.rows) continue;
-        if constexpr (kFinal) {
-          ((F*)a.final.out)[m * a.final.n + n] = (F)final_of<F>(a.final, m, n, t.acc[i][j][r]);
-        } else {
-          float* p = out + m * a.pitch + n;
-          *p = a.add ? *p + t.acc[i][j][r] : t.acc[i][j][r];
+        for (int r = 0; r < 16; ++r) {
+          // rows past the last one are the last one again, and not stored
+          const int64_t row = w.m0 + t.row0 + Tile::down(i, r);
+          const Gradient<F> g(a.final, row < a.rows ? row : a.rows - 1);
+#pragma unroll
+          for (int j = 0; j < Tile::kJ; ++j) {
+            const int64_t n = w.n0 + t.col0 + 32 * j;
+            to.store(to.at(lane[j], Tile::down(i, r)),
+                     (F)g(t.acc[i][j][r], n < a.b.rows ? n : a.b.rows - 1));
+          }
+        }
+    } else {
+      const MmPatch<float> to(a.out + split * a.split + w.m0 * a.pitch + w.n0, a.pitch,
+                              a.rows - w.m0, a.b.rows - w.n0);
+#pragma unroll
+      for (int j = 0; j < Tile::kJ; ++j) {
+        const auto lane = to.lane(t.row0, t.col0 + 32 * j);
+#pragma unroll
+        for (int i = 0; i < Tile::kI; ++i) {
+          f32x16 v = t.acc[i][j];
+          if (a.add) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) v[r] += to.load(to.at(lane, Tile::down(i, r)));
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) to.store(to.at(lane, Tile::down(i, r)), v[r]);
         }
       }
+    }
   }
+  t.stop();
 }
 
-// The splits' sum as a gradient: a wave a row.
+// The splits' sum as a gradient, 4 values of a row at a time.
 struct Finish {
   const float* x;
   int64_t rows, pitch, split;
   int splits;
   Final final;
+  int pieces;            // of a row
+  int together;          // rows of a work-group
+  uint32_t mul;          // index / pieces = (index * mul) >> 32
 };
 
 template <typename F>
 __global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows;
-       row += (int64_t)gridDim.x * 4) {
-    F* out = (F*)a.final.out + row * a.final.n;
-    const float* x = a.x + row * a.pitch;
+  for (int64_t first = (int64_t)blockIdx.x * a.together; first < a.rows;
+       first += (int64_t)gridDim.x * a.together) {
+    const int rows = (int)(a.rows - first < a.together ? a.rows - first : a.together);
+    for (int i = threadIdx.x; i < rows * a.pieces; i += 256) {
+      const int in = a.pieces == 1 ? i : (int)__umulhi((uint32_t)i, a.mul);
+      const int64_t row = first + in;
+      const int col = (i - in * a.pieces) * 4;
+      const Gradient<F> g(a.final, row);
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      const float* x = a.x + row * a.pitch + col;  // rows are padded to multiples of 8
 #pragma unroll 4
-    for (int col = lane; col < a.final.n; col += 64) {
-      float v = 0.f;
-      for (int s = 0; s < a.splits; ++s) v += x[s * a.split + col];
-      out[col] = (F)final_of<F>(a.final, row, col, v);
+      for (int s = 0; s < a.splits; ++s) {
+        const EncVec<float, 4> p = enc_load<float, 4>(x + s * a.split);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += p.v[e];
+      }
+      F* out = (F*)a.final.out + row * a.final.n + col;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < a.final.n) out[e] = (F)g(v[e], col + e);
     }
   }
 }
@@ -670,6 +793,17 @@ void by_type(int32_t dtype, F f) {
   else f(bf16{}, bf16{});
 }
 
+template <typename F>
+void finish(const float* x, int64_t rows, int64_t pitch, int64_t split, int splits,
+            const Final& final, hipStream_t s) {
+  Finish a{x, rows, pitch, split, splits, final, (final.n + 3) / 4, 1, 0};
+  // some 4 pieces a thread; indexes stay below 2^15, where the multiplier is exact
+  a.together = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / a.pieces, rows / 512));
+  a.mul = (uint32_t)(((uint64_t(1) << 32) + a.pieces - 1) / a.pieces);
+  const int64_t groups = (rows + a.together - 1) / a.together;
+  loss_finish_kernel<F><<<(int)std::min<int64_t>(groups, 65536), 256, 0, s>>>(a);
+}
+
 uint32_t tiles_of(int64_t n, int size) { return (uint32_t)((n + size - 1) / size); }
 
 // f(the shape)
@@ -693,16 +827,15 @@ void product(Product& p, const Spread& spread, bool last, hipStream_t s) {
     p.per = (each + kStep - 1) / kStep * kStep;
     p.tiles_m = tiles_of(p.rows, S::BM);
     p.tiles_n = tiles_of(p.final.n, S::BN);
-    const uint32_t grid = p.tiles_m * p.tiles_n * spread.splits;
+    p.splits = spread.splits;
+    const uint32_t grid = mm_grid((uint64_t)p.tiles_m * p.tiles_n * p.splits, S::kMost);
     if (last && !p.add && spread.splits == 1)
       loss_product_kernel<F, T, S, kAcrossA, true><<<grid, S::kThreads, S::kLds, s>>>(p);
     else
       loss_product_kernel<F, T, S, kAcrossA, false><<<grid, S::kThreads, S::kLds, s>>>(p);
   });
-  if (last && (p.add || spread.splits > 1)) {
-    const Finish fin{p.out, p.rows, p.pitch, p.split, spread.splits, p.final};
-    loss_finish_kernel<F><<<(int)std::min<int64_t>((p.rows + 3) / 4, 8192), 256, 0, s>>>(fin);
-  }
+  if (last && (p.add || spread.splits > 1))
+    finish<F>(p.out, p.rows, p.pitch, p.split, spread.splits, p.final, s);
 }
 
 }  // namespace
@@ -762,7 +895,8 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
         a.part = (Part*)(w + l.part) + v0 / side * a.h.rows;
         by_shape(large, [&](auto shape) {
           typedef decltype(shape) S;
-          loss_forward_kernel<T, S><<<a.tiles_m * a.tiles_n, S::kThreads, S::kLds, s>>>(a);
+          loss_forward_kernel<T, S>
+              <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
         });
       }
       loss_join_kernel<<<tiles_of(a.h.rows, 32), 256, 0, s>>>(
@@ -801,9 +935,8 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     const Targets tg{targets, target_bytes, vocab};
     const float factor = std::is_same_v<F, f16> ? scale / kHalfScale : scale;
     if (rows == 0) {
-      const Finish fin{nullptr, vocab, 0, 0, 0, {dtable, n, 0.f, nullptr, nullptr, nullptr, tg,
-                                                 nullptr, 0}};
-      loss_finish_kernel<F><<<(int)std::min<int64_t>((vocab + 3) / 4, 8192), 256, 0, s>>>(fin);
+      finish<F>(nullptr, vocab, 0, 0, 0, {dtable, n, 0.f, nullptr, nullptr, nullptr, tg, nullptr, 0},
+                s);
       return;
     }
     int* power = (int*)(w + l.power);
@@ -833,7 +966,8 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
         typedef decltype(shape) S;
         a.tiles_m = tiles_of(vs, S::BM);
         a.tiles_n = tiles_of(rows, S::BN);
-        loss_gradient_kernel<F, T, S><<<a.tiles_m * a.tiles_n, S::kThreads, S::kLds, s>>>(a);
+        loss_gradient_kernel<F, T, S>
+            <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
       });
       Product p{};
       p.pairs = l.pairs;

@@ -7,14 +7,12 @@
 // operand is transposed in memory.  Values of 32 bits come as planes of 16-bit parts, and the
 // sum then runs over those pairs of planes whose product is above fp32's last bit.
 //
-// A work-group of four waves (2 x 2) owns BM x BN values, a wave a quarter of it in 32 x 32
-// tiles.  Steps of 32 along k go through three LDS buffers: while one is read, the loads of the
-// next two are on their way, straight into LDS.  Two work-groups share a CU, so that one's
-// epilogue and waits lie under the other's products.
+// A work-group's waves share BM x BN values, in 32 x 32 tiles.  Steps along k go through LDS
+// buffers: while one is read, the loads of the next are on their way, straight into LDS.
 //
 // LDS holds 16-byte pieces of an operand in the order of its memory rows, permuted within a
 // row by the row's number so that the reads below touch every bank equally:
-//   along k: 64 bytes a row; a read takes one piece of each of 32 rows;
+//   along k: a step's values a row; a read takes one piece of each of 32 rows;
 //   across k: 2 BM bytes a row; a transposing read takes 4 rows by 16 columns a quarter wave.
 #pragma once
 
@@ -109,10 +107,11 @@ struct MmStage {
   // value of the step; to: the LDS address of the buffer.
   __device__ __forceinline__ void load(const char* base, int left, uint32_t to) const {
     const uint64_t b = (uint64_t)base;
-    const mm_i32x4 rsrc = {(int)(uint32_t)b, (int)(uint32_t)(b >> 32 & 0xffff), (int)kMmNowhere,
-                           0x00027000};
-    const uint32_t wave_to =
-        to + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
+    const mm_i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
+                           __builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32 & 0xffff)),
+                           (int)kMmNowhere, 0x00027000};
+    const uint32_t wave_to = (uint32_t)__builtin_amdgcn_readfirstlane(
+        (int)(to + (threadIdx.x >> 6) * 1024));
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const uint32_t o = k_first + i * kKStep < left ? off[i] : kMmNowhere;
@@ -159,9 +158,101 @@ struct MmStage {
   }
 };
 
-// WM x WN waves own BM x BN values.
-template <typename T, int BM, int BN, bool kAcrossA, bool kAcrossB, int WM = 2, int WN = 2,
-          int kStep = 32, int kStages = 3>
+// One tile's share of a product.
+struct MmWork {
+  int64_t m0, n0;   // its first row of A and of B
+  int64_t k0, k1;   // the values of k that it sums
+};
+
+// The places of a work-group among `all` tiles that the whole grid shares out.  Consecutive
+// work-groups go to the chip's eight dies in turn, each with an L2 of its own, so a die takes a
+// run of places, and its work-groups take them side by side.
+struct MmPlaces {
+  uint32_t place, end, step;
+  __device__ __forceinline__ explicit MmPlaces(uint32_t all) {
+    const uint32_t die = blockIdx.x % 8, each = all / 8, more = all % 8;
+    const uint32_t first = die * each + (die < more ? die : more);
+    end = first + each + (die < more ? 1 : 0);
+    place = first + blockIdx.x / 8;
+    step = (gridDim.x - die + 7) / 8;
+  }
+  __device__ __forceinline__ bool there() const { return place < end; }
+  __device__ __forceinline__ void next() { place += step; }
+};
+// Work-groups for `all` tiles where `most` fit on the chip at once.
+inline uint32_t mm_grid(uint64_t all, uint32_t most) {
+  return (uint32_t)(all < most ? all : most);
+}
+
+// The tile at a place: runs go through `high` tiles of m before the next of n.
+__device__ __forceinline__ void mm_tile_at(uint32_t place, uint32_t tiles_m, uint32_t tiles_n,
+                                           uint32_t high, uint32_t& tm, uint32_t& tn) {
+  const uint32_t strip = high * tiles_n;
+  const uint32_t s = place / strip, in = place % strip;
+  const uint32_t rows = tiles_m - s * high < high ? tiles_m - s * high : high;
+  tm = s * high + in % rows;
+  tn = in / rows;
+}
+
+// A pointer that is the same in all lanes, known to be.
+template <typename V>
+__device__ __forceinline__ V* mm_uniform(V* p) {
+  const uint64_t b = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32));
+  return (V*)((uint64_t)hi << 32 | lo);
+}
+
+// A tile's values in memory: rows x cols of them are there; loads of the others give zeros, and
+// stores are dropped, without a branch.  pitch: values between rows, 256 of which span less than
+// 2^31 bytes.
+template <typename V>
+struct MmPatch {
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t pitch;
+  int rows, cols;
+  __device__ __forceinline__ MmPatch(V* first, int64_t pitch_, int64_t rows_, int64_t cols_)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc(mm_uniform(first), 0, (int)kMmNowhere, 0x00027000)),
+        pitch((uint32_t)pitch_), rows((int)(rows_ < 65536 ? rows_ : 65536)),
+        cols((int)(cols_ < 65536 ? cols_ : 65536)) {}
+  // A lane's place: a row and a column, and what is left of the rows from there.
+  struct Lane {
+    uint32_t base;
+    int left;
+  };
+  __device__ __forceinline__ Lane lane(int row, int col) const {
+    const uint32_t o = ((uint32_t)row * pitch + (uint32_t)col) * (uint32_t)sizeof(V);
+    return {col < cols ? o : kMmNowhere, rows - row};
+  }
+  // d rows on.  What is added to kMmNowhere leads nowhere, too.
+  __device__ __forceinline__ uint32_t at(const Lane& l, int d) const {
+    const uint32_t o = l.base + (uint32_t)d * pitch * (uint32_t)sizeof(V);
+    return d < l.left ? o : kMmNowhere;
+  }
+  __device__ __forceinline__ V load(uint32_t at) const {
+    static_assert(sizeof(V) == 4);
+    return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)at, 0, 0));
+  }
+  __device__ __forceinline__ void store(uint32_t at, V v) const {
+    if constexpr (sizeof(V) == 4)
+      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rsrc, (int)at, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), rsrc, (int)at, 0, 0);
+  }
+  // 4 neighbours of a row, at a multiple of 8 bytes
+  __device__ __forceinline__ void store4(uint32_t at, const V (&v)[4]) const {
+    static_assert(sizeof(V) == 2);
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    u32x2 d;
+    __builtin_memcpy(&d, v, 8);
+    __builtin_amdgcn_raw_buffer_store_b64(d, rsrc, (int)at, 0, 0);
+  }
+};
+
+// WM x WN waves own BM x BN values at a time.  A work-group goes through its tiles as through one
+// long sum: the first steps of the next tile are on their way while a tile's epilogue runs.
+template <typename T, int BM, int BN, bool kAcrossA, bool kAcrossB, int WM, int WN, int kStep,
+          int kStages>
 struct MmTile {
   static constexpr int kThreads = 64 * WM * WN;
   typedef MmStage<BM, kAcrossA, kStep, kThreads> A;
@@ -172,60 +263,101 @@ struct MmTile {
   static constexpr int kLoads = A::kLoads + B::kLoads;
   mm_f32x16 acc[kI][kJ];
 
-  // Register r of tile (i, j) of a wave holds row row(i, r) and column col(j) of the
+  // Register r of tile (i, j) of a wave holds row row0 + down(i, r) and column col0 + 32 j of the
   // work-group's values.
-  static __device__ __forceinline__ int row(int i, int r) {
-    return (int)(threadIdx.x >> 6) / WN * (BM / WM) + i * 32 + (r >> 2) * 8 +
-           (int)(threadIdx.x >> 5 & 1) * 4 + (r & 3);
+  int row0, col0;
+  static __device__ __forceinline__ constexpr int down(int i, int r) {
+    return i * 32 + (r >> 2) * 8 + (r & 3);
   }
-  static __device__ __forceinline__ int col(int j) {
-    return (int)(threadIdx.x >> 6) % WN * (BN / WN) + j * 32 + (int)(threadIdx.x & 31);
+  static __device__ __forceinline__ int wave() {
+    return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   }
 
-  // lds: the address of kLds bytes, a multiple of 1024; free again on return.
-  __device__ __forceinline__ void run(const MmOperand& a, int64_t m0, const MmOperand& b,
-                                      int64_t n0, int64_t k0, int64_t k1, int pairs,
-                                      uint32_t lds) {
-    A sa;
-    B sb;
-    sa.place(a, m0);
-    sb.place(b, n0);
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const uint32_t a_at = lds + A::lane_at(wave / WN * (BM / WM));
-    const uint32_t b_at = lds + A::kBytes + B::lane_at(wave % WN * (BN / WN));
+  const MmOperand &a, &b;
+  const int pairs;
+  const uint32_t lds;
+  A sa;
+  B sb;
+  MmWork ahead;     // the tile whose steps are being loaded, and where in it
+  int64_t k;
+  int pair;
+  int buffer = 0;   // of the next step to be multiplied
+  uint32_t a_at, b_at;
+
+  // lds: the address of kLds bytes, a multiple of 1024, that nothing else uses.
+  __device__ __forceinline__ MmTile(const MmOperand& a_, const MmOperand& b_, int pairs_,
+                                    uint32_t lds_)
+      : a(a_), b(b_), pairs(pairs_), lds(lds_) {
+    const int wave_row = wave() / WN * (BM / WM), wave_col = wave() % WN * (BN / WN);
+    a_at = lds + A::lane_at(wave_row);
+    b_at = lds + A::kBytes + B::lane_at(wave_col);
+    row0 = wave_row + (int)(threadIdx.x >> 5 & 1) * 4;
+    col0 = wave_col + (int)(threadIdx.x & 31);
+  }
+
+  // Starts the next step's loads.  next(w): the work of the tile after the one that was loaded
+  // last, false where there is none.
+  template <typename Next>
+  __device__ __forceinline__ void load(int to, Next& next) {
+    // past the last step nothing is there: the loads are counted all the same
+    const int left = pair < 6 ? (int)(ahead.k1 - k < kStep ? ahead.k1 - k : kStep) : 0;
+    const int p = pair < 6 ? pair : 5;
+    const int64_t at_a =
+        mm_plane_a(p) * a.plane + (kAcrossA ? k * a.stride + ahead.m0 : ahead.m0 * a.stride + k);
+    const int64_t at_b =
+        mm_plane_b(p) * b.plane + (kAcrossB ? k * b.stride + ahead.n0 : ahead.n0 * b.stride + k);
+    sa.load((const char*)a.p + at_a * 2, left, lds + to * kStage);
+    sb.load((const char*)b.p + at_b * 2, left, lds + to * kStage + A::kBytes);
+    if (pair == 6) return;
+    k += kStep;
+    if (k >= ahead.k1) {
+      k = ahead.k0;
+      if (++pair == 6) begin(next);
+    }
+  }
+  template <typename Next>
+  __device__ __forceinline__ void begin(Next& next) {
+    MmWork w;
+    while (next(w)) {
+      if (w.k0 >= w.k1) continue;  // no steps: see steps_of
+      ahead = w;
+      k = w.k0;
+      pair = 6 - pairs;
+      sa.place(a, w.m0);
+      sb.place(b, w.n0);
+      return;
+    }
+  }
+  __device__ __forceinline__ int steps_of(const MmWork& w) const {
+    return w.k1 > w.k0 ? (int)((w.k1 - w.k0 + kStep - 1) / kStep) * pairs : 0;
+  }
+
+  // Starts the loads of the first tile's first steps; the work-group has one at least.
+  template <typename Next>
+  __device__ __forceinline__ void start(Next& next) {
+    ahead = {0, 0, 0, 0};
+    k = 0;
+    pair = 6;
+    sa.place(a, 0);
+    sb.place(b, 0);
+    begin(next);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) load(i, next);
+  }
+
+  // Sums a tile of so many steps into acc.
+  template <typename Next>
+  __device__ __forceinline__ void sum(int steps, Next& next) {
 #pragma unroll
     for (int i = 0; i < kI; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    const int steps = (int)((k1 - k0 + kStep - 1) / kStep) * pairs;
-    if (steps <= 0) return;
-    int64_t k = k0;
-    int pair = 6 - pairs;
-    // past the last step nothing is there: the loads are counted all the same
-    auto load = [&](int buffer) {
-      const int left = pair < 6 ? (int)(k1 - k < kStep ? k1 - k : kStep) : 0;
-      const int p = pair < 6 ? pair : 5;
-      const int64_t at_a =
-          mm_plane_a(p) * a.plane + (kAcrossA ? k * a.stride + m0 : m0 * a.stride + k);
-      const int64_t at_b =
-          mm_plane_b(p) * b.plane + (kAcrossB ? k * b.stride + n0 : n0 * b.stride + k);
-      sa.load((const char*)a.p + at_a * 2, left, lds + buffer * kStage);
-      sb.load((const char*)b.p + at_b * 2, left, lds + buffer * kStage + A::kBytes);
-      k += kStep;
-      if (k >= k1) {
-        k = k0;
-        ++pair;
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) load(i);
-    int buffer = 0;
     for (int step = 0; step < steps; ++step) {
       mm_wait_loads<(kStages - 2) * kLoads>();  // this step's; the next ones' stay in flight
       mm_barrier();
-      load(buffer == 0 ? kStages - 1 : buffer - 1);
+      load(buffer == 0 ? kStages - 1 : buffer - 1, next);
       const uint32_t at = buffer * kStage;
 #pragma unroll
       for (int s = 0; s < kStep / 16; ++s) {
@@ -241,26 +373,10 @@ struct MmTile {
       }
       buffer = buffer == kStages - 1 ? 0 : buffer + 1;
     }
-    mm_wait_loads<0>();
-    mm_barrier();
   }
+
+  // What was loaded past the last tile has arrived: LDS may be given back.
+  __device__ __forceinline__ void stop() { mm_wait_loads<0>(); }
 };
-
-// The place of a work-group among `all`: consecutive work-groups go to the chip's eight dies in
-// turn, each with an L2 of its own, so a die takes a run of places.
-__device__ __forceinline__ uint32_t mm_place_of(uint32_t index, uint32_t all) {
-  const uint32_t each = all / 8, more = all % 8, die = index % 8;
-  return die * each + (die < more ? die : more) + index / 8;
-}
-
-// The tile at a place: runs go through `high` tiles of m before the next of n.
-__device__ __forceinline__ void mm_tile_at(uint32_t place, uint32_t tiles_m, uint32_t tiles_n,
-                                           uint32_t high, uint32_t& tm, uint32_t& tn) {
-  const uint32_t strip = high * tiles_n;
-  const uint32_t s = place / strip, in = place % strip;
-  const uint32_t rows = tiles_m - s * high < high ? tiles_m - s * high : high;
-  tm = s * high + in % rows;
-  tn = in / rows;
-}
 
 }  // namespace sieve

@@ -6,17 +6,17 @@
 // (with |G| the root of the sum of squares; matrices taller than wide: A = X^T X, X <- X B).  Each
 // step maps every singular value s of X to a s + b s^3 + c s^5 and leaves the singular vectors.
 //
-// A step is three products and nothing else: A and A A are symmetric, so only the tiles on and
-// below the diagonal are computed and written to both sides; B is made in the epilogue of A A,
-// with a on its diagonal, so that the third product's accumulators are the next X.
+// A step is three products and nothing else: A = X X^T with C = b I + c A in its epilogue, then
+// B = a I + A C, then B X, whose accumulators are the next X.  A, C and B are symmetric: only the
+// tiles on and below the diagonal are computed, those below it written to both sides.
 //
 // What is weak in G is multiplied by up to a^steps (484 for the usual five), and rounding errors
 // with it, so 16-bit values are not enough between the products, whatever G's type is.  Every
 // matrix is kept as two binary16 parts, hi = round(v), lo = round(v - hi): 24 bits together, and
 // a product is hi hi + hi lo + lo hi, summed in fp32.  That is fp32's precision at a third of
 // the 16-bit rate, 5 times the fp32 matrix rate.  All values are bounded by singular values, so
-// fixed powers of two keep them in binary16's range (kScale): |X| below 4, |A| and |B| below 16,
-// which the host checks for the coefficients that it is given.
+// fixed powers of two keep them in binary16's range (kScaleX, kScaleA): |X| below 4, |A|, |B| and
+// |C| below 16, which the host checks for the coefficients that it is given.
 //
 // The matrix units bound it from some 256 x 256 on, launches below.
 #include <math.h>
@@ -34,12 +34,23 @@ typedef __bf16 bf16;
 typedef _Float16 f16;
 
 constexpr int kThreads = 256;
-constexpr int kTileSize = 128;
+// A work-group's tile: the usual one at two work-groups a CU; one for few tiles, which are bound
+// by the latency of their loads, with more of these on their way.
+template <int kSide_, int kStages>
+struct Shape {
+  static constexpr int kSide = kSide_;
+  template <bool kAcrossA, bool kAcrossB>
+  using Tile = MmTile<mm_f16, kSide, kSide, kAcrossA, kAcrossB, 2, 2, 64, kStages>;
+  static constexpr int kLds = Tile<false, false>::kLds;
+};
+typedef Shape<128, 2> Usual;
+typedef Shape<64, 4> Few;
 constexpr float kScaleX = 16384.f, kScaleA = 4096.f;  // of X; of A and B
 constexpr double kMaxX = 3.9, kMaxA = 15.9;           // below 65504 times these
 constexpr int kMaxSide = 65536;
 constexpr int kMaxSteps = 1000;
 constexpr int kSums = 64;                             // parts of a matrix's sum of squares
+constexpr int64_t kFewTiles = 128;                    // of the usual shape
 constexpr int64_t kMostBytes = int64_t(1) << 31;      // of the workspace, for one matrix or more
 
 struct Source {
@@ -103,73 +114,136 @@ struct Product {
   int64_t rows, cols;    // that are written: zeros past the matrix's, up to the pitch
   int64_t side;
   uint32_t tiles, tiles_m, tiles_n;  // tiles of a matrix
-  float fa, fb, fc;      // B's coefficients
-  const f16* gram;       // A, for B
+  uint32_t all;
+  float fa, fb, fc;      // the coefficients
   void* out;             // planes or the result
+  void* second;          // b I + c A, with A
   int64_t pitch, next, plane;
 };
 
 enum { kGram, kPolynomial, kUpdate, kLast };
 
-template <typename T, int kKind, bool kAcrossA, bool kAcrossB>
-__global__ __launch_bounds__(kThreads, 3) void orth_product_kernel(Product a) {
-  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
-  const uint32_t place = mm_place_of(blockIdx.x, gridDim.x);
-  const int64_t matrix = place / a.tiles;
-  const uint32_t in = place % a.tiles;
-  uint32_t tm, tn;
-  if constexpr (kKind == kGram || kKind == kPolynomial) {
-    // tiles on and below the diagonal, row by row
-    tm = (uint32_t)((sqrtf(8.f * in + 1.f) - 1.f) * 0.5f);
-    while (tm * (tm + 1) / 2 > in) --tm;
-    while ((tm + 1) * (tm + 2) / 2 <= in) ++tm;
-    tn = in - tm * (tm + 1) / 2;
-  } else {
-    mm_tile_at(in, a.tiles_m, a.tiles_n, 8, tm, tn);
+// The tiles of every matrix's product.
+template <int kKind, int kSide>
+struct Tiles {
+  MmPlaces at;
+  uint32_t tiles, tiles_m, tiles_n;
+  int64_t k;
+  __device__ __forceinline__ explicit Tiles(const Product& a)
+      : at(a.all), tiles(a.tiles), tiles_m(a.tiles_m), tiles_n(a.tiles_n), k(a.k) {}
+  __device__ __forceinline__ void get(MmWork& w, int64_t& matrix) const {
+    matrix = at.place / tiles;
+    const uint32_t in = at.place % tiles;
+    uint32_t tm, tn;
+    if constexpr (kKind == kGram || kKind == kPolynomial) {
+      // tiles on and below the diagonal, row by row
+      tm = (uint32_t)((sqrtf(8.f * in + 1.f) - 1.f) * 0.5f);
+      while (tm * (tm + 1) / 2 > in) --tm;
+      while ((tm + 1) * (tm + 2) / 2 <= in) ++tm;
+      tn = in - tm * (tm + 1) / 2;
+    } else {
+      mm_tile_at(in, tiles_m, tiles_n, 8, tm, tn);
+    }
+    w = {(int64_t)tm * kSide, (int64_t)tn * kSide, 0, k};
   }
-  const int64_t m0 = (int64_t)tm * kTileSize, n0 = (int64_t)tn * kTileSize;
+};
+
+template <typename T, int kKind, typename S, bool kAcrossA, bool kAcrossB>
+__global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+  typedef typename S::template Tile<kAcrossA, kAcrossB> Tile;
+  Tiles<kKind, S::kSide> tiles(a);
+  // one tile a work-group: matrices lie apart
+  MmWork w;
+  int64_t matrix;
+  tiles.get(w, matrix);
   MmOperand x = a.a, y = a.b;
   x.p = (const f16*)x.p + matrix * a.a_next;
   y.p = (const f16*)y.p + matrix * a.b_next;
-  typedef MmTile<f16, kTileSize, kTileSize, kAcrossA, kAcrossB> Tile;
-  Tile t;
-  t.run(x, m0, y, n0, 0, a.k, 3,
-        (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_memory);
-  const int64_t first = matrix * a.next;
+  Tile t(x, y, 3,
+         (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_memory);
+  bool first_one = true;
+  auto next = [&](MmWork& to) {
+    to = w;
+    const bool was = first_one;
+    first_one = false;
+    return was;
+  };
+  t.start(next);
+  t.sum(t.steps_of(w), next);
+  const int64_t at = matrix * a.next + w.m0 * a.pitch + w.n0;
+  const int64_t rows = a.rows - w.m0, cols = a.cols - w.n0;
+  if constexpr (kKind == kLast) {
+    const MmPatch<T> to((T*)a.out + at, a.pitch, rows, cols);
+#pragma unroll
+    for (int j = 0; j < Tile::kJ; ++j) {
+      const auto lane = to.lane(t.row0, t.col0 + 32 * j);
+#pragma unroll
+      for (int i = 0; i < Tile::kI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          to.store(to.at(lane, Tile::down(i, r)),
+                   (T)(t.acc[i][j][r] * (1.f / (kScaleA * kScaleX))));
+    }
+    t.stop();
+    return;
+  }
+  const MmPatch<f16> hi((f16*)a.out + at, a.pitch, rows, cols);
+  const MmPatch<f16> lo((f16*)a.out + a.plane + at, a.pitch, rows, cols);
+  // A and B below the diagonal also go to the other side of it; tiles on it are whole
+  const int64_t other = matrix * a.next + w.n0 * a.pitch + w.m0;
+  const bool mirrored = kKind != kUpdate && w.m0 != w.n0;
+  const MmPatch<f16> hi2((f16*)a.out + other, a.pitch, mirrored ? cols : 0, rows);
+  const MmPatch<f16> lo2((f16*)a.out + a.plane + other, a.pitch, mirrored ? cols : 0, rows);
+  // and with A goes b I + c A
+  f16* second = (f16*)a.second;
+  const MmPatch<f16> hi3(second + at, a.pitch, rows, cols);
+  const MmPatch<f16> lo3(second + a.plane + at, a.pitch, rows, cols);
+  const MmPatch<f16> hi4(second + other, a.pitch, mirrored ? cols : 0, rows);
+  const MmPatch<f16> lo4(second + a.plane + other, a.pitch, mirrored ? cols : 0, rows);
 #pragma unroll
   for (int j = 0; j < Tile::kJ; ++j) {
-    const int64_t n = n0 + Tile::col(j);
+    const int col = t.col0 + 32 * j;
+    const auto lane = hi.lane(t.row0, col);
+    const int64_t gap = w.n0 + col - w.m0 - t.row0;  // rows down to the diagonal
+    const int diagonal = w.n0 + col < a.side && gap >= 0 && gap < S::kSide ? (int)gap : -1;
 #pragma unroll
     for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + Tile::row(i, r);
-        if (m >= a.rows || n >= a.cols) continue;
-        float v = t.acc[i][j][r];
-        if constexpr (kKind == kLast) {
-          ((T*)a.out)[first + m * a.pitch + n] = (T)(v * (1.f / (kScaleA * kScaleX)));
-        } else if constexpr (kKind == kUpdate) {
-          f16* p = (f16*)a.out + first + m * a.pitch + n;
-          split(v * (1.f / kScaleA), p[0], p[a.plane]);
-        } else {
-          // one value for both sides: the lower one's
-          if (m < n) continue;
-          f16* p = (f16*)a.out + first;
-          const int64_t at = m * a.pitch + n, mirror = n * a.pitch + m;
+      for (int g = 0; g < 4; ++g) {
+        f16 h[4], l[4], h3[4], l3[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = Tile::down(i, 4 * g + e);
+          float v = t.acc[i][j][4 * g + e];
+          if constexpr (kKind == kGram) v *= kScaleA / (kScaleX * kScaleX);
+          else v *= 1.f / kScaleA;
+          if constexpr (kKind == kPolynomial) v += d == diagonal ? a.fa * kScaleA : 0.f;
+          split(v, h[e], l[e]);
+          const uint32_t o = hi.at(lane, d);
+          hi.store(o, h[e]);
+          lo.store(o, l[e]);
           if constexpr (kKind == kGram) {
-            v *= kScaleA / (kScaleX * kScaleX);
-          } else {
-            const f16* g = a.gram + first + at;
-            v = a.fc * (v * (1.f / kScaleA)) + a.fb * ((float)g[0] + (float)g[a.plane]);
-            if (m == n && m < a.side) v += a.fa * kScaleA;
+            split(a.fc * v + (d == diagonal ? a.fb * kScaleA : 0.f), h3[e], l3[e]);
+            hi3.store(o, h3[e]);
+            lo3.store(o, l3[e]);
           }
-          f16 hi, lo;
-          split(v, hi, lo);
-          p[at] = p[mirror] = hi;
-          p[a.plane + at] = p[a.plane + mirror] = lo;
+        }
+        if (mirrored) {
+          // the lane's column is a row there, its 4 rows neighbours in it (all there, or none)
+          const int d = Tile::down(i, 4 * g);
+          const uint32_t o = t.row0 + d < hi2.cols && col < hi2.rows
+                                 ? ((uint32_t)col * hi2.pitch + t.row0 + d) * 2 : kMmNowhere;
+          hi2.store4(o, h);
+          lo2.store4(o, l);
+          if constexpr (kKind == kGram) {
+            hi4.store4(o, h3);
+            lo4.store4(o, l3);
+          }
         }
       }
   }
+  t.stop();
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -179,7 +253,7 @@ int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 struct Layout {
   int64_t side, pitch, side_pitch;  // of A and B; of X's rows; of A's and B's rows
   int64_t batch;                    // matrices at a time
-  int64_t sums, x[2], gram, poly, bytes;
+  int64_t sums, x[2], gram, second, poly, bytes;
 };
 
 Layout layout_of(int64_t batch, int64_t m, int64_t n) {
@@ -187,9 +261,9 @@ Layout layout_of(int64_t batch, int64_t m, int64_t n) {
   l.side = std::min(m, n);
   l.pitch = (n + 7) & ~int64_t(7);
   l.side_pitch = (l.side + 7) & ~int64_t(7);
-  const int64_t one = 2 * 2 * 2 * (m * l.pitch + l.side_pitch * l.side_pitch);
+  const int64_t one = 4 * (2 * m * l.pitch + 3 * l.side_pitch * l.side_pitch);
   // a launch's work-groups have fewer than 2^32 threads
-  const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128);
+  const int64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
   l.batch = std::max<int64_t>(1, std::min({batch, kMostBytes / one, (int64_t(1) << 23) / tiles,
                                            int64_t(65535)}));
   int64_t at = 0;
@@ -201,6 +275,7 @@ Layout layout_of(int64_t batch, int64_t m, int64_t n) {
   l.sums = take(l.batch * kSums * 8);
   for (int i = 0; i < 2; ++i) l.x[i] = take(l.batch * m * l.pitch * 4);
   l.gram = take(l.batch * l.side_pitch * l.side_pitch * 4);
+  l.second = take(l.batch * l.side_pitch * l.side_pitch * 4);
   l.poly = take(l.batch * l.side_pitch * l.side_pitch * 4);
   l.bytes = at;
   return l;
@@ -231,6 +306,7 @@ bool in_range(double a, double b, double c, int steps) {
     }
     for (double r : roots)
       if (r > 0.0 && r < s * s) top = std::max(top, p(sqrt(r)));
+    most = std::max({most, fabs(b), fabs(b + c * s * s)});  // of b I + c A
     if (!(s * s <= kMaxA && most <= kMaxA && top <= kMaxX)) return false;
     s = top;
   }
@@ -245,8 +321,7 @@ int check_orth(int64_t batch, int64_t m, int64_t n) {
   return SIEVE_OK;
 }
 
-constexpr int kLds = MmTile<f16, kTileSize, kTileSize, false, false>::kLds;
-static_assert(kLds <= 65536, "no larger LDS has to be asked for");
+static_assert(Usual::kLds <= 65536 && Few::kLds <= 65536, "no larger LDS has to be asked for");
 
 template <typename T>
 void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t m,
@@ -262,16 +337,33 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     return;
   }
   orth_scale_kernel<T, false><<<rows, 256, 0, s>>>(src);
-  const int64_t side = l.side, sp = l.side_pitch;
-  const int64_t square = sp * sp;
-  const uint32_t ts = (uint32_t)((side + kTileSize - 1) / kTileSize);
-  f16 *gram = (f16*)(w + l.gram), *poly = (f16*)(w + l.poly);
-  const MmOperand of_a{gram, sp, side, batch * square}, of_b{poly, sp, side, batch * square};
+  const int64_t side = l.side, sp = l.side_pitch, square = sp * sp;
+  f16 *gram = (f16*)(w + l.gram), *second = (f16*)(w + l.second), *poly = (f16*)(w + l.poly);
+  const MmOperand of_a{gram, sp, side, batch * square}, of_c{second, sp, side, batch * square},
+      of_b{poly, sp, side, batch * square};
+  // the product's kernel with tiles of the shape that it asks for
+  auto launch = [&](Product p, auto kind, auto across_a, auto across_b) {
+    constexpr int kKind = decltype(kind)::value;
+    constexpr bool kA = decltype(across_a)::value, kB = decltype(across_b)::value;
+    constexpr bool kHalf = kKind == kGram || kKind == kPolynomial;
+    auto with = [&](auto shape) {
+      typedef decltype(shape) S;
+      p.tiles_m = (uint32_t)((p.rows + S::kSide - 1) / S::kSide);
+      p.tiles_n = (uint32_t)((p.cols + S::kSide - 1) / S::kSide);
+      p.tiles = kHalf ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+      p.all = p.tiles * (uint32_t)batch;
+      orth_product_kernel<T, kKind, S, kA, kB><<<p.all, kThreads, S::kLds, s>>>(p);
+    };
+    const int64_t tiles = ((p.rows + 127) / 128) * ((p.cols + 127) / 128) * batch;
+    if (tiles / (kHalf ? 2 : 1) <= kFewTiles) with(Few{});
+    else with(Usual{});
+  };
+  const std::integral_constant<bool, true> across;
+  const std::integral_constant<bool, false> along;
   for (int i = 0; i < steps; ++i) {
     const f16* x = (const f16*)(w + l.x[i & 1]);
     f16* to = (f16*)(w + l.x[(i + 1) & 1]);
     const bool last = i == steps - 1;
-    const uint32_t half = ts * (ts + 1) / 2;
     // A: over the longer side
     Product p{};
     p.a = p.b = {x, l.pitch, side, src.plane};
@@ -279,28 +371,24 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     p.k = tall ? m : n;
     p.rows = p.cols = sp;
     p.side = side;
-    p.tiles = half;
-    p.out = gram;
-    p.pitch = sp;
-    p.next = square;
-    p.plane = batch * square;
-    if (tall)
-      orth_product_kernel<T, kGram, true, true>
-          <<<half * (uint32_t)batch, kThreads, kLds, s>>>(p);
-    else
-      orth_product_kernel<T, kGram, false, false>
-          <<<half * (uint32_t)batch, kThreads, kLds, s>>>(p);
-    // B
-    p.a = p.b = of_a;
-    p.a_next = p.b_next = square;
-    p.k = side;
     p.fa = coefficients[0];
     p.fb = coefficients[1];
     p.fc = coefficients[2];
-    p.gram = gram;
+    p.out = gram;
+    p.second = second;
+    p.pitch = sp;
+    p.next = square;
+    p.plane = batch * square;
+    const std::integral_constant<int, kGram> gram_kind;
+    if (tall) launch(p, gram_kind, across, across);
+    else launch(p, gram_kind, along, along);
+    // B
+    p.a = of_a;
+    p.b = of_c;
+    p.a_next = p.b_next = square;
+    p.k = side;
     p.out = poly;
-    orth_product_kernel<T, kPolynomial, false, false>
-        <<<half * (uint32_t)batch, kThreads, kLds, s>>>(p);
+    launch(p, std::integral_constant<int, kPolynomial>{}, along, along);
     // the next X, or the result
     p.a = tall ? MmOperand{x, l.pitch, m, src.plane} : of_b;
     p.b = tall ? of_b : MmOperand{x, l.pitch, n, src.plane};
@@ -308,22 +396,16 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     p.b_next = tall ? square : m * l.pitch;
     p.rows = m;
     p.cols = last ? n : l.pitch;
-    p.tiles_m = (uint32_t)((m + kTileSize - 1) / kTileSize);
-    p.tiles_n = (uint32_t)((n + kTileSize - 1) / kTileSize);
-    p.tiles = p.tiles_m * p.tiles_n;
     p.out = last ? out : (void*)to;
     p.pitch = last ? n : l.pitch;
     p.next = m * p.pitch;
     p.plane = src.plane;
-    const uint32_t grid = p.tiles * (uint32_t)batch;
-    if (tall && last)
-      orth_product_kernel<T, kLast, false, false><<<grid, kThreads, kLds, s>>>(p);
-    else if (tall)
-      orth_product_kernel<T, kUpdate, false, false><<<grid, kThreads, kLds, s>>>(p);
-    else if (last)
-      orth_product_kernel<T, kLast, false, true><<<grid, kThreads, kLds, s>>>(p);
-    else
-      orth_product_kernel<T, kUpdate, false, true><<<grid, kThreads, kLds, s>>>(p);
+    const std::integral_constant<int, kUpdate> update;
+    const std::integral_constant<int, kLast> the_last;
+    if (tall && last) launch(p, the_last, along, along);
+    else if (tall) launch(p, update, along, along);
+    else if (last) launch(p, the_last, along, across);
+    else launch(p, update, along, across);
   }
 }
 

@@ -118,5 +118,5 @@ def test_orthogonalize_argument_errors_without_a_gpu(lib):
     assert call(batch=0, steps=1, c=(8, -8, 0)) == 0 and call(batch=0, steps=1, c=(11, -11, 0)) == -4
     assert lib.sieve_orthogonalize_workspace(0, 8, 8) == 0
     assert lib.sieve_orthogonalize_workspace(1, 0, 8) == -1
-    # X twice, A and B, each in two parts of 2 bytes
-    assert lib.sieve_orthogonalize_workspace(2, 64, 128) == 2 * 8 * (64 * 128 + 64 * 64) + 1024
+    # X twice, and three products, each in two parts of 2 bytes
+    assert lib.sieve_orthogonalize_workspace(2, 64, 128) == 2 * 4 * (2 * 64 * 128 + 3 * 64 * 64) + 1024
