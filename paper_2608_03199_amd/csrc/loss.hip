@@ -18,9 +18,13 @@
 // 16-bit inputs are multiplied as they are.  32-bit ones come as three bf16 planes whose sum is
 // the value (8 bits each), six products of planes: what is left out is below fp32's last bit.
 //
-// g is rounded once, to the inputs' type; binary16 does not have fp32's range, so there it is
-// scaled by 2^14.  dloss enters g by its mantissa only: its power of two goes, exactly, into a
-// row's factor of dh and into the copy of h that dw's product reads.
+// g is rounded once, to the inputs' type, and what its target has outweighs the rest of its row:
+// g_t,target = -(1 - p_t) dloss_t.  A rounding of it would be the same for every token of a
+// frequent word and add up over them, so each row is divided by c_t = 1 - p_t first, from a dot
+// product of its own: its target's value is then -1, and the others are at most 1 together.
+// dloss_t c_t is a row's exact factor of dh; in dw's product it goes with h, where its rounding is
+// another one for each value and column.  binary16 does not have fp32's range: there g is scaled
+// by 2^14, and h's factors by a power of two that brings the largest below 1.
 #include <math.h>
 
 #include <algorithm>
@@ -94,11 +98,9 @@ __device__ __forceinline__ Part join(Part a, Part b) {
   return {top, a.sum * exp2_of(a.top - at) + b.sum * exp2_of(b.top - at)};
 }
 
-// A row's dloss: the mantissa, with its sign, and the power of two; (0, 0) where the row gives
-// no gradient.
+// What a row's g is divided by, inverse (0 where the row gives no gradient), and its factor.
 struct Row {
-  float mantissa;
-  int power;
+  float inverse, factor;
 };
 
 struct Logits {
@@ -116,7 +118,6 @@ struct Logits {
   // backward
   const float* lse;
   const Row* row;        // [rows]
-  float* rest;           // [rows]: what rounding took from the target's g
   void* g;               // [planes][rows][g_stride]
   int64_t g_stride, g_plane;
 };
@@ -255,32 +256,72 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const Part* part, const 
         targets.at(t_first + row) < 0 ? 0.f : (more + (p.top - target_logit[row])) * kLn2;
 }
 
-__device__ __forceinline__ Row row_of(const Targets& targets, const float* dloss, int64_t row) {
-  const float d = dloss[row];
-  if (targets.at(row) < 0 || d == 0.f) return {0.f, 0};
-  if (!isfinite(d)) return {d, 0};
-  int e;
-  const float m = frexpf(d, &e);
-  return {2.f * m, e - 1};
+// The rows' factors, a wave a row, and the largest of them of each work-group.
+struct Rows {
+  const void *h, *table;
+  int64_t h_stride, t_stride, rows;
+  int n;
+  float scale;
+  Targets targets;
+  const float *lse, *dloss;
+  Row* to;
+  float* largest;        // [work-group]
+};
+constexpr int kMostLargest = 1024;
+
+template <typename F, int E>
+__global__ __launch_bounds__(256) void loss_rows_kernel(Rows a) {
+  __shared__ float s[4];
+  const int lane = threadIdx.x & 63;
+  float largest = 0.f;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows;
+       row += (int64_t)gridDim.x * 4) {
+    const int64_t target = a.targets.at(row);
+    const float d = a.dloss[row];
+    Row r{0.f, 0.f};
+    if (target >= 0 && d != 0.f) {
+      const F* h = (const F*)a.h + row * a.h_stride;
+      const F* w = (const F*)a.table + target * a.t_stride;
+      float dot = 0.f;
+      for (int col = lane * E; col < a.n; col += 64 * E) {
+        if constexpr (E > 1) {
+          const EncVec<F, E> x = enc_load<F, E>(h + col), y = enc_load<F, E>(w + col);
+#pragma unroll
+          for (int j = 0; j < E; ++j) dot = fmaf((float)x.v[j], (float)y.v[j], dot);
+        } else {
+          dot = fmaf((float)h[col], (float)w[col], dot);
+        }
+      }
+#pragma unroll
+      for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
+      const float logit = dot * a.scale, lse = a.lse[row];
+      // 1 - p, but no less than what rounding leaves of it: the others of the row may be as much
+      const float least = 0x1p-20f * (4.f + fabsf(logit) + fabsf(lse));
+      const float c = fmaxf(-expm1f(logit - lse), least);
+      r = {1.f / c, c * d};
+    }
+    if (lane == 0) a.to[row] = r;
+    if (isfinite(r.factor)) largest = fmaxf(largest, fabsf(r.factor));
+  }
+  if (lane == 0) s[threadIdx.x >> 6] = largest;
+  __syncthreads();
+  if (threadIdx.x == 0) a.largest[blockIdx.x] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
 }
 
-// The rows' weights, and the largest of their powers of two.
-__global__ __launch_bounds__(1024) void loss_rows_kernel(Targets targets, const float* dloss,
-                                                         int64_t rows, Row* to, int* power) {
-  __shared__ int s[16];
-  int top = -1000;
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) {
-    const Row w = row_of(targets, dloss, r);
-    to[r] = w;
-    if (w.mantissa != 0.f) top = max(top, w.power);
-  }
+// The power of two next above all of the rows' factors.
+__global__ __launch_bounds__(256) void loss_power_kernel(const float* largest, int count,
+                                                         int* power) {
+  __shared__ float s[4];
+  float top = 0.f;
+  for (int i = threadIdx.x; i < count; i += 256) top = fmaxf(top, largest[i]);
 #pragma unroll
-  for (int o = 32; o; o >>= 1) top = max(top, __shfl_xor(top, o));
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; ++i) top = max(top, s[i]);
-    *power = top == -1000 ? 0 : top;
+    int e = 0;
+    frexpf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), &e);
+    *power = e;
   }
 }
 
@@ -297,8 +338,8 @@ __device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
 }
 
 // Rows of n values as the products take them: zeros up to the next multiple of 8, 32-bit values
-// as planes; with `row` each row times its weight's power of two over the largest, or zeros where
-// it has none.
+// as planes; with `row` each row times its factor (over the power of two), or zeros where it has
+// none.
 struct Pack {
   const void* x;
   int64_t stride, rows;
@@ -321,13 +362,12 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
     float factor = 1.f;
     if (a.row) {
       const Row w = a.row[row];
-      factor = w.mantissa == 0.f ? 0.f : ldexpf(1.f, w.power - *a.power);
+      factor = w.inverse == 0.f ? 0.f : a.power ? ldexpf(w.factor, -*a.power) : w.factor;
     }
     const T* x = (const T*)a.x + row * a.stride + col;
     EncVec<U, 8> out[3];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      // the factor is a power of two: nothing is rounded but what leaves binary16's range
       const float v = col + j < a.n && factor != 0.f ? (float)x[j] * factor : 0.f;
       if constexpr (std::is_same_v<T, float>) {
         bf16 p[3];
@@ -363,17 +403,17 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
     const int64_t first = w.m0 + wave_m * kWave;
     const int left = (int)(a.w.rows - first < kWave ? a.w.rows - first : kWave);
     int rel[Tile::kJ];
-    float weight[Tile::kJ], lse2[Tile::kJ];
+    float inverse[Tile::kJ], lse2[Tile::kJ];
 #pragma unroll
     for (int j = 0; j < Tile::kJ; ++j) {
       const int64_t row = w.n0 + t.col0 + 32 * j;
       rel[j] = -1;
-      weight[j] = lse2[j] = 0.f;
+      inverse[j] = lse2[j] = 0.f;
       if (row < a.h.rows) {
         const int64_t v = a.targets.at(row), at = v - a.v_first - first;
         if (v >= 0 && at >= 0 && at < kWave) rel[j] = (int)at;
-        weight[j] = a.row[row].mantissa;
-        if constexpr (std::is_same_v<F, f16>) weight[j] *= kHalfScale;
+        inverse[j] = a.row[row].inverse;
+        if constexpr (std::is_same_v<F, f16>) inverse[j] *= kHalfScale;
         lse2[j] = a.lse[row] * kLog2e;
       }
     }
@@ -388,14 +428,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
       for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[i][r] = exp2_of(fmaf(t.acc[i][j][r], a.c2, -lse2[j]));
-      each_target(p, rel[j], [&](float x) {
-        x -= 1.f;
-        if constexpr (!std::is_same_v<F, float>) {
-          const float own = x * weight[j];
-          a.rest[row] = own - (float)(T)own;
-        }
-        return x;
-      });
+      each_target(p, rel[j], [](float x) { return x - 1.f; });
 #pragma unroll
       for (int i = 0; i < Tile::kI; ++i) {
         f32x16 x = p[i];
@@ -404,9 +437,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
           for (int r = 0; r < 16; ++r)
             if (Tile::down(i, r) >= left - 4 * half) x[r] = 0.f;
         }
-        // a row without weight gives nothing, whatever it holds
+        // a row without a factor gives nothing, whatever it holds
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = weight[j] == 0.f ? 0.f : x[r] * weight[j];
+        for (int r = 0; r < 16; ++r) x[r] = inverse[j] == 0.f ? 0.f : x[r] * inverse[j];
         // pairs of 16-bit values; halves of a wave change places so that each lane has 8
         // neighbours
 #pragma unroll
@@ -446,37 +479,16 @@ struct Final {
   void* out;               // [rows][n]
   int n;
   float factor;            // scale, over what g was scaled by
-  const int* power;        // dtable: the largest of the rows'
-  const Row* row;          // dh: the row's own; zeros where it has no weight
-  // dh of 16-bit inputs: what rounding took from the target's g, times the target's vector
-  const float* rest;
-  Targets targets;
-  const void* table;
-  int64_t t_stride;
+  const int* power;        // dtable: the power of two that h was divided by, where it was
+  const Row* row;          // dh: the row's own factor; zeros where it has none
 };
 
-// A row's values from their sums.
-template <typename F>
-struct Gradient {
-  float factor, rest = 0.f;
-  const F* target = nullptr;
-  __device__ __forceinline__ Gradient(const Final& a, int64_t row) {
-    if (!a.row) {
-      factor = a.power ? ldexpf(a.factor, *a.power) : 0.f;
-      return;
-    }
-    const Row w = a.row[row];
-    factor = w.mantissa == 0.f ? 0.f : ldexpf(a.factor, w.power);
-    if (a.rest && factor != 0.f) {
-      rest = a.rest[row];
-      target = (const F*)a.table + a.targets.at(row) * a.t_stride;
-    }
-  }
-  __device__ __forceinline__ float operator()(float sum, int64_t col) const {
-    if (target) sum += rest * (float)target[col];
-    return factor == 0.f ? 0.f : sum * factor;
-  }
-};
+// A row's factor.
+__device__ __forceinline__ float factor_of(const Final& a, int64_t row) {
+  if (!a.row) return a.power ? ldexpf(a.factor, *a.power) : a.factor;
+  const Row w = a.row[row];
+  return w.inverse == 0.f ? 0.f : w.factor * a.factor;
+}
 
 // A gradient's product: sums in fp32, [split][rows of m][pitch], or added to what is there; or
 // the gradient itself.
@@ -543,13 +555,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product a)
         for (int r = 0; r < 16; ++r) {
           // rows past the last one are the last one again, and not stored
           const int64_t row = w.m0 + t.row0 + Tile::down(i, r);
-          const Gradient<F> g(a.final, row < a.rows ? row : a.rows - 1);
+          const float factor = factor_of(a.final, row < a.rows ? row : a.rows - 1);
 #pragma unroll
-          for (int j = 0; j < Tile::kJ; ++j) {
-            const int64_t n = w.n0 + t.col0 + 32 * j;
+          for (int j = 0; j < Tile::kJ; ++j)
             to.store(to.at(lane[j], Tile::down(i, r)),
-                     (F)g(t.acc[i][j][r], n < a.b.rows ? n : a.b.rows - 1));
-          }
+                     (F)(factor == 0.f ? 0.f : t.acc[i][j][r] * factor));
         }
     } else {
       const MmPatch<float> to(a.out + split * a.split + w.m0 * a.pitch + w.n0, a.pitch,
@@ -593,7 +603,7 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
       const int in = a.pieces == 1 ? i : (int)__umulhi((uint32_t)i, a.mul);
       const int64_t row = first + in;
       const int col = (i - in * a.pieces) * 4;
-      const Gradient<F> g(a.final, row);
+      const float factor = factor_of(a.final, row);
       float v[4] = {0.f, 0.f, 0.f, 0.f};
       const float* x = a.x + row * a.pitch + col;  // rows are padded to multiples of 8
 #pragma unroll 4
@@ -605,7 +615,7 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
       F* out = (F*)a.final.out + row * a.final.n + col;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (col + e < a.final.n) out[e] = (F)g(v[e], col + e);
+        if (col + e < a.final.n) out[e] = (F)(factor == 0.f ? 0.f : v[e] * factor);
     }
   }
 }
@@ -647,7 +657,7 @@ struct Layout {
   int64_t k;                     // n, up to the next multiple of 8
   int planes, pairs;
   Spread h_spread, w_spread;
-  int64_t h, w, part, target, g, weighed, row, rest, dh, dw, power, bytes;
+  int64_t h, w, part, target, g, weighed, row, largest, dh, dw, power, bytes;
 };
 
 Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool backward) {
@@ -677,7 +687,7 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
     l.g = take(rows * l.piece * 2 * l.planes);
     l.weighed = take(rows * l.k * 2 * l.planes);
     l.row = take(rows * (int64_t)sizeof(Row));
-    l.rest = take(rows * 4);
+    l.largest = take(kMostLargest * 4);
     l.dh = take(l.h_spread.splits * rows * l.k * 4);
     l.dw = take(l.w_spread.splits * l.piece * l.k * 4);
     l.power = take(4);
@@ -724,6 +734,11 @@ void pack(const void* x, int64_t stride, int64_t rows, int32_t n, int64_t k, voi
           const int* power = nullptr) {
   const Pack a{x, stride, rows, n, (int)k, to, plane, row, power};
   loss_pack_kernel<T><<<blocks_of(rows * (k / 8)), 256, 0, s>>>(a);
+}
+
+template <typename F>
+bool rows_aligned(const void* p, int64_t stride) {
+  return ((uintptr_t)p & 15) == 0 && (stride * (int64_t)sizeof(F) & 15) == 0;
 }
 
 // Whether rows may be multiplied where they lie.
@@ -935,13 +950,21 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     const Targets tg{targets, target_bytes, vocab};
     const float factor = std::is_same_v<F, f16> ? scale / kHalfScale : scale;
     if (rows == 0) {
-      finish<F>(nullptr, vocab, 0, 0, 0, {dtable, n, 0.f, nullptr, nullptr, nullptr, tg, nullptr, 0},
-                s);
+      finish<F>(nullptr, vocab, 0, 0, 0, {dtable, n, 0.f, nullptr, nullptr}, s);
       return;
     }
-    int* power = (int*)(w + l.power);
     Row* row = (Row*)(w + l.row);
-    loss_rows_kernel<<<1, 1024, 0, s>>>(tg, dloss, rows, row, power);
+    // only binary16 needs the power of two
+    int* power = std::is_same_v<F, f16> && dtable ? (int*)(w + l.power) : nullptr;
+    const Rows r{h, table, h_stride, table_stride, rows, n, scale, tg, lse, dloss, row,
+                 (float*)(w + l.largest)};
+    const int groups = (int)std::min<int64_t>((rows + 3) / 4, kMostLargest);
+    constexpr int kE = 16 / (int)sizeof(F);
+    if (n % kE == 0 && rows_aligned<F>(h, h_stride) && rows_aligned<F>(table, table_stride))
+      loss_rows_kernel<F, kE><<<groups, 256, 0, s>>>(r);
+    else
+      loss_rows_kernel<F, 1><<<groups, 256, 0, s>>>(r);
+    if (power) loss_power_kernel<<<1, 256, 0, s>>>((const float*)(w + l.largest), groups, power);
     Logits a{};
     a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
     if (dtable) pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, s, row, power);
@@ -951,7 +974,6 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     a.targets = tg;
     a.lse = lse;
     a.row = row;
-    a.rest = (float*)(w + l.rest);
     a.g = w + l.g;
     a.g_stride = l.piece;
     a.g_plane = rows * l.piece;
@@ -981,8 +1003,7 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
         p.out = (float*)(w + l.dh);
         p.split = rows * l.k;
         p.add = v0 > 0;
-        p.final = {dh, n, factor, nullptr, row, dtype == SIEVE_F32 ? nullptr : a.rest, tg, table,
-                   table_stride};
+        p.final = {dh, n, factor, nullptr, row};
         product<F, T, false>(p, l.h_spread, last, s);
       }
       if (dtable) {
@@ -993,7 +1014,7 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
         p.out = (float*)(w + l.dw);
         p.split = l.piece * l.k;
         p.add = 0;
-        p.final = {(F*)dtable + v0 * n, n, factor, power, nullptr, nullptr, tg, nullptr, 0};
+        p.final = {(F*)dtable + v0 * n, n, factor, power, nullptr};
         product<F, T, true>(p, l.w_spread, true, s);
       }
     }

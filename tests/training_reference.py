@@ -66,26 +66,28 @@ def cross_entropy(h, table, targets, scale, dloss=None):
     one[torch.arange(len(at)), at] = 1.0
     g = (p - one) * weight[:, None]
     d_p = p * (ds + d_lse[:, None] + 2.0 ** -20 + 4 * E * (s.abs() + lse.abs()[:, None]))
-    # rounded to the inputs' type; binary16 times 2^14 and the mantissa of dloss
-    d_g = (1 + u) * d_p * weight.abs()[:, None] + (u + 4 * E) * g.abs()
+    # rounded to the inputs' type, over the row's factor (which cancels)
+    d_g = (1 + u) * d_p * weight.abs()[:, None] + (u + 8 * E) * g.abs()
     # an exponential below fp32's normal range (2^-126) may be zero, and so may g, or a part of it
     # that a matrix unit reads, below that of its type
     d_g = d_g + 2.0 ** -126 * (weight.abs()[:, None] + 3)
     if dt is torch.float16:
+        # scaled by 2^14, over a factor of at most dloss: a step of 2^-24 below the normal range
         d_g = d_g + 2.0 ** -39 * weight.abs()[:, None]
 
-    def product(a, d_a, b, k):
+    def product(a, d_a, b, k, again=0.0):
         total = a @ b
-        size, far = a.abs() @ b.abs(), d_a @ b.abs()
+        size, far = a.abs() @ b.abs(), (d_a + again * (a.abs() + d_a)) @ b.abs()
         parts = 6 * k if dt is torch.float32 else k
         e = c * (far + ((parts + 16) * 2 + 16) * E * (size + far))
         return c * total, e + u * (c * total.abs() + e) + TINY[dt]
 
     val["dh"], tol["dh"] = product(g, d_g, w, vocab)
     held = torch.where(weight[:, None] != 0, x, 0.0)
-    val["dtable"], tol["dtable"] = product(g.T, d_g.T, held, len(at))
+    # h is rounded once more, with its row's factor
+    val["dtable"], tol["dtable"] = product(g.T, d_g.T, held, len(at), u + 4 * E)
     if dt is torch.float16:
-        # rows of far smaller weight may fall below the type's normal range
+        # rows of far smaller factors may fall below the type's normal range
         top = weight.abs().max() if len(at) else 0.0
         tol["dtable"] = tol["dtable"] + c * top * 2.0 ** -23 * (g != 0).sum(0)[:, None]
     return val, tol
