@@ -39,7 +39,8 @@ namespace {
 typedef mm_bf16 bf16;
 typedef mm_f16 f16;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr double kLog2e = 1.4426950408889634;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kStep = 64;                 // values of k a step
 constexpr int kHigh = 8;                  // tiles of m before the next of n, see mm_tile_at
 constexpr int64_t kMaxRows = 1 << 24;     // of h, and of the table
@@ -88,14 +89,16 @@ __device__ __forceinline__ uint32_t lds_of(const void* p) {
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// Two rows' parts of a sum of exponentials: (maximum, sum), in base 2.
+// A part of a row's sum: the largest dot product of it, and the sum of
+// exp(scale (dot product - largest)).  Differences of dot products are taken before they are
+// scaled: a loss near 0 keeps its bits, however large the logits are.
 struct Part {
   float top, sum;
 };
-__device__ __forceinline__ Part join(Part a, Part b) {
+__device__ __forceinline__ Part join(Part a, Part b, float c2) {
   const float top = fmaxf(a.top, b.top);
   const float at = top == -INFINITY ? 0.f : top;
-  return {top, a.sum * exp2_of(a.top - at) + b.sum * exp2_of(b.top - at)};
+  return {top, a.sum * exp2_of((a.top - at) * c2) + b.sum * exp2_of((b.top - at) * c2)};
 }
 
 // What a row's g is divided by, inverse (0 where the row gives no gradient), and its factor.
@@ -110,11 +113,12 @@ struct Logits {
   int64_t k;             // n, up to the next multiple of 8
   int pairs;
   uint32_t tiles_m, tiles_n;
-  float c2;              // scale log2(e)
+  float c2, c2_rest;     // scale log2(e), and what rounding took from it
+  float scale;
   Targets targets;
   // forward
   Part* part;            // [tile of vectors][rows]
-  float* target_logit;   // [rows], in base 2
+  float* target_dot;     // [rows]
   // backward
   const float* lse;
   const Row* row;        // [rows]
@@ -207,24 +211,26 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_forward_kernel(Logits a) 
         for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][r]);
       }
       top = fmaxf(top, other_half(top));
-      const float top2 = top * a.c2, at = top == -INFINITY ? 0.f : top2;
+      const float at = top == -INFINITY ? 0.f : top * a.c2;
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum += exp2_of(fmaf(acc[i][r], a.c2, -at));
       sum += other_half(sum);
+      // the sum is of 2^(c2 x - at), with at rounded: by as much it is of 2^(c2 (x - top))
+      if (top != -INFINITY) sum *= exp2_of(-fmaf(top, a.c2, -at));
       each_target(acc, rel[j], [&](float x) {
-        a.target_logit[w.n0 + t.col0 + 32 * j] = x * a.c2;
+        a.target_dot[w.n0 + t.col0 + 32 * j] = x;
         return x;
       });
-      if ((threadIdx.x & 32) == 0) s_part[wave_m * S::BN + t.col0 + 32 * j] = Part{top2, sum};
+      if ((threadIdx.x & 32) == 0) s_part[wave_m * S::BN + t.col0 + 32 * j] = Part{top, sum};
     }
     mm_barrier();
     if (threadIdx.x < S::BN && w.n0 + threadIdx.x < a.h.rows) {
       Part p = s_part[threadIdx.x];
 #pragma unroll
-      for (int i = 1; i < S::WM; ++i) p = join(p, s_part[i * S::BN + threadIdx.x]);
+      for (int i = 1; i < S::WM; ++i) p = join(p, s_part[i * S::BN + threadIdx.x], a.c2);
       a.part[(int64_t)tm * a.h.rows + w.n0 + threadIdx.x] = p;
     }
     // the next tile's first step has a barrier between these reads and the next parts
@@ -233,27 +239,33 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_forward_kernel(Logits a) 
 }
 
 // Joins the tiles' parts: a work-group takes 32 rows, its 8 groups of 32 threads every 8th tile.
-__global__ __launch_bounds__(256) void loss_join_kernel(const Part* part, const float* target_logit,
-                                                        Targets targets, int64_t t_first,
-                                                        int64_t rows, int64_t tiles, float* loss,
-                                                        float* lse) {
+struct Join {
+  const Part* part;
+  const float* target_dot;
+  Targets targets;
+  int64_t t_first, rows, tiles;
+  float c2, scale;
+  float *loss, *lse;
+};
+__global__ __launch_bounds__(256) void loss_join_kernel(Join a) {
   __shared__ Part s[8][32];
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
   const int64_t row = (int64_t)blockIdx.x * 32 + c;
   Part p{-INFINITY, 0.f};
-  if (row < rows) {
+  if (row < a.rows) {
 #pragma unroll 4
-    for (int64_t i = g; i < tiles; i += 8) p = join(p, part[i * rows + row]);
+    for (int64_t i = g; i < a.tiles; i += 8) p = join(p, a.part[i * a.rows + row], a.c2);
   }
   s[g][c] = p;
   __syncthreads();
-  if (g != 0 || row >= rows) return;
-  for (int i = 1; i < 8; ++i) p = join(p, s[i][c]);
+  if (g != 0 || row >= a.rows) return;
+  for (int i = 1; i < 8; ++i) p = join(p, s[i][c], a.c2);
   const float more = log2f(p.sum);
-  lse[t_first + row] = (p.top + more) * kLn2;
-  if (loss)
-    loss[t_first + row] =
-        targets.at(t_first + row) < 0 ? 0.f : (more + (p.top - target_logit[row])) * kLn2;
+  a.lse[a.t_first + row] = (float)((double)p.top * a.scale + (double)more * 0.6931471805599453);
+  if (a.loss)
+    a.loss[a.t_first + row] = a.targets.at(a.t_first + row) < 0
+                                  ? 0.f
+                                  : fmaf(more, kLn2, (p.top - a.target_dot[row]) * a.scale);
 }
 
 // The rows' factors, a wave a row, and the largest of them of each work-group.
@@ -338,7 +350,7 @@ __device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
 }
 
 // Rows of n values as the products take them: zeros up to the next multiple of 8, 32-bit values
-// as planes; with `row` each row times its factor (over the power of two), or zeros where it has
+// as three planes, or 16-bit ones and what rounding took from them as two; with `row` each row times its factor (over the power of two), or zeros where it has
 // none.
 struct Pack {
   const void* x;
@@ -346,6 +358,7 @@ struct Pack {
   int n, k;
   void* to;
   int64_t plane;
+  int planes;
   const Row* row;
   const int* power;
 };
@@ -365,7 +378,8 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
       factor = w.inverse == 0.f ? 0.f : a.power ? ldexpf(w.factor, -*a.power) : w.factor;
     }
     const T* x = (const T*)a.x + row * a.stride + col;
-    EncVec<U, 8> out[3];
+    constexpr int kPlanes = std::is_same_v<T, float> ? 3 : 2;
+    EncVec<U, 8> out[kPlanes];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float v = col + j < a.n && factor != 0.f ? (float)x[j] * factor : 0.f;
@@ -376,11 +390,12 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(Pack a) {
         for (int q = 0; q < 3; ++q) out[q].v[j] = p[q];
       } else {
         out[0].v[j] = (U)v;
+        out[1].v[j] = (U)(v - (float)out[0].v[j]);
       }
     }
 #pragma unroll
-    for (int q = 0; q < (std::is_same_v<T, float> ? 3 : 1); ++q)
-      enc_store<U, 8>((U*)a.to + q * a.plane + row * a.k + col, out[q]);
+    for (int q = 0; q < kPlanes; ++q)
+      if (q < a.planes) enc_store<U, 8>((U*)a.to + q * a.plane + row * a.k + col, out[q]);
   }
 }
 
@@ -403,18 +418,24 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
     const int64_t first = w.m0 + wave_m * kWave;
     const int left = (int)(a.w.rows - first < kWave ? a.w.rows - first : kWave);
     int rel[Tile::kJ];
-    float inverse[Tile::kJ], lse2[Tile::kJ];
+    float inverse[Tile::kJ], lse2[Tile::kJ], rest[Tile::kJ];
 #pragma unroll
     for (int j = 0; j < Tile::kJ; ++j) {
       const int64_t row = w.n0 + t.col0 + 32 * j;
       rel[j] = -1;
-      inverse[j] = lse2[j] = 0.f;
+      inverse[j] = lse2[j] = rest[j] = 0.f;
       if (row < a.h.rows) {
         const int64_t v = a.targets.at(row), at = v - a.v_first - first;
         if (v >= 0 && at >= 0 && at < kWave) rel[j] = (int)at;
         inverse[j] = a.row[row].inverse;
         if constexpr (std::is_same_v<F, f16>) inverse[j] *= kHalfScale;
-        lse2[j] = a.lse[row] * kLog2e;
+        // lse in base 2 and the rounding of it and of c2, both by as much as it matters: for
+        // logits near lse
+        const float lse = a.lse[row];
+        const double exact = (double)lse * kLog2e;
+        lse2[j] = (float)exact;
+        rest[j] = exp2_of(lse / a.scale * a.c2_rest - (float)(exact - (double)lse2[j]));
+        if (inverse[j] != 0.f) inverse[j] *= rest[j];
       }
     }
     t.sum(t.steps_of(w), ahead);
@@ -428,7 +449,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
       for (int i = 0; i < Tile::kI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[i][r] = exp2_of(fmaf(t.acc[i][j][r], a.c2, -lse2[j]));
-      each_target(p, rel[j], [](float x) { return x - 1.f; });
+      each_target(p, rel[j], [&](float x) { return x - 1.f / rest[j]; });
 #pragma unroll
       for (int i = 0; i < Tile::kI; ++i) {
         f32x16 x = p[i];
@@ -656,6 +677,7 @@ struct Layout {
   int64_t piece;                 // vectors of a piece, a multiple of 256
   int64_t k;                     // n, up to the next multiple of 8
   int planes, pairs;
+  int weighed_planes, weighed_pairs;  // of dw's product
   Spread h_spread, w_spread;
   int64_t h, w, part, target, g, weighed, row, largest, dh, dw, power, bytes;
 };
@@ -683,9 +705,14 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
   } else {
     const int64_t vs = std::min(l.piece, vocab);
     l.h_spread = spread_of(rows, n, vs * l.pairs, 16);
-    l.w_spread = spread_of(vs, n, rows * l.pairs, 16);
+    // h times its row's factor is rounded a second time: where dw's product takes a few us at the
+    // most (2^31 products: 4 us), what that loses is a plane of its own
+    const bool few = dtype != SIEVE_F32 && rows * vocab <= (int64_t(1) << 31) / n;
+    l.weighed_planes = few ? 2 : l.planes;
+    l.weighed_pairs = few ? 2 : l.pairs;
+    l.w_spread = spread_of(vs, n, rows * l.weighed_pairs, 16);
     l.g = take(rows * l.piece * 2 * l.planes);
-    l.weighed = take(rows * l.k * 2 * l.planes);
+    l.weighed = take(rows * l.k * 2 * l.weighed_planes);
     l.row = take(rows * (int64_t)sizeof(Row));
     l.largest = take(kMostLargest * 4);
     l.dh = take(l.h_spread.splits * rows * l.k * 4);
@@ -730,9 +757,9 @@ int blocks_of(int64_t work) { return (int)std::min<int64_t>((work + 255) / 256, 
 
 template <typename T>
 void pack(const void* x, int64_t stride, int64_t rows, int32_t n, int64_t k, void* to,
-          int64_t plane, hipStream_t s, const Row* row = nullptr,
+          int64_t plane, int planes, hipStream_t s, const Row* row = nullptr,
           const int* power = nullptr) {
-  const Pack a{x, stride, rows, n, (int)k, to, plane, row, power};
+  const Pack a{x, stride, rows, n, (int)k, to, plane, planes, row, power};
   loss_pack_kernel<T><<<blocks_of(rows * (k / 8)), 256, 0, s>>>(a);
 }
 
@@ -752,7 +779,7 @@ template <typename T>
 MmOperand operand(const void* x, int64_t stride, int64_t rows, int32_t n, int32_t dtype, int64_t k,
                   void* to, hipStream_t s) {
   if (direct(x, stride, n, dtype)) return {x, stride, rows, 0};
-  pack<T>(x, stride, rows, n, k, to, rows * k, s);
+  pack<T>(x, stride, rows, n, k, to, rows * k, dtype == SIEVE_F32 ? 3 : 1, s);
   return {to, k, rows, rows * k};
 }
 
@@ -798,6 +825,13 @@ int allow_lds() {
   });
   ENC_HIP_TRY(e);
   return SIEVE_OK;
+}
+
+void set_scale(Logits& a, float scale) {
+  const double c2 = (double)scale * kLog2e;
+  a.scale = scale;
+  a.c2 = (float)c2;
+  a.c2_rest = (float)(c2 - (double)a.c2);
 }
 
 // f(inputs' type, planes' type)
@@ -886,9 +920,9 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
     a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
     a.k = l.k;
     a.pairs = l.pairs;
-    a.c2 = scale * kLog2e;
+    set_scale(a, scale);
     a.targets = {targets, target_bytes, vocab};
-    a.target_logit = (float*)(w + l.target);
+    a.target_dot = (float*)(w + l.target);
     const MmOperand all_h = a.h;
     // a table that has to be packed is taken in pieces; any is, where a launch would be too large
     const bool as_is = direct(table, table_stride, n, dtype);
@@ -915,8 +949,8 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
         });
       }
       loss_join_kernel<<<tiles_of(a.h.rows, 32), 256, 0, s>>>(
-          (const Part*)(w + l.part), a.target_logit, a.targets, t0, a.h.rows,
-          tiles_of(vocab, side), loss, lse);
+          {(const Part*)(w + l.part), a.target_dot, a.targets, t0, a.h.rows, tiles_of(vocab, side),
+           a.c2, scale, loss, lse});
     }
   });
   ENC_HIP_TRY(hipGetLastError());
@@ -967,10 +1001,12 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     if (power) loss_power_kernel<<<1, 256, 0, s>>>((const float*)(w + l.largest), groups, power);
     Logits a{};
     a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
-    if (dtable) pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, s, row, power);
+    if (dtable)
+      pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, l.weighed_planes, s, row,
+              power);
     a.k = l.k;
     a.pairs = l.pairs;
-    a.c2 = scale * kLog2e;
+    set_scale(a, scale);
     a.targets = tg;
     a.lse = lse;
     a.row = row;
@@ -1009,6 +1045,7 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
       if (dtable) {
         p.a = {a.g, l.piece, l.piece, a.g_plane};
         p.b = {w + l.weighed, l.k, n, rows * l.k};
+        p.pairs = l.weighed_pairs;
         p.k = rows;
         p.rows = vs;
         p.out = (float*)(w + l.dw);
