@@ -10,7 +10,8 @@
 //
 // The sort is a stable radix sort of (number, token) pairs, so equal tokens stay in the order of
 // the batch: a tile's digits are counted, the counts summed over the tiles, and each pair is
-// written to its place.  Sums are in a fixed order, without atomics: equal calls give equal bits.
+// written to its place.  Digits are of up to 11 bits: one pass for vocabularies below 2^11, two
+// below 2^22.  Sums are in a fixed order, without atomics: equal calls give equal bits.
 //
 // A frequent token would leave one row with most of the work, so runs of equal numbers are
 // summed ahead in pieces: a piece of 32 sorted places that holds one number alone is summed by
@@ -42,32 +43,46 @@ struct EmbedFwd {
   uint32_t mul, shift;   // index / pieces = (index * mul) >> shift
 };
 
-// E values of type T as floats, in one move where they fill 16 bytes or more.
-template <typename T, int E>
-__device__ __forceinline__ void load_values(const T* p, float (&v)[E]) {
-  if constexpr (E * sizeof(T) >= 16) {
+// E values of type T as floats, in one move.  kWhole: they lie at a multiple of 16 bytes (or of
+// E values' size); else anywhere, and only `left` of them are there.
+template <typename T, int E, bool kWhole>
+__device__ __forceinline__ void load_values(const T* p, int left, float (&v)[E]) {
+  if constexpr (kWhole) {
     const EncVec<T, E> q = enc_load<T, E>(p);
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = (float)q.v[j];
+  } else if (left >= E) {
+    T q[E];
+    __builtin_memcpy(q, p, sizeof(q));
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = (float)q[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < E; ++j) v[j] = (float)p[j];
+    for (int j = 0; j < E; ++j) v[j] = j < left ? (float)p[j] : 0.f;
   }
 }
-template <typename T, int E>
-__device__ __forceinline__ void store_values(T* p, const float (&v)[E]) {
-  if constexpr (E * sizeof(T) >= 16) {
+template <typename T, int E, bool kWhole>
+__device__ __forceinline__ void store_values(T* p, int left, const float (&v)[E]) {
+  if constexpr (kWhole) {
     EncVec<T, E> q;
 #pragma unroll
     for (int j = 0; j < E; ++j) q.v[j] = (T)v[j];
     enc_store<T, E>(p, q);
+  } else if (left >= E) {
+    T q[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) q[j] = (T)v[j];
+    __builtin_memcpy(p, q, sizeof(q));
   } else {
 #pragma unroll
-    for (int j = 0; j < E; ++j) p[j] = (T)v[j];
+    for (int j = 0; j < E; ++j)
+      if (j < left) p[j] = (T)v[j];
   }
 }
 
-template <typename W, typename T, typename I, int E>
+constexpr int kMoves = 4;
+
+template <typename W, typename T, typename I, int E, bool kWhole>
 __global__ __launch_bounds__(kThreads) void embed_forward_kernel(EmbedFwd a) {
   for (int64_t first = (int64_t)blockIdx.x * a.rows; first < a.count;
        first += (int64_t)gridDim.x * a.rows) {
@@ -75,37 +90,59 @@ __global__ __launch_bounds__(kThreads) void embed_forward_kernel(EmbedFwd a) {
     const int rows = left < a.rows ? (int)left : a.rows;
     const I* ids = (const I*)a.ids + first;
     T* out = (T*)a.out + first * a.n;
-    for (int i = threadIdx.x; i < rows * a.pieces; i += kThreads) {
-      const int row = (int)(((uint64_t)(uint32_t)i * a.mul) >> a.shift);
-      const int col = (i - row * a.pieces) * E;
-      const int64_t id = (int64_t)ids[row];
-      float v[E];
-      if (id >= 0 && id < a.vocab) {
-        load_values<W, E>((const W*)a.table + id * a.t_stride + col, v);
+    const int all = rows * a.pieces;
+    // kMoves of a thread at a time: their numbers, then their values are on the way together
+    for (int i0 = threadIdx.x; i0 < all; i0 += kMoves * kThreads) {
+      int64_t id[kMoves];
+      int row[kMoves];
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[j] *= a.scale;
-      } else {
-#pragma unroll
-        for (int j = 0; j < E; ++j) v[j] = 0.f;
+      for (int u = 0; u < kMoves; ++u) {
+        const int i = i0 + u * kThreads;
+        row[u] = (int)(((uint64_t)(uint32_t)i * a.mul) >> a.shift);
+        id[u] = i < all ? (int64_t)ids[row[u]] : -1;
       }
-      store_values<T, E>(out + (int64_t)row * a.n + col, v);
+      float v[kMoves][E];
+#pragma unroll
+      for (int u = 0; u < kMoves; ++u) {
+        const int col = (i0 + u * kThreads - row[u] * a.pieces) * E;
+        if (id[u] >= 0 && id[u] < a.vocab) {
+          load_values<W, E, kWhole>((const W*)a.table + id[u] * a.t_stride + col, a.n - col, v[u]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < E; ++j) v[u][j] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kMoves; ++u) {
+        const int i = i0 + u * kThreads, col = (i - row[u] * a.pieces) * E;
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[u][j] *= a.scale;
+        if (i < all) store_values<T, E, kWhole>(out + (int64_t)row[u] * a.n + col, a.n - col, v[u]);
+      }
     }
   }
 }
 
 // ---- sorting ---------------------------------------------------------------------------------
 
-constexpr int kMaxDigit = 10;                 // bits of a digit
+constexpr int kMaxDigit = 11;                 // bits of a digit
 constexpr int kBins = 1 << kMaxDigit;
 constexpr int kRounds = 8;                    // pairs of a thread
 constexpr int kTile = kThreads * kRounds;     // pairs of a work-group
 constexpr int kWaves = kThreads / 64;
+constexpr int kEach = kBins / kThreads;       // bins of a thread
+// Up to so many counts a thread every tile adds them up by itself; more go through a kernel of
+// their own, another launch.
+constexpr int kFewCounts = 64;
+inline __host__ __device__ bool few_counts(int tiles, int bins) {
+  return tiles * ((bins + kThreads - 1) / kThreads) <= kFewCounts;
+}
 
 struct Pass {
   const void* ids;                // the first pass reads these (I), later ones `from`
   const uint32_t *from_key, *from_at;
   uint32_t *to_key, *to_at;
-  uint32_t* counts;               // [bins][tiles], then their exclusive sums along the tiles
+  uint32_t* counts;               // [tiles][bins], then their exclusive sums along the tiles
   uint32_t* totals;               // [bins]
   int64_t count, vocab;
   int tiles, shift, bits;
@@ -136,41 +173,40 @@ __global__ __launch_bounds__(kThreads) void sort_count_kernel(Pass a) {
   }
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += kThreads)
-    a.counts[(int64_t)b * a.tiles + blockIdx.x] = s_count[b];
+    a.counts[(int64_t)blockIdx.x * bins + b] = s_count[b];
 }
 
-// A wave sums one digit's counts along the tiles.
+// A work-group sums 32 digits' counts along the tiles, in 8 runs of tiles.
 __global__ __launch_bounds__(kThreads) void sort_sum_kernel(Pass a) {
-  const int bin = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (bin >= 1 << a.bits) return;
-  uint32_t* c = a.counts + (int64_t)bin * a.tiles;
-  uint32_t before = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 64) {
-    const int t = t0 + lane;
-    const uint32_t own = t < a.tiles ? c[t] : 0;
-    uint32_t sum = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
-    }
-    if (t < a.tiles) c[t] = before + sum - own;
-    before += __shfl(sum, 63);
+  __shared__ uint32_t s_run[8][32];
+  const int c = threadIdx.x & 31, g = threadIdx.x >> 5, bins = 1 << a.bits;
+  const int bin = blockIdx.x * 32 + c, per = (a.tiles + 7) / 8;
+  const int first = g * per, last = first + per < a.tiles ? first + per : a.tiles;
+  uint32_t sum = 0;
+  if (bin < bins) {
+#pragma unroll 8
+    for (int t = first; t < last; ++t) sum += a.counts[(int64_t)t * bins + bin];
   }
-  if (lane == 0) a.totals[bin] = before;
+  s_run[g][c] = sum;
+  __syncthreads();
+  if (bin >= bins) return;
+  uint32_t before = 0;
+  for (int i = 0; i < g; ++i) before += s_run[i][c];
+#pragma unroll 8
+  for (int t = first; t < last; ++t) {
+    const uint32_t own = a.counts[(int64_t)t * bins + bin];
+    a.counts[(int64_t)t * bins + bin] = before;
+    before += own;
+  }
+  if (g == 7) a.totals[bin] = before;
 }
 
 // Exclusive sums of `bins` values in LDS, by the whole work-group.
 __device__ __forceinline__ void sum_bins(uint32_t* s, int bins, uint32_t* s_wave) {
-  constexpr int kEach = kBins / kThreads;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t v[kEach], sum = 0;
-#pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int b = threadIdx.x * kEach + j;
-    v[j] = b < bins ? s[b] : 0;
-    sum += v[j];
-  }
+  const int each = (bins + kThreads - 1) / kThreads, first = threadIdx.x * each;
+  uint32_t sum = 0;
+  for (int j = 0; j < each; ++j) sum += first + j < bins ? s[first + j] : 0;
   uint32_t all = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -181,12 +217,12 @@ __device__ __forceinline__ void sum_bins(uint32_t* s, int bins, uint32_t* s_wave
   __syncthreads();
   uint32_t before = all - sum;
   for (int w = 0; w < wave; ++w) before += s_wave[w];
-#pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int b = threadIdx.x * kEach + j;
-    if (b < bins) s[b] = before;
-    before += v[j];
-  }
+  for (int j = 0; j < each; ++j)
+    if (first + j < bins) {
+      const uint32_t own = s[first + j];
+      s[first + j] = before;
+      before += own;
+    }
   __syncthreads();
 }
 
@@ -201,23 +237,41 @@ __device__ __forceinline__ void wave_fence() {
 // order, 64 at a time: a pair's rank among the equal digits of its 64 comes from ballots.
 template <typename I, bool kFirst>
 __global__ __launch_bounds__(kThreads) void sort_place_kernel(Pass a) {
-  __shared__ uint32_t s_place[kBins], s_wave[kWaves];
+  __shared__ uint32_t s_wave[kWaves], s_total[kBins];
   __shared__ uint32_t s_count[kWaves][kBins];
   const int bins = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = threadIdx.x; b < bins; b += kThreads) {
-    s_place[b] = a.totals[b];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) s_count[w][b] = 0;
-  }
-  __syncthreads();
-  sum_bins(s_place, bins, s_wave);
   const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTile / kWaves);
-  uint32_t key[kRounds], rank[kRounds];
+  uint32_t key[kRounds], at[kRounds], rank[kRounds];
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     const int64_t i = first + r * 64 + lane;
     key[r] = i < a.count ? key_of<I, kFirst>(a, i) : 0;
+    at[r] = kFirst || i >= a.count ? (uint32_t)i : a.from_at[i];
   }
+  // all pairs of each bin, and those of the tiles before: bins threadIdx.x + 256 j
+  uint32_t before[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int b = threadIdx.x + j * kThreads;
+    before[j] = 0;
+    if (b >= bins) break;
+    uint32_t total = 0;
+    if (!few_counts(a.tiles, bins)) {
+      total = a.totals[b];
+      before[j] = a.counts[(int64_t)blockIdx.x * bins + b];
+    } else if (a.tiles > 1) {
+#pragma unroll 16
+      for (int t = 0; t < a.tiles; ++t) {
+        const uint32_t c = a.counts[(int64_t)t * bins + b];
+        total += c;
+        before[j] += t < (int)blockIdx.x ? c : 0;
+      }
+    }
+    s_total[b] = total;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s_count[w][b] = 0;
+  }
+  __syncthreads();
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     const bool ok = first + r * 64 + lane < a.count;
@@ -234,24 +288,36 @@ __global__ __launch_bounds__(kThreads) void sort_place_kernel(Pass a) {
     wave_fence();
   }
   __syncthreads();
+  if (a.tiles == 1) {  // no counts: they are this tile's
+    for (int b = threadIdx.x; b < bins; b += kThreads) {
+      uint32_t total = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) total += s_count[w][b];
+      s_total[b] = total;
+    }
+    __syncthreads();
+  }
+  sum_bins(s_total, bins, s_wave);
   // where the waves' pairs of each digit begin
-  for (int b = threadIdx.x; b < bins; b += kThreads) {
-    uint32_t at = s_place[b] + a.counts[(int64_t)b * a.tiles + blockIdx.x];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int b = threadIdx.x + j * kThreads;
+    if (b >= bins) break;
+    uint32_t to = s_total[b] + before[j];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const uint32_t c = s_count[w][b];
-      s_count[w][b] = at;
-      at += c;
+      s_count[w][b] = to;
+      to += c;
     }
   }
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = first + r * 64 + lane;
-    if (i >= a.count) continue;
+    if (first + r * 64 + lane >= a.count) continue;
     const uint32_t to = s_count[wave][(key[r] >> a.shift) & (bins - 1)] + rank[r];
     a.to_key[to] = key[r];
-    a.to_at[to] = kFirst ? (uint32_t)i : a.from_at[i];
+    a.to_at[to] = at[r];
   }
 }
 
@@ -276,7 +342,7 @@ struct EmbedBwd {
   int rows;                    // table rows of a work-group
 };
 
-template <typename T, int E>
+template <typename T, int E, bool kWhole>
 struct Sum {
   const EmbedBwd& a;
   int col;
@@ -285,24 +351,45 @@ struct Sum {
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = 0.f;
   }
-  // sorted places begin .. end - 1
-  __device__ __forceinline__ void places(int64_t begin, int64_t end) {
-#pragma unroll 8
-    for (int64_t p = begin; p < end; ++p) {
-      float x[E];
-      load_values<T, E>((const T*)a.dy + (int64_t)a.at[p] * a.dy_stride + col, x);
+  // Adds load(i) for i = 0 .. count - 1, in order, kAhead of them on their way at a time.
+  static constexpr int kAhead = 16 / E;
+  template <typename F>
+  __device__ __forceinline__ void all(int count, F load) {
+    for (int i = 0; i < count; i += kAhead) {
+      float x[kAhead][E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) v[j] += x[j];
+      for (int u = 0; u < kAhead; ++u) {
+        if (i + u < count) {
+          load(i + u, x[u]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < E; ++j) x[u][j] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] += x[u][j];
+    }
+  }
+  // Sorted places begin .. end - 1.  The row's threads (of a wave) load the tokens' numbers
+  // together and pass them round: one wait for all of them.
+  __device__ __forceinline__ void places(int64_t begin, int64_t end) {
+    const int many = a.group < 64 ? a.group : 64, lane = threadIdx.x & 63;
+    const int first = lane & ~(many - 1);
+    for (int64_t p = begin; p < end; p += many) {
+      const int count = end - p < many ? (int)(end - p) : many;
+      const uint32_t mine = a.at[p + (lane - first < count ? lane - first : count - 1)];
+      all(count, [&](int i, float (&x)[E]) {
+        const int64_t token = (int64_t)(uint32_t)__shfl((int)mine, first + i);
+        load_values<T, E, kWhole>((const T*)a.dy + token * a.dy_stride + col, a.n - col, x);
+      });
     }
   }
   __device__ __forceinline__ void pieces(int kind, int64_t begin, int64_t end) {
-#pragma unroll 8
-    for (int64_t p = begin; p < end; ++p) {
-      float x[E];
-      load_values<float, E>(a.part[kind] + p * a.pitch + col, x);
-#pragma unroll
-      for (int j = 0; j < E; ++j) v[j] += x[j];
-    }
+    all((int)(end - begin), [&](int i, float (&x)[E]) {
+      load_values<float, E, true>(a.part[kind] + (begin + i) * a.pitch + col, E, x);
+    });
   }
   // places of one number: what is left at both ends of the largest pieces inside, kind by kind
   __device__ __forceinline__ void interval(int64_t begin, int64_t end) {
@@ -325,7 +412,7 @@ struct Sum {
 };
 
 // Sums of the pieces of a kind that hold one number alone, by groups of threads.
-template <typename T, int E>
+template <typename T, int E, bool kWhole>
 __global__ __launch_bounds__(kThreads) void embed_pieces_kernel(EmbedBwd a, int kind,
                                                                 int64_t span) {
   const int lane = threadIdx.x % a.group;
@@ -334,16 +421,17 @@ __global__ __launch_bounds__(kThreads) void embed_pieces_kernel(EmbedBwd a, int 
        (j + 1) * span <= a.count; j += (int64_t)gridDim.x * groups) {
     const uint32_t key = a.key[j * span];
     if (key != a.key[(j + 1) * span - 1] || key == (uint32_t)a.vocab) continue;
-    for (int col = lane * E; col < a.n; col += a.group * E) {
-      Sum<T, E> s(a, col);
+    for (int c = 0; c < a.n; c += a.group * E) {
+      const int col = c + lane * E;
+      Sum<T, E, kWhole> s(a, col < a.n ? col : 0);  // a row's threads stay together
       if (kind == 1) s.places(j * kRun, (j + 1) * kRun);
       else s.pieces(kind - 1, j * kRun, (j + 1) * kRun);
-      store_values<float, E>(a.part[kind] + j * a.pitch + col, s.v);
+      if (col < a.n) store_values<float, E, true>(a.part[kind] + j * a.pitch + col, E, s.v);
     }
   }
 }
 
-template <typename T, typename W, int E>
+template <typename T, typename W, int E, bool kWhole>
 __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedBwd a) {
   __shared__ int64_t s_begin[kMaxRows + 1];
   const int lane = threadIdx.x % a.group;
@@ -366,18 +454,20 @@ __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedBwd a) {
       const int64_t begin = s_begin[r], end = s_begin[r + 1];
       if (a.accumulate && begin == end) continue;
       W* row = (W*)a.dtable + (v0 + r) * a.n;
-      for (int col = lane * E; col < a.n; col += a.group * E) {
-        Sum<T, E> s(a, col);
+      for (int c = 0; c < a.n; c += a.group * E) {
+        const int col = c + lane * E;
+        Sum<T, E, kWhole> s(a, col < a.n ? col : 0);  // a row's threads stay together
         s.interval(begin, end);
+        if (col >= a.n) continue;
 #pragma unroll
         for (int j = 0; j < E; ++j) s.v[j] *= a.scale;
         if (a.accumulate) {
           float old[E];
-          load_values<W, E>(row + col, old);
+          load_values<W, E, kWhole>(row + col, a.n - col, old);
 #pragma unroll
           for (int j = 0; j < E; ++j) s.v[j] += old[j];
         }
-        store_values<W, E>(row + col, s.v);
+        store_values<W, E, kWhole>(row + col, a.n - col, s.v);
       }
     }
   }
@@ -469,15 +559,17 @@ void sort(Pass a, const Layout& l, char* w, hipStream_t s) {
     a.from_at = (const uint32_t*)(w + l.at[(p + 1) & 1]);
     a.to_key = (uint32_t*)(w + l.key[p & 1]);
     a.to_at = (uint32_t*)(w + l.at[p & 1]);
-    if (p == 0) sort_count_kernel<I, true><<<l.tiles, kThreads, 0, s>>>(a);
-    else sort_count_kernel<I, false><<<l.tiles, kThreads, 0, s>>>(a);
-    sort_sum_kernel<<<(bins + kWaves - 1) / kWaves, kThreads, 0, s>>>(a);
+    if (l.tiles > 1) {
+      if (p == 0) sort_count_kernel<I, true><<<l.tiles, kThreads, 0, s>>>(a);
+      else sort_count_kernel<I, false><<<l.tiles, kThreads, 0, s>>>(a);
+    }
+    if (!few_counts(l.tiles, bins)) sort_sum_kernel<<<(bins + 31) / 32, kThreads, 0, s>>>(a);
     if (p == 0) sort_place_kernel<I, true><<<l.tiles, kThreads, 0, s>>>(a);
     else sort_place_kernel<I, false><<<l.tiles, kThreads, 0, s>>>(a);
   }
 }
 
-template <typename T, typename W, int E>
+template <typename T, typename W, int E, bool kWhole>
 void backward_typed(EmbedBwd a, hipStream_t s) {
   const int pieces = (a.n + E - 1) / E;
   a.group = 8;
@@ -486,12 +578,12 @@ void backward_typed(EmbedBwd a, hipStream_t s) {
   int64_t span = 1;
   for (int kind = 1; kind <= a.kinds; ++kind) {
     span *= kRun;
-    embed_pieces_kernel<T, E><<<grid_of((a.count / span + groups - 1) / groups), kThreads, 0, s>>>(
+    embed_pieces_kernel<T, E, kWhole><<<grid_of((a.count / span + groups - 1) / groups), kThreads, 0, s>>>(
         a, kind, span);
   }
   const int64_t want = a.vocab / 2048;
   a.rows = want < 1 ? 1 : want < kMaxRows ? (int)want : kMaxRows;  // few in a small table
-  embed_rows_kernel<T, W, E><<<grid_of((a.vocab + a.rows - 1) / a.rows), kThreads, 0, s>>>(a);
+  embed_rows_kernel<T, W, E, kWhole><<<grid_of((a.vocab + a.rows - 1) / a.rows), kThreads, 0, s>>>(a);
 }
 
 }  // namespace
@@ -509,12 +601,12 @@ SIEVE_API int sieve_embed_forward(const void* ids, int32_t id_bytes, int64_t cou
     typedef decltype(t) T;
     typedef decltype(w) W;
     constexpr int kE = 16 / (int)sizeof(T);
-    const bool vec = n % kE == 0 && vec_ok(table, table_stride, sizeof(W)) &&
-                     vec_ok(out, n, sizeof(T));
+    const bool whole = n % kE == 0 && vec_ok(table, table_stride, sizeof(W)) &&
+                       vec_ok(out, n, sizeof(T));
     EmbedFwd a{ids, table, count, table_stride, vocab, n, scale, out, 0, 0, 0, 0};
-    a.pieces = vec ? n / kE : n;
-    // about 8 moves a thread, so that a work-group's loads overlap; few rows where there are few
-    a.rows = 8 * kThreads / a.pieces;
+    a.pieces = (n + kE - 1) / kE;
+    // kMoves a thread; few rows where there are few
+    a.rows = 4 * kThreads / a.pieces;
     while (a.rows > 1 && count / a.rows < 512) a.rows /= 2;
     if (a.rows < 1) a.rows = 1;
     // indexes stay below 2^17: exact with a multiplier of 2^36 / pieces rounded up
@@ -527,11 +619,11 @@ SIEVE_API int sieve_embed_forward(const void* ids, int32_t id_bytes, int64_t cou
     const int grid = grid_of((count + a.rows - 1) / a.rows);
     hipStream_t s = (hipStream_t)stream;
     if (id_bytes == 8) {
-      if (vec) embed_forward_kernel<W, T, int64_t, kE><<<grid, kThreads, 0, s>>>(a);
-      else embed_forward_kernel<W, T, int64_t, 1><<<grid, kThreads, 0, s>>>(a);
+      if (whole) embed_forward_kernel<W, T, int64_t, kE, true><<<grid, kThreads, 0, s>>>(a);
+      else embed_forward_kernel<W, T, int64_t, kE, false><<<grid, kThreads, 0, s>>>(a);
     } else {
-      if (vec) embed_forward_kernel<W, T, int32_t, kE><<<grid, kThreads, 0, s>>>(a);
-      else embed_forward_kernel<W, T, int32_t, 1><<<grid, kThreads, 0, s>>>(a);
+      if (whole) embed_forward_kernel<W, T, int32_t, kE, true><<<grid, kThreads, 0, s>>>(a);
+      else embed_forward_kernel<W, T, int32_t, kE, false><<<grid, kThreads, 0, s>>>(a);
     }
   });
   ENC_HIP_TRY(hipGetLastError());
@@ -591,10 +683,10 @@ SIEVE_API int sieve_embed_backward(const void* dy, int64_t dy_stride, int32_t dt
     typedef decltype(t) T;
     typedef decltype(wt) W;
     constexpr int kE = 16 / (int)sizeof(T);
-    const bool vec = n % kE == 0 && (count == 0 || vec_ok(dy, dy_stride, sizeof(T))) &&
-                     vec_ok(dtable, n, sizeof(W));
-    if (vec) backward_typed<T, W, kE>(a, s);
-    else backward_typed<T, W, 1>(a, s);
+    const bool whole = n % kE == 0 && (count == 0 || vec_ok(dy, dy_stride, sizeof(T))) &&
+                       vec_ok(dtable, n, sizeof(W));
+    if (whole) backward_typed<T, W, kE, true>(a, s);
+    else backward_typed<T, W, kE, false>(a, s);
   });
   ENC_HIP_TRY(hipGetLastError());
   return SIEVE_OK;
