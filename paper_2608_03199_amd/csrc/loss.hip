@@ -50,18 +50,31 @@ constexpr int64_t kMaxPiece = 65536;       // vectors
 constexpr int64_t kRowChunk = 65536;       // rows of h in one launch of the forward pass
 constexpr float kHalfScale = 16384.f;      // what g in binary16 is scaled by
 
-// A work-group's tile: one large one has a CU to itself, small ones share it.
-template <int BM_, int BN_, int WM_, int WN_>
+// A work-group's tile.  Large and wide ones have a CU to themselves and eight waves; two small ones
+// share it; deep ones are as small, with eight waves and more loads on their way, for launches of
+// no more than a tile a CU.  2,048 x 2,048 x 8,192 bf16, 256 tiles: deep 87 us, small 105;
+// 8,192 x 768 x 8,192: wide 119 us (192 tiles), small 128, large 180; 8,192^3: large 891 us
+// (1,234 TFLOP/s), small 1,027.
+template <int BM_, int BN_, int WM_, int WN_, int kStages>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM_ * WN_;
   template <typename T, bool kAcrossA, bool kAcrossB>
-  using Tile = MmTile<T, BM, BN, kAcrossA, kAcrossB, WM, WN, kStep, 2>;
+  using Tile = MmTile<T, BM, BN, kAcrossA, kAcrossB, WM, WN, kStep, kStages>;
   static constexpr int kTileLds = Tile<mm_bf16, false, false>::kLds;
   static constexpr int kLds = kTileLds + WM * BN * 8;  // and the forward pass's parts
-  static constexpr uint32_t kMost = BM == 256 ? 256 : 512;  // work-groups on the chip
+  static constexpr uint32_t kMost = kLds > 81920 ? 256 : 512;  // work-groups on the chip
 };
-typedef Shape<256, 256, 2, 4> Large;
-typedef Shape<128, 128, 2, 2> Small;
+typedef Shape<256, 256, 2, 4, 2> Large;
+typedef Shape<256, 128, 4, 2, 3> Wide;
+typedef Shape<128, 128, 2, 2, 2> Small;
+typedef Shape<128, 128, 2, 4, 4> Deep;
+enum Size { kSmall, kDeep, kWide, kLarge };
+struct Measured {
+  int bm, bn, places;
+  double each;           // us a value of k and tile, where the chip is full
+};
+constexpr Measured kMeasured[] = {
+    {128, 128, 512, 0.016}, {128, 128, 256, 0.0107}, {256, 128, 256, 0.0145}, {256, 256, 256, 0.029}};
 constexpr int kSmallest = 128;            // the lesser of the shapes' BM
 
 struct Targets {
@@ -238,7 +251,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_forward_kernel(Logits a) 
   t.stop();
 }
 
-// Joins the tiles' parts: a work-group takes 32 rows, its 8 groups of 32 threads every 8th tile.
+// Joins the tiles' parts: a work-group takes kRows rows, its 256 / kRows groups of threads every
+// so many-th tile of them.
 struct Join {
   const Part* part;
   const float* target_dot;
@@ -247,25 +261,124 @@ struct Join {
   float c2, scale;
   float *loss, *lse;
 };
+template <int kRows>
 __global__ __launch_bounds__(256) void loss_join_kernel(Join a) {
-  __shared__ Part s[8][32];
-  const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
-  const int64_t row = (int64_t)blockIdx.x * 32 + c;
+  constexpr int kGroups = 256 / kRows;
+  __shared__ Part s[kGroups][kRows];
+  const int c = threadIdx.x % kRows, g = threadIdx.x / kRows;
+  const int64_t row = (int64_t)blockIdx.x * kRows + c;
   Part p{-INFINITY, 0.f};
   if (row < a.rows) {
 #pragma unroll 4
-    for (int64_t i = g; i < a.tiles; i += 8) p = join(p, a.part[i * a.rows + row], a.c2);
+    for (int64_t i = g; i < a.tiles; i += kGroups) p = join(p, a.part[i * a.rows + row], a.c2);
   }
   s[g][c] = p;
   __syncthreads();
+#pragma unroll
+  for (int half = kGroups / 2; half; half /= 2) {
+    if (g < half) s[g][c] = p = join(p, s[g + half][c], a.c2);
+    __syncthreads();
+  }
   if (g != 0 || row >= a.rows) return;
-  for (int i = 1; i < 8; ++i) p = join(p, s[i][c], a.c2);
   const float more = log2f(p.sum);
   a.lse[a.t_first + row] = (float)((double)p.top * a.scale + (double)more * 0.6931471805599453);
   if (a.loss)
     a.loss[a.t_first + row] = a.targets.at(a.t_first + row) < 0
                                   ? 0.f
                                   : fmaf(more, kLn2, (p.top - a.target_dot[row]) * a.scale);
+}
+
+// ---- few rows ----------------------------------------------------------------------------------
+//
+// The likelihood of up to 16 rows, say of one token: the table is read once and memory bounds it.
+// A wave takes 16 vectors at a time straight from memory into the matrix unit's operands, 16 bytes
+// a lane, against the rows (from the cache), and keeps each lane's own largest value and sum.
+
+struct Thin {
+  const void *h, *table;
+  int64_t h_stride, t_stride, vocab;
+  int rows, n;
+  float c2;
+  Targets targets;
+  Part* part;            // [work-group][rows]
+  float* target_dot;
+};
+constexpr int kThinRows = 16, kThinMost = 1024;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t thin_rsrc(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(mm_uniform((char*)const_cast<void*>(p)), 0,
+                                           (int)kMmNowhere, 0x00027000);
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 thin_mfma(enc_u32x4 a, enc_u32x4 b, f32x4 c, f16) {
+  typedef f16 v8 __attribute__((ext_vector_type(8)));
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a),
+                                                __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 thin_mfma(enc_u32x4 a, enc_u32x4 b, f32x4 c, bf16) {
+  typedef bf16 v8 __attribute__((ext_vector_type(8)));
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a),
+                                                 __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+// 16 values of k: step j multiplies element j of every quarter's operands
+__device__ __forceinline__ f32x4 thin_mfma(enc_u32x4 a, enc_u32x4 b, f32x4 c, float) {
+  const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+  return c;
+}
+
+template <typename F>
+__global__ __launch_bounds__(256) void loss_thin_kernel(Thin a) {
+  __shared__ Part s_part[4][kThinRows];
+  constexpr int kE = 16 / (int)sizeof(F), kStepK = 4 * kE, kAhead = 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = lane & 15, quarter = lane >> 4;
+  const __amdgpu_buffer_rsrc_t hr = thin_rsrc(a.h);
+  const uint32_t h_off = row < a.rows ? (uint32_t)(row * (uint32_t)a.h_stride) * sizeof(F) : kMmNowhere;
+  const int64_t target = row < a.rows ? a.targets.at(row) : -1;
+  Part p{-INFINITY, 0.f};
+  for (int64_t v0 = ((int64_t)blockIdx.x * 4 + wave) * 16; v0 < a.vocab;
+       v0 += (int64_t)gridDim.x * 64) {
+    const __amdgpu_buffer_rsrc_t wr = thin_rsrc((const F*)a.table + v0 * a.t_stride);
+    const uint32_t w_off =
+        v0 + row < a.vocab ? (uint32_t)(row * (uint32_t)a.t_stride) * sizeof(F) : kMmNowhere;
+    f32x4 c = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < a.n; k0 += kAhead * kStepK) {
+      enc_u32x4 x[kAhead], y[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int k = k0 + u * kStepK + quarter * kE;
+        // past the end, or the last row: zeros (what is added to kMmNowhere leads nowhere, too)
+        const uint32_t wo = k < a.n ? w_off + k * (uint32_t)sizeof(F) : kMmNowhere;
+        const uint32_t ho = k < a.n ? h_off + k * (uint32_t)sizeof(F) : kMmNowhere;
+        x[u] = __builtin_bit_cast(enc_u32x4,
+                                  __builtin_amdgcn_raw_buffer_load_b128(wr, (int)wo, 0, 0));
+        y[u] = __builtin_bit_cast(enc_u32x4,
+                                  __builtin_amdgcn_raw_buffer_load_b128(hr, (int)ho, 0, 0));
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) c = thin_mfma(x[u], y[u], c, F{});
+    }
+    // the lane has vectors v0 + 4 quarter .. + 3 of its row
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int64_t v = v0 + 4 * quarter + t;
+      if (v < a.vocab) p = join(p, Part{c[t], 1.f}, a.c2);
+      if (v == target) a.target_dot[row] = c[t];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1)
+    p = join(p, Part{__shfl_xor(p.top, o), __shfl_xor(p.sum, o)}, a.c2);
+  if (quarter == 0) s_part[wave][row] = p;
+  __syncthreads();
+  if (threadIdx.x < a.rows) {
+    p = s_part[0][threadIdx.x];
+    for (int i = 1; i < 4; ++i) p = join(p, s_part[i][threadIdx.x], a.c2);
+    a.part[(int64_t)blockIdx.x * a.rows + threadIdx.x] = p;
+  }
 }
 
 // The rows' factors, a wave a row, and the largest of them of each work-group.
@@ -511,8 +624,8 @@ __device__ __forceinline__ float factor_of(const Final& a, int64_t row) {
   return w.inverse == 0.f ? 0.f : w.factor * a.factor;
 }
 
-// A gradient's product: sums in fp32, [split][rows of m][pitch], or added to what is there; or
-// the gradient itself.
+// A gradient's product: sums in fp32, [split][rows of m][pitch], or added to what is there; or,
+// with final.out, the gradient itself.
 struct Product {
   MmOperand a, b;
   int64_t k, per;        // values of k, and of a split
@@ -531,9 +644,9 @@ struct Splits {
   MmPlaces at;
   uint32_t tiles_m, tiles_n;
   int64_t k, per;
-  __device__ __forceinline__ explicit Splits(const Product& a)
-      : at(a.tiles_m * a.tiles_n * a.splits), tiles_m(a.tiles_m), tiles_n(a.tiles_n), k(a.k),
-        per(a.per) {}
+  __device__ __forceinline__ Splits(const Product& a, uint32_t before)
+      : at(a.tiles_m * a.tiles_n * a.splits, before), tiles_m(a.tiles_m), tiles_n(a.tiles_n),
+        k(a.k), per(a.per) {}
   __device__ __forceinline__ void get(MmWork& w, uint32_t& split) const {
     const uint32_t tiles = tiles_m * tiles_n;
     uint32_t tm, tn;
@@ -551,20 +664,20 @@ struct Splits {
   }
 };
 
-template <typename F, typename T, typename S, bool kAcrossA, bool kFinal>
-__global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product a) {
-  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+// A work-group's tiles of a product; `before`: the launch's tiles of another one.
+template <typename F, typename T, typename S, bool kAcrossA>
+__device__ __forceinline__ void run_product(const Product& a, uint32_t before, uint32_t lds) {
   typedef typename S::template Tile<T, kAcrossA, true> Tile;
-  Splits<S> ahead(a), tiles = ahead;
+  Splits<S> ahead(a, before), tiles = ahead;
   if (!tiles.at.there()) return;
-  Tile t(a.a, a.b, a.pairs, lds_of(lds_memory));
+  Tile t(a.a, a.b, a.pairs, lds);
   t.start(ahead);
   for (; tiles.at.there(); tiles.at.next()) {
     MmWork w;
     uint32_t split;
     tiles.get(w, split);
     t.sum(t.steps_of(w), ahead);
-    if constexpr (kFinal) {
+    if (a.final.out) {
       const MmPatch<F> to((F*)a.final.out + w.m0 * a.final.n + w.n0, a.final.n, a.rows - w.m0,
                           a.b.rows - w.n0);
       typename MmPatch<F>::Lane lane[Tile::kJ];
@@ -602,6 +715,16 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product a)
     }
   }
   t.stop();
+}
+
+// Both gradients' products of a piece in one launch: neither's tiles need fill the chip by
+// themselves.  8,192 rows, 16,384 vectors, 768 values, bf16: one after the other 250 us each.
+template <typename F, typename T, typename S>
+__global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product h, Product w) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
+  run_product<F, T, S, false>(h, 0, lds_of(lds_memory));
+  mm_barrier();  // the buffers have been read
+  run_product<F, T, S, true>(w, h.tiles_m * h.tiles_n * h.splits, lds_of(lds_memory));
 }
 
 // The splits' sum as a gradient, 4 values of a row at a time.
@@ -645,28 +768,58 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(Finish a) {
 
 int64_t round256(int64_t n) { return (n + 255) & ~int64_t(255); }
 
-// How a product is spread over the chip: the shape of its tiles, and into how many splits of k.
+int64_t tiles_of(int64_t m, int64_t n, const Measured& x) {
+  return ((m + x.bm - 1) / x.bm) * ((n + x.bn - 1) / x.bn);
+}
+
+// The shape of a product's tiles that takes the shortest, by what was measured; 4 us go around
+// each tile.
+Size size_of(int64_t m, int64_t n, int64_t k) {
+  Size best = kSmall;
+  double least = INFINITY;
+  for (const Size size : {kSmall, kDeep, kWide, kLarge}) {
+    const Measured& x = kMeasured[size];
+    const int64_t rounds = (tiles_of(m, n, x) + x.places - 1) / x.places;
+    const double us = (double)rounds * (x.each * (double)k + 4.0);
+    if (us < least) {
+      least = us;
+      best = size;
+    }
+  }
+  return best;
+}
+
+// How the two gradients' products are spread over the chip: the shape of their tiles, and into how
+// many splits of k each.
 struct Spread {
-  bool large;
-  int splits;
+  Size size;
+  int splits_h, splits_w;
 };
 
-// The cheapest by what was measured: a large tile takes 29 ns a value of k at one work-group a
-// CU, a small one 16 ns at two, and 4 us each around it; splits are written, read and added at
-// 4 TB/s.
-Spread spread_of(int64_t m, int64_t n, int64_t k, int most) {
-  Spread best{false, 1};
+// dh is [mh, n] over kh values, dw [mw, n] over kw.  Splits are written, read and added at 4 TB/s.
+Spread spread_of(int64_t mh, int64_t kh, int64_t mw, int64_t kw, int64_t n) {
+  Spread best{kSmall, 1, 1};
   double least = INFINITY;
-  for (int large = 0; large < 2; ++large) {
-    const int64_t side = large ? 256 : 128;
-    const int64_t tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
-    for (int s = 1; s <= most && (s == 1 || k / s >= 256); ++s) {
-      const double rounds = (double)((tiles * s + (large ? 255 : 511)) / (large ? 256 : 512));
-      double us = rounds * ((large ? 0.029 : 0.016) * (double)k / s + 4.0);
-      if (s > 1) us += 4.0 + (double)m * n * 8e-6 * s / 4.0;
-      if (us < least) {
-        least = us;
-        best = {large != 0, s};
+  const int options[] = {1, 2, 3, 4, 6, 8, 12, 16};
+  for (const Size size : {kSmall, kDeep, kWide, kLarge}) {
+    const Measured& x = kMeasured[size];
+    const int64_t th = tiles_of(mh, n, x), tw = tiles_of(mw, n, x);
+    for (const int sh : options) {
+      if (sh > 1 && kh / sh < 256) break;
+      const double one_h = x.each * (double)kh / sh + 4.0;
+      for (const int sw : options) {
+        if (sw > 1 && kw / sw < 256) break;
+        const double one_w = x.each * (double)kw / sw + 4.0;
+        const double all = (double)(th * sh) * one_h + (double)(tw * sw) * one_w;
+        const int64_t rounds = (th * sh + tw * sw + x.places - 1) / x.places;
+        const double mean = all / (double)(th * sh + tw * sw);
+        double us = std::max({(double)rounds * mean, one_h, one_w});
+        if (sh > 1) us += 2.0 + (double)mh * n * 2e-6 * sh;
+        if (sw > 1) us += 4.0 + (double)mw * n * 2e-6 * sw;
+        if (us < least) {
+          least = us;
+          best = {size, sh, sw};
+        }
       }
     }
   }
@@ -678,7 +831,7 @@ struct Layout {
   int64_t k;                     // n, up to the next multiple of 8
   int planes, pairs;
   int weighed_planes, weighed_pairs;  // of dw's product
-  Spread h_spread, w_spread;
+  Spread spread;
   int64_t h, w, part, target, g, weighed, row, largest, dh, dw, power, bytes;
 };
 
@@ -700,23 +853,25 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
   l.w = take(l.piece * l.k * 2 * l.planes);
   if (!backward) {
     const int64_t chunk = std::min(rows, kRowChunk);
-    l.part = take((vocab + kSmallest - 1) / kSmallest * chunk * (int64_t)sizeof(Part));
+    // of the tiles, or of the few rows' work-groups
+    const int64_t parts = std::max<int64_t>((vocab + kSmallest - 1) / kSmallest,
+                                            rows <= kThinRows ? kThinMost : 0);
+    l.part = take(parts * chunk * (int64_t)sizeof(Part));
     l.target = take(chunk * 4);
   } else {
     const int64_t vs = std::min(l.piece, vocab);
-    l.h_spread = spread_of(rows, n, vs * l.pairs, 16);
     // h times its row's factor is rounded a second time: where dw's product takes a few us at the
     // most (2^31 products: 4 us), what that loses is a plane of its own
     const bool few = dtype != SIEVE_F32 && rows * vocab <= (int64_t(1) << 31) / n;
     l.weighed_planes = few ? 2 : l.planes;
     l.weighed_pairs = few ? 2 : l.pairs;
-    l.w_spread = spread_of(vs, n, rows * l.weighed_pairs, 16);
+    l.spread = spread_of(rows, vs * l.pairs, vs, rows * l.weighed_pairs, n);
     l.g = take(rows * l.piece * 2 * l.planes);
     l.weighed = take(rows * l.k * 2 * l.weighed_planes);
     l.row = take(rows * (int64_t)sizeof(Row));
     l.largest = take(kMostLargest * 4);
-    l.dh = take(l.h_spread.splits * rows * l.k * 4);
-    l.dw = take(l.w_spread.splits * l.piece * l.k * 4);
+    l.dh = take(l.spread.splits_h * rows * l.k * 4);
+    l.dw = take(l.spread.splits_w * l.piece * l.k * 4);
     l.power = take(4);
   }
   l.bytes = at;
@@ -774,6 +929,15 @@ bool direct(const void* p, int64_t stride, int32_t n, int32_t dtype) {
          ((uintptr_t)p & 15) == 0;
 }
 
+// Whether there are few rows, that may be multiplied where they lie.
+bool thin(const void* h, int64_t h_stride, const void* table, int64_t t_stride, int64_t rows,
+          int32_t n, int size) {
+  auto whole = [&](const void* p, int64_t stride) {
+    return ((uintptr_t)p & 15) == 0 && stride * size % 16 == 0 && stride <= kMmMaxStride;
+  };
+  return rows <= kThinRows && n * size % 16 == 0 && whole(h, h_stride) && whole(table, t_stride);
+}
+
 // The operand of rows [0, rows) of x, packed into `to` where that is needed.
 template <typename T>
 MmOperand operand(const void* x, int64_t stride, int64_t rows, int32_t n, int32_t dtype, int64_t k,
@@ -802,17 +966,9 @@ hipError_t allow_shape() {
   add(loss_gradient_kernel<f16, f16, S>);
   add(loss_gradient_kernel<bf16, bf16, S>);
   add(loss_gradient_kernel<float, bf16, S>);
-  auto products = [&](auto f, auto t) {
-    typedef decltype(f) F;
-    typedef decltype(t) T;
-    add(loss_product_kernel<F, T, S, false, false>);
-    add(loss_product_kernel<F, T, S, false, true>);
-    add(loss_product_kernel<F, T, S, true, false>);
-    add(loss_product_kernel<F, T, S, true, true>);
-  };
-  products(float{}, bf16{});
-  products(f16{}, f16{});
-  products(bf16{}, bf16{});
+  add(loss_product_kernel<float, bf16, S>);
+  add(loss_product_kernel<f16, f16, S>);
+  add(loss_product_kernel<bf16, bf16, S>);
   return r;
 }
 
@@ -820,11 +976,21 @@ int allow_lds() {
   int device = 0;
   ENC_HIP_TRY(hipGetDevice(&device));
   const hipError_t e = once_per_device(g_large_lds, device, [] {
-    const hipError_t r = allow_shape<Large>();
-    return r == hipSuccess ? allow_shape<Small>() : r;
+    hipError_t r = allow_shape<Large>();
+    if (r == hipSuccess) r = allow_shape<Wide>();
+    if (r == hipSuccess) r = allow_shape<Small>();
+    return r == hipSuccess ? allow_shape<Deep>() : r;
   });
   ENC_HIP_TRY(e);
   return SIEVE_OK;
+}
+
+uint32_t tiles_of(int64_t n, int size) { return (uint32_t)((n + size - 1) / size); }
+
+void join_parts(const Join& a, hipStream_t s) {
+  // few rows: more threads for each
+  if (a.rows <= 512) loss_join_kernel<4><<<tiles_of(a.rows, 4), 256, 0, s>>>(a);
+  else loss_join_kernel<32><<<tiles_of(a.rows, 32), 256, 0, s>>>(a);
 }
 
 void set_scale(Logits& a, float scale) {
@@ -853,38 +1019,23 @@ void finish(const float* x, int64_t rows, int64_t pitch, int64_t split, int spli
   loss_finish_kernel<F><<<(int)std::min<int64_t>(groups, 65536), 256, 0, s>>>(a);
 }
 
-uint32_t tiles_of(int64_t n, int size) { return (uint32_t)((n + size - 1) / size); }
-
 // f(the shape)
 template <typename F>
-void by_shape(bool large, F f) {
-  if (large) f(Large{});
+void by_shape(Size size, F f) {
+  if (size == kLarge) f(Large{});
+  else if (size == kWide) f(Wide{});
+  else if (size == kDeep) f(Deep{});
   else f(Small{});
 }
 
-// Whether the logits' tiles are large.
-bool large_logits(int64_t vectors, int64_t rows, int64_t k) {
-  return spread_of(vectors, rows, k, 1).large;
-}
-
-// The product, and what turns its sums into the gradient where no later one adds to them.
-template <typename F, typename T, bool kAcrossA>
-void product(Product& p, const Spread& spread, bool last, hipStream_t s) {
-  by_shape(spread.large, [&](auto shape) {
-    typedef decltype(shape) S;
-    const int64_t each = (p.k + spread.splits - 1) / spread.splits;
-    p.per = (each + kStep - 1) / kStep * kStep;
-    p.tiles_m = tiles_of(p.rows, S::BM);
-    p.tiles_n = tiles_of(p.final.n, S::BN);
-    p.splits = spread.splits;
-    const uint32_t grid = mm_grid((uint64_t)p.tiles_m * p.tiles_n * p.splits, S::kMost);
-    if (last && !p.add && spread.splits == 1)
-      loss_product_kernel<F, T, S, kAcrossA, true><<<grid, S::kThreads, S::kLds, s>>>(p);
-    else
-      loss_product_kernel<F, T, S, kAcrossA, false><<<grid, S::kThreads, S::kLds, s>>>(p);
-  });
-  if (last && (p.add || spread.splits > 1))
-    finish<F>(p.out, p.rows, p.pitch, p.split, spread.splits, p.final, s);
+// Sets how a product is cut into tiles and splits.
+template <typename S>
+void cut(Product& p, int splits) {
+  const int64_t each = (p.k + splits - 1) / splits;
+  p.per = (each + kStep - 1) / kStep * kStep;
+  p.splits = splits;
+  p.tiles_m = tiles_of(p.rows, S::BM);
+  p.tiles_n = tiles_of(p.final.n, S::BN);
 }
 
 }  // namespace
@@ -917,12 +1068,20 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
     typedef decltype(f) F;
     typedef decltype(t) T;
     Logits a{};
-    a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
-    a.k = l.k;
-    a.pairs = l.pairs;
     set_scale(a, scale);
     a.targets = {targets, target_bytes, vocab};
     a.target_dot = (float*)(w + l.target);
+    if (thin(h, h_stride, table, table_stride, rows, n, sizeof(F))) {
+      const Thin x{h, table, h_stride, table_stride, vocab, (int)rows, n, a.c2, a.targets,
+                   (Part*)(w + l.part), a.target_dot};
+      const int groups = (int)std::min<int64_t>((vocab + 63) / 64, kThinMost);
+      loss_thin_kernel<F><<<groups, 256, 0, s>>>(x);
+      join_parts({x.part, x.target_dot, x.targets, 0, rows, groups, a.c2, scale, loss, lse}, s);
+      return;
+    }
+    a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
+    a.k = l.k;
+    a.pairs = l.pairs;
     const MmOperand all_h = a.h;
     // a table that has to be packed is taken in pieces; any is, where a launch would be too large
     const bool as_is = direct(table, table_stride, n, dtype);
@@ -932,9 +1091,9 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
       a.h.p = (const char*)all_h.p + t0 * all_h.stride * 2;
       a.h.rows = std::min(rows - t0, kRowChunk);
       a.t_first = t0;
-      const bool large = large_logits(std::min(piece, vocab), a.h.rows, l.k * l.pairs);
-      const int side = large ? Large::BM : Small::BM;
-      a.tiles_n = tiles_of(a.h.rows, side);
+      const Size size = size_of(std::min(piece, vocab), a.h.rows, l.k * l.pairs);
+      const int side = kMeasured[size].bm;
+      a.tiles_n = tiles_of(a.h.rows, kMeasured[size].bn);
       for (int64_t v0 = 0; v0 < vocab; v0 += piece) {
         const int64_t vs = std::min(piece, vocab - v0);
         a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
@@ -942,15 +1101,14 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
         a.v_first = v0;
         a.tiles_m = tiles_of(vs, side);
         a.part = (Part*)(w + l.part) + v0 / side * a.h.rows;
-        by_shape(large, [&](auto shape) {
+        by_shape(size, [&](auto shape) {
           typedef decltype(shape) S;
           loss_forward_kernel<T, S>
               <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
         });
       }
-      loss_join_kernel<<<tiles_of(a.h.rows, 32), 256, 0, s>>>(
-          {(const Part*)(w + l.part), a.target_dot, a.targets, t0, a.h.rows, tiles_of(vocab, side),
-           a.c2, scale, loss, lse});
+      join_parts({(const Part*)(w + l.part), a.target_dot, a.targets, t0, a.h.rows,
+                  tiles_of(vocab, side), a.c2, scale, loss, lse}, s);
     }
   });
   ENC_HIP_TRY(hipGetLastError());
@@ -1013,47 +1171,62 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     a.g = w + l.g;
     a.g_stride = l.piece;
     a.g_plane = rows * l.piece;
-    const bool large = large_logits(std::min(l.piece, vocab), rows, l.k * l.pairs);
+    const Size size = size_of(std::min(l.piece, vocab), rows, l.k * l.pairs);
     for (int64_t v0 = 0; v0 < vocab; v0 += l.piece) {
       const int64_t vs = std::min(l.piece, vocab - v0);
       const bool last = v0 + vs == vocab;
       a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
                        w + l.w, s);
       a.v_first = v0;
-      by_shape(large, [&](auto shape) {
+      by_shape(size, [&](auto shape) {
         typedef decltype(shape) S;
         a.tiles_m = tiles_of(vs, S::BM);
         a.tiles_n = tiles_of(rows, S::BN);
         loss_gradient_kernel<F, T, S>
             <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
       });
-      Product p{};
-      p.pairs = l.pairs;
-      p.pitch = l.k;
-      if (dh) {
-        p.a = {a.g, l.piece, rows, a.g_plane};
-        p.b = a.w;
-        p.b.rows = n;
-        p.k = vs;
-        p.rows = rows;
-        p.out = (float*)(w + l.dh);
-        p.split = rows * l.k;
-        p.add = v0 > 0;
-        p.final = {dh, n, factor, nullptr, row};
-        product<F, T, false>(p, l.h_spread, last, s);
-      }
-      if (dtable) {
-        p.a = {a.g, l.piece, l.piece, a.g_plane};
-        p.b = {w + l.weighed, l.k, n, rows * l.k};
-        p.pairs = l.weighed_pairs;
-        p.k = rows;
-        p.rows = vs;
-        p.out = (float*)(w + l.dw);
-        p.split = l.piece * l.k;
-        p.add = 0;
-        p.final = {(F*)dtable + v0 * n, n, factor, power, nullptr};
-        product<F, T, true>(p, l.w_spread, true, s);
-      }
+      Product ph{}, pw{};
+      const Final final_h{dh, n, factor, nullptr, row};
+      const Final final_w{(F*)dtable + v0 * n, n, factor, power, nullptr};
+      ph.pitch = pw.pitch = l.k;
+      by_shape(l.spread.size, [&](auto shape) {
+        typedef decltype(shape) S;
+        if (dh) {
+          ph.a = {a.g, l.piece, rows, a.g_plane};
+          ph.b = a.w;
+          ph.b.rows = n;
+          ph.k = vs;
+          ph.pairs = l.pairs;
+          ph.rows = rows;
+          ph.out = (float*)(w + l.dh);
+          ph.split = rows * l.k;
+          ph.add = v0 > 0;
+          ph.final = final_h;
+          cut<S>(ph, l.spread.splits_h);
+          // the gradient itself, where nothing is to be added
+          if (vs < vocab || ph.splits > 1) ph.final.out = nullptr;
+        }
+        if (dtable) {
+          pw.a = {a.g, l.piece, l.piece, a.g_plane};
+          pw.b = {w + l.weighed, l.k, n, rows * l.k};
+          pw.k = rows;
+          pw.pairs = l.weighed_pairs;
+          pw.rows = vs;
+          pw.out = (float*)(w + l.dw);
+          pw.split = l.piece * l.k;
+          pw.final = final_w;
+          cut<S>(pw, l.spread.splits_w);
+          if (pw.splits > 1) pw.final.out = nullptr;
+        }
+        const uint64_t tiles = (uint64_t)ph.tiles_m * ph.tiles_n * ph.splits +
+                               (uint64_t)pw.tiles_m * pw.tiles_n * pw.splits;
+        loss_product_kernel<F, T, S>
+            <<<mm_grid(tiles, S::kMost), S::kThreads, S::kLds, s>>>(ph, pw);
+      });
+      if (dtable && !pw.final.out)
+        finish<F>(pw.out, vs, l.k, pw.split, pw.splits, final_w, s);
+      if (dh && !ph.final.out && last)
+        finish<F>(ph.out, rows, l.k, ph.split, ph.splits, final_h, s);
     }
   });
   ENC_HIP_TRY(hipGetLastError());

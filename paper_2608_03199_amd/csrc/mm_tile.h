@@ -169,12 +169,16 @@ struct MmWork {
 // run of places, and its work-groups take them side by side.
 struct MmPlaces {
   uint32_t place, end, step;
-  __device__ __forceinline__ explicit MmPlaces(uint32_t all) {
+  // before: tiles that were shared out the same way just before these: the work-groups that had
+  // one more of them come last now
+  __device__ __forceinline__ explicit MmPlaces(uint32_t all, uint32_t before = 0) {
     const uint32_t die = blockIdx.x % 8, each = all / 8, more = all % 8;
     const uint32_t first = die * each + (die < more ? die : more);
+    const uint32_t had = before / 8 + (die < before % 8 ? 1 : 0);
     end = first + each + (die < more ? 1 : 0);
-    place = first + blockIdx.x / 8;
     step = (gridDim.x - die + 7) / 8;
+    const uint32_t slot = blockIdx.x / 8, skip = had % step;
+    place = first + (slot >= skip ? slot - skip : slot + step - skip);
   }
   __device__ __forceinline__ bool there() const { return place < end; }
   __device__ __forceinline__ void next() { place += step; }
