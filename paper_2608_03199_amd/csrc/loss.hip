@@ -50,11 +50,10 @@ constexpr int64_t kMaxPiece = 65536;       // vectors
 constexpr int64_t kRowChunk = 65536;       // rows of h in one launch of the forward pass
 constexpr float kHalfScale = 16384.f;      // what g in binary16 is scaled by
 
-// A work-group's tile.  Large and wide ones have a CU to themselves and eight waves; two small ones
-// share it; deep ones are as small, with eight waves and more loads on their way, for launches of
-// no more than a tile a CU.  2,048 x 2,048 x 8,192 bf16, 256 tiles: deep 87 us, small 105;
-// 8,192 x 768 x 8,192: wide 119 us (192 tiles), small 128, large 180; 8,192^3: large 891 us
-// (1,234 TFLOP/s), small 1,027.
+// A work-group's tile.  A large one has a CU to itself and eight waves; two small ones share it;
+// deep ones are as small, with eight waves and more loads on their way, for launches of no more
+// than a tile a CU.  2,048 x 2,048 x 8,192 bf16, 256 tiles: deep 87 us, small 105; 8,192^3: large
+// 891 us (1,234 TFLOP/s), small 1,027.
 template <int BM_, int BN_, int WM_, int WN_, int kStages>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM_ * WN_;
@@ -65,16 +64,15 @@ struct Shape {
   static constexpr uint32_t kMost = kLds > 81920 ? 256 : 512;  // work-groups on the chip
 };
 typedef Shape<256, 256, 2, 4, 2> Large;
-typedef Shape<256, 128, 4, 2, 3> Wide;
 typedef Shape<128, 128, 2, 2, 2> Small;
 typedef Shape<128, 128, 2, 4, 4> Deep;
-enum Size { kSmall, kDeep, kWide, kLarge };
+enum Size { kSmall, kDeep, kLarge };
 struct Measured {
   int bm, bn, places;
   double each;           // us a value of k and tile, where the chip is full
 };
 constexpr Measured kMeasured[] = {
-    {128, 128, 512, 0.016}, {128, 128, 256, 0.0107}, {256, 128, 256, 0.0145}, {256, 256, 256, 0.029}};
+    {128, 128, 512, 0.0175}, {128, 128, 256, 0.0107}, {256, 256, 256, 0.029}};
 constexpr int kSmallest = 128;            // the lesser of the shapes' BM
 
 struct Targets {
@@ -718,7 +716,8 @@ __device__ __forceinline__ void run_product(const Product& a, uint32_t before, u
 }
 
 // Both gradients' products of a piece in one launch: neither's tiles need fill the chip by
-// themselves.  8,192 rows, 16,384 vectors, 768 values, bf16: one after the other 250 us each.
+// themselves.  8,192 rows, 16,384 vectors, 768 values, bf16: 462 us in large tiles, 511 in small
+// ones; one after the other 250 us each.
 template <typename F, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, 2) void loss_product_kernel(Product h, Product w) {
   extern __shared__ __attribute__((aligned(1024))) char lds_memory[];
@@ -777,7 +776,7 @@ int64_t tiles_of(int64_t m, int64_t n, const Measured& x) {
 Size size_of(int64_t m, int64_t n, int64_t k) {
   Size best = kSmall;
   double least = INFINITY;
-  for (const Size size : {kSmall, kDeep, kWide, kLarge}) {
+  for (const Size size : {kSmall, kDeep, kLarge}) {
     const Measured& x = kMeasured[size];
     const int64_t rounds = (tiles_of(m, n, x) + x.places - 1) / x.places;
     const double us = (double)rounds * (x.each * (double)k + 4.0);
@@ -801,7 +800,7 @@ Spread spread_of(int64_t mh, int64_t kh, int64_t mw, int64_t kw, int64_t n) {
   Spread best{kSmall, 1, 1};
   double least = INFINITY;
   const int options[] = {1, 2, 3, 4, 6, 8, 12, 16};
-  for (const Size size : {kSmall, kDeep, kWide, kLarge}) {
+  for (const Size size : {kSmall, kDeep, kLarge}) {
     const Measured& x = kMeasured[size];
     const int64_t th = tiles_of(mh, n, x), tw = tiles_of(mw, n, x);
     for (const int sh : options) {
@@ -977,7 +976,6 @@ int allow_lds() {
   ENC_HIP_TRY(hipGetDevice(&device));
   const hipError_t e = once_per_device(g_large_lds, device, [] {
     hipError_t r = allow_shape<Large>();
-    if (r == hipSuccess) r = allow_shape<Wide>();
     if (r == hipSuccess) r = allow_shape<Small>();
     return r == hipSuccess ? allow_shape<Deep>() : r;
   });
@@ -1023,7 +1021,6 @@ void finish(const float* x, int64_t rows, int64_t pitch, int64_t split, int spli
 template <typename F>
 void by_shape(Size size, F f) {
   if (size == kLarge) f(Large{});
-  else if (size == kWide) f(Wide{});
   else if (size == kDeep) f(Deep{});
   else f(Small{});
 }

@@ -49,6 +49,7 @@ constexpr float kScaleX = 16384.f, kScaleA = 4096.f;  // of X; of A and B
 constexpr double kMaxX = 3.9, kMaxA = 15.9;           // below 65504 times these
 constexpr int kMaxSide = 65536;
 constexpr int kMaxSteps = 1000;
+constexpr int kPlainSteps = 2;                        // of the last, for bfloat16
 constexpr int kSums = 64;                             // parts of a matrix's sum of squares
 constexpr int64_t kFewTiles = 128;                    // of the usual shape
 constexpr int64_t kMostBytes = int64_t(1) << 31;      // of the workspace, for one matrix or more
@@ -64,16 +65,44 @@ struct Source {
   void* out;             // without steps: the result
 };
 
-template <typename T>
+// 8 values of a row from a column that is a multiple of 8, zeros past its end.
+template <typename T, bool kWhole>
+__device__ __forceinline__ void load8(const T* row, int col, int n, float (&v)[8]) {
+  if constexpr (kWhole) {
+    const EncVec<T, 8> q = enc_load<T, 8>(row + col);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)q.v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = col + j < n ? (float)row[col + j] : 0.f;
+  }
+}
+
+// A work-group's parts of a matrix: moves blockIdx.x * 256 + thread, and so on, by gridDim.x * 256.
+// f(row, column of 8)
+template <typename F>
+__device__ __forceinline__ void each_move(const Source& a, F f) {
+  const uint32_t moves = (uint32_t)(a.pitch / 8);
+  const uint64_t all = (uint64_t)a.m * moves;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+       i += (uint64_t)gridDim.x * 256) {
+    // fewer than 2^16 x 2^13 moves
+    const uint32_t row = (uint32_t)i / moves;
+    f((int)row, (int)((uint32_t)i - row * moves) * 8);
+  }
+}
+
+template <typename T, bool kWhole>
 __global__ __launch_bounds__(256) void orth_norm_kernel(Source a) {
   __shared__ double s[4];
   const T* g = (const T*)a.g + blockIdx.y * a.batch_stride;
   double sum = 0.0;
-  for (int64_t row = blockIdx.x; row < a.m; row += kSums)
-    for (int64_t col = threadIdx.x; col < a.n; col += 256) {
-      const double v = (double)(float)g[row * a.row_stride + col];
-      sum += v * v;
-    }
+  each_move(a, [&](int row, int col) {
+    float v[8];
+    load8<T, kWhole>(g + row * a.row_stride, col, (int)a.n, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fma((double)v[j], (double)v[j], sum);
+  });
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
@@ -87,30 +116,43 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
 }
 
 // X of the matrix, zeros up to the pitch.
-template <typename T, bool kOut>
+template <typename T, bool kWhole, bool kOut>
 __global__ __launch_bounds__(256) void orth_scale_kernel(Source a) {
-  double sum = 0.0;
+  __shared__ double s_inv;
+  if (threadIdx.x < 64) {
+    double sum = a.sums[blockIdx.y * kSums + threadIdx.x];
 #pragma unroll
-  for (int i = 0; i < kSums; ++i) sum += a.sums[blockIdx.y * kSums + i];
-  const double inv = 1.0 / (sqrt(sum) + (double)a.eps);
-  const T* g = (const T*)a.g + blockIdx.y * a.batch_stride;
-  const int64_t width = kOut ? a.n : a.pitch;
-  for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
-    const int64_t at = (blockIdx.y * a.m + row) * width;
-    for (int64_t col = threadIdx.x; col < width; col += 256) {
-      const float v =
-          col < a.n ? (float)((double)(float)g[row * a.row_stride + col] * inv) : 0.f;
-      if constexpr (kOut) ((T*)a.out)[at + col] = (T)v;
-      else split(v * kScaleX, a.x[at + col], a.x[a.plane + at + col]);
-    }
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (threadIdx.x == 0) s_inv = 1.0 / (sqrt(sum) + (double)a.eps);
   }
+  __syncthreads();
+  const double inv = s_inv;
+  const T* g = (const T*)a.g + blockIdx.y * a.batch_stride;
+  each_move(a, [&](int row, int col) {
+    float v[8];
+    load8<T, kWhole>(g + row * a.row_stride, col, (int)a.n, v);
+    const int64_t matrix_row = blockIdx.y * a.m + row;
+    if constexpr (kOut) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col + j < a.n) ((T*)a.out)[matrix_row * a.n + col + j] = (T)(float)(v[j] * inv);
+    } else {
+      EncVec<f16, 8> hi, lo;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) split((float)(v[j] * inv) * kScaleX, hi.v[j], lo.v[j]);
+      enc_store<f16, 8>(a.x + matrix_row * a.pitch + col, hi);
+      enc_store<f16, 8>(a.x + a.plane + matrix_row * a.pitch + col, lo);
+    }
+  });
 }
+static_assert(kSums == 64, "a wave adds up the parts");
 
 // One product of a step, for every matrix.
 struct Product {
   MmOperand a, b;        // of the first matrix
   int64_t a_next, b_next;
   int64_t k;
+  int pairs;             // of planes: 3, or 1 where the first parts are enough
   int64_t rows, cols;    // that are written: zeros past the matrix's, up to the pitch
   int64_t side;
   uint32_t tiles, tiles_m, tiles_n;  // tiles of a matrix
@@ -160,7 +202,7 @@ __global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
   MmOperand x = a.a, y = a.b;
   x.p = (const f16*)x.p + matrix * a.a_next;
   y.p = (const f16*)y.p + matrix * a.b_next;
-  Tile t(x, y, 3,
+  Tile t(x, y, a.pairs,
          (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_memory);
   bool first_one = true;
   auto next = [&](MmWork& to) {
@@ -330,13 +372,21 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
   const bool tall = m > n;
   Source src{g, batch_stride, row_stride, m, n, l.pitch, eps, (double*)(w + l.sums),
              (f16*)(w + l.x[0]), batch * m * l.pitch, out};
-  orth_norm_kernel<T><<<dim3(kSums, (uint32_t)batch), 256, 0, s>>>(src);
-  const dim3 rows((uint32_t)std::min<int64_t>(m, 1024), (uint32_t)batch);
-  if (steps == 0) {
-    orth_scale_kernel<T, true><<<rows, 256, 0, s>>>(src);
-    return;
-  }
-  orth_scale_kernel<T, false><<<rows, 256, 0, s>>>(src);
+  const dim3 parts(kSums, (uint32_t)batch);
+  // some 4 moves a thread
+  const int64_t groups = (m * (l.pitch / 8) + 1023) / 1024;
+  const dim3 rows((uint32_t)std::min<int64_t>(groups, 4096), (uint32_t)batch);
+  const bool whole = n % 8 == 0 && ((uintptr_t)g & 15) == 0 && row_stride * sizeof(T) % 16 == 0 &&
+                     batch_stride * sizeof(T) % 16 == 0;
+  auto begin = [&](auto w8) {
+    constexpr bool kWhole = decltype(w8)::value;
+    orth_norm_kernel<T, kWhole><<<parts, 256, 0, s>>>(src);
+    if (steps == 0) orth_scale_kernel<T, kWhole, true><<<rows, 256, 0, s>>>(src);
+    else orth_scale_kernel<T, kWhole, false><<<rows, 256, 0, s>>>(src);
+  };
+  if (whole) begin(std::true_type{});
+  else begin(std::false_type{});
+  if (steps == 0) return;
   const int64_t side = l.side, sp = l.side_pitch, square = sp * sp;
   f16 *gram = (f16*)(w + l.gram), *second = (f16*)(w + l.second), *poly = (f16*)(w + l.poly);
   const MmOperand of_a{gram, sp, side, batch * square}, of_c{second, sp, side, batch * square},
@@ -366,6 +416,7 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     const bool last = i == steps - 1;
     // A: over the longer side
     Product p{};
+    p.pairs = std::is_same_v<T, bf16> && steps - i <= kPlainSteps ? 1 : 3;
     p.a = p.b = {x, l.pitch, side, src.plane};
     p.a_next = p.b_next = m * l.pitch;
     p.k = tall ? m : n;
