@@ -17,6 +17,7 @@
 //
 // 16-bit inputs are multiplied as they are.  32-bit ones come as three bf16 planes whose sum is
 // the value (8 bits each), six products of planes: what is left out is below fp32's last bit.
+// 2,001 x 7,919 x 515, both passes: 580 us with the pairs one after the other.
 //
 // g is rounded once, to the inputs' type, and what its target has outweighs the rest of its row:
 // g_t,target = -(1 - p_t) dloss_t.  A rounding of it would be the same for every token of a
@@ -41,7 +42,6 @@ typedef mm_f16 f16;
 
 constexpr double kLog2e = 1.4426950408889634;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kStep = 64;                 // values of k a step
 constexpr int kHigh = 8;                  // tiles of m before the next of n, see mm_tile_at
 constexpr int64_t kMaxRows = 1 << 24;     // of h, and of the table
 constexpr int kMaxN = 65536;
@@ -54,25 +54,30 @@ constexpr float kHalfScale = 16384.f;      // what g in binary16 is scaled by
 // deep ones are as small, with eight waves and more loads on their way, for launches of no more
 // than a tile a CU.  2,048 x 2,048 x 8,192 bf16, 256 tiles: deep 87 us, small 105; 8,192^3: large
 // 891 us (1,234 TFLOP/s), small 1,027.
-template <int BM_, int BN_, int WM_, int WN_, int kStages>
+// Triple ones are for values of three planes.
+template <int BM_, int BN_, int WM_, int WN_, int kStep_, int kStages, int kPlanes_>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM_ * WN_;
+  static constexpr int kStep = kStep_, kPlanes = kPlanes_;
   template <typename T, bool kAcrossA, bool kAcrossB>
-  using Tile = MmTile<T, BM, BN, kAcrossA, kAcrossB, WM, WN, kStep, kStages>;
+  using Tile = MmTile<T, BM, BN, kAcrossA, kAcrossB, WM, WN, kStep, kStages, kPlanes>;
   static constexpr int kTileLds = Tile<mm_bf16, false, false>::kLds;
   static constexpr int kLds = kTileLds + WM * BN * 8;  // and the forward pass's parts
   static constexpr uint32_t kMost = kLds > 81920 ? 256 : 512;  // work-groups on the chip
 };
-typedef Shape<256, 256, 2, 4, 2> Large;
-typedef Shape<128, 128, 2, 2, 2> Small;
-typedef Shape<128, 128, 2, 4, 4> Deep;
-enum Size { kSmall, kDeep, kLarge };
+typedef Shape<256, 256, 2, 4, 64, 2, 1> Large;
+typedef Shape<128, 128, 2, 2, 64, 2, 1> Small;
+typedef Shape<128, 128, 2, 4, 64, 4, 1> Deep;
+typedef Shape<128, 128, 2, 4, 32, 3, 3> Triple;
+enum Size { kSmall, kDeep, kLarge, kTriple };
 struct Measured {
   int bm, bn, places;
   double each;           // us a value of k and tile, where the chip is full
 };
-constexpr Measured kMeasured[] = {
-    {128, 128, 512, 0.0175}, {128, 128, 256, 0.0107}, {256, 256, 256, 0.029}};
+constexpr Measured kMeasured[] = {{128, 128, 512, 0.0175},
+                                  {128, 128, 256, 0.0107},
+                                  {256, 256, 256, 0.029},
+                                  {128, 128, 256, 0.05}};
 constexpr int kSmallest = 128;            // the lesser of the shapes' BM
 
 struct Targets {
@@ -122,7 +127,6 @@ struct Logits {
   int64_t v_first;       // the piece's first vector
   int64_t t_first;       // the rows' first
   int64_t k;             // n, up to the next multiple of 8
-  int pairs;
   uint32_t tiles_m, tiles_n;
   float c2, c2_rest;     // scale log2(e), and what rounding took from it
   float scale;
@@ -187,7 +191,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_forward_kernel(Logits a) 
   typedef typename S::template Tile<T, false, false> Tile;
   Tiles<S> ahead(a.tiles_m, a.tiles_n, a.k), tiles = ahead;
   if (!tiles.at.there()) return;
-  Tile t(a.w, a.h, a.pairs, lds_of(lds_memory));
+  Tile t(a.w, a.h, 1, lds_of(lds_memory));
   t.start(ahead);
   constexpr int kWave = S::BM / S::WM;   // vectors of a wave
   const int wave_m = Tile::wave() / S::WN, half = (int)threadIdx.x >> 5 & 1;
@@ -518,7 +522,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
   typedef typename S::template Tile<T, false, false> Tile;
   Tiles<S> ahead(a.tiles_m, a.tiles_n, a.k), tiles = ahead;
   if (!tiles.at.there()) return;
-  Tile t(a.w, a.h, a.pairs, lds_of(lds_memory));
+  Tile t(a.w, a.h, 1, lds_of(lds_memory));
   t.start(ahead);
   constexpr int kWave = S::BM / S::WM;
   const int wave_m = Tile::wave() / S::WN, half = (int)threadIdx.x >> 5 & 1;
@@ -627,7 +631,7 @@ __device__ __forceinline__ float factor_of(const Final& a, int64_t row) {
 struct Product {
   MmOperand a, b;
   int64_t k, per;        // values of k, and of a split
-  int pairs;
+  int planes_b;          // of b, for one of a
   uint32_t tiles_m, tiles_n, splits;
   int64_t rows;          // of m, that are written
   float* out;
@@ -668,7 +672,7 @@ __device__ __forceinline__ void run_product(const Product& a, uint32_t before, u
   typedef typename S::template Tile<T, kAcrossA, true> Tile;
   Splits<S> ahead(a, before), tiles = ahead;
   if (!tiles.at.there()) return;
-  Tile t(a.a, a.b, a.pairs, lds);
+  Tile t(a.a, a.b, a.planes_b, lds);
   t.start(ahead);
   for (; tiles.at.there(); tiles.at.next()) {
     MmWork w;
@@ -773,7 +777,8 @@ int64_t tiles_of(int64_t m, int64_t n, const Measured& x) {
 
 // The shape of a product's tiles that takes the shortest, by what was measured; 4 us go around
 // each tile.
-Size size_of(int64_t m, int64_t n, int64_t k) {
+Size size_of(int64_t m, int64_t n, int64_t k, int planes) {
+  if (planes == 3) return kTriple;
   Size best = kSmall;
   double least = INFINITY;
   for (const Size size : {kSmall, kDeep, kLarge}) {
@@ -796,11 +801,12 @@ struct Spread {
 };
 
 // dh is [mh, n] over kh values, dw [mw, n] over kw.  Splits are written, read and added at 4 TB/s.
-Spread spread_of(int64_t mh, int64_t kh, int64_t mw, int64_t kw, int64_t n) {
+Spread spread_of(int64_t mh, int64_t kh, int64_t mw, int64_t kw, int64_t n, int planes) {
   Spread best{kSmall, 1, 1};
   double least = INFINITY;
   const int options[] = {1, 2, 3, 4, 6, 8, 12, 16};
-  for (const Size size : {kSmall, kDeep, kLarge}) {
+  for (const Size size : {kSmall, kDeep, kLarge, kTriple}) {
+    if ((planes == 3) != (size == kTriple)) continue;
     const Measured& x = kMeasured[size];
     const int64_t th = tiles_of(mh, n, x), tw = tiles_of(mw, n, x);
     for (const int sh : options) {
@@ -828,8 +834,8 @@ Spread spread_of(int64_t mh, int64_t kh, int64_t mw, int64_t kw, int64_t n) {
 struct Layout {
   int64_t piece;                 // vectors of a piece, a multiple of 256
   int64_t k;                     // n, up to the next multiple of 8
-  int planes, pairs;
-  int weighed_planes, weighed_pairs;  // of dw's product
+  int planes;
+  int weighed_planes;            // of h in dw's product
   Spread spread;
   int64_t h, w, part, target, g, weighed, row, largest, dh, dw, power, bytes;
 };
@@ -837,7 +843,6 @@ struct Layout {
 Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool backward) {
   Layout l{};
   l.planes = dtype == SIEVE_F32 ? 3 : 1;
-  l.pairs = dtype == SIEVE_F32 ? 6 : 1;
   l.k = (n + 7) & ~7;
   int64_t piece = std::min(kPieceValues / (l.planes * std::max<int64_t>(rows, 1)), kMaxPiece);
   piece = std::max<int64_t>(piece & ~int64_t(255), 256);
@@ -863,8 +868,7 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
     // most (2^31 products: 4 us), what that loses is a plane of its own
     const bool few = dtype != SIEVE_F32 && rows * vocab <= (int64_t(1) << 31) / n;
     l.weighed_planes = few ? 2 : l.planes;
-    l.weighed_pairs = few ? 2 : l.pairs;
-    l.spread = spread_of(rows, vs * l.pairs, vs, rows * l.weighed_pairs, n);
+    l.spread = spread_of(rows, vs, vs, few ? 2 * rows : rows, n, l.planes);
     l.g = take(rows * l.piece * 2 * l.planes);
     l.weighed = take(rows * l.k * 2 * l.weighed_planes);
     l.row = take(rows * (int64_t)sizeof(Row));
@@ -960,14 +964,17 @@ hipError_t allow_shape() {
   auto add = [&](auto* kernel) {
     if (r == hipSuccess) r = allow(kernel, S::kLds);
   };
-  add(loss_forward_kernel<f16, S>);
   add(loss_forward_kernel<bf16, S>);
-  add(loss_gradient_kernel<f16, f16, S>);
-  add(loss_gradient_kernel<bf16, bf16, S>);
-  add(loss_gradient_kernel<float, bf16, S>);
-  add(loss_product_kernel<float, bf16, S>);
-  add(loss_product_kernel<f16, f16, S>);
-  add(loss_product_kernel<bf16, bf16, S>);
+  if constexpr (S::kPlanes == 3) {
+    add(loss_gradient_kernel<float, bf16, S>);
+    add(loss_product_kernel<float, bf16, S>);
+  } else {
+    add(loss_forward_kernel<f16, S>);
+    add(loss_gradient_kernel<f16, f16, S>);
+    add(loss_gradient_kernel<bf16, bf16, S>);
+    add(loss_product_kernel<f16, f16, S>);
+    add(loss_product_kernel<bf16, bf16, S>);
+  }
   return r;
 }
 
@@ -977,7 +984,8 @@ int allow_lds() {
   const hipError_t e = once_per_device(g_large_lds, device, [] {
     hipError_t r = allow_shape<Large>();
     if (r == hipSuccess) r = allow_shape<Small>();
-    return r == hipSuccess ? allow_shape<Deep>() : r;
+    if (r == hipSuccess) r = allow_shape<Deep>();
+    return r == hipSuccess ? allow_shape<Triple>() : r;
   });
   ENC_HIP_TRY(e);
   return SIEVE_OK;
@@ -1017,19 +1025,23 @@ void finish(const float* x, int64_t rows, int64_t pitch, int64_t split, int spli
   loss_finish_kernel<F><<<(int)std::min<int64_t>(groups, 65536), 256, 0, s>>>(a);
 }
 
-// f(the shape)
-template <typename F>
-void by_shape(Size size, F f) {
-  if (size == kLarge) f(Large{});
-  else if (size == kDeep) f(Deep{});
-  else f(Small{});
+// f(the shape), for inputs of type F
+template <typename F, typename G>
+void by_shape(Size size, G f) {
+  if constexpr (std::is_same_v<F, float>) {
+    f(Triple{});
+  } else {
+    if (size == kLarge) f(Large{});
+    else if (size == kDeep) f(Deep{});
+    else f(Small{});
+  }
 }
 
 // Sets how a product is cut into tiles and splits.
 template <typename S>
 void cut(Product& p, int splits) {
   const int64_t each = (p.k + splits - 1) / splits;
-  p.per = (each + kStep - 1) / kStep * kStep;
+  p.per = (each + S::kStep - 1) / S::kStep * S::kStep;
   p.splits = splits;
   p.tiles_m = tiles_of(p.rows, S::BM);
   p.tiles_n = tiles_of(p.final.n, S::BN);
@@ -1078,7 +1090,6 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
     }
     a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
     a.k = l.k;
-    a.pairs = l.pairs;
     const MmOperand all_h = a.h;
     // a table that has to be packed is taken in pieces; any is, where a launch would be too large
     const bool as_is = direct(table, table_stride, n, dtype);
@@ -1088,7 +1099,7 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
       a.h.p = (const char*)all_h.p + t0 * all_h.stride * 2;
       a.h.rows = std::min(rows - t0, kRowChunk);
       a.t_first = t0;
-      const Size size = size_of(std::min(piece, vocab), a.h.rows, l.k * l.pairs);
+      const Size size = size_of(std::min(piece, vocab), a.h.rows, l.k, l.planes);
       const int side = kMeasured[size].bm;
       a.tiles_n = tiles_of(a.h.rows, kMeasured[size].bn);
       for (int64_t v0 = 0; v0 < vocab; v0 += piece) {
@@ -1098,7 +1109,7 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
         a.v_first = v0;
         a.tiles_m = tiles_of(vs, side);
         a.part = (Part*)(w + l.part) + v0 / side * a.h.rows;
-        by_shape(size, [&](auto shape) {
+        by_shape<F>(size, [&](auto shape) {
           typedef decltype(shape) S;
           loss_forward_kernel<T, S>
               <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
@@ -1160,7 +1171,6 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
       pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, l.weighed_planes, s, row,
               power);
     a.k = l.k;
-    a.pairs = l.pairs;
     set_scale(a, scale);
     a.targets = tg;
     a.lse = lse;
@@ -1168,14 +1178,14 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     a.g = w + l.g;
     a.g_stride = l.piece;
     a.g_plane = rows * l.piece;
-    const Size size = size_of(std::min(l.piece, vocab), rows, l.k * l.pairs);
+    const Size size = size_of(std::min(l.piece, vocab), rows, l.k, l.planes);
     for (int64_t v0 = 0; v0 < vocab; v0 += l.piece) {
       const int64_t vs = std::min(l.piece, vocab - v0);
       const bool last = v0 + vs == vocab;
       a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
                        w + l.w, s);
       a.v_first = v0;
-      by_shape(size, [&](auto shape) {
+      by_shape<F>(size, [&](auto shape) {
         typedef decltype(shape) S;
         a.tiles_m = tiles_of(vs, S::BM);
         a.tiles_n = tiles_of(rows, S::BN);
@@ -1186,14 +1196,14 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
       const Final final_h{dh, n, factor, nullptr, row};
       const Final final_w{(F*)dtable + v0 * n, n, factor, power, nullptr};
       ph.pitch = pw.pitch = l.k;
-      by_shape(l.spread.size, [&](auto shape) {
+      by_shape<F>(l.spread.size, [&](auto shape) {
         typedef decltype(shape) S;
         if (dh) {
           ph.a = {a.g, l.piece, rows, a.g_plane};
           ph.b = a.w;
           ph.b.rows = n;
           ph.k = vs;
-          ph.pairs = l.pairs;
+          ph.planes_b = 1;
           ph.rows = rows;
           ph.out = (float*)(w + l.dh);
           ph.split = rows * l.k;
@@ -1207,7 +1217,7 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
           pw.a = {a.g, l.piece, l.piece, a.g_plane};
           pw.b = {w + l.weighed, l.k, n, rows * l.k};
           pw.k = rows;
-          pw.pairs = l.weighed_pairs;
+          pw.planes_b = l.weighed_planes;
           pw.rows = vs;
           pw.out = (float*)(w + l.dw);
           pw.split = l.piece * l.k;

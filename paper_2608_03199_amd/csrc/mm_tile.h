@@ -4,8 +4,10 @@
 //   acc(m, n) = sum over k of A(m, k) B(n, k), in fp32
 //
 // Each operand lies in memory along k (its rows are m or n) or across it (its rows are k): no
-// operand is transposed in memory.  Values of 32 bits come as planes of 16-bit parts, and the
-// sum then runs over those pairs of planes whose product is above fp32's last bit.
+// operand is transposed in memory.  Values of more than 16 bits come as planes of 16-bit parts,
+// and the sum then takes those pairs of planes whose product is above fp32's last bit: three of
+// two planes, six of three.  A step's planes are in LDS together, so that each is read once for
+// all of its products.
 //
 // A work-group's waves share BM x BN values, in 32 x 32 tiles.  Steps along k go through LDS
 // buffers: while one is read, the loads of the next are on their way, straight into LDS.
@@ -41,11 +43,6 @@ struct MmOperand {
   int64_t rows;    // of m or n
   int64_t plane;   // values between planes
 };
-
-// Pairs of planes, smallest products first: all six for three planes, the last three for two,
-// the last for one.
-__device__ __forceinline__ int mm_plane_a(int i) { return (0x001102 >> (4 * i)) & 15; }
-__device__ __forceinline__ int mm_plane_b(int i) { return (0x010120 >> (4 * i)) & 15; }
 
 template <typename T>
 __device__ __forceinline__ mm_f32x16 mm_mfma(enc_u32x4 a, enc_u32x4 b, mm_f32x16 c) {
@@ -243,6 +240,18 @@ struct MmPatch {
     else
       __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), rsrc, (int)at, 0, 0);
   }
+  // A row's value v0 and the next row's v1 of every lane's column, two neighbours of a row a store:
+  // even lanes store the row's, odd ones the next row's.  at: of lane(row + odd, column - odd).
+  __device__ __forceinline__ void store_rows(uint32_t at, V v0, V v1) const {
+    static_assert(sizeof(V) == 2);
+    const bool odd = threadIdx.x & 1;
+    const uint32_t a = __builtin_bit_cast(uint16_t, v0), b = __builtin_bit_cast(uint16_t, v1);
+    // what the neighbour stores goes there, what this lane stores comes (quad_perm 1 0 3 2)
+    const uint32_t came = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(odd ? a : b), 0xb1, 0xf,
+                                                                0xf, true);
+    const uint32_t d = odd ? came | b << 16 : a | came << 16;
+    __builtin_amdgcn_raw_buffer_store_b32(d, rsrc, (int)at, 0, 0);
+  }
   // 4 neighbours of a row, at a multiple of 8 bytes
   __device__ __forceinline__ void store4(uint32_t at, const V (&v)[4]) const {
     static_assert(sizeof(V) == 2);
@@ -255,16 +264,17 @@ struct MmPatch {
 
 // WM x WN waves own BM x BN values at a time.  A work-group goes through its tiles as through one
 // long sum: the first steps of the next tile are on their way while a tile's epilogue runs.
+// kPlanes: of both operands, or 1, and then `planes_b` of B's in turn.
 template <typename T, int BM, int BN, bool kAcrossA, bool kAcrossB, int WM, int WN, int kStep,
-          int kStages>
+          int kStages, int kPlanes = 1>
 struct MmTile {
   static constexpr int kThreads = 64 * WM * WN;
   typedef MmStage<BM, kAcrossA, kStep, kThreads> A;
   typedef MmStage<BN, kAcrossB, kStep, kThreads> B;
   static constexpr int kI = BM / WM / 32, kJ = BN / WN / 32;
-  static constexpr int kStage = A::kBytes + B::kBytes;
+  static constexpr int kStage = kPlanes * (A::kBytes + B::kBytes);
   static constexpr int kLds = kStages * kStage;
-  static constexpr int kLoads = A::kLoads + B::kLoads;
+  static constexpr int kLoads = kPlanes * (A::kLoads + B::kLoads);
   mm_f32x16 acc[kI][kJ];
 
   // Register r of tile (i, j) of a wave holds row row0 + down(i, r) and column col0 + 32 j of the
@@ -278,23 +288,23 @@ struct MmTile {
   }
 
   const MmOperand &a, &b;
-  const int pairs;
+  const int planes_b;
   const uint32_t lds;
   A sa;
   B sb;
   MmWork ahead;     // the tile whose steps are being loaded, and where in it
   int64_t k;
-  int pair;
+  int plane;        // of B, the last one first; -1: nothing is left
   int buffer = 0;   // of the next step to be multiplied
   uint32_t a_at, b_at;
 
   // lds: the address of kLds bytes, a multiple of 1024, that nothing else uses.
-  __device__ __forceinline__ MmTile(const MmOperand& a_, const MmOperand& b_, int pairs_,
+  __device__ __forceinline__ MmTile(const MmOperand& a_, const MmOperand& b_, int planes_b_,
                                     uint32_t lds_)
-      : a(a_), b(b_), pairs(pairs_), lds(lds_) {
+      : a(a_), b(b_), planes_b(kPlanes == 1 ? planes_b_ : 1), lds(lds_) {
     const int wave_row = wave() / WN * (BM / WM), wave_col = wave() % WN * (BN / WN);
     a_at = lds + A::lane_at(wave_row);
-    b_at = lds + A::kBytes + B::lane_at(wave_col);
+    b_at = lds + kPlanes * A::kBytes + B::lane_at(wave_col);
     row0 = wave_row + (int)(threadIdx.x >> 5 & 1) * 4;
     col0 = wave_col + (int)(threadIdx.x & 31);
   }
@@ -304,19 +314,23 @@ struct MmTile {
   template <typename Next>
   __device__ __forceinline__ void load(int to, Next& next) {
     // past the last step nothing is there: the loads are counted all the same
-    const int left = pair < 6 ? (int)(ahead.k1 - k < kStep ? ahead.k1 - k : kStep) : 0;
-    const int p = pair < 6 ? pair : 5;
-    const int64_t at_a =
-        mm_plane_a(p) * a.plane + (kAcrossA ? k * a.stride + ahead.m0 : ahead.m0 * a.stride + k);
-    const int64_t at_b =
-        mm_plane_b(p) * b.plane + (kAcrossB ? k * b.stride + ahead.n0 : ahead.n0 * b.stride + k);
-    sa.load((const char*)a.p + at_a * 2, left, lds + to * kStage);
-    sb.load((const char*)b.p + at_b * 2, left, lds + to * kStage + A::kBytes);
-    if (pair == 6) return;
+    const bool there = plane >= 0;
+    const int left = there ? (int)(ahead.k1 - k < kStep ? ahead.k1 - k : kStep) : 0;
+    const int64_t at_a = kAcrossA ? k * a.stride + ahead.m0 : ahead.m0 * a.stride + k;
+    const int64_t at_b = (kAcrossB ? k * b.stride + ahead.n0 : ahead.n0 * b.stride + k) +
+                         (there ? plane : 0) * b.plane;
+    const uint32_t at = lds + to * kStage;
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) {
+      sa.load((const char*)a.p + (at_a + p * a.plane) * 2, left, at + p * A::kBytes);
+      sb.load((const char*)b.p + (at_b + p * b.plane) * 2, left,
+              at + kPlanes * A::kBytes + p * B::kBytes);
+    }
+    if (!there) return;
     k += kStep;
     if (k >= ahead.k1) {
       k = ahead.k0;
-      if (++pair == 6) begin(next);
+      if (--plane < 0) begin(next);
     }
   }
   template <typename Next>
@@ -326,14 +340,14 @@ struct MmTile {
       if (w.k0 >= w.k1) continue;  // no steps: see steps_of
       ahead = w;
       k = w.k0;
-      pair = 6 - pairs;
+      plane = planes_b - 1;
       sa.place(a, w.m0);
       sb.place(b, w.n0);
       return;
     }
   }
   __device__ __forceinline__ int steps_of(const MmWork& w) const {
-    return w.k1 > w.k0 ? (int)((w.k1 - w.k0 + kStep - 1) / kStep) * pairs : 0;
+    return w.k1 > w.k0 ? (int)((w.k1 - w.k0 + kStep - 1) / kStep) * planes_b : 0;
   }
 
   // Starts the loads of the first tile's first steps; the work-group has one at least.
@@ -341,7 +355,7 @@ struct MmTile {
   __device__ __forceinline__ void start(Next& next) {
     ahead = {0, 0, 0, 0};
     k = 0;
-    pair = 6;
+    plane = -1;
     sa.place(a, 0);
     sb.place(b, 0);
     begin(next);
@@ -365,15 +379,24 @@ struct MmTile {
       const uint32_t at = buffer * kStage;
 #pragma unroll
       for (int s = 0; s < kStep / 16; ++s) {
-        enc_u32x4 fa[kI], fb[kJ];
+        enc_u32x4 fa[kPlanes][kI], fb[kPlanes][kJ];
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) fb[j] = B::frag(b_at + at, j, s);
+        for (int p = 0; p < kPlanes; ++p) {
 #pragma unroll
-        for (int i = 0; i < kI; ++i) fa[i] = A::frag(a_at + at, i, s);
+          for (int j = 0; j < kJ; ++j) fb[p][j] = B::frag(b_at + at + p * B::kBytes, j, s);
 #pragma unroll
-        for (int i = 0; i < kI; ++i)
+          for (int i = 0; i < kI; ++i) fa[p][i] = A::frag(a_at + at + p * A::kBytes, i, s);
+        }
+        // the smallest products first
 #pragma unroll
-          for (int j = 0; j < kJ; ++j) acc[i][j] = mm_mfma<T>(fa[i], fb[j], acc[i][j]);
+        for (int both = kPlanes - 1; both >= 0; --both)
+#pragma unroll
+          for (int p = 0; p <= both; ++p)
+#pragma unroll
+            for (int i = 0; i < kI; ++i)
+#pragma unroll
+              for (int j = 0; j < kJ; ++j)
+                acc[i][j] = mm_mfma<T>(fa[p][i], fb[both - p][j], acc[i][j]);
       }
       buffer = buffer == kStages - 1 ? 0 : buffer + 1;
     }

@@ -36,20 +36,23 @@ typedef _Float16 f16;
 constexpr int kThreads = 256;
 // A work-group's tile: the usual one at two work-groups a CU; one for few tiles, which are bound
 // by the latency of their loads, with more of these on their way.
-template <int kSide_, int kStages>
+template <int kSide_, int kStep, int kStages, int kPlanes_>
 struct Shape {
-  static constexpr int kSide = kSide_;
+  static constexpr int kSide = kSide_, kPlanes = kPlanes_;
   template <bool kAcrossA, bool kAcrossB>
-  using Tile = MmTile<mm_f16, kSide, kSide, kAcrossA, kAcrossB, 2, 2, 64, kStages>;
+  using Tile = MmTile<mm_f16, kSide, kSide, kAcrossA, kAcrossB, 2, 2, kStep, kStages, kPlanes>;
   static constexpr int kLds = Tile<false, false>::kLds;
 };
-typedef Shape<128, 2> Usual;
-typedef Shape<64, 4> Few;
+// of both parts, and of the first alone
+typedef Shape<128, 32, 2, 2> Usual;
+typedef Shape<64, 32, 4, 2> Few;
+typedef Shape<128, 64, 2, 1> UsualPlain;
+typedef Shape<64, 64, 4, 1> FewPlain;
 constexpr float kScaleX = 16384.f, kScaleA = 4096.f;  // of X; of A and B
 constexpr double kMaxX = 3.9, kMaxA = 15.9;           // below 65504 times these
 constexpr int kMaxSide = 65536;
 constexpr int kMaxSteps = 1000;
-constexpr int kPlainSteps = 2;                        // of the last, for bfloat16
+constexpr int kPlainSteps = 1;                        // of the last, for bfloat16
 constexpr int kSums = 64;                             // parts of a matrix's sum of squares
 constexpr int64_t kFewTiles = 128;                    // of the usual shape
 constexpr int64_t kMostBytes = int64_t(1) << 31;      // of the workspace, for one matrix or more
@@ -152,7 +155,6 @@ struct Product {
   MmOperand a, b;        // of the first matrix
   int64_t a_next, b_next;
   int64_t k;
-  int pairs;             // of planes: 3, or 1 where the first parts are enough
   int64_t rows, cols;    // that are written: zeros past the matrix's, up to the pitch
   int64_t side;
   uint32_t tiles, tiles_m, tiles_n;  // tiles of a matrix
@@ -202,7 +204,7 @@ __global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
   MmOperand x = a.a, y = a.b;
   x.p = (const f16*)x.p + matrix * a.a_next;
   y.p = (const f16*)y.p + matrix * a.b_next;
-  Tile t(x, y, a.pairs,
+  Tile t(x, y, 1,
          (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_memory);
   bool first_one = true;
   auto next = [&](MmWork& to) {
@@ -230,6 +232,7 @@ __global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
     t.stop();
     return;
   }
+  const bool plain = S::kPlanes == 1;  // what is multiplied next has first parts alone, too
   const MmPatch<f16> hi((f16*)a.out + at, a.pitch, rows, cols);
   const MmPatch<f16> lo((f16*)a.out + a.plane + at, a.pitch, rows, cols);
   // A and B below the diagonal also go to the other side of it; tiles on it are whole
@@ -246,7 +249,8 @@ __global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
 #pragma unroll
   for (int j = 0; j < Tile::kJ; ++j) {
     const int col = t.col0 + 32 * j;
-    const auto lane = hi.lane(t.row0, col);
+    const int odd = (int)threadIdx.x & 1;
+    const auto lane = hi.lane(t.row0 + odd, col - odd);
     const int64_t gap = w.n0 + col - w.m0 - t.row0;  // rows down to the diagonal
     const int diagonal = w.n0 + col < a.side && gap >= 0 && gap < S::kSide ? (int)gap : -1;
 #pragma unroll
@@ -262,13 +266,17 @@ __global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
           else v *= 1.f / kScaleA;
           if constexpr (kKind == kPolynomial) v += d == diagonal ? a.fa * kScaleA : 0.f;
           split(v, h[e], l[e]);
-          const uint32_t o = hi.at(lane, d);
-          hi.store(o, h[e]);
-          lo.store(o, l[e]);
-          if constexpr (kKind == kGram) {
+          if constexpr (kKind == kGram)
             split(a.fc * v + (d == diagonal ? a.fb * kScaleA : 0.f), h3[e], l3[e]);
-            hi3.store(o, h3[e]);
-            lo3.store(o, l3[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const uint32_t o = hi.at(lane, Tile::down(i, 4 * g + e));
+          hi.store_rows(o, h[e], h[e + 1]);
+          if (!plain) lo.store_rows(o, l[e], l[e + 1]);
+          if constexpr (kKind == kGram) {
+            hi3.store_rows(o, h3[e], h3[e + 1]);
+            if (!plain) lo3.store_rows(o, l3[e], l3[e + 1]);
           }
         }
         if (mirrored) {
@@ -277,10 +285,10 @@ __global__ __launch_bounds__(kThreads, 2) void orth_product_kernel(Product a) {
           const uint32_t o = t.row0 + d < hi2.cols && col < hi2.rows
                                  ? ((uint32_t)col * hi2.pitch + t.row0 + d) * 2 : kMmNowhere;
           hi2.store4(o, h);
-          lo2.store4(o, l);
+          if (!plain) lo2.store4(o, l);
           if constexpr (kKind == kGram) {
             hi4.store4(o, h3);
-            lo4.store4(o, l3);
+            if (!plain) lo4.store4(o, l3);
           }
         }
       }
@@ -363,7 +371,7 @@ int check_orth(int64_t batch, int64_t m, int64_t n) {
   return SIEVE_OK;
 }
 
-static_assert(Usual::kLds <= 65536 && Few::kLds <= 65536, "no larger LDS has to be asked for");
+static_assert(std::max({Usual::kLds, Few::kLds, UsualPlain::kLds, FewPlain::kLds}) <= 65536, "no larger LDS has to be asked for");
 
 template <typename T>
 void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t m,
@@ -391,6 +399,7 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
   f16 *gram = (f16*)(w + l.gram), *second = (f16*)(w + l.second), *poly = (f16*)(w + l.poly);
   const MmOperand of_a{gram, sp, side, batch * square}, of_c{second, sp, side, batch * square},
       of_b{poly, sp, side, batch * square};
+  bool plain = false;  // the first parts alone
   // the product's kernel with tiles of the shape that it asks for
   auto launch = [&](Product p, auto kind, auto across_a, auto across_b) {
     constexpr int kKind = decltype(kind)::value;
@@ -405,7 +414,15 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
       orth_product_kernel<T, kKind, S, kA, kB><<<p.all, kThreads, S::kLds, s>>>(p);
     };
     const int64_t tiles = ((p.rows + 127) / 128) * ((p.cols + 127) / 128) * batch;
-    if (tiles / (kHalf ? 2 : 1) <= kFewTiles) with(Few{});
+    const bool few = tiles / (kHalf ? 2 : 1) <= kFewTiles;
+    if constexpr (std::is_same_v<T, bf16> && kKind != kUpdate) {  // kUpdate: never the last
+      if (plain) {
+        if (few) with(FewPlain{});
+        else with(UsualPlain{});
+        return;
+      }
+    }
+    if (few) with(Few{});
     else with(Usual{});
   };
   const std::integral_constant<bool, true> across;
@@ -416,7 +433,7 @@ void run(const void* g, int64_t batch_stride, int64_t row_stride, int64_t batch,
     const bool last = i == steps - 1;
     // A: over the longer side
     Product p{};
-    p.pairs = std::is_same_v<T, bf16> && steps - i <= kPlainSteps ? 1 : 3;
+    plain = steps - i <= kPlainSteps;
     p.a = p.b = {x, l.pitch, side, src.plane};
     p.a_next = p.b_next = m * l.pitch;
     p.k = tall ? m : n;
