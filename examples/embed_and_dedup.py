@@ -1,12 +1,14 @@
 """A text encoder trained on near-duplicate pairs, its embeddings, and their self-join.
 
-The library's operators as they are used together: documents of ragged lengths are packed, an
-encoder block runs layer norm and attention with a learned relative position bias over the
-packed batch, one query per document pools its tokens, a contrastive loss trains all of it on
-pairs of near duplicates, and the embedded corpus is loaded into an index and joined with itself
-at a threshold.  The matrix products around the operators are torch's.
+The library's operators as they are used together: documents of ragged lengths are packed, their
+tokens looked up in a table, an encoder block runs layer norm and attention with a learned
+relative position bias over the packed batch, one query per document pools its tokens, a
+contrastive loss (cross entropy of each document against all of the batch's others) trains all of
+it on pairs of near duplicates, and the embedded corpus is loaded into an index and joined with
+itself at a threshold.  The matrix products around the operators are torch's, and so is the
+optimizer, unless --orthogonal asks for orthogonalised momentum of the blocks' matrices.
 
-    python examples/embed_and_dedup.py [--docs 2000] [--steps 60]
+    python examples/embed_and_dedup.py [--docs 2000] [--steps 60] [--orthogonal]
 """
 import argparse
 import os
@@ -60,7 +62,7 @@ class Encoder(torch.nn.Module):
 
     def forward(self, batch):
         dt = self.dtype
-        h = self.embed.to(dt)[batch.tokens]
+        h = ps.embed(batch.tokens, self.embed, dtype=dt)
         bias = self.bias.to(dt)  # one table for all layers
         branch = torch.zeros_like(h)
         for p in self.layers:
@@ -93,18 +95,41 @@ def make_documents(count, generator):
     return docs
 
 
-def train(model, steps, pairs, generator, say=print):
-    opt = torch.optim.Adam(model.parameters(), lr=2e-3)
+class Orthogonal:
+    """Steps along the momentum of matrices, orthogonalised: those of one shape in one call."""
+
+    def __init__(self, matrices, lr=0.02, beta=0.9):
+        self.lr, self.beta, self.groups = lr, beta, {}
+        for p in matrices:
+            self.groups.setdefault(tuple(p.shape), []).append(p)
+        self.momentum = {shape: torch.zeros(len(ps_), *shape, device="cuda")
+                         for shape, ps_ in self.groups.items()}
+
+    @torch.no_grad()
+    def step(self):
+        for shape, params in self.groups.items():
+            m = self.momentum[shape]
+            m.mul_(self.beta).add_(torch.stack([p.grad for p in params]))
+            rate = self.lr * max(1.0, shape[1] / shape[0]) ** 0.5
+            for p, x in zip(params, ps.orthogonalize(m)):
+                p.sub_(x, alpha=rate)
+
+
+def train(model, steps, pairs, generator, say=print, orthogonal=False):
+    matrices = [p for p in model.layers.parameters() if p.dim() == 2] if orthogonal else []
+    rest = [p for p in model.parameters() if all(p is not q for q in matrices)]
+    opt = torch.optim.Adam(rest, lr=2e-3)
+    matrix_opt = Orthogonal(matrices)
+    target = torch.arange(pairs, device="cuda")
     losses = []
     for step in range(steps):
         batch = Batch(make_documents(2 * pairs, generator), model.dtype)
         e = model(batch)
-        score = e[0::2] @ e[1::2].T / 0.05
-        target = torch.arange(pairs, device="cuda")
-        loss = torch.nn.functional.cross_entropy(score, target)
-        opt.zero_grad()
+        loss = ps.linear_cross_entropy(e[0::2], e[1::2], target, 1 / 0.05).mean()
+        model.zero_grad()
         loss.backward()
         opt.step()
+        matrix_opt.step()
         losses.append(float(loss.detach()))
         if step % 20 == 0 or step == steps - 1:
             say(f"step {step}: loss {losses[-1]:.4f}")
@@ -147,11 +172,12 @@ def main(argv=None):
     args.add_argument("--steps", type=int, default=60)
     args.add_argument("--pairs", type=int, default=128)
     args.add_argument("--tau", type=float, default=0.8)
+    args.add_argument("--orthogonal", action="store_true")
     args = args.parse_args(argv)
     torch.manual_seed(0)
     g = torch.Generator().manual_seed(1)
     model = Encoder()
-    losses = train(model, args.steps, args.pairs, g)
+    losses = train(model, args.steps, args.pairs, g, orthogonal=args.orthogonal)
     docs = make_documents(args.docs // 2 * 2, g)
     found, _ = self_join(embed(model, docs), args.tau)
     partner = torch.arange(len(docs), device="cuda") ^ 1
