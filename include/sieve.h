@@ -322,8 +322,9 @@ SIEVE_API int sieve_round_log(const sieve_index* idx, sieve_round* out, int32_t 
  * The vectors of an index are rows that a text encoder wrote, and tau separates
  * near duplicates only for an encoder trained to do so.  These are the encoder's
  * own operators over a packed batch of documents, for embedding a corpus and for
- * training: layer norm, and attention with a learned relative position bias, each
- * with its backward pass.
+ * training: layer norm, attention with a learned relative position bias, rows of a
+ * token table, and the cross entropy against a table of vectors, each with its
+ * backward pass; and the orthogonalised update of a layer's matrices.
  *
  * They follow the conventions above (argument checks before any HIP call, errors
  * leave the outputs untouched, device pointers), with three differences:
@@ -541,7 +542,8 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
 
 /*
  * sieve_loss_backward -- gradients of sieve_loss_forward.  With p_tv = exp(s_tv - lse_t) and
- * g_tv = (p_tv - [v = target_t]) * dloss_t (rounded to dtype for the products),
+ * g_tv = (p_tv - [v = target_t]) * dloss_t (rounded to dtype for the products, relative to
+ * the row's 1 - p at its target),
  *   dh_t = scale * sum_v g_tv table_v,  dtable_v = scale * sum_t g_tv h_t
  *   dloss        [rows] fp32: the gradient of each row's loss.  A row with dloss = 0 is left
  *                out, as one without a target is.

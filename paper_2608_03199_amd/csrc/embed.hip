@@ -16,6 +16,13 @@
 // A frequent token would leave one row with most of the work, so runs of equal numbers are
 // summed ahead in pieces: a piece of 32 sorted places that holds one number alone is summed by
 // itself, so is a piece of 32 such pieces, and so on.  A row then adds up to 62 of each kind.
+//
+// A row moves 16 bytes a thread, wherever it lies.  Measured: 262,144 rows of 768 f16 are written
+// in 117 us, 3.9 TB/s.  65,536 x 1,024 bf16 of a table of 50,000 fp32 rows: forward 49 us; backward
+// 15 us a pass of the sort, 16 for the runs and 91 for the rows, of which what they read
+// and write, 339 MB, takes 69 at the rate of a copy.
+#include <algorithm>
+
 #include "enc_common.h"
 
 using namespace sieve;
@@ -132,7 +139,8 @@ constexpr int kTile = kThreads * kRounds;     // pairs of a work-group
 constexpr int kWaves = kThreads / 64;
 constexpr int kEach = kBins / kThreads;       // bins of a thread
 // Up to so many counts a thread every tile adds them up by itself; more go through a kernel of
-// their own, another launch.
+// their own, another launch.  65,536 tokens, 8,000 rows, 32 counts a thread: 54 us for 60 with the
+// kernel; 20,001 tokens, 2,000 rows, 80: 59 us without it for 43.
 constexpr int kFewCounts = 64;
 inline __host__ __device__ bool few_counts(int tiles, int bins) {
   return tiles * ((bins + kThreads - 1) / kThreads) <= kFewCounts;
@@ -323,6 +331,9 @@ __global__ __launch_bounds__(kThreads) void sort_place_kernel(Pass a) {
 
 // ---- backward --------------------------------------------------------------------------------
 
+// 65,536 x 1,024 bf16, 50,000 rows, the rows' kernel with four values ahead: 105 us; with runs of
+// 64 it takes 124, with 16 it is 8% shorter but more kinds of pieces are launched; with 8 rows a
+// work-group 125, with 4 148, with 32 no less.
 constexpr int kRun = 32;       // places of a piece, pieces of a piece of the next kind
 constexpr int kKinds = 6;      // 32^6 places are more than kMaxCount
 constexpr int kMaxRows = 16;   // table rows of a work-group
@@ -351,7 +362,8 @@ struct Sum {
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = 0.f;
   }
-  // Adds load(i) for i = 0 .. count - 1, in order, kAhead of them on their way at a time.
+  // Adds load(i) for i = 0 .. count - 1, in order, kAhead of them on their way at a time: 8 values
+  // of 16 bits twice, 91 us where one takes 101 and four 105 (as above).
   static constexpr int kAhead = 16 / E;
   template <typename F>
   __device__ __forceinline__ void all(int count, F load) {
@@ -578,12 +590,15 @@ void backward_typed(EmbedBwd a, hipStream_t s) {
   int64_t span = 1;
   for (int kind = 1; kind <= a.kinds; ++kind) {
     span *= kRun;
-    embed_pieces_kernel<T, E, kWhole><<<grid_of((a.count / span + groups - 1) / groups), kThreads, 0, s>>>(
-        a, kind, span);
+    const int grid = grid_of((a.count / span + groups - 1) / groups);
+    embed_pieces_kernel<T, E, kWhole><<<grid, kThreads, 0, s>>>(a, kind, span);
   }
-  const int64_t want = a.vocab / 2048;
-  a.rows = want < 1 ? 1 : want < kMaxRows ? (int)want : kMaxRows;  // few in a small table
-  embed_rows_kernel<T, W, E, kWhole><<<grid_of((a.vocab + a.rows - 1) / a.rows), kThreads, 0, s>>>(a);
+  // few in a small table, 2,000 x 515 fp32: 43 us for 81 with 16; but one a group of threads,
+  // 65,536 tokens of 8,000 x 256 bf16: 45 us for 54 with 3 rows, which leave half of them idle
+  const int64_t want = std::max<int64_t>(a.vocab / 2048, groups);
+  a.rows = (int)std::min<int64_t>(want, kMaxRows);
+  const int grid = grid_of((a.vocab + a.rows - 1) / a.rows);
+  embed_rows_kernel<T, W, E, kWhole><<<grid, kThreads, 0, s>>>(a);
 }
 
 }  // namespace

@@ -16,6 +16,9 @@
 // row by the row's number so that the reads below touch every bank equally:
 //   along k: a step's values a row; a read takes one piece of each of 32 rows;
 //   across k: 2 BM bytes a row; a transposing read takes 4 rows by 16 columns a quarter wave.
+//
+// 8,192^3 bf16, both along k, 256 x 256 tiles, steps of 64, two buffers: 891 us, 1,234 TFLOP/s
+// (with 256 x 128, steps of 32 and three buffers 1,189 us).
 #pragma once
 
 #include <type_traits>
