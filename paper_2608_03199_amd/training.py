@@ -197,16 +197,16 @@ def _loss_inputs(h, table, targets):
 def _loss_forward(h, table, targets, scale):
     lib = _library()
     hr, h_stride, tr, t_stride, code, rows, vocab, n, tg, size = _loss_inputs(h, table, targets)
-    out = h.new_empty((2,) + targets.shape, dtype=torch.float32)
+    # not of one allocation: a caller may change the losses where they are, and lse is kept
+    loss, lse = (h.new_empty(targets.shape, dtype=torch.float32) for _ in range(2))
     need = lib.sieve_loss_workspace(rows, vocab, n, code, 0)
     space = _workspace(lib, need, h.device)
     if rows:
-        at = out.data_ptr()
         _check(lib, lib.sieve_loss_forward(hr.data_ptr(), h_stride, tr.data_ptr(), t_stride, code,
-                                           rows, vocab, n, tg.data_ptr(), size, scale, at,
-                                           at + 4 * rows, _ptr(space), need,
+                                           rows, vocab, n, tg.data_ptr(), size, scale,
+                                           loss.data_ptr(), lse.data_ptr(), _ptr(space), need,
                                            _raw_stream(h.device)))
-    return out[0], out[1]
+    return loss, lse
 
 
 def linear_cross_entropy_backward(dloss: torch.Tensor, h: torch.Tensor, table: torch.Tensor,

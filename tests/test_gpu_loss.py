@@ -255,6 +255,19 @@ def test_loss_autograd_streams_and_graph(ps):
         assert all(torch.equal(x, y) for x, y in zip(held, want)), k
 
 
+def test_loss_weighted_in_place(ps):
+    """The losses are the caller's: what becomes of them touches nothing that the backward pass
+    reads."""
+    h, table, targets, dloss = _inputs(40, 300, 64, torch.float32, 17)
+    val, tol = cross_entropy(h, table, targets, 1.0, dloss)
+    a, b = h.cuda().requires_grad_(), table.cuda().requires_grad_()
+    loss = ps.linear_cross_entropy(a, b, targets.cuda())
+    loss.mul_(dloss.cuda())
+    loss.sum().backward()
+    check("dh", a.grad, val["dh"], tol["dh"])
+    check("dtable", b.grad, val["dtable"], tol["dtable"])
+
+
 def test_loss_against_differences(ps):
     """The summed loss's change along a direction against the gradients.  The step's truncation
     error is the oracle's at the same step; a loss is off by at most its bound."""
