@@ -450,16 +450,19 @@ __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedBwd a) {
   for (int64_t v0 = (int64_t)blockIdx.x * a.rows; v0 < a.vocab;
        v0 += (int64_t)gridDim.x * a.rows) {
     __syncthreads();  // the rows before have been read
-    if (threadIdx.x <= a.rows) {
-      // the first place whose number is not below v0 + threadIdx.x
-      const int64_t v = v0 + threadIdx.x;
-      int64_t lo = 0, hi = a.count;
+    if (threadIdx.x < 8 * (a.rows + 1)) {
+      // the first place whose number is not below v, which is one of lo .. hi: 8 threads look at 8
+      // places at a time, of which the first c hold numbers below it
+      const int64_t v = v0 + threadIdx.x / 8;
+      uint32_t lo = 0, hi = (uint32_t)a.count;
       while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if ((int64_t)a.key[mid] < v) lo = mid + 1;
-        else hi = mid;
+        const uint32_t step = (hi - lo + 8) / 9, at = lo + (threadIdx.x % 8 + 1) * step - 1;
+        const uint64_t below = __ballot(at < hi && (int64_t)a.key[at] < v);
+        const uint32_t c = __popc((uint32_t)(below >> (threadIdx.x & 56)) & 255u);
+        if (c < 8) hi = min(hi, lo + (c + 1) * step - 1);
+        lo += c * step;
       }
-      s_begin[threadIdx.x] = lo;
+      if (threadIdx.x % 8 == 0) s_begin[threadIdx.x / 8] = lo;
     }
     __syncthreads();
     for (int r = threadIdx.x / a.group; r < a.rows && v0 + r < a.vocab; r += kThreads / a.group) {
