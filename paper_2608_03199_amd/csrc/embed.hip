@@ -19,7 +19,7 @@
 //
 // A row moves 16 bytes a thread, wherever it lies.  Measured: 262,144 rows of 768 f16 are written
 // in 117 us, 3.9 TB/s.  65,536 x 1,024 bf16 of a table of 50,000 fp32 rows: forward 49 us; backward
-// 15 us a pass of the sort, 16 for the runs and 91 for the rows, of which what they read
+// 15 us a pass of the sort, 16 for the runs and 85 for the rows, of which what they read
 // and write, 339 MB, takes 69 at the rate of a copy.
 #include <algorithm>
 
@@ -363,7 +363,7 @@ struct Sum {
     for (int j = 0; j < E; ++j) v[j] = 0.f;
   }
   // Adds load(i) for i = 0 .. count - 1, in order, kAhead of them on their way at a time: 8 values
-  // of 16 bits twice, 91 us where one takes 101 and four 105 (as above).
+  // of 16 bits twice, 91 us where one takes 101 and four 105 (as above, with rows found by halves).
   static constexpr int kAhead = 16 / E;
   template <typename F>
   __device__ __forceinline__ void all(int count, F load) {
@@ -452,7 +452,8 @@ __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedBwd a) {
     __syncthreads();  // the rows before have been read
     if (threadIdx.x < 8 * (a.rows + 1)) {
       // the first place whose number is not below v, which is one of lo .. hi: 8 threads look at 8
-      // places at a time, of which the first c hold numbers below it
+      // places at a time, of which the first c hold numbers below it: this kernel takes 20.8 us at
+      // 20,001 x 515 fp32 and 85 at 65,536 x 1,024 bf16, by halves 23.6 and 91
       const int64_t v = v0 + threadIdx.x / 8;
       uint32_t lo = 0, hi = (uint32_t)a.count;
       while (lo < hi) {
