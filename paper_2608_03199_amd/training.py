@@ -1,10 +1,15 @@
-"""Operators of libsieve around a text encoder's blocks: the table's lookup, and the cross entropy of
-hidden states against a table, each with its gradient; and the orthogonalised update of the
+"""Operators of libsieve around a text encoder's blocks: the table's lookup, and the cross entropy
+of hidden states against a table, each with its gradient; and the orthogonalised update of the
 matrices between them (``include/sieve.h``).
 
 As in ``encoder.py``, the ``*_forward`` / ``*_backward`` functions marshal the arguments of the
 library's calls, the others join them for torch's autograd, all calls are asynchronous on the
 given or current stream, and there is no CPU fallback.
+
+Into a graph, capture the ``*_forward`` / ``*_backward`` functions.  A backward pass of torch's own
+is captured only where no result of an eager pass over the same parameters is alive: what
+accumulates their gradients would still belong to the eager pass's stream, which ends the
+process.
 """
 from __future__ import annotations
 
