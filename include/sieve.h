@@ -543,7 +543,8 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
 /*
  * sieve_loss_backward -- gradients of sieve_loss_forward.  With p_tv = exp(s_tv - lse_t) and
  * g_tv = (p_tv - [v = target_t]) * dloss_t (rounded to dtype for the products, relative to
- * the row's 1 - p at its target),
+ * the row's 1 - p at its target, or to what rounding may leave of that in fp32; a finite one
+ * stays finite),
  *   dh_t = scale * sum_v g_tv table_v,  dtable_v = scale * sum_t g_tv h_t
  *   dloss        [rows] fp32: the gradient of each row's loss.  A row with dloss = 0 is left
  *                out, as one without a target is.

@@ -23,7 +23,8 @@
 // g is rounded once, to the inputs' type, and what its target has outweighs the rest of its row:
 // g_t,target = -(1 - p_t) dloss_t.  A rounding of it would be the same for every token of a
 // frequent word and add up over them, so each row is divided by c_t = 1 - p_t first, from a dot
-// product of its own: its target's value is then -1, and the others are at most 1 together.
+// product of its own: its target's value is then -1, and the others are at most 1 together (or less,
+// where 1 - p_t is below what rounding may leave of it: c_t is never less than that).
 // dloss_t c_t is a row's exact factor of dh; in dw's product it goes with h, where its rounding is
 // another one for each value and column.  binary16 does not have fp32's range: there g is scaled
 // by 2^14, and h's factors by a power of two that brings the largest below 1.
@@ -56,6 +57,7 @@ constexpr int64_t kPieceValues = 1 << 27;  // of g
 constexpr int64_t kMaxPiece = 65536;       // vectors
 constexpr int64_t kRowChunk = 65536;       // rows of h in one launch of the forward pass
 constexpr float kHalfScale = 16384.f;      // what g in binary16 is scaled by
+constexpr float kMostHalf = 65504.f;       // binary16's largest value
 
 // A work-group's tile.  A large one has a CU to itself and eight waves; two small ones share it;
 // deep ones are as small, with eight waves and more loads on their way, for launches of no more
@@ -420,21 +422,31 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(Rows a) {
     if (target >= 0 && d != 0.f) {
       const F* h = (const F*)a.h + row * a.h_stride;
       const F* w = (const F*)a.table + target * a.t_stride;
-      float dot = 0.f;
+      float dot = 0.f, size = 0.f;
       for (int col = lane * E; col < a.n; col += 64 * E) {
         if constexpr (E > 1) {
           const EncVec<F, E> x = enc_load<F, E>(h + col), y = enc_load<F, E>(w + col);
 #pragma unroll
-          for (int j = 0; j < E; ++j) dot = fmaf((float)x.v[j], (float)y.v[j], dot);
+          for (int j = 0; j < E; ++j) {
+            dot = fmaf((float)x.v[j], (float)y.v[j], dot);
+            size = fmaf(fabsf((float)x.v[j]), fabsf((float)y.v[j]), size);
+          }
         } else {
           dot = fmaf((float)h[col], (float)w[col], dot);
+          size = fmaf(fabsf((float)h[col]), fabsf((float)w[col]), size);
         }
       }
 #pragma unroll
-      for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
+      for (int o = 32; o; o >>= 1) {
+        dot += __shfl_xor(dot, o);
+        size += __shfl_xor(size, o);
+      }
       const float logit = dot * a.scale, lse = a.lse[row];
-      // 1 - p, but no less than what rounding leaves of it: the others of the row may be as much
-      const float least = 0x1p-20f * (4.f + fabsf(logit) + fabsf(lse));
+      // 1 - p, but no less than what rounding leaves of it, as the row's g may be as much: this sum
+      // of n products, and the matrix units' in another order, are each off by up to
+      // n 2^-24 sum |h w|, which is far above |logit| where large products cancel
+      const float least = 0x1p-20f * (4.f + fabsf(logit) + fabsf(lse)) +
+                          0x1p-23f * (float)a.n * size * a.scale;
       const float c = fmaxf(-expm1f(logit - lse), least);
       r = {1.f / c, c * d};
     }
@@ -587,6 +599,13 @@ __global__ __launch_bounds__(S::kThreads, 2) void loss_gradient_kernel(Logits a)
         // a row without a factor gives nothing, whatever it holds
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] = inverse[j] == 0.f ? 0.f : x[r] * inverse[j];
+        if constexpr (std::is_same_v<F, f16>) {
+          // up to 4 times c fit; logits that are good to no more than that give no infinities, but
+          // a row that is not a number stays one (its lse is not one, either)
+          const float most = fmaf(inverse[j], 0.f, kMostHalf);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_fmed3f(x[r], -most, most);
+        }
         // pairs of 16-bit values; halves of a wave change places so that each lane has 8
         // neighbours
 #pragma unroll
