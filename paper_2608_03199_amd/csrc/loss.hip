@@ -444,10 +444,11 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(Rows a) {
       const float logit = dot * a.scale, lse = a.lse[row];
       // 1 - p, but no less than what rounding leaves of it, as the row's g may be as much: this sum
       // of n products, and the matrix units' in another order, are each off by up to
-      // n 2^-24 sum |h w|, which is far above |logit| where large products cancel
+      // n 2^-24 sum |h w|, which is far above |logit| where large products cancel.  g is at most 1 in
+      // any case: of a logit that is infinite, too
       const float least = 0x1p-20f * (4.f + fabsf(logit) + fabsf(lse)) +
                           0x1p-23f * (float)a.n * size * a.scale;
-      const float c = fmaxf(-expm1f(logit - lse), least);
+      const float c = fmaxf(-expm1f(logit - lse), fminf(least, 1.f));
       r = {1.f / c, c * d};
     }
     if (lane == 0) a.to[row] = r;

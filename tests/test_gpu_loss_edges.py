@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from encoder_reference import check
+from encoder_reference import UNIT, check
 from test_gpu_loss import DTYPES, _inputs, _rnd, _run, ps  # noqa: F401
 from training_reference import cross_entropy
 
@@ -47,3 +47,54 @@ def test_loss_of_rows_that_are_not_numbers_in_any_type(ps, dtype, bad):  # noqa:
     got = _run(ps, h, table, targets, dloss)
     for name in ("loss", "lse", "dh", "dtable"):
         assert got[name].isnan().all(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_loss_that_is_infinite(ps, dtype, rows):  # noqa: F811
+    """A target whose logit lies below fp32's range: its loss is infinite, and the row's gradients
+    are those of a probability of 0."""
+    h, table, targets, dloss = _inputs(rows, 200, 64, DTYPES[dtype], 22, left_out=0.0)
+    t = int(targets[0])
+    table[:, 0], h[:, 0] = 0.0, 0.0
+    h[0, 0], table[t, 0] = 2.0 ** 66, -2.0 ** 66
+    got = _run(ps, h, table, targets, dloss)
+    # a logit of some -256 has no probability either, and the first column of dh, which no other
+    # vector has a part in, is then 2^124 times smaller
+    near_ = table.clone()
+    near_[t, 0] = -2.0 ** -58
+    val, tol = cross_entropy(h, near_, targets, 1.0, dloss)
+    val["loss"][0] = math.inf
+    val["dh"][:, 0] *= 2.0 ** 124
+    tol["dh"][:, 0] *= 2.0 ** 124
+    for name in val:
+        check(name, got[name], val[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("scale", [1.0, 1000.0, 2.0 ** 14])
+def test_loss_of_logits_far_apart(ps, dtype, scale):  # noqa: F811
+    """Whole numbers, whose logits are exact in fp32: with all others at least 64 below a row's
+    largest logit, its gradient is that of the difference of two vectors."""
+    g, rnd = _rnd(23)
+    h = torch.randint(-3, 4, (50, 16), generator=g).float()
+    table = torch.randint(-3, 4, (90, 16), generator=g).float() * 64
+    dot = h @ table.t()
+    top = dot.argmax(1)
+    targets = torch.randint(90, (50,), generator=g)
+    only = ((dot == dot.max(1, keepdim=True).values).sum(1) == 1) & (targets != top)
+    assert int(only.sum()) > 40
+    dt = DTYPES[dtype]
+    dloss = torch.full((50,), 1 / scale)
+    got = _run(ps, h.to(dt), table.to(dt), torch.where(only, targets, -100), dloss, scale)
+    c = only[:, None].double() * scale * float(dloss[0])
+    # an exponential is good to 2^-20, g is rounded to dt, and so is the gradient
+    off = UNIT[dt] + 2.0 ** -19
+    a, b = table[top].double() * c, table[targets].double() * c
+    check("dh", got["dh"], a - b, UNIT[dt] * (a - b).abs() + off * (a.abs() + b.abs()) + 1e-20)
+    want, size = torch.zeros(90, 16).double(), torch.zeros(90, 16).double()
+    for to, sign in ((top, 1), (targets, -1)):
+        want.index_add_(0, to, sign * h.double() * c)
+        size.index_add_(0, to, h.double().abs() * c)
+    # h times its row's factor is rounded, too
+    check("dtable", got["dtable"], want, (UNIT[dt] + off) * size + UNIT[dt] * want.abs() + 1e-20)
