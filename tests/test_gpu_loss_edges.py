@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from encoder_reference import UNIT, check
+from encoder_reference import E, UNIT, check
 from test_gpu_loss import DTYPES, _inputs, _rnd, _run, ps  # noqa: F401
 from training_reference import cross_entropy
 
@@ -98,3 +98,30 @@ def test_loss_of_logits_far_apart(ps, dtype, scale):  # noqa: F811
         size.index_add_(0, to, h.double().abs() * c)
     # h times its row's factor is rounded, too
     check("dtable", got["dtable"], want, (UNIT[dt] + off) * size + UNIT[dt] * want.abs() + 1e-20)
+
+
+@pytest.mark.parametrize("v", [1 + 2.0 ** -7 - 2.0 ** -23, 2 - 2.0 ** -23, 1 + 2.0 ** -8,
+                               1 + 2.0 ** -8 + 2.0 ** -16 - 2.0 ** -23, -1.7182817, 1.5])
+def test_loss_of_values_that_fill_their_bits(ps, v):  # noqa: F811
+    """One product of two fp32 values: the parts left out are at most 2^-24 of it (two products of
+    parts of 2^-8 and 2^-17), those kept are added in fp32 with one rounding of the size of the
+    sum, cut off at the worst (2^-23), and another below 2^-24."""
+    h = torch.tensor([v, 1 + 2.0 ** -7 - 2.0 ** -23, 1.1, 3.3333333, -1.0]).repeat(8)[:, None]
+    for w in (v, 1 + 2.0 ** -7 - 2.0 ** -23, 2.0 ** -100 * 1.7182817):
+        table = torch.tensor([[w]])
+        w = float(table)
+        _, lse = ps.linear_cross_entropy_forward(h.cuda(), table.cuda(),
+                                                 torch.zeros(40, dtype=torch.int64).cuda())
+        val = h[:, 0].double() * w
+        check("lse", lse, val, 4 * E * val.abs())
+
+
+def test_loss_of_the_largest_values(ps):  # noqa: F811
+    """No part of a value is past the range that the value is in."""
+    top = float(torch.finfo(torch.float32).max)
+    h = torch.tensor([top, -top, top * (1 - 2.0 ** -9), 1.0]).repeat(10)[:, None]
+    table = torch.tensor([[2.0 ** -120]])
+    _, lse = ps.linear_cross_entropy_forward(h.cuda(), table.cuda(),
+                                             torch.zeros(40, dtype=torch.int64).cuda())
+    val = h[:, 0].double() * 2.0 ** -120
+    check("lse", lse, val, 4 * E * val.abs())
