@@ -10,8 +10,8 @@
 //
 // Backward: the logits are computed again, a piece of the vocabulary at a time; the piece's g is
 // rounded to 16 bits and kept until both gradients' products have read it (a workspace of at most
-// 2^27 values, which the last-level cache holds for the most part).  dw of the piece is then
-// complete; dh is summed in fp32 over the pieces.
+// 2^27 values, which the last-level cache holds for the most part: beyond 2^19 rows, a piece of the
+// rows at a time, too).  dw of the piece is then complete; dh is summed in fp32 over the pieces.
 //
 // The matrix units bound all of it: 2 rows vocab n operations for the loss, 6 for the gradients.
 //
@@ -866,6 +866,7 @@ Spread spread_of(int64_t mh, int64_t kh, int64_t mw, int64_t kw, int64_t n, int 
 
 struct Layout {
   int64_t piece;                 // vectors of a piece, a multiple of 256
+  int64_t chunk;                 // rows that g is kept of at a time, in the backward pass
   int64_t k;                     // n, up to the next multiple of 8
   int planes;
   int weighed_planes;            // of h in dw's product
@@ -877,8 +878,10 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
   Layout l{};
   l.planes = dtype == SIEVE_F32 ? 3 : 1;
   l.k = (n + 7) & ~7;
-  int64_t piece = std::min(kPieceValues / (l.planes * std::max<int64_t>(rows, 1)), kMaxPiece);
-  piece = std::max<int64_t>(piece & ~int64_t(255), 256);
+  // as many as leave a piece its 256 vectors
+  l.chunk = std::min(std::max<int64_t>(rows, 1), kPieceValues / (l.planes * 256) & ~int64_t(255));
+  int64_t piece = std::min(kPieceValues / (l.planes * l.chunk), kMaxPiece);
+  piece = piece & ~int64_t(255);
   l.piece = std::min(piece, round256(vocab));
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -901,8 +904,8 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
     // most (2^31 products: 4 us), what that loses is a plane of its own
     const bool few = dtype != SIEVE_F32 && rows * vocab <= (int64_t(1) << 31) / n;
     l.weighed_planes = few ? 2 : l.planes;
-    l.spread = spread_of(rows, vs, vs, few ? 2 * rows : rows, n, l.planes);
-    l.g = take(rows * l.piece * 2 * l.planes);
+    l.spread = spread_of(l.chunk, vs, vs, few ? 2 * l.chunk : l.chunk, n, l.planes);
+    l.g = take(l.chunk * l.piece * 2 * l.planes);
     l.weighed = take(rows * l.k * 2 * l.weighed_planes);
     l.row = take(rows * (int64_t)sizeof(Row));
     l.largest = take(kMostLargest * 4);
@@ -1200,75 +1203,83 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
       loss_rows_kernel<F, 1><<<groups, 256, 0, s>>>(r);
     if (power) loss_power_kernel<<<1, 256, 0, s>>>((const float*)(w + l.largest), groups, power);
     Logits a{};
-    a.h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
+    const MmOperand all_h = operand<F>(h, h_stride, rows, n, dtype, l.k, w + l.h, s);
     if (dtable)
       pack<F>(h, h_stride, rows, n, l.k, w + l.weighed, rows * l.k, l.weighed_planes, s, row,
               power);
     a.k = l.k;
     set_scale(a, scale);
-    a.targets = tg;
-    a.lse = lse;
-    a.row = row;
     a.g = w + l.g;
     a.g_stride = l.piece;
-    a.g_plane = rows * l.piece;
-    const Size size = size_of(std::min(l.piece, vocab), rows, l.k, l.planes);
+    a.g_plane = l.chunk * l.piece;
+    const Size size = size_of(std::min(l.piece, vocab), l.chunk, l.k, l.planes);
+    const Final final_h{dh, n, factor, nullptr, row};
+    float *sums_h = (float*)(w + l.dh), *sums_w = (float*)(w + l.dw);
+    // sums of splits, and dh's over the pieces, dw's over the chunks: else the gradient itself
+    const bool sum_h = l.piece < vocab || l.spread.splits_h > 1;
+    const bool sum_w = l.chunk < rows || l.spread.splits_w > 1;
     for (int64_t v0 = 0; v0 < vocab; v0 += l.piece) {
       const int64_t vs = std::min(l.piece, vocab - v0);
-      const bool last = v0 + vs == vocab;
       a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
                        w + l.w, s);
       a.v_first = v0;
-      by_shape<F>(size, [&](auto shape) {
-        typedef decltype(shape) S;
-        a.tiles_m = tiles_of(vs, S::BM);
-        a.tiles_n = tiles_of(rows, S::BN);
-        loss_gradient_kernel<F, T, S>
-            <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
-      });
-      Product ph{}, pw{};
-      const Final final_h{dh, n, factor, nullptr, row};
       const Final final_w{(F*)dtable + v0 * n, n, factor, power, nullptr};
-      ph.pitch = pw.pitch = l.k;
-      by_shape<F>(l.spread.size, [&](auto shape) {
-        typedef decltype(shape) S;
-        if (dh) {
-          ph.a = {a.g, l.piece, rows, a.g_plane};
-          ph.b = a.w;
-          ph.b.rows = n;
-          ph.k = vs;
-          ph.planes_b = 1;
-          ph.rows = rows;
-          ph.out = (float*)(w + l.dh);
-          ph.split = rows * l.k;
-          ph.add = v0 > 0;
-          ph.final = final_h;
-          cut<S>(ph, l.spread.splits_h);
-          // the gradient itself, where nothing is to be added
-          if (vs < vocab || ph.splits > 1) ph.final.out = nullptr;
-        }
-        if (dtable) {
-          pw.a = {a.g, l.piece, l.piece, a.g_plane};
-          pw.b = {w + l.weighed, l.k, n, rows * l.k};
-          pw.k = rows;
-          pw.planes_b = l.weighed_planes;
-          pw.rows = vs;
-          pw.out = (float*)(w + l.dw);
-          pw.split = l.piece * l.k;
-          pw.final = final_w;
-          cut<S>(pw, l.spread.splits_w);
-          if (pw.splits > 1) pw.final.out = nullptr;
-        }
-        const uint64_t tiles = (uint64_t)ph.tiles_m * ph.tiles_n * ph.splits +
-                               (uint64_t)pw.tiles_m * pw.tiles_n * pw.splits;
-        loss_product_kernel<F, T, S>
-            <<<mm_grid(tiles, S::kMost), S::kThreads, S::kLds, s>>>(ph, pw);
-      });
-      if (dtable && !pw.final.out)
-        finish<F>(pw.out, vs, l.k, pw.split, pw.splits, final_w, s);
-      if (dh && !ph.final.out && last)
-        finish<F>(ph.out, rows, l.k, ph.split, ph.splits, final_h, s);
+      for (int64_t t0 = 0; t0 < rows; t0 += l.chunk) {
+        const int64_t ts = std::min(l.chunk, rows - t0);
+        a.h = all_h;
+        a.h.p = (const char*)all_h.p + t0 * all_h.stride * 2;
+        a.h.rows = ts;
+        a.targets = {(const char*)targets + t0 * target_bytes, target_bytes, vocab};
+        a.lse = lse + t0;
+        a.row = row + t0;
+        by_shape<F>(size, [&](auto shape) {
+          typedef decltype(shape) S;
+          a.tiles_m = tiles_of(vs, S::BM);
+          a.tiles_n = tiles_of(ts, S::BN);
+          loss_gradient_kernel<F, T, S>
+              <<<mm_grid((uint64_t)a.tiles_m * a.tiles_n, S::kMost), S::kThreads, S::kLds, s>>>(a);
+        });
+        Product ph{}, pw{};
+        ph.pitch = pw.pitch = l.k;
+        by_shape<F>(l.spread.size, [&](auto shape) {
+          typedef decltype(shape) S;
+          if (dh) {
+            ph.a = {a.g, l.piece, ts, a.g_plane};
+            ph.b = a.w;
+            ph.b.rows = n;
+            ph.k = vs;
+            ph.planes_b = 1;
+            ph.rows = ts;
+            ph.out = sums_h + t0 * l.k;
+            ph.split = rows * l.k;
+            ph.add = v0 > 0;
+            ph.final = {(F*)dh + t0 * n, n, factor, nullptr, row + t0};
+            cut<S>(ph, l.spread.splits_h);
+            if (sum_h) ph.final.out = nullptr;
+          }
+          if (dtable) {
+            pw.a = {a.g, l.piece, l.piece, a.g_plane};
+            pw.b = {(const T*)(w + l.weighed) + t0 * l.k, l.k, n, rows * l.k};
+            pw.k = ts;
+            pw.planes_b = l.weighed_planes;
+            pw.rows = vs;
+            pw.out = sums_w;
+            pw.split = l.piece * l.k;
+            pw.add = t0 > 0;
+            pw.final = final_w;
+            cut<S>(pw, l.spread.splits_w);
+            if (sum_w) pw.final.out = nullptr;
+          }
+          const uint64_t tiles = (uint64_t)ph.tiles_m * ph.tiles_n * ph.splits +
+                                 (uint64_t)pw.tiles_m * pw.tiles_n * pw.splits;
+          loss_product_kernel<F, T, S>
+              <<<mm_grid(tiles, S::kMost), S::kThreads, S::kLds, s>>>(ph, pw);
+        });
+      }
+      if (dtable && sum_w)
+        finish<F>(sums_w, vs, l.k, l.piece * l.k, l.spread.splits_w, final_w, s);
     }
+    if (dh && sum_h) finish<F>(sums_h, rows, l.k, rows * l.k, l.spread.splits_h, final_h, s);
   });
   ENC_HIP_TRY(hipGetLastError());
   return SIEVE_OK;

@@ -125,3 +125,19 @@ def test_loss_of_the_largest_values(ps):  # noqa: F811
                                              torch.zeros(40, dtype=torch.int64).cuda())
     val = h[:, 0].double() * 2.0 ** -120
     check("lse", lse, val, 4 * E * val.abs())
+
+
+@pytest.mark.parametrize("rows, dtype", [((1 << 19) + 1501, "bf16"), ((1 << 19) + 1501, "f16"),
+                                         (175101, "f32"), (350001, "f32")])
+def test_loss_of_many_rows(ps, rows, dtype):  # noqa: F811
+    """More rows than g is kept of at a time."""
+    x = _inputs(rows, 50, 8, DTYPES[dtype], 24)
+    got = _run(ps, *x)
+    c = [t.cuda() for t in x]
+    val, tol = cross_entropy(*c[:3], 1.0, c[3])
+    for name in val:
+        check(name, got[name], val[name].cpu(), tol[name].cpu())
+    again = _run(ps, *x, h_grad=False)
+    assert torch.equal(got["dtable"], again["dtable"])
+    again = _run(ps, *x, table_grad=False)
+    assert torch.equal(got["dh"], again["dh"])
