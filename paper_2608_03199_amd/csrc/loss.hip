@@ -871,6 +871,8 @@ struct Layout {
   int planes;
   int weighed_planes;            // of h in dw's product
   Spread spread;
+  bool sum_h, sum_w;             // sums of splits, and dh's over the pieces, dw's over the chunks:
+                                 // else the products write the gradients themselves
   int64_t h, w, part, target, g, weighed, row, largest, dh, dw, power, bytes;
 };
 
@@ -909,8 +911,10 @@ Layout layout_of(int64_t rows, int64_t vocab, int32_t n, int32_t dtype, bool bac
     l.weighed = take(rows * l.k * 2 * l.weighed_planes);
     l.row = take(rows * (int64_t)sizeof(Row));
     l.largest = take(kMostLargest * 4);
-    l.dh = take(l.spread.splits_h * rows * l.k * 4);
-    l.dw = take(l.spread.splits_w * l.piece * l.k * 4);
+    l.sum_h = l.piece < vocab || l.spread.splits_h > 1;
+    l.sum_w = l.chunk < rows || l.spread.splits_w > 1;
+    l.dh = take(l.sum_h ? l.spread.splits_h * rows * l.k * 4 : 0);
+    l.dw = take(l.sum_w ? l.spread.splits_w * l.piece * l.k * 4 : 0);
     l.power = take(4);
   }
   l.bytes = at;
@@ -1215,9 +1219,6 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
     const Size size = size_of(std::min(l.piece, vocab), l.chunk, l.k, l.planes);
     const Final final_h{dh, n, factor, nullptr, row};
     float *sums_h = (float*)(w + l.dh), *sums_w = (float*)(w + l.dw);
-    // sums of splits, and dh's over the pieces, dw's over the chunks: else the gradient itself
-    const bool sum_h = l.piece < vocab || l.spread.splits_h > 1;
-    const bool sum_w = l.chunk < rows || l.spread.splits_w > 1;
     for (int64_t v0 = 0; v0 < vocab; v0 += l.piece) {
       const int64_t vs = std::min(l.piece, vocab - v0);
       a.w = operand<F>((const F*)table + v0 * table_stride, table_stride, vs, n, dtype, l.k,
@@ -1255,7 +1256,7 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
             ph.add = v0 > 0;
             ph.final = {(F*)dh + t0 * n, n, factor, nullptr, row + t0};
             cut<S>(ph, l.spread.splits_h);
-            if (sum_h) ph.final.out = nullptr;
+            if (l.sum_h) ph.final.out = nullptr;
           }
           if (dtable) {
             pw.a = {a.g, l.piece, l.piece, a.g_plane};
@@ -1268,7 +1269,7 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
             pw.add = t0 > 0;
             pw.final = final_w;
             cut<S>(pw, l.spread.splits_w);
-            if (sum_w) pw.final.out = nullptr;
+            if (l.sum_w) pw.final.out = nullptr;
           }
           const uint64_t tiles = (uint64_t)ph.tiles_m * ph.tiles_n * ph.splits +
                                  (uint64_t)pw.tiles_m * pw.tiles_n * pw.splits;
@@ -1276,10 +1277,10 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
               <<<mm_grid(tiles, S::kMost), S::kThreads, S::kLds, s>>>(ph, pw);
         });
       }
-      if (dtable && sum_w)
+      if (dtable && l.sum_w)
         finish<F>(sums_w, vs, l.k, l.piece * l.k, l.spread.splits_w, final_w, s);
     }
-    if (dh && sum_h) finish<F>(sums_h, rows, l.k, rows * l.k, l.spread.splits_h, final_h, s);
+    if (dh && l.sum_h) finish<F>(sums_h, rows, l.k, rows * l.k, l.spread.splits_h, final_h, s);
   });
   ENC_HIP_TRY(hipGetLastError());
   return SIEVE_OK;
