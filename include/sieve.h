@@ -587,9 +587,10 @@ SIEVE_API int64_t sieve_loss_workspace(int64_t rows, int64_t vocab, int32_t n, i
  *   x            [batch, m, n] of dtype, contiguous (may be a contiguous g).
  *   workspace    device memory of sieve_orthogonalize_workspace(batch, m, n) bytes, 16-byte
  *                aligned (only used in the call).
- * Between the steps matrices are kept to 24 bits and products summed in fp32 whatever dtype is;
- * the sum of squares is in 64 bits.  batch >= 0, 1 <= m, n <= 65536 (above these
- * SIEVE_EUNSUPPORTED).
+ * Between the steps matrices are kept to 24 bits and products summed in fp32 whatever dtype is,
+ * but for the last step of a bfloat16 result, which multiplies 11 bits of each value (off by
+ * 2^-11 where the result is rounded by 2^-8); the sum of squares is in 64 bits.  batch >= 0,
+ * 1 <= m, n <= 65536 (above these SIEVE_EUNSUPPORTED).
  */
 SIEVE_API int sieve_orthogonalize(const void* g, int64_t batch_stride, int64_t row_stride,
                                   int32_t dtype, int64_t batch, int64_t m, int64_t n,

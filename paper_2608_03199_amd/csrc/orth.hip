@@ -14,7 +14,8 @@
 // with it, so 16-bit values are not enough between the products, whatever G's type is.  Every
 // matrix is kept as two binary16 parts, hi = round(v), lo = round(v - hi): 24 bits together, and
 // a product is hi hi + hi lo + lo hi, summed in fp32.  That is fp32's precision at a third of
-// the 16-bit rate, 5 times the fp32 matrix rate.  All values are bounded by singular values, so
+// the 16-bit rate, 5 times the fp32 matrix rate.  Nothing multiplies what the last step leaves, so
+// a bfloat16 result's has the hi parts alone (kPlainSteps).  All values are bounded by singular values, so
 // fixed powers of two keep them in binary16's range (kScaleX, kScaleA): |X| below 4, |A|, |B| and
 // |C| below 16, which the host checks for the coefficients that it is given.
 //
