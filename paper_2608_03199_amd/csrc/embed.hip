@@ -335,7 +335,9 @@ __global__ __launch_bounds__(kThreads) void sort_place_kernel(Pass a) {
 // 64 it takes 124, with 16 it is 8% shorter but more kinds of pieces are launched; with 8 rows a
 // work-group 125, with 4 148, with 32 no less.
 constexpr int kRun = 32;       // places of a piece, pieces of a piece of the next kind
-constexpr int kKinds = 6;      // 32^6 places are more than kMaxCount
+constexpr int kKinds = 6;      // of 32^kind places each; 32^7 are more than kMaxCount
+constexpr int64_t places_of(int kind) { return kind ? kRun * places_of(kind - 1) : 1; }
+static_assert(places_of(kKinds) <= kMaxCount && places_of(kKinds + 1) > kMaxCount);
 constexpr int kMaxRows = 16;   // table rows of a work-group
 
 struct EmbedBwd {
