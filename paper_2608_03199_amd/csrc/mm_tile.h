@@ -71,6 +71,9 @@ __device__ __forceinline__ void mm_barrier() {
   asm volatile("" ::: "memory");
 }
 
+#pragma clang diagnostic push
+// m0 is named as written all the same: nothing may be kept in it across the loads
+#pragma clang diagnostic ignored "-Winline-asm"
 // One operand's way into LDS, R rows of m or n, kStep values of k at a time.
 template <int R, bool kAcross, int kStep, int kThreads>
 struct MmStage {
@@ -119,7 +122,7 @@ struct MmStage {
       // front of the step that reads it
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                    ::"s"(wave_to + i * kThreads * 16), "v"(o), "s"(rsrc)
-                   : "memory");
+                   : "m0", "memory");
     }
   }
 
@@ -157,6 +160,8 @@ struct MmStage {
     }
   }
 };
+
+#pragma clang diagnostic pop
 
 // One tile's share of a product.
 struct MmWork {
