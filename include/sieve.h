@@ -553,7 +553,9 @@ SIEVE_API int sieve_loss_forward(const void* h, int64_t h_stride, const void* ta
  *   dtable       NULL or [vocab, n] of dtype, contiguous.
  *   workspace    device memory of sieve_loss_workspace(rows, vocab, n, dtype, 1) bytes,
  *                16-byte aligned (only used in the call).
- * rows = 0 writes zeros to dtable (no workspace is needed).  The gradient of scale is
+ * rows = 0 writes zeros to dtable (no workspace is needed).  lse has 24 bits: p is good to about
+ * 2^-24 |lse| of itself, and a row whose |lse| is 2^30 or more may give gradients that are not
+ * numbers.  The gradient of scale is
  * sum(dh * h) / scale.
  */
 SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_stride,

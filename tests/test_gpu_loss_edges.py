@@ -100,6 +100,30 @@ def test_loss_of_logits_far_apart(ps, dtype, scale):  # noqa: F811
     check("dtable", got["dtable"], want, (UNIT[dt] + off) * size + UNIT[dt] * want.abs() + 1e-20)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("power", [17, 19, 20, 21, 22])
+def test_loss_of_logits_past_any_use(ps, dtype, power):  # noqa: F811
+    """Logits of 2^28 to 2^34: a row's gradient is right, or it is not a number."""
+    g, rnd = _rnd(25)
+    h = torch.randint(-3, 4, (80, 16), generator=g).float()
+    table = torch.randint(-3, 4, (90, 16), generator=g).float() * 64
+    dot = h @ table.t()
+    top = dot.argmax(1)
+    targets = torch.randint(90, (80,), generator=g)
+    only = ((dot == dot.max(1, keepdim=True).values).sum(1) == 1) & (targets != top)
+    dt, scale = DTYPES[dtype], 2.0 ** power
+    got = _run(ps, h.to(dt), table.to(dt), torch.where(only, targets, -100),
+               torch.full((80,), 1 / scale), scale)
+    fine = got["dh"].isfinite().all(1).cpu()
+    assert (got["dh"].cpu()[~fine].isnan().all() and fine[~only].all())
+    # what fp32 rounds off lse in base 2 is given back: an exponent of up to 2^-23 of it, which is
+    # itself good to 2^-23
+    off = UNIT[dt] + 2.0 ** -19 + 2.0 ** -46 * 1.45 * scale * float(dot.max())
+    a, b = (table[i].double() * only[:, None].double() for i in (top, targets))
+    tol = UNIT[dt] * (a - b).abs() + off * (a.abs() + b.abs()) + 1e-20
+    check("dh", got["dh"].cpu()[fine], (a - b)[fine], tol[fine])
+
+
 @pytest.mark.parametrize("v", [1 + 2.0 ** -7 - 2.0 ** -23, 2 - 2.0 ** -23, 1 + 2.0 ** -8,
                                1 + 2.0 ** -8 + 2.0 ** -16 - 2.0 ** -23, -1.7182817, 1.5])
 def test_loss_of_values_that_fill_their_bits(ps, v):  # noqa: F811
