@@ -13,28 +13,29 @@
 // 2^27 values, which the last-level cache holds for the most part: beyond 2^19 rows, a piece of the
 // rows at a time, too).  dw of the piece is then complete; dh is summed in fp32 over the pieces.
 //
-// The matrix units bound all of it: 2 rows vocab n operations for the loss, 6 for the gradients.
+// The matrix products are nearly all of it: 2 rows vocab n operations for the loss, 6 for the
+// gradients.
 //
 // 16-bit inputs are multiplied as they are.  32-bit ones come as three bf16 planes whose sum is
 // the value (8 bits each, rounded to nearest), six products of planes: what is left out is at most
-// 2^-24 of a product, and as often above as below.
-// 2,001 x 7,919 x 515, both passes: 498 us with a step's planes in LDS together, 580 with the pairs
-// of planes one after the other.
+// 2^-24 of a product, and as often above as below.  2,001 x 7,919 x 515, both passes: 526 us (518
+// to 546 in four runs).  With the pairs of planes one after the other they took 580 where a step's
+// planes in LDS together took 498.
 //
 // g is rounded once, to the inputs' type, and what its target has outweighs the rest of its row:
 // g_t,target = -(1 - p_t) dloss_t.  A rounding of it would be the same for every token of a
 // frequent word and add up over them, so each row is divided by c_t = 1 - p_t first, from a dot
-// product of its own: its target's value is then -1, and the others are at most 1 together (or less,
-// where 1 - p_t is below what rounding may leave of it: c_t is never less than that).
+// product of its own: its target's value is then -1, and the others are at most 1 together (or
+// less, where 1 - p_t is below what rounding may leave of it: c_t is never less than that).
 // dloss_t c_t is a row's exact factor of dh; in dw's product it goes with h, where its rounding is
 // another one for each value and column.  binary16 does not have fp32's range: there g is scaled
 // by 2^14, and h's factors by a power of two that brings the largest below 1.
 //
-// Measured, 8,192 rows, 32,768 vectors, 768 values, bf16: forward 426 us; two pieces of 254 for g
-// and 440 for the products (both of 412 GFLOP); 1.65 ms with everything, 1.0 PFLOP/s.  12,007 x
-// 100,003 x 1,024: 10.1 ms, 0.98 PFLOP/s.  The matrix units are busy 49% of the forward pass's
-// time, 46% of the products'; LDS has no bank conflicts.  2,048 x 2,048 x 768 f16, 73 us: seven
-// kernels after each other.
+// Measured, 8,192 rows, 32,768 vectors, 768 values, bf16: forward 420 us; two pieces of 252 for g
+// and 430 for the products (both of 412 GFLOP); 1.70 ms with everything, 0.97 PFLOP/s.  12,007 x
+// 100,003 x 1,024: 10.5 ms, 0.94 PFLOP/s.  The matrix units are busy 49% of the forward pass's
+// time, 38% of g's, 46% of the products'; LDS has no bank conflicts.  2,048 x 2,048 x 768 f16: 74
+// us, seven kernels after each other.
 #include <math.h>
 
 #include <algorithm>
@@ -418,8 +419,8 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(Rows a) {
       const float logit = dot * a.scale, lse = a.lse[row];
       // 1 - p, but no less than what rounding leaves of it, as the row's g may be as much: this sum
       // of n products, and the matrix units' in another order, are each off by up to
-      // n 2^-24 sum |h w|, which is far above |logit| where large products cancel.  g is at most 1 in
-      // any case: of a logit that is infinite, too
+      // n 2^-24 sum |h w|, which is far above |logit| where large products cancel.  g is at most 1
+      // in any case: of a logit that is infinite, too
       const float least = 0x1p-20f * (4.f + fabsf(logit) + fabsf(lse)) +
                           0x1p-23f * (float)a.n * size * a.scale;
       const float c = fmaxf(-expm1f(logit - lse), fminf(least, 1.f));
@@ -451,8 +452,8 @@ __global__ __launch_bounds__(256) void loss_power_kernel(const float* largest, i
 }
 
 // v as three 8-bit parts, largest first, each rounded to nearest: the second is at most 2^-8 of v,
-// the third 2^-17, and their sum is v.  What is not finite is the first part's alone, and what would
-// round past the largest value is cut off instead.
+// the third 2^-17, and their sum is v.  What is not finite is the first part's alone, and what
+// would round past the largest value is cut off instead.
 __device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
   const float near = (float)(bf16)v;
   const float cut = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xffff0000u);

@@ -43,8 +43,9 @@ struct Row {
 };
 
 // Up to so many rows, and of 16-bit values: each 16 vectors read the rows again, and tiles keep up
-// from some rows on.  131,072 x 1,024 f16, tables from memory: one row 54 us, in tiles 56; 16 rows
-// 68 and 56.  fp32 has no planes to pack here: 16 rows 140 us, in tiles 633.
+// from some rows on.  131,072 x 1,024 f16, tables from memory: one row 52 us, 4 rows 55, 16 rows
+// 68; in tiles 56, whatever the rows.  fp32 has no planes to pack here: one row 126 us, 16 rows
+// 137; in tiles 636 (17 to 32 rows), and no others than a matrix instruction's 16 fit here.
 constexpr int kThinRows = 16, kThinRows16 = 4, kThinMost = 1024;
 
 constexpr int kMostLargest = 1024;  // work-groups that each leave their largest factor
