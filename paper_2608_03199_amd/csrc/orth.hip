@@ -56,8 +56,9 @@ constexpr float kScaleX = 16384.f, kScaleA = 4096.f;  // of X; of A and B
 constexpr double kMaxX = 3.9, kMaxA = 15.9;           // below 65504 times these
 constexpr int kMaxSide = 65536;
 constexpr int kMaxSteps = 1000;
-// Of the last steps, for bfloat16: 36 of 768 x 768 in 1,632 us, the error 1.12 times that of rounding
-// the exact result; with none 1,838 us and 1.00 times, with two 1.4 times at 98% of the time.
+// Of the last steps, for bfloat16: 36 of 768 x 768 in 1,632 us, the error 1.12 times that of
+// rounding the exact result; with none 1,838 us and 1.00 times, with two 1.4 times at 98% of the
+// time.
 constexpr int kPlainSteps = 1;
 constexpr int kSums = 64;                             // parts of a matrix's sum of squares
 // Up to so many tiles of the usual shape leave half of the CUs idle, and are computed in four times
