@@ -566,10 +566,10 @@ SIEVE_API int sieve_loss_backward(const float* dloss, const void* h, int64_t h_s
                                   void* stream);
 /* Bytes that the forward (backward = 0) or the backward pass (1) needs, or a negative
  * sieve_status.  For any strides and alignment: copies of h and of a piece of up to 65536 vectors
- * are counted, which 16-bit values with rows at multiples of 16 bytes leave unused.  The
- * backward pass keeps g (a 16-bit value, or three for 32-bit inputs, for each of rows times vocab,
- * 2^28 bytes of them at most), h times its rows' factors, and, where
- * products are split, up to 16 fp32 sums of dh and of a piece of dtable. */
+ * are counted, which 16-bit values with rows at multiples of 16 bytes leave unused.  The backward
+ * pass keeps g (a 16-bit value, or three for 32-bit inputs, for each of rows times vocab, 2^28
+ * bytes of them at most), h times its rows' factors, and, where products are split, up to 16 fp32
+ * sums of dh and of a piece of dtable. */
 SIEVE_API int64_t sieve_loss_workspace(int64_t rows, int64_t vocab, int32_t n, int32_t dtype,
                                        int32_t backward);
 
